@@ -46,6 +46,7 @@ extern "C" {
 /* feature element types */
 #define COOP_F32 0
 #define COOP_F16 1
+#define COOP_BF16 2  /* the learning operators only (coop_embed and below); feature tables and caches hold COOP_F32 or COOP_F16 */
 
 /* coop_graph_load flags */
 #define COOP_VALIDATE 1
@@ -310,6 +311,131 @@ int coop_map_host_pointer(const void* host, void** device_out);
 /* Device pointer to the cache's slot table (vertex id per slot, -1 = empty, int32 [capacity_rows]) and the
  * number of cached vertices; valid until coop_cache_free.  For inspection and tests. */
 int coop_cache_vertices(const coop_cache* c, const int32_t** vertex_of_out, int64_t* size_out);
+
+/*
+ * Operators of learned vertex representations: what a program that trains rows for the vertices (in the place of, or on top
+ * of, given features) does with sampled blocks.  Elements are COOP_F32, COOP_F16 or COOP_BF16; arithmetic, sums and
+ * statistics are in 32 bits and are rounded once, to nearest, when a result is stored.  Pointers need the alignment of their
+ * elements only, workspaces 256 bytes; rows are dense.  All calls are asynchronous on `stream`, allocate nothing, copy
+ * nothing to or from the host, and give the same bits for the same input on every call (no sum's order depends on time), so
+ * that they can be captured into a graph.  A workspace's contents are undefined before and after; calls that overlap need
+ * one each.  Ids and targets outside their range are reported by coop_gather_status.
+ */
+
+/*
+ * Learned rows: out[i, :] = s_i table[ids[i], :] with s_i = alpha scale[i] (alpha where scale is NULL).
+ *   table  device [n_rows, dim] of dtype; out device [n_ids, dim] of out_dtype
+ *   ids    device int32 [n_ids]; the id `pad` (COOP_NO_PAD: none) stands for a place without a row: zeros.  Other ids
+ *          outside [0, n_rows) give zeros and are reported
+ *   scale  device float [n_ids], or NULL
+ */
+#define COOP_NO_PAD (-2147483647 - 1)
+int coop_embed(const void* table, int64_t n_rows, int32_t dim, int dtype, const int32_t* ids, int64_t n_ids, const float* scale,
+               float alpha, int32_t pad, void* out, int out_dtype, void* stream);
+
+/*
+ * The table's gradient: grad[v, :] = sum over the places i with ids[i] = v of s_i dout[i, :], in the order of the places in
+ * parts of up to 32 whose sums are added in their order; 0 for a row that no place has.  Places with `pad` and ids out of
+ * range (reported) are left out.
+ *   dout       device [n_ids, dim] of dtype, n_ids <= 2^30
+ *   grad       device [n_rows, dim] of grad_dtype, all of it written
+ *   workspace  at least coop_embed_grad_workspace_bytes(n_ids, dim) bytes
+ */
+size_t coop_embed_grad_workspace_bytes(int64_t n_ids, int32_t dim);
+int coop_embed_grad(const void* dout, int dtype, const int32_t* ids, int64_t n_ids, const float* scale, float alpha, int32_t pad,
+                    int64_t n_rows, int32_t dim, void* grad, int grad_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The same for a table of which few rows are touched: only these.
+ *   rows_out   device int32 [min(n_ids, n_rows)]: the ids that some place has, ascending
+ *   grad       device [min(n_ids, n_rows), dim]: row k is the gradient of table row rows_out[k]
+ *   count_out  device int32: how many there are; what is behind them in rows_out and grad is left as it was
+ */
+int coop_embed_grad_rows(const void* dout, int dtype, const int32_t* ids, int64_t n_ids, const float* scale, float alpha,
+                         int32_t pad, int64_t n_rows, int32_t dim, int32_t* rows_out, void* grad, int grad_dtype,
+                         int32_t* count_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Layer norm over the last dimension: mean and rstd = 1 / sqrt(variance + eps) of each row, y = (x - mean) rstd weight + bias.
+ *   x, out           device [n_rows, dim] of dtype (may be the same array); dim <= 32768 (COOP_F32) or 65536
+ *   weight, bias     device [dim] of weight_dtype (COOP_F32, or dtype), or NULL: 1 and 0
+ *   mean_out, rstd_out  device float [n_rows]
+ */
+int coop_layer_norm(const void* x, int64_t n_rows, int32_t dim, int dtype, const void* weight, const void* bias, int weight_dtype,
+                    float eps, void* out, float* mean_out, float* rstd_out, void* stream);
+
+/*
+ * Its gradient: with h = (x - mean) rstd and d = dy weight, dx = rstd (d - avg(d) - h avg(d h)); dweight = sum over the rows
+ * of dy h, dbias = sum over the rows of dy.
+ *   dx              device [n_rows, dim] of dtype (may be dy)
+ *   dweight, dbias  device float [dim], each may be NULL (workspace may then be NULL if both are)
+ *   workspace       at least coop_layer_norm_grad_workspace_bytes(n_rows, dim, dtype) bytes
+ */
+size_t coop_layer_norm_grad_workspace_bytes(int64_t n_rows, int32_t dim, int dtype);
+int coop_layer_norm_grad(const void* dy, const void* x, int64_t n_rows, int32_t dim, int dtype, const float* mean, const float* rstd,
+                         const void* weight, int weight_dtype, void* dx, float* dweight, float* dbias, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/*
+ * Softmax cross entropy over a vocabulary (the vertices of a graph, say) without the logits in memory: with
+ * z_iv = alpha <hidden_i, weight_v>, lse_i = log sum over v of exp z_iv and loss_i = lse_i - z_i,targets[i].
+ *   hidden   device [n, dim], weight device [vocab, dim], both of dtype; n < 2^24, dim <= 2^20
+ *   targets  device int32 [n]; a row whose target is `ignore` has loss 0 and no gradient; other targets outside [0, vocab)
+ *            likewise, and are reported
+ *   loss_out, lse_out  device float [n]
+ *   workspace  at least coop_softmax_xent_workspace_bytes(n, vocab, dim, dtype, aligned, 0) bytes, aligned = 1 if hidden and
+ *              weight are both multiples of 16, else 0.  (Operands that are not, or whose rows are no multiple of 16 bytes,
+ *              are copied into the workspace.)
+ */
+size_t coop_softmax_xent_workspace_bytes(int64_t n, int64_t vocab, int32_t dim, int dtype, int aligned, int grad);
+int coop_softmax_xent(const void* hidden, int64_t n, const void* weight, int64_t vocab, int32_t dim, int dtype, const int32_t* targets,
+                      float alpha, int32_t ignore, float* loss_out, float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its gradient, for dloss device float [n] and the forward call's lse: with
+ * G_iv = alpha dloss_i (exp(z_iv - lse_i) - [v = targets[i]]), dhidden = G weight and dweight = transposed G hidden.  The
+ * logits are computed again; G is held for a piece of the vocabulary at a time, as dtype (the products' operands have one
+ * type; in 16 bits over the largest |alpha dloss_i|).
+ *   dhidden, dweight  device, of dtype, all of it written; either may be NULL
+ *   workspace         at least coop_softmax_xent_workspace_bytes(n, vocab, dim, dtype, aligned, 1) bytes (some 256 MB for G)
+ */
+int coop_softmax_xent_grad(const void* hidden, int64_t n, const void* weight, int64_t vocab, int32_t dim, int dtype,
+                           const int32_t* targets, float alpha, int32_t ignore, const float* lse, const float* dloss, void* dhidden,
+                           void* dweight, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * An AdamW step over many tensors at once, or over the touched rows of tables: with g = grad (times *grad_scale),
+ *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
+ *   p <- p (1 - lr weight_decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps).
+ * A tensor is n_rows rows of dim elements (a tensor without rows: one row).  Where `rows` is given, its gradient has a row
+ * for each of the listed rows and no other row is read or written: n_list of them, or the first *n_list_dev.  The listed
+ * rows must differ (coop_embed_grad_rows gives them so); rows outside [0, n_rows) are skipped and reported.
+ * bits = 32: m, v are float arrays of the parameter's shape.  bits = 8: m and the root of v are 8-bit floats (4 exponent
+ * and 3 mantissa bits, OCP E4M3) of the parameter's shape, and m_scale, v_scale float arrays [n_rows, ceil(dim / 256)]: a
+ * value is the 8-bit float times the scale of its 256 neighbouring elements of a row.  They are rounded up or down at random,
+ * with the value itself as the mean, by a hash of (seed, step, place of the tensor in the list, element): the same arguments
+ * give the same bits.  All zeros are the state before step 1, either way.
+ */
+typedef struct {
+  void* param;            /* device, param_dtype */
+  const void* grad;       /* device, grad_dtype */
+  void* copy;             /* device, copy_dtype, or NULL: gets the new parameter as well */
+  void* m;
+  void* v;
+  float* m_scale;         /* bits = 8 */
+  float* v_scale;
+  const int32_t* rows;    /* device, or NULL: all rows */
+  const int32_t* n_list_dev; /* device, or NULL */
+  int64_t n_list;         /* entries of rows */
+  int64_t n_rows, dim;
+  int32_t param_dtype, grad_dtype, copy_dtype, reserved;
+} coop_adamw_tensor;
+/*   tensors     host, read before the call returns
+ *   step        1 for the first one
+ *   grad_scale  device float, or NULL
+ * A tensor or list has at most 2^35 elements. */
+int coop_adamw(const coop_adamw_tensor* tensors, int n, int bits, double lr, double beta1, double beta2, double eps, double weight_decay,
+               int64_t step, uint64_t seed, const float* grad_scale, void* stream);
 
 /* Name of an error code (static string). */
 const char* coop_strerror(int code);

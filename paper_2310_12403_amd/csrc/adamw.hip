@@ -1,0 +1,292 @@
+// AdamW over many tensors, or over the touched rows of a table, in one pass: with g the gradient (times *grad_scale),
+//   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
+//   p <- p (1 - lr wd) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps).
+//
+// Bound by HBM: parameter, gradient and moments are read once and written once.  All arithmetic is in 32 bits; every product and sum
+// is rounded on its own (the file is compiled without contraction).
+//
+// Moments in 8 bits.  m, and the root of v (half the exponents, and never negative), are kept as 8-bit floats of 4 exponent and 3
+// mantissa bits (OCP E4M3) over a 32-bit scale for each 256 neighbouring elements of a row: scale = largest magnitude / 448, so the
+// smallest number that is not lost is 2^-17.8 of the block's largest.  Neighbouring numbers lie 6 to 12 % apart: rounded to the nearest, a
+// decay of 0.1 % a step would never be seen, and v could not leave its value until g^2 were dozens of times as large.  So they are
+// rounded up or down at random with the mean at the value itself; the random number is a hash of (seed, step, tensor, element), the
+// same on every run.  A root that is not zero is never rounded to zero, or a parameter whose gradient stops would be divided by eps.
+// With y the value over its scale, the bits of the 32-bit float 2^-120 |y| are exponent and mantissa of the 8-bit one and 20 bits below
+// them, E4M3's subnormals included: adding 20 random bits and cutting them off is the rounding.
+// A moment that is not finite makes its block's scale NaN or infinite, and so all of the block's moments.
+#include <type_traits>
+
+#include "coop_internal.h"
+#include "elements.h"
+#include "variates.h"
+
+namespace coop {
+namespace {
+
+constexpr int kMomentBlock = 256;  // elements that share a scale: 4 neighbouring ones for each lane of a wave
+constexpr int kPerLane = 4;
+constexpr int kBlocksPerWave = 4;
+constexpr int kBlocksPerGroup = kWavesPerBlock * kBlocksPerWave;
+
+struct Tensor {
+  char *param, *copy, *m, *v;
+  const char* grad;
+  float *m_scale, *v_scale;
+  const int32_t *rows, *n_active;
+  int64_t n_rows, dim;
+  uint32_t row_blocks;   // blocks of 256 elements per row, the last one of what is left
+  uint32_t n_blocks;     // of all rows, or of as many rows as the list may have
+  uint32_t first_group;  // of the launch's thread blocks
+  int8_t param_type, grad_type, copy_type;
+  uint32_t key[4];
+};
+
+// A launch's tensors are its arguments (at most 4 KB): nothing is copied to the device ahead of it, and nothing is kept.
+constexpr int kTensorsPerLaunch = 28;
+struct Step {
+  float keep1, take1, keep2, take2, decay, rate, undo, eps;
+  int n;
+  int32_t* bad;
+  const float* grad_scale;
+  Tensor t[kTensorsPerLaunch];
+};
+static_assert(sizeof(Step) <= 4096, "kernel arguments");
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// Elements i .. i + 3 of an array of the type, those beyond n as zero
+__device__ __forceinline__ void load4(const char* p, int type, int64_t i, int n, float (&f)[4]) {
+  if (n >= 4) {
+    if (type == COOP_F32) Pack<COOP_F32, 4>::load(p + i * 4).get(f);
+    else if (type == COOP_F16) Pack<COOP_F16, 4>::load(p + i * 2).get(f);
+    else Pack<COOP_BF16, 4>::load(p + i * 2).get(f);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f[e] = 0.f;
+    if (e < n) f[e] = type == COOP_F32 ? ((const float*)p)[i + e] : type == COOP_F16 ? (float)((const _Float16*)p)[i + e] : (float)((const __bf16*)p)[i + e];
+  }
+}
+__device__ __forceinline__ void store4(char* p, int type, int64_t i, int n, const float (&f)[4]) {
+  if (n >= 4) {
+    if (type == COOP_F32) { Pack<COOP_F32, 4> x; x.set(f); x.store(p + i * 4); }
+    else if (type == COOP_F16) { Pack<COOP_F16, 4> x; x.set(f); x.store(p + i * 2); }
+    else { Pack<COOP_BF16, 4> x; x.set(f); x.store(p + i * 2); }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (e < n) {
+      if (type == COOP_F32) ((float*)p)[i + e] = f[e];
+      else if (type == COOP_F16) ((_Float16*)p)[i + e] = (_Float16)f[e];
+      else ((__bf16*)p)[i + e] = (__bf16)f[e];
+    }
+}
+typedef uint32_t u32_any __attribute__((aligned(1)));
+__device__ __forceinline__ uint32_t load_codes(const char* p, int n) {
+  if (n >= 4) return *reinterpret_cast<const u32_any*>(p);
+  uint32_t c = 0;
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (e < n) c |= (uint32_t)(uint8_t)p[e] << (8 * e);
+  return c;
+}
+__device__ __forceinline__ void store_codes(char* p, int n, uint32_t c) {
+  if (n >= 4) { *reinterpret_cast<u32_any*>(p) = c; return; }
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (e < n) p[e] = (char)(c >> (8 * e));
+}
+
+__device__ __forceinline__ float code_value(uint32_t code) {  // of the 8-bit float
+  const float a = __uint_as_float((code & 0x7Fu) << 20) * 0x1p120f;
+  const float x = (code & 0x7Fu) == 0x7Fu ? __uint_as_float(0x7FC00000u) : a;
+  return code & 0x80u ? -x : x;
+}
+
+// The four codes of a lane; scale: of the wave's block.  `floor`: the code of a value that is not zero is at least this.
+__device__ __forceinline__ uint32_t encode(const float (&x)[4], float scale, const uint32_t (&noise)[4], uint32_t floor) {
+  uint32_t c = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float y = x[e] / scale;
+    const uint32_t bits = __float_as_uint(fabsf(y) * 0x1p-120f);
+    uint32_t code = (bits + noise[e]) >> 20;
+    code = code < 0x7Eu ? code : 0x7Eu;
+    if (code == 0) code = floor;
+    if (x[e] == 0.f || scale == 0.f) code = 0;
+    if (x[e] < 0.f) code |= 0x80u;
+    c |= code << (8 * e);
+  }
+  return c;
+}
+// largest magnitude of the wave's values; a NaN counts as larger than any number
+__device__ __forceinline__ float wave_largest(const float (&x)[4]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t b = __float_as_uint(x[e]) & 0x7FFFFFFFu;
+    top = top > b ? top : b;
+  }
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) {
+    const uint32_t o = __shfl_xor(top, off, kWave);
+    top = top > o ? top : o;
+  }
+  return __uint_as_float(top);
+}
+
+template <int BITS>
+__global__ __launch_bounds__(kBlock) void k_adamw(Step st) {
+  // the tensor that this block belongs to: the last one that begins at or before it
+  int lo = 0, hi = st.n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (st.t[mid].first_group <= blockIdx.x) lo = mid;
+    else hi = mid;
+  }
+  const Tensor& t = st.t[lo];
+  const float gs = st.grad_scale != nullptr ? *st.grad_scale : 1.f;
+  const int32_t active = t.n_active != nullptr ? *t.n_active : 0x7FFFFFFF;
+  const int lane = lane_id();
+#pragma unroll 1
+  for (int q = 0; q < kBlocksPerWave; ++q) {
+    const uint32_t b = (blockIdx.x - t.first_group) * kBlocksPerGroup + q * kWavesPerBlock + uniform_wave_in_block();
+    if (b >= t.n_blocks) return;
+    const uint32_t entry = b / t.row_blocks, in_row = b - entry * t.row_blocks;
+    int64_t row = entry;
+    if (t.rows != nullptr) {
+      if ((int32_t)entry >= active) return;
+      row = t.rows[entry];
+      if ((uint64_t)row >= (uint64_t)t.n_rows) {
+        if (lane == 0 && in_row == 0) atomicOr(st.bad, 1);
+        continue;
+      }
+    }
+    const int64_t col = (int64_t)in_row * kMomentBlock + lane * kPerLane, left = t.dim - col;
+    const int n = left < 0 ? 0 : left < 4 ? (int)left : 4;
+    const int64_t at = row * t.dim + col, grad_at = (int64_t)entry * t.dim + col;
+    const int64_t scale_at = row * t.row_blocks + in_row;
+    float p[4], g[4], m[4], v[4], root[4];
+    load4(t.grad, t.grad_type, grad_at, n, g);
+    load4(t.param, t.param_type, at, n, p);
+    if constexpr (BITS == 32) {
+      load4(t.m, COOP_F32, at, n, m);
+      load4(t.v, COOP_F32, at, n, v);
+    } else {
+      const uint32_t mc = load_codes(t.m + at, n), vc = load_codes(t.v + at, n);
+      const float ms = t.m_scale[scale_at], vs = t.v_scale[scale_at];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        m[e] = code_value(mc >> (8 * e) & 0xFFu) * ms;
+        root[e] = code_value(vc >> (8 * e) & 0xFFu) * vs;
+        v[e] = root[e] * root[e];
+        if (e >= n) m[e] = v[e] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (st.grad_scale != nullptr) g[e] *= gs;
+      m[e] = m[e] * st.keep1 + g[e] * st.take1;
+      v[e] = v[e] * st.keep2 + (g[e] * g[e]) * st.take2;
+      root[e] = sqrtf(v[e]);
+      p[e] = p[e] * st.decay - (m[e] / (root[e] * st.undo + st.eps)) * st.rate;
+      if (e >= n) m[e] = root[e] = 0.f;
+    }
+    store4(t.param, t.param_type, at, n, p);
+    if (t.copy != nullptr) store4(t.copy, t.copy_type, at, n, p);
+    if constexpr (BITS == 32) {
+      store4(t.m, COOP_F32, at, n, m);
+      store4(t.v, COOP_F32, at, n, v);
+    } else {
+      const float ms = wave_largest(m) * (1.f / 448.f), vs = wave_largest(root) * (1.f / 448.f);
+      const uint64_t element = ((uint64_t)row * t.row_blocks + in_row) * kMomentBlock + (uint32_t)(lane * kPerLane);
+      const uint32_t high = mix32((uint32_t)(element >> 32) ^ t.key[2]) ^ t.key[1];  // (a block's elements share the high word)
+      uint32_t nm[4], nv[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t u = mix32(mix32((uint32_t)(element + e) ^ t.key[0]) ^ high) ^ t.key[3];
+        nm[e] = ((u & 0xFFFFu) << 4) + 8;  // 16 random bits each, in the middle of the 16 values they stand for
+        nv[e] = (u >> 16 << 4) + 8;
+      }
+      const uint32_t mc = encode(m, ms, nm, 0u), vc = encode(root, vs, nv, 1u);
+      store_codes(t.m + at, n, mc);
+      store_codes(t.v + at, n, vc);
+      if (lane == 0) {
+        t.m_scale[scale_at] = ms;
+        t.v_scale[scale_at] = vs;
+      }
+    }
+  }
+}
+
+}  // namespace
+}  // namespace coop
+
+using namespace coop;
+
+extern "C" int coop_adamw(const coop_adamw_tensor* tensors, int n, int bits, double lr, double beta1, double beta2, double eps,
+                          double weight_decay, int64_t step, uint64_t seed, const float* grad_scale, void* stream) {
+  if (n < 0 || (bits != 32 && bits != 8) || step < 1) return COOP_E_ARG;
+  if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0) || !(lr >= 0.0) || !(weight_decay >= 0.0)) return COOP_E_ARG;
+  if (n == 0) return COOP_OK;
+  if (!tensors) return COOP_E_NULL;
+  for (int i = 0; i < n; ++i) {  // every tensor is looked at before the first launch
+    const coop_adamw_tensor& t = tensors[i];
+    if (!known_dtype(t.param_dtype) || !known_dtype(t.grad_dtype) || (t.copy && !known_dtype(t.copy_dtype))) return COOP_E_ARG;
+    if (t.n_rows < 0 || t.dim < 0 || t.n_list < 0 || t.n_rows >= ((int64_t)1 << 31) || t.n_list >= ((int64_t)1 << 31)) return COOP_E_ARG;
+    if (t.rows == nullptr && t.n_list_dev != nullptr) return COOP_E_ARG;
+    const int64_t rows = t.rows ? t.n_list : t.n_rows;
+    if (rows == 0 || t.dim == 0) continue;
+    if (t.dim > INT64_MAX / 8 / (t.n_rows > 0 ? t.n_rows : 1)) return COOP_E_ARG;
+    const int64_t row_blocks = (t.dim - 1) / kMomentBlock + 1;
+    // (a launch has fewer than 2^32 threads, a quarter of them for all blocks of a wave)
+    if (row_blocks >= ((int64_t)1 << 27) || rows * row_blocks > ((int64_t)1 << 27)) return COOP_E_ARG;
+    if (!t.param || !t.grad || !t.m || !t.v || (bits == 8 && (!t.m_scale || !t.v_scale))) return COOP_E_NULL;
+    if (!aligned_for(t.param, t.param_dtype) || !aligned_for(t.grad, t.grad_dtype) || (t.copy && !aligned_for(t.copy, t.copy_dtype))) return COOP_E_ARG;
+    if ((bits == 32 && (((uintptr_t)t.m | (uintptr_t)t.v) & 3) != 0) || (((uintptr_t)t.m_scale | (uintptr_t)t.v_scale) & 3) != 0) return COOP_E_ARG;
+  }
+  Step st;
+  st.bad = bad_flag();
+  if (!st.bad) return COOP_E_HIP;
+  st.keep1 = (float)beta1;
+  st.take1 = (float)(1.0 - beta1);
+  st.keep2 = (float)beta2;
+  st.take2 = (float)(1.0 - beta2);
+  st.decay = (float)(1.0 - lr * weight_decay);
+  st.rate = (float)(lr / (1.0 - pow(beta1, (double)step)));
+  st.undo = (float)(1.0 / sqrt(1.0 - pow(beta2, (double)step)));
+  st.eps = (float)eps;
+  st.grad_scale = grad_scale;
+  hipStream_t s = (hipStream_t)stream;
+  uint32_t groups = 0;
+  st.n = 0;
+  const auto flush = [&] {
+    if (st.n > 0) {
+      if (bits == 32) COOP_LAUNCH(K_ADAMW, k_adamw<32>, dim3(groups), dim3(kBlock), 0, s, st);
+      else COOP_LAUNCH(K_ADAMW, k_adamw<8>, dim3(groups), dim3(kBlock), 0, s, st);
+    }
+    st.n = 0;
+    groups = 0;
+  };
+  for (int i = 0; i < n; ++i) {
+    const coop_adamw_tensor& t = tensors[i];
+    const int64_t rows = t.rows ? t.n_list : t.n_rows;
+    if (rows == 0 || t.dim == 0) continue;
+    Tensor& d = st.t[st.n];
+    d.param = (char*)t.param, d.copy = (char*)t.copy, d.m = (char*)t.m, d.v = (char*)t.v, d.grad = (const char*)t.grad;
+    d.m_scale = t.m_scale, d.v_scale = t.v_scale, d.rows = t.rows, d.n_active = t.n_list_dev;
+    d.n_rows = t.n_rows, d.dim = t.dim;
+    d.row_blocks = (uint32_t)((t.dim - 1) / kMomentBlock + 1);
+    d.n_blocks = (uint32_t)(rows * d.row_blocks);
+    d.first_group = groups;
+    d.param_type = (int8_t)t.param_dtype, d.grad_type = (int8_t)t.grad_dtype, d.copy_type = (int8_t)t.copy_dtype;
+    const uint32_t ctr[4] = {(uint32_t)step, (uint32_t)((uint64_t)step >> 32), (uint32_t)i, 0x4144414Du}, key[2] = {(uint32_t)seed, (uint32_t)(seed >> 32)};
+    philox4x32_10(ctr, key, d.key);
+    groups += (d.n_blocks + kBlocksPerGroup - 1) / kBlocksPerGroup;
+    if (++st.n == kTensorsPerLaunch || groups >= (1u << 22)) flush();
+  }
+  flush();
+  return hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
+}

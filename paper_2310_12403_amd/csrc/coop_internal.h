@@ -44,6 +44,24 @@ enum KernelId {
   K_CACHE_EVICT,
   K_CACHE_UPDATE,
   K_CACHE_GATHER,
+  K_EMBED,           // learned rows: lookup with a scale
+  K_SORT_COUNT,      // ... their gradient: digits of the ids per tile
+  K_SORT_PLACE,      // ... tokens placed in the order of a digit
+  K_EMBED_HEADS,     // ... first tokens of the rows
+  K_EMBED_SUM,       // ... sums of the rows' tokens
+  K_EMBED_JOIN,      // ... partial sums of rows with many tokens
+  K_NORM,            // layer norm
+  K_NORM_GRAD,       // ... its gradient
+  K_NORM_JOIN,       // ... the weight's, from the blocks' partial sums
+  K_ADAMW,           // AdamW step
+  K_XENT_PAD,        // cross entropy: operands into rows of a multiple of 16 bytes
+  K_XENT_STATS,      // ... logits, left as maximum and sum per row
+  K_XENT_LOSS,       // ... joined, the loss
+  K_XENT_TERMS,      // ... gradient: what a row's part of it needs
+  K_XENT_G,          // ... the logits' gradient for a piece of the vocabulary
+  K_XENT_DH,         // ... its product with the weight
+  K_XENT_DH_OUT,     // ... summed and rounded
+  K_XENT_DW,         // ... its product with the hidden states
   K_COUNT_
 };
 
@@ -179,6 +197,8 @@ struct TiledScan {
 TiledScan<uint32_t> scan_u32_tiled(const uint32_t* in, int64_t n, uint32_t* out, void* tmp, Ctl* ctl, hipStream_t s);
 
 void fill_u64(uint64_t* p, int64_t n, uint64_t v, hipStream_t s);
+// zeros; p and bytes are even
+void clear_bytes(void* p, int64_t bytes, hipStream_t s);
 
 // The current device's sticky "an id was out of range" word (device memory; read and cleared by coop_gather_status).
 int32_t* bad_flag();

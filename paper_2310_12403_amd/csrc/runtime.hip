@@ -25,7 +25,9 @@ struct Prof {
 const char* const kKernelNames[K_COUNT_] = {
     "fill", "labor_scan", "labor_fill", "labor_fill_overflow", "labor_exact", "segments", "enum_list", "enum_walk", "ns_count", "ns_fill", "ns_select", "rw_walk", "rw_fill", "scan_local", "scan_offset",
     "unique_insert", "unique_flag", "unique_filter", "unique_collect", "unique_relabel", "unique_part_count", "unique_part_scatter", "unique_part_first", "copy_ids", "gather", "gather_mean", "owner_count", "owner_scatter", "validate_csr",
-    "cache_lookup", "cache_select", "cache_evict", "cache_miss_rows", "cache_hit_rows"};
+    "cache_lookup", "cache_select", "cache_evict", "cache_miss_rows", "cache_hit_rows",
+    "embed", "sort_count", "sort_place", "embed_heads", "embed_sum", "embed_join", "layer_norm", "layer_norm_grad", "layer_norm_join", "adamw",
+    "xent_pad", "xent_stats", "xent_loss", "xent_terms", "xent_g", "xent_dh", "xent_dh_out", "xent_dw"};
 
 hipEvent_t take_event() {
   if (!g_prof.pool.empty()) { hipEvent_t e = g_prof.pool.back(); g_prof.pool.pop_back(); return e; }
@@ -90,6 +92,18 @@ void fill_u64(uint64_t* p, int64_t n, uint64_t v, hipStream_t s) {
   if (blocks > 256 * 64) blocks = 256 * 64;
   if (blocks < 1) blocks = 1;
   COOP_LAUNCH(K_FILL, k_fill_u64, dim3((unsigned)blocks), dim3(kBlock), 0, s, p, n, v);
+}
+
+// (what is in front of the first whole 8-byte word and behind the last one)
+__global__ void k_clear_tail(uint16_t* p, int n) { if ((int)threadIdx.x < n) p[threadIdx.x] = 0; }
+
+void clear_bytes(void* p, int64_t bytes, hipStream_t s) {
+  // (tensors are 2-byte aligned at least; the head up to a multiple of 8 and the tail by 2-byte stores)
+  const int64_t head = (int64_t)((8 - ((uintptr_t)p & 7)) & 7) < bytes ? (int64_t)((8 - ((uintptr_t)p & 7)) & 7) : bytes;
+  const int64_t words = (bytes - head) / 8, tail = bytes - head - 8 * words;
+  if (head) COOP_LAUNCH(K_FILL, k_clear_tail, dim3(1), dim3(64), 0, s, (uint16_t*)p, (int)(head / 2));
+  fill_u64((uint64_t*)((char*)p + head), words, 0, s);
+  if (tail) COOP_LAUNCH(K_FILL, k_clear_tail, dim3(1), dim3(64), 0, s, (uint16_t*)((char*)p + head + 8 * words), (int)(tail / 2));
 }
 
 // ---- device-wide exclusive scan -------------------------------------------------------------------------------

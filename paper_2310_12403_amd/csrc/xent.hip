@@ -1,0 +1,672 @@
+// Softmax cross entropy over a large vocabulary without the logits kept, and its gradient.
+//
+// With z = alpha H W^T (H [n, dim] hidden states, W [vocab, dim]), t the rows' targets:
+//   lse_i = log sum_v exp z_iv,   loss_i = lse_i - z_i,t(i),
+//   G_iv = alpha dloss_i (exp(z_iv - lse_i) - [v = t(i)]),   dH = G W,   dW = G^T H.
+// Forward: one product, whose tiles stay in registers and leave as a running maximum and sum per row.  Backward: the logits again, a
+// piece of the vocabulary at a time, left as G of that piece in 16 bits (32 for fp32), and the two products with it.
+//
+// The products run on the matrix units from tiles in LDS.  All three are the same kernel: C = A B^T over a common dimension k, where an
+// operand either has k as its contiguous dimension (rows of 128 bytes of k per stage) or as its row number (then its fragments are
+// transposed on the way from LDS to the registers).  The columns of C lie on the lanes and its rows in a lane's registers, so C is
+// computed as vocabulary x hidden for the logits: a lane then holds many logits of one row of H, and neither maximum, sum nor target
+// takes another lane until the end.
+#include <type_traits>
+
+#include "coop_internal.h"
+#include "elements.h"
+
+namespace coop {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char LdsByte;
+
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+constexpr int kStageBytes = 128;  // of k per row and stage: 64 elements of 16 bits, 32 of 32
+constexpr float kNoMax = -3.402823466e38f;
+
+template <int T> constexpr int kElem = T == COOP_F32 ? 4 : 2;
+template <int T> constexpr int kStageK = kStageBytes / kElem<T>;
+
+// One 16-byte fragment of each operand into a 32 x 32 tile of C: 16 of k in 16 bits, 8 in 32.
+template <int T>
+__device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
+  if constexpr (T == COOP_F16) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  } else if constexpr (T == COOP_BF16) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
+    return c;
+  }
+}
+
+// An operand in memory: rows of `ld` bytes (a multiple of 16, as is the base).  k contiguous: `rows` rows, `k` bytes of each are there.
+// k strided: `k` rows (one for each k), `rows` bytes of each are there.
+struct Operand {
+  const char* base;
+  int64_t ld, rows, k;
+};
+
+// How a stage of R rows of an operand lies in LDS, in 16-byte slots filled in order by the loads, 64 to a wave's load.
+//   k contiguous: a row's 8 chunks, exchanged by the row's number so that 8 neighbouring rows' same chunk lie in different banks;
+//   k strided: a row of k holds R elements; its chunks are exchanged by k so that what one fragment reads lies in different banks.
+template <int T, int R, bool STRIDED, int WAVES>
+struct Staged {
+  static constexpr int kBytes = R * kStageBytes;
+  static constexpr int kChunks = STRIDED ? R * kElem<T> / 16 : kStageBytes / 16;  // of a row
+  static constexpr int kLoads = kBytes / 1024;                                    // of a wave each
+  static_assert(kLoads % WAVES == 0 || kLoads < WAVES, "loads are dealt to the waves evenly");
+  static __device__ __forceinline__ int swizzle(int row) {
+    if constexpr (!STRIDED) return row & 7;
+    else if constexpr (T == COOP_F32) return (row >> 2 & 1) << 3;
+    else return (((row & 3) | (row >> 3 & 1) << 2) << 2) & (kChunks - 1);
+  }
+  // starts the loads of the stage whose first k is k0; row0: the tile's first row
+  static __device__ __forceinline__ void load(const Operand& op, int64_t row0, int64_t k0, char* lds) {
+    const char* base;
+    int64_t there;  // rows of the memory layout that exist from the base on
+    if constexpr (STRIDED) {
+      base = op.base + k0 * op.ld + row0 * kElem<T>;
+      there = op.k - k0;
+      if (there > kStageK<T>) there = kStageK<T>;
+    } else {
+      base = op.base + row0 * op.ld + k0 * kElem<T>;
+      there = op.rows - row0;
+      if (there > R) there = R;
+    }
+    if (there < 0) there = 0;
+    // (what lies behind the last row, and chunks beyond a row's end, read as zero)
+    const int64_t in_row = STRIDED ? op.rows - row0 * kElem<T> : op.k - k0 * kElem<T>;
+    const int records = there > 0 ? (int)((there - 1) * op.ld + (in_row < op.ld ? in_row : op.ld)) : 0;
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, records, 0x00020000);
+    const int wave = uniform_wave_in_block(), lane = lane_id();
+#pragma unroll
+    for (int i = 0; i < (kLoads + WAVES - 1) / WAVES; ++i) {
+      const int l = i * WAVES + wave;
+      if (kLoads % WAVES != 0 && l >= kLoads) break;
+      const int slot = l * kWave + lane, row = slot / kChunks, chunk = (slot % kChunks) ^ swizzle(row);
+      const int at = chunk * 16 < in_row ? row * (int)op.ld + chunk * 16 : 0x7FFFFF00;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(LdsByte*)(lds + l * 1024), 16, at, 0, 0, 0);
+    }
+  }
+  // the fragment of rows row .. row + 31 at step kk of the stage
+  static __device__ __forceinline__ u32x4 fragment(const char* lds, int row, int kk) {
+    const int lane = lane_id();
+    if constexpr (!STRIDED) {
+      const int r = row + (lane & 31), chunk = kk * 2 + (lane >> 5);
+      return *reinterpret_cast<const u32x4*>(lds + r * kStageBytes + ((chunk ^ swizzle(r)) << 4));
+    } else if constexpr (T == COOP_F32) {
+      const int m = row + (lane & 31);
+      u32x4 f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k = kk * 8 + (lane >> 5) * 4 + j;
+        f[j] = *reinterpret_cast<const uint32_t*>(lds + k * (R * 4) + (((m >> 2) ^ swizzle(k)) << 4) + (m & 3) * 4);
+      }
+      return f;
+    } else {
+      // 16 lanes read 4 rows of k by 16 elements and get an element's 4 k each
+      const int b = lane >> 4, t = lane & 15;
+      u32x4 f;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int k = kk * 16 + (b >> 1) * 8 + q * 4 + (t >> 2), m = row + (b & 1) * 16 + (t & 3) * 4;
+        const char* at = lds + k * (R * 2) + (((m >> 3) ^ swizzle(k)) << 4) + (m & 7) * 2;
+        const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(LdsByte*)at);
+        const u32x2 y = __builtin_bit_cast(u32x2, x);
+        f[2 * q] = y[0];
+        f[2 * q + 1] = y[1];
+      }
+      return f;
+    }
+  }
+};
+
+// The loads into LDS that this wave has started have arrived, and then the waves meet.  (A barrier alone does not wait for them.)
+__device__ __forceinline__ void arrive_and_meet() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
+
+// A block's tile of C: WA x WB waves with TA x TB tiles of 32 x 32 each, rows of A by rows of B.
+template <int T, int WA, int WB, int TA, int TB, bool SA, bool SB>
+struct Product {
+  static constexpr int kWaves = WA * WB, kThreads = kWaves * kWave;
+  static constexpr int kRowsA = WA * TA * 32, kRowsB = WB * TB * 32;
+  typedef Staged<T, kRowsA, SA, kWaves> A;
+  typedef Staged<T, kRowsB, SB, kWaves> B;
+  static constexpr int kLds = 2 * (A::kBytes + B::kBytes);
+  f32x16 acc[TA][TB];
+
+  __device__ __forceinline__ static int a0() { return uniform_wave_in_block() / WB * (TA * 32); }
+  __device__ __forceinline__ static int b0() { return uniform_wave_in_block() % WB * (TB * 32); }
+  // C's element j of a 32 x 32 tile: its row; its column is lane & 31
+  __device__ __forceinline__ static int row_of(int j) { return (j >> 2) * 8 + (lane_id() >> 5) * 4 + (j & 3); }
+
+  // `lds` is free for use, as far as this block's waves have met since they last read it; the waves meet once more at the end
+  __device__ __forceinline__ void run(const Operand& a, const Operand& b, int64_t row_a, int64_t row_b, int64_t k0, int64_t k1, char* lds) {
+#pragma unroll
+    for (int i = 0; i < TA; ++i)
+#pragma unroll
+      for (int j = 0; j < TB; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    char* la[2] = {lds, lds + A::kBytes};
+    char* lb[2] = {lds + 2 * A::kBytes, lds + 2 * A::kBytes + B::kBytes};
+    A::load(a, row_a, k0, la[0]);
+    B::load(b, row_b, k0, lb[0]);
+    arrive_and_meet();
+    int at = 0;
+    for (int64_t k = k0; k < k1; k += kStageK<T>) {
+      if (k + kStageK<T> < k1) {
+        A::load(a, row_a, k + kStageK<T>, la[at ^ 1]);
+        B::load(b, row_b, k + kStageK<T>, lb[at ^ 1]);
+      }
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        u32x4 fa[TA], fb[TB];
+#pragma unroll
+        for (int i = 0; i < TA; ++i) fa[i] = A::fragment(la[at], a0() + i * 32, kk);
+#pragma unroll
+        for (int j = 0; j < TB; ++j) fb[j] = B::fragment(lb[at], b0() + j * 32, kk);
+#pragma unroll
+        for (int i = 0; i < TA; ++i)
+#pragma unroll
+          for (int j = 0; j < TB; ++j) acc[i][j] = mma<T>(fa[i], fb[j], acc[i][j]);
+      }
+      arrive_and_meet();
+      at ^= 1;
+    }
+  }
+};
+
+// ---- forward -------------------------------------------------------------------------------------------------------------
+// A block has kRowsB rows of H and every `splits`-th tile of the vocabulary; it leaves the rows' maximum, sum and target logit (all
+// base 2: times log2 e) as part[split][row].
+struct RowStat { float top, sum, target, pad; };
+
+template <int T, int WA, int WB, int TA, int TB>
+__global__ __launch_bounds__(WA* WB* kWave) void k_xent_stats(Operand w, Operand h, int64_t n, int64_t vocab, int64_t k, float scale2,
+                                                               const int32_t* __restrict__ targets, int splits, RowStat* __restrict__ part) {
+  typedef Product<T, WA, WB, TA, TB, false, false> P;
+  extern __shared__ char lds[];
+  const int split = blockIdx.x % splits;
+  const int64_t row0 = (int64_t)(blockIdx.x / splits) * P::kRowsB;
+  P p;
+  float top[TB], sum[TB], target[TB];
+  int32_t t[TB];
+#pragma unroll
+  for (int j = 0; j < TB; ++j) {
+    const int64_t i = row0 + P::b0() + j * 32 + (lane_id() & 31);
+    t[j] = i < n ? targets[i] : -1;
+    top[j] = kNoMax;
+    sum[j] = target[j] = 0.f;
+  }
+  for (int64_t v0 = (int64_t)split * P::kRowsA; v0 < vocab; v0 += (int64_t)splits * P::kRowsA) {
+    p.run(w, h, v0, row0, 0, k, lds);
+    const int64_t first = v0 + P::a0();
+    const bool ragged = first + TA * 32 > vocab;
+#pragma unroll
+    for (int j = 0; j < TB; ++j) {
+#pragma unroll
+      for (int i = 0; i < TA; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) p.acc[i][j][e] *= scale2;
+      const int64_t mine = (int64_t)t[j] - first;
+      if (ballot64(mine >= 0 && mine < TA * 32) != 0) {
+#pragma unroll
+        for (int i = 0; i < TA; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (mine == i * 32 + P::row_of(e)) target[j] = p.acc[i][j][e];
+      }
+      if (ragged) {
+#pragma unroll
+        for (int i = 0; i < TA; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (first + i * 32 + P::row_of(e) >= vocab) p.acc[i][j][e] = -__builtin_inff();
+      }
+      float m = top[j];
+#pragma unroll
+      for (int i = 0; i < TA; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) m = fmaxf(m, p.acc[i][j][e]);
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < TA; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f(p.acc[i][j][e] - m);
+      sum[j] = sum[j] * __builtin_amdgcn_exp2f(top[j] - m) + s;
+      top[j] = m;
+    }
+  }
+  // lanes l and l + 32 have the same rows, and so have the waves of a column of waves
+  RowStat* stat = reinterpret_cast<RowStat*>(lds);
+#pragma unroll
+  for (int j = 0; j < TB; ++j) {
+    const float m = fmaxf(top[j], __shfl_xor(top[j], 32, kWave));
+    float s = sum[j] * __builtin_amdgcn_exp2f(top[j] - m);
+    s += __shfl_xor(s, 32, kWave);
+    const float tt = target[j] + __shfl_xor(target[j], 32, kWave);
+    if (lane_id() < 32) stat[uniform_wave_in_block() / WB * P::kRowsB + P::b0() + j * 32 + lane_id()] = RowStat{m, s, tt, 0.f};
+  }
+  __syncthreads();
+  for (int r = threadIdx.x; r < P::kRowsB; r += P::kThreads) {
+    if (row0 + r >= n) break;
+    RowStat all = stat[r];
+#pragma unroll
+    for (int a = 1; a < WA; ++a) {
+      const RowStat x = stat[a * P::kRowsB + r];
+      const float m = fmaxf(all.top, x.top);
+      all.sum = all.sum * __builtin_amdgcn_exp2f(all.top - m) + x.sum * __builtin_amdgcn_exp2f(x.top - m);
+      all.top = m;
+      all.target += x.target;
+    }
+    part[(int64_t)split * n + row0 + r] = all;
+  }
+}
+
+__global__ __launch_bounds__(kBlock) void k_xent_loss(const RowStat* __restrict__ part, int splits, int64_t n, int64_t vocab,
+                                                      const int32_t* __restrict__ targets, int32_t ignore, float* __restrict__ loss,
+                                                      float* __restrict__ lse, int32_t* __restrict__ bad) {
+  const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+  if (i >= n) return;
+  float m = kNoMax;
+  for (int s = 0; s < splits; ++s) m = fmaxf(m, part[s * n + i].top);
+  float sum = 0.f, target = 0.f;
+  for (int s = 0; s < splits; ++s) {
+    const RowStat x = part[s * n + i];
+    sum += x.sum * __builtin_amdgcn_exp2f(x.top - m);
+    target += x.target;
+  }
+  const int32_t t = targets[i];
+  const bool ok = t != ignore && (uint64_t)(int64_t)t < (uint64_t)vocab;
+  if (!ok && t != ignore) atomicOr(bad, 1);
+  const float l = log2f(sum);
+  lse[i] = (m + l) * kLn2;
+  loss[i] = ok ? ((m - target) + l) * kLn2 : 0.f;
+}
+
+// ---- backward ------------------------------------------------------------------------------------------------------------
+// What a row of G needs; target -1: the row has none, and G is zero there whatever its logits are.
+struct RowTerm { float coef, lse2; int32_t target; int32_t pad; };
+
+// In 16 bits G holds coef over the largest |coef| (and times 2^13 in fp16, whose exponents would otherwise not reach from 1 to a
+// probability times dloss): where all rows count alike, as in a mean, the factor is 1 (a power of two), and so a target's p - 1 of a
+// small p is not rounded away from -1 twice; with dloss itself in G, dH and dW of the mean were off by 3.0e-3 instead of 2.0e-3 (bf16).
+template <bool LIFT>
+__global__ __launch_bounds__(1024) void k_xent_terms(const int32_t* __restrict__ targets, int32_t ignore, const float* __restrict__ lse,
+                                                     const float* __restrict__ dloss, float alpha, float most, int64_t n, int64_t rows, int64_t vocab,
+                                                     RowTerm* __restrict__ term, float* __restrict__ unlift, int32_t* __restrict__ bad) {
+  __shared__ float lds[16];
+  float top = 0.f;
+  if constexpr (LIFT) {  // (every block looks at all rows: no second launch, and n floats are little)
+    for (int64_t i = threadIdx.x; i < n; i += 1024) {
+      const int32_t t = targets[i];
+      const float c = fabsf(alpha * dloss[i]);
+      if (t != ignore && (uint64_t)(int64_t)t < (uint64_t)vocab && c < __builtin_inff()) top = fmaxf(top, c);
+    }
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
+    if (lane_id() == 0) lds[wave_in_block()] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 16; ++w) top = fmaxf(top, lds[w]);
+    if (top < 0x1p-100f) top = 0x1p-100f;
+    if (top > 0x1p100f) top = 0x1p100f;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *unlift = LIFT ? top / most : 1.f;
+  const int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x;
+  if (i >= rows) return;
+  RowTerm r{0.f, 0.f, -1, 0};
+  if (i < n) {
+    const int32_t t = targets[i];
+    const bool ok = t != ignore && (uint64_t)(int64_t)t < (uint64_t)vocab;
+    if (ok) r = RowTerm{LIFT ? alpha * dloss[i] / top * most : alpha * dloss[i], lse[i] * kLog2e, t, 0};
+    else if (t != ignore) atomicOr(bad, 1);
+  }
+  term[i] = r;
+}
+
+template <int T>
+__device__ __forceinline__ void put4(char* p, const float (&f)[4]) {
+  Pack<T, 4> x;
+  x.set(f);
+  x.store(p);
+}
+
+// G of the piece of the vocabulary that begins at v_first, [rows of H, ld bytes]; all of G's tiles are there, beyond the vocabulary's
+// and the rows' end it is zero
+template <int T, int WA, int WB, int TA, int TB>
+__global__ __launch_bounds__(WA* WB* kWave) void k_xent_g(Operand w, Operand h, int64_t vocab, int64_t k, float scale2, int64_t v_first,
+                                                           uint32_t tiles_a, const RowTerm* __restrict__ term, char* __restrict__ g, int64_t ld) {
+  typedef Product<T, WA, WB, TA, TB, false, false> P;
+  extern __shared__ char lds[];
+  const int64_t piece0 = (int64_t)(blockIdx.x % tiles_a) * P::kRowsA, row0 = (int64_t)(blockIdx.x / tiles_a) * P::kRowsB;
+  P p;
+  p.run(w, h, v_first + piece0, row0, 0, k, lds);
+  const int64_t first = v_first + piece0 + P::a0();
+  const bool ragged = first + TA * 32 > vocab;
+#pragma unroll
+  for (int j = 0; j < TB; ++j) {
+    const int64_t i = row0 + P::b0() + j * 32 + (lane_id() & 31);
+    const RowTerm r = term[i];
+    const int64_t mine = r.target - first;
+    const bool hit = ballot64(r.target >= 0 && mine >= 0 && mine < TA * 32) != 0;
+#pragma unroll
+    for (int a = 0; a < TA; ++a) {
+      f32x16 x = p.acc[a][j];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale2, -r.lse2));
+      if (hit) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (mine == a * 32 + P::row_of(e)) x[e] -= 1.f;
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = r.target < 0 ? 0.f : x[e] * r.coef;
+      if (ragged) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (first + a * 32 + P::row_of(e) >= vocab) x[e] = 0.f;
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float f[4] = {x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+        put4<T>(g + i * ld + (piece0 + P::a0() + a * 32 + P::row_of(4 * q)) * kElem<T>, f);
+      }
+    }
+  }
+}
+
+// dH: sums[split][row][dim] (+)= the split's part of G W over the piece
+template <int T, int WA, int WB, int TA, int TB>
+__global__ __launch_bounds__(WA* WB* kWave) void k_xent_dh(Operand wt, Operand g, int64_t k, int splits, uint32_t tiles_a, uint32_t tiles_b,
+                                                            bool add, float* __restrict__ sums, int64_t width) {
+  typedef Product<T, WA, WB, TA, TB, true, false> P;
+  extern __shared__ char lds[];
+  const uint32_t tile = blockIdx.x / splits, split = blockIdx.x % splits;
+  const int64_t col0 = (int64_t)(tile % tiles_a) * P::kRowsA, row0 = (int64_t)(tile / tiles_a) * P::kRowsB;
+  const int64_t stages = (k + kStageK<T> - 1) / kStageK<T>;
+  const int64_t k0 = stages * split / splits * kStageK<T>, k1 = stages * (split + 1) / splits * kStageK<T>;
+  P p;
+  p.run(wt, g, col0, row0, k0, k1, lds);
+  float* to = sums + (int64_t)split * tiles_b * P::kRowsB * width;
+#pragma unroll
+  for (int j = 0; j < TB; ++j)
+#pragma unroll
+    for (int a = 0; a < TA; ++a)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int64_t c = col0 + P::a0() + a * 32 + P::row_of(4 * q);
+        if (c >= width) continue;
+        float* at = to + (row0 + P::b0() + j * 32 + (lane_id() & 31)) * width + c;
+        f32x16& x = p.acc[a][j];
+        u32x4 old = add ? *reinterpret_cast<const u32x4*>(at) : u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) old[e] = __float_as_uint(__uint_as_float(old[e]) + x[4 * q + e]);
+        *reinterpret_cast<u32x4*>(at) = old;
+      }
+}
+
+template <int T>
+__global__ __launch_bounds__(kBlock) void k_xent_dh_out(const float* __restrict__ sums, int splits, int64_t rows, int64_t width, int64_t n,
+                                                        int32_t dim, const float* __restrict__ unlift, char* __restrict__ out) {
+  const int64_t step = (int64_t)gridDim.x * kBlock;
+  for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < n * dim; i += step) {
+    const int64_t row = i / dim;
+    const int32_t c = (int32_t)(i - row * dim);
+    float s = 0.f;
+    for (int q = 0; q < splits; ++q) s += sums[((int64_t)q * rows + row) * width + c];
+    ((typename Element<T>::M*)out)[i] = (typename Element<T>::M)(s * *unlift);
+  }
+}
+
+// dW of the piece: rows v_first .. of the weight's gradient
+template <int T, int WA, int WB, int TA, int TB>
+__global__ __launch_bounds__(WA* WB* kWave) void k_xent_dw(Operand ht, Operand gt, int64_t k, int64_t vocab, int64_t v_first, int32_t dim,
+                                                            uint32_t tiles_a, const float* __restrict__ unlift, char* __restrict__ out) {
+  typedef Product<T, WA, WB, TA, TB, true, true> P;
+  extern __shared__ char lds[];
+  const int64_t col0 = (int64_t)(blockIdx.x % tiles_a) * P::kRowsA, piece0 = (int64_t)(blockIdx.x / tiles_a) * P::kRowsB;
+  P p;
+  p.run(ht, gt, col0, piece0, 0, k, lds);
+  const float u = *unlift;
+#pragma unroll
+  for (int j = 0; j < TB; ++j) {
+    const int64_t v = v_first + piece0 + P::b0() + j * 32 + (lane_id() & 31);
+    if (v >= vocab) continue;
+#pragma unroll
+    for (int a = 0; a < TA; ++a)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int64_t c = col0 + P::a0() + a * 32 + P::row_of(4 * q);
+        float f[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = p.acc[a][j][4 * q + e] * u;
+        if (c + 4 <= dim) {
+          put4<T>(out + (v * dim + c) * kElem<T>, f);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (c + e < dim) ((typename Element<T>::M*)out)[v * dim + c + e] = (typename Element<T>::M)f[e];
+        }
+      }
+  }
+}
+
+// rows of `dim` elements into rows of `ld` bytes, what is behind a row's end zero
+template <int T>
+__global__ __launch_bounds__(kBlock) void k_xent_pad(const char* __restrict__ in, int64_t rows, int32_t dim, char* __restrict__ out, int32_t width) {
+  const int64_t step = (int64_t)gridDim.x * kBlock;
+  for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < rows * width; i += step) {
+    const int64_t row = i / width;
+    const int32_t c = (int32_t)(i - row * width);
+    typedef typename Element<T>::M M;
+    ((M*)out)[i] = c < dim ? ((const M*)in)[row * dim + c] : (M)0.f;
+  }
+}
+
+// ---- the workspace ---------------------------------------------------------------------------------------------------------
+constexpr int64_t kPieceBytes = (int64_t)256 << 20;  // of G
+constexpr int kTile = 256;                            // rows of a block's tile, either way
+
+int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+struct XentPlan {
+  int64_t n, vocab, width, ld;  // width: elements of a padded row
+  int64_t rows, piece, pieces;
+  int splits, dh_splits;
+  bool few, pad;
+  size_t h, w, part, term, unlift, g, sums, bytes;
+  XentPlan(int64_t n_, int64_t vocab_, int32_t dim, int dtype, bool aligned, bool grad) : n(n_), vocab(vocab_) {
+    const int es = element_bytes(dtype);
+    width = round_up(dim, 16 / es);
+    ld = width * es;
+    pad = !aligned || width != dim;
+    few = n <= 32;
+    rows = round_up(n, kTile);
+    const int64_t row_tiles = few ? 1 : rows / kTile, vocab_tiles = (vocab + kTile - 1) / kTile;
+    int64_t s = (few ? 1024 : 256) / row_tiles;
+    s = s < 1 ? 1 : s;
+    splits = (int)(s < vocab_tiles ? s : vocab_tiles);
+    piece = kPieceBytes / (rows * es) / kTile * kTile;
+    if (piece < kTile) piece = kTile;
+    if (piece > vocab_tiles * kTile) piece = vocab_tiles * kTile;
+    pieces = (vocab + piece - 1) / piece;
+    const int64_t dh_tiles = rows / kTile * ((width + kTile - 1) / kTile);
+    int64_t ds = 256 / dh_tiles;
+    const int64_t stages = piece * es / kStageBytes;
+    ds = ds < 1 ? 1 : ds > 16 ? 16 : ds;
+    dh_splits = (int)(ds < stages ? ds : stages);
+    size_t at = 0;
+    auto take = [&](size_t b) { const size_t o = at; at += (b + 255) & ~(size_t)255; return o; };
+    h = take(pad ? (size_t)n * ld : 0);
+    w = take(pad ? (size_t)vocab * ld : 0);
+    part = take(grad ? 0 : (size_t)splits * n * sizeof(RowStat));
+    term = take(grad ? (size_t)rows * sizeof(RowTerm) : 0);
+    unlift = take(grad ? sizeof(float) : 0);
+    g = take(grad ? (size_t)rows * piece * es : 0);
+    sums = take(grad ? (size_t)dh_splits * rows * width * sizeof(float) : 0);
+    bytes = at + 256;
+  }
+};
+
+template <int T>
+void pad_rows(const void* in, int64_t rows, int32_t dim, const XentPlan& p, void* out, hipStream_t s) {
+  const int64_t blocks = (rows * p.width + kBlock - 1) / kBlock;
+  COOP_LAUNCH(K_XENT_PAD, k_xent_pad<T>, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(kBlock), 0, s, (const char*)in, rows, dim, (char*)out,
+              (int32_t)p.width);
+}
+
+// (blocks of more than 64 KB of LDS have to be allowed, once for each kernel and device; it costs a fraction of a microsecond)
+template <typename K>
+bool allow_lds(K kernel, int bytes) {
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess;
+}
+
+bool xent_aligned(const void* hidden, const void* weight) { return (((uintptr_t)hidden | (uintptr_t)weight) & 15) == 0; }
+
+int xent_check(const void* hidden, int64_t n, const void* weight, int64_t vocab, int32_t dim, int dtype, const int32_t* targets) {
+  if (!known_dtype(dtype)) return COOP_E_ARG;
+  if (n < 0 || n >= ((int64_t)1 << 24) || vocab < 1 || vocab >= ((int64_t)1 << 31) || dim < 1 || dim > (1 << 20)) return COOP_E_ARG;
+  if (n > 0 && (!hidden || !weight || !targets)) return COOP_E_NULL;
+  if (!aligned_for(hidden, dtype) || !aligned_for(weight, dtype)) return COOP_E_ARG;
+  return COOP_OK;
+}
+
+template <int T, int WA, int WB, int TA, int TB>
+bool launch_stats(const XentPlan& p, Operand w, Operand h, float alpha, const int32_t* targets, RowStat* part, hipStream_t s) {
+  typedef Product<T, WA, WB, TA, TB, false, false> P;
+  constexpr int lds = P::kLds > WA * P::kRowsB * (int)sizeof(RowStat) ? P::kLds : WA * P::kRowsB * (int)sizeof(RowStat);
+  const auto kernel = k_xent_stats<T, WA, WB, TA, TB>;
+  if (!allow_lds(kernel, lds)) return false;
+  const int64_t row_tiles = (p.n + P::kRowsB - 1) / P::kRowsB;
+  COOP_LAUNCH(K_XENT_STATS, kernel, dim3((unsigned)(row_tiles * p.splits)), dim3(P::kThreads), lds, s, w, h, p.n, p.vocab, p.width, alpha * kLog2e,
+              targets, p.splits, part);
+  return true;
+}
+
+template <int T>
+int forward(const XentPlan& p, const void* hidden, const void* weight, int32_t dim, const int32_t* targets, float alpha, int32_t ignore,
+            float* loss, float* lse, char* ws, int32_t* bad, hipStream_t s) {
+  if (p.pad) {
+    pad_rows<T>(hidden, p.n, dim, p, ws + p.h, s);
+    pad_rows<T>(weight, p.vocab, dim, p, ws + p.w, s);
+    hidden = ws + p.h;
+    weight = ws + p.w;
+  }
+  const Operand w{(const char*)weight, p.ld, p.vocab, p.ld}, h{(const char*)hidden, p.ld, p.n, p.ld};
+  RowStat* part = (RowStat*)(ws + p.part);
+  const bool ok = p.few ? launch_stats<T, 8, 1, 1, 1>(p, w, h, alpha, targets, part, s) : launch_stats<T, 2, 4, 4, 2>(p, w, h, alpha, targets, part, s);
+  if (!ok) return COOP_E_HIP;
+  COOP_LAUNCH(K_XENT_LOSS, k_xent_loss, dim3((unsigned)((p.n + kBlock - 1) / kBlock)), dim3(kBlock), 0, s, (const RowStat*)part, p.splits, p.n,
+              p.vocab, targets, ignore, loss, lse, bad);
+  return hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
+}
+
+template <int T>
+int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t dim, const int32_t* targets, float alpha, int32_t ignore,
+             const float* lse, const float* dloss, void* dhidden, void* dweight, char* ws, int32_t* bad, hipStream_t s) {
+  if (p.pad) {
+    pad_rows<T>(hidden, p.n, dim, p, ws + p.h, s);
+    pad_rows<T>(weight, p.vocab, dim, p, ws + p.w, s);
+    hidden = ws + p.h;
+    weight = ws + p.w;
+  }
+  RowTerm* term = (RowTerm*)(ws + p.term);
+  float* unlift = (float*)(ws + p.unlift);
+  char* g = ws + p.g;
+  float* sums = (float*)(ws + p.sums);
+  COOP_LAUNCH(K_XENT_TERMS, (k_xent_terms<T != COOP_F32>), dim3((unsigned)((p.rows + 1023) / 1024)), dim3(1024), 0, s, targets, ignore, lse, dloss,
+              alpha, T == COOP_F16 ? 8192.f : 1.f, p.n, p.rows, p.vocab, term, unlift, bad);
+  const int64_t g_ld = p.piece * kElem<T>;
+  const Operand w{(const char*)weight, p.ld, p.vocab, p.ld}, h{(const char*)hidden, p.ld, p.n, p.ld};
+  typedef Product<T, 2, 4, 4, 2, false, false> P;
+  const auto kg = k_xent_g<T, 2, 4, 4, 2>;
+  const auto kh = k_xent_dh<T, 2, 4, 4, 2>;
+  const auto kw = k_xent_dw<T, 2, 4, 4, 2>;
+  if (!allow_lds(kg, P::kLds) || !allow_lds(kh, P::kLds) || !allow_lds(kw, P::kLds)) return COOP_E_HIP;
+  const uint32_t row_tiles = (uint32_t)(p.rows / kTile), col_tiles = (uint32_t)((p.width + kTile - 1) / kTile);
+  for (int64_t v = 0; v < p.vocab; v += p.piece) {
+    const int64_t len = p.vocab - v < p.piece ? p.vocab - v : p.piece;
+    const uint32_t tiles = (uint32_t)((len + kTile - 1) / kTile);
+    COOP_LAUNCH(K_XENT_G, kg, dim3(tiles * row_tiles), dim3(P::kThreads), P::kLds, s, w, h, p.vocab, p.width, alpha * kLog2e, v, tiles,
+                (const RowTerm*)term, g, g_ld);
+    if (dhidden != nullptr) {
+      const Operand wt{(const char*)weight + v * p.ld, p.ld, p.ld, len}, gi{g, g_ld, p.rows, (int64_t)tiles * kTile * kElem<T>};
+      COOP_LAUNCH(K_XENT_DH, kh, dim3(row_tiles * col_tiles * p.dh_splits), dim3(P::kThreads), P::kLds, s, wt, gi, len, p.dh_splits, col_tiles,
+                  row_tiles, v != 0, sums, p.width);
+    }
+    if (dweight != nullptr) {
+      const Operand ht{(const char*)hidden, p.ld, p.ld, p.n}, gt{g, g_ld, (int64_t)tiles * kTile * kElem<T>, p.rows};
+      COOP_LAUNCH(K_XENT_DW, kw, dim3(tiles * col_tiles), dim3(P::kThreads), P::kLds, s, ht, gt, p.n, p.vocab, v, dim, col_tiles,
+                  (const float*)unlift, (char*)dweight);
+    }
+  }
+  const int64_t out_blocks = (p.n * dim + kBlock - 1) / kBlock;
+  if (dhidden != nullptr)
+    COOP_LAUNCH(K_XENT_DH_OUT, k_xent_dh_out<T>, dim3((unsigned)(out_blocks < 16384 ? out_blocks : 16384)), dim3(kBlock), 0, s, (const float*)sums,
+                p.dh_splits, p.rows, p.width, p.n, dim, (const float*)unlift, (char*)dhidden);
+  return hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
+}
+
+}  // namespace
+}  // namespace coop
+
+using namespace coop;
+
+extern "C" size_t coop_softmax_xent_workspace_bytes(int64_t n, int64_t vocab, int32_t dim, int dtype, int aligned, int grad) {
+  if (xent_check(nullptr, 0, nullptr, vocab, dim, dtype, nullptr) != COOP_OK || n < 0 || n >= ((int64_t)1 << 24)) return 0;
+  return n == 0 ? 256 : XentPlan(n, vocab, dim, dtype, aligned != 0, grad != 0).bytes;
+}
+
+extern "C" int coop_softmax_xent(const void* hidden, int64_t n, const void* weight, int64_t vocab, int32_t dim, int dtype,
+                                 const int32_t* targets, float alpha, int32_t ignore, float* loss_out, float* lse_out, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  const int rc = xent_check(hidden, n, weight, vocab, dim, dtype, targets);
+  if (rc != COOP_OK) return rc;
+  if (n == 0) return COOP_OK;
+  if (!loss_out || !lse_out || !workspace) return COOP_E_NULL;
+  const XentPlan p(n, vocab, dim, dtype, xent_aligned(hidden, weight), false);
+  if (workspace_bytes < p.bytes || ((uintptr_t)workspace & 255) != 0) return COOP_E_ARG;
+  int32_t* bad = bad_flag();
+  if (!bad) return COOP_E_HIP;
+  int r = COOP_OK;
+  with_dtype(dtype, [&](auto t) {
+    r = forward<decltype(t)::value>(p, hidden, weight, dim, targets, alpha, ignore, loss_out, lse_out, (char*)workspace, bad, (hipStream_t)stream);
+  });
+  return r;
+}
+
+extern "C" int coop_softmax_xent_grad(const void* hidden, int64_t n, const void* weight, int64_t vocab, int32_t dim, int dtype,
+                                      const int32_t* targets, float alpha, int32_t ignore, const float* lse, const float* dloss, void* dhidden,
+                                      void* dweight, void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = xent_check(hidden, n, weight, vocab, dim, dtype, targets);
+  if (rc != COOP_OK) return rc;
+  if (!aligned_for(dhidden, dtype) || !aligned_for(dweight, dtype)) return COOP_E_ARG;
+  if (!dhidden && !dweight) return COOP_OK;
+  if (n == 0) {
+    if (dweight != nullptr) clear_bytes(dweight, vocab * dim * element_bytes(dtype), (hipStream_t)stream);
+    return hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
+  }
+  if (!lse || !dloss || !workspace) return COOP_E_NULL;
+  const XentPlan p(n, vocab, dim, dtype, xent_aligned(hidden, weight), true);
+  if (workspace_bytes < p.bytes || ((uintptr_t)workspace & 255) != 0) return COOP_E_ARG;
+  int32_t* bad = bad_flag();
+  if (!bad) return COOP_E_HIP;
+  int r = COOP_OK;
+  with_dtype(dtype, [&](auto t) {
+    r = backward<decltype(t)::value>(p, hidden, weight, dim, targets, alpha, ignore, lse, dloss, dhidden, dweight, (char*)workspace, bad,
+                                     (hipStream_t)stream);
+  });
+  return r;
+}
