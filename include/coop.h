@@ -379,7 +379,7 @@ int coop_layer_norm_grad(const void* dy, const void* x, int64_t n_rows, int32_t 
 /*
  * Softmax cross entropy over a vocabulary (the vertices of a graph, say) without the logits in memory: with
  * z_iv = alpha <hidden_i, weight_v>, lse_i = log sum over v of exp z_iv and loss_i = lse_i - z_i,targets[i].
- *   hidden   device [n, dim], weight device [vocab, dim], both of dtype; n < 2^24, dim <= 2^20
+ *   hidden   device [n, dim], weight device [vocab, dim], both of dtype; n < 2^24, dim <= 2^18
  *   targets  device int32 [n]; a row whose target is `ignore` has loss 0 and no gradient; other targets outside [0, vocab)
  *            likewise, and are reported
  *   loss_out, lse_out  device float [n]

@@ -26,7 +26,8 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char LdsByte;
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
-constexpr int kStageBytes = 128;  // of k per row and stage: 64 elements of 16 bits, 32 of 32
+constexpr int kStageBytes = 64;  // of k per row and stage: 32 elements of 16 bits, 16 of 32
+constexpr int kStages = 4;       // in LDS: one is read, the others are on their way
 constexpr float kNoMax = -3.402823466e38f;
 
 template <int T> constexpr int kElem = T == COOP_F32 ? 4 : 2;
@@ -55,47 +56,54 @@ struct Operand {
 };
 
 // How a stage of R rows of an operand lies in LDS, in 16-byte slots filled in order by the loads, 64 to a wave's load.
-//   k contiguous: a row's 8 chunks, exchanged by the row's number so that 8 neighbouring rows' same chunk lie in different banks;
+//   k contiguous: a row's 4 chunks, exchanged by the row's number so that what 16 lanes read together lies in different banks;
 //   k strided: a row of k holds R elements; its chunks are exchanged by k so that what one fragment reads lies in different banks.
+// Both exchanges are an exclusive or with bits that neither the next tile of 32 rows nor the next step of k changes.
 template <int T, int R, bool STRIDED, int WAVES>
 struct Staged {
   static constexpr int kBytes = R * kStageBytes;
   static constexpr int kChunks = STRIDED ? R * kElem<T> / 16 : kStageBytes / 16;  // of a row
-  static constexpr int kLoads = kBytes / 1024;                                    // of a wave each
-  static_assert(kLoads % WAVES == 0 || kLoads < WAVES, "loads are dealt to the waves evenly");
+  static constexpr int kAll = kBytes / 1024;                                      // loads of a stage
+  static_assert(kAll % WAVES == 0 || kAll < WAVES, "loads are dealt to the waves evenly, or the first ones have one");
+  static constexpr int kLoads = kAll / WAVES;  // that every wave has
   static __device__ __forceinline__ int swizzle(int row) {
-    if constexpr (!STRIDED) return row & 7;
-    else if constexpr (T == COOP_F32) return (row >> 2 & 1) << 3;
+    if constexpr (!STRIDED) return row >> 2 & 3;
+    else if constexpr (T == COOP_F32) return (row >> 2 & 1) << 3 & (kChunks - 1);
     else return (((row & 3) | (row >> 3 & 1) << 2) << 2) & (kChunks - 1);
   }
-  // starts the loads of the stage whose first k is k0; row0: the tile's first row
-  static __device__ __forceinline__ void load(const Operand& op, int64_t row0, int64_t k0, char* lds) {
-    const char* base;
-    int64_t there;  // rows of the memory layout that exist from the base on
-    if constexpr (STRIDED) {
-      base = op.base + k0 * op.ld + row0 * kElem<T>;
-      there = op.k - k0;
-      if (there > kStageK<T>) there = kStageK<T>;
-    } else {
-      base = op.base + row0 * op.ld + k0 * kElem<T>;
-      there = op.rows - row0;
-      if (there > R) there = R;
+  // The stage that is loaded next: where it begins in memory, how many of the memory layout's rows there are, and bytes in each.
+  struct Feed {
+    const char* p;
+    int ld, there, in_row;
+    __device__ __forceinline__ void begin(const Operand& op, int64_t row0, int64_t k0) {
+      const int64_t most = 1 << 30, rows = STRIDED ? op.k - k0 : op.rows - row0, bytes = STRIDED ? op.rows - row0 * kElem<T> : op.k - k0 * kElem<T>;
+      p = op.base + (STRIDED ? k0 * op.ld + row0 * kElem<T> : row0 * op.ld + k0 * kElem<T>);
+      ld = (int)op.ld;
+      there = (int)(rows < 0 ? 0 : rows < most ? rows : most);
+      in_row = (int)(bytes < 0 ? 0 : bytes < most ? bytes : most);
     }
-    if (there < 0) there = 0;
-    // (what lies behind the last row, and chunks beyond a row's end, read as zero)
-    const int64_t in_row = STRIDED ? op.rows - row0 * kElem<T> : op.k - k0 * kElem<T>;
-    const int records = there > 0 ? (int)((there - 1) * op.ld + (in_row < op.ld ? in_row : op.ld)) : 0;
-    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, records, 0x00020000);
-    const int wave = uniform_wave_in_block(), lane = lane_id();
+    __device__ __forceinline__ void next() {
+      if constexpr (STRIDED) p += (int64_t)ld * kStageK<T>, there -= kStageK<T>;
+      else p += kStageBytes, in_row -= kStageBytes;
+    }
+    // starts this wave's loads; rows that are not there, and chunks behind a row's end, read as zero
+    __device__ __forceinline__ void load(char* lds) const {
+      constexpr int kRows = STRIDED ? kStageK<T> : R;
+      const int rows = there < kRows ? there : kRows, last = (rows - 1) * ld + (in_row < ld ? in_row : ld);
+      const int records = rows > 0 && in_row > 0 ? last : 0;
+      const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, records, 0x00020000);
+      const int wave = uniform_wave_in_block(), lane = lane_id();
 #pragma unroll
-    for (int i = 0; i < (kLoads + WAVES - 1) / WAVES; ++i) {
-      const int l = i * WAVES + wave;
-      if (kLoads % WAVES != 0 && l >= kLoads) break;
-      const int slot = l * kWave + lane, row = slot / kChunks, chunk = (slot % kChunks) ^ swizzle(row);
-      const int at = chunk * 16 < in_row ? row * (int)op.ld + chunk * 16 : 0x7FFFFF00;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(LdsByte*)(lds + l * 1024), 16, at, 0, 0, 0);
+      for (int i = 0; i < (kAll + WAVES - 1) / WAVES; ++i) {
+        const int l = i * WAVES + wave;
+        if (kAll < WAVES && l >= kAll) break;
+        const int slot = l * kWave + lane, row = slot / kChunks, chunk = (slot % kChunks) ^ swizzle(row);
+        // (an offset beyond all records where the chunk is not there)
+        const int at = (chunk * 16 < in_row ? lane / kChunks * ld + chunk * 16 : 0x3FFFFFFF) + l * kWave / kChunks * ld;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(LdsByte*)(lds + l * 1024), 16, at, 0, 0, 0);
+      }
     }
-  }
+  };
   // the fragment of rows row .. row + 31 at step kk of the stage
   static __device__ __forceinline__ u32x4 fragment(const char* lds, int row, int kk) {
     const int lane = lane_id();
@@ -129,61 +137,112 @@ struct Staged {
   }
 };
 
-// The loads into LDS that this wave has started have arrived, and then the waves meet.  (A barrier alone does not wait for them.)
-__device__ __forceinline__ void arrive_and_meet() {
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-}
-
-// A block's tile of C: WA x WB waves with TA x TB tiles of 32 x 32 each, rows of A by rows of B.
+// A block's tile of C: WA x WB waves with TA x TB tiles of 32 x 32 each, rows of A by rows of B.  The stages of all of a block's tiles
+// are one stream: while one is multiplied the next kStages - 1 are on their way, the first of the next tile among them.
 template <int T, int WA, int WB, int TA, int TB, bool SA, bool SB>
 struct Product {
   static constexpr int kWaves = WA * WB, kThreads = kWaves * kWave;
   static constexpr int kRowsA = WA * TA * 32, kRowsB = WB * TB * 32;
   typedef Staged<T, kRowsA, SA, kWaves> A;
   typedef Staged<T, kRowsB, SB, kWaves> B;
-  static constexpr int kLds = 2 * (A::kBytes + B::kBytes);
+  static constexpr int kStage = A::kBytes + B::kBytes, kLds = kStages * kStage;
   f32x16 acc[TA][TB];
+  u32x4 fa[TA], fb[TB];  // the second half of the last stage that was read
+  typename A::Feed a;    // the stage that is loaded next ...
+  typename B::Feed b;
+  int left;              // ... so many of its tile's are to be loaded
+  int slot;              // where it goes; the one behind it is read next
+  char* lds;
+  Operand op_a, op_b;
+  int64_t k0, row_a, row_b, step_a;  // tiles follow one another step_a rows of A apart, or there is one (0)
+  int stages;
 
   __device__ __forceinline__ static int a0() { return uniform_wave_in_block() / WB * (TA * 32); }
   __device__ __forceinline__ static int b0() { return uniform_wave_in_block() % WB * (TB * 32); }
   // C's element j of a 32 x 32 tile: its row; its column is lane & 31
   __device__ __forceinline__ static int row_of(int j) { return (j >> 2) * 8 + (lane_id() >> 5) * 4 + (j & 3); }
 
-  // `lds` is free for use, as far as this block's waves have met since they last read it; the waves meet once more at the end
-  __device__ __forceinline__ void run(const Operand& a, const Operand& b, int64_t row_a, int64_t row_b, int64_t k0, int64_t k1, char* lds) {
+  __device__ __forceinline__ void load(char* into) {
+    a.load(into);
+    b.load(into + A::kBytes);
+    a.next();
+    b.next();
+    if (--left == 0) {
+      left = stages;
+      row_a += step_a;
+      a.begin(op_a, row_a, k0);
+      b.begin(op_b, row_b, k0);
+      if (step_a == 0) a.there = b.there = 0;  // (behind the only tile there is nothing to load)
+    }
+  }
+  // Of this wave's loads, those of the stage that is read next have arrived (only younger ones are left: loads arrive in the order in
+  // which they were sent), and its reads are done; then the waves meet.  (A barrier alone does not wait for loads into LDS.)
+  static __device__ __forceinline__ void meet() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * (A::kLoads + B::kLoads)) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  __device__ __forceinline__ void multiply(const u32x4 (&x)[TA], const u32x4 (&y)[TB]) {
+#pragma unroll
+    for (int i = 0; i < TA; ++i)
+#pragma unroll
+      for (int j = 0; j < TB; ++j) acc[i][j] = mma<T>(x[i], y[j], acc[i][j]);
+  }
+  static __device__ __forceinline__ void read(const char* from, int kk, u32x4 (&x)[TA], u32x4 (&y)[TB]) {
+#pragma unroll
+    for (int i = 0; i < TA; ++i) x[i] = A::fragment(from, a0() + i * 32, kk);
+#pragma unroll
+    for (int j = 0; j < TB; ++j) y[j] = B::fragment(from + A::kBytes, b0() + j * 32, kk);
+  }
+  // Reads the stage in `from`, each half while the one before it is multiplied; `into`, which held the stage before, gets a new one.
+  // (The two are never the same memory, and the compiler is told so: no read waits for the loads that are started here.)
+  template <bool FIRST>
+  __device__ __forceinline__ void stage(char* __restrict__ into, const char* __restrict__ from) {
+    load(into);
+    u32x4 na[TA], nb[TB];
+    read(from, 0, na, nb);
+    if constexpr (!FIRST) multiply(fa, fb);
+    read(from, 1, fa, fb);
+    multiply(na, nb);
+  }
+
+  // the first tile is at rows row_a, row_b; k from k0 to k1 (k1 > k0)
+  __device__ __forceinline__ void begin(const Operand& a_, const Operand& b_, int64_t row_a_, int64_t row_b_, int64_t k0_, int64_t k1, int64_t step,
+                                        char* lds_) {
+    op_a = a_, op_b = b_, lds = lds_, k0 = k0_, row_a = row_a_, row_b = row_b_, step_a = step;
+    left = stages = (int)((k1 - k0 + kStageK<T> - 1) / kStageK<T>);
+    a.begin(op_a, row_a, k0);
+    b.begin(op_b, row_b, k0);
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) load(lds + s * kStage);
+    slot = kStages - 1;
+  }
+  // the next tile's product
+  __device__ __forceinline__ void tile() {
 #pragma unroll
     for (int i = 0; i < TA; ++i)
 #pragma unroll
       for (int j = 0; j < TB; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-    char* la[2] = {lds, lds + A::kBytes};
-    char* lb[2] = {lds + 2 * A::kBytes, lds + 2 * A::kBytes + B::kBytes};
-    A::load(a, row_a, k0, la[0]);
-    B::load(b, row_b, k0, lb[0]);
-    arrive_and_meet();
-    int at = 0;
-    for (int64_t k = k0; k < k1; k += kStageK<T>) {
-      if (k + kStageK<T> < k1) {
-        A::load(a, row_a, k + kStageK<T>, la[at ^ 1]);
-        B::load(b, row_b, k + kStageK<T>, lb[at ^ 1]);
-      }
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        u32x4 fa[TA], fb[TB];
-#pragma unroll
-        for (int i = 0; i < TA; ++i) fa[i] = A::fragment(la[at], a0() + i * 32, kk);
-#pragma unroll
-        for (int j = 0; j < TB; ++j) fb[j] = B::fragment(lb[at], b0() + j * 32, kk);
-#pragma unroll
-        for (int i = 0; i < TA; ++i)
-#pragma unroll
-          for (int j = 0; j < TB; ++j) acc[i][j] = mma<T>(fa[i], fb[j], acc[i][j]);
-      }
-      arrive_and_meet();
-      at ^= 1;
+    int from = slot + 1 < kStages ? slot + 1 : 0;
+    meet();
+    stage<true>(lds + slot * kStage, lds + from * kStage);
+    slot = from;
+    for (int s = 1; s < stages; ++s) {
+      from = slot + 1 < kStages ? slot + 1 : 0;
+      meet();
+      stage<false>(lds + slot * kStage, lds + from * kStage);
+      slot = from;
     }
+    multiply(fa, fb);
+  }
+  // LDS is free for other use: what is on its way has arrived, and all waves have read.  A block does not end without it.
+  static __device__ __forceinline__ void end() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();
   }
 };
 
@@ -193,7 +252,7 @@ struct Product {
 struct RowStat { float top, sum, target, pad; };
 
 template <int T, int WA, int WB, int TA, int TB>
-__global__ __launch_bounds__(WA* WB* kWave) void k_xent_stats(Operand w, Operand h, int64_t n, int64_t vocab, int64_t k, float scale2,
+__global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1))) void k_xent_stats(Operand w, Operand h, int64_t n, int64_t vocab, int64_t k, float scale2,
                                                                const int32_t* __restrict__ targets, int splits, RowStat* __restrict__ part) {
   typedef Product<T, WA, WB, TA, TB, false, false> P;
   extern __shared__ char lds[];
@@ -209,45 +268,52 @@ __global__ __launch_bounds__(WA* WB* kWave) void k_xent_stats(Operand w, Operand
     top[j] = kNoMax;
     sum[j] = target[j] = 0.f;
   }
+  p.begin(w, h, (int64_t)split * P::kRowsA, row0, 0, k, (int64_t)splits * P::kRowsA, lds);
   for (int64_t v0 = (int64_t)split * P::kRowsA; v0 < vocab; v0 += (int64_t)splits * P::kRowsA) {
-    p.run(w, h, v0, row0, 0, k, lds);
+    p.tile();
     const int64_t first = v0 + P::a0();
     const bool ragged = first + TA * 32 > vocab;
 #pragma unroll
     for (int j = 0; j < TB; ++j) {
-#pragma unroll
-      for (int i = 0; i < TA; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) p.acc[i][j][e] *= scale2;
+      __builtin_amdgcn_sched_barrier(0);  // (a column of tiles at a time: all of them at once do not fit into the registers)
       const int64_t mine = (int64_t)t[j] - first;
       if (ballot64(mine >= 0 && mine < TA * 32) != 0) {
 #pragma unroll
         for (int i = 0; i < TA; ++i)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (mine == i * 32 + P::row_of(e)) target[j] = p.acc[i][j][e];
+            if (mine == i * 32 + P::row_of(e)) target[j] = p.acc[i][j][e] * scale2;
       }
-      if (ragged) {
+      if (ragged) {  // (what is not there never is the largest, and adds nothing)
 #pragma unroll
         for (int i = 0; i < TA; ++i)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (first + i * 32 + P::row_of(e) >= vocab) p.acc[i][j][e] = -__builtin_inff();
+            if (first + i * 32 + P::row_of(e) >= vocab) p.acc[i][j][e] = scale2 < 0.f ? __builtin_inff() : -__builtin_inff();
       }
-      float m = top[j];
+      float x[TA * 16];
 #pragma unroll
       for (int i = 0; i < TA; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) m = fmaxf(m, p.acc[i][j][e]);
-      float s = 0.f;
+        for (int e = 0; e < 16; ++e) x[i * 16 + e] = p.acc[i][j][e];
+      // the largest times a positive factor is the largest product, rounded or not
+      float m = x[0];
+      if (scale2 < 0.f) {
 #pragma unroll
-      for (int i = 0; i < TA; ++i)
+        for (int e = 1; e < TA * 16; ++e) m = fminf(m, x[e]);
+      } else {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f(p.acc[i][j][e] - m);
-      sum[j] = sum[j] * __builtin_amdgcn_exp2f(top[j] - m) + s;
+        for (int e = 1; e < TA * 16; ++e) m = fmaxf(m, x[e]);
+      }
+      m = fmaxf(top[j], m * scale2);
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < TA * 16; ++e) s[e & 3] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale2, -m));
+      sum[j] = sum[j] * __builtin_amdgcn_exp2f(top[j] - m) + ((s[0] + s[1]) + (s[2] + s[3]));
       top[j] = m;
     }
   }
+  P::end();
   // lanes l and l + 32 have the same rows, and so have the waves of a column of waves
   RowStat* stat = reinterpret_cast<RowStat*>(lds);
 #pragma unroll
@@ -274,19 +340,28 @@ __global__ __launch_bounds__(WA* WB* kWave) void k_xent_stats(Operand w, Operand
   }
 }
 
+// a wave joins a row's splits
 __global__ __launch_bounds__(kBlock) void k_xent_loss(const RowStat* __restrict__ part, int splits, int64_t n, int64_t vocab,
                                                       const int32_t* __restrict__ targets, int32_t ignore, float* __restrict__ loss,
                                                       float* __restrict__ lse, int32_t* __restrict__ bad) {
-  const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+  const int64_t i = (int64_t)blockIdx.x * kWavesPerBlock + uniform_wave_in_block();
   if (i >= n) return;
-  float m = kNoMax;
-  for (int s = 0; s < splits; ++s) m = fmaxf(m, part[s * n + i].top);
-  float sum = 0.f, target = 0.f;
-  for (int s = 0; s < splits; ++s) {
+  float m = kNoMax, sum = 0.f, target = 0.f;
+  for (int s = lane_id(); s < splits; s += kWave) {
     const RowStat x = part[s * n + i];
-    sum += x.sum * __builtin_amdgcn_exp2f(x.top - m);
+    const float top = fmaxf(m, x.top);
+    sum = sum * __builtin_amdgcn_exp2f(m - top) + x.sum * __builtin_amdgcn_exp2f(x.top - top);
+    m = top;
     target += x.target;
   }
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) {
+    const float top = fmaxf(m, __shfl_xor(m, off, kWave)), mine = sum * __builtin_amdgcn_exp2f(m - top);
+    sum = mine + __shfl_xor(mine, off, kWave);
+    target += __shfl_xor(target, off, kWave);
+    m = top;
+  }
+  if (lane_id() != 0) return;
   const int32_t t = targets[i];
   const bool ok = t != ignore && (uint64_t)(int64_t)t < (uint64_t)vocab;
   if (!ok && t != ignore) atomicOr(bad, 1);
@@ -346,13 +421,15 @@ __device__ __forceinline__ void put4(char* p, const float (&f)[4]) {
 // G of the piece of the vocabulary that begins at v_first, [rows of H, ld bytes]; all of G's tiles are there, beyond the vocabulary's
 // and the rows' end it is zero
 template <int T, int WA, int WB, int TA, int TB>
-__global__ __launch_bounds__(WA* WB* kWave) void k_xent_g(Operand w, Operand h, int64_t vocab, int64_t k, float scale2, int64_t v_first,
+__global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1))) void k_xent_g(Operand w, Operand h, int64_t vocab, int64_t k, float scale2, int64_t v_first,
                                                            uint32_t tiles_a, const RowTerm* __restrict__ term, char* __restrict__ g, int64_t ld) {
   typedef Product<T, WA, WB, TA, TB, false, false> P;
   extern __shared__ char lds[];
   const int64_t piece0 = (int64_t)(blockIdx.x % tiles_a) * P::kRowsA, row0 = (int64_t)(blockIdx.x / tiles_a) * P::kRowsB;
   P p;
-  p.run(w, h, v_first + piece0, row0, 0, k, lds);
+  p.begin(w, h, v_first + piece0, row0, 0, k, 0, lds);
+  p.tile();
+  P::end();
   const int64_t first = v_first + piece0 + P::a0();
   const bool ragged = first + TA * 32 > vocab;
 #pragma unroll
@@ -389,7 +466,7 @@ __global__ __launch_bounds__(WA* WB* kWave) void k_xent_g(Operand w, Operand h, 
 
 // dH: sums[split][row][dim] (+)= the split's part of G W over the piece
 template <int T, int WA, int WB, int TA, int TB>
-__global__ __launch_bounds__(WA* WB* kWave) void k_xent_dh(Operand wt, Operand g, int64_t k, int splits, uint32_t tiles_a, uint32_t tiles_b,
+__global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1))) void k_xent_dh(Operand wt, Operand g, int64_t k, int splits, uint32_t tiles_a, uint32_t tiles_b,
                                                             bool add, float* __restrict__ sums, int64_t width) {
   typedef Product<T, WA, WB, TA, TB, true, false> P;
   extern __shared__ char lds[];
@@ -398,7 +475,9 @@ __global__ __launch_bounds__(WA* WB* kWave) void k_xent_dh(Operand wt, Operand g
   const int64_t stages = (k + kStageK<T> - 1) / kStageK<T>;
   const int64_t k0 = stages * split / splits * kStageK<T>, k1 = stages * (split + 1) / splits * kStageK<T>;
   P p;
-  p.run(wt, g, col0, row0, k0, k1, lds);
+  p.begin(wt, g, col0, row0, k0, k1, 0, lds);
+  p.tile();
+  P::end();
   float* to = sums + (int64_t)split * tiles_b * P::kRowsB * width;
 #pragma unroll
   for (int j = 0; j < TB; ++j)
@@ -432,13 +511,15 @@ __global__ __launch_bounds__(kBlock) void k_xent_dh_out(const float* __restrict_
 
 // dW of the piece: rows v_first .. of the weight's gradient
 template <int T, int WA, int WB, int TA, int TB>
-__global__ __launch_bounds__(WA* WB* kWave) void k_xent_dw(Operand ht, Operand gt, int64_t k, int64_t vocab, int64_t v_first, int32_t dim,
+__global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1))) void k_xent_dw(Operand ht, Operand gt, int64_t k, int64_t vocab, int64_t v_first, int32_t dim,
                                                             uint32_t tiles_a, const float* __restrict__ unlift, char* __restrict__ out) {
   typedef Product<T, WA, WB, TA, TB, true, true> P;
   extern __shared__ char lds[];
   const int64_t col0 = (int64_t)(blockIdx.x % tiles_a) * P::kRowsA, piece0 = (int64_t)(blockIdx.x / tiles_a) * P::kRowsB;
   P p;
-  p.run(ht, gt, col0, piece0, 0, k, lds);
+  p.begin(ht, gt, col0, piece0, 0, k, 0, lds);
+  p.tile();
+  P::end();
   const float u = *unlift;
 #pragma unroll
   for (int j = 0; j < TB; ++j) {
@@ -504,7 +585,7 @@ struct XentPlan {
     pieces = (vocab + piece - 1) / piece;
     const int64_t dh_tiles = rows / kTile * ((width + kTile - 1) / kTile);
     int64_t ds = 256 / dh_tiles;
-    const int64_t stages = piece * es / kStageBytes;
+    const int64_t first = piece < vocab ? piece : vocab, stages = (first * es + kStageBytes - 1) / kStageBytes;
     ds = ds < 1 ? 1 : ds > 16 ? 16 : ds;
     dh_splits = (int)(ds < stages ? ds : stages);
     size_t at = 0;
@@ -537,7 +618,7 @@ bool xent_aligned(const void* hidden, const void* weight) { return (((uintptr_t)
 
 int xent_check(const void* hidden, int64_t n, const void* weight, int64_t vocab, int32_t dim, int dtype, const int32_t* targets) {
   if (!known_dtype(dtype)) return COOP_E_ARG;
-  if (n < 0 || n >= ((int64_t)1 << 24) || vocab < 1 || vocab >= ((int64_t)1 << 31) || dim < 1 || dim > (1 << 20)) return COOP_E_ARG;
+  if (n < 0 || n >= ((int64_t)1 << 24) || vocab < 1 || vocab >= ((int64_t)1 << 31) || dim < 1 || dim > (1 << 18)) return COOP_E_ARG;
   if (n > 0 && (!hidden || !weight || !targets)) return COOP_E_NULL;
   if (!aligned_for(hidden, dtype) || !aligned_for(weight, dtype)) return COOP_E_ARG;
   return COOP_OK;
@@ -566,9 +647,9 @@ int forward(const XentPlan& p, const void* hidden, const void* weight, int32_t d
   }
   const Operand w{(const char*)weight, p.ld, p.vocab, p.ld}, h{(const char*)hidden, p.ld, p.n, p.ld};
   RowStat* part = (RowStat*)(ws + p.part);
-  const bool ok = p.few ? launch_stats<T, 8, 1, 1, 1>(p, w, h, alpha, targets, part, s) : launch_stats<T, 2, 4, 4, 2>(p, w, h, alpha, targets, part, s);
+  const bool ok = p.few ? launch_stats<T, 4, 1, 2, 1>(p, w, h, alpha, targets, part, s) : launch_stats<T, 2, 2, 4, 4>(p, w, h, alpha, targets, part, s);
   if (!ok) return COOP_E_HIP;
-  COOP_LAUNCH(K_XENT_LOSS, k_xent_loss, dim3((unsigned)((p.n + kBlock - 1) / kBlock)), dim3(kBlock), 0, s, (const RowStat*)part, p.splits, p.n,
+  COOP_LAUNCH(K_XENT_LOSS, k_xent_loss, dim3((unsigned)((p.n + kWavesPerBlock - 1) / kWavesPerBlock)), dim3(kBlock), 0, s, (const RowStat*)part, p.splits, p.n,
               p.vocab, targets, ignore, loss, lse, bad);
   return hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
 }
@@ -590,10 +671,10 @@ int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t 
               alpha, T == COOP_F16 ? 8192.f : 1.f, p.n, p.rows, p.vocab, term, unlift, bad);
   const int64_t g_ld = p.piece * kElem<T>;
   const Operand w{(const char*)weight, p.ld, p.vocab, p.ld}, h{(const char*)hidden, p.ld, p.n, p.ld};
-  typedef Product<T, 2, 4, 4, 2, false, false> P;
-  const auto kg = k_xent_g<T, 2, 4, 4, 2>;
-  const auto kh = k_xent_dh<T, 2, 4, 4, 2>;
-  const auto kw = k_xent_dw<T, 2, 4, 4, 2>;
+  typedef Product<T, 2, 2, 4, 4, false, false> P;
+  const auto kg = k_xent_g<T, 2, 2, 4, 4>;
+  const auto kh = k_xent_dh<T, 2, 2, 4, 4>;
+  const auto kw = k_xent_dw<T, 2, 2, 4, 4>;
   if (!allow_lds(kg, P::kLds) || !allow_lds(kh, P::kLds) || !allow_lds(kw, P::kLds)) return COOP_E_HIP;
   const uint32_t row_tiles = (uint32_t)(p.rows / kTile), col_tiles = (uint32_t)((p.width + kTile - 1) / kTile);
   for (int64_t v = 0; v < p.vocab; v += p.piece) {
@@ -603,8 +684,11 @@ int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t 
                 (const RowTerm*)term, g, g_ld);
     if (dhidden != nullptr) {
       const Operand wt{(const char*)weight + v * p.ld, p.ld, p.ld, len}, gi{g, g_ld, p.rows, (int64_t)tiles * kTile * kElem<T>};
-      COOP_LAUNCH(K_XENT_DH, kh, dim3(row_tiles * col_tiles * p.dh_splits), dim3(P::kThreads), P::kLds, s, wt, gi, len, p.dh_splits, col_tiles,
-                  row_tiles, v != 0, sums, p.width);
+      // (every split has something to do: the last piece may be too short for all of them, and then adds nothing to the others' sums)
+      const int64_t stages = (len + kStageK<T> - 1) / kStageK<T>;
+      const int splits = (int)(p.dh_splits < stages ? p.dh_splits : stages);
+      COOP_LAUNCH(K_XENT_DH, kh, dim3(row_tiles * col_tiles * splits), dim3(P::kThreads), P::kLds, s, wt, gi, len, splits, col_tiles, row_tiles,
+                  v != 0, sums, p.width);
     }
     if (dweight != nullptr) {
       const Operand ht{(const char*)hidden, p.ld, p.ld, p.n}, gt{g, g_ld, (int64_t)tiles * kTile * kElem<T>, p.rows};
