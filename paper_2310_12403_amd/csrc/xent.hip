@@ -71,37 +71,54 @@ struct Staged {
     else if constexpr (T == COOP_F32) return (row >> 2 & 1) << 3 & (kChunks - 1);
     else return (((row & 3) | (row >> 3 & 1) << 2) << 2) & (kChunks - 1);
   }
-  // The stage that is loaded next: where it begins in memory, how many of the memory layout's rows there are, and bytes in each.
-  struct Feed {
+  // A stage that is to be loaded: where it begins in memory, how many of the memory layout's rows there are, and bytes in each.
+  struct Place {
     const char* p;
-    int ld, there, in_row;
-    __device__ __forceinline__ void begin(const Operand& op, int64_t row0, int64_t k0) {
-      const int64_t most = 1 << 30, rows = STRIDED ? op.k - k0 : op.rows - row0, bytes = STRIDED ? op.rows - row0 * kElem<T> : op.k - k0 * kElem<T>;
+    int there, in_row;
+    __device__ __forceinline__ Place() {}
+    __device__ __forceinline__ Place(const Operand& op, int64_t row0, int64_t k0) {
+      const int64_t most = 0x7FFFFFFF, rows = STRIDED ? op.k - k0 : op.rows - row0, bytes = STRIDED ? op.rows - row0 * kElem<T> : op.k - k0 * kElem<T>;
       p = op.base + (STRIDED ? k0 * op.ld + row0 * kElem<T> : row0 * op.ld + k0 * kElem<T>);
-      ld = (int)op.ld;
       there = (int)(rows < 0 ? 0 : rows < most ? rows : most);
       in_row = (int)(bytes < 0 ? 0 : bytes < most ? bytes : most);
     }
-    __device__ __forceinline__ void next() {
+    __device__ __forceinline__ void next(int ld) {
       if constexpr (STRIDED) p += (int64_t)ld * kStageK<T>, there -= kStageK<T>;
       else p += kStageBytes, in_row -= kStageBytes;
     }
-    // starts this wave's loads; rows that are not there, and chunks behind a row's end, read as zero
-    __device__ __forceinline__ void load(char* lds) const {
-      constexpr int kRows = STRIDED ? kStageK<T> : R;
-      const int rows = there < kRows ? there : kRows, last = (rows - 1) * ld + (in_row < ld ? in_row : ld);
-      const int records = rows > 0 && in_row > 0 ? last : 0;
-      const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, records, 0x00020000);
+  };
+  // What a lane loads of every stage: offsets from the stage's beginning.  What is not there reads as zero: rows because they lie behind
+  // the last record; chunks behind a row's end because their offsets are put there, with k strided once and for all.
+  struct Loads {
+    static constexpr int kMine = (kAll + WAVES - 1) / WAVES, kNowhere = 0x3FFFFFFF;
+    int ld, chunk, at[kMine];
+    __device__ __forceinline__ void begin(const Operand& op, const Place& first) {
       const int wave = uniform_wave_in_block(), lane = lane_id();
+      ld = (int)op.ld;
 #pragma unroll
-      for (int i = 0; i < (kAll + WAVES - 1) / WAVES; ++i) {
-        const int l = i * WAVES + wave;
-        if (kAll < WAVES && l >= kAll) break;
-        const int slot = l * kWave + lane, row = slot / kChunks, chunk = (slot % kChunks) ^ swizzle(row);
-        // (an offset beyond all records where the chunk is not there)
-        const int at = (chunk * 16 < in_row ? lane / kChunks * ld + chunk * 16 : 0x3FFFFFFF) + l * kWave / kChunks * ld;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(LdsByte*)(lds + l * 1024), 16, at, 0, 0, 0);
+      for (int i = 0; i < kMine; ++i) {
+        const int slot = (i * WAVES + wave) * kWave + lane, row = slot / kChunks;
+        chunk = ((slot % kChunks) ^ swizzle(row)) * 16;  // (k contiguous: the same for all of a lane's loads)
+        at[i] = row * ld + chunk;
+        if (STRIDED && chunk >= first.in_row) at[i] = kNowhere;
       }
+    }
+    // what the loads of a stage have in common
+    struct Stage {
+      __amdgpu_buffer_rsrc_t rsrc;
+      int off;
+    };
+    __device__ __forceinline__ Stage stage(const Place& s) const {
+      constexpr int kRows = STRIDED ? kStageK<T> : R;
+      const int rows = s.there < kRows ? s.there : kRows, in_row = s.in_row < ld ? s.in_row : ld, last = (rows - 1) * ld + in_row;
+      const int records = (rows < in_row ? rows : in_row) > 0 ? last : 0;
+      return Stage{__builtin_amdgcn_make_buffer_rsrc((void*)s.p, 0, records, 0x00020000), !STRIDED && chunk >= s.in_row ? kNowhere : 0};
+    }
+    __device__ __forceinline__ void start(const Stage& s, char* lds, int i) const {
+      const int l = i * WAVES + uniform_wave_in_block();
+      if (kAll < WAVES && l >= kAll) return;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(s.rsrc, (__attribute__((address_space(3))) void*)(LdsByte*)(lds + l * 1024), 16,
+                                               STRIDED ? at[i] : at[i] + s.off, 0, 0, 0);
     }
   };
   // the fragment of rows row .. row + 31 at step kk of the stage
@@ -148,32 +165,41 @@ struct Product {
   static constexpr int kStage = A::kBytes + B::kBytes, kLds = kStages * kStage;
   f32x16 acc[TA][TB];
   u32x4 fa[TA], fb[TB];  // the second half of the last stage that was read
-  typename A::Feed a;    // the stage that is loaded next ...
-  typename B::Feed b;
-  int left;              // ... so many of its tile's are to be loaded
-  int slot;              // where it goes; the one behind it is read next
-  char* lds;
-  Operand op_a, op_b;
-  int64_t k0, row_a, row_b, step_a;  // tiles follow one another step_a rows of A apart, or there is one (0)
+  typename A::Loads loads_a;
+  typename B::Loads loads_b;
+  typename A::Place a, next_a;  // the stage that is loaded next, and the first one of the tile behind its
+  typename B::Place b, next_b;
+  typename A::Loads::Stage sa;
+  typename B::Loads::Stage sb;
+  int left;                     // stages of its tile that are to be loaded
+  int slot;                     // where in LDS it goes; the one behind it is read next
   int stages;
+  int step_rows;                // from tile to tile, of A; 0: there is one tile
+  int64_t step_bytes;
+  char* lds;
 
   __device__ __forceinline__ static int a0() { return uniform_wave_in_block() / WB * (TA * 32); }
   __device__ __forceinline__ static int b0() { return uniform_wave_in_block() % WB * (TB * 32); }
   // C's element j of a 32 x 32 tile: its row; its column is lane & 31
   __device__ __forceinline__ static int row_of(int j) { return (j >> 2) * 8 + (lane_id() >> 5) * 4 + (j & 3); }
 
-  __device__ __forceinline__ void load(char* into) {
-    a.load(into);
-    b.load(into + A::kBytes);
-    a.next();
-    b.next();
-    if (--left == 0) {
-      left = stages;
-      row_a += step_a;
-      a.begin(op_a, row_a, k0);
-      b.begin(op_b, row_b, k0);
-      if (step_a == 0) a.there = b.there = 0;  // (behind the only tile there is nothing to load)
-    }
+  // to the next stage of the stream
+  __device__ __forceinline__ void next() {
+    a.next(loads_a.ld);
+    b.next(loads_b.ld);
+    --left;
+    const bool done = left == 0;  // (chosen, not branched around: the products go on meanwhile)
+    left = done ? stages : left;
+    a.p = done ? next_a.p : a.p;
+    a.there = done ? next_a.there : a.there;
+    a.in_row = done ? next_a.in_row : a.in_row;
+    b.p = done ? next_b.p : b.p;
+    b.there = done ? next_b.there : b.there;
+    b.in_row = done ? next_b.in_row : b.in_row;
+    next_a.p += done ? step_bytes : 0;
+    next_a.there -= done ? step_rows : 0;
+    sa = loads_a.stage(a);
+    sb = loads_b.stage(b);
   }
   // Of this wave's loads, those of the stage that is read next have arrived (only younger ones are left: loads arrive in the order in
   // which they were sent), and its reads are done; then the waves meet.  (A barrier alone does not wait for loads into LDS.)
@@ -190,34 +216,71 @@ struct Product {
 #pragma unroll
       for (int j = 0; j < TB; ++j) acc[i][j] = mma<T>(x[i], y[j], acc[i][j]);
   }
-  static __device__ __forceinline__ void read(const char* from, int kk, u32x4 (&x)[TA], u32x4 (&y)[TB]) {
+  static constexpr int kMine = A::Loads::kMine + B::Loads::kMine;
+  __device__ __forceinline__ void start(char* into, int i) const {
+    if (i < A::Loads::kMine) loads_a.start(sa, into, i);
+    else if (i < kMine) loads_b.start(sb, into + A::kBytes, i - A::Loads::kMine);
+  }
+  // Half a stage's products, x times y, and between them, one after each of the first products, the reads of the next half (kk of the
+  // stage in `from`) and, with LOADS, the loads of the stage that comes: a wave has its SIMD to itself, so nothing is hidden but by
+  // its own products, and the order is held as it stands here.
+  template <bool PRODUCTS, bool LOADS>
+  __device__ __forceinline__ void half(const u32x4 (&x)[TA], const u32x4 (&y)[TB], const char* from, int kk, u32x4 (&na)[TA], u32x4 (&nb)[TB],
+                                       char* into) {
+    constexpr int kSteps = TA * TB, kReads = TA + TB, kEarly = kSteps >= 2 ? kSteps / 2 : 1, kEach = (kReads + kEarly - 1) / kEarly;
+    constexpr int kLoadEach = (kMine + kSteps - 1) / kSteps;
 #pragma unroll
-    for (int i = 0; i < TA; ++i) x[i] = A::fragment(from, a0() + i * 32, kk);
+    for (int q = 0; q < kSteps; ++q) {
 #pragma unroll
-    for (int j = 0; j < TB; ++j) y[j] = B::fragment(from + A::kBytes, b0() + j * 32, kk);
+      for (int r = q * kEach; r < (q + 1) * kEach && r < kReads; ++r) {  // (the first of A, all of B, the others of A: as they are needed)
+        if (r >= 1 && r <= TB) nb[r - 1] = B::fragment(from + A::kBytes, b0() + (r - 1) * 32, kk);
+        else na[r == 0 ? 0 : r - TB] = A::fragment(from, a0() + (r == 0 ? 0 : r - TB) * 32, kk);
+      }
+      if constexpr (LOADS) {
+#pragma unroll
+        for (int i = q * kLoadEach; i < (q + 1) * kLoadEach && i < kMine; ++i) start(into, i);
+      }
+      if constexpr (PRODUCTS) {
+        acc[q / TB][q % TB] = mma<T>(x[q / TB], y[q % TB], acc[q / TB][q % TB]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
   }
   // Reads the stage in `from`, each half while the one before it is multiplied; `into`, which held the stage before, gets a new one.
   // (The two are never the same memory, and the compiler is told so: no read waits for the loads that are started here.)
   template <bool FIRST>
   __device__ __forceinline__ void stage(char* __restrict__ into, const char* __restrict__ from) {
-    load(into);
     u32x4 na[TA], nb[TB];
-    read(from, 0, na, nb);
-    if constexpr (!FIRST) multiply(fa, fb);
-    read(from, 1, fa, fb);
-    multiply(na, nb);
+    half<!FIRST, true>(fa, fb, from, 0, na, nb, into);
+    next();
+    half<true, false>(na, nb, from, 1, fa, fb, into);
   }
 
   // the first tile is at rows row_a, row_b; k from k0 to k1 (k1 > k0)
-  __device__ __forceinline__ void begin(const Operand& a_, const Operand& b_, int64_t row_a_, int64_t row_b_, int64_t k0_, int64_t k1, int64_t step,
+  __device__ __forceinline__ void begin(const Operand& op_a, const Operand& op_b, int64_t row_a, int64_t row_b, int64_t k0, int64_t k1, int step,
                                         char* lds_) {
-    op_a = a_, op_b = b_, lds = lds_, k0 = k0_, row_a = row_a_, row_b = row_b_, step_a = step;
+    lds = lds_;
+    step_rows = step;
+    step_bytes = step * op_a.ld;
     left = stages = (int)((k1 - k0 + kStageK<T> - 1) / kStageK<T>);
-    a.begin(op_a, row_a, k0);
-    b.begin(op_b, row_b, k0);
-#pragma unroll
-    for (int s = 0; s < kStages - 1; ++s) load(lds + s * kStage);
+    a = typename A::Place(op_a, row_a, k0);
+    b = typename B::Place(op_b, row_b, k0);
+    loads_a.begin(op_a, a);
+    loads_b.begin(op_b, b);
+    next_a = a;
+    next_b = b;
+    next_a.p += step_bytes;
+    next_a.there -= step;
+    if (step == 0) next_a.there = next_b.there = 0;  // (behind the only tile there is nothing to load)
     slot = kStages - 1;
+    sa = loads_a.stage(a);
+    sb = loads_b.stage(b);
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) {
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) start(lds + s * kStage, i);
+      next();
+    }
   }
   // the next tile's product
   __device__ __forceinline__ void tile() {
@@ -268,7 +331,7 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
     top[j] = kNoMax;
     sum[j] = target[j] = 0.f;
   }
-  p.begin(w, h, (int64_t)split * P::kRowsA, row0, 0, k, (int64_t)splits * P::kRowsA, lds);
+  p.begin(w, h, (int64_t)split * P::kRowsA, row0, 0, k, splits * P::kRowsA, lds);
   for (int64_t v0 = (int64_t)split * P::kRowsA; v0 < vocab; v0 += (int64_t)splits * P::kRowsA) {
     p.tile();
     const int64_t first = v0 + P::a0();
@@ -565,6 +628,7 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 struct XentPlan {
   int64_t n, vocab, width, ld;  // width: elements of a padded row
   int64_t rows, piece, pieces;
+  int64_t g_ld;  // bytes from row to row of G: not a power of two, or a tile's rows would all lie in the same few channels of memory
   int splits, dh_splits;
   bool few, pad;
   size_t h, w, part, term, unlift, g, sums, bytes;
@@ -595,7 +659,8 @@ struct XentPlan {
     part = take(grad ? 0 : (size_t)splits * n * sizeof(RowStat));
     term = take(grad ? (size_t)rows * sizeof(RowTerm) : 0);
     unlift = take(grad ? sizeof(float) : 0);
-    g = take(grad ? (size_t)rows * piece * es : 0);
+    g_ld = piece * es + 256;
+    g = take(grad ? (size_t)rows * g_ld : 0);
     sums = take(grad ? (size_t)dh_splits * rows * width * sizeof(float) : 0);
     bytes = at + 256;
   }
@@ -669,7 +734,7 @@ int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t 
   float* sums = (float*)(ws + p.sums);
   COOP_LAUNCH(K_XENT_TERMS, (k_xent_terms<T != COOP_F32>), dim3((unsigned)((p.rows + 1023) / 1024)), dim3(1024), 0, s, targets, ignore, lse, dloss,
               alpha, T == COOP_F16 ? 8192.f : 1.f, p.n, p.rows, p.vocab, term, unlift, bad);
-  const int64_t g_ld = p.piece * kElem<T>;
+  const int64_t g_ld = p.g_ld;
   const Operand w{(const char*)weight, p.ld, p.vocab, p.ld}, h{(const char*)hidden, p.ld, p.n, p.ld};
   typedef Product<T, 2, 2, 4, 4, false, false> P;
   const auto kg = k_xent_g<T, 2, 2, 4, 4>;
