@@ -26,12 +26,12 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char LdsByte;
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
-constexpr int kStageBytes = 64;  // of k per row and stage: 32 elements of 16 bits, 16 of 32
-constexpr int kStages = 4;       // in LDS: one is read, the others are on their way
+// Bytes of k per row and stage: 64 (32 elements of 16 bits, 16 of 32), four stages in LDS, or 128, two of them.  One is read, the others
+// are on their way.  Rows of 64 bytes are half a cache line, so operands with k contiguous take 128.
+constexpr int kWide = 128, kNarrow = 64;
 constexpr float kNoMax = -3.402823466e38f;
 
 template <int T> constexpr int kElem = T == COOP_F32 ? 4 : 2;
-template <int T> constexpr int kStageK = kStageBytes / kElem<T>;
 
 // One 16-byte fragment of each operand into a 32 x 32 tile of C: 16 of k in 16 bits, 8 in 32.
 template <int T>
@@ -56,18 +56,18 @@ struct Operand {
 };
 
 // How a stage of R rows of an operand lies in LDS, in 16-byte slots filled in order by the loads, 64 to a wave's load.
-//   k contiguous: a row's 4 chunks, exchanged by the row's number so that what 16 lanes read together lies in different banks;
+//   k contiguous: a row's 4 or 8 chunks, exchanged by the row's number so that what 8 or 16 lanes read together lies in different banks;
 //   k strided: a row of k holds R elements; its chunks are exchanged by k so that what one fragment reads lies in different banks.
 // Both exchanges are an exclusive or with bits that neither the next tile of 32 rows nor the next step of k changes.
-template <int T, int R, bool STRIDED, int WAVES>
+template <int T, int R, bool STRIDED, int SIZE, int WAVES>
 struct Staged {
-  static constexpr int kBytes = R * kStageBytes;
-  static constexpr int kChunks = STRIDED ? R * kElem<T> / 16 : kStageBytes / 16;  // of a row
+  static constexpr int kBytes = R * SIZE, kK = SIZE / kElem<T>;
+  static constexpr int kChunks = STRIDED ? R * kElem<T> / 16 : SIZE / 16;  // of a row
   static constexpr int kAll = kBytes / 1024;                                      // loads of a stage
   static_assert(kAll % WAVES == 0 || kAll < WAVES, "loads are dealt to the waves evenly, or the first ones have one");
   static constexpr int kLoads = kAll / WAVES;  // that every wave has
   static __device__ __forceinline__ int swizzle(int row) {
-    if constexpr (!STRIDED) return row >> 2 & 3;
+    if constexpr (!STRIDED) return SIZE == 128 ? (row & 7) ^ (row >> 3 & 1) : (row >> 1 & 3) ^ (row >> 3 & 1);
     else if constexpr (T == COOP_F32) return (row >> 2 & 1) << 3 & (kChunks - 1);
     else return (((row & 3) | (row >> 3 & 1) << 2) << 2) & (kChunks - 1);
   }
@@ -83,8 +83,8 @@ struct Staged {
       in_row = (int)(bytes < 0 ? 0 : bytes < most ? bytes : most);
     }
     __device__ __forceinline__ void next(int ld) {
-      if constexpr (STRIDED) p += (int64_t)ld * kStageK<T>, there -= kStageK<T>;
-      else p += kStageBytes, in_row -= kStageBytes;
+      if constexpr (STRIDED) p += (int64_t)ld * kK, there -= kK;
+      else p += SIZE, in_row -= SIZE;
     }
   };
   // What a lane loads of every stage: offsets from the stage's beginning.  What is not there reads as zero: rows because they lie behind
@@ -109,7 +109,7 @@ struct Staged {
       int off;
     };
     __device__ __forceinline__ Stage stage(const Place& s) const {
-      constexpr int kRows = STRIDED ? kStageK<T> : R;
+      constexpr int kRows = STRIDED ? kK : R;
       const int rows = s.there < kRows ? s.there : kRows, in_row = s.in_row < ld ? s.in_row : ld, last = (rows - 1) * ld + in_row;
       const int records = (rows < in_row ? rows : in_row) > 0 ? last : 0;
       return Stage{__builtin_amdgcn_make_buffer_rsrc((void*)s.p, 0, records, 0x00020000), !STRIDED && chunk >= s.in_row ? kNowhere : 0};
@@ -126,7 +126,7 @@ struct Staged {
     const int lane = lane_id();
     if constexpr (!STRIDED) {
       const int r = row + (lane & 31), chunk = kk * 2 + (lane >> 5);
-      return *reinterpret_cast<const u32x4*>(lds + r * kStageBytes + ((chunk ^ swizzle(r)) << 4));
+      return *reinterpret_cast<const u32x4*>(lds + r * SIZE + ((chunk ^ swizzle(r)) << 4));
     } else if constexpr (T == COOP_F32) {
       const int m = row + (lane & 31);
       u32x4 f;
@@ -156,15 +156,16 @@ struct Staged {
 
 // A block's tile of C: WA x WB waves with TA x TB tiles of 32 x 32 each, rows of A by rows of B.  The stages of all of a block's tiles
 // are one stream: while one is multiplied the next kStages - 1 are on their way, the first of the next tile among them.
-template <int T, int WA, int WB, int TA, int TB, bool SA, bool SB>
+template <int T, int WA, int WB, int TA, int TB, bool SA, bool SB, int SIZE>
 struct Product {
   static constexpr int kWaves = WA * WB, kThreads = kWaves * kWave;
   static constexpr int kRowsA = WA * TA * 32, kRowsB = WB * TB * 32;
-  typedef Staged<T, kRowsA, SA, kWaves> A;
-  typedef Staged<T, kRowsB, SB, kWaves> B;
+  static constexpr int kK = SIZE / kElem<T>, kSteps = SIZE / 32, kStages = 256 / SIZE;
+  typedef Staged<T, kRowsA, SA, SIZE, kWaves> A;
+  typedef Staged<T, kRowsB, SB, SIZE, kWaves> B;
   static constexpr int kStage = A::kBytes + B::kBytes, kLds = kStages * kStage;
   f32x16 acc[TA][TB];
-  u32x4 fa[TA], fb[TB];  // the second half of the last stage that was read
+  u32x4 fa[TA], fb[TB];  // the last step of the last stage that was read
   typename A::Loads loads_a;
   typename B::Loads loads_b;
   typename A::Place a, next_a;  // the stage that is loaded next, and the first one of the tile behind its
@@ -180,8 +181,9 @@ struct Product {
 
   __device__ __forceinline__ static int a0() { return uniform_wave_in_block() / WB * (TA * 32); }
   __device__ __forceinline__ static int b0() { return uniform_wave_in_block() % WB * (TB * 32); }
-  // C's element j of a 32 x 32 tile: its row; its column is lane & 31
-  __device__ __forceinline__ static int row_of(int j) { return (j >> 2) * 8 + (lane_id() >> 5) * 4 + (j & 3); }
+  // C's element j of a 32 x 32 tile: its row is the lane's own plus one that all lanes have; its column is lane & 31
+  __device__ __forceinline__ static int own_row() { return (lane_id() >> 5) * 4; }
+  __device__ __forceinline__ static constexpr int row_of(int j) { return (j >> 2) * 8 + (j & 3); }
 
   // to the next stage of the stream
   __device__ __forceinline__ void next() {
@@ -221,16 +223,16 @@ struct Product {
     if (i < A::Loads::kMine) loads_a.start(sa, into, i);
     else if (i < kMine) loads_b.start(sb, into + A::kBytes, i - A::Loads::kMine);
   }
-  // Half a stage's products, x times y, and between them, one after each of the first products, the reads of the next half (kk of the
+  // A step's products, x times y, and between them, one after each of the first products, the reads of the next step (kk of the
   // stage in `from`) and, with LOADS, the loads of the stage that comes: a wave has its SIMD to itself, so nothing is hidden but by
   // its own products, and the order is held as it stands here.
   template <bool PRODUCTS, bool LOADS>
-  __device__ __forceinline__ void half(const u32x4 (&x)[TA], const u32x4 (&y)[TB], const char* from, int kk, u32x4 (&na)[TA], u32x4 (&nb)[TB],
+  __device__ __forceinline__ void step(const u32x4 (&x)[TA], const u32x4 (&y)[TB], const char* from, int kk, u32x4 (&na)[TA], u32x4 (&nb)[TB],
                                        char* into) {
-    constexpr int kSteps = TA * TB, kReads = TA + TB, kEarly = kSteps >= 2 ? kSteps / 2 : 1, kEach = (kReads + kEarly - 1) / kEarly;
-    constexpr int kLoadEach = (kMine + kSteps - 1) / kSteps;
+    constexpr int kMmas = TA * TB, kReads = TA + TB, kEarly = kMmas >= 2 ? kMmas / 2 : 1, kEach = (kReads + kEarly - 1) / kEarly;
+    constexpr int kLoadEach = (kMine + kMmas - 1) / kMmas;
 #pragma unroll
-    for (int q = 0; q < kSteps; ++q) {
+    for (int q = 0; q < kMmas; ++q) {
 #pragma unroll
       for (int r = q * kEach; r < (q + 1) * kEach && r < kReads; ++r) {  // (the first of A, all of B, the others of A: as they are needed)
         if (r >= 1 && r <= TB) nb[r - 1] = B::fragment(from + A::kBytes, b0() + (r - 1) * 32, kk);
@@ -246,14 +248,19 @@ struct Product {
       }
     }
   }
-  // Reads the stage in `from`, each half while the one before it is multiplied; `into`, which held the stage before, gets a new one.
+  // Reads the stage in `from`, each step while the one before it is multiplied; `into`, which held the stage before, gets a new one.
   // (The two are never the same memory, and the compiler is told so: no read waits for the loads that are started here.)
   template <bool FIRST>
   __device__ __forceinline__ void stage(char* __restrict__ into, const char* __restrict__ from) {
     u32x4 na[TA], nb[TB];
-    half<!FIRST, true>(fa, fb, from, 0, na, nb, into);
+    step<!FIRST, true>(fa, fb, from, 0, na, nb, into);
     next();
-    half<true, false>(na, nb, from, 1, fa, fb, into);
+    step<true, false>(na, nb, from, 1, fa, fb, into);
+#pragma unroll
+    for (int kk = 2; kk < kSteps; kk += 2) {
+      step<true, false>(fa, fb, from, kk, na, nb, into);
+      step<true, false>(na, nb, from, kk + 1, fa, fb, into);
+    }
   }
 
   // the first tile is at rows row_a, row_b; k from k0 to k1 (k1 > k0)
@@ -262,7 +269,7 @@ struct Product {
     lds = lds_;
     step_rows = step;
     step_bytes = step * op_a.ld;
-    left = stages = (int)((k1 - k0 + kStageK<T> - 1) / kStageK<T>);
+    left = stages = (int)((k1 - k0 + kK - 1) / kK);
     a = typename A::Place(op_a, row_a, k0);
     b = typename B::Place(op_b, row_b, k0);
     loads_a.begin(op_a, a);
@@ -317,7 +324,7 @@ struct RowStat { float top, sum, target, pad; };
 template <int T, int WA, int WB, int TA, int TB>
 __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1))) void k_xent_stats(Operand w, Operand h, int64_t n, int64_t vocab, int64_t k, float scale2,
                                                                const int32_t* __restrict__ targets, int splits, RowStat* __restrict__ part) {
-  typedef Product<T, WA, WB, TA, TB, false, false> P;
+  typedef Product<T, WA, WB, TA, TB, false, false, kWide> P;
   extern __shared__ char lds[];
   const int split = blockIdx.x % splits;
   const int64_t row0 = (int64_t)(blockIdx.x / splits) * P::kRowsB;
@@ -334,25 +341,24 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
   p.begin(w, h, (int64_t)split * P::kRowsA, row0, 0, k, splits * P::kRowsA, lds);
   for (int64_t v0 = (int64_t)split * P::kRowsA; v0 < vocab; v0 += (int64_t)splits * P::kRowsA) {
     p.tile();
-    const int64_t first = v0 + P::a0();
-    const bool ragged = first + TA * 32 > vocab;
+    const int first = (int)v0 + P::a0() + P::own_row(), left = (int)vocab - first;
 #pragma unroll
     for (int j = 0; j < TB; ++j) {
       __builtin_amdgcn_sched_barrier(0);  // (a column of tiles at a time: all of them at once do not fit into the registers)
-      const int64_t mine = (int64_t)t[j] - first;
-      if (ballot64(mine >= 0 && mine < TA * 32) != 0) {
+      const int mine = t[j] - first;
+      if (ballot64((uint32_t)mine < (uint32_t)(TA * 32)) != 0) {
 #pragma unroll
         for (int i = 0; i < TA; ++i)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
             if (mine == i * 32 + P::row_of(e)) target[j] = p.acc[i][j][e] * scale2;
       }
-      if (ragged) {  // (what is not there never is the largest, and adds nothing)
+      if (v0 + P::kRowsA > vocab) {  // (what is not there never is the largest, and adds nothing)
 #pragma unroll
         for (int i = 0; i < TA; ++i)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (first + i * 32 + P::row_of(e) >= vocab) p.acc[i][j][e] = scale2 < 0.f ? __builtin_inff() : -__builtin_inff();
+            if (i * 32 + P::row_of(e) >= left) p.acc[i][j][e] = scale2 < 0.f ? __builtin_inff() : -__builtin_inff();
       }
       float x[TA * 16];
 #pragma unroll
@@ -486,21 +492,23 @@ __device__ __forceinline__ void put4(char* p, const float (&f)[4]) {
 template <int T, int WA, int WB, int TA, int TB>
 __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1))) void k_xent_g(Operand w, Operand h, int64_t vocab, int64_t k, float scale2, int64_t v_first,
                                                            uint32_t tiles_a, const RowTerm* __restrict__ term, char* __restrict__ g, int64_t ld) {
-  typedef Product<T, WA, WB, TA, TB, false, false> P;
+  typedef Product<T, WA, WB, TA, TB, false, false, kWide> P;
   extern __shared__ char lds[];
   const int64_t piece0 = (int64_t)(blockIdx.x % tiles_a) * P::kRowsA, row0 = (int64_t)(blockIdx.x / tiles_a) * P::kRowsB;
   P p;
   p.begin(w, h, v_first + piece0, row0, 0, k, 0, lds);
   p.tile();
   P::end();
-  const int64_t first = v_first + piece0 + P::a0();
-  const bool ragged = first + TA * 32 > vocab;
+  const int first = (int)(v_first + piece0) + P::a0() + P::own_row(), left = (int)vocab - first;
+  const bool ragged = v_first + piece0 + P::kRowsA > vocab;
 #pragma unroll
   for (int j = 0; j < TB; ++j) {
+    __builtin_amdgcn_sched_barrier(0);
     const int64_t i = row0 + P::b0() + j * 32 + (lane_id() & 31);
     const RowTerm r = term[i];
-    const int64_t mine = r.target - first;
-    const bool hit = ballot64(r.target >= 0 && mine >= 0 && mine < TA * 32) != 0;
+    const int mine = r.target - first;
+    const bool none = r.target < 0, hit = ballot64(!none && (uint32_t)mine < (uint32_t)(TA * 32)) != 0;
+    char* to = g + i * ld + (piece0 + P::a0() + P::own_row()) * kElem<T>;
 #pragma unroll
     for (int a = 0; a < TA; ++a) {
       f32x16 x = p.acc[a][j];
@@ -509,19 +517,19 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
       if (hit) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (mine == a * 32 + P::row_of(e)) x[e] -= 1.f;
+          if (!none && mine == a * 32 + P::row_of(e)) x[e] -= 1.f;
       }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = r.target < 0 ? 0.f : x[e] * r.coef;
+      for (int e = 0; e < 16; ++e) x[e] = none ? 0.f : x[e] * r.coef;
       if (ragged) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (first + a * 32 + P::row_of(e) >= vocab) x[e] = 0.f;
+          if (a * 32 + P::row_of(e) >= left) x[e] = 0.f;
       }
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const float f[4] = {x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
-        put4<T>(g + i * ld + (piece0 + P::a0() + a * 32 + P::row_of(4 * q)) * kElem<T>, f);
+        put4<T>(to + (a * 32 + P::row_of(4 * q)) * kElem<T>, f);
       }
     }
   }
@@ -531,12 +539,12 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
 template <int T, int WA, int WB, int TA, int TB>
 __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1))) void k_xent_dh(Operand wt, Operand g, int64_t k, int splits, uint32_t tiles_a, uint32_t tiles_b,
                                                             bool add, float* __restrict__ sums, int64_t width) {
-  typedef Product<T, WA, WB, TA, TB, true, false> P;
+  typedef Product<T, WA, WB, TA, TB, true, false, kWide> P;
   extern __shared__ char lds[];
   const uint32_t tile = blockIdx.x / splits, split = blockIdx.x % splits;
   const int64_t col0 = (int64_t)(tile % tiles_a) * P::kRowsA, row0 = (int64_t)(tile / tiles_a) * P::kRowsB;
-  const int64_t stages = (k + kStageK<T> - 1) / kStageK<T>;
-  const int64_t k0 = stages * split / splits * kStageK<T>, k1 = stages * (split + 1) / splits * kStageK<T>;
+  const int64_t stages = (k + P::kK - 1) / P::kK;
+  const int64_t k0 = stages * split / splits * P::kK, k1 = stages * (split + 1) / splits * P::kK;
   P p;
   p.begin(wt, g, col0, row0, k0, k1, 0, lds);
   p.tile();
@@ -548,7 +556,7 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
     for (int a = 0; a < TA; ++a)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int64_t c = col0 + P::a0() + a * 32 + P::row_of(4 * q);
+        const int64_t c = col0 + P::a0() + P::own_row() + a * 32 + P::row_of(4 * q);
         if (c >= width) continue;
         float* at = to + (row0 + P::b0() + j * 32 + (lane_id() & 31)) * width + c;
         f32x16& x = p.acc[a][j];
@@ -576,7 +584,7 @@ __global__ __launch_bounds__(kBlock) void k_xent_dh_out(const float* __restrict_
 template <int T, int WA, int WB, int TA, int TB>
 __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1))) void k_xent_dw(Operand ht, Operand gt, int64_t k, int64_t vocab, int64_t v_first, int32_t dim,
                                                             uint32_t tiles_a, const float* __restrict__ unlift, char* __restrict__ out) {
-  typedef Product<T, WA, WB, TA, TB, true, true> P;
+  typedef Product<T, WA, WB, TA, TB, true, true, kNarrow> P;
   extern __shared__ char lds[];
   const int64_t col0 = (int64_t)(blockIdx.x % tiles_a) * P::kRowsA, piece0 = (int64_t)(blockIdx.x / tiles_a) * P::kRowsB;
   P p;
@@ -592,7 +600,7 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
     for (int a = 0; a < TA; ++a)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int64_t c = col0 + P::a0() + a * 32 + P::row_of(4 * q);
+        const int64_t c = col0 + P::a0() + P::own_row() + a * 32 + P::row_of(4 * q);
         float f[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) f[e] = p.acc[a][j][4 * q + e] * u;
@@ -621,6 +629,7 @@ __global__ __launch_bounds__(kBlock) void k_xent_pad(const char* __restrict__ in
 
 // ---- the workspace ---------------------------------------------------------------------------------------------------------
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;  // of G
+constexpr int64_t kMaxVocab = 0x7FFFF000;            // (a tile's row numbers stay below 2^31)
 constexpr int kTile = 256;                            // rows of a block's tile, either way
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
@@ -649,7 +658,7 @@ struct XentPlan {
     pieces = (vocab + piece - 1) / piece;
     const int64_t dh_tiles = rows / kTile * ((width + kTile - 1) / kTile);
     int64_t ds = 256 / dh_tiles;
-    const int64_t first = piece < vocab ? piece : vocab, stages = (first * es + kStageBytes - 1) / kStageBytes;
+    const int64_t first = piece < vocab ? piece : vocab, stages = (first * es + kWide - 1) / kWide;
     ds = ds < 1 ? 1 : ds > 16 ? 16 : ds;
     dh_splits = (int)(ds < stages ? ds : stages);
     size_t at = 0;
@@ -683,7 +692,7 @@ bool xent_aligned(const void* hidden, const void* weight) { return (((uintptr_t)
 
 int xent_check(const void* hidden, int64_t n, const void* weight, int64_t vocab, int32_t dim, int dtype, const int32_t* targets) {
   if (!known_dtype(dtype)) return COOP_E_ARG;
-  if (n < 0 || n >= ((int64_t)1 << 24) || vocab < 1 || vocab >= ((int64_t)1 << 31) || dim < 1 || dim > (1 << 18)) return COOP_E_ARG;
+  if (n < 0 || n >= ((int64_t)1 << 24) || vocab < 1 || vocab > kMaxVocab || dim < 1 || dim > (1 << 18)) return COOP_E_ARG;
   if (n > 0 && (!hidden || !weight || !targets)) return COOP_E_NULL;
   if (!aligned_for(hidden, dtype) || !aligned_for(weight, dtype)) return COOP_E_ARG;
   return COOP_OK;
@@ -691,7 +700,7 @@ int xent_check(const void* hidden, int64_t n, const void* weight, int64_t vocab,
 
 template <int T, int WA, int WB, int TA, int TB>
 bool launch_stats(const XentPlan& p, Operand w, Operand h, float alpha, const int32_t* targets, RowStat* part, hipStream_t s) {
-  typedef Product<T, WA, WB, TA, TB, false, false> P;
+  typedef Product<T, WA, WB, TA, TB, false, false, kWide> P;
   constexpr int lds = P::kLds > WA * P::kRowsB * (int)sizeof(RowStat) ? P::kLds : WA * P::kRowsB * (int)sizeof(RowStat);
   const auto kernel = k_xent_stats<T, WA, WB, TA, TB>;
   if (!allow_lds(kernel, lds)) return false;
@@ -736,7 +745,7 @@ int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t 
               alpha, T == COOP_F16 ? 8192.f : 1.f, p.n, p.rows, p.vocab, term, unlift, bad);
   const int64_t g_ld = p.g_ld;
   const Operand w{(const char*)weight, p.ld, p.vocab, p.ld}, h{(const char*)hidden, p.ld, p.n, p.ld};
-  typedef Product<T, 2, 2, 4, 4, false, false> P;
+  typedef Product<T, 2, 2, 4, 4, false, false, kWide> P;
   const auto kg = k_xent_g<T, 2, 2, 4, 4>;
   const auto kh = k_xent_dh<T, 2, 2, 4, 4>;
   const auto kw = k_xent_dw<T, 2, 2, 4, 4>;
@@ -750,7 +759,7 @@ int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t 
     if (dhidden != nullptr) {
       const Operand wt{(const char*)weight + v * p.ld, p.ld, p.ld, len}, gi{g, g_ld, p.rows, (int64_t)tiles * kTile * kElem<T>};
       // (every split has something to do: the last piece may be too short for all of them, and then adds nothing to the others' sums)
-      const int64_t stages = (len + kStageK<T> - 1) / kStageK<T>;
+      const int64_t stages = (len + P::kK - 1) / P::kK;
       const int splits = (int)(p.dh_splits < stages ? p.dh_splits : stages);
       COOP_LAUNCH(K_XENT_DH, kh, dim3(row_tiles * col_tiles * splits), dim3(P::kThreads), P::kLds, s, wt, gi, len, splits, col_tiles, row_tiles,
                   v != 0, sums, p.width);
