@@ -60,8 +60,8 @@ enum KernelId {
   K_XENT_TERMS,      // ... gradient: what a row's part of it needs
   K_XENT_G,          // ... the logits' gradient for a piece of the vocabulary
   K_XENT_DH,         // ... its product with the weight
-  K_XENT_DH_OUT,     // ... summed and rounded
   K_XENT_DW,         // ... its product with the hidden states
+  K_XENT_OUT,        // ... sums of a product's parts, rounded
   K_COUNT_
 };
 

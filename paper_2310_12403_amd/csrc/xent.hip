@@ -6,315 +6,24 @@
 // Forward: one product, whose tiles stay in registers and leave as a running maximum and sum per row.  Backward: the logits again, a
 // piece of the vocabulary at a time, left as G of that piece in 16 bits (32 for fp32), and the two products with it.
 //
-// The products run on the matrix units from tiles in LDS.  All three are the same kernel: C = A B^T over a common dimension k, where an
-// operand either has k as its contiguous dimension (rows of 128 bytes of k per stage) or as its row number (then its fragments are
-// transposed on the way from LDS to the registers).  The columns of C lie on the lanes and its rows in a lane's registers, so C is
-// computed as vocabulary x hidden for the logits: a lane then holds many logits of one row of H, and neither maximum, sum nor target
+// The logits are computed as vocabulary x hidden: a lane then holds many logits of one row of H, and neither maximum, sum nor target
 // takes another lane until the end.
+//
+// Rows of up to 128 elements of 16 bits (narrow) go another way: there the exponentials weigh as much as the products, and G would be
+// written and read for little arithmetic.  A wave keeps 64 rows of one operand in its registers as fragments, the other operand streams
+// through LDS, and G never leaves the registers: the 32 x 32 tile of logits that a product leaves is, rounded and packed, a fragment of
+// the next product, if that takes its k in the order in which the first one left its rows.
 #include <type_traits>
 
 #include "coop_internal.h"
-#include "elements.h"
+#include "products.h"
 
 namespace coop {
 namespace {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) char LdsByte;
-
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
-// Bytes of k per row and stage: 64 (32 elements of 16 bits, 16 of 32), four stages in LDS, or 128, two of them.  One is read, the others
-// are on their way.  Rows of 64 bytes are half a cache line, so operands with k contiguous take 128.
-constexpr int kWide = 128, kNarrow = 64;
 constexpr float kNoMax = -3.402823466e38f;
 
-template <int T> constexpr int kElem = T == COOP_F32 ? 4 : 2;
-
-// One 16-byte fragment of each operand into a 32 x 32 tile of C: 16 of k in 16 bits, 8 in 32.
-template <int T>
-__device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
-  if constexpr (T == COOP_F16) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-  } else if constexpr (T == COOP_BF16) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
-    return c;
-  }
-}
-
-// An operand in memory: rows of `ld` bytes (a multiple of 16, as is the base).  k contiguous: `rows` rows, `k` bytes of each are there.
-// k strided: `k` rows (one for each k), `rows` bytes of each are there.
-struct Operand {
-  const char* base;
-  int64_t ld, rows, k;
-};
-
-// How a stage of R rows of an operand lies in LDS, in 16-byte slots filled in order by the loads, 64 to a wave's load.
-//   k contiguous: a row's 4 or 8 chunks, exchanged by the row's number so that what 8 or 16 lanes read together lies in different banks;
-//   k strided: a row of k holds R elements; its chunks are exchanged by k so that what one fragment reads lies in different banks.
-// Both exchanges are an exclusive or with bits that neither the next tile of 32 rows nor the next step of k changes.
-template <int T, int R, bool STRIDED, int SIZE, int WAVES>
-struct Staged {
-  static constexpr int kBytes = R * SIZE, kK = SIZE / kElem<T>;
-  static constexpr int kChunks = STRIDED ? R * kElem<T> / 16 : SIZE / 16;  // of a row
-  static constexpr int kAll = kBytes / 1024;                                      // loads of a stage
-  static_assert(kAll % WAVES == 0 || kAll < WAVES, "loads are dealt to the waves evenly, or the first ones have one");
-  static constexpr int kLoads = kAll / WAVES;  // that every wave has
-  static __device__ __forceinline__ int swizzle(int row) {
-    if constexpr (!STRIDED) return SIZE == 128 ? (row & 7) ^ (row >> 3 & 1) : (row >> 1 & 3) ^ (row >> 3 & 1);
-    else if constexpr (T == COOP_F32) return (row >> 2 & 1) << 3 & (kChunks - 1);
-    else return (((row & 3) | (row >> 3 & 1) << 2) << 2) & (kChunks - 1);
-  }
-  // A stage that is to be loaded: where it begins in memory, how many of the memory layout's rows there are, and bytes in each.
-  struct Place {
-    const char* p;
-    int there, in_row;
-    __device__ __forceinline__ Place() {}
-    __device__ __forceinline__ Place(const Operand& op, int64_t row0, int64_t k0) {
-      const int64_t most = 0x7FFFFFFF, rows = STRIDED ? op.k - k0 : op.rows - row0, bytes = STRIDED ? op.rows - row0 * kElem<T> : op.k - k0 * kElem<T>;
-      p = op.base + (STRIDED ? k0 * op.ld + row0 * kElem<T> : row0 * op.ld + k0 * kElem<T>);
-      there = (int)(rows < 0 ? 0 : rows < most ? rows : most);
-      in_row = (int)(bytes < 0 ? 0 : bytes < most ? bytes : most);
-    }
-    __device__ __forceinline__ void next(int ld) {
-      if constexpr (STRIDED) p += (int64_t)ld * kK, there -= kK;
-      else p += SIZE, in_row -= SIZE;
-    }
-  };
-  // What a lane loads of every stage: offsets from the stage's beginning.  What is not there reads as zero: rows because they lie behind
-  // the last record; chunks behind a row's end because their offsets are put there, with k strided once and for all.
-  struct Loads {
-    static constexpr int kMine = (kAll + WAVES - 1) / WAVES, kNowhere = 0x3FFFFFFF;
-    int ld, chunk, at[kMine];
-    __device__ __forceinline__ void begin(const Operand& op, const Place& first) {
-      const int wave = uniform_wave_in_block(), lane = lane_id();
-      ld = (int)op.ld;
-#pragma unroll
-      for (int i = 0; i < kMine; ++i) {
-        const int slot = (i * WAVES + wave) * kWave + lane, row = slot / kChunks;
-        chunk = ((slot % kChunks) ^ swizzle(row)) * 16;  // (k contiguous: the same for all of a lane's loads)
-        at[i] = row * ld + chunk;
-        if (STRIDED && chunk >= first.in_row) at[i] = kNowhere;
-      }
-    }
-    // what the loads of a stage have in common
-    struct Stage {
-      __amdgpu_buffer_rsrc_t rsrc;
-      int off;
-    };
-    __device__ __forceinline__ Stage stage(const Place& s) const {
-      constexpr int kRows = STRIDED ? kK : R;
-      const int rows = s.there < kRows ? s.there : kRows, in_row = s.in_row < ld ? s.in_row : ld, last = (rows - 1) * ld + in_row;
-      const int records = (rows < in_row ? rows : in_row) > 0 ? last : 0;
-      return Stage{__builtin_amdgcn_make_buffer_rsrc((void*)s.p, 0, records, 0x00020000), !STRIDED && chunk >= s.in_row ? kNowhere : 0};
-    }
-    __device__ __forceinline__ void start(const Stage& s, char* lds, int i) const {
-      const int l = i * WAVES + uniform_wave_in_block();
-      if (kAll < WAVES && l >= kAll) return;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(s.rsrc, (__attribute__((address_space(3))) void*)(LdsByte*)(lds + l * 1024), 16,
-                                               STRIDED ? at[i] : at[i] + s.off, 0, 0, 0);
-    }
-  };
-  // the fragment of rows row .. row + 31 at step kk of the stage
-  static __device__ __forceinline__ u32x4 fragment(const char* lds, int row, int kk) {
-    const int lane = lane_id();
-    if constexpr (!STRIDED) {
-      const int r = row + (lane & 31), chunk = kk * 2 + (lane >> 5);
-      return *reinterpret_cast<const u32x4*>(lds + r * SIZE + ((chunk ^ swizzle(r)) << 4));
-    } else if constexpr (T == COOP_F32) {
-      const int m = row + (lane & 31);
-      u32x4 f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int k = kk * 8 + (lane >> 5) * 4 + j;
-        f[j] = *reinterpret_cast<const uint32_t*>(lds + k * (R * 4) + (((m >> 2) ^ swizzle(k)) << 4) + (m & 3) * 4);
-      }
-      return f;
-    } else {
-      // 16 lanes read 4 rows of k by 16 elements and get an element's 4 k each
-      const int b = lane >> 4, t = lane & 15;
-      u32x4 f;
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const int k = kk * 16 + (b >> 1) * 8 + q * 4 + (t >> 2), m = row + (b & 1) * 16 + (t & 3) * 4;
-        const char* at = lds + k * (R * 2) + (((m >> 3) ^ swizzle(k)) << 4) + (m & 7) * 2;
-        const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(LdsByte*)at);
-        const u32x2 y = __builtin_bit_cast(u32x2, x);
-        f[2 * q] = y[0];
-        f[2 * q + 1] = y[1];
-      }
-      return f;
-    }
-  }
-};
-
-// A block's tile of C: WA x WB waves with TA x TB tiles of 32 x 32 each, rows of A by rows of B.  The stages of all of a block's tiles
-// are one stream: while one is multiplied the next kStages - 1 are on their way, the first of the next tile among them.
-template <int T, int WA, int WB, int TA, int TB, bool SA, bool SB, int SIZE>
-struct Product {
-  static constexpr int kWaves = WA * WB, kThreads = kWaves * kWave;
-  static constexpr int kRowsA = WA * TA * 32, kRowsB = WB * TB * 32;
-  static constexpr int kK = SIZE / kElem<T>, kSteps = SIZE / 32, kStages = 256 / SIZE;
-  typedef Staged<T, kRowsA, SA, SIZE, kWaves> A;
-  typedef Staged<T, kRowsB, SB, SIZE, kWaves> B;
-  static constexpr int kStage = A::kBytes + B::kBytes, kLds = kStages * kStage;
-  f32x16 acc[TA][TB];
-  u32x4 fa[TA], fb[TB];  // the last step of the last stage that was read
-  typename A::Loads loads_a;
-  typename B::Loads loads_b;
-  typename A::Place a, next_a;  // the stage that is loaded next, and the first one of the tile behind its
-  typename B::Place b, next_b;
-  typename A::Loads::Stage sa;
-  typename B::Loads::Stage sb;
-  int left;                     // stages of its tile that are to be loaded
-  int slot;                     // where in LDS it goes; the one behind it is read next
-  int stages;
-  int step_rows;                // from tile to tile, of A; 0: there is one tile
-  int64_t step_bytes;
-  char* lds;
-
-  __device__ __forceinline__ static int a0() { return uniform_wave_in_block() / WB * (TA * 32); }
-  __device__ __forceinline__ static int b0() { return uniform_wave_in_block() % WB * (TB * 32); }
-  // C's element j of a 32 x 32 tile: its row is the lane's own plus one that all lanes have; its column is lane & 31
-  __device__ __forceinline__ static int own_row() { return (lane_id() >> 5) * 4; }
-  __device__ __forceinline__ static constexpr int row_of(int j) { return (j >> 2) * 8 + (j & 3); }
-
-  // to the next stage of the stream
-  __device__ __forceinline__ void next() {
-    a.next(loads_a.ld);
-    b.next(loads_b.ld);
-    --left;
-    const bool done = left == 0;  // (chosen, not branched around: the products go on meanwhile)
-    left = done ? stages : left;
-    a.p = done ? next_a.p : a.p;
-    a.there = done ? next_a.there : a.there;
-    a.in_row = done ? next_a.in_row : a.in_row;
-    b.p = done ? next_b.p : b.p;
-    b.there = done ? next_b.there : b.there;
-    b.in_row = done ? next_b.in_row : b.in_row;
-    next_a.p += done ? step_bytes : 0;
-    next_a.there -= done ? step_rows : 0;
-    sa = loads_a.stage(a);
-    sb = loads_b.stage(b);
-  }
-  // Of this wave's loads, those of the stage that is read next have arrived (only younger ones are left: loads arrive in the order in
-  // which they were sent), and its reads are done; then the waves meet.  (A barrier alone does not wait for loads into LDS.)
-  static __device__ __forceinline__ void meet() {
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * (A::kLoads + B::kLoads)) : "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-  }
-  __device__ __forceinline__ void multiply(const u32x4 (&x)[TA], const u32x4 (&y)[TB]) {
-#pragma unroll
-    for (int i = 0; i < TA; ++i)
-#pragma unroll
-      for (int j = 0; j < TB; ++j) acc[i][j] = mma<T>(x[i], y[j], acc[i][j]);
-  }
-  static constexpr int kMine = A::Loads::kMine + B::Loads::kMine;
-  __device__ __forceinline__ void start(char* into, int i) const {
-    if (i < A::Loads::kMine) loads_a.start(sa, into, i);
-    else if (i < kMine) loads_b.start(sb, into + A::kBytes, i - A::Loads::kMine);
-  }
-  // A step's products, x times y, and between them, one after each of the first products, the reads of the next step (kk of the
-  // stage in `from`) and, with LOADS, the loads of the stage that comes: a wave has its SIMD to itself, so nothing is hidden but by
-  // its own products, and the order is held as it stands here.
-  template <bool PRODUCTS, bool LOADS>
-  __device__ __forceinline__ void step(const u32x4 (&x)[TA], const u32x4 (&y)[TB], const char* from, int kk, u32x4 (&na)[TA], u32x4 (&nb)[TB],
-                                       char* into) {
-    constexpr int kMmas = TA * TB, kReads = TA + TB, kEarly = kMmas >= 2 ? kMmas / 2 : 1, kEach = (kReads + kEarly - 1) / kEarly;
-    constexpr int kLoadEach = (kMine + kMmas - 1) / kMmas;
-#pragma unroll
-    for (int q = 0; q < kMmas; ++q) {
-#pragma unroll
-      for (int r = q * kEach; r < (q + 1) * kEach && r < kReads; ++r) {  // (the first of A, all of B, the others of A: as they are needed)
-        if (r >= 1 && r <= TB) nb[r - 1] = B::fragment(from + A::kBytes, b0() + (r - 1) * 32, kk);
-        else na[r == 0 ? 0 : r - TB] = A::fragment(from, a0() + (r == 0 ? 0 : r - TB) * 32, kk);
-      }
-      if constexpr (LOADS) {
-#pragma unroll
-        for (int i = q * kLoadEach; i < (q + 1) * kLoadEach && i < kMine; ++i) start(into, i);
-      }
-      if constexpr (PRODUCTS) {
-        acc[q / TB][q % TB] = mma<T>(x[q / TB], y[q % TB], acc[q / TB][q % TB]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-  }
-  // Reads the stage in `from`, each step while the one before it is multiplied; `into`, which held the stage before, gets a new one.
-  // (The two are never the same memory, and the compiler is told so: no read waits for the loads that are started here.)
-  template <bool FIRST>
-  __device__ __forceinline__ void stage(char* __restrict__ into, const char* __restrict__ from) {
-    u32x4 na[TA], nb[TB];
-    step<!FIRST, true>(fa, fb, from, 0, na, nb, into);
-    next();
-    step<true, false>(na, nb, from, 1, fa, fb, into);
-#pragma unroll
-    for (int kk = 2; kk < kSteps; kk += 2) {
-      step<true, false>(fa, fb, from, kk, na, nb, into);
-      step<true, false>(na, nb, from, kk + 1, fa, fb, into);
-    }
-  }
-
-  // the first tile is at rows row_a, row_b; k from k0 to k1 (k1 > k0)
-  __device__ __forceinline__ void begin(const Operand& op_a, const Operand& op_b, int64_t row_a, int64_t row_b, int64_t k0, int64_t k1, int step,
-                                        char* lds_) {
-    lds = lds_;
-    step_rows = step;
-    step_bytes = step * op_a.ld;
-    left = stages = (int)((k1 - k0 + kK - 1) / kK);
-    a = typename A::Place(op_a, row_a, k0);
-    b = typename B::Place(op_b, row_b, k0);
-    loads_a.begin(op_a, a);
-    loads_b.begin(op_b, b);
-    next_a = a;
-    next_b = b;
-    next_a.p += step_bytes;
-    next_a.there -= step;
-    if (step == 0) next_a.there = next_b.there = 0;  // (behind the only tile there is nothing to load)
-    slot = kStages - 1;
-    sa = loads_a.stage(a);
-    sb = loads_b.stage(b);
-#pragma unroll
-    for (int s = 0; s < kStages - 1; ++s) {
-#pragma unroll
-      for (int i = 0; i < kMine; ++i) start(lds + s * kStage, i);
-      next();
-    }
-  }
-  // the next tile's product
-  __device__ __forceinline__ void tile() {
-#pragma unroll
-    for (int i = 0; i < TA; ++i)
-#pragma unroll
-      for (int j = 0; j < TB; ++j)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-    int from = slot + 1 < kStages ? slot + 1 : 0;
-    meet();
-    stage<true>(lds + slot * kStage, lds + from * kStage);
-    slot = from;
-    for (int s = 1; s < stages; ++s) {
-      from = slot + 1 < kStages ? slot + 1 : 0;
-      meet();
-      stage<false>(lds + slot * kStage, lds + from * kStage);
-      slot = from;
-    }
-    multiply(fa, fb);
-  }
-  // LDS is free for other use: what is on its way has arrived, and all waves have read.  A block does not end without it.
-  static __device__ __forceinline__ void end() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __syncthreads();
-  }
-};
 
 // ---- forward -------------------------------------------------------------------------------------------------------------
 // A block has kRowsB rows of H and every `splits`-th tile of the vocabulary; it leaves the rows' maximum, sum and target logit (all
@@ -440,8 +149,9 @@ __global__ __launch_bounds__(kBlock) void k_xent_loss(const RowStat* __restrict_
 }
 
 // ---- backward ------------------------------------------------------------------------------------------------------------
-// What a row of G needs; target -1: the row has none, and G is zero there whatever its logits are.
-struct RowTerm { float coef, lse2; int32_t target; int32_t pad; };
+// What the rows of G need, all of them filled up to a multiple of a tile; target -1: the row has none, coef is 0, and its hidden state is
+// taken as zeros whatever it holds.
+struct RowTerms { float *coef, *lse2; int32_t* target; };
 
 // In 16 bits G holds coef over the largest |coef| (and times 2^13 in fp16, whose exponents would otherwise not reach from 1 to a
 // probability times dloss): where all rows count alike, as in a mean, the factor is 1 (a power of two), and so a target's p - 1 of a
@@ -449,7 +159,7 @@ struct RowTerm { float coef, lse2; int32_t target; int32_t pad; };
 template <bool LIFT>
 __global__ __launch_bounds__(1024) void k_xent_terms(const int32_t* __restrict__ targets, int32_t ignore, const float* __restrict__ lse,
                                                      const float* __restrict__ dloss, float alpha, float most, int64_t n, int64_t rows, int64_t vocab,
-                                                     RowTerm* __restrict__ term, float* __restrict__ unlift, int32_t* __restrict__ bad) {
+                                                     RowTerms term, float* __restrict__ unlift, int32_t* __restrict__ bad) {
   __shared__ float lds[16];
   float top = 0.f;
   if constexpr (LIFT) {  // (every block looks at all rows: no second launch, and n floats are little)
@@ -470,14 +180,21 @@ __global__ __launch_bounds__(1024) void k_xent_terms(const int32_t* __restrict__
   if (blockIdx.x == 0 && threadIdx.x == 0) *unlift = LIFT ? top / most : 1.f;
   const int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x;
   if (i >= rows) return;
-  RowTerm r{0.f, 0.f, -1, 0};
+  float coef = 0.f, lse2 = 0.f;
+  int32_t target = -1;
   if (i < n) {
     const int32_t t = targets[i];
-    const bool ok = t != ignore && (uint64_t)(int64_t)t < (uint64_t)vocab;
-    if (ok) r = RowTerm{LIFT ? alpha * dloss[i] / top * most : alpha * dloss[i], lse[i] * kLog2e, t, 0};
-    else if (t != ignore) atomicOr(bad, 1);
+    if (t != ignore && (uint64_t)(int64_t)t < (uint64_t)vocab) {
+      coef = LIFT ? alpha * dloss[i] / top * most : alpha * dloss[i];
+      lse2 = lse[i] * kLog2e;
+      target = t;
+    } else if (t != ignore) {
+      atomicOr(bad, 1);
+    }
   }
-  term[i] = r;
+  term.coef[i] = coef;
+  term.lse2[i] = lse2;
+  term.target[i] = target;
 }
 
 template <int T>
@@ -487,11 +204,24 @@ __device__ __forceinline__ void put4(char* p, const float (&f)[4]) {
   x.store(p);
 }
 
+// columns c .. c + 3 of a row of `dim`, those that there are
+template <int T>
+__device__ __forceinline__ void put_columns(char* out, int64_t row, int64_t c, int32_t dim, const float (&f)[4]) {
+  char* to = out + (row * dim + c) * kElem<T>;
+  if (c + 4 <= dim) {
+    put4<T>(to, f);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < dim) ((typename Element<T>::M*)to)[e] = (typename Element<T>::M)f[e];
+  }
+}
+
 // G of the piece of the vocabulary that begins at v_first, [rows of H, ld bytes]; all of G's tiles are there, beyond the vocabulary's
 // and the rows' end it is zero
 template <int T, int WA, int WB, int TA, int TB>
 __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1))) void k_xent_g(Operand w, Operand h, int64_t vocab, int64_t k, float scale2, int64_t v_first,
-                                                           uint32_t tiles_a, const RowTerm* __restrict__ term, char* __restrict__ g, int64_t ld) {
+                                                           uint32_t tiles_a, RowTerms term, char* __restrict__ g, int64_t ld) {
   typedef Product<T, WA, WB, TA, TB, false, false, kWide> P;
   extern __shared__ char lds[];
   const int64_t piece0 = (int64_t)(blockIdx.x % tiles_a) * P::kRowsA, row0 = (int64_t)(blockIdx.x / tiles_a) * P::kRowsB;
@@ -505,22 +235,22 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
   for (int j = 0; j < TB; ++j) {
     __builtin_amdgcn_sched_barrier(0);
     const int64_t i = row0 + P::b0() + j * 32 + (lane_id() & 31);
-    const RowTerm r = term[i];
-    const int mine = r.target - first;
-    const bool none = r.target < 0, hit = ballot64(!none && (uint32_t)mine < (uint32_t)(TA * 32)) != 0;
+    const float coef = term.coef[i], lse2 = term.lse2[i];
+    const int mine = term.target[i] - first;
+    const bool hit = ballot64(mine >= 0 && mine < TA * 32) != 0;
     char* to = g + i * ld + (piece0 + P::a0() + P::own_row()) * kElem<T>;
 #pragma unroll
     for (int a = 0; a < TA; ++a) {
       f32x16 x = p.acc[a][j];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale2, -r.lse2));
+      for (int e = 0; e < 16; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale2, -lse2));
       if (hit) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (!none && mine == a * 32 + P::row_of(e)) x[e] -= 1.f;
+          if (mine == a * 32 + P::row_of(e)) x[e] -= 1.f;
       }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = none ? 0.f : x[e] * r.coef;
+      for (int e = 0; e < 16; ++e) x[e] *= coef;
       if (ragged) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
@@ -567,16 +297,27 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
       }
 }
 
+// out[row, :] = the splits' sums of the row, times *unlift
 template <int T>
-__global__ __launch_bounds__(kBlock) void k_xent_dh_out(const float* __restrict__ sums, int splits, int64_t rows, int64_t width, int64_t n,
-                                                        int32_t dim, const float* __restrict__ unlift, char* __restrict__ out) {
+__global__ __launch_bounds__(kBlock) void k_xent_out(const float* __restrict__ sums, int splits, int64_t rows, int32_t width, int64_t n,
+                                                     int32_t dim, const float* __restrict__ unlift, char* __restrict__ out) {
   const int64_t step = (int64_t)gridDim.x * kBlock;
-  for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < n * dim; i += step) {
-    const int64_t row = i / dim;
-    const int32_t c = (int32_t)(i - row * dim);
-    float s = 0.f;
-    for (int q = 0; q < splits; ++q) s += sums[((int64_t)q * rows + row) * width + c];
-    ((typename Element<T>::M*)out)[i] = (typename Element<T>::M)(s * *unlift);
+  const int32_t packs = (dim + 3) / 4;
+  const float u = *unlift;
+  for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < n * packs; i += step) {
+    const int64_t row = i / packs;
+    const int32_t c = (int32_t)(i - row * packs) * 4;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int q = 0; q < splits; ++q) {
+      float f[4];
+      load_elements<COOP_F32, 4>(sums + ((int64_t)q * rows + row) * width + c, f);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += f[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] *= u;
+    put_columns<T>(out, row, c, dim, s);
   }
 }
 
@@ -604,26 +345,423 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
         float f[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) f[e] = p.acc[a][j][4 * q + e] * u;
-        if (c + 4 <= dim) {
-          put4<T>(out + (v * dim + c) * kElem<T>, f);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (c + e < dim) ((typename Element<T>::M*)out)[v * dim + c + e] = (typename Element<T>::M)f[e];
-        }
+        put_columns<T>(out, v, c, dim, f);
       }
   }
 }
 
-// rows of `dim` elements into rows of `ld` bytes, what is behind a row's end zero
+// ---- narrow: rows of up to 128 elements of 16 bits -----------------------------------------------------------------------------
+// A stage: 64 rows of 16 KS elements, in LDS as their chunks of 16 bytes, exchanged by the row's number: what 8 or 16 lanes read of one
+// chunk of successive rows lies in different banks, and so does what they read of four rows' same 16 elements (transposed).
+template <int T, int KS>
+struct RowStage {
+  static constexpr int kRows = 64, kRowBytes = KS * 32, kChunks = KS * 2, kBytes = kRows * kRowBytes, kMine = kBytes / 4096;
+  static __device__ __forceinline__ int swizzle(int row) {
+    const int r0 = row & 1, r1 = row >> 1 & 1, r2 = row >> 2 & 1, r3 = row >> 3 & 1;
+    return KS == 8 ? r2 | r0 << 1 | r1 << 2 | r3 << 3 : KS == 4 ? r2 | (r0 ^ r3) << 1 | r1 << 2 : r2 | (r1 ^ r3) << 1;
+  }
+  // rows block * 32 + .., elements kk * 16 + ..: a fragment with the elements as k
+  static __device__ __forceinline__ u32x4 fragment(const char* lds, int block, int kk) {
+    const int r = block * 32 + (lane_id() & 31), chunk = kk * 2 + (lane_id() >> 5);
+    return *reinterpret_cast<const u32x4*>(lds + r * kRowBytes + ((chunk ^ swizzle(r)) << 4));
+  }
+  // elements tile * 32 + .., with 16 of the block's rows as k, in the order in which a lane's registers hold the rows of a product
+  static __device__ __forceinline__ u32x4 transposed(const char* lds, int block, int tile, int s) {
+    const int lane = lane_id(), b = lane >> 4, t = lane & 15;
+    u32x4 f;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int r = block * 32 + s * 16 + q * 8 + (b >> 1) * 4 + (t >> 2), c = tile * 32 + (b & 1) * 16 + (t & 3) * 4;
+      const char* at = lds + r * kRowBytes + (((c >> 3) ^ swizzle(r)) << 4) + (c & 7) * 2;
+      const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(LdsByte*)at));
+      f[2 * q] = y[0];
+      f[2 * q + 1] = y[1];
+    }
+    return f;
+  }
+};
+
+// The stages of rows first, first + step, .. of an operand, four in LDS as in Product; with TERMS the rows' coef, lse2 and target go with
+// them.  Four waves.
+template <int T, int KS, bool TERMS>
+struct RowStream {
+  typedef RowStage<T, KS> S;
+  static constexpr int kStages = 4, kStage = S::kBytes + (TERMS ? 1024 : 0), kLds = kStages * kStage, kLoads = S::kMine + (TERMS ? 1 : 0);
+  const char* base;
+  int64_t next, step, end;
+  int ld, at[S::kMine];
+  const char* terms;
+  int slot;
+  char* lds;
+  __device__ __forceinline__ void start(char* __restrict__ into) {
+    const int64_t there = end - next;
+    const int rows = there < 0 ? 0 : there < S::kRows ? (int)there : S::kRows;
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(base + next * ld), 0, rows * ld, 0x00020000);
+    const int wave = uniform_wave_in_block();
+#pragma unroll
+    for (int i = 0; i < S::kMine; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(LdsByte*)(into + (i * 4 + wave) * 1024), 16, at[i], 0, 0, 0);
+    if constexpr (TERMS) {  // a wave has one of the three arrays (the last one the first again: all waves have as many loads)
+      const auto tr = __builtin_amdgcn_make_buffer_rsrc((void*)(terms + next * 4), 0, rows * 4, 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(tr, (__attribute__((address_space(3))) void*)(LdsByte*)(into + S::kBytes + (wave == 3 ? 0 : wave) * 256), 4,
+                                               lane_id() * 4, 0, 0, 0);
+    }
+    next += step;
+  }
+  __device__ __forceinline__ void begin(const Operand& op, int64_t first, int64_t step_, const RowTerms* t, char* lds_) {
+    base = op.base, ld = (int)op.ld, next = first, step = step_, end = op.rows, lds = lds_;
+    const int wave = uniform_wave_in_block();
+#pragma unroll
+    for (int i = 0; i < S::kMine; ++i) {
+      const int s = (i * 4 + wave) * kWave + lane_id(), row = s / S::kChunks, chunk = (s % S::kChunks) ^ S::swizzle(row);
+      at[i] = chunk * 16 < ld ? row * ld + chunk * 16 : 0x3FFFFFFF;
+    }
+    if constexpr (TERMS) terms = wave == 1 ? (const char*)t->coef : wave == 2 ? (const char*)t->target : (const char*)t->lse2;
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) start(lds + s * kStage);
+    slot = kStages - 1;
+  }
+  static __device__ __forceinline__ void meet() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * kLoads) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  // f(stage) for the next stage, while another one is loaded into the place of the one before it
+  template <typename F>
+  __device__ __forceinline__ void stage(F&& f) {
+    const int from = slot + 1 < kStages ? slot + 1 : 0;
+    meet();
+    both(lds + slot * kStage, lds + from * kStage, f);
+    slot = from;
+  }
+  template <typename F>
+  __device__ __forceinline__ void both(char* __restrict__ into, const char* __restrict__ from, F&& f) {
+    start(into);
+    f(from);
+  }
+};
+
+// the fragments of 64 rows of an operand that a wave keeps: rows row0 + j * 32 + ..
+template <int KS>
+__device__ __forceinline__ void keep_rows(const Operand& op, int64_t row0, u32x4 (&x)[2][KS]) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+      const int64_t row = row0 + j * 32 + (lane_id() & 31);
+      const int at = kk * 32 + (lane_id() >> 5) * 16;
+      x[j][kk] = row < op.rows && at < op.ld ? *reinterpret_cast<const u32x4*>(op.base + row * op.ld + at) : u32x4{0, 0, 0, 0};
+    }
+}
+__device__ __forceinline__ constexpr int row_of(int e) { return (e >> 2) * 8 + (e & 3); }  // (as in Product)
+__device__ __forceinline__ int own_row() { return (lane_id() >> 5) * 4; }
+
+// 16 values as two fragments: elements 0 .. 7 and 8 .. 15
 template <int T>
-__global__ __launch_bounds__(kBlock) void k_xent_pad(const char* __restrict__ in, int64_t rows, int32_t dim, char* __restrict__ out, int32_t width) {
+__device__ __forceinline__ void pack(const f32x16& x, u32x4 (&f)[2]) {
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    Pack<T, 8> p;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p.x[e] = (typename Element<T>::M)x[s * 8 + e];
+    f[s] = __builtin_bit_cast(u32x4, p);
+  }
+}
+
+// Forward: as k_xent_stats; a block has 256 rows of H, a wave 64 of them, and every splits-th stage of 64 rows of W.
+template <int T, int KS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_xent_stats_narrow(
+    Operand w, Operand h, int64_t n, int64_t vocab, float scale2, const int32_t* __restrict__ targets, int splits, RowStat* __restrict__ part) {
+  typedef RowStream<T, KS, false> Stream;
+  typedef typename Stream::S S;
+  extern __shared__ char lds[];
+  const int split = blockIdx.x % splits;
+  const int64_t row0 = (int64_t)(blockIdx.x / splits) * 256 + uniform_wave_in_block() * 64;
+  u32x4 hf[2][KS];
+  keep_rows<KS>(h, row0, hf);
+  float top[2], sum[2], target[2];
+  int32_t t[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int64_t i = row0 + j * 32 + (lane_id() & 31);
+    t[j] = i < n ? targets[i] : -1;
+    top[j] = kNoMax;
+    sum[j] = target[j] = 0.f;
+  }
+  Stream stream;
+  stream.begin(w, (int64_t)split * S::kRows, (int64_t)splits * S::kRows, nullptr, lds);
+  for (int64_t v0 = (int64_t)split * S::kRows; v0 < vocab; v0 += (int64_t)splits * S::kRows) {
+    f32x16 z[2][2];
+    stream.stage([&](const char* from) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z[b][0][e] = z[b][1][e] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) {
+          const u32x4 a = S::fragment(from, b, kk);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) z[b][j] = mma<T>(a, hf[j][kk], z[b][j]);
+        }
+      }
+    });
+    const int first = (int)v0 + own_row(), left = (int)vocab - first;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int mine = t[j] - first;
+      if (ballot64((uint32_t)mine < 64u) != 0) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (mine == b * 32 + row_of(e)) target[j] = z[b][j][e] * scale2;
+      }
+      if (v0 + S::kRows > vocab) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (b * 32 + row_of(e) >= left) z[b][j][e] = scale2 < 0.f ? __builtin_inff() : -__builtin_inff();
+      }
+      float m = z[0][j][0];
+      if (scale2 < 0.f) {
+#pragma unroll
+        for (int e = 1; e < 32; ++e) m = fminf(m, z[e >> 4][j][e & 15]);
+      } else {
+#pragma unroll
+        for (int e = 1; e < 32; ++e) m = fmaxf(m, z[e >> 4][j][e & 15]);
+      }
+      m = fmaxf(top[j], m * scale2);
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < 32; ++e) s[e & 3] += __builtin_amdgcn_exp2f(__builtin_fmaf(z[e >> 4][j][e & 15], scale2, -m));
+      sum[j] = sum[j] * __builtin_amdgcn_exp2f(top[j] - m) + ((s[0] + s[1]) + (s[2] + s[3]));
+      top[j] = m;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {  // lanes l and l + 32 have the same row
+    const float m = fmaxf(top[j], __shfl_xor(top[j], 32, kWave));
+    float s = sum[j] * __builtin_amdgcn_exp2f(top[j] - m);
+    s += __shfl_xor(s, 32, kWave);
+    const float tt = target[j] + __shfl_xor(target[j], 32, kWave);
+    const int64_t i = row0 + j * 32 + lane_id();
+    if (lane_id() < 32 && i < n) part[(int64_t)split * n + i] = RowStat{m, s, tt, 0.f};
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (no load into LDS is left when the block ends)
+}
+
+// dH: sums[split][row][width] = the split's part of G W; rows, splits and stages as in the forward kernel
+template <int T, int KS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_xent_dh_narrow(
+    Operand w, Operand h, int64_t rows, int64_t vocab, float scale2, RowTerms term, int splits, float* __restrict__ sums, int32_t width) {
+  typedef RowStream<T, KS, false> Stream;
+  typedef typename Stream::S S;
+  extern __shared__ char lds[];
+  const int split = blockIdx.x % splits;
+  const int64_t row0 = (int64_t)(blockIdx.x / splits) * 256 + uniform_wave_in_block() * 64;
+  u32x4 hf[2][KS];
+  keep_rows<KS>(h, row0, hf);
+  float coef[2], lse2[2];
+  int32_t t[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int64_t i = row0 + j * 32 + (lane_id() & 31);
+    coef[j] = term.coef[i], lse2[j] = term.lse2[i], t[j] = term.target[i];
+  }
+  f32x16 acc[KS / 2][2];
+#pragma unroll
+  for (int c = 0; c < KS / 2; ++c)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[c][0][e] = acc[c][1][e] = 0.f;
+  Stream stream;
+  stream.begin(w, (int64_t)split * S::kRows, (int64_t)splits * S::kRows, nullptr, lds);
+  for (int64_t v0 = (int64_t)split * S::kRows; v0 < vocab; v0 += (int64_t)splits * S::kRows) {
+    const int first = (int)v0 + own_row(), left = (int)vocab - first;
+    const bool ragged = v0 + S::kRows > vocab;
+    stream.stage([&](const char* from) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        f32x16 z[2];
+        u32x4 p[2][2];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z[0][e] = z[1][e] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) {
+          const u32x4 a = S::fragment(from, b, kk);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) z[j] = mma<T>(a, hf[j][kk], z[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) z[j][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][e], scale2, -lse2[j]));
+          const int mine = t[j] - first - b * 32;
+          if (ballot64((uint32_t)mine < 32u) != 0) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (mine == row_of(e)) z[j][e] -= 1.f;
+          }
+#pragma unroll
+          for (int e = 0; e < 16; ++e) z[j][e] *= coef[j];
+          if (ragged) {  // (rows of W that are not there are zeros in the next product, but an exponential may be infinite)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (b * 32 + row_of(e) >= left) z[j][e] = 0.f;
+          }
+          pack<T>(z[j], p[j]);
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int c = 0; c < KS / 2; ++c) {
+            const u32x4 a = S::transposed(from, b, c, s);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[c][j] = mma<T>(a, p[j][s], acc[c][j]);
+          }
+      }
+    });
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    float* to = sums + ((int64_t)split * rows + row0 + j * 32 + (lane_id() & 31)) * width;
+#pragma unroll
+    for (int c = 0; c < KS / 2; ++c)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int col = c * 32 + row_of(4 * q) + own_row();
+        const float f[4] = {acc[c][j][4 * q], acc[c][j][4 * q + 1], acc[c][j][4 * q + 2], acc[c][j][4 * q + 3]};
+        if (col < width) put4<COOP_F32>((char*)(to + col), f);
+      }
+  }
+}
+
+// dW: a block has 256 rows of W, a wave 64 of them, and every splits-th stage of 64 rows of H with their terms; to out, or, split, to
+// sums[split][row][width].
+template <int T, int KS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_xent_dw_narrow(
+    Operand w, Operand h, int64_t vocab, float scale2, RowTerms term, int splits, const float* __restrict__ unlift, int32_t dim,
+    char* __restrict__ out, float* __restrict__ sums, int64_t rows, int32_t width) {
+  typedef RowStream<T, KS, true> Stream;
+  typedef typename Stream::S S;
+  extern __shared__ char lds[];
+  const int split = blockIdx.x % splits, lane = lane_id();
+  const int64_t v0 = (int64_t)(blockIdx.x / splits) * 256 + uniform_wave_in_block() * 64;
+  u32x4 wf[2][KS];
+  keep_rows<KS>(w, v0, wf);
+  f32x16 acc[KS / 2][2];
+#pragma unroll
+  for (int c = 0; c < KS / 2; ++c)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[c][0][e] = acc[c][1][e] = 0.f;
+  Stream stream;
+  stream.begin(h, (int64_t)split * S::kRows, (int64_t)splits * S::kRows, &term, lds);
+  for (int64_t i0 = (int64_t)split * S::kRows; i0 < h.rows; i0 += (int64_t)splits * S::kRows) {
+    stream.stage([&](const char* from) {
+      const float* lse2 = reinterpret_cast<const float*>(from + S::kBytes);
+      const float* coef = lse2 + 64;
+      const int hit = reinterpret_cast<const int32_t*>(coef + 64)[lane] - (int)v0;  // of row `lane` of the stage
+      const uint64_t hits = ballot64((uint32_t)hit < 64u);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        f32x16 z[2];
+        u32x4 p[2][2];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z[0][e] = z[1][e] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) {
+          const u32x4 a = S::fragment(from, b, kk);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) z[j] = mma<T>(a, wf[j][kk], z[j]);
+        }
+        f32x16 c4;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int at = b * 32 + row_of(4 * q) + own_row();
+          float l[4], c[4];
+          load_elements<COOP_F32, 4>(lse2 + at, l);
+          load_elements<COOP_F32, 4>(coef + at, c);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            c4[4 * q + e] = c[e];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) z[j][4 * q + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][4 * q + e], scale2, -l[e]));
+          }
+        }
+        // a row whose target is among the wave's: its 1 goes off where the target's column and the row meet
+        for (uint32_t todo = (uint32_t)(hits >> (b * 32)); todo != 0; todo &= todo - 1) {
+          const int r = __builtin_ctz(todo), v = __builtin_amdgcn_readlane(hit, b * 32 + r);
+          const bool here = lane == (v & 31) + (r >> 2 & 1) * 32;
+          const int at = (r >> 3) * 4 + (r & 3);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float one = e == at && here ? 1.f : 0.f;
+            z[0][e] -= v < 32 ? one : 0.f;
+            z[1][e] -= v < 32 ? 0.f : one;
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) z[j][e] *= c4[e];
+          pack<T>(z[j], p[j]);
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int c = 0; c < KS / 2; ++c) {
+            const u32x4 a = S::transposed(from, b, c, s);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[c][j] = mma<T>(a, p[j][s], acc[c][j]);
+          }
+      }
+    });
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  const float u = sums != nullptr ? 1.f : *unlift;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int64_t v = v0 + j * 32 + (lane & 31);
+    if (v >= vocab) continue;
+#pragma unroll
+    for (int c = 0; c < KS / 2; ++c)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int col = c * 32 + row_of(4 * q) + own_row();
+        float f[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = acc[c][j][4 * q + e] * u;
+        if (sums == nullptr) put_columns<T>(out, v, col, dim, f);
+        else if (col < width) put4<COOP_F32>((char*)(sums + ((int64_t)split * rows + v) * width + col), f);
+      }
+  }
+}
+
+// rows of `dim` elements into `rows` rows of `width`, zeros behind a row's end, behind the last of n rows, and in rows whose target is
+// negative (null: all have one)
+template <int T>
+__global__ __launch_bounds__(kBlock) void k_xent_pad(const char* __restrict__ in, int64_t n, int32_t dim, const int32_t* __restrict__ target,
+                                                     int64_t rows, char* __restrict__ out, int32_t width) {
   const int64_t step = (int64_t)gridDim.x * kBlock;
-  for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < rows * width; i += step) {
-    const int64_t row = i / width;
-    const int32_t c = (int32_t)(i - row * width);
-    typedef typename Element<T>::M M;
-    ((M*)out)[i] = c < dim ? ((const M*)in)[row * dim + c] : (M)0.f;
+  typedef typename Element<T>::M M;
+  constexpr int E = 16 / (int)sizeof(M);  // (a row of the copy is a multiple of 16 bytes)
+  const int32_t packs = width / E;
+  for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < rows * packs; i += step) {
+    const int64_t row = i / packs;
+    const int32_t c = (int32_t)(i - row * packs) * E;
+    const bool there = row < n && (target == nullptr || target[row] >= 0);
+    const M* from = (const M*)in + row * dim + c;
+    Pack<T, E> x;
+    if (there && c + E <= dim) {
+      x = Pack<T, E>::load(from);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) x.x[e] = there && c + e < dim ? from[e] : (M)0.f;
+    }
+    x.store((M*)out + row * width + c);
   }
 }
 
@@ -634,52 +772,61 @@ constexpr int kTile = 256;                            // rows of a block's tile,
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
+// How a call is cut, and what of the workspace it uses for what.
+//   few:    up to 32 rows.  W is read once and that is all there is to it: tiles of 32 rows of H, as many blocks as there are tiles of W.
+//   narrow: more rows, of up to 128 elements of 16 bits (above).
+//   else products of 256 x 256 tiles, one block of four waves on a CU.
 struct XentPlan {
   int64_t n, vocab, width, ld;  // width: elements of a padded row
-  int64_t rows, piece, pieces;
+  int64_t rows, piece, vocab_rows;
   int64_t g_ld;  // bytes from row to row of G: not a power of two, or a tile's rows would all lie in the same few channels of memory
-  int splits, dh_splits;
-  bool few, pad;
-  size_t h, w, part, term, unlift, g, sums, bytes;
+  int splits, dh_splits, dw_splits;
+  bool few, narrow, pad;
+  size_t h, w, part, coef, lse2, target, unlift, g, sums, bytes;
+  static int at_most(int64_t x, int64_t most) { return (int)(x < 1 ? 1 : x < most ? x : most); }
   XentPlan(int64_t n_, int64_t vocab_, int32_t dim, int dtype, bool aligned, bool grad) : n(n_), vocab(vocab_) {
     const int es = element_bytes(dtype);
     width = round_up(dim, 16 / es);
     ld = width * es;
     pad = !aligned || width != dim;
-    few = n <= 32;
+    narrow = es == 2 && width <= 128 && (grad || n > 32);
+    few = n <= 32 && !grad;
     rows = round_up(n, kTile);
-    const int64_t row_tiles = few ? 1 : rows / kTile, vocab_tiles = (vocab + kTile - 1) / kTile;
-    int64_t s = (few ? 1024 : 256) / row_tiles;
-    s = s < 1 ? 1 : s;
-    splits = (int)(s < vocab_tiles ? s : vocab_tiles);
+    const int64_t row_tiles = rows / kTile, vocab_tiles = (vocab + kTile - 1) / kTile;
+    vocab_rows = vocab_tiles * kTile;
+    // blocks: two of a narrow kernel on a CU, three of few rows, one of the others; a multiple of 8 splits where there are so many, so that
+    // the blocks of an XCD have the same splits' tiles of W
+    if (few) splits = at_most(vocab_tiles, 1024);
+    else splits = at_most((narrow ? 512 : 256) / row_tiles, narrow ? (vocab + 63) / 64 : vocab_tiles);
+    if (splits > 8) splits = splits / 8 * 8;
     piece = kPieceBytes / (rows * es) / kTile * kTile;
     if (piece < kTile) piece = kTile;
-    if (piece > vocab_tiles * kTile) piece = vocab_tiles * kTile;
-    pieces = (vocab + piece - 1) / piece;
-    const int64_t dh_tiles = rows / kTile * ((width + kTile - 1) / kTile);
-    int64_t ds = 256 / dh_tiles;
-    const int64_t first = piece < vocab ? piece : vocab, stages = (first * es + kWide - 1) / kWide;
-    ds = ds < 1 ? 1 : ds > 16 ? 16 : ds;
-    dh_splits = (int)(ds < stages ? ds : stages);
+    if (piece > vocab_rows) piece = vocab_rows;
+    const int64_t dh_tiles = row_tiles * ((width + kTile - 1) / kTile), first = piece < vocab ? piece : vocab;
+    dh_splits = narrow ? splits : at_most(at_most(256 / dh_tiles, 16), (first * es + kWide - 1) / kWide);
+    dw_splits = narrow ? at_most(512 / vocab_tiles, (n + 63) / 64) : 1;
     size_t at = 0;
     auto take = [&](size_t b) { const size_t o = at; at += (b + 255) & ~(size_t)255; return o; };
-    h = take(pad ? (size_t)n * ld : 0);
+    h = take(grad ? (size_t)rows * ld : pad ? (size_t)n * ld : 0);
     w = take(pad ? (size_t)vocab * ld : 0);
     part = take(grad ? 0 : (size_t)splits * n * sizeof(RowStat));
-    term = take(grad ? (size_t)rows * sizeof(RowTerm) : 0);
+    coef = take(grad ? (size_t)rows * 4 : 0);
+    lse2 = take(grad ? (size_t)rows * 4 : 0);
+    target = take(grad ? (size_t)rows * 4 : 0);
     unlift = take(grad ? sizeof(float) : 0);
     g_ld = piece * es + 256;
-    g = take(grad ? (size_t)rows * g_ld : 0);
-    sums = take(grad ? (size_t)dh_splits * rows * width * sizeof(float) : 0);
+    g = take(grad && !narrow ? (size_t)rows * g_ld : 0);
+    const size_t dh = (size_t)dh_splits * rows * width * 4, dw = dw_splits > 1 ? (size_t)dw_splits * vocab_rows * width * 4 : 0;
+    sums = take(grad ? (dh > dw ? dh : dw) : 0);
     bytes = at + 256;
   }
 };
 
 template <int T>
-void pad_rows(const void* in, int64_t rows, int32_t dim, const XentPlan& p, void* out, hipStream_t s) {
-  const int64_t blocks = (rows * p.width + kBlock - 1) / kBlock;
-  COOP_LAUNCH(K_XENT_PAD, k_xent_pad<T>, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(kBlock), 0, s, (const char*)in, rows, dim, (char*)out,
-              (int32_t)p.width);
+void pad_rows(const void* in, int64_t n, int32_t dim, const int32_t* target, int64_t rows, const XentPlan& p, void* out, hipStream_t s) {
+  const int64_t blocks = (rows * p.ld / 16 + kBlock - 1) / kBlock;
+  COOP_LAUNCH(K_XENT_PAD, k_xent_pad<T>, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(kBlock), 0, s, (const char*)in, n, dim, target, rows,
+              (char*)out, (int32_t)p.width);
 }
 
 // (blocks of more than 64 KB of LDS have to be allowed, once for each kernel and device; it costs a fraction of a microsecond)
@@ -710,18 +857,40 @@ bool launch_stats(const XentPlan& p, Operand w, Operand h, float alpha, const in
   return true;
 }
 
+// f(KS), for the steps of 16 elements that a narrow row is padded to
+template <typename F>
+void with_steps(int64_t width, F&& f) {
+  if (width <= 32) f(std::integral_constant<int, 2>());
+  else if (width <= 64) f(std::integral_constant<int, 4>());
+  else f(std::integral_constant<int, 8>());
+}
+
 template <int T>
 int forward(const XentPlan& p, const void* hidden, const void* weight, int32_t dim, const int32_t* targets, float alpha, int32_t ignore,
             float* loss, float* lse, char* ws, int32_t* bad, hipStream_t s) {
   if (p.pad) {
-    pad_rows<T>(hidden, p.n, dim, p, ws + p.h, s);
-    pad_rows<T>(weight, p.vocab, dim, p, ws + p.w, s);
+    pad_rows<T>(hidden, p.n, dim, nullptr, p.n, p, ws + p.h, s);
+    pad_rows<T>(weight, p.vocab, dim, nullptr, p.vocab, p, ws + p.w, s);
     hidden = ws + p.h;
     weight = ws + p.w;
   }
   const Operand w{(const char*)weight, p.ld, p.vocab, p.ld}, h{(const char*)hidden, p.ld, p.n, p.ld};
   RowStat* part = (RowStat*)(ws + p.part);
-  const bool ok = p.few ? launch_stats<T, 4, 1, 2, 1>(p, w, h, alpha, targets, part, s) : launch_stats<T, 2, 2, 4, 4>(p, w, h, alpha, targets, part, s);
+  bool ok = true;
+  if (p.few) {
+    ok = launch_stats<T, 4, 1, 2, 1>(p, w, h, alpha, targets, part, s);
+  } else if (!p.narrow) {
+    ok = launch_stats<T, 2, 2, 4, 4>(p, w, h, alpha, targets, part, s);
+  } else if constexpr (T != COOP_F32) {
+    with_steps(p.width, [&](auto ks) {
+      constexpr int KS = decltype(ks)::value, lds = RowStream<T, KS, false>::kLds;
+      const auto kernel = k_xent_stats_narrow<T, KS>;
+      ok = allow_lds(kernel, lds);
+      if (!ok) return;
+      COOP_LAUNCH(K_XENT_STATS, kernel, dim3((unsigned)(p.rows / kTile * p.splits)), dim3(256), lds, s, w, h, p.n, p.vocab, alpha * kLog2e, targets,
+                  p.splits, part);
+    });
+  }
   if (!ok) return COOP_E_HIP;
   COOP_LAUNCH(K_XENT_LOSS, k_xent_loss, dim3((unsigned)((p.n + kWavesPerBlock - 1) / kWavesPerBlock)), dim3(kBlock), 0, s, (const RowStat*)part, p.splits, p.n,
               p.vocab, targets, ignore, loss, lse, bad);
@@ -729,22 +898,58 @@ int forward(const XentPlan& p, const void* hidden, const void* weight, int32_t d
 }
 
 template <int T>
+void write_out(const float* sums, int splits, int64_t rows, const XentPlan& p, int64_t n, int32_t dim, const float* unlift, void* out, hipStream_t s) {
+  const int64_t blocks = (n * ((dim + 3) / 4) + kBlock - 1) / kBlock;
+  COOP_LAUNCH(K_XENT_OUT, k_xent_out<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(kBlock), 0, s, sums, splits, rows, (int32_t)p.width, n, dim,
+              unlift, (char*)out);
+}
+
+template <int T>
+bool backward_narrow(const XentPlan& p, const Operand& w, const Operand& h, int32_t dim, float alpha, const RowTerms& term, const float* unlift,
+                     void* dhidden, void* dweight, float* sums, hipStream_t s) {
+  bool ok = true;
+  with_steps(p.width, [&](auto ks) {
+    constexpr int KS = decltype(ks)::value, lds_h = RowStream<T, KS, false>::kLds, lds_w = RowStream<T, KS, true>::kLds;
+    const auto kh = k_xent_dh_narrow<T, KS>;
+    const auto kw = k_xent_dw_narrow<T, KS>;
+    ok = allow_lds(kh, lds_h) && allow_lds(kw, lds_w);
+    if (!ok) return;
+    if (dhidden != nullptr) {
+      COOP_LAUNCH(K_XENT_DH, kh, dim3((unsigned)(p.rows / kTile * p.dh_splits)), dim3(256), lds_h, s, w, h, p.rows, p.vocab, alpha * kLog2e, term,
+                  p.dh_splits, sums, (int32_t)p.width);
+      write_out<T>(sums, p.dh_splits, p.rows, p, p.n, dim, unlift, dhidden, s);
+    }
+    if (dweight != nullptr) {
+      float* parts = p.dw_splits > 1 ? sums : nullptr;
+      COOP_LAUNCH(K_XENT_DW, kw, dim3((unsigned)(p.vocab_rows / kTile * p.dw_splits)), dim3(256), lds_w, s, w, h, p.vocab, alpha * kLog2e, term, p.dw_splits,
+                  unlift, dim, (char*)dweight, parts, p.vocab_rows, (int32_t)p.width);
+      if (parts != nullptr) write_out<T>(parts, p.dw_splits, p.vocab_rows, p, p.vocab, dim, unlift, dweight, s);
+    }
+  });
+  return ok;
+}
+
+template <int T>
 int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t dim, const int32_t* targets, float alpha, int32_t ignore,
              const float* lse, const float* dloss, void* dhidden, void* dweight, char* ws, int32_t* bad, hipStream_t s) {
-  if (p.pad) {
-    pad_rows<T>(hidden, p.n, dim, p, ws + p.h, s);
-    pad_rows<T>(weight, p.vocab, dim, p, ws + p.w, s);
-    hidden = ws + p.h;
-    weight = ws + p.w;
-  }
-  RowTerm* term = (RowTerm*)(ws + p.term);
+  const RowTerms term{(float*)(ws + p.coef), (float*)(ws + p.lse2), (int32_t*)(ws + p.target)};
   float* unlift = (float*)(ws + p.unlift);
-  char* g = ws + p.g;
   float* sums = (float*)(ws + p.sums);
   COOP_LAUNCH(K_XENT_TERMS, (k_xent_terms<T != COOP_F32>), dim3((unsigned)((p.rows + 1023) / 1024)), dim3(1024), 0, s, targets, ignore, lse, dloss,
               alpha, T == COOP_F16 ? 8192.f : 1.f, p.n, p.rows, p.vocab, term, unlift, bad);
-  const int64_t g_ld = p.g_ld;
+  pad_rows<T>(hidden, p.n, dim, term.target, p.rows, p, ws + p.h, s);
+  if (p.pad) {
+    pad_rows<T>(weight, p.vocab, dim, nullptr, p.vocab, p, ws + p.w, s);
+    weight = ws + p.w;
+  }
+  hidden = ws + p.h;
   const Operand w{(const char*)weight, p.ld, p.vocab, p.ld}, h{(const char*)hidden, p.ld, p.n, p.ld};
+  if constexpr (T != COOP_F32)
+    if (p.narrow) {
+      if (!backward_narrow<T>(p, w, h, dim, alpha, term, unlift, dhidden, dweight, sums, s)) return COOP_E_HIP;
+      return hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
+    }
+  char* g = ws + p.g;
   typedef Product<T, 2, 2, 4, 4, false, false, kWide> P;
   const auto kg = k_xent_g<T, 2, 2, 4, 4>;
   const auto kh = k_xent_dh<T, 2, 2, 4, 4>;
@@ -754,10 +959,9 @@ int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t 
   for (int64_t v = 0; v < p.vocab; v += p.piece) {
     const int64_t len = p.vocab - v < p.piece ? p.vocab - v : p.piece;
     const uint32_t tiles = (uint32_t)((len + kTile - 1) / kTile);
-    COOP_LAUNCH(K_XENT_G, kg, dim3(tiles * row_tiles), dim3(P::kThreads), P::kLds, s, w, h, p.vocab, p.width, alpha * kLog2e, v, tiles,
-                (const RowTerm*)term, g, g_ld);
+    COOP_LAUNCH(K_XENT_G, kg, dim3(tiles * row_tiles), dim3(P::kThreads), P::kLds, s, w, h, p.vocab, p.width, alpha * kLog2e, v, tiles, term, g, p.g_ld);
     if (dhidden != nullptr) {
-      const Operand wt{(const char*)weight + v * p.ld, p.ld, p.ld, len}, gi{g, g_ld, p.rows, (int64_t)tiles * kTile * kElem<T>};
+      const Operand wt{(const char*)weight + v * p.ld, p.ld, p.ld, len}, gi{g, p.g_ld, p.rows, (int64_t)tiles * kTile * kElem<T>};
       // (every split has something to do: the last piece may be too short for all of them, and then adds nothing to the others' sums)
       const int64_t stages = (len + P::kK - 1) / P::kK;
       const int splits = (int)(p.dh_splits < stages ? p.dh_splits : stages);
@@ -765,15 +969,12 @@ int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t 
                   v != 0, sums, p.width);
     }
     if (dweight != nullptr) {
-      const Operand ht{(const char*)hidden, p.ld, p.ld, p.n}, gt{g, g_ld, (int64_t)tiles * kTile * kElem<T>, p.rows};
+      const Operand ht{(const char*)hidden, p.ld, p.ld, p.n}, gt{g, p.g_ld, (int64_t)tiles * kTile * kElem<T>, p.rows};
       COOP_LAUNCH(K_XENT_DW, kw, dim3(tiles * col_tiles), dim3(P::kThreads), P::kLds, s, ht, gt, p.n, p.vocab, v, dim, col_tiles,
                   (const float*)unlift, (char*)dweight);
     }
   }
-  const int64_t out_blocks = (p.n * dim + kBlock - 1) / kBlock;
-  if (dhidden != nullptr)
-    COOP_LAUNCH(K_XENT_DH_OUT, k_xent_dh_out<T>, dim3((unsigned)(out_blocks < 16384 ? out_blocks : 16384)), dim3(kBlock), 0, s, (const float*)sums,
-                p.dh_splits, p.rows, p.width, p.n, dim, (const float*)unlift, (char*)dhidden);
+  if (dhidden != nullptr) write_out<T>(sums, p.dh_splits, p.rows, p, p.n, dim, unlift, dhidden, s);
   return hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
 }
 
