@@ -13,7 +13,8 @@
 // same on every run.  A root that is not zero is never rounded to zero, or a parameter whose gradient stops would be divided by eps.
 // With y the value over its scale, the bits of the 32-bit float 2^-120 |y| are exponent and mantissa of the 8-bit one and 20 bits below
 // them, E4M3's subnormals included: adding 20 random bits and cutting them off is the rounding.
-// A moment that is not finite makes its block's scale NaN or infinite, and so all of the block's moments.
+// A moment that is not finite makes its block's scale NaN or infinite, and so all of the block's moments; blocks whose largest is below
+// 2^-117 are kept as zeros.
 #include <type_traits>
 
 #include "coop_internal.h"
@@ -23,7 +24,8 @@
 namespace coop {
 namespace {
 
-constexpr int kMomentBlock = 256;  // elements that share a scale: 4 neighbouring ones for each lane of a wave
+constexpr int kMomentBlock = 256;  // elements that share a scale: 4 neighbouring ones for each lane of a wave.  Rows of up to 128 (64, 32)
+                                   // elements are a block each and take 32 (16, 8) lanes, two or more to a wave.
 constexpr int kPerLane = 4;
 constexpr int kBlocksPerWave = 4;
 constexpr int kBlocksPerGroup = kWavesPerBlock * kBlocksPerWave;
@@ -35,6 +37,7 @@ struct Tensor {
   const int32_t *rows, *n_active;
   int64_t n_rows, dim;
   uint32_t row_blocks;   // blocks of 256 elements per row, the last one of what is left
+  uint32_t lanes_log2;   // lanes for a block: 64, or fewer that hold all of a row
   uint32_t n_blocks;     // of all rows, or of as many rows as the list may have
   uint32_t first_group;  // of the launch's thread blocks
   int8_t param_type, grad_type, copy_type;
@@ -42,7 +45,7 @@ struct Tensor {
 };
 
 // A launch's tensors are its arguments (at most 4 KB): nothing is copied to the device ahead of it, and nothing is kept.
-constexpr int kTensorsPerLaunch = 28;
+constexpr int kTensorsPerLaunch = 27;
 struct Step {
   float keep1, take1, keep2, take2, decay, rate, undo, eps;
   int n;
@@ -105,12 +108,14 @@ __device__ __forceinline__ float code_value(uint32_t code) {  // of the 8-bit fl
   return code & 0x80u ? -x : x;
 }
 
-// The four codes of a lane; scale: of the wave's block.  `floor`: the code of a value that is not zero is at least this.
+// The four codes of a lane; scale: of its block.  `floor`: the code of a value that is not zero is at least this.  The quotients are
+// taken times the reciprocal, off by 2^-23: that moves the bound between two codes by a millionth of their distance.
 __device__ __forceinline__ uint32_t encode(const float (&x)[4], float scale, const uint32_t (&noise)[4], uint32_t floor) {
+  const float by = 1.f / scale;
   uint32_t c = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const float y = x[e] / scale;
+    const float y = x[e] * by;
     const uint32_t bits = __float_as_uint(fabsf(y) * 0x1p-120f);
     uint32_t code = (bits + noise[e]) >> 20;
     code = code < 0x7Eu ? code : 0x7Eu;
@@ -121,20 +126,21 @@ __device__ __forceinline__ uint32_t encode(const float (&x)[4], float scale, con
   }
   return c;
 }
-// largest magnitude of the wave's values; a NaN counts as larger than any number
-__device__ __forceinline__ float wave_largest(const float (&x)[4]) {
+// The scale of a block that `lanes` lanes share.  A NaN counts as larger than any number; below 2^-126 (its reciprocal would not be a
+// number) the block is taken as zeros.
+__device__ __forceinline__ float block_scale(const float (&x)[4], int lanes) {
   uint32_t top = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const uint32_t b = __float_as_uint(x[e]) & 0x7FFFFFFFu;
     top = top > b ? top : b;
   }
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) {
+  for (int off = 1; off < lanes; off <<= 1) {
     const uint32_t o = __shfl_xor(top, off, kWave);
     top = top > o ? top : o;
   }
-  return __uint_as_float(top);
+  const float scale = __uint_as_float(top) * (1.f / 448.f);
+  return scale < 0x1p-126f ? 0.f : scale;
 }
 
 template <int BITS>
@@ -149,21 +155,31 @@ __global__ __launch_bounds__(kBlock) void k_adamw(Step st) {
   const Tensor& t = st.t[lo];
   const float gs = st.grad_scale != nullptr ? *st.grad_scale : 1.f;
   const int32_t active = t.n_active != nullptr ? *t.n_active : 0x7FFFFFFF;
-  const int lane = lane_id();
+  const int lanes = 1 << t.lanes_log2, lane = lane_id() & (lanes - 1);
+  const uint32_t each = kWave >> t.lanes_log2;  // blocks that a wave has at a time
 #pragma unroll 1
   for (int q = 0; q < kBlocksPerWave; ++q) {
-    const uint32_t b = (blockIdx.x - t.first_group) * kBlocksPerGroup + q * kWavesPerBlock + uniform_wave_in_block();
+    const uint32_t b = ((blockIdx.x - t.first_group) * kBlocksPerGroup + q * kWavesPerBlock + uniform_wave_in_block()) * each;
+    uint32_t entry, in_row;
+    if (each == 1) {
+      entry = b / t.row_blocks;
+      in_row = b - entry * t.row_blocks;
+    } else {
+      entry = b + (lane_id() >> t.lanes_log2);
+      in_row = 0;
+    }
     if (b >= t.n_blocks) return;
-    const uint32_t entry = b / t.row_blocks, in_row = b - entry * t.row_blocks;
     int64_t row = entry;
+    bool there = each == 1 || entry < t.n_blocks;
     if (t.rows != nullptr) {
-      if ((int32_t)entry >= active) return;
-      row = t.rows[entry];
+      there = there && (int32_t)entry < active;
+      row = there ? t.rows[entry] : 0;
       if ((uint64_t)row >= (uint64_t)t.n_rows) {
         if (lane == 0 && in_row == 0) atomicOr(st.bad, 1);
-        continue;
+        there = false;
       }
     }
+    if (!there) continue;
     const int64_t col = (int64_t)in_row * kMomentBlock + lane * kPerLane, left = t.dim - col;
     const int n = left < 0 ? 0 : left < 4 ? (int)left : 4;
     const int64_t at = row * t.dim + col, grad_at = (int64_t)entry * t.dim + col;
@@ -200,7 +216,7 @@ __global__ __launch_bounds__(kBlock) void k_adamw(Step st) {
       store4(t.m, COOP_F32, at, n, m);
       store4(t.v, COOP_F32, at, n, v);
     } else {
-      const float ms = wave_largest(m) * (1.f / 448.f), vs = wave_largest(root) * (1.f / 448.f);
+      const float ms = block_scale(m, lanes), vs = block_scale(root, lanes);
       const uint64_t element = ((uint64_t)row * t.row_blocks + in_row) * kMomentBlock + (uint32_t)(lane * kPerLane);
       const uint32_t high = mix32((uint32_t)(element >> 32) ^ t.key[2]) ^ t.key[1];  // (a block's elements share the high word)
       uint32_t nm[4], nv[4];
@@ -281,10 +297,12 @@ extern "C" int coop_adamw(const coop_adamw_tensor* tensors, int n, int bits, dou
     d.row_blocks = (uint32_t)((t.dim - 1) / kMomentBlock + 1);
     d.n_blocks = (uint32_t)(rows * d.row_blocks);
     d.first_group = groups;
+    d.lanes_log2 = t.dim <= 32 ? 3 : t.dim <= 64 ? 4 : t.dim <= 128 ? 5 : 6;
+    const uint32_t per_group = kBlocksPerGroup << (6 - d.lanes_log2);
     d.param_type = (int8_t)t.param_dtype, d.grad_type = (int8_t)t.grad_dtype, d.copy_type = (int8_t)t.copy_dtype;
     const uint32_t ctr[4] = {(uint32_t)step, (uint32_t)((uint64_t)step >> 32), (uint32_t)i, 0x4144414Du}, key[2] = {(uint32_t)seed, (uint32_t)(seed >> 32)};
     philox4x32_10(ctr, key, d.key);
-    groups += (d.n_blocks + kBlocksPerGroup - 1) / kBlocksPerGroup;
+    groups += (d.n_blocks + per_group - 1) / per_group;
     if (++st.n == kTensorsPerLaunch || groups >= (1u << 22)) flush();
   }
   flush();

@@ -49,6 +49,7 @@ enum KernelId {
   K_SORT_PLACE,      // ... tokens placed in the order of a digit
   K_EMBED_HEADS,     // ... first tokens of the rows
   K_EMBED_SUM,       // ... sums of the rows' tokens
+  K_EMBED_SPANS,     // ... partial sums of rows with very many tokens, ahead
   K_EMBED_JOIN,      // ... partial sums of rows with many tokens
   K_NORM,            // layer norm
   K_NORM_GRAD,       // ... its gradient

@@ -65,161 +65,301 @@ __global__ __launch_bounds__(kBlock) void k_embed(const char* __restrict__ table
 }
 
 // ---- the tokens in the order of their ids ------------------------------------------------------------------------------
-// A stable radix sort of (id, place), least significant digit first: per pass a count of every tile's digits, the exclusive scan of
-// the counts in the order (digit, tile), and the placement.  A place without a row has the key n_rows and comes last.
+// A stable radix sort of (id, place), 8 bits at a time, least significant first.  Per pass the digits of every tile are counted, and then
+// every tile goes to its places: tokens of the digits in front, and of the same digit in the tiles in front.  A block of the second kernel
+// adds these up from the counts itself (up to kOwnTiles of them; above that a scan does).  Inside a tile a wave ranks its tokens 64 at a
+// time: the lanes with the same digit are found by a ballot per bit, and a counter per wave and digit holds how many came before; the
+// tile is brought into its order in LDS, so that tokens of a digit, some 32 of them, leave side by side.  A place without a row has the
+// key n_rows and comes last.  Up to 8,192 tokens one block does all passes, the tokens in its LDS between them.
+//
+// A million ids of 22 bits: 138 us in three passes of count, scan and unordered stores; 125 us in two of 11 bits (the runs of a digit are
+// then 4 tokens, and single stores to memory go at 80 a nanosecond at best).
+constexpr int kKeysPerThread = 8;
+constexpr int kSortBlock = 1024;
+constexpr int kSortWaves = kSortBlock / kWave;
+constexpr int kSortTile = kSortBlock * kKeysPerThread;
 constexpr int kDigitBits = 8;
 constexpr int kDigits = 1 << kDigitBits;
-constexpr int kKeysPerThread = 16;
-constexpr int kSortTile = kBlock * kKeysPerThread;
+constexpr int64_t kOwnTiles = 512;
 
-struct SortInput {  // the first pass reads the ids, the others what the pass before has left
+struct SortInput {  // the first pass reads the ids, the others the (key, place) pairs that the pass before has left
   const int32_t* ids;
-  const uint32_t *keys, *places;
+  const u32x2* pairs;
   int64_t n_rows;
   int32_t pad;
-  __device__ __forceinline__ uint32_t key(int64_t i) const {
-    if (ids == nullptr) return keys[i];
+  __device__ __forceinline__ u32x2 at(int64_t i, bool* wrong) const {
+    if (ids == nullptr) return pairs[i];
     const int32_t id = ids[i];
-    return id != pad && (uint64_t)(int64_t)id < (uint64_t)n_rows ? (uint32_t)id : (uint32_t)n_rows;
+    const bool row = id != pad && (uint64_t)(int64_t)id < (uint64_t)n_rows;
+    *wrong |= !row && id != pad;
+    return u32x2{row ? (uint32_t)id : (uint32_t)n_rows, (uint32_t)i};
   }
-  __device__ __forceinline__ uint32_t place(int64_t i) const { return ids == nullptr ? places[i] : (uint32_t)i; }
 };
 
-__global__ __launch_bounds__(kBlock) void k_sort_count(SortInput in, int64_t n, int shift, uint32_t* __restrict__ matrix, uint32_t tiles,
-                                                       int32_t* __restrict__ bad) {
+// matrix: [tile][digit], or [digit][tile] for a scan
+template <bool OWN>
+__global__ __launch_bounds__(kSortBlock) void k_sort_count(SortInput in, int64_t n, int shift, uint32_t* __restrict__ matrix, uint32_t tiles,
+                                                           int32_t* __restrict__ bad) {
   __shared__ uint32_t cnt[kDigits];
-  cnt[threadIdx.x] = 0;
-  __syncthreads();
+  if (threadIdx.x < kDigits) cnt[threadIdx.x] = 0;
   const int64_t base = (int64_t)blockIdx.x * kSortTile;
   bool wrong = false;
-#pragma unroll 4
+  uint32_t key[kKeysPerThread];
+#pragma unroll
   for (int u = 0; u < kKeysPerThread; ++u) {
-    const int64_t i = base + u * kBlock + threadIdx.x;
-    if (i < n) {
-      const uint32_t k = in.key(i);
-      atomicAdd(&cnt[k >> shift & (kDigits - 1)], 1u);
-      wrong |= in.ids != nullptr && k == (uint32_t)in.n_rows && in.ids[i] != in.pad;
-    }
+    const int64_t i = base + u * kSortBlock + threadIdx.x;
+    key[u] = i < n ? in.at(i, &wrong)[0] : 0u;
   }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kKeysPerThread; ++u)
+    if (base + u * kSortBlock + threadIdx.x < n) atomicAdd(&cnt[key[u] >> shift & (kDigits - 1)], 1u);
   if (wrong) atomicOr(bad, 1);
   __syncthreads();
-  matrix[(size_t)threadIdx.x * tiles + blockIdx.x] = cnt[threadIdx.x];
+  if (threadIdx.x < kDigits) matrix[OWN ? (size_t)blockIdx.x * kDigits + threadIdx.x : (size_t)threadIdx.x * tiles + blockIdx.x] = cnt[threadIdx.x];
 }
 
-// the lanes of this wave whose digit is the same
-__device__ __forceinline__ uint64_t same_digit(uint32_t digit, uint64_t live) {
-  uint64_t m = live;
-#pragma unroll
-  for (int b = 0; b < kDigitBits; ++b) {
-    const uint64_t set = ballot64(digit >> b & 1);
-    m &= digit >> b & 1 ? set : ~set;
-  }
-  return m;
-}
+// LDS of a block that brings its tokens into order
+struct SortLds {
+  u32x2 pair[kSortTile];
+  uint16_t cnt[kSortWaves][kDigits];
+  uint32_t local[kDigits];  // the block's tokens of the digits in front
+  uint32_t sums[kSortWaves];
+  uint32_t parts[2][kSortBlock];
+};
 
-__global__ __launch_bounds__(kBlock) void k_sort_place(SortInput in, int64_t n, int shift, const uint32_t* __restrict__ first, uint32_t tiles,
-                                                       uint32_t* __restrict__ keys_out, uint32_t* __restrict__ places_out) {
-  static_assert(kDigits == kBlock, "a thread has a digit");
-  __shared__ uint32_t cnt[kWavesPerBlock][kDigits];
-#pragma unroll
-  for (int w = 0; w < kWavesPerBlock; ++w) cnt[w][threadIdx.x] = 0;
+// exclusive sums over the digits, a thread of the first kDigits for each
+__device__ __forceinline__ uint32_t digit_offset(uint32_t mine, SortLds* lds) {
+  uint32_t upto = 0;
   __syncthreads();
-  const int wave = uniform_wave_in_block();
-  const int64_t base = (int64_t)blockIdx.x * kSortTile + wave * (kKeysPerThread * kWave) + lane_id();
-  uint32_t key[kKeysPerThread], place[kKeysPerThread], rank[kKeysPerThread];
-#pragma unroll
-  for (int u = 0; u < kKeysPerThread; ++u) {
-    const int64_t i = base + u * kWave;
-    key[u] = i < n ? in.key(i) : 0u;
-    place[u] = i < n ? in.place(i) : 0u;
+  if (threadIdx.x < kDigits) {
+    upto = wave_incl_scan(mine);
+    if (lane_id() == kWave - 1) lds->sums[wave_in_block()] = upto;
   }
-  // a wave's keys in order, 64 at a time: how many of the same digit are in front
+  __syncthreads();
+  uint32_t at = upto - mine;
+  if (threadIdx.x < kDigits)
+    for (int w = 0; w < wave_in_block(); ++w) at += lds->sums[w];
+  return at;
+}
+
+// A thread's tokens into the block's LDS in the order of the digit
+__device__ __forceinline__ void order_block(const u32x2 (&x)[kKeysPerThread], const bool (&live)[kKeysPerThread], int shift, SortLds* lds) {
+  for (int d = threadIdx.x; d < kDigits * kSortWaves / 2; d += kSortBlock) reinterpret_cast<uint32_t*>(lds->cnt)[d] = 0;
+  __syncthreads();
+  uint16_t* cnt = lds->cnt[uniform_wave_in_block()];
+  uint32_t rank[kKeysPerThread];
 #pragma unroll
   for (int u = 0; u < kKeysPerThread; ++u) {
-    const bool live = base + u * kWave < n;
-    const uint32_t d = key[u] >> shift & (kDigits - 1);
-    const uint64_t same = same_digit(d, ballot64(live));
-    const uint32_t before = lanes_below(same);
-    const uint32_t ran = live ? cnt[wave][d] : 0u;
+    const uint32_t d = x[u][0] >> shift & (kDigits - 1);
+    uint64_t same = ballot64(live[u]);
+#pragma unroll
+    for (int b = 0; b < kDigitBits; ++b) {
+      const uint64_t set = ballot64(d >> b & 1);
+      same &= d >> b & 1 ? set : ~set;
+    }
+    const uint32_t before = lanes_below(same), ran = cnt[d];
     rank[u] = ran + before;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    if (live && before == 0) cnt[wave][d] = ran + (uint32_t)__popcll(same);
+    if (live[u] && before == 0) cnt[d] = (uint16_t)(ran + (uint32_t)__popcll(same));
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
   __syncthreads();
-  uint32_t at = first[(size_t)threadIdx.x * tiles + blockIdx.x];
+  uint32_t all = 0;
+  if (threadIdx.x < kDigits) {
 #pragma unroll
-  for (int w = 0; w < kWavesPerBlock; ++w) {
-    const uint32_t c = cnt[w][threadIdx.x];
-    cnt[w][threadIdx.x] = at;
-    at += c;
+    for (int w = 0; w < kSortWaves; ++w) all += lds->cnt[w][threadIdx.x];
+  }
+  uint32_t at = digit_offset(all, lds);
+  if (threadIdx.x < kDigits) {
+    lds->local[threadIdx.x] = at;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+      const uint32_t c = lds->cnt[w][threadIdx.x];
+      lds->cnt[w][threadIdx.x] = (uint16_t)at;  // (below the tile's 8,192 tokens)
+      at += c;
+    }
   }
   __syncthreads();
 #pragma unroll
+  for (int u = 0; u < kKeysPerThread; ++u)
+    if (live[u]) lds->pair[cnt[x[u][0] >> shift & (kDigits - 1)] + rank[u]] = x[u];
+  __syncthreads();
+}
+
+// counts: OWN, the matrix [tile][digit]; else its scan [digit][tile].  The last pass leaves keys and places apart.
+template <bool OWN>
+__global__ __launch_bounds__(kSortBlock) void k_sort_place(SortInput in, int64_t n, int shift, const uint32_t* __restrict__ counts, uint32_t tiles,
+                                                           u32x2* __restrict__ pairs_out, uint32_t* __restrict__ keys_out,
+                                                           uint32_t* __restrict__ places_out) {
+  extern __shared__ char sort_lds[];
+  SortLds* lds = reinterpret_cast<SortLds*>(sort_lds);
+  const int64_t first = (int64_t)blockIdx.x * kSortTile, base = first + uniform_wave_in_block() * (kKeysPerThread * kWave) + lane_id();
+  u32x2 x[kKeysPerThread];
+  bool live[kKeysPerThread], unused = false;
+#pragma unroll
   for (int u = 0; u < kKeysPerThread; ++u) {
-    if (base + u * kWave >= n) continue;
-    const uint32_t to = cnt[wave][key[u] >> shift & (kDigits - 1)] + rank[u];
-    keys_out[to] = key[u];
-    places_out[to] = place[u];
+    live[u] = base + u * kWave < n;
+    x[u] = live[u] ? in.at(base + u * kWave, &unused) : u32x2{0, 0};
   }
+  uint32_t from = 0;  // of digit threadIdx.x: where its tokens of this tile begin
+  if constexpr (OWN) {
+    constexpr int kParts = kSortBlock / kDigits;
+    const uint32_t d = threadIdx.x & (kDigits - 1), part = threadIdx.x / kDigits;
+    uint32_t in_front = 0, all = 0;
+#pragma unroll 8
+    for (uint32_t t = part; t < tiles; t += kParts) {
+      const uint32_t c = counts[(size_t)t * kDigits + d];
+      all += c;
+      in_front += t < blockIdx.x ? c : 0;
+    }
+    lds->parts[0][threadIdx.x] = in_front;
+    lds->parts[1][threadIdx.x] = all;
+    __syncthreads();
+    in_front = all = 0;
+#pragma unroll
+    for (int p = 0; p < kParts; ++p) {
+      in_front += lds->parts[0][p * kDigits + d];
+      all += lds->parts[1][p * kDigits + d];
+    }
+    from = in_front + digit_offset(all, lds);
+  } else if (threadIdx.x < kDigits) {
+    from = counts[(size_t)threadIdx.x * tiles + blockIdx.x];
+  }
+  order_block(x, live, shift, lds);
+  if (threadIdx.x < kDigits) lds->parts[0][threadIdx.x] = from - lds->local[threadIdx.x];
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kKeysPerThread; ++u) {
+    const int at = u * kSortBlock + threadIdx.x;
+    if (first + at >= n) break;
+    const u32x2 p = lds->pair[at];
+    const uint32_t to = lds->parts[0][p[0] >> shift & (kDigits - 1)] + at;
+    if (keys_out == nullptr) {
+      pairs_out[to] = p;
+    } else {
+      keys_out[to] = p[0];
+      places_out[to] = p[1];
+    }
+  }
+}
+
+// n <= kSortTile: all passes
+__global__ __launch_bounds__(kSortBlock) void k_sort_small(SortInput in, int n, int bits, uint32_t* __restrict__ keys_out,
+                                                           uint32_t* __restrict__ places_out, int32_t* __restrict__ bad) {
+  extern __shared__ char sort_lds[];
+  SortLds* lds = reinterpret_cast<SortLds*>(sort_lds);
+  const int base = uniform_wave_in_block() * (kKeysPerThread * kWave) + lane_id();
+  u32x2 x[kKeysPerThread];
+  bool live[kKeysPerThread], wrong = false;
+#pragma unroll
+  for (int u = 0; u < kKeysPerThread; ++u) {
+    live[u] = base + u * kWave < n;
+    x[u] = live[u] ? in.at(base + u * kWave, &wrong) : u32x2{0, 0};
+  }
+  if (wrong) atomicOr(bad, 1);
+  for (int shift = 0; shift < bits; shift += kDigitBits) {
+    order_block(x, live, shift, lds);
+#pragma unroll
+    for (int u = 0; u < kKeysPerThread; ++u)
+      if (live[u]) x[u] = lds->pair[base + u * kWave];
+  }
+#pragma unroll
+  for (int u = 0; u < kKeysPerThread; ++u)
+    if (live[u]) keys_out[base + u * kWave] = x[u][0], places_out[base + u * kWave] = x[u][1];
 }
 
 // ---- the rows' sums ----------------------------------------------------------------------------------------------------
 // The sorted tokens are cut into chunks of kChunk, each summed by a group of lanes that holds a row's columns (E of them each; wider
 // rows in column tiles, blockIdx.y).  What begins and ends inside a chunk is written as it is; a row whose tokens run over a chunk's
-// end leaves a partial sum per chunk (slot 1 of the chunk it begins in, slot 0 of the others), which k_embed_join adds up in order.
-// No order depends on time: the same input gives the same bits.
+// end leaves a partial sum per chunk: in slot 1 of the chunk it begins in, in slot 0 of the others.  A row with very many tokens fills
+// whole spans of 32 and of 1,024 chunks, whose partial sums k_embed_spans adds up ahead, and k_embed_join adds a row's chunks and
+// spans in their order.  No order depends on time: the same input gives the same bits.
 constexpr int kChunk = 32;
-constexpr int kAhead = 8;  // rows in flight per group
-constexpr int64_t kMaxTokens = (int64_t)1 << 30;  // of a gradient: its launches stay below 2^32 threads
+constexpr int kAhead = 8;      // rows in flight per group
+constexpr int kSpan = 32;      // chunks
+constexpr int kSpan2 = 1024;
+constexpr int kHeadTile = 4096;                      // tokens
+constexpr int kTileChunks = kHeadTile / kChunk;
+constexpr int64_t kMaxTokens = (int64_t)1 << 30;     // of a gradient: its launches stay below 2^32 threads
 
 struct ReduceShape {
-  int64_t n_ids;
+  int64_t n_ids, n_chunks;
   int32_t dim;
   uint32_t n_rows;
   int lanes, lanes_log2;  // per row
 };
 
-// heads: the tokens of each chunk that are the first with their id
-__global__ __launch_bounds__(kBlock) void k_embed_heads(const uint32_t* __restrict__ keys, int64_t n, uint32_t n_rows, uint32_t* __restrict__ heads,
-                                                        int64_t n_chunks) {
-  const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-  const uint32_t k = i < n ? keys[i] : n_rows;
-  const bool head = k != n_rows && (i == 0 || keys[i - 1] != k);
-  const uint64_t m = ballot64(head);
-  static_assert(kChunk == 32, "half a wave has a chunk");
-  if ((lane_id() & 31) == 0 && i / kChunk < n_chunks) heads[i / kChunk] = (uint32_t)__popcll(lane_id() == 0 ? m & 0xFFFFFFFFull : m >> 32);
+// The rows form: where a chunk's rows go.  A tile's chunks hold the rows that begin in the tile's chunks in front of them, and a tile those
+// in the tiles in front (of one tile only: none).
+struct RowPlaces {
+  const uint32_t *in_tile, *tile;
+  const uint32_t* total;
+  __device__ __forceinline__ bool used() const { return in_tile != nullptr; }
+  __device__ __forceinline__ int64_t first(int64_t chunk) const {
+    return (int64_t)in_tile[chunk] + (tile != nullptr ? (int64_t)tile[chunk / kTileChunks] : 0);
+  }
+};
+
+__global__ __launch_bounds__(kBlock) void k_embed_heads(const uint32_t* __restrict__ keys, int64_t n, uint32_t n_rows, uint32_t* __restrict__ in_tile,
+                                                        uint32_t* __restrict__ tile_sum) {
+  static_assert(kChunk == 32 && kTileChunks == 2 * kWave, "half a wave has a chunk; a wave scans the tile's chunks, two a lane");
+  __shared__ uint32_t heads[kTileChunks];
+  const int64_t base = (int64_t)blockIdx.x * kHeadTile;
+#pragma unroll 4
+  for (int u = 0; u < kHeadTile / kBlock; ++u) {
+    const int at = u * kBlock + threadIdx.x;
+    const int64_t i = base + at;
+    const uint32_t k = i < n ? keys[i] : n_rows, before = i < n && i > 0 ? keys[i - 1] : n_rows;
+    const uint64_t m = ballot64(k != n_rows && k != before);
+    if ((lane_id() & 31) == 0) heads[at / kChunk] = (uint32_t)__popcll(lane_id() == 0 ? m & 0xFFFFFFFFull : m >> 32);
+  }
+  __syncthreads();
+  if (threadIdx.x >= kWave) return;
+  const uint32_t a = heads[2 * threadIdx.x], b = heads[2 * threadIdx.x + 1], upto = wave_incl_scan(a + b);
+  const int64_t chunk = base / kChunk + 2 * threadIdx.x, chunks = (n + kChunk - 1) / kChunk;
+  if (chunk < chunks) in_tile[chunk] = upto - a - b;
+  if (chunk + 1 < chunks) in_tile[chunk + 1] = upto - b;
+  if (threadIdx.x == kWave - 1) tile_sum[blockIdx.x] = upto;
 }
 
 template <int TO, int E>
 __device__ __forceinline__ void put_row(char* __restrict__ out, int64_t row, int32_t dim, int32_t col, const float (&acc)[E]) {
   Pack<TO, E> y;
   y.set(acc);
-  y.store_nt(out + (row * dim + col) * (int64_t)sizeof(typename Pack<TO, E>::M));
+  y.store_nt(out + (row * dim + col) * (int64_t)sizeof(typename Element<TO>::M));
 }
 
-// `first`: the rows in front of each chunk's first head (the rows form), or null: a row's place is its id
+// a lane's columns of a row; false for a lane that has none
+template <int E>
+__device__ __forceinline__ bool lane_columns(const ReduceShape& sh, int32_t* col) {
+  const int32_t item = (int32_t)blockIdx.y * sh.lanes + (threadIdx.x & (sh.lanes - 1));
+  *col = item * E < sh.dim - E ? item * E : sh.dim - E;
+  return (int64_t)item * E < sh.dim;
+}
+
 template <int TI, int TO, int E>
 __global__ __launch_bounds__(kBlock) void k_embed_sum(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ places, ReduceShape sh,
                                                       const char* __restrict__ dout, const float* __restrict__ scale, float alpha,
-                                                      const uint32_t* __restrict__ first, int32_t* __restrict__ rows_out,
+                                                      RowPlaces rp, int32_t* __restrict__ rows_out, int32_t* __restrict__ count,
                                                       char* __restrict__ out, float* __restrict__ part) {
   typedef Pack<TI, E> In;
   const int64_t chunk = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> sh.lanes_log2;
-  const int lane = threadIdx.x & (sh.lanes - 1);
   const int64_t beg = chunk * kChunk, end = beg + kChunk < sh.n_ids ? beg + kChunk : sh.n_ids;
-  const int32_t item = (int32_t)blockIdx.y * sh.lanes + lane;
-  if (beg >= end || (int64_t)item * E >= sh.dim) return;
-  const int32_t col = item * E < sh.dim - E ? item * E : sh.dim - E;
+  int32_t col;
+  const bool mine = lane_columns<E>(sh, &col), names = col == 0 && rp.used();  // (dim >= E: a column 0 is a row's first item)
+  if (rp.used() && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *count = (int32_t)*rp.total;
+  if (beg >= end || !mine) return;
   uint32_t cur = keys[beg];
   if (cur == sh.n_rows) return;
   bool begun = beg == 0 || keys[beg - 1] != cur;  // the current row's first token is in this chunk
-  int64_t row = first != nullptr ? (int64_t)first[chunk] + (begun ? 0 : -1) : (int64_t)cur;
+  int64_t row = rp.used() ? rp.first(chunk) + (begun ? 0 : -1) : (int64_t)cur;
   float acc[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) acc[e] = 0.f;
-  if (begun && first != nullptr && item == 0) rows_out[row] = (int32_t)cur;
+  if (begun && names) rows_out[row] = (int32_t)cur;
   bool live = true;
   for (int64_t i = beg; i < end && live; i += kAhead) {
     uint32_t key[kAhead];
@@ -242,8 +382,8 @@ __global__ __launch_bounds__(kBlock) void k_embed_sum(const uint32_t* __restrict
         cur = key[u];
         live = cur != sh.n_rows;
         begun = true;
-        row = first != nullptr ? row + 1 : (int64_t)cur;
-        if (live && first != nullptr && item == 0) rows_out[row] = (int32_t)cur;
+        row = rp.used() ? row + 1 : (int64_t)cur;
+        if (live && names) rows_out[row] = (int32_t)cur;
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[e] = 0.f;
       }
@@ -261,67 +401,186 @@ __global__ __launch_bounds__(kBlock) void k_embed_sum(const uint32_t* __restrict
   else store_elements<COOP_F32, E>(part + ((2 * chunk + (begun ? 1 : 0)) * sh.dim + col), acc);
 }
 
+// acc += the partial sums from, from + 1, .. to - 1, `stride` floats apart, in their order
+template <int E>
+__device__ __forceinline__ void add_parts(const float* p, int64_t stride, int64_t from, int64_t to, float (&acc)[E]) {
+  for (int64_t c = from; c < to; c += kAhead) {
+    float f[kAhead][E];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) load_elements<COOP_F32, E>(p + (c + u < to ? c + u : to - 1) * stride, f[u]);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (c + u < to)
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] += f[u][e];
+  }
+}
+
+// One row's tokens, begun earlier, fill chunks [c, c + n) (all of them there)
+__device__ __forceinline__ bool filled(const uint32_t* keys, const ReduceShape& sh, int64_t c, int n) {
+  const int64_t beg = c * kChunk, end = beg + (int64_t)n * kChunk;
+  if (beg == 0 || end > sh.n_ids) return false;
+  const uint32_t k = keys[beg];
+  return k != sh.n_rows && keys[beg - 1] == k && keys[end - 1] == k;
+}
+
+// spans[s]: the sum of the partial sums of 32 chunks, by a group of lanes; spans2[t] of 1,024, by a block (the first n_span2 of them)
+template <int E>
+__global__ __launch_bounds__(kBlock) void k_embed_spans(const uint32_t* __restrict__ keys, ReduceShape sh, const float* __restrict__ part,
+                                                        float* __restrict__ spans, float* __restrict__ spans2, int64_t n_span2) {
+  __shared__ float lds[E * kBlock];
+  int32_t col;
+  const bool mine = lane_columns<E>(sh, &col);
+  float acc[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.f;
+  if (blockIdx.x < n_span2) {
+    const int64_t c = (int64_t)blockIdx.x * kSpan2;
+    if (!filled(keys, sh, c, kSpan2)) return;  // (the whole block)
+    const int groups = kBlock >> sh.lanes_log2, g = threadIdx.x >> sh.lanes_log2, each = kSpan2 / groups;
+    if (mine) add_parts<E>(part + col, 2 * (int64_t)sh.dim, c + g * each, c + (g + 1) * each, acc);
+#pragma unroll
+    for (int e = 0; e < E; ++e) lds[e * kBlock + threadIdx.x] = acc[e];
+    __syncthreads();
+    if (g != 0 || !mine) return;
+    for (int o = 1; o < groups; ++o)
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += lds[e * kBlock + (o << sh.lanes_log2) + threadIdx.x];
+    store_elements<COOP_F32, E>(spans2 + (int64_t)blockIdx.x * sh.dim + col, acc);
+    return;
+  }
+  const int64_t s = (((int64_t)blockIdx.x - n_span2) * kBlock + threadIdx.x) >> sh.lanes_log2;
+  if (s * kSpan >= sh.n_chunks || !mine || !filled(keys, sh, s * kSpan, kSpan)) return;
+  add_parts<E>(part + col, 2 * (int64_t)sh.dim, s * kSpan, (s + 1) * kSpan, acc);
+  store_elements<COOP_F32, E>(spans + s * sh.dim + col, acc);
+}
+
 // A group of lanes per chunk: if a row begins in the chunk and runs over its end, the partial sums of all its chunks.
 template <int TO, int E>
-__global__ __launch_bounds__(kBlock) void k_embed_join(const uint32_t* __restrict__ keys, ReduceShape sh, const uint32_t* __restrict__ first,
-                                                       int64_t n_chunks, const float* __restrict__ part, char* __restrict__ out) {
+__global__ __launch_bounds__(kBlock) void k_embed_join(const uint32_t* __restrict__ keys, ReduceShape sh, RowPlaces rp,
+                                                       const float* __restrict__ part, const float* __restrict__ spans,
+                                                       const float* __restrict__ spans2, char* __restrict__ out) {
   const int64_t chunk = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> sh.lanes_log2;
-  const int lane = threadIdx.x & (sh.lanes - 1);
-  const int32_t item = (int32_t)blockIdx.y * sh.lanes + lane;
-  if (chunk + 1 >= n_chunks || (int64_t)item * E >= sh.dim) return;
-  const int32_t col = item * E < sh.dim - E ? item * E : sh.dim - E;
+  int32_t col;
+  if (!lane_columns<E>(sh, &col) || chunk + 1 >= sh.n_chunks) return;
   const int64_t beg = chunk * kChunk, next = beg + kChunk;
   const uint32_t cur = keys[next];
   if (cur == sh.n_rows || keys[next - 1] != cur || (keys[beg] == cur && beg != 0 && keys[beg - 1] == cur)) return;
-  float acc[E];
-  load_elements<COOP_F32, E>(part + ((2 * chunk + 1) * sh.dim + col), acc);
-  for (int64_t c = chunk + 1; c < n_chunks && keys[c * kChunk] == cur; ++c) {
-    float f[E];
-    load_elements<COOP_F32, E>(part + (2 * c * sh.dim + col), f);
-#pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] += f[e];
+  // the first chunk that does not begin with this row: doubling steps, then halving
+  int64_t in = chunk + 1, out_of = sh.n_chunks;
+  for (int64_t step = 1; in + step < out_of; step *= 2) {
+    if (keys[(in + step) * kChunk] != cur) {
+      out_of = in + step;
+      break;
+    }
+    in += step;
   }
-  put_row<TO, E>(out, first != nullptr ? (int64_t)first[chunk + 1] - 1 : (int64_t)cur, sh.dim, col, acc);
+  while (out_of - in > 1) {
+    const int64_t mid = (in + out_of) / 2;
+    if (keys[mid * kChunk] == cur) in = mid;
+    else out_of = mid;
+  }
+  float acc[E];
+  const float* slot0 = part + col;
+  const int64_t stride = 2 * (int64_t)sh.dim;
+  load_elements<COOP_F32, E>(part + ((2 * chunk + 1) * sh.dim + col), acc);
+  // what is whole of the spans; the last chunk may hold other rows as well, and then is none of a span's
+  const int64_t whole = out_of * kChunk <= sh.n_ids && keys[out_of * kChunk - 1] == cur ? out_of : out_of - 1;
+  int64_t c = chunk + 1;
+  const auto up_to = [](int64_t x, int64_t to) { return (x + to - 1) / to * to; };
+  const int64_t s0 = up_to(c, kSpan), s1 = whole / kSpan * kSpan;
+  if (spans != nullptr && s0 < s1) {
+    add_parts<E>(slot0, stride, c, s0, acc);
+    c = s0;
+    const int64_t t0 = up_to(s0, kSpan2), t1 = s1 / kSpan2 * kSpan2;
+    if (t0 < t1) {
+      add_parts<E>(spans + col, sh.dim, c / kSpan, t0 / kSpan, acc);
+      add_parts<E>(spans2 + col, sh.dim, t0 / kSpan2, t1 / kSpan2, acc);
+      c = t1;
+    }
+    add_parts<E>(spans + col, sh.dim, c / kSpan, s1 / kSpan, acc);
+    c = s1;
+  }
+  add_parts<E>(slot0, stride, c, out_of, acc);
+  put_row<TO, E>(out, rp.used() ? rp.first(chunk + 1) - 1 : (int64_t)cur, sh.dim, col, acc);
 }
 
-__global__ void k_embed_count(const uint32_t* __restrict__ total, int32_t* __restrict__ count) {
-  *count = total != nullptr ? (int32_t)*total : 0;
-}
+__global__ void k_embed_none(int32_t* __restrict__ count) { *count = 0; }
 
 // ---- the workspace of a gradient -----------------------------------------------------------------------------------------
 struct GradPlan {
-  int64_t n, tiles, cells, chunks;
-  size_t keys[2], places[2], matrix, place, scan, heads, first, part, bytes;
+  int64_t n, tiles, head_tiles, chunks, n_span, n_span2;
+  size_t pairs[2], keys, places, matrix, place, scan, in_tile, tile_sum, tile, part, spans, spans2, bytes;
   GradPlan(int64_t n_ids, int32_t dim) : n(n_ids) {
     tiles = (n + kSortTile - 1) / kSortTile;
-    cells = tiles * kDigits;
+    head_tiles = (n + kHeadTile - 1) / kHeadTile;
     chunks = (n + kChunk - 1) / kChunk;
+    n_span = chunks / kSpan;
+    n_span2 = chunks / kSpan2;
+    const int64_t cells = tiles > 1 ? tiles << kDigitBits : 0;
     size_t at = 0;
     auto take = [&](size_t b) { const size_t o = at; at += (b + 255) & ~(size_t)255; return o; };
-    for (int i = 0; i < 2; ++i) keys[i] = take((size_t)n * 4), places[i] = take((size_t)n * 4);
+    for (int i = 0; i < 2; ++i) pairs[i] = take(tiles > 1 ? (size_t)n * 8 : 0);
+    keys = take((size_t)n * 4);
+    places = take((size_t)n * 4);
     matrix = take((size_t)(cells + 1) * 4);
-    place = take((size_t)(cells + 1) * 4);
-    heads = take((size_t)(chunks + 1) * 4);
-    first = take((size_t)(chunks + 1) * 4);
-    const size_t t1 = scan_tmp_bytes(cells), t2 = scan_tmp_bytes(chunks);
+    place = take(tiles > kOwnTiles ? (size_t)(cells + 1) * 4 : 0);
+    in_tile = take((size_t)chunks * 4);
+    tile_sum = take((size_t)(head_tiles + 1) * 4);
+    tile = take((size_t)(head_tiles + 1) * 4);
+    const size_t t1 = scan_tmp_bytes(cells), t2 = scan_tmp_bytes(head_tiles);
     scan = take(t1 > t2 ? t1 : t2);
     part = take((size_t)chunks * 2 * (size_t)dim * 4);
+    spans = take((size_t)n_span * (size_t)dim * 4);
+    spans2 = take((size_t)n_span2 * (size_t)dim * 4);
     bytes = at + 256;
   }
 };
 
 template <int TI, int TO, int E>
-void launch_reduce(const GradPlan& plan, char* ws, const uint32_t* keys, const uint32_t* places, const uint32_t* first, int64_t n_rows,
-                   int32_t dim, const void* dout, const float* scale, float alpha, int32_t* rows_out, void* grad, hipStream_t s) {
+void launch_reduce(const GradPlan& plan, char* ws, const uint32_t* keys, const uint32_t* places, const RowPlaces& rp, int64_t n_rows,
+                   int32_t dim, const void* dout, const float* scale, float alpha, int32_t* rows_out, int32_t* count, void* grad, hipStream_t s) {
   const int32_t items = (dim + E - 1) / E;
-  ReduceShape sh{plan.n, dim, (uint32_t)n_rows, 1, 0};
+  ReduceShape sh{plan.n, plan.chunks, dim, (uint32_t)n_rows, 1, 0};
   while (sh.lanes < items && sh.lanes < kWave) sh.lanes *= 2, ++sh.lanes_log2;
-  const dim3 grid((unsigned)((plan.chunks * sh.lanes + kBlock - 1) / kBlock), (unsigned)((items + sh.lanes - 1) / sh.lanes));
+  const unsigned col_tiles = (unsigned)((items + sh.lanes - 1) / sh.lanes);
+  const auto blocks = [&](int64_t groups) { return (groups * sh.lanes + kBlock - 1) / kBlock; };
+  const dim3 grid((unsigned)blocks(plan.chunks), col_tiles);
   float* part = (float*)(ws + plan.part);
-  COOP_LAUNCH(K_EMBED_SUM, (k_embed_sum<TI, TO, E>), grid, dim3(kBlock), 0, s, keys, places, sh, (const char*)dout, scale, alpha, first,
-              rows_out, (char*)grad, part);
-  if (plan.chunks > 1)
-    COOP_LAUNCH(K_EMBED_JOIN, (k_embed_join<TO, E>), grid, dim3(kBlock), 0, s, keys, sh, first, plan.chunks, (const float*)part, (char*)grad);
+  float* spans = plan.n_span > 0 ? (float*)(ws + plan.spans) : nullptr;
+  float* spans2 = (float*)(ws + plan.spans2);
+  COOP_LAUNCH(K_EMBED_SUM, (k_embed_sum<TI, TO, E>), grid, dim3(kBlock), 0, s, keys, places, sh, (const char*)dout, scale, alpha, rp,
+              rows_out, count, (char*)grad, part);
+  if (plan.chunks == 1) return;
+  if (spans != nullptr)
+    COOP_LAUNCH(K_EMBED_SPANS, k_embed_spans<E>, dim3((unsigned)(plan.n_span2 + blocks(plan.n_span)), col_tiles), dim3(kBlock), 0, s, keys, sh,
+                (const float*)part, spans, spans2, plan.n_span2);
+  COOP_LAUNCH(K_EMBED_JOIN, (k_embed_join<TO, E>), grid, dim3(kBlock), 0, s, keys, sh, rp, (const float*)part, (const float*)spans,
+              (const float*)spans2, (char*)grad);
+}
+
+// the ids' tokens, sorted, into the workspace's keys and places
+template <bool OWN>
+void sort_passes(const GradPlan& plan, char* ws, SortInput in, int bits, int32_t* bad, hipStream_t s) {
+  uint32_t* matrix = (uint32_t*)(ws + plan.matrix);
+  uint32_t* counts = OWN ? matrix : (uint32_t*)(ws + plan.place);
+  const dim3 grid((unsigned)plan.tiles), block(kSortBlock);
+  int to = 0;
+  for (int shift = 0; shift < bits; shift += kDigitBits, to ^= 1) {
+    const bool last = shift + kDigitBits >= bits;
+    u32x2* pairs = (u32x2*)(ws + plan.pairs[to]);
+    COOP_LAUNCH(K_SORT_COUNT, k_sort_count<OWN>, grid, block, 0, s, in, plan.n, shift, matrix, (uint32_t)plan.tiles, bad);
+    if (!OWN) scan_u32_to_u32(matrix, plan.tiles << kDigitBits, counts, ws + plan.scan, s);
+    COOP_LAUNCH(K_SORT_PLACE, k_sort_place<OWN>, grid, block, sizeof(SortLds), s, in, plan.n, shift, (const uint32_t*)counts, (uint32_t)plan.tiles, pairs,
+                last ? (uint32_t*)(ws + plan.keys) : nullptr, last ? (uint32_t*)(ws + plan.places) : nullptr);
+    in.ids = nullptr;
+    in.pairs = pairs;
+  }
+}
+
+template <typename K>
+bool allow_sort(K kernel) {
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SortLds)) == hipSuccess;
 }
 
 int grad_launch(const void* dout, int dtype, const int32_t* ids, int64_t n, const float* scale, float alpha, int32_t pad, int64_t n_rows,
@@ -339,43 +598,43 @@ int grad_launch(const void* dout, int dtype, const int32_t* ids, int64_t n, cons
   if (!bad) return COOP_E_HIP;
   if (!rows_form) clear_bytes(grad, n_rows * dim * element_bytes(grad_dtype), s);
   if (n == 0) {
-    if (rows_form) COOP_LAUNCH(K_EMBED_HEADS, k_embed_count, dim3(1), dim3(1), 0, s, (const uint32_t*)nullptr, count);
+    if (rows_form) COOP_LAUNCH(K_EMBED_HEADS, k_embed_none, dim3(1), dim3(1), 0, s, count);
     return hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
   }
   char* ws = (char*)workspace;
-  uint32_t* matrix = (uint32_t*)(ws + plan.matrix);
-  uint32_t* place = (uint32_t*)(ws + plan.place);
-  SortInput in{ids, nullptr, nullptr, n_rows, pad};
-  int to = 0;
-  for (int shift = 0; shift == 0 || (n_rows >> shift) != 0; shift += kDigitBits) {
-    uint32_t* keys_out = (uint32_t*)(ws + plan.keys[to]);
-    uint32_t* places_out = (uint32_t*)(ws + plan.places[to]);
-    COOP_LAUNCH(K_SORT_COUNT, k_sort_count, dim3((unsigned)plan.tiles), dim3(kBlock), 0, s, in, n, shift, matrix, (uint32_t)plan.tiles, bad);
-    scan_u32_to_u32(matrix, plan.cells, place, ws + plan.scan, s);
-    COOP_LAUNCH(K_SORT_PLACE, k_sort_place, dim3((unsigned)plan.tiles), dim3(kBlock), 0, s, in, n, shift, (const uint32_t*)place,
-                (uint32_t)plan.tiles, keys_out, places_out);
-    in = SortInput{nullptr, keys_out, places_out, n_rows, pad};
-    to ^= 1;
+  int bits = 1;
+  while ((n_rows >> bits) != 0) ++bits;  // (the keys are 0 .. n_rows)
+  const SortInput in{ids, nullptr, n_rows, pad};
+  uint32_t* keys = (uint32_t*)(ws + plan.keys);
+  uint32_t* places = (uint32_t*)(ws + plan.places);
+  if (plan.tiles == 1) {
+    if (!allow_sort(k_sort_small)) return COOP_E_HIP;
+    COOP_LAUNCH(K_SORT_PLACE, k_sort_small, dim3(1), dim3(kSortBlock), sizeof(SortLds), s, in, (int)n, bits, keys, places, bad);
+  } else if (plan.tiles <= kOwnTiles) {
+    if (!allow_sort(k_sort_place<true>)) return COOP_E_HIP;
+    sort_passes<true>(plan, ws, in, bits, bad, s);
+  } else {
+    if (!allow_sort(k_sort_place<false>)) return COOP_E_HIP;
+    sort_passes<false>(plan, ws, in, bits, bad, s);
   }
-  const uint32_t* first = nullptr;
+  RowPlaces rp{nullptr, nullptr, nullptr};
   if (rows_form) {
-    uint32_t* heads = (uint32_t*)(ws + plan.heads);
-    uint32_t* f = (uint32_t*)(ws + plan.first);
-    COOP_LAUNCH(K_EMBED_HEADS, k_embed_heads, dim3((unsigned)((n + kBlock - 1) / kBlock)), dim3(kBlock), 0, s, in.keys, n, (uint32_t)n_rows,
-                heads, plan.chunks);
-    scan_u32_to_u32(heads, plan.chunks, f, ws + plan.scan, s);
-    COOP_LAUNCH(K_EMBED_HEADS, k_embed_count, dim3(1), dim3(1), 0, s, (const uint32_t*)(f + plan.chunks), count);
-    first = f;
+    uint32_t* tile_sum = (uint32_t*)(ws + plan.tile_sum);
+    uint32_t* tile = (uint32_t*)(ws + plan.tile);
+    COOP_LAUNCH(K_EMBED_HEADS, k_embed_heads, dim3((unsigned)plan.head_tiles), dim3(kBlock), 0, s, keys, n, (uint32_t)n_rows,
+                (uint32_t*)(ws + plan.in_tile), tile_sum);
+    const bool one = plan.head_tiles == 1;
+    if (!one) scan_u32_to_u32(tile_sum, plan.head_tiles, tile, ws + plan.scan, s);
+    rp = RowPlaces{(const uint32_t*)(ws + plan.in_tile), one ? nullptr : tile, one ? tile_sum : tile + plan.head_tiles};
   }
   with_dtype(dtype, [&](auto ti) {
     with_dtype(grad_dtype, [&](auto to_) {
-      constexpr int TI = decltype(ti)::value, TO = decltype(to_)::value, E = TI == COOP_F32 ? 4 : 8;
+      constexpr int TI = decltype(ti)::value, TO = decltype(to_)::value, E = TI == COOP_F32 || TO == COOP_F32 ? 4 : 8;
       const auto go = [&](auto e) {
-        launch_reduce<TI, TO, decltype(e)::value>(plan, ws, in.keys, in.places, first, n_rows, dim, dout, scale, alpha, rows_out, grad, s);
+        launch_reduce<TI, TO, decltype(e)::value>(plan, ws, keys, places, rp, n_rows, dim, dout, scale, alpha, rows_out, count, grad, s);
       };
-      // (an accumulator of 8 columns leaves in two 16-byte stores as fp32; rows of fewer columns than a lane holds go one by one)
-      constexpr int EO = TO == COOP_F32 ? 4 : E;
-      if (dim >= EO) go(std::integral_constant<int, EO>());
+      // (16 bytes a lane of the gradient's row, or of the tokens'; rows of fewer columns go one by one)
+      if (dim >= E) go(std::integral_constant<int, E>());
       else go(std::integral_constant<int, 1>());
     });
   });

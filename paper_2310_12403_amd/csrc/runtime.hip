@@ -26,7 +26,7 @@ const char* const kKernelNames[K_COUNT_] = {
     "fill", "labor_scan", "labor_fill", "labor_fill_overflow", "labor_exact", "segments", "enum_list", "enum_walk", "ns_count", "ns_fill", "ns_select", "rw_walk", "rw_fill", "scan_local", "scan_offset",
     "unique_insert", "unique_flag", "unique_filter", "unique_collect", "unique_relabel", "unique_part_count", "unique_part_scatter", "unique_part_first", "copy_ids", "gather", "gather_mean", "owner_count", "owner_scatter", "validate_csr",
     "cache_lookup", "cache_select", "cache_evict", "cache_miss_rows", "cache_hit_rows",
-    "embed", "sort_count", "sort_place", "embed_heads", "embed_sum", "embed_join", "layer_norm", "layer_norm_grad", "layer_norm_join", "adamw",
+    "embed", "sort_count", "sort_place", "embed_heads", "embed_sum", "embed_spans", "embed_join", "layer_norm", "layer_norm_grad", "layer_norm_join", "adamw",
     "xent_pad", "xent_stats", "xent_loss", "xent_terms", "xent_g", "xent_dh", "xent_dw", "xent_out"};
 
 hipEvent_t take_event() {
@@ -94,16 +94,25 @@ void fill_u64(uint64_t* p, int64_t n, uint64_t v, hipStream_t s) {
   COOP_LAUNCH(K_FILL, k_fill_u64, dim3((unsigned)blocks), dim3(kBlock), 0, s, p, n, v);
 }
 
-// (what is in front of the first whole 8-byte word and behind the last one)
-__global__ void k_clear_tail(uint16_t* p, int n) { if ((int)threadIdx.x < n) p[threadIdx.x] = 0; }
+// zeros from p on: whole 16-byte pieces by the grid, what is in front of the first and behind the last by the first block, 2 bytes a thread
+__global__ __launch_bounds__(kBlock) void k_clear(char* __restrict__ p, int64_t head, int64_t pieces, int64_t tail) {
+  const int64_t stride = (int64_t)gridDim.x * kBlock;
+  const u64x2 zero = {0, 0};
+  for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < pieces; i += stride) reinterpret_cast<u64x2*>(p + head)[i] = zero;
+  if (blockIdx.x != 0 || threadIdx.x >= 8) return;
+  if (2 * (int64_t)threadIdx.x < head) reinterpret_cast<uint16_t*>(p)[threadIdx.x] = 0;
+  if (2 * (int64_t)threadIdx.x < tail) reinterpret_cast<uint16_t*>(p + head + 16 * pieces)[threadIdx.x] = 0;
+}
 
 void clear_bytes(void* p, int64_t bytes, hipStream_t s) {
-  // (tensors are 2-byte aligned at least; the head up to a multiple of 8 and the tail by 2-byte stores)
-  const int64_t head = (int64_t)((8 - ((uintptr_t)p & 7)) & 7) < bytes ? (int64_t)((8 - ((uintptr_t)p & 7)) & 7) : bytes;
-  const int64_t words = (bytes - head) / 8, tail = bytes - head - 8 * words;
-  if (head) COOP_LAUNCH(K_FILL, k_clear_tail, dim3(1), dim3(64), 0, s, (uint16_t*)p, (int)(head / 2));
-  fill_u64((uint64_t*)((char*)p + head), words, 0, s);
-  if (tail) COOP_LAUNCH(K_FILL, k_clear_tail, dim3(1), dim3(64), 0, s, (uint16_t*)((char*)p + head + 8 * words), (int)(tail / 2));
+  if (bytes <= 0) return;
+  int64_t head = (int64_t)((16 - ((uintptr_t)p & 15)) & 15);
+  if (head > bytes) head = bytes;
+  const int64_t pieces = (bytes - head) / 16, tail = bytes - head - 16 * pieces;
+  int64_t blocks = (pieces + kBlock - 1) / kBlock;
+  if (blocks > 256 * 64) blocks = 256 * 64;
+  if (blocks < 1) blocks = 1;
+  COOP_LAUNCH(K_FILL, k_clear, dim3((unsigned)blocks), dim3(kBlock), 0, s, (char*)p, head, pieces, tail);
 }
 
 // ---- device-wide exclusive scan -------------------------------------------------------------------------------
