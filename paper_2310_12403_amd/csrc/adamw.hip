@@ -109,9 +109,9 @@ __device__ __forceinline__ float code_value(uint32_t code) {  // of the 8-bit fl
 }
 
 // The four codes of a lane; scale: of its block.  `floor`: the code of a value that is not zero is at least this.  The quotients are
-// taken times the reciprocal, off by 2^-23: that moves the bound between two codes by a millionth of their distance.
+// taken times the reciprocal, off by 2^-22: that moves the bound between two codes by a millionth of their distance.
 __device__ __forceinline__ uint32_t encode(const float (&x)[4], float scale, const uint32_t (&noise)[4], uint32_t floor) {
-  const float by = 1.f / scale;
+  const float by = __builtin_amdgcn_rcpf(scale);
   uint32_t c = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -206,8 +206,15 @@ __global__ __launch_bounds__(kBlock) void k_adamw(Step st) {
       if (st.grad_scale != nullptr) g[e] *= gs;
       m[e] = m[e] * st.keep1 + g[e] * st.take1;
       v[e] = v[e] * st.keep2 + (g[e] * g[e]) * st.take2;
-      root[e] = sqrtf(v[e]);
-      p[e] = p[e] * st.decay - (m[e] / (root[e] * st.undo + st.eps)) * st.rate;
+      if constexpr (BITS == 32) {
+        root[e] = sqrtf(v[e]);
+        p[e] = p[e] * st.decay - (m[e] / (root[e] * st.undo + st.eps)) * st.rate;
+      } else {
+        // The hardware's own root and reciprocal, each within an ulp: the moments behind them are good for four bits, and the exact
+        // quotient and root of four elements were a third of the kernel's instructions (touched rows of 100: 311 us with them).
+        root[e] = v[e] != 0.f ? fmaxf(__builtin_amdgcn_sqrtf(v[e]), 0x1p-75f) : v[e];  // (not zero where v is not)
+        p[e] = p[e] * st.decay - (m[e] * __builtin_amdgcn_rcpf(root[e] * st.undo + st.eps)) * st.rate;
+      }
       if (e >= n) m[e] = root[e] = 0.f;
     }
     store4(t.param, t.param_type, at, n, p);
@@ -218,11 +225,13 @@ __global__ __launch_bounds__(kBlock) void k_adamw(Step st) {
     } else {
       const float ms = block_scale(m, lanes), vs = block_scale(root, lanes);
       const uint64_t element = ((uint64_t)row * t.row_blocks + in_row) * kMomentBlock + (uint32_t)(lane * kPerLane);
-      const uint32_t high = mix32((uint32_t)(element >> 32) ^ t.key[2]) ^ t.key[1];  // (a block's elements share the high word)
+      // u = mix(mix(low ^ key0) ^ key1 ^ mix(high ^ key2)) ^ key3 of the element's number.  A block's elements share the high word, and a
+      // lane's the low one but for its last two bits; the fold that ends the inner mixer and the one that begins the outer cancel.
+      const uint32_t high = fold16(mix32((uint32_t)(element >> 32) ^ t.key[2]) ^ t.key[1]), low = (uint32_t)element ^ t.key[0];
       uint32_t nm[4], nv[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t u = mix32(mix32((uint32_t)(element + e) ^ t.key[0]) ^ high) ^ t.key[3];
+        const uint32_t u = fold16_xor(mix_body(mix_body(fold16(low ^ (uint32_t)e)) ^ high), t.key[3]);
         nm[e] = ((u & 0xFFFFu) << 4) + 8;  // 16 random bits each, in the middle of the 16 values they stand for
         nv[e] = (u >> 16 << 4) + 8;
       }

@@ -361,18 +361,27 @@ __global__ __launch_bounds__(kBlock) void k_embed_sum(const uint32_t* __restrict
   for (int e = 0; e < E; ++e) acc[e] = 0.f;
   if (begun && names) rows_out[row] = (int32_t)cur;
   bool live = true;
+  uint32_t next_key[kAhead], next_place[kAhead];  // (known a round ahead: a round then waits for its rows alone)
+  const auto look_ahead = [&](int64_t i) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int64_t j = i + u < end ? i + u : end - 1;
+      next_place[u] = places[j];
+      next_key[u] = i + u < end ? keys[j] : sh.n_rows;
+    }
+  };
+  look_ahead(beg);
   for (int64_t i = beg; i < end && live; i += kAhead) {
     uint32_t key[kAhead];
     In x[kAhead];
     float s[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const int64_t j = i + u < end ? i + u : end - 1;
-      const uint32_t place = places[j];
-      key[u] = i + u < end ? keys[j] : sh.n_rows;
-      s[u] = scale != nullptr ? scale[place] * alpha : alpha;
-      x[u] = In::load(dout + ((int64_t)place * sh.dim + col) * (int64_t)sizeof(typename In::M));
+      key[u] = next_key[u];
+      s[u] = scale != nullptr ? scale[next_place[u]] * alpha : alpha;
+      x[u] = In::load(dout + ((int64_t)next_place[u] * sh.dim + col) * (int64_t)sizeof(typename In::M));
     }
+    if (i + kAhead < end) look_ahead(i + kAhead);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       if (!live || i + u >= end) continue;

@@ -93,6 +93,19 @@ struct Rows {
   __device__ __forceinline__ int lanes(const NormShape& sh) const { return WAVES == 1 ? sh.lanes : WAVES * kWave; }
 };
 
+// a lane's K packs of a row, as they are in memory
+template <int T, int E, int K>
+struct RowPacks {
+  Pack<T, E> x[K];
+  __device__ __forceinline__ void load(const char* row, int lane, int lanes, int32_t dim) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const Columns<E> c(lane + k * lanes, dim);
+      x[k] = Pack<T, E>::load(row + (int64_t)c.at * (int64_t)sizeof(typename Element<T>::M));  // (a lane without columns: the first ones)
+    }
+  }
+};
+
 template <int T, int E>
 __device__ __forceinline__ void load_row(const char* p, int32_t at, bool live, float (&f)[E]) {
   if (live) {
@@ -112,13 +125,17 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_norm(const char* __restri
   const int lanes = rows.lanes(sh);
   const int64_t row_bytes = (int64_t)sh.dim * (int64_t)sizeof(typename Element<T>::M);
   const float n = (float)sh.dim;
+  RowPacks<T, E, K> next;  // (the next row is on its way while this one is worked on)
+  if (rows.first < sh.rows) next.load(x + rows.first * row_bytes, rows.lane, lanes, sh.dim);
   for (int64_t r = rows.first; r < sh.rows; r += rows.step) {
     float f[K][E];
     float sum = 0.f;
 #pragma unroll
+    for (int k = 0; k < K; ++k) next.x[k].get(f[k]);
+    if (r + rows.step < sh.rows) next.load(x + (r + rows.step) * row_bytes, rows.lane, lanes, sh.dim);
+#pragma unroll
     for (int k = 0; k < K; ++k) {
       const Columns<E> c(rows.lane + k * lanes, sh.dim);
-      load_row<T, E>(x + r * row_bytes, c.at, c.live, f[k]);
 #pragma unroll
       for (int e = 0; e < E; ++e) sum += e >= c.own ? f[k][e] : 0.f;
     }
@@ -176,16 +193,25 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_norm_grad(const char* __r
   for (int k = 0; k < K; ++k)
 #pragma unroll
     for (int e = 0; e < E; ++e) dw[k][e] = db[k][e] = 0.f;
+  RowPacks<T, E, K> next_x, next_dy;  // (as in the forward kernel)
+  float next_mean = 0.f, next_rstd = 0.f;
+  const auto look_ahead = [&](int64_t r) {
+    next_x.load(x + r * row_bytes, rows.lane, lanes, sh.dim);
+    next_dy.load(dy + r * row_bytes, rows.lane, lanes, sh.dim);
+    next_mean = mean_in[r];
+    next_rstd = rstd_in[r];
+  };
+  if (rows.first < sh.rows) look_ahead(rows.first);
   for (int64_t r = rows.first; r < sh.rows; r += rows.step) {
-    const float mean = mean_in[r], rstd = rstd_in[r];
+    const float mean = next_mean, rstd = next_rstd;
     float h[K][E], d[K][E];
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const Columns<E> c(rows.lane + k * lanes, sh.dim);
-      load_row<T, E>(x + r * row_bytes, c.at, c.live, h[k]);
-      load_row<T, E>(dy + r * row_bytes, c.at, c.live, d[k]);
+      next_x.x[k].get(h[k]);
+      next_dy.x[k].get(d[k]);
     }
+    if (r + rows.step < sh.rows) look_ahead(r + rows.step);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const Columns<E> c(rows.lane + k * lanes, sh.dim);
