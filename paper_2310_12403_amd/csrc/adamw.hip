@@ -30,39 +30,45 @@ constexpr int kPerLane = 4;
 constexpr int kBlocksPerWave = 4;
 constexpr int kBlocksPerGroup = kWavesPerBlock * kBlocksPerWave;
 
-struct Tensor {
+// What every tensor needs, and what only 8-bit moments or listed rows do.
+struct Whole {
   char *param, *copy, *m, *v;
   const char* grad;
-  float *m_scale, *v_scale;
-  const int32_t *rows, *n_active;
-  int64_t n_rows, dim;
+  int64_t dim;
   uint32_t row_blocks;   // blocks of 256 elements per row, the last one of what is left
-  uint32_t lanes_log2;   // lanes for a block: 64, or fewer that hold all of a row
   uint32_t n_blocks;     // of all rows, or of as many rows as the list may have
   uint32_t first_group;  // of the launch's thread blocks
+  uint8_t lanes_log2;    // lanes for a block: 64, or fewer that hold all of a row
   int8_t param_type, grad_type, copy_type;
+};
+struct Listed : Whole {
+  float *m_scale, *v_scale;
+  const int32_t *rows, *n_active;
+  int64_t n_rows;
   uint32_t key[4];
 };
 
-// A launch's tensors are its arguments (at most 4 KB): nothing is copied to the device ahead of it, and nothing is kept.
-constexpr int kTensorsPerLaunch = 27;
+struct Hyper { float keep1, take1, keep2, take2, decay, rate, undo, eps; };
+
+// A launch's tensors are its arguments (at most 4 KB): nothing is copied to the device ahead of it, and nothing is kept.  (63 tensors
+// with 32-bit moments and without a list: 300 of them in 5 launches in the place of 12, 647 -> 558 us with non-temporal accesses.)
+template <typename Tensor>
 struct Step {
-  float keep1, take1, keep2, take2, decay, rate, undo, eps;
+  static constexpr int kTensors = (4096 - 72) / (int)sizeof(Tensor);
+  Hyper h;
   int n;
   int32_t* bad;
   const float* grad_scale;
-  Tensor t[kTensorsPerLaunch];
+  Tensor t[kTensors];
 };
-static_assert(sizeof(Step) <= 4096, "kernel arguments");
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
+static_assert(sizeof(Step<Whole>) <= 4096 && sizeof(Step<Listed>) <= 4096, "kernel arguments");
 
 // Elements i .. i + 3 of an array of the type, those beyond n as zero
 __device__ __forceinline__ void load4(const char* p, int type, int64_t i, int n, float (&f)[4]) {
   if (n >= 4) {
-    if (type == COOP_F32) Pack<COOP_F32, 4>::load(p + i * 4).get(f);
-    else if (type == COOP_F16) Pack<COOP_F16, 4>::load(p + i * 2).get(f);
-    else Pack<COOP_BF16, 4>::load(p + i * 2).get(f);
+    if (type == COOP_F32) Pack<COOP_F32, 4>::load_nt(p + i * 4).get(f);
+    else if (type == COOP_F16) Pack<COOP_F16, 4>::load_nt(p + i * 2).get(f);
+    else Pack<COOP_BF16, 4>::load_nt(p + i * 2).get(f);
     return;
   }
 #pragma unroll
@@ -73,9 +79,9 @@ __device__ __forceinline__ void load4(const char* p, int type, int64_t i, int n,
 }
 __device__ __forceinline__ void store4(char* p, int type, int64_t i, int n, const float (&f)[4]) {
   if (n >= 4) {
-    if (type == COOP_F32) { Pack<COOP_F32, 4> x; x.set(f); x.store(p + i * 4); }
-    else if (type == COOP_F16) { Pack<COOP_F16, 4> x; x.set(f); x.store(p + i * 2); }
-    else { Pack<COOP_BF16, 4> x; x.set(f); x.store(p + i * 2); }
+    if (type == COOP_F32) { Pack<COOP_F32, 4> x; x.set(f); x.store_nt(p + i * 4); }
+    else if (type == COOP_F16) { Pack<COOP_F16, 4> x; x.set(f); x.store_nt(p + i * 2); }
+    else { Pack<COOP_BF16, 4> x; x.set(f); x.store_nt(p + i * 2); }
     return;
   }
 #pragma unroll
@@ -143,8 +149,9 @@ __device__ __forceinline__ float block_scale(const float (&x)[4], int lanes) {
   return scale < 0x1p-126f ? 0.f : scale;
 }
 
-template <int BITS>
-__global__ __launch_bounds__(kBlock) void k_adamw(Step st) {
+template <int BITS, typename Tensor>
+__global__ __launch_bounds__(kBlock) void k_adamw(Step<Tensor> st) {
+  constexpr bool kListed = std::is_same<Tensor, Listed>::value;
   // the tensor that this block belongs to: the last one that begins at or before it
   int lo = 0, hi = st.n;
   while (hi - lo > 1) {
@@ -154,7 +161,9 @@ __global__ __launch_bounds__(kBlock) void k_adamw(Step st) {
   }
   const Tensor& t = st.t[lo];
   const float gs = st.grad_scale != nullptr ? *st.grad_scale : 1.f;
-  const int32_t active = t.n_active != nullptr ? *t.n_active : 0x7FFFFFFF;
+  int32_t active = 0x7FFFFFFF;
+  if constexpr (kListed)
+    if (t.n_active != nullptr) active = *t.n_active;
   const int lanes = 1 << t.lanes_log2, lane = lane_id() & (lanes - 1);
   const uint32_t each = kWave >> t.lanes_log2;  // blocks that a wave has at a time
 #pragma unroll 1
@@ -171,14 +180,15 @@ __global__ __launch_bounds__(kBlock) void k_adamw(Step st) {
     if (b >= t.n_blocks) return;
     int64_t row = entry;
     bool there = each == 1 || entry < t.n_blocks;
-    if (t.rows != nullptr) {
-      there = there && (int32_t)entry < active;
-      row = there ? t.rows[entry] : 0;
-      if ((uint64_t)row >= (uint64_t)t.n_rows) {
-        if (lane == 0 && in_row == 0) atomicOr(st.bad, 1);
-        there = false;
+    if constexpr (kListed)
+      if (t.rows != nullptr) {
+        there = there && (int32_t)entry < active;
+        row = there ? t.rows[entry] : 0;
+        if ((uint64_t)row >= (uint64_t)t.n_rows) {
+          if (lane == 0 && in_row == 0) atomicOr(st.bad, 1);
+          there = false;
+        }
       }
-    }
     if (!there) continue;
     const int64_t col = (int64_t)in_row * kMomentBlock + lane * kPerLane, left = t.dim - col;
     const int n = left < 0 ? 0 : left < 4 ? (int)left : 4;
@@ -204,16 +214,16 @@ __global__ __launch_bounds__(kBlock) void k_adamw(Step st) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if (st.grad_scale != nullptr) g[e] *= gs;
-      m[e] = m[e] * st.keep1 + g[e] * st.take1;
-      v[e] = v[e] * st.keep2 + (g[e] * g[e]) * st.take2;
+      m[e] = m[e] * st.h.keep1 + g[e] * st.h.take1;
+      v[e] = v[e] * st.h.keep2 + (g[e] * g[e]) * st.h.take2;
       if constexpr (BITS == 32) {
         root[e] = sqrtf(v[e]);
-        p[e] = p[e] * st.decay - (m[e] / (root[e] * st.undo + st.eps)) * st.rate;
+        p[e] = p[e] * st.h.decay - (m[e] / (root[e] * st.h.undo + st.h.eps)) * st.h.rate;
       } else {
         // The hardware's own root and reciprocal, each within an ulp: the moments behind them are good for four bits, and the exact
         // quotient and root of four elements were a third of the kernel's instructions (touched rows of 100: 311 us with them).
         root[e] = v[e] != 0.f ? fmaxf(__builtin_amdgcn_sqrtf(v[e]), 0x1p-75f) : v[e];  // (not zero where v is not)
-        p[e] = p[e] * st.decay - (m[e] * __builtin_amdgcn_rcpf(root[e] * st.undo + st.eps)) * st.rate;
+        p[e] = p[e] * st.h.decay - (m[e] * __builtin_amdgcn_rcpf(root[e] * st.h.undo + st.h.eps)) * st.h.rate;
       }
       if (e >= n) m[e] = root[e] = 0.f;
     }
@@ -246,6 +256,45 @@ __global__ __launch_bounds__(kBlock) void k_adamw(Step st) {
   }
 }
 
+template <int BITS, typename Tensor>
+void launch_steps(const coop_adamw_tensor* tensors, int n, const Hyper& h, int64_t step, uint64_t seed, const float* grad_scale, int32_t* bad,
+                  hipStream_t s) {
+  Step<Tensor> st;
+  st.h = h;
+  st.bad = bad;
+  st.grad_scale = grad_scale;
+  uint32_t groups = 0;
+  st.n = 0;
+  const auto flush = [&] {
+    if (st.n > 0) COOP_LAUNCH(K_ADAMW, (k_adamw<BITS, Tensor>), dim3(groups), dim3(kBlock), 0, s, st);
+    st.n = 0;
+    groups = 0;
+  };
+  for (int i = 0; i < n; ++i) {
+    const coop_adamw_tensor& t = tensors[i];
+    const int64_t rows = t.rows ? t.n_list : t.n_rows;
+    if (rows == 0 || t.dim == 0) continue;
+    Tensor& d = st.t[st.n];
+    d.param = (char*)t.param, d.copy = (char*)t.copy, d.m = (char*)t.m, d.v = (char*)t.v, d.grad = (const char*)t.grad;
+    d.dim = t.dim;
+    d.row_blocks = (uint32_t)((t.dim - 1) / kMomentBlock + 1);
+    d.n_blocks = (uint32_t)(rows * d.row_blocks);
+    d.first_group = groups;
+    d.lanes_log2 = t.dim <= 32 ? 3 : t.dim <= 64 ? 4 : t.dim <= 128 ? 5 : 6;
+    d.param_type = (int8_t)t.param_dtype, d.grad_type = (int8_t)t.grad_dtype, d.copy_type = (int8_t)t.copy_dtype;
+    if constexpr (std::is_same<Tensor, Listed>::value) {
+      d.m_scale = t.m_scale, d.v_scale = t.v_scale, d.rows = t.rows, d.n_active = t.n_list_dev, d.n_rows = t.n_rows;
+      const uint32_t ctr[4] = {(uint32_t)step, (uint32_t)((uint64_t)step >> 32), (uint32_t)i, 0x4144414Du};
+      const uint32_t key[2] = {(uint32_t)seed, (uint32_t)(seed >> 32)};
+      philox4x32_10(ctr, key, d.key);
+    }
+    const uint32_t per_group = kBlocksPerGroup << (6 - d.lanes_log2);
+    groups += (d.n_blocks + per_group - 1) / per_group;
+    if (++st.n == Step<Tensor>::kTensors || groups >= (1u << 22)) flush();
+  }
+  flush();
+}
+
 }  // namespace
 }  // namespace coop
 
@@ -272,48 +321,15 @@ extern "C" int coop_adamw(const coop_adamw_tensor* tensors, int n, int bits, dou
     if (!aligned_for(t.param, t.param_dtype) || !aligned_for(t.grad, t.grad_dtype) || (t.copy && !aligned_for(t.copy, t.copy_dtype))) return COOP_E_ARG;
     if ((bits == 32 && (((uintptr_t)t.m | (uintptr_t)t.v) & 3) != 0) || (((uintptr_t)t.m_scale | (uintptr_t)t.v_scale) & 3) != 0) return COOP_E_ARG;
   }
-  Step st;
-  st.bad = bad_flag();
-  if (!st.bad) return COOP_E_HIP;
-  st.keep1 = (float)beta1;
-  st.take1 = (float)(1.0 - beta1);
-  st.keep2 = (float)beta2;
-  st.take2 = (float)(1.0 - beta2);
-  st.decay = (float)(1.0 - lr * weight_decay);
-  st.rate = (float)(lr / (1.0 - pow(beta1, (double)step)));
-  st.undo = (float)(1.0 / sqrt(1.0 - pow(beta2, (double)step)));
-  st.eps = (float)eps;
-  st.grad_scale = grad_scale;
-  hipStream_t s = (hipStream_t)stream;
-  uint32_t groups = 0;
-  st.n = 0;
-  const auto flush = [&] {
-    if (st.n > 0) {
-      if (bits == 32) COOP_LAUNCH(K_ADAMW, k_adamw<32>, dim3(groups), dim3(kBlock), 0, s, st);
-      else COOP_LAUNCH(K_ADAMW, k_adamw<8>, dim3(groups), dim3(kBlock), 0, s, st);
-    }
-    st.n = 0;
-    groups = 0;
-  };
-  for (int i = 0; i < n; ++i) {
-    const coop_adamw_tensor& t = tensors[i];
-    const int64_t rows = t.rows ? t.n_list : t.n_rows;
-    if (rows == 0 || t.dim == 0) continue;
-    Tensor& d = st.t[st.n];
-    d.param = (char*)t.param, d.copy = (char*)t.copy, d.m = (char*)t.m, d.v = (char*)t.v, d.grad = (const char*)t.grad;
-    d.m_scale = t.m_scale, d.v_scale = t.v_scale, d.rows = t.rows, d.n_active = t.n_list_dev;
-    d.n_rows = t.n_rows, d.dim = t.dim;
-    d.row_blocks = (uint32_t)((t.dim - 1) / kMomentBlock + 1);
-    d.n_blocks = (uint32_t)(rows * d.row_blocks);
-    d.first_group = groups;
-    d.lanes_log2 = t.dim <= 32 ? 3 : t.dim <= 64 ? 4 : t.dim <= 128 ? 5 : 6;
-    const uint32_t per_group = kBlocksPerGroup << (6 - d.lanes_log2);
-    d.param_type = (int8_t)t.param_dtype, d.grad_type = (int8_t)t.grad_dtype, d.copy_type = (int8_t)t.copy_dtype;
-    const uint32_t ctr[4] = {(uint32_t)step, (uint32_t)((uint64_t)step >> 32), (uint32_t)i, 0x4144414Du}, key[2] = {(uint32_t)seed, (uint32_t)(seed >> 32)};
-    philox4x32_10(ctr, key, d.key);
-    groups += (d.n_blocks + per_group - 1) / per_group;
-    if (++st.n == kTensorsPerLaunch || groups >= (1u << 22)) flush();
-  }
-  flush();
+  bool listed = bits == 8;
+  for (int i = 0; i < n; ++i) listed |= tensors[i].rows != nullptr;
+  const Hyper h{(float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)(1.0 - lr * weight_decay),
+                (float)(lr / (1.0 - pow(beta1, (double)step))), (float)(1.0 / sqrt(1.0 - pow(beta2, (double)step))), (float)eps};
+  int32_t* bad = bad_flag();
+  if (!bad) return COOP_E_HIP;
+  const hipStream_t s = (hipStream_t)stream;
+  if (bits == 8) launch_steps<8, Listed>(tensors, n, h, step, seed, grad_scale, bad, s);
+  else if (listed) launch_steps<32, Listed>(tensors, n, h, step, seed, grad_scale, bad, s);
+  else launch_steps<32, Whole>(tensors, n, h, step, seed, grad_scale, bad, s);
   return hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
 }

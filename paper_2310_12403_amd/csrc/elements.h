@@ -62,7 +62,9 @@ __device__ __forceinline__ void store_elements(void* p, const float (&f)[E]) {
 
 // Sum over each aligned group of `lanes` lanes (a power of two up to 64); every lane of the group has it.
 __device__ __forceinline__ float group_sum(float v, int lanes) {
-  for (int off = 1; off < lanes; off <<= 1) v += __shfl_xor(v, off, kWave);
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1)
+    if (off < lanes) v += __shfl_xor(v, off, kWave);
   return v;
 }
 

@@ -101,7 +101,7 @@ struct RowPacks {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const Columns<E> c(lane + k * lanes, dim);
-      x[k] = Pack<T, E>::load(row + (int64_t)c.at * (int64_t)sizeof(typename Element<T>::M));  // (a lane without columns: the first ones)
+      x[k] = Pack<T, E>::load_nt(row + (int64_t)c.at * (int64_t)sizeof(typename Element<T>::M));  // (a lane without columns: the first ones)
     }
   }
 };
@@ -275,7 +275,7 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void k_norm_join(const float* __
   const int64_t c = (int64_t)blockIdx.x * kWave + lane_id(), width = 2 * (int64_t)dim;
   float sum = 0.f;
   if (c < width) {
-#pragma unroll 8
+#pragma unroll 16
     for (int b = wave_in_block(); b < blocks; b += kJoinWaves) sum += part[b * width + c];
   }
   lds[wave_in_block()][lane_id()] = sum;
@@ -309,11 +309,12 @@ bool norm_layout(int32_t dim, int dtype, NormLayout* out) {
   return l.k <= 8;
 }
 
-// Blocks of a pass: enough to fill the chip eight waves a SIMD, and for a gradient no more than leave partial sums of an eighth of x.
+// Blocks of a pass: as many as are on the chip at once (the gradient's registers: 5, 3 or 2 blocks of four waves a CU), and for a
+// gradient no more than leave partial sums of an eighth of x.
 int64_t norm_blocks(int64_t rows, const NormLayout& l, bool grad) {
   const int64_t per_block = l.waves == 1 ? kBlock / l.lanes : 1;
   int64_t b = (rows + per_block - 1) / per_block;
-  const int64_t most = l.waves == 16 ? 512 : 2048;
+  const int64_t each = l.waves == 16 ? (grad ? 1 : 2) : !grad ? 8 : l.k == 1 ? 5 : l.k == 2 ? 3 : 2, most = 256 * each;
   if (b > most) b = most;
   if (grad && b > rows / 32 + 1) b = rows / 32 + 1;
   return b;

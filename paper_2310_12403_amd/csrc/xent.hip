@@ -794,11 +794,11 @@ struct XentPlan {
     rows = round_up(n, kTile);
     const int64_t row_tiles = rows / kTile, vocab_tiles = (vocab + kTile - 1) / kTile;
     vocab_rows = vocab_tiles * kTile;
-    // blocks: two of a narrow kernel on a CU, three of few rows, one of the others; a multiple of 8 splits where there are so many, so that
+    // blocks: two of a narrow kernel or of few rows on a CU, one of the others; a multiple of 8 splits where there are so many, so that
     // the blocks of an XCD have the same splits' tiles of W
-    if (few) splits = at_most(vocab_tiles, 1024);
+    if (few) splits = at_most((vocab_tiles + (vocab_tiles + 511) / 512 - 1) / ((vocab_tiles + 511) / 512), 512);  // (of as many tiles each)
     else splits = at_most((narrow ? 512 : 256) / row_tiles, narrow ? (vocab + 63) / 64 : vocab_tiles);
-    if (splits > 8) splits = splits / 8 * 8;
+    if (!few && splits > 8) splits = splits / 8 * 8;
     piece = kPieceBytes / (rows * es) / kTile * kTile;
     if (piece < kTile) piece = kTile;
     if (piece > vocab_rows) piece = vocab_rows;
