@@ -397,7 +397,7 @@ int coop_softmax_xent(const void* hidden, int64_t n, const void* weight, int64_t
  * logits are computed again; G is held for a piece of the vocabulary at a time, as dtype (the products' operands have one
  * type; in 16 bits over the largest |alpha dloss_i|).
  *   dhidden, dweight  device, of dtype, all of it written; either may be NULL
- *   workspace         at least coop_softmax_xent_workspace_bytes(n, vocab, dim, dtype, aligned, 1) bytes (some 256 MB for G)
+ *   workspace         at least coop_softmax_xent_workspace_bytes(n, vocab, dim, dtype, aligned, 1) bytes (up to 512 MB for G, where n <= 2^20)
  */
 int coop_softmax_xent_grad(const void* hidden, int64_t n, const void* weight, int64_t vocab, int32_t dim, int dtype,
                            const int32_t* targets, float alpha, int32_t ignore, const float* lse, const float* dloss, void* dhidden,

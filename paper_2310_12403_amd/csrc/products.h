@@ -275,14 +275,16 @@ struct Product {
       next();
     }
   }
-  // the next tile's product
-  __device__ __forceinline__ void tile() {
+  __device__ __forceinline__ void zero() {
 #pragma unroll
     for (int i = 0; i < TA; ++i)
 #pragma unroll
       for (int j = 0; j < TB; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  }
+  // the next tile's product, added to acc
+  __device__ __forceinline__ void tile() {
     int from = slot + 1 < kStages ? slot + 1 : 0;
     meet();
     stage<true>(lds + slot * kStage, lds + from * kStage);

@@ -49,6 +49,7 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
   }
   p.begin(w, h, (int64_t)split * P::kRowsA, row0, 0, k, splits * P::kRowsA, lds);
   for (int64_t v0 = (int64_t)split * P::kRowsA; v0 < vocab; v0 += (int64_t)splits * P::kRowsA) {
+    p.zero();
     p.tile();
     const int first = (int)v0 + P::a0() + P::own_row(), left = (int)vocab - first;
 #pragma unroll
@@ -218,7 +219,8 @@ __device__ __forceinline__ void put_columns(char* out, int64_t row, int64_t c, i
 }
 
 // G of the piece of the vocabulary that begins at v_first, [rows of H, ld bytes]; all of G's tiles are there, beyond the vocabulary's
-// and the rows' end it is zero
+// and the rows' end it is zero.  A tile a block: its stores to G, which take a quarter of its time (128 KB a CU), go on while the next
+// block is at its products.  (Blocks that went from tile to tile waited for them behind their next loads: 677 us a piece of 512 MB, 630 so.)
 template <int T, int WA, int WB, int TA, int TB>
 __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1))) void k_xent_g(Operand w, Operand h, int64_t vocab, int64_t k, float scale2, int64_t v_first,
                                                            uint32_t tiles_a, RowTerms term, char* __restrict__ g, int64_t ld) {
@@ -227,6 +229,7 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
   const int64_t piece0 = (int64_t)(blockIdx.x % tiles_a) * P::kRowsA, row0 = (int64_t)(blockIdx.x / tiles_a) * P::kRowsB;
   P p;
   p.begin(w, h, v_first + piece0, row0, 0, k, 0, lds);
+  p.zero();
   p.tile();
   P::end();
   const int first = (int)(v_first + piece0) + P::a0() + P::own_row(), left = (int)vocab - first;
@@ -277,23 +280,36 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
   const int64_t k0 = stages * split / splits * P::kK, k1 = stages * (split + 1) / splits * P::kK;
   P p;
   p.begin(wt, g, col0, row0, k0, k1, 0, lds);
+  float* to = sums + ((int64_t)split * tiles_b * P::kRowsB + row0 + P::b0() + (lane_id() & 31)) * width;
+  const int c0 = (int)col0 + P::a0() + P::own_row();
+  p.zero();
+  if (add) {  // (the pieces' sums before this one are what it adds to)
+#pragma unroll
+    for (int j = 0; j < TB; ++j)
+#pragma unroll
+      for (int a = 0; a < TA; ++a)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int c = c0 + a * 32 + P::row_of(4 * q);
+          if (c >= width) continue;
+          float f[4];
+          load_elements<COOP_F32, 4>(to + (int64_t)j * 32 * width + c, f);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p.acc[a][j][4 * q + e] = f[e];
+        }
+  }
   p.tile();
   P::end();
-  float* to = sums + (int64_t)split * tiles_b * P::kRowsB * width;
 #pragma unroll
   for (int j = 0; j < TB; ++j)
 #pragma unroll
     for (int a = 0; a < TA; ++a)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int64_t c = col0 + P::a0() + P::own_row() + a * 32 + P::row_of(4 * q);
+        const int c = c0 + a * 32 + P::row_of(4 * q);
         if (c >= width) continue;
-        float* at = to + (row0 + P::b0() + j * 32 + (lane_id() & 31)) * width + c;
-        f32x16& x = p.acc[a][j];
-        u32x4 old = add ? *reinterpret_cast<const u32x4*>(at) : u32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) old[e] = __float_as_uint(__uint_as_float(old[e]) + x[4 * q + e]);
-        *reinterpret_cast<u32x4*>(at) = old;
+        const float f[4] = {p.acc[a][j][4 * q], p.acc[a][j][4 * q + 1], p.acc[a][j][4 * q + 2], p.acc[a][j][4 * q + 3]};
+        store_elements<COOP_F32, 4>(to + (int64_t)j * 32 * width + c, f);
       }
 }
 
@@ -330,6 +346,7 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
   const int64_t col0 = (int64_t)(blockIdx.x % tiles_a) * P::kRowsA, piece0 = (int64_t)(blockIdx.x / tiles_a) * P::kRowsB;
   P p;
   p.begin(ht, gt, col0, piece0, 0, k, 0, lds);
+  p.zero();
   p.tile();
   P::end();
   const float u = *unlift;
@@ -766,21 +783,24 @@ __global__ __launch_bounds__(kBlock) void k_xent_pad(const char* __restrict__ in
 }
 
 // ---- the workspace ---------------------------------------------------------------------------------------------------------
-constexpr int64_t kPieceBytes = (int64_t)256 << 20;  // of G
+constexpr int64_t kPieceBytes = (int64_t)512 << 20;  // of G
 constexpr int64_t kMaxVocab = 0x7FFFF000;            // (a tile's row numbers stay below 2^31)
-constexpr int kTile = 256;                            // rows of a block's tile, either way
+// Rows of a block's tile, either way, and of a wave's: in 16 bits what the registers hold, since the matrix units then take all that LDS
+// gives; in 32 bits they are sixteen times slower and smaller tiles, two blocks on a CU, fill the chip better.
+template <int T> constexpr int kWaveTiles = T == COOP_F32 ? 2 : 4;
+constexpr int tile_rows(int dtype) { return dtype == COOP_F32 ? 128 : 256; }
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 // How a call is cut, and what of the workspace it uses for what.
 //   few:    up to 32 rows.  W is read once and that is all there is to it: tiles of 32 rows of H, as many blocks as there are tiles of W.
 //   narrow: more rows, of up to 128 elements of 16 bits (above).
-//   else products of 256 x 256 tiles, one block of four waves on a CU.
+//   else products in tiles, a piece of the vocabulary at a time.
 struct XentPlan {
   int64_t n, vocab, width, ld;  // width: elements of a padded row
   int64_t rows, piece, vocab_rows;
   int64_t g_ld;  // bytes from row to row of G: not a power of two, or a tile's rows would all lie in the same few channels of memory
-  int splits, dh_splits, dw_splits;
+  int splits, dh_splits, dw_splits, tile;
   bool few, narrow, pad;
   size_t h, w, part, coef, lse2, target, unlift, g, sums, bytes;
   static int at_most(int64_t x, int64_t most) { return (int)(x < 1 ? 1 : x < most ? x : most); }
@@ -791,19 +811,22 @@ struct XentPlan {
     pad = !aligned || width != dim;
     narrow = es == 2 && width <= 128 && (grad || n > 32);
     few = n <= 32 && !grad;
-    rows = round_up(n, kTile);
-    const int64_t row_tiles = rows / kTile, vocab_tiles = (vocab + kTile - 1) / kTile;
-    vocab_rows = vocab_tiles * kTile;
+    tile = tile_rows(dtype);
+    rows = round_up(n, tile);
+    const int blocks = 256 * (narrow || dtype == COOP_F32 ? 2 : 1);
+    const int64_t row_tiles = rows / tile, vocab_tiles = (vocab + tile - 1) / tile;
+    vocab_rows = vocab_tiles * tile;
     // blocks: two of a narrow kernel or of few rows on a CU, one of the others; a multiple of 8 splits where there are so many, so that
     // the blocks of an XCD have the same splits' tiles of W
-    if (few) splits = at_most((vocab_tiles + (vocab_tiles + 511) / 512 - 1) / ((vocab_tiles + 511) / 512), 512);  // (of as many tiles each)
-    else splits = at_most((narrow ? 512 : 256) / row_tiles, narrow ? (vocab + 63) / 64 : vocab_tiles);
+    const int64_t few_tiles = (vocab + 255) / 256;
+    if (few) splits = at_most((few_tiles + (few_tiles + 511) / 512 - 1) / ((few_tiles + 511) / 512), 512);  // (of as many tiles each)
+    else splits = at_most(blocks / row_tiles, narrow ? (vocab + 63) / 64 : vocab_tiles);
     if (!few && splits > 8) splits = splits / 8 * 8;
-    piece = kPieceBytes / (rows * es) / kTile * kTile;
-    if (piece < kTile) piece = kTile;
+    piece = kPieceBytes / (rows * es) / tile * tile;
+    if (piece < tile) piece = tile;
     if (piece > vocab_rows) piece = vocab_rows;
-    const int64_t dh_tiles = row_tiles * ((width + kTile - 1) / kTile), first = piece < vocab ? piece : vocab;
-    dh_splits = narrow ? splits : at_most(at_most(256 / dh_tiles, 16), (first * es + kWide - 1) / kWide);
+    const int64_t dh_tiles = row_tiles * ((width + tile - 1) / tile), first = piece < vocab ? piece : vocab;
+    dh_splits = narrow ? splits : at_most(at_most(blocks / dh_tiles, 64), (first * es + kWide - 1) / kWide);
     dw_splits = narrow ? at_most(512 / vocab_tiles, (n + 63) / 64) : 1;
     size_t at = 0;
     auto take = [&](size_t b) { const size_t o = at; at += (b + 255) & ~(size_t)255; return o; };
@@ -880,14 +903,14 @@ int forward(const XentPlan& p, const void* hidden, const void* weight, int32_t d
   if (p.few) {
     ok = launch_stats<T, 4, 1, 2, 1>(p, w, h, alpha, targets, part, s);
   } else if (!p.narrow) {
-    ok = launch_stats<T, 2, 2, 4, 4>(p, w, h, alpha, targets, part, s);
+    ok = launch_stats<T, 2, 2, kWaveTiles<T>, kWaveTiles<T>>(p, w, h, alpha, targets, part, s);
   } else if constexpr (T != COOP_F32) {
     with_steps(p.width, [&](auto ks) {
       constexpr int KS = decltype(ks)::value, lds = RowStream<T, KS, false>::kLds;
       const auto kernel = k_xent_stats_narrow<T, KS>;
       ok = allow_lds(kernel, lds);
       if (!ok) return;
-      COOP_LAUNCH(K_XENT_STATS, kernel, dim3((unsigned)(p.rows / kTile * p.splits)), dim3(256), lds, s, w, h, p.n, p.vocab, alpha * kLog2e, targets,
+      COOP_LAUNCH(K_XENT_STATS, kernel, dim3((unsigned)(p.rows / p.tile * p.splits)), dim3(256), lds, s, w, h, p.n, p.vocab, alpha * kLog2e, targets,
                   p.splits, part);
     });
   }
@@ -915,13 +938,13 @@ bool backward_narrow(const XentPlan& p, const Operand& w, const Operand& h, int3
     ok = allow_lds(kh, lds_h) && allow_lds(kw, lds_w);
     if (!ok) return;
     if (dhidden != nullptr) {
-      COOP_LAUNCH(K_XENT_DH, kh, dim3((unsigned)(p.rows / kTile * p.dh_splits)), dim3(256), lds_h, s, w, h, p.rows, p.vocab, alpha * kLog2e, term,
+      COOP_LAUNCH(K_XENT_DH, kh, dim3((unsigned)(p.rows / p.tile * p.dh_splits)), dim3(256), lds_h, s, w, h, p.rows, p.vocab, alpha * kLog2e, term,
                   p.dh_splits, sums, (int32_t)p.width);
       write_out<T>(sums, p.dh_splits, p.rows, p, p.n, dim, unlift, dhidden, s);
     }
     if (dweight != nullptr) {
       float* parts = p.dw_splits > 1 ? sums : nullptr;
-      COOP_LAUNCH(K_XENT_DW, kw, dim3((unsigned)(p.vocab_rows / kTile * p.dw_splits)), dim3(256), lds_w, s, w, h, p.vocab, alpha * kLog2e, term, p.dw_splits,
+      COOP_LAUNCH(K_XENT_DW, kw, dim3((unsigned)(p.vocab_rows / p.tile * p.dw_splits)), dim3(256), lds_w, s, w, h, p.vocab, alpha * kLog2e, term, p.dw_splits,
                   unlift, dim, (char*)dweight, parts, p.vocab_rows, (int32_t)p.width);
       if (parts != nullptr) write_out<T>(parts, p.dw_splits, p.vocab_rows, p, p.vocab, dim, unlift, dweight, s);
     }
@@ -950,18 +973,19 @@ int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t 
       return hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
     }
   char* g = ws + p.g;
-  typedef Product<T, 2, 2, 4, 4, false, false, kWide> P;
-  const auto kg = k_xent_g<T, 2, 2, 4, 4>;
-  const auto kh = k_xent_dh<T, 2, 2, 4, 4>;
-  const auto kw = k_xent_dw<T, 2, 2, 4, 4>;
+  constexpr int N = kWaveTiles<T>;
+  typedef Product<T, 2, 2, N, N, false, false, kWide> P;
+  const auto kg = k_xent_g<T, 2, 2, N, N>;
+  const auto kh = k_xent_dh<T, 2, 2, N, N>;
+  const auto kw = k_xent_dw<T, 2, 2, N, N>;
   if (!allow_lds(kg, P::kLds) || !allow_lds(kh, P::kLds) || !allow_lds(kw, P::kLds)) return COOP_E_HIP;
-  const uint32_t row_tiles = (uint32_t)(p.rows / kTile), col_tiles = (uint32_t)((p.width + kTile - 1) / kTile);
+  const uint32_t row_tiles = (uint32_t)(p.rows / p.tile), col_tiles = (uint32_t)((p.width + p.tile - 1) / p.tile);
   for (int64_t v = 0; v < p.vocab; v += p.piece) {
     const int64_t len = p.vocab - v < p.piece ? p.vocab - v : p.piece;
-    const uint32_t tiles = (uint32_t)((len + kTile - 1) / kTile);
+    const uint32_t tiles = (uint32_t)((len + p.tile - 1) / p.tile);
     COOP_LAUNCH(K_XENT_G, kg, dim3(tiles * row_tiles), dim3(P::kThreads), P::kLds, s, w, h, p.vocab, p.width, alpha * kLog2e, v, tiles, term, g, p.g_ld);
     if (dhidden != nullptr) {
-      const Operand wt{(const char*)weight + v * p.ld, p.ld, p.ld, len}, gi{g, p.g_ld, p.rows, (int64_t)tiles * kTile * kElem<T>};
+      const Operand wt{(const char*)weight + v * p.ld, p.ld, p.ld, len}, gi{g, p.g_ld, p.rows, (int64_t)tiles * p.tile * kElem<T>};
       // (every split has something to do: the last piece may be too short for all of them, and then adds nothing to the others' sums)
       const int64_t stages = (len + P::kK - 1) / P::kK;
       const int splits = (int)(p.dh_splits < stages ? p.dh_splits : stages);
@@ -969,7 +993,7 @@ int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t 
                   v != 0, sums, p.width);
     }
     if (dweight != nullptr) {
-      const Operand ht{(const char*)hidden, p.ld, p.ld, p.n}, gt{g, p.g_ld, (int64_t)tiles * kTile * kElem<T>, p.rows};
+      const Operand ht{(const char*)hidden, p.ld, p.ld, p.n}, gt{g, p.g_ld, (int64_t)tiles * p.tile * kElem<T>, p.rows};
       COOP_LAUNCH(K_XENT_DW, kw, dim3(tiles * col_tiles), dim3(P::kThreads), P::kLds, s, ht, gt, p.n, p.vocab, v, dim, col_tiles,
                   (const float*)unlift, (char*)dweight);
     }
