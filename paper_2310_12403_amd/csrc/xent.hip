@@ -377,20 +377,34 @@ struct RowStage {
     const int r0 = row & 1, r1 = row >> 1 & 1, r2 = row >> 2 & 1, r3 = row >> 3 & 1;
     return KS == 8 ? r2 | r0 << 1 | r1 << 2 | r3 << 3 : KS == 4 ? r2 | (r0 ^ r3) << 1 | r1 << 2 : r2 | (r1 ^ r3) << 1;
   }
+  // A lane's place in what it reads; from step to step and tile to tile it is an exclusive or with a few bits.  (Taken anew every stage: the
+  // places of all reads, kept in registers, do not fit beside the rows and sums.)
+  struct Reads {
+    uint32_t rows, across;
+    __device__ __forceinline__ Reads() {
+      const int lane = lane_id(), r = lane & 31, b = lane >> 4, t = lane & 15, q = (b >> 1) * 4 + (t >> 2), c = (b & 1) * 16 + (t & 3) * 4;
+      rows = (uint32_t)(r * kRowBytes + (((lane >> 5) ^ swizzle(r)) << 4));
+      across = (uint32_t)(q * kRowBytes + (((c >> 3) ^ swizzle(q)) << 4) + (c & 7) * 2);
+    }
+    __device__ __forceinline__ Reads again() const {
+      Reads x = *this;
+#ifdef __HIP_DEVICE_COMPILE__
+      asm volatile("" : "+v"(x.rows), "+v"(x.across));
+#endif
+      return x;
+    }
+  };
   // rows block * 32 + .., elements kk * 16 + ..: a fragment with the elements as k
-  static __device__ __forceinline__ u32x4 fragment(const char* lds, int block, int kk) {
-    const int r = block * 32 + (lane_id() & 31), chunk = kk * 2 + (lane_id() >> 5);
-    return *reinterpret_cast<const u32x4*>(lds + r * kRowBytes + ((chunk ^ swizzle(r)) << 4));
+  static __device__ __forceinline__ u32x4 fragment(const char* lds, const Reads& at, int block, int kk) {
+    return *reinterpret_cast<const u32x4*>(lds + (at.rows ^ (uint32_t)(kk << 5)) + block * 32 * kRowBytes);
   }
   // elements tile * 32 + .., with 16 of the block's rows as k, in the order in which a lane's registers hold the rows of a product
-  static __device__ __forceinline__ u32x4 transposed(const char* lds, int block, int tile, int s) {
-    const int lane = lane_id(), b = lane >> 4, t = lane & 15;
+  static __device__ __forceinline__ u32x4 transposed(const char* lds, const Reads& at, int block, int tile, int s) {
     u32x4 f;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      const int r = block * 32 + s * 16 + q * 8 + (b >> 1) * 4 + (t >> 2), c = tile * 32 + (b & 1) * 16 + (t & 3) * 4;
-      const char* at = lds + r * kRowBytes + (((c >> 3) ^ swizzle(r)) << 4) + (c & 7) * 2;
-      const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(LdsByte*)at));
+      const char* from = lds + (at.across ^ (uint32_t)((tile << 6) ^ ((swizzle(q * 8) & (kChunks - 1)) << 4))) + (block * 32 + s * 16 + q * 8) * kRowBytes;
+      const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(LdsByte*)from));
       f[2 * q] = y[0];
       f[2 * q + 1] = y[1];
     }
@@ -406,7 +420,7 @@ struct RowStream {
   static constexpr int kStages = 4, kStage = S::kBytes + (TERMS ? 1024 : 0), kLds = kStages * kStage, kLoads = S::kMine + (TERMS ? 1 : 0);
   const char* base;
   int64_t next, step, end;
-  int ld, at[S::kMine];
+  int ld, at;  // a lane's first load of a stage; the others are as many rows further on, in the same chunk
   const char* terms;
   int slot;
   char* lds;
@@ -417,7 +431,7 @@ struct RowStream {
     const int wave = uniform_wave_in_block();
 #pragma unroll
     for (int i = 0; i < S::kMine; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(LdsByte*)(into + (i * 4 + wave) * 1024), 16, at[i], 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(LdsByte*)(into + (i * 4 + wave) * 1024), 16, at + i * (4096 / S::kRowBytes) * ld, 0, 0, 0);
     if constexpr (TERMS) {  // a wave has one of the three arrays (the last one the first again: all waves have as many loads)
       const auto tr = __builtin_amdgcn_make_buffer_rsrc((void*)(terms + next * 4), 0, rows * 4, 0x00020000);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(tr, (__attribute__((address_space(3))) void*)(LdsByte*)(into + S::kBytes + (wave == 3 ? 0 : wave) * 256), 4,
@@ -427,12 +441,9 @@ struct RowStream {
   }
   __device__ __forceinline__ void begin(const Operand& op, int64_t first, int64_t step_, const RowTerms* t, char* lds_) {
     base = op.base, ld = (int)op.ld, next = first, step = step_, end = op.rows, lds = lds_;
-    const int wave = uniform_wave_in_block();
-#pragma unroll
-    for (int i = 0; i < S::kMine; ++i) {
-      const int s = (i * 4 + wave) * kWave + lane_id(), row = s / S::kChunks, chunk = (s % S::kChunks) ^ S::swizzle(row);
-      at[i] = chunk * 16 < ld ? row * ld + chunk * 16 : 0x3FFFFFFF;
-    }
+    const int wave = uniform_wave_in_block(), s = wave * kWave + lane_id(), row = s / S::kChunks, chunk = (s % S::kChunks) ^ S::swizzle(row);
+    static_assert(4096 / S::kRowBytes % 16 == 0, "the exchange of chunks goes by the row's last four bits");
+    at = chunk * 16 < ld ? row * ld + chunk * 16 : 0x3FFFFFFF;
     if constexpr (TERMS) terms = wave == 1 ? (const char*)t->coef : wave == 2 ? (const char*)t->target : (const char*)t->lse2;
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) start(lds + s * kStage);
@@ -508,17 +519,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     sum[j] = target[j] = 0.f;
   }
   Stream stream;
+  const typename S::Reads reads;
   stream.begin(w, (int64_t)split * S::kRows, (int64_t)splits * S::kRows, nullptr, lds);
   for (int64_t v0 = (int64_t)split * S::kRows; v0 < vocab; v0 += (int64_t)splits * S::kRows) {
     f32x16 z[2][2];
     stream.stage([&](const char* from) {
+      const typename S::Reads at = reads.again();
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) z[b][0][e] = z[b][1][e] = 0.f;
 #pragma unroll
         for (int kk = 0; kk < KS; ++kk) {
-          const u32x4 a = S::fragment(from, b, kk);
+          const u32x4 a = S::fragment(from, at, b, kk);
 #pragma unroll
           for (int j = 0; j < 2; ++j) z[b][j] = mma<T>(a, hf[j][kk], z[b][j]);
         }
@@ -594,11 +607,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[c][0][e] = acc[c][1][e] = 0.f;
   Stream stream;
+  const typename S::Reads reads;
   stream.begin(w, (int64_t)split * S::kRows, (int64_t)splits * S::kRows, nullptr, lds);
   for (int64_t v0 = (int64_t)split * S::kRows; v0 < vocab; v0 += (int64_t)splits * S::kRows) {
     const int first = (int)v0 + own_row(), left = (int)vocab - first;
     const bool ragged = v0 + S::kRows > vocab;
     stream.stage([&](const char* from) {
+      const typename S::Reads at = reads.again();
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         f32x16 z[2];
@@ -607,7 +622,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int e = 0; e < 16; ++e) z[0][e] = z[1][e] = 0.f;
 #pragma unroll
         for (int kk = 0; kk < KS; ++kk) {
-          const u32x4 a = S::fragment(from, b, kk);
+          const u32x4 a = S::fragment(from, at, b, kk);
 #pragma unroll
           for (int j = 0; j < 2; ++j) z[j] = mma<T>(a, hf[j][kk], z[j]);
         }
@@ -634,7 +649,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int c = 0; c < KS / 2; ++c) {
-            const u32x4 a = S::transposed(from, b, c, s);
+            const u32x4 a = S::transposed(from, at, b, c, s);
 #pragma unroll
             for (int j = 0; j < 2; ++j) acc[c][j] = mma<T>(a, p[j][s], acc[c][j]);
           }
@@ -675,9 +690,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[c][0][e] = acc[c][1][e] = 0.f;
   Stream stream;
+  const typename S::Reads reads;
   stream.begin(h, (int64_t)split * S::kRows, (int64_t)splits * S::kRows, &term, lds);
   for (int64_t i0 = (int64_t)split * S::kRows; i0 < h.rows; i0 += (int64_t)splits * S::kRows) {
     stream.stage([&](const char* from) {
+      const typename S::Reads at = reads.again();
       const float* lse2 = reinterpret_cast<const float*>(from + S::kBytes);
       const float* coef = lse2 + 64;
       const int hit = reinterpret_cast<const int32_t*>(coef + 64)[lane] - (int)v0;  // of row `lane` of the stage
@@ -690,17 +707,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int e = 0; e < 16; ++e) z[0][e] = z[1][e] = 0.f;
 #pragma unroll
         for (int kk = 0; kk < KS; ++kk) {
-          const u32x4 a = S::fragment(from, b, kk);
+          const u32x4 a = S::fragment(from, at, b, kk);
 #pragma unroll
           for (int j = 0; j < 2; ++j) z[j] = mma<T>(a, wf[j][kk], z[j]);
         }
         f32x16 c4;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int at = b * 32 + row_of(4 * q) + own_row();
+          const int i = b * 32 + row_of(4 * q) + own_row();
           float l[4], c[4];
-          load_elements<COOP_F32, 4>(lse2 + at, l);
-          load_elements<COOP_F32, 4>(coef + at, c);
+          load_elements<COOP_F32, 4>(lse2 + i, l);
+          load_elements<COOP_F32, 4>(coef + i, c);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             c4[4 * q + e] = c[e];
@@ -712,10 +729,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (uint32_t todo = (uint32_t)(hits >> (b * 32)); todo != 0; todo &= todo - 1) {
           const int r = __builtin_ctz(todo), v = __builtin_amdgcn_readlane(hit, b * 32 + r);
           const bool here = lane == (v & 31) + (r >> 2 & 1) * 32;
-          const int at = (r >> 3) * 4 + (r & 3);
+          const int element = (r >> 3) * 4 + (r & 3);
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const float one = e == at && here ? 1.f : 0.f;
+            const float one = e == element && here ? 1.f : 0.f;
             z[0][e] -= v < 32 ? one : 0.f;
             z[1][e] -= v < 32 ? 0.f : one;
           }
@@ -730,7 +747,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int c = 0; c < KS / 2; ++c) {
-            const u32x4 a = S::transposed(from, b, c, s);
+            const u32x4 a = S::transposed(from, at, b, c, s);
 #pragma unroll
             for (int j = 0; j < 2; ++j) acc[c][j] = mma<T>(a, p[j][s], acc[c][j]);
           }
