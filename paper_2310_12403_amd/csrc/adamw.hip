@@ -115,13 +115,14 @@ __device__ __forceinline__ float code_value(uint32_t code) {  // of the 8-bit fl
 }
 
 // The four codes of a lane; scale: of its block.  `floor`: the code of a value that is not zero is at least this.  The quotients are
-// taken times the reciprocal, off by 2^-22: that moves the bound between two codes by a millionth of their distance.
+// the reciprocal's, made exact by one step: an ulp more or less could take a value over the bound between two codes.
 __device__ __forceinline__ uint32_t encode(const float (&x)[4], float scale, const uint32_t (&noise)[4], uint32_t floor) {
-  const float by = __builtin_amdgcn_rcpf(scale);
+  float by = __builtin_amdgcn_rcpf(scale);
+  by = __builtin_fmaf(__builtin_fmaf(-scale, by, 1.f), by, by);
   uint32_t c = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const float y = x[e] * by;
+    const float q = x[e] * by, y = __builtin_fmaf(__builtin_fmaf(-q, scale, x[e]), by, q);
     const uint32_t bits = __float_as_uint(fabsf(y) * 0x1p-120f);
     uint32_t code = (bits + noise[e]) >> 20;
     code = code < 0x7Eu ? code : 0x7Eu;
@@ -216,15 +217,9 @@ __global__ __launch_bounds__(kBlock) void k_adamw(Step<Tensor> st) {
       if (st.grad_scale != nullptr) g[e] *= gs;
       m[e] = m[e] * st.h.keep1 + g[e] * st.h.take1;
       v[e] = v[e] * st.h.keep2 + (g[e] * g[e]) * st.h.take2;
-      if constexpr (BITS == 32) {
-        root[e] = sqrtf(v[e]);
-        p[e] = p[e] * st.h.decay - (m[e] / (root[e] * st.h.undo + st.h.eps)) * st.h.rate;
-      } else {
-        // The hardware's own root and reciprocal, each within an ulp: the moments behind them are good for four bits, and the exact
-        // quotient and root of four elements were a third of the kernel's instructions (touched rows of 100: 311 us with them).
-        root[e] = v[e] != 0.f ? fmaxf(__builtin_amdgcn_sqrtf(v[e]), 0x1p-75f) : v[e];  // (not zero where v is not)
-        p[e] = p[e] * st.h.decay - (m[e] * __builtin_amdgcn_rcpf(root[e] * st.h.undo + st.h.eps)) * st.h.rate;
-      }
+      root[e] = sqrtf(v[e]);
+      if constexpr (BITS == 32) p[e] = p[e] * st.h.decay - (m[e] / (root[e] * st.h.undo + st.h.eps)) * st.h.rate;
+      else p[e] = p[e] * st.h.decay - (m[e] * __builtin_amdgcn_rcpf(root[e] * st.h.undo + st.h.eps)) * st.h.rate;  // (moments of four bits)
       if (e >= n) m[e] = root[e] = 0.f;
     }
     store4(t.param, t.param_type, at, n, p);

@@ -246,9 +246,10 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_place(SortInput in, int64_t
   }
 }
 
-// n <= kSortTile: all passes
+// n <= kSortTile: all passes, and where the rows form's rows go (RowPlaces: of one tile of chunks)
 __global__ __launch_bounds__(kSortBlock) void k_sort_small(SortInput in, int n, int bits, uint32_t* __restrict__ keys_out,
-                                                           uint32_t* __restrict__ places_out, int32_t* __restrict__ bad) {
+                                                           uint32_t* __restrict__ places_out, uint32_t* __restrict__ in_tile,
+                                                           uint32_t* __restrict__ total, int32_t* __restrict__ bad) {
   extern __shared__ char sort_lds[];
   SortLds* lds = reinterpret_cast<SortLds*>(sort_lds);
   const int base = uniform_wave_in_block() * (kKeysPerThread * kWave) + lane_id();
@@ -266,9 +267,28 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_small(SortInput in, int n, 
     for (int u = 0; u < kKeysPerThread; ++u)
       if (live[u]) x[u] = lds->pair[base + u * kWave];
   }
+  // a wave's 512 tokens are 16 chunks: the rows that begin in each, and in front of it
+  uint32_t heads = 0;  // of chunk `lane` of the wave
 #pragma unroll
-  for (int u = 0; u < kKeysPerThread; ++u)
-    if (live[u]) keys_out[base + u * kWave] = x[u][0], places_out[base + u * kWave] = x[u][1];
+  for (int u = 0; u < kKeysPerThread; ++u) {
+    const int i = base + u * kWave;
+    if (live[u]) keys_out[i] = x[u][0], places_out[i] = x[u][1];
+    const uint64_t m = ballot64(live[u] && x[u][0] != (uint32_t)in.n_rows && (i == 0 || lds->pair[i - 1][0] != x[u][0]));
+    if (lane_id() == 2 * u) heads = (uint32_t)__popcll(m & 0xFFFFFFFFull);
+    if (lane_id() == 2 * u + 1) heads = (uint32_t)__popcll(m >> 32);
+  }
+  if (in_tile == nullptr) return;
+  const uint32_t upto = wave_incl_scan(heads);
+  if (lane_id() == kWave - 1) lds->sums[wave_in_block()] = upto;
+  __syncthreads();
+  uint32_t before = 0, all = 0;
+  for (int w = 0; w < kSortWaves; ++w) {
+    before += w < wave_in_block() ? lds->sums[w] : 0;
+    all += lds->sums[w];
+  }
+  const int chunk = wave_in_block() * (2 * kKeysPerThread) + lane_id();
+  if (lane_id() < 2 * kKeysPerThread && chunk * 32 < n) in_tile[chunk] = before + upto - heads;
+  if (threadIdx.x == 0) *total = all;
 }
 
 // ---- the rows' sums ----------------------------------------------------------------------------------------------------
@@ -293,7 +313,7 @@ struct ReduceShape {
 };
 
 // The rows form: where a chunk's rows go.  A tile's chunks hold the rows that begin in the tile's chunks in front of them, and a tile those
-// in the tiles in front (of one tile only: none).
+// in the tiles in front (null: there is one tile).
 struct RowPlaces {
   const uint32_t *in_tile, *tile;
   const uint32_t* total;
@@ -618,7 +638,8 @@ int grad_launch(const void* dout, int dtype, const int32_t* ids, int64_t n, cons
   uint32_t* places = (uint32_t*)(ws + plan.places);
   if (plan.tiles == 1) {
     if (!allow_sort(k_sort_small)) return COOP_E_HIP;
-    COOP_LAUNCH(K_SORT_PLACE, k_sort_small, dim3(1), dim3(kSortBlock), sizeof(SortLds), s, in, (int)n, bits, keys, places, bad);
+    COOP_LAUNCH(K_SORT_PLACE, k_sort_small, dim3(1), dim3(kSortBlock), sizeof(SortLds), s, in, (int)n, bits, keys, places,
+                rows_form ? (uint32_t*)(ws + plan.in_tile) : nullptr, (uint32_t*)(ws + plan.tile_sum), bad);
   } else if (plan.tiles <= kOwnTiles) {
     if (!allow_sort(k_sort_place<true>)) return COOP_E_HIP;
     sort_passes<true>(plan, ws, in, bits, bad, s);
@@ -630,9 +651,9 @@ int grad_launch(const void* dout, int dtype, const int32_t* ids, int64_t n, cons
   if (rows_form) {
     uint32_t* tile_sum = (uint32_t*)(ws + plan.tile_sum);
     uint32_t* tile = (uint32_t*)(ws + plan.tile);
-    COOP_LAUNCH(K_EMBED_HEADS, k_embed_heads, dim3((unsigned)plan.head_tiles), dim3(kBlock), 0, s, keys, n, (uint32_t)n_rows,
+    const bool one = plan.tiles == 1;  // (k_sort_small has left it)
+    if (!one) COOP_LAUNCH(K_EMBED_HEADS, k_embed_heads, dim3((unsigned)plan.head_tiles), dim3(kBlock), 0, s, keys, n, (uint32_t)n_rows,
                 (uint32_t*)(ws + plan.in_tile), tile_sum);
-    const bool one = plan.head_tiles == 1;
     if (!one) scan_u32_to_u32(tile_sum, plan.head_tiles, tile, ws + plan.scan, s);
     rp = RowPlaces{(const uint32_t*)(ws + plan.in_tile), one ? nullptr : tile, one ? tile_sum : tile + plan.head_tiles};
   }

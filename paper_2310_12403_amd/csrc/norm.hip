@@ -310,13 +310,13 @@ bool norm_layout(int32_t dim, int dtype, NormLayout* out) {
 }
 
 // Blocks of a pass: as many as are on the chip at once (the gradient's registers: 5, 3 or 2 blocks of four waves a CU), and for a
-// gradient no more than leave partial sums of an eighth of x.
+// gradient no more than leave each group two rows.
 int64_t norm_blocks(int64_t rows, const NormLayout& l, bool grad) {
   const int64_t per_block = l.waves == 1 ? kBlock / l.lanes : 1;
   int64_t b = (rows + per_block - 1) / per_block;
   const int64_t each = l.waves == 16 ? (grad ? 1 : 2) : !grad ? 8 : l.k == 1 ? 5 : l.k == 2 ? 3 : 2, most = 256 * each;
   if (b > most) b = most;
-  if (grad && b > rows / 32 + 1) b = rows / 32 + 1;
+  if (grad && b > rows / (2 * per_block) + 1) b = rows / (2 * per_block) + 1;
   return b;
 }
 

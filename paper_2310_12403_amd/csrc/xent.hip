@@ -211,10 +211,11 @@ __device__ __forceinline__ void put_columns(char* out, int64_t row, int64_t c, i
   char* to = out + (row * dim + c) * kElem<T>;
   if (c + 4 <= dim) {
     put4<T>(to, f);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (c + e < dim) ((typename Element<T>::M*)to)[e] = (typename Element<T>::M)f[e];
+  } else if (c < dim) {  // (one to three)
+    typename Element<T>::M* at = (typename Element<T>::M*)to;
+    at[0] = (typename Element<T>::M)f[0];
+    if (c + 1 < dim) at[1] = (typename Element<T>::M)f[1];
+    if (c + 2 < dim) at[2] = (typename Element<T>::M)f[2];
   }
 }
 
@@ -313,24 +314,38 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
       }
 }
 
-// out[row, :] = the splits' sums of the row, times *unlift
+// out[row, :] = the splits' sums of the row, times *unlift.  A block has 64 packs of four columns; its waves deal the splits among
+// themselves, and the first adds up what they have, in their order.
+constexpr int kOutWaves = 8;
 template <int T>
-__global__ __launch_bounds__(kBlock) void k_xent_out(const float* __restrict__ sums, int splits, int64_t rows, int32_t width, int64_t n,
-                                                     int32_t dim, const float* __restrict__ unlift, char* __restrict__ out) {
-  const int64_t step = (int64_t)gridDim.x * kBlock;
+__global__ __launch_bounds__(kOutWaves* kWave) void k_xent_out(const float* __restrict__ sums, int splits, int64_t rows, int32_t width, int64_t n,
+                                                               int32_t dim, const float* __restrict__ unlift, char* __restrict__ out) {
+  __shared__ float lds[4][kOutWaves][kWave];
   const int32_t packs = (dim + 3) / 4;
   const float u = *unlift;
-  for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < n * packs; i += step) {
-    const int64_t row = i / packs;
+  const int wave = uniform_wave_in_block(), lane = lane_id();
+  for (int64_t first = (int64_t)blockIdx.x * kWave; first < n * packs; first += (int64_t)gridDim.x * kWave) {
+    const int64_t i = first + lane, row = i / packs;
     const int32_t c = (int32_t)(i - row * packs) * 4;
+    const bool live = row < n;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
+    if (live) {
 #pragma unroll 4
-    for (int q = 0; q < splits; ++q) {
-      float f[4];
-      load_elements<COOP_F32, 4>(sums + ((int64_t)q * rows + row) * width + c, f);
+      for (int q = wave; q < splits; q += kOutWaves) {
+        float f[4];
+        load_elements<COOP_F32, 4>(sums + ((int64_t)q * rows + row) * width + c, f);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] += f[e];
+        for (int e = 0; e < 4; ++e) s[e] += f[e];
+      }
     }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) lds[e][wave][lane] = s[e];
+    __syncthreads();
+    if (wave != 0 || !live) continue;
+    for (int w = 1; w < kOutWaves && w < splits; ++w)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += lds[e][w][lane];
 #pragma unroll
     for (int e = 0; e < 4; ++e) s[e] *= u;
     put_columns<T>(out, row, c, dim, s);
@@ -614,7 +629,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const bool ragged = v0 + S::kRows > vocab;
     stream.stage([&](const char* from) {
       const typename S::Reads at = reads.again();
-#pragma unroll
+#pragma unroll 1
       for (int b = 0; b < 2; ++b) {
         f32x16 z[2];
         u32x4 p[2][2];
@@ -641,7 +656,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
           if (ragged) {  // (rows of W that are not there are zeros in the next product, but an exponential may be infinite)
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-              if (b * 32 + row_of(e) >= left) z[j][e] = 0.f;
+              if (row_of(e) >= left - b * 32) z[j][e] = 0.f;
           }
           pack<T>(z[j], p[j]);
         }
@@ -699,7 +714,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       const float* coef = lse2 + 64;
       const int hit = reinterpret_cast<const int32_t*>(coef + 64)[lane] - (int)v0;  // of row `lane` of the stage
       const uint64_t hits = ballot64((uint32_t)hit < 64u);
-#pragma unroll
+#pragma unroll 1
       for (int b = 0; b < 2; ++b) {
         f32x16 z[2];
         u32x4 p[2][2];
@@ -802,17 +817,15 @@ __global__ __launch_bounds__(kBlock) void k_xent_pad(const char* __restrict__ in
 // ---- the workspace ---------------------------------------------------------------------------------------------------------
 constexpr int64_t kPieceBytes = (int64_t)512 << 20;  // of G
 constexpr int64_t kMaxVocab = 0x7FFFF000;            // (a tile's row numbers stay below 2^31)
-// Rows of a block's tile, either way, and of a wave's: in 16 bits what the registers hold, since the matrix units then take all that LDS
-// gives; in 32 bits they are sixteen times slower and smaller tiles, two blocks on a CU, fill the chip better.
-template <int T> constexpr int kWaveTiles = T == COOP_F32 ? 2 : 4;
-constexpr int tile_rows(int dtype) { return dtype == COOP_F32 ? 128 : 256; }
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 // How a call is cut, and what of the workspace it uses for what.
 //   few:    up to 32 rows.  W is read once and that is all there is to it: tiles of 32 rows of H, as many blocks as there are tiles of W.
 //   narrow: more rows, of up to 128 elements of 16 bits (above).
-//   else products in tiles, a piece of the vocabulary at a time.
+//   else products in tiles, a piece of the vocabulary at a time.  Of 256 x 256, what a wave's registers hold, where there are enough of
+//   them for the chip: the matrix units then take all that LDS gives.  Else, and in fp32, where they are sixteen times slower, of
+//   128 x 128, two blocks on a CU (2,236 rows, 170 vertices, 768 elements of bf16: 148 -> @A us).  Few rows' gradients take tiles of 32 rows.
 struct XentPlan {
   int64_t n, vocab, width, ld;  // width: elements of a padded row
   int64_t rows, piece, vocab_rows;
@@ -827,11 +840,11 @@ struct XentPlan {
     ld = width * es;
     pad = !aligned || width != dim;
     narrow = es == 2 && width <= 128 && (grad || n > 32);
-    few = n <= 32 && !grad;
-    tile = tile_rows(dtype);
-    rows = round_up(n, tile);
-    const int blocks = 256 * (narrow || dtype == COOP_F32 ? 2 : 1);
-    const int64_t row_tiles = rows / tile, vocab_tiles = (vocab + tile - 1) / tile;
+    few = n <= 32 && !narrow;
+    tile = narrow || few || (es == 2 && ((n + 255) / 256) * ((vocab + 255) / 256) >= 256) ? 256 : 128;
+    rows = few ? 32 : round_up(n, tile);
+    const int blocks = 256 * (narrow || few || tile == 128 ? 2 : 1);
+    const int64_t row_tiles = few ? 1 : rows / tile, vocab_tiles = (vocab + tile - 1) / tile;
     vocab_rows = vocab_tiles * tile;
     // blocks: two of a narrow kernel or of few rows on a CU, one of the others; a multiple of 8 splits where there are so many, so that
     // the blocks of an XCD have the same splits' tiles of W
@@ -919,8 +932,10 @@ int forward(const XentPlan& p, const void* hidden, const void* weight, int32_t d
   bool ok = true;
   if (p.few) {
     ok = launch_stats<T, 4, 1, 2, 1>(p, w, h, alpha, targets, part, s);
+  } else if (!p.narrow && p.tile == 128) {
+    ok = launch_stats<T, 2, 2, 2, 2>(p, w, h, alpha, targets, part, s);
   } else if (!p.narrow) {
-    ok = launch_stats<T, 2, 2, kWaveTiles<T>, kWaveTiles<T>>(p, w, h, alpha, targets, part, s);
+    if constexpr (T != COOP_F32) ok = launch_stats<T, 2, 2, 4, 4>(p, w, h, alpha, targets, part, s);
   } else if constexpr (T != COOP_F32) {
     with_steps(p.width, [&](auto ks) {
       constexpr int KS = decltype(ks)::value, lds = RowStream<T, KS, false>::kLds;
@@ -939,8 +954,8 @@ int forward(const XentPlan& p, const void* hidden, const void* weight, int32_t d
 
 template <int T>
 void write_out(const float* sums, int splits, int64_t rows, const XentPlan& p, int64_t n, int32_t dim, const float* unlift, void* out, hipStream_t s) {
-  const int64_t blocks = (n * ((dim + 3) / 4) + kBlock - 1) / kBlock;
-  COOP_LAUNCH(K_XENT_OUT, k_xent_out<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(kBlock), 0, s, sums, splits, rows, (int32_t)p.width, n, dim,
+  const int64_t blocks = (n * ((dim + 3) / 4) + kWave - 1) / kWave;
+  COOP_LAUNCH(K_XENT_OUT, k_xent_out<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(kOutWaves * kWave), 0, s, sums, splits, rows, (int32_t)p.width, n, dim,
               unlift, (char*)out);
 }
 
@@ -969,6 +984,42 @@ bool backward_narrow(const XentPlan& p, const Operand& w, const Operand& h, int3
   return ok;
 }
 
+// tiles of W's (or G's) rows or columns by H's rows: WA x WB waves of TA x TB; the weight's gradient in square ones
+template <int T, int WA, int WB, int TA, int TB>
+bool backward_pieces(const XentPlan& p, const Operand& w, const Operand& h, int32_t dim, float alpha, const RowTerms& term, const float* unlift,
+                     void* dhidden, void* dweight, char* g, float* sums, hipStream_t s) {
+  constexpr int N = TA == 4 ? 4 : 2;
+  typedef Product<T, WA, WB, TA, TB, false, false, kWide> G;
+  typedef Product<T, WA, WB, TA, TB, true, false, kWide> H;
+  typedef Product<T, 2, 2, N, N, true, true, kNarrow> W;
+  const auto kg = k_xent_g<T, WA, WB, TA, TB>;
+  const auto kh = k_xent_dh<T, WA, WB, TA, TB>;
+  const auto kw = k_xent_dw<T, 2, 2, N, N>;
+  if (!allow_lds(kg, G::kLds) || !allow_lds(kh, H::kLds) || !allow_lds(kw, W::kLds)) return false;
+  const auto tiles_of = [](int64_t n, int rows) { return (uint32_t)((n + rows - 1) / rows); };
+  const uint32_t row_tiles = tiles_of(p.n, G::kRowsB), col_tiles = tiles_of(p.width, H::kRowsA), w_tiles = tiles_of(p.width, W::kRowsA);
+  for (int64_t v = 0; v < p.vocab; v += p.piece) {
+    const int64_t len = p.vocab - v < p.piece ? p.vocab - v : p.piece;
+    const uint32_t tiles = tiles_of(len, G::kRowsA);
+    COOP_LAUNCH(K_XENT_G, kg, dim3(tiles * row_tiles), dim3(G::kThreads), G::kLds, s, w, h, p.vocab, p.width, alpha * kLog2e, v, tiles, term, g, p.g_ld);
+    const int64_t g_bytes = (int64_t)tiles * G::kRowsA * kElem<T>;
+    if (dhidden != nullptr) {
+      const Operand wt{w.base + v * p.ld, p.ld, p.ld, len}, gi{g, p.g_ld, p.rows, g_bytes};
+      // (every split has something to do: the last piece may be too short for all of them, and then adds nothing to the others' sums)
+      const int64_t stages = (len + H::kK - 1) / H::kK;
+      const int splits = (int)(p.dh_splits < stages ? p.dh_splits : stages);
+      COOP_LAUNCH(K_XENT_DH, kh, dim3(row_tiles * col_tiles * splits), dim3(H::kThreads), H::kLds, s, wt, gi, len, splits, col_tiles, row_tiles,
+                  v != 0, sums, p.width);
+    }
+    if (dweight != nullptr) {
+      const Operand ht{h.base, p.ld, p.ld, p.n}, gt{g, p.g_ld, g_bytes, p.rows};
+      COOP_LAUNCH(K_XENT_DW, kw, dim3(tiles_of(len, W::kRowsB) * w_tiles), dim3(W::kThreads), W::kLds, s, ht, gt, p.n, p.vocab, v, dim, w_tiles, unlift,
+                  (char*)dweight);
+    }
+  }
+  return true;
+}
+
 template <int T>
 int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t dim, const int32_t* targets, float alpha, int32_t ignore,
              const float* lse, const float* dloss, void* dhidden, void* dweight, char* ws, int32_t* bad, hipStream_t s) {
@@ -989,32 +1040,18 @@ int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t 
       if (!backward_narrow<T>(p, w, h, dim, alpha, term, unlift, dhidden, dweight, sums, s)) return COOP_E_HIP;
       return hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
     }
-  char* g = ws + p.g;
-  constexpr int N = kWaveTiles<T>;
-  typedef Product<T, 2, 2, N, N, false, false, kWide> P;
-  const auto kg = k_xent_g<T, 2, 2, N, N>;
-  const auto kh = k_xent_dh<T, 2, 2, N, N>;
-  const auto kw = k_xent_dw<T, 2, 2, N, N>;
-  if (!allow_lds(kg, P::kLds) || !allow_lds(kh, P::kLds) || !allow_lds(kw, P::kLds)) return COOP_E_HIP;
-  const uint32_t row_tiles = (uint32_t)(p.rows / p.tile), col_tiles = (uint32_t)((p.width + p.tile - 1) / p.tile);
-  for (int64_t v = 0; v < p.vocab; v += p.piece) {
-    const int64_t len = p.vocab - v < p.piece ? p.vocab - v : p.piece;
-    const uint32_t tiles = (uint32_t)((len + p.tile - 1) / p.tile);
-    COOP_LAUNCH(K_XENT_G, kg, dim3(tiles * row_tiles), dim3(P::kThreads), P::kLds, s, w, h, p.vocab, p.width, alpha * kLog2e, v, tiles, term, g, p.g_ld);
-    if (dhidden != nullptr) {
-      const Operand wt{(const char*)weight + v * p.ld, p.ld, p.ld, len}, gi{g, p.g_ld, p.rows, (int64_t)tiles * p.tile * kElem<T>};
-      // (every split has something to do: the last piece may be too short for all of them, and then adds nothing to the others' sums)
-      const int64_t stages = (len + P::kK - 1) / P::kK;
-      const int splits = (int)(p.dh_splits < stages ? p.dh_splits : stages);
-      COOP_LAUNCH(K_XENT_DH, kh, dim3(row_tiles * col_tiles * splits), dim3(P::kThreads), P::kLds, s, wt, gi, len, splits, col_tiles, row_tiles,
-                  v != 0, sums, p.width);
-    }
-    if (dweight != nullptr) {
-      const Operand ht{(const char*)hidden, p.ld, p.ld, p.n}, gt{g, p.g_ld, (int64_t)tiles * p.tile * kElem<T>, p.rows};
-      COOP_LAUNCH(K_XENT_DW, kw, dim3(tiles * col_tiles), dim3(P::kThreads), P::kLds, s, ht, gt, p.n, p.vocab, v, dim, col_tiles,
-                  (const float*)unlift, (char*)dweight);
-    }
-  }
+  bool ok = true;
+  const auto pieces = [&](auto wa, auto wb, auto ta, auto tb) {
+    ok = backward_pieces<T, decltype(wa)::value, decltype(wb)::value, decltype(ta)::value, decltype(tb)::value>(p, w, h, dim, alpha, term, unlift, dhidden,
+                                                                                                       dweight, ws + p.g, sums, s);
+  };
+  typedef std::integral_constant<int, 1> One;
+  typedef std::integral_constant<int, 2> Two;
+  typedef std::integral_constant<int, 4> Four;
+  if (p.few) pieces(Four(), One(), Two(), One());
+  else if (p.tile == 128) pieces(Two(), Two(), Two(), Two());
+  else if constexpr (T != COOP_F32) pieces(Two(), Two(), Four(), Four());
+  if (!ok) return COOP_E_HIP;
   if (dhidden != nullptr) write_out<T>(sums, p.dh_splits, p.rows, p, p.n, dim, unlift, dhidden, s);
   return hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
 }

@@ -236,19 +236,19 @@ class AdamW:
             state = {x: [torch.zeros(s if x.endswith("scale") else p.numel(), dtype=torch.float32 if x.endswith("scale") else kind, device=p.device)
                          for p, s in zip(self.params, scales)] for x in names}
         self.state = {x: list(state[x]) for x in names}
-        for x in names:
-            assert len(self.state[x]) == n
-            for t, p, s in zip(self.state[x], self.params, scales):
-                want, count = (torch.float32, s) if x.endswith("scale") else (kind, p.numel())
-                assert t.is_cuda and t.is_contiguous() and t.dtype == want and t.numel() == count, "%s of a parameter: %d %s" % (x, count, want)
+        assert all(len(self.state[x]) == n for x in names)
         self._c = (_CAdamWTensor * max(n, 1))()
-        for i, p in enumerate(self.params):
-            c, copy = self._c[i], self.copies[i]
-            c.param, c.param_dtype, (c.n_rows, c.dim) = p.data_ptr(), _DTYPES[p.dtype], self.shapes[i]
-            for x in names:
-                setattr(c, x, self.state[x][i].data_ptr())
+        for c, p, copy, shape, s, *mine in zip(self._c, self.params, self.copies, self.shapes, scales, *(self.state[x] for x in names)):
+            k = p.numel()
+            for i, t in enumerate(mine):
+                assert t.is_cuda and t.is_contiguous() and t.dtype == (kind if i < 2 else torch.float32) and t.numel() == (k if i < 2 else s), \
+                    "%s of a parameter: %d %s" % (names[i], k if i < 2 else s, kind if i < 2 else torch.float32)
+            c.param, c.param_dtype, c.n_rows, c.dim = p.data_ptr(), _DTYPES[p.dtype], *shape
+            c.m, c.v = mine[0].data_ptr(), mine[1].data_ptr()
+            if bits == 8:
+                c.m_scale, c.v_scale = mine[2].data_ptr(), mine[3].data_ptr()
             if copy is not None:
-                assert copy.is_cuda and copy.is_contiguous() and copy.numel() == p.numel() and copy.dtype in _DTYPES
+                assert copy.is_cuda and copy.is_contiguous() and copy.numel() == k and copy.dtype in _DTYPES
                 c.copy, c.copy_dtype = copy.data_ptr(), _DTYPES[copy.dtype]
         self.set_grads([None] * n if grads is None else grads)
 
@@ -275,7 +275,7 @@ class AdamW:
             _matrix(g, "row gradients", ids.numel(), dim)
             c = self._c[i]
             c.n_rows, c.dim, c.grad, c.grad_dtype = n_rows, dim, g.data_ptr(), _DTYPES[g.dtype]
-            c.rows, c.n_list = _vector(ids, ids.numel(), torch.int32, "rows") or 1, ids.numel()
+            c.rows, c.n_list = _vector(ids, ids.numel(), torch.int32, "rows") or 1, ids.numel()  # (an empty list has no address)
             c.n_list_dev = None if count is None else _vector(count, 1, torch.int32, "count")
         gs = None if grad_scale is None else _vector(grad_scale, 1, torch.float32, "grad_scale")
         try:
