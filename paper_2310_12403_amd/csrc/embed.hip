@@ -291,6 +291,44 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_small(SortInput in, int n, 
   if (threadIdx.x == 0) *total = all;
 }
 
+// n <= kFewTokens: a token's place is the number of those in front of it, one comparison each; 512 of them, ids of 19 bits: 6 us, three
+// passes by digits 22.
+constexpr int kFewTokens = 512;
+__global__ __launch_bounds__(kFewTokens) void k_sort_few(SortInput in, int n, uint32_t* __restrict__ keys_out, uint32_t* __restrict__ places_out,
+                                                         uint32_t* __restrict__ in_tile, uint32_t* __restrict__ total, int32_t* __restrict__ bad) {
+  __shared__ __attribute__((aligned(16))) uint32_t key[kFewTokens];
+  __shared__ uint32_t sorted[kFewTokens];
+  __shared__ uint32_t heads[2 * kFewTokens / kWave];
+  const int i = threadIdx.x;
+  bool wrong = false;
+  const uint32_t mine = i < n ? in.at(i, &wrong)[0] : 0xFFFFFFFFu;  // (larger than any key)
+  if (wrong) atomicOr(bad, 1);
+  key[i] = mine;
+  __syncthreads();
+  uint32_t rank = 0;
+#pragma unroll 4
+  for (int j = 0; j < n; j += 4) {
+    const u32x4 k = *reinterpret_cast<const u32x4*>(key + j);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) rank += k[e] < mine || (k[e] == mine && j + e < i) ? 1u : 0u;
+  }
+  if (i < n) {
+    sorted[rank] = mine;
+    keys_out[rank] = mine;
+    places_out[rank] = (uint32_t)i;
+  }
+  if (in_tile == nullptr) return;
+  __syncthreads();
+  const uint64_t m = ballot64(i < n && sorted[i] != (uint32_t)in.n_rows && (i == 0 || sorted[i - 1] != sorted[i]));
+  if ((lane_id() & 31) == 0) heads[i / 32] = (uint32_t)__popcll(lane_id() == 0 ? m & 0xFFFFFFFFull : m >> 32);
+  __syncthreads();
+  if (i > 2 * kFewTokens / kWave) return;
+  uint32_t before = 0;
+  for (int c = 0; c < i; ++c) before += heads[c];
+  if (i * 32 < n) in_tile[i] = before;
+  if (i == 2 * kFewTokens / kWave) *total = before;
+}
+
 // ---- the rows' sums ----------------------------------------------------------------------------------------------------
 // The sorted tokens are cut into chunks of kChunk, each summed by a group of lanes that holds a row's columns (E of them each; wider
 // rows in column tiles, blockIdx.y).  What begins and ends inside a chunk is written as it is; a row whose tokens run over a chunk's
@@ -636,7 +674,10 @@ int grad_launch(const void* dout, int dtype, const int32_t* ids, int64_t n, cons
   const SortInput in{ids, nullptr, n_rows, pad};
   uint32_t* keys = (uint32_t*)(ws + plan.keys);
   uint32_t* places = (uint32_t*)(ws + plan.places);
-  if (plan.tiles == 1) {
+  if (n <= kFewTokens) {
+    COOP_LAUNCH(K_SORT_PLACE, k_sort_few, dim3(1), dim3(kFewTokens), 0, s, in, (int)n, keys, places,
+                rows_form ? (uint32_t*)(ws + plan.in_tile) : nullptr, (uint32_t*)(ws + plan.tile_sum), bad);
+  } else if (plan.tiles == 1) {
     if (!allow_sort(k_sort_small)) return COOP_E_HIP;
     COOP_LAUNCH(K_SORT_PLACE, k_sort_small, dim3(1), dim3(kSortBlock), sizeof(SortLds), s, in, (int)n, bits, keys, places,
                 rows_form ? (uint32_t*)(ws + plan.in_tile) : nullptr, (uint32_t*)(ws + plan.tile_sum), bad);
@@ -651,7 +692,7 @@ int grad_launch(const void* dout, int dtype, const int32_t* ids, int64_t n, cons
   if (rows_form) {
     uint32_t* tile_sum = (uint32_t*)(ws + plan.tile_sum);
     uint32_t* tile = (uint32_t*)(ws + plan.tile);
-    const bool one = plan.tiles == 1;  // (k_sort_small has left it)
+    const bool one = plan.tiles == 1;  // (the sort has left it)
     if (!one) COOP_LAUNCH(K_EMBED_HEADS, k_embed_heads, dim3((unsigned)plan.head_tiles), dim3(kBlock), 0, s, keys, n, (uint32_t)n_rows,
                 (uint32_t*)(ws + plan.in_tile), tile_sum);
     if (!one) scan_u32_to_u32(tile_sum, plan.head_tiles, tile, ws + plan.scan, s);
