@@ -157,24 +157,47 @@ struct RowTerms { float *coef, *lse2; int32_t* target; };
 // In 16 bits G holds coef over the largest |coef| (and times 2^13 in fp16, whose exponents would otherwise not reach from 1 to a
 // probability times dloss): where all rows count alike, as in a mean, the factor is 1 (a power of two), and so a target's p - 1 of a
 // small p is not rounded away from -1 twice; with dloss itself in G, dH and dW of the mean were off by 3.0e-3 instead of 2.0e-3 (bf16).
+template <int T>
+constexpr float kLift = T == COOP_F16 ? 13.f : 0.f;
+template <int T>
+constexpr float kOne = T == COOP_F16 ? 8192.f : 1.f;
+
+// the largest |coef| among the rows first, first + step, .. that count, of a block
+__device__ __forceinline__ float block_top(const int32_t* __restrict__ targets, int32_t ignore, const float* __restrict__ dloss, float alpha,
+                                           int64_t first, int64_t step, int64_t n, int64_t vocab) {
+  __shared__ float lds[16];
+  float top = 0.f;
+  for (int64_t i = first; i < n; i += step) {
+    const int32_t t = targets[i];
+    const float c = fabsf(alpha * dloss[i]);
+    if (t != ignore && (uint64_t)(int64_t)t < (uint64_t)vocab && c < __builtin_inff()) top = fmaxf(top, c);
+  }
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
+  if (lane_id() == 0) lds[wave_in_block()] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 16; ++w) top = fmaxf(top, lds[w]);
+  return top;
+}
+
+// Up to kTopRows rows every block of k_xent_terms looks for the largest itself, which costs less than a launch; of more rows, up to 256
+// blocks do, and it looks through theirs.
+constexpr int64_t kTopRows = 32768;
+__global__ __launch_bounds__(1024) void k_xent_top(const int32_t* __restrict__ targets, int32_t ignore, const float* __restrict__ dloss, float alpha,
+                                                   int64_t n, int64_t vocab, float* __restrict__ tops) {
+  const float top = block_top(targets, ignore, dloss, alpha, (int64_t)blockIdx.x * 1024 + threadIdx.x, (int64_t)gridDim.x * 1024, n, vocab);
+  if (threadIdx.x == 0) tops[blockIdx.x] = top;
+}
+
 template <bool LIFT>
 __global__ __launch_bounds__(1024) void k_xent_terms(const int32_t* __restrict__ targets, int32_t ignore, const float* __restrict__ lse,
                                                      const float* __restrict__ dloss, float alpha, float most, int64_t n, int64_t rows, int64_t vocab,
-                                                     RowTerms term, float* __restrict__ unlift, int32_t* __restrict__ bad) {
-  __shared__ float lds[16];
+                                                     const float* __restrict__ tops, int n_tops, RowTerms term, float* __restrict__ unlift, int32_t* __restrict__ bad) {
   float top = 0.f;
-  if constexpr (LIFT) {  // (every block looks at all rows: no second launch, and n floats are little)
-    for (int64_t i = threadIdx.x; i < n; i += 1024) {
-      const int32_t t = targets[i];
-      const float c = fabsf(alpha * dloss[i]);
-      if (t != ignore && (uint64_t)(int64_t)t < (uint64_t)vocab && c < __builtin_inff()) top = fmaxf(top, c);
-    }
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
-    if (lane_id() == 0) lds[wave_in_block()] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < 16; ++w) top = fmaxf(top, lds[w]);
+  if constexpr (LIFT) {
+    if (n_tops == 0) top = block_top(targets, ignore, dloss, alpha, threadIdx.x, 1024, n, vocab);
+    for (int b = 0; b < n_tops; ++b) top = fmaxf(top, tops[b]);
     if (top < 0x1p-100f) top = 0x1p-100f;
     if (top > 0x1p100f) top = 0x1p100f;
   }
@@ -314,38 +337,40 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
       }
 }
 
-// out[row, :] = the splits' sums of the row, times *unlift.  A block has 64 packs of four columns; its waves deal the splits among
-// themselves, and the first adds up what they have, in their order.
+// out[row, :] = the splits' sums of the row, times *unlift.  A wave has 64 packs of four columns; where there are many splits the block's
+// waves deal those of the same packs among themselves (`share` of them), and the first adds up what they have, in their order.
 constexpr int kOutWaves = 8;
 template <int T>
-__global__ __launch_bounds__(kOutWaves* kWave) void k_xent_out(const float* __restrict__ sums, int splits, int64_t rows, int32_t width, int64_t n,
-                                                               int32_t dim, const float* __restrict__ unlift, char* __restrict__ out) {
+__global__ __launch_bounds__(kOutWaves* kWave) void k_xent_out(const float* __restrict__ sums, int splits, int share, int64_t rows, int32_t width,
+                                                               int64_t n, int32_t dim, const float* __restrict__ unlift, char* __restrict__ out) {
   __shared__ float lds[4][kOutWaves][kWave];
   const int32_t packs = (dim + 3) / 4;
   const float u = *unlift;
-  const int wave = uniform_wave_in_block(), lane = lane_id();
-  for (int64_t first = (int64_t)blockIdx.x * kWave; first < n * packs; first += (int64_t)gridDim.x * kWave) {
-    const int64_t i = first + lane, row = i / packs;
+  const int wave = uniform_wave_in_block(), lane = lane_id(), mine = wave % share, each = kOutWaves / share * kWave;
+  for (int64_t first = (int64_t)blockIdx.x * each; first < n * packs; first += (int64_t)gridDim.x * each) {
+    const int64_t i = first + wave / share * kWave + lane, row = i / packs;
     const int32_t c = (int32_t)(i - row * packs) * 4;
     const bool live = row < n;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
     if (live) {
 #pragma unroll 4
-      for (int q = wave; q < splits; q += kOutWaves) {
+      for (int q = mine; q < splits; q += share) {
         float f[4];
         load_elements<COOP_F32, 4>(sums + ((int64_t)q * rows + row) * width + c, f);
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[e] += f[e];
       }
     }
-    __syncthreads();
+    if (share > 1) {
+      __syncthreads();
 #pragma unroll
-    for (int e = 0; e < 4; ++e) lds[e][wave][lane] = s[e];
-    __syncthreads();
-    if (wave != 0 || !live) continue;
-    for (int w = 1; w < kOutWaves && w < splits; ++w)
+      for (int e = 0; e < 4; ++e) lds[e][wave][lane] = s[e];
+      __syncthreads();
+    }
+    if (mine != 0 || !live) continue;
+    for (int w = 1; w < share; ++w)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] += lds[e][w][lane];
+      for (int e = 0; e < 4; ++e) s[e] += lds[e][wave + w][lane];
 #pragma unroll
     for (int e = 0; e < 4; ++e) s[e] *= u;
     put_columns<T>(out, row, c, dim, s);
@@ -392,33 +417,31 @@ struct RowStage {
     const int r0 = row & 1, r1 = row >> 1 & 1, r2 = row >> 2 & 1, r3 = row >> 3 & 1;
     return KS == 8 ? r2 | r0 << 1 | r1 << 2 | r3 << 3 : KS == 4 ? r2 | (r0 ^ r3) << 1 | r1 << 2 : r2 | (r1 ^ r3) << 1;
   }
-  // A lane's place in what it reads; from step to step and tile to tile it is an exclusive or with a few bits.  (Taken anew every stage: the
-  // places of all reads, kept in registers, do not fit beside the rows and sums.)
-  struct Reads {
+  // A lane's places in what it reads (from step to step and tile to tile they are an exclusive or with a few bits) and in what it loads:
+  // 16 bytes of a row, the other loads of a stage in the same chunk as many rows further on.
+  struct Places {
     uint32_t rows, across;
-    __device__ __forceinline__ Reads() {
-      const int lane = lane_id(), r = lane & 31, b = lane >> 4, t = lane & 15, q = (b >> 1) * 4 + (t >> 2), c = (b & 1) * 16 + (t & 3) * 4;
+    int load;
+    __device__ __forceinline__ Places() {}
+    __device__ __forceinline__ Places(int wave, int lane, int ld) {
+      const int r = lane & 31, b = lane >> 4, t = lane & 15, q = (b >> 1) * 4 + (t >> 2), c = (b & 1) * 16 + (t & 3) * 4;
       rows = (uint32_t)(r * kRowBytes + (((lane >> 5) ^ swizzle(r)) << 4));
       across = (uint32_t)(q * kRowBytes + (((c >> 3) ^ swizzle(q)) << 4) + (c & 7) * 2);
-    }
-    __device__ __forceinline__ Reads again() const {
-      Reads x = *this;
-#ifdef __HIP_DEVICE_COMPILE__
-      asm volatile("" : "+v"(x.rows), "+v"(x.across));
-#endif
-      return x;
+      const int place = wave * kWave + lane, row = place / kChunks, chunk = (place % kChunks) ^ swizzle(row);
+      static_assert(4096 / kRowBytes % 16 == 0, "the exchange of chunks goes by the row's last four bits");
+      load = chunk * 16 < ld ? row * ld + chunk * 16 : 0x3FFFFFFF;
     }
   };
   // rows block * 32 + .., elements kk * 16 + ..: a fragment with the elements as k
-  static __device__ __forceinline__ u32x4 fragment(const char* lds, const Reads& at, int block, int kk) {
-    return *reinterpret_cast<const u32x4*>(lds + (at.rows ^ (uint32_t)(kk << 5)) + block * 32 * kRowBytes);
+  static __device__ __forceinline__ u32x4 fragment(const char* lds, uint32_t rows, int block, int kk) {
+    return *reinterpret_cast<const u32x4*>(lds + (rows ^ (uint32_t)(kk << 5)) + block * 32 * kRowBytes);
   }
   // elements tile * 32 + .., with 16 of the block's rows as k, in the order in which a lane's registers hold the rows of a product
-  static __device__ __forceinline__ u32x4 transposed(const char* lds, const Reads& at, int block, int tile, int s) {
+  static __device__ __forceinline__ u32x4 transposed(const char* lds, uint32_t across, int block, int tile, int s) {
     u32x4 f;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      const char* from = lds + (at.across ^ (uint32_t)((tile << 6) ^ ((swizzle(q * 8) & (kChunks - 1)) << 4))) + (block * 32 + s * 16 + q * 8) * kRowBytes;
+      const char* from = lds + (across ^ (uint32_t)((tile << 6) ^ ((swizzle(q * 8) & (kChunks - 1)) << 4))) + (block * 32 + s * 16 + q * 8) * kRowBytes;
       const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(LdsByte*)from));
       f[2 * q] = y[0];
       f[2 * q + 1] = y[1];
@@ -427,41 +450,55 @@ struct RowStage {
   }
 };
 
+// lane_id(), of which the compiler does not know that it stays the same: what is made of it is made again where it is used, and not kept
+__device__ __forceinline__ int lane_anew() {
+  uint32_t none = 0;
+#ifdef __HIP_DEVICE_COMPILE__
+  asm volatile("" : "+s"(none));
+#endif
+  return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, none));
+}
+
 // The stages of rows first, first + step, .. of an operand, four in LDS as in Product; with TERMS the rows' coef, lse2 and target go with
-// them.  Four waves.
-template <int T, int KS, bool TERMS>
+// them.  Four waves.  SUMS: the waves keep sums beside their rows, and there are no registers for the lanes' places: they lie in LDS, and are
+// read each stage.  (Spilled, a wait for them would be a wait for the loads of the stages ahead; made anew they cost 4% of dW's time.)
+template <int T, int KS, bool TERMS, bool SUMS>
 struct RowStream {
   typedef RowStage<T, KS> S;
-  static constexpr int kStages = 4, kStage = S::kBytes + (TERMS ? 1024 : 0), kLds = kStages * kStage, kLoads = S::kMine + (TERMS ? 1 : 0);
-  const char* base;
-  int64_t next, step, end;
-  int ld, at;  // a lane's first load of a stage; the others are as many rows further on, in the same chunk
-  const char* terms;
-  int slot;
+  static constexpr int kStages = 4, kStage = S::kBytes + (TERMS ? 1024 : 0), kLds = kStages * kStage + (SUMS ? 4096 : 0), kLoads = S::kMine + (TERMS ? 1 : 0);
+  const char* base;   // of the next stage
+  const char* terms;  // of its rows: a wave has one of the three arrays (the last one the first again: all waves have as many loads)
+  int left, step;     // rows that there are from the next stage's first (or less than none); from stage to stage
+  int ld, wave, slot;
+  typename S::Places kept;
   char* lds;
-  __device__ __forceinline__ void start(char* __restrict__ into) {
-    const int64_t there = end - next;
-    const int rows = there < 0 ? 0 : there < S::kRows ? (int)there : S::kRows;
-    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(base + next * ld), 0, rows * ld, 0x00020000);
-    const int wave = uniform_wave_in_block();
+  __device__ __forceinline__ u32x4* mine() const { return reinterpret_cast<u32x4*>(lds + kStages * kStage) + wave * kWave + lane_anew(); }
+  __device__ __forceinline__ void start(char* __restrict__ into, int at) {
 #pragma unroll
-    for (int i = 0; i < S::kMine; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(LdsByte*)(into + (i * 4 + wave) * 1024), 16, at + i * (4096 / S::kRowBytes) * ld, 0, 0, 0);
-    if constexpr (TERMS) {  // a wave has one of the three arrays (the last one the first again: all waves have as many loads)
-      const auto tr = __builtin_amdgcn_make_buffer_rsrc((void*)(terms + next * 4), 0, rows * 4, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(tr, (__attribute__((address_space(3))) void*)(LdsByte*)(into + S::kBytes + (wave == 3 ? 0 : wave) * 256), 4,
-                                               lane_id() * 4, 0, 0, 0);
+    for (int i = 0; i < S::kMine; ++i) {  // (a buffer for each: the places further on would take registers that there are not)
+      const int skip = i * (4096 / S::kRowBytes), there = left < S::kRows ? left - skip : S::kRows - skip;
+      const int bytes = __builtin_amdgcn_readfirstlane(there > 0 ? there * ld : 0);
+      const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(base + skip * ld), 0, bytes, 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(LdsByte*)(into + (i * 4 + wave) * 1024), 16, at, 0, 0, 0);
     }
-    next += step;
+    if constexpr (TERMS) {  // (arrays padded to 256 rows)
+      const auto tr = __builtin_amdgcn_make_buffer_rsrc((void*)terms, 0, left > 0 ? S::kRows * 4 : 0, 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(tr, (__attribute__((address_space(3))) void*)(LdsByte*)(into + S::kBytes + (wave == 3 ? 0 : wave) * 256), 4,
+                                               lane_anew() * 4, 0, 0, 0);
+      terms += (int64_t)step * 4;
+    }
+    base += (int64_t)step * ld;
+    left -= step;
   }
-  __device__ __forceinline__ void begin(const Operand& op, int64_t first, int64_t step_, const RowTerms* t, char* lds_) {
-    base = op.base, ld = (int)op.ld, next = first, step = step_, end = op.rows, lds = lds_;
-    const int wave = uniform_wave_in_block(), s = wave * kWave + lane_id(), row = s / S::kChunks, chunk = (s % S::kChunks) ^ S::swizzle(row);
-    static_assert(4096 / S::kRowBytes % 16 == 0, "the exchange of chunks goes by the row's last four bits");
-    at = chunk * 16 < ld ? row * ld + chunk * 16 : 0x3FFFFFFF;
-    if constexpr (TERMS) terms = wave == 1 ? (const char*)t->coef : wave == 2 ? (const char*)t->target : (const char*)t->lse2;
+  __device__ __forceinline__ RowStream(const Operand& op, int first, int step_, const RowTerms* t, char* lds_)
+      : left((int)op.rows - first), step(step_), ld((int)op.ld), wave(uniform_wave_in_block()), lds(lds_) {
+    base = op.base + (int64_t)first * ld;
+    if constexpr (TERMS) terms = (wave == 1 ? (const char*)t->coef : wave == 2 ? (const char*)t->target : (const char*)t->lse2) + (int64_t)first * 4;
+    const typename S::Places places(wave, lane_id(), ld);
+    if constexpr (SUMS) *mine() = u32x4{places.rows, places.across, (uint32_t)places.load, 0u};
+    else kept = places;
 #pragma unroll
-    for (int s = 0; s < kStages - 1; ++s) start(lds + s * kStage);
+    for (int s = 0; s < kStages - 1; ++s) start(lds + s * kStage, places.load);
     slot = kStages - 1;
   }
   static __device__ __forceinline__ void meet() {
@@ -471,31 +508,38 @@ struct RowStream {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   }
-  // f(stage) for the next stage, while another one is loaded into the place of the one before it
+  // f(stage, places) for the next stage, while another one is loaded into the place of the one before it
   template <typename F>
   __device__ __forceinline__ void stage(F&& f) {
     const int from = slot + 1 < kStages ? slot + 1 : 0;
     meet();
+    if constexpr (SUMS) {
+      const u32x4 x = *mine();
+      kept.rows = x[0], kept.across = x[1], kept.load = (int)x[2];
+    }
     both(lds + slot * kStage, lds + from * kStage, f);
     slot = from;
   }
   template <typename F>
   __device__ __forceinline__ void both(char* __restrict__ into, const char* __restrict__ from, F&& f) {
-    start(into);
-    f(from);
+    start(into, kept.load);
+    f(from, kept);
   }
 };
 
-// the fragments of 64 rows of an operand that a wave keeps: rows row0 + j * 32 + ..
+// the fragments of 64 rows of an operand that a wave keeps: rows row0 + j * 32 + .. (zeros where there are none; loads of a buffer, since
+// behind a branch each would be waited for by itself)
 template <int KS>
 __device__ __forceinline__ void keep_rows(const Operand& op, int64_t row0, u32x4 (&x)[2][KS]) {
+  const int64_t there = op.rows - row0;
+  const int rows = there < 0 ? 0 : there < 64 ? (int)there : 64, ld = (int)op.ld;
+  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(op.base + (there > 0 ? row0 : 0) * ld), 0, rows * ld, 0x00020000);
 #pragma unroll
   for (int j = 0; j < 2; ++j)
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) {
-      const int64_t row = row0 + j * 32 + (lane_id() & 31);
       const int at = kk * 32 + (lane_id() >> 5) * 16;
-      x[j][kk] = row < op.rows && at < op.ld ? *reinterpret_cast<const u32x4*>(op.base + row * op.ld + at) : u32x4{0, 0, 0, 0};
+      x[j][kk] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at < ld ? (j * 32 + (lane_id() & 31)) * ld + at : 0x3FFFFFFF, 0, 0);
     }
 }
 __device__ __forceinline__ constexpr int row_of(int e) { return (e >> 2) * 8 + (e & 3); }  // (as in Product)
@@ -517,7 +561,7 @@ __device__ __forceinline__ void pack(const f32x16& x, u32x4 (&f)[2]) {
 template <int T, int KS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_xent_stats_narrow(
     Operand w, Operand h, int64_t n, int64_t vocab, float scale2, const int32_t* __restrict__ targets, int splits, RowStat* __restrict__ part) {
-  typedef RowStream<T, KS, false> Stream;
+  typedef RowStream<T, KS, false, false> Stream;
   typedef typename Stream::S S;
   extern __shared__ char lds[];
   const int split = blockIdx.x % splits;
@@ -533,29 +577,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     top[j] = kNoMax;
     sum[j] = target[j] = 0.f;
   }
-  Stream stream;
-  const typename S::Reads reads;
-  stream.begin(w, (int64_t)split * S::kRows, (int64_t)splits * S::kRows, nullptr, lds);
-  for (int64_t v0 = (int64_t)split * S::kRows; v0 < vocab; v0 += (int64_t)splits * S::kRows) {
+  Stream stream(w, split * S::kRows, splits * S::kRows, nullptr, lds);
+  for (int left = (int)vocab - split * S::kRows; left > 0; left -= splits * S::kRows) {
+    const int v0 = (int)vocab - left;
     f32x16 z[2][2];
-    stream.stage([&](const char* from) {
-      const typename S::Reads at = reads.again();
+    stream.stage([&](const char* from, const typename S::Places& at) {
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) z[b][0][e] = z[b][1][e] = 0.f;
 #pragma unroll
         for (int kk = 0; kk < KS; ++kk) {
-          const u32x4 a = S::fragment(from, at, b, kk);
+          const u32x4 a = S::fragment(from, at.rows, b, kk);
 #pragma unroll
           for (int j = 0; j < 2; ++j) z[b][j] = mma<T>(a, hf[j][kk], z[b][j]);
         }
       }
     });
-    const int first = (int)v0 + own_row(), left = (int)vocab - first;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int mine = t[j] - first;
+      const int mine = t[j] - v0 - own_row();
       if (ballot64((uint32_t)mine < 64u) != 0) {
 #pragma unroll
         for (int b = 0; b < 2; ++b)
@@ -563,12 +604,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
           for (int e = 0; e < 16; ++e)
             if (mine == b * 32 + row_of(e)) target[j] = z[b][j][e] * scale2;
       }
-      if (v0 + S::kRows > vocab) {
+      if (left < S::kRows) {
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (b * 32 + row_of(e) >= left) z[b][j][e] = scale2 < 0.f ? __builtin_inff() : -__builtin_inff();
+            if (b * 32 + row_of(e) + own_row() >= left) z[b][j][e] = scale2 < 0.f ? __builtin_inff() : -__builtin_inff();
       }
       float m = z[0][j][0];
       if (scale2 < 0.f) {
@@ -598,37 +639,34 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (no load into LDS is left when the block ends)
 }
 
-// dH: sums[split][row][width] = the split's part of G W; rows, splits and stages as in the forward kernel
+// dH: sums[split][row][width] = the split's part of G W; rows, splits and stages as in the forward kernel.  A row's coef waits for the end,
+// where it is one product for a sum: what is rounded to 16 bits is p itself, the target's less 1 (in fp16 times 2^13, as G below).
 template <int T, int KS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_xent_dh_narrow(
     Operand w, Operand h, int64_t rows, int64_t vocab, float scale2, RowTerms term, int splits, float* __restrict__ sums, int32_t width) {
-  typedef RowStream<T, KS, false> Stream;
+  typedef RowStream<T, KS, false, true> Stream;
   typedef typename Stream::S S;
   extern __shared__ char lds[];
   const int split = blockIdx.x % splits;
   const int64_t row0 = (int64_t)(blockIdx.x / splits) * 256 + uniform_wave_in_block() * 64;
   u32x4 hf[2][KS];
   keep_rows<KS>(h, row0, hf);
-  float coef[2], lse2[2];
+  float lse2[2];
   int32_t t[2];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     const int64_t i = row0 + j * 32 + (lane_id() & 31);
-    coef[j] = term.coef[i], lse2[j] = term.lse2[i], t[j] = term.target[i];
+    lse2[j] = term.lse2[i] - kLift<T>, t[j] = term.target[i] - own_row();
   }
   f32x16 acc[KS / 2][2];
 #pragma unroll
   for (int c = 0; c < KS / 2; ++c)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[c][0][e] = acc[c][1][e] = 0.f;
-  Stream stream;
-  const typename S::Reads reads;
-  stream.begin(w, (int64_t)split * S::kRows, (int64_t)splits * S::kRows, nullptr, lds);
-  for (int64_t v0 = (int64_t)split * S::kRows; v0 < vocab; v0 += (int64_t)splits * S::kRows) {
-    const int first = (int)v0 + own_row(), left = (int)vocab - first;
-    const bool ragged = v0 + S::kRows > vocab;
-    stream.stage([&](const char* from) {
-      const typename S::Reads at = reads.again();
+  Stream stream(w, split * S::kRows, splits * S::kRows, nullptr, lds);
+  for (int left = (int)vocab - split * S::kRows; left > 0; left -= splits * S::kRows) {
+    const int v0 = (int)vocab - left;
+    stream.stage([&](const char* from, const typename S::Places& at) {
 #pragma unroll 1
       for (int b = 0; b < 2; ++b) {
         f32x16 z[2];
@@ -637,7 +675,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int e = 0; e < 16; ++e) z[0][e] = z[1][e] = 0.f;
 #pragma unroll
         for (int kk = 0; kk < KS; ++kk) {
-          const u32x4 a = S::fragment(from, at, b, kk);
+          const u32x4 a = S::fragment(from, at.rows, b, kk);
 #pragma unroll
           for (int j = 0; j < 2; ++j) z[j] = mma<T>(a, hf[j][kk], z[j]);
         }
@@ -645,18 +683,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int j = 0; j < 2; ++j) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) z[j][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][e], scale2, -lse2[j]));
-          const int mine = t[j] - first - b * 32;
+          const int mine = t[j] - v0 - b * 32;
           if (ballot64((uint32_t)mine < 32u) != 0) {
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-              if (mine == row_of(e)) z[j][e] -= 1.f;
+              if (mine == row_of(e)) z[j][e] -= kOne<T>;
           }
-#pragma unroll
-          for (int e = 0; e < 16; ++e) z[j][e] *= coef[j];
-          if (ragged) {  // (rows of W that are not there are zeros in the next product, but an exponential may be infinite)
+          if (left < S::kRows) {  // (rows of W that are not there are zeros in the next product, but an exponential may be infinite)
+            const int own = (lane_anew() >> 5) * 4;
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-              if (row_of(e) >= left - b * 32) z[j][e] = 0.f;
+              if (row_of(e) + own >= left - b * 32) z[j][e] = 0.f;
           }
           pack<T>(z[j], p[j]);
         }
@@ -664,23 +701,28 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int c = 0; c < KS / 2; ++c) {
-            const u32x4 a = S::transposed(from, at, b, c, s);
+            const u32x4 a = S::transposed(from, at.across, b, c, s);
 #pragma unroll
             for (int j = 0; j < 2; ++j) acc[c][j] = mma<T>(a, p[j][s], acc[c][j]);
           }
       }
     });
   }
+  const int lane = lane_anew(), own = (lane >> 5) * 4;
+  float coef[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) coef[j] = term.coef[row0 + j * 32 + (lane & 31)] / kOne<T>;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    float* to = sums + ((int64_t)split * rows + row0 + j * 32 + (lane_id() & 31)) * width;
+    const int64_t i = row0 + j * 32 + (lane & 31);
+    float* to = sums + ((int64_t)split * rows + i) * width;
 #pragma unroll
     for (int c = 0; c < KS / 2; ++c)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int col = c * 32 + row_of(4 * q) + own_row();
-        const float f[4] = {acc[c][j][4 * q], acc[c][j][4 * q + 1], acc[c][j][4 * q + 2], acc[c][j][4 * q + 3]};
+        const int col = c * 32 + row_of(4 * q) + own;
+        const float f[4] = {acc[c][j][4 * q] * coef[j], acc[c][j][4 * q + 1] * coef[j], acc[c][j][4 * q + 2] * coef[j], acc[c][j][4 * q + 3] * coef[j]};
         if (col < width) put4<COOP_F32>((char*)(to + col), f);
       }
   }
@@ -692,10 +734,10 @@ template <int T, int KS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_xent_dw_narrow(
     Operand w, Operand h, int64_t vocab, float scale2, RowTerms term, int splits, const float* __restrict__ unlift, int32_t dim,
     char* __restrict__ out, float* __restrict__ sums, int64_t rows, int32_t width) {
-  typedef RowStream<T, KS, true> Stream;
+  typedef RowStream<T, KS, true, true> Stream;
   typedef typename Stream::S S;
   extern __shared__ char lds[];
-  const int split = blockIdx.x % splits, lane = lane_id();
+  const int split = blockIdx.x % splits;
   const int64_t v0 = (int64_t)(blockIdx.x / splits) * 256 + uniform_wave_in_block() * 64;
   u32x4 wf[2][KS];
   keep_rows<KS>(w, v0, wf);
@@ -704,16 +746,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   for (int c = 0; c < KS / 2; ++c)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[c][0][e] = acc[c][1][e] = 0.f;
-  Stream stream;
-  const typename S::Reads reads;
-  stream.begin(h, (int64_t)split * S::kRows, (int64_t)splits * S::kRows, &term, lds);
-  for (int64_t i0 = (int64_t)split * S::kRows; i0 < h.rows; i0 += (int64_t)splits * S::kRows) {
-    stream.stage([&](const char* from) {
-      const typename S::Reads at = reads.again();
+  Stream stream(h, split * S::kRows, splits * S::kRows, &term, lds);
+  for (int left = (int)h.rows - split * S::kRows; left > 0; left -= splits * S::kRows) {
+    stream.stage([&](const char* from, const typename S::Places& at) {
+      const int lane = lane_anew(), own = (lane >> 5) * 4;
       const float* lse2 = reinterpret_cast<const float*>(from + S::kBytes);
       const float* coef = lse2 + 64;
-      const int hit = reinterpret_cast<const int32_t*>(coef + 64)[lane] - (int)v0;  // of row `lane` of the stage
-      const uint64_t hits = ballot64((uint32_t)hit < 64u);
+      const uint64_t hits = ballot64(reinterpret_cast<const uint32_t*>(coef + 64)[lane] - (uint32_t)v0 < 64u);  // of row `lane` of the stage
 #pragma unroll 1
       for (int b = 0; b < 2; ++b) {
         f32x16 z[2];
@@ -722,47 +761,44 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int e = 0; e < 16; ++e) z[0][e] = z[1][e] = 0.f;
 #pragma unroll
         for (int kk = 0; kk < KS; ++kk) {
-          const u32x4 a = S::fragment(from, at, b, kk);
+          const u32x4 a = S::fragment(from, at.rows, b, kk);
 #pragma unroll
           for (int j = 0; j < 2; ++j) z[j] = mma<T>(a, wf[j][kk], z[j]);
         }
-        f32x16 c4;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int i = b * 32 + row_of(4 * q) + own_row();
           float l[4], c[4];
-          load_elements<COOP_F32, 4>(lse2 + i, l);
-          load_elements<COOP_F32, 4>(coef + i, c);
+          load_elements<COOP_F32, 4>(lse2 + b * 32 + row_of(4 * q) + own, l);
+          load_elements<COOP_F32, 4>(coef + b * 32 + row_of(4 * q) + own, c);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            c4[4 * q + e] = c[e];
+          for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) z[j][4 * q + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][4 * q + e], scale2, -l[e]));
+            for (int j = 0; j < 2; ++j) z[j][4 * q + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][4 * q + e], scale2, -l[e])) * c[e];
+        }
+        // rows whose target is among the wave's: the 1 (of coef) goes off where the target's column and the row meet
+        if ((uint32_t)(hits >> (b * 32)) != 0) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            asm volatile("" ::: "memory");  // (no registers for all of the terms at once)
+            const float* at_coef = coef + b * 32 + row_of(4 * q) + own;
+            const u32x4 t = *reinterpret_cast<const u32x4*>(at_coef + 64);
+            float c[4];
+            load_elements<COOP_F32, 4>(at_coef, c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t at_column = t[e] - (uint32_t)v0 - (uint32_t)(lane & 31);
+#pragma unroll
+              for (int j = 0; j < 2; ++j) z[j][4 * q + e] -= at_column == (uint32_t)(j * 32) ? c[e] : 0.f;
+            }
           }
         }
-        // a row whose target is among the wave's: its 1 goes off where the target's column and the row meet
-        for (uint32_t todo = (uint32_t)(hits >> (b * 32)); todo != 0; todo &= todo - 1) {
-          const int r = __builtin_ctz(todo), v = __builtin_amdgcn_readlane(hit, b * 32 + r);
-          const bool here = lane == (v & 31) + (r >> 2 & 1) * 32;
-          const int element = (r >> 3) * 4 + (r & 3);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float one = e == element && here ? 1.f : 0.f;
-            z[0][e] -= v < 32 ? one : 0.f;
-            z[1][e] -= v < 32 ? 0.f : one;
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) z[j][e] *= c4[e];
-          pack<T>(z[j], p[j]);
-        }
+        for (int j = 0; j < 2; ++j) pack<T>(z[j], p[j]);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int c = 0; c < KS / 2; ++c) {
-            const u32x4 a = S::transposed(from, at, b, c, s);
+            const u32x4 a = S::transposed(from, at.across, b, c, s);
 #pragma unroll
             for (int j = 0; j < 2; ++j) acc[c][j] = mma<T>(a, p[j][s], acc[c][j]);
           }
@@ -770,22 +806,56 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     });
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  const float u = sums != nullptr ? 1.f : *unlift;
+  const int lane = lane_anew(), own = (lane >> 5) * 4;
+  if (sums != nullptr) {
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int64_t v = v0 + j * 32 + (lane & 31);
-    if (v >= vocab) continue;
+    for (int j = 0; j < 2; ++j) {
+      const int64_t v = v0 + j * 32 + (lane & 31);
+      if (v >= vocab) continue;
+#pragma unroll
+      for (int c = 0; c < KS / 2; ++c)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int col = c * 32 + row_of(4 * q) + own;
+          const float f[4] = {acc[c][j][4 * q], acc[c][j][4 * q + 1], acc[c][j][4 * q + 2], acc[c][j][4 * q + 3]};
+          if (col < width) put4<COOP_F32>((char*)(sums + ((int64_t)split * rows + v) * width + col), f);
+        }
+    }
+    return;
+  }
+  // rounded, and through LDS into whole rows: a short loop with one test for a row's end, in the place of as many as a lane has packs
+  __syncthreads();
+  const float u = *unlift;
+  constexpr int kRow = KS * 32 + 8;  // bytes (and 8 more: the lanes' rows begin in different banks)
+  static_assert(4 * 64 * kRow <= Stream::kLds, "the waves' rows lie where the stages were");
+  char* mine = lds + uniform_wave_in_block() * (64 * kRow);
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
 #pragma unroll
     for (int c = 0; c < KS / 2; ++c)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int col = c * 32 + row_of(4 * q) + own_row();
-        float f[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = acc[c][j][4 * q + e] * u;
-        if (sums == nullptr) put_columns<T>(out, v, col, dim, f);
-        else if (col < width) put4<COOP_F32>((char*)(sums + ((int64_t)split * rows + v) * width + col), f);
+        const float f[4] = {acc[c][j][4 * q] * u, acc[c][j][4 * q + 1] * u, acc[c][j][4 * q + 2] * u, acc[c][j][4 * q + 3] * u};
+        Pack<T, 4> x;
+        x.set(f);
+        *reinterpret_cast<u32x2*>(mine + (j * 32 + (lane & 31)) * kRow + (c * 32 + row_of(4 * q) + own) * 2) = __builtin_bit_cast(u32x2, x);
       }
+  __syncthreads();
+  constexpr int kPacks = KS * 4, kEach = kWave / kPacks;  // of 4 columns in a row, rows at a time
+#pragma unroll 2
+  for (int r = lane / kPacks; r < 64; r += kEach) {
+    const int col = lane % kPacks * 4;
+    const int64_t v = v0 + r;
+    if (v >= vocab || col >= dim) continue;
+    const Pack<T, 4> x = __builtin_bit_cast(Pack<T, 4>, *reinterpret_cast<const u32x2*>(mine + r * kRow + col * 2));
+    typename Element<T>::M* to = (typename Element<T>::M*)out + v * dim + col;
+    if (col + 4 <= dim) {
+      x.store(to);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (col + e < dim) to[e] = x.x[e];
+    }
   }
 }
 
@@ -825,14 +895,14 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 //   narrow: more rows, of up to 128 elements of 16 bits (above).
 //   else products in tiles, a piece of the vocabulary at a time.  Of 256 x 256, what a wave's registers hold, where there are enough of
 //   them for the chip: the matrix units then take all that LDS gives.  Else, and in fp32, where they are sixteen times slower, of
-//   128 x 128, two blocks on a CU (2,236 rows, 170 vertices, 768 elements of bf16: 148 -> @A us).  Few rows' gradients take tiles of 32 rows.
+//   128 x 128, two blocks on a CU (2,236 rows, 170 vertices, 768 elements of bf16: 148 -> 82 us).  Few rows' gradients take tiles of 32 rows.
 struct XentPlan {
   int64_t n, vocab, width, ld;  // width: elements of a padded row
   int64_t rows, piece, vocab_rows;
   int64_t g_ld;  // bytes from row to row of G: not a power of two, or a tile's rows would all lie in the same few channels of memory
   int splits, dh_splits, dw_splits, tile;
   bool few, narrow, pad;
-  size_t h, w, part, coef, lse2, target, unlift, g, sums, bytes;
+  size_t h, w, part, coef, lse2, target, unlift, tops, g, sums, bytes;
   static int at_most(int64_t x, int64_t most) { return (int)(x < 1 ? 1 : x < most ? x : most); }
   XentPlan(int64_t n_, int64_t vocab_, int32_t dim, int dtype, bool aligned, bool grad) : n(n_), vocab(vocab_) {
     const int es = element_bytes(dtype);
@@ -867,6 +937,7 @@ struct XentPlan {
     lse2 = take(grad ? (size_t)rows * 4 : 0);
     target = take(grad ? (size_t)rows * 4 : 0);
     unlift = take(grad ? sizeof(float) : 0);
+    tops = take(grad ? 256 * sizeof(float) : 0);
     g_ld = piece * es + 256;
     g = take(grad && !narrow ? (size_t)rows * g_ld : 0);
     const size_t dh = (size_t)dh_splits * rows * width * 4, dw = dw_splits > 1 ? (size_t)dw_splits * vocab_rows * width * 4 : 0;
@@ -938,7 +1009,7 @@ int forward(const XentPlan& p, const void* hidden, const void* weight, int32_t d
     if constexpr (T != COOP_F32) ok = launch_stats<T, 2, 2, 4, 4>(p, w, h, alpha, targets, part, s);
   } else if constexpr (T != COOP_F32) {
     with_steps(p.width, [&](auto ks) {
-      constexpr int KS = decltype(ks)::value, lds = RowStream<T, KS, false>::kLds;
+      constexpr int KS = decltype(ks)::value, lds = RowStream<T, KS, false, false>::kLds;
       const auto kernel = k_xent_stats_narrow<T, KS>;
       ok = allow_lds(kernel, lds);
       if (!ok) return;
@@ -954,8 +1025,9 @@ int forward(const XentPlan& p, const void* hidden, const void* weight, int32_t d
 
 template <int T>
 void write_out(const float* sums, int splits, int64_t rows, const XentPlan& p, int64_t n, int32_t dim, const float* unlift, void* out, hipStream_t s) {
-  const int64_t blocks = (n * ((dim + 3) / 4) + kWave - 1) / kWave;
-  COOP_LAUNCH(K_XENT_OUT, k_xent_out<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(kOutWaves * kWave), 0, s, sums, splits, rows, (int32_t)p.width, n, dim,
+  const int share = splits >= kOutWaves ? kOutWaves : 1, each = kOutWaves / share * kWave;
+  const int64_t blocks = (n * ((dim + 3) / 4) + each - 1) / each;
+  COOP_LAUNCH(K_XENT_OUT, k_xent_out<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(kOutWaves * kWave), 0, s, sums, splits, share, rows, (int32_t)p.width, n, dim,
               unlift, (char*)out);
 }
 
@@ -964,7 +1036,7 @@ bool backward_narrow(const XentPlan& p, const Operand& w, const Operand& h, int3
                      void* dhidden, void* dweight, float* sums, hipStream_t s) {
   bool ok = true;
   with_steps(p.width, [&](auto ks) {
-    constexpr int KS = decltype(ks)::value, lds_h = RowStream<T, KS, false>::kLds, lds_w = RowStream<T, KS, true>::kLds;
+    constexpr int KS = decltype(ks)::value, lds_h = RowStream<T, KS, false, true>::kLds, lds_w = RowStream<T, KS, true, true>::kLds;
     const auto kh = k_xent_dh_narrow<T, KS>;
     const auto kw = k_xent_dw_narrow<T, KS>;
     ok = allow_lds(kh, lds_h) && allow_lds(kw, lds_w);
@@ -1026,8 +1098,11 @@ int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t 
   const RowTerms term{(float*)(ws + p.coef), (float*)(ws + p.lse2), (int32_t*)(ws + p.target)};
   float* unlift = (float*)(ws + p.unlift);
   float* sums = (float*)(ws + p.sums);
+  float* tops = (float*)(ws + p.tops);
+  const int n_tops = T == COOP_F32 || p.n <= kTopRows ? 0 : 256;
+  if (n_tops != 0) COOP_LAUNCH(K_XENT_TERMS, k_xent_top, dim3(n_tops), dim3(1024), 0, s, targets, ignore, dloss, alpha, p.n, p.vocab, tops);
   COOP_LAUNCH(K_XENT_TERMS, (k_xent_terms<T != COOP_F32>), dim3((unsigned)((p.rows + 1023) / 1024)), dim3(1024), 0, s, targets, ignore, lse, dloss,
-              alpha, T == COOP_F16 ? 8192.f : 1.f, p.n, p.rows, p.vocab, term, unlift, bad);
+              alpha, kOne<T>, p.n, p.rows, p.vocab, tops, n_tops, term, unlift, bad);
   pad_rows<T>(hidden, p.n, dim, term.target, p.rows, p, ws + p.h, s);
   if (p.pad) {
     pad_rows<T>(weight, p.vocab, dim, nullptr, p.vocab, p, ws + p.w, s);
