@@ -969,6 +969,10 @@ int xent_check(const void* hidden, int64_t n, const void* weight, int64_t vocab,
   return COOP_OK;
 }
 
+// what logits are multiplied by for their exponentials in base 2.  (Of a scale of 0 the least number: what lies behind the vocabulary's end
+// counts as minus infinity, which times 0 would be no number.)
+float scale_of(float alpha) { return alpha == 0.f ? 0x1p-126f : alpha * kLog2e; }
+
 template <int T, int WA, int WB, int TA, int TB>
 bool launch_stats(const XentPlan& p, Operand w, Operand h, float alpha, const int32_t* targets, RowStat* part, hipStream_t s) {
   typedef Product<T, WA, WB, TA, TB, false, false, kWide> P;
@@ -976,7 +980,7 @@ bool launch_stats(const XentPlan& p, Operand w, Operand h, float alpha, const in
   const auto kernel = k_xent_stats<T, WA, WB, TA, TB>;
   if (!allow_lds(kernel, lds)) return false;
   const int64_t row_tiles = (p.n + P::kRowsB - 1) / P::kRowsB;
-  COOP_LAUNCH(K_XENT_STATS, kernel, dim3((unsigned)(row_tiles * p.splits)), dim3(P::kThreads), lds, s, w, h, p.n, p.vocab, p.width, alpha * kLog2e,
+  COOP_LAUNCH(K_XENT_STATS, kernel, dim3((unsigned)(row_tiles * p.splits)), dim3(P::kThreads), lds, s, w, h, p.n, p.vocab, p.width, scale_of(alpha),
               targets, p.splits, part);
   return true;
 }
@@ -1013,7 +1017,7 @@ int forward(const XentPlan& p, const void* hidden, const void* weight, int32_t d
       const auto kernel = k_xent_stats_narrow<T, KS>;
       ok = allow_lds(kernel, lds);
       if (!ok) return;
-      COOP_LAUNCH(K_XENT_STATS, kernel, dim3((unsigned)(p.rows / p.tile * p.splits)), dim3(256), lds, s, w, h, p.n, p.vocab, alpha * kLog2e, targets,
+      COOP_LAUNCH(K_XENT_STATS, kernel, dim3((unsigned)(p.rows / p.tile * p.splits)), dim3(256), lds, s, w, h, p.n, p.vocab, scale_of(alpha), targets,
                   p.splits, part);
     });
   }

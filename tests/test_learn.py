@@ -101,12 +101,11 @@ def test_embed_offsets_beyond_32_bits():
 
 # ---- its gradient ---------------------------------------------------------------------------------------------------------
 def plain_embed_grad(dout, ids, n_rows, factor, live):
-    x = dout.double() * factor[:, None]
-    grad = torch.zeros((n_rows, dout.shape[1]), dtype=torch.float64, device="cuda")
-    grad.index_add_(0, ids.long()[live], x[live])
-    size = torch.zeros_like(grad).index_add_(0, ids.long()[live], x[live].abs())
-    count = torch.zeros(n_rows, dtype=torch.float64, device="cuda").index_add_(0, ids.long()[live], torch.ones_like(factor[live]))
-    return grad, size, count
+    x, at = (dout.double() * factor[:, None])[live].cpu(), ids.long()[live].cpu()     # (on the host: 100,000 atomics on one row take many seconds)
+    grad = torch.zeros((n_rows, dout.shape[1]), dtype=torch.float64).index_add_(0, at, x)
+    size = torch.zeros_like(grad).index_add_(0, at, x.abs())
+    count = torch.zeros(n_rows, dtype=torch.float64).index_add_(0, at, torch.ones(at.shape[0], dtype=torch.float64))
+    return grad.cuda(), size.cuda(), count.cuda()
 
 
 ID_SETS = {
@@ -139,6 +138,23 @@ def test_embed_grad(ids_of, n, n_rows, dim):
     assert torch.equal(part, got[rows.long()])          # one order of the sums, either way
     rows2, part2, k = P.coop_embed_grad_rows(dout, ids, n_rows, scale=scale, alpha=1.7, pad=-7, dtype=out_dtype, wait=False)
     assert int(k) == rows.numel() and torch.equal(rows2[:int(k)], rows) and torch.equal(part2[:int(k)], part)
+    assert status_is(0)
+
+
+# around the numbers of tokens at which the sort changes its way, the last of them past 512 tiles of 8,192
+@gpu
+@pytest.mark.parametrize("ids_of", ["spread", "hub", "pads", "each once"])
+@pytest.mark.parametrize("n,n_rows,dim", [(511, 100000, 2), (512, 300, 3), (513, 300, 2), (8192, 9000, 2), (8193, 400000, 1), (4194305, 5000000, 1)])
+def test_embed_grad_orders(ids_of, n, n_rows, dim):
+    g = rng(n)
+    ids = ID_SETS[ids_of](g, n, n_rows).to(torch.int32)
+    dout = torch.randint(-8, 9, (n, dim), generator=g, device="cuda").float()       # small whole numbers: the sums are exact
+    live = (ids >= 0).cpu().numpy()
+    at, x = ids.cpu().numpy()[live], dout.double().cpu().numpy()[live]              # (on the host: millions of atomics on one row take minutes)
+    want = torch.from_numpy(np.stack([np.bincount(at, x[:, d], n_rows) for d in range(dim)], 1)).cuda()
+    assert torch.equal(P.coop_embed_grad(dout, ids, n_rows, pad=-7).double(), want)
+    rows, part = P.coop_embed_grad_rows(dout, ids, n_rows, pad=-7)
+    assert torch.equal(rows.long(), torch.unique(ids[ids >= 0]).long()) and torch.equal(part.double(), want[rows.long()])
     assert status_is(0)
 
 
@@ -283,6 +299,28 @@ XENT_SIZES = [(1, 1, 1), (1, 5, 16), (2, 300, 3), (24, 1000, 128), (32, 257, 64)
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 @pytest.mark.parametrize("n,vocab,dim", XENT_SIZES)
 def test_softmax_xent(dtype, n, vocab, dim):
+    check_xent(dtype, n, vocab, dim, 0.8)
+
+
+# products in tiles of 256 rows; a vocabulary in three pieces; one split with several stages of rows; more rows than one block looks through
+# for the largest coefficient, of a few classes; rows that end in each quarter of a stage
+@gpu
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,vocab,dim", [(4097, 4100, 200), (16384, 20000, 136), (300, 140000, 40), (200, 131100, 128), (40000, 47, 24), (33000, 70, 200),
+                                         (16, 70, 8), (17, 81, 24), (48, 113, 72), (63, 127, 120)])
+def test_softmax_xent_of_many_and_of_few(dtype, n, vocab, dim):
+    check_xent(dtype, n, vocab, dim, 0.8)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("alpha", [-0.7, 0.0])
+@pytest.mark.parametrize("n,vocab,dim", [(20, 700, 100), (300, 700, 100), (300, 700, 200)])
+def test_softmax_xent_scale(dtype, alpha, n, vocab, dim):
+    check_xent(dtype, n, vocab, dim, alpha)
+
+
+def check_xent(dtype, n, vocab, dim, alpha):
     g = rng(n + vocab + dim)
     h, w = normal(g, n, dim, dtype=dtype), normal(g, vocab, dim, dtype=dtype, scale=2 * dim ** -0.5)
     if n % 2:
@@ -290,7 +328,6 @@ def test_softmax_xent(dtype, n, vocab, dim):
     t = torch.randint(0, vocab, (n,), generator=g, device="cuda", dtype=torch.int32)
     t[torch.rand(n, generator=g, device="cuda") < 0.2] = -1
     t[:1] = vocab - 1
-    alpha = 0.8
     loss, lse = P.coop_softmax_xent(h, w, t, alpha=alpha)
     want, want_lse, z = plain_xent(h, w, t, alpha)
     ez, el = xent_bounds(h, w, z, want_lse, alpha)
@@ -470,6 +507,27 @@ def test_adamw_8_bit_moments(rows, dim, by_rows):
             if name == "m" or y.min() > 2.0 ** -9:
                 assert abs(off.sum()) <= 6 * (0.25 * off.numel()) ** 0.5 + 1
         m, r = decoded(opt, 0, "m", *shape)[0], decoded(opt, 0, "v", *shape)[0]
+
+
+@gpu
+def test_adamw_8_bit_many_tensors():
+    """More tensors than one launch takes; the parameter follows the moments before they are rounded."""
+    g = rng(14)
+    sizes = [1, 0, 255, 256, 257, 3000] + [100 + 13 * i for i in range(70)]
+    params, grads = [normal(g, s) for s in sizes], [normal(g, s) for s in sizes]
+    opt = P.AdamW(params, grads, bits=8)
+    for step in (1, 2):
+        old, state = [p.double() for p in params], [(decoded(opt, i, "m", 1, s)[0][0], decoded(opt, i, "v", 1, s)[0][0]) if s else None for i, s in enumerate(sizes)]
+        opt.step(step, seed=3, **HYPER)
+        for i, s in enumerate(sizes):
+            if s == 0:
+                continue
+            want, m, v, move = plain_adamw(old[i], grads[i].double(), state[i][0], state[i][1] ** 2, step, **HYPER)
+            within(params[i], want, 4 * U * (want.abs() + old[i].abs()) + 32 * U * move.abs() + 32 * U * HYPER["lr"])
+            for name, x in (("m", m), ("v", torch.sqrt(v))):
+                got, scale = decoded(opt, i, name, 1, s)
+                scale = scale.repeat_interleave(256, 1)[0, :s]
+                assert ((got[0] / scale - x / scale).abs() <= gap(x / scale) * (1 + 1e-4) + 64 * U * 448).all()
 
 
 @gpu
