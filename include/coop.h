@@ -207,9 +207,10 @@ int coop_gather(const void* feat, int64_t n_rows, int32_t dim, int dtype, const 
 int coop_gather_mean(const void* feat, int64_t n_rows, int32_t dim, int dtype, const int64_t* indptr,
                      const int32_t* col_global, int64_t n_dst, void* out, void* stream);
 
-/* Synchronises `stream` and returns COOP_E_RANGE if any coop_gather / coop_gather_mean / coop_bucket_by_owner since the
- * last call of this function met an id outside its range (such rows of `out` are left zero-filled; such ids are left
- * out of every group), else COOP_OK.  Clears the condition. */
+/* Synchronises `stream` and returns COOP_E_RANGE if any coop_gather / coop_gather_mean / coop_bucket_by_owner / coop_embed
+ * / coop_embed_grad(_rows) / coop_softmax_xent(_grad) / coop_adamw since the last call of this function met an id, a target
+ * or a row outside its range (such rows of `out` are left zero-filled; such ids are left out of every group; what the others
+ * do with theirs is said there), else COOP_OK.  Clears the condition. */
 int coop_gather_status(void* stream);
 
 /* vertex partitions of Sec. 3.1 (1-D: every vertex, with its in-edges, belongs to one PE) */

@@ -4,12 +4,15 @@ targets where they can go wrong; gradients against the formulas and against diff
 Tolerances are bounds, elementwise: u = 2^-24 for an operation in 32 bits, the sums' worst order included, and half a unit in
 the last place of the type that a result is stored in (for fp16 also of its smallest numbers)."""
 import ctypes as C
+import importlib.util
+import os
 
 import numpy as np
 import pytest
 import torch
 
 import paper_2310_12403_amd as P
+import synth
 from paper_2310_12403_amd import learn
 
 U = 2.0 ** -24
@@ -685,6 +688,28 @@ def test_workspaces_are_the_callers():
     assert all(torch.equal(x, y) for x, y in zip(want, P.coop_softmax_xent_grad(h, w, t, lse, loss, workspace=ws)))
     with pytest.raises(P.CoopError):
         P.coop_softmax_xent_grad(h, w, t, lse, loss, workspace=ws[:1024])
+
+
+# ---- together ----------------------------------------------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("bits,dim", [(8, 128), (32, 75)])
+def test_vertex_embeddings_learn(bits, dim):
+    """Trained rows tell a neighbour better than the neighbours' frequencies do halfway from none to all of their information."""
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "vertex_embeddings.py")
+    spec = importlib.util.spec_from_file_location("vertex_embeddings", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    indptr, indices = synth.rmat_csr(scale=12, n_edges=65536)
+    model, losses = example.train(indptr, indices, dim=dim, batch=512, steps=120, bits=bits, log=None)
+    degrees = np.diff(indptr.numpy())                             # a vertex's neighbours are drawn min(10, degree) at a time
+    share = np.bincount(indices.numpy(), np.repeat(np.minimum(10, degrees) / np.maximum(degrees, 1), degrees), 4096)
+    share /= share.sum()
+    entropy = -(share[share > 0] * np.log(share[share > 0])).sum()
+    assert abs(losses[0] - np.log(4096)) < 1e-4                  # output weights of zero: all vertices alike
+    assert np.mean(losses[-10:]) < (np.log(4096) + entropy) / 2
+    assert torch.equal(model.out16, model.out.to(torch.bfloat16))
+    _, again = example.train(indptr, indices, dim=dim, batch=512, steps=120, bits=bits, log=None)
+    assert again == losses                                       # the same bits on every run
 
 
 # ---- refusals ----------------------------------------------------------------------------------------------------------------
