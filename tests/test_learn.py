@@ -690,6 +690,65 @@ def test_workspaces_are_the_callers():
         P.coop_softmax_xent_grad(h, w, t, lse, loss, workspace=ws[:1024])
 
 
+# ---- offsets beyond 32 bits -----------------------------------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("n,dim,dtype", [(40, 128, torch.bfloat16), (40, 136, torch.float16), (3, 136, torch.bfloat16)])
+def test_softmax_xent_offsets_beyond_32_bits(n, dim, dtype):
+    torch.cuda.empty_cache()
+    check_xent(dtype, n, 17000001, dim, 0.8)                     # 4.3 GB of weight, and of its gradient
+
+
+@gpu
+def test_layer_norm_offsets_beyond_32_bits():
+    torch.cuda.empty_cache()
+    rows, dim, k = 70001, 32768, 7                               # 2.3e9 elements
+    g = rng(21)
+    x, dy = (torch.zeros((rows, dim), dtype=torch.float16, device="cuda") for _ in range(2))
+    x[-k:], dy[-k:] = normal(g, k, dim, dtype=torch.float16), normal(g, k, dim, dtype=torch.float16)
+    y, mean, rstd = P.coop_layer_norm(x)
+    few, few_mean, few_rstd = P.coop_layer_norm(x[-k:].contiguous())
+    assert torch.equal(y[-k:], few) and torch.equal(mean[-k:], few_mean) and torch.equal(rstd[-k:], few_rstd) and not y[:-k].any()
+    dx, dw, db = P.coop_layer_norm_grad(dy, x, mean, rstd)
+    few, few_dw, few_db = P.coop_layer_norm_grad(dy[-k:].contiguous(), x[-k:].contiguous(), few_mean, few_rstd)
+    assert torch.equal(dx[-k:], few) and not dx[:-k].any()
+    # sums of 7 numbers, in another order
+    size = (dy[-k:].double().abs() * (1 + y[-k:].double().abs())).sum(0) * 16 * U
+    within(dw, few_dw, size)
+    within(db, few_db, size)
+
+
+@gpu
+@pytest.mark.parametrize("bits", [8, 32])
+def test_adamw_offsets_beyond_32_bits(bits):
+    torch.cuda.empty_cache()
+    n = 2 ** 31 + 4099
+    spots = [slice(0, 2048), slice(2 ** 31 - 1024, 2 ** 31 + 1024), slice(n - 1027, n)]
+    p, grad = torch.ones(n, dtype=torch.bfloat16, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g = rng(22)
+    for s in spots:
+        grad[s] = normal(g, s.stop - s.start, dtype=torch.bfloat16)
+    opt = P.AdamW([p], [grad], bits=bits)
+    opt.step(1, **HYPER)
+    for s in spots:
+        want, m, v, move = plain_adamw(torch.ones(s.stop - s.start, dtype=torch.float64, device="cuda"), grad[s].double(), 0.0, 0.0, 1, **HYPER)
+        within(p[s], want, 64 * U + want.abs() * HALF[torch.bfloat16])
+        if bits == 32:
+            within(opt.state["m"][0][s], m, 8 * U * m.abs())
+            within(opt.state["v"][0][s], v, 8 * U * v)
+        else:
+            got = opt.state["m"][0][s].float() * opt.state["m_scale"][0][s.start // 256:-(-s.stop // 256)].repeat_interleave(256)[:s.stop - s.start]
+            within(got, m, m.abs() * 2.0 ** -3 * 1.01 + opt.state["m_scale"][0].max() * 2.0 ** -9 * 1.01)
+    del p, grad, opt
+    table = torch.zeros((60000, 40000), dtype=torch.bfloat16, device="cuda")
+    rows = torch.tensor([0, 53687, 53688, 59999], dtype=torch.int32, device="cuda")
+    opt = P.AdamW([table], bits=bits, by_rows=True)
+    grads = normal(g, 4, 40000)
+    opt.step(1, rows={0: (rows, grads, None)}, **HYPER)
+    want = plain_adamw(torch.zeros_like(grads.double()), grads.double(), 0.0, 0.0, 1, **HYPER)[0]
+    within(table[rows.long()], want, 64 * U * HYPER["lr"] + want.abs() * HALF[torch.bfloat16])
+    assert int((table != 0).any(1).sum()) == 4
+
+
 # ---- together ----------------------------------------------------------------------------------------------------------------
 @gpu
 @pytest.mark.parametrize("bits,dim", [(8, 128), (32, 75)])
