@@ -859,20 +859,28 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   }
 }
 
-// rows of `dim` elements into `rows` rows of `width`, zeros behind a row's end, behind the last of n rows, and in rows whose target is
-// negative (null: all have one)
+// Rows of `dim` elements into `rows` rows of `width`, zeros behind a row's end, behind the last of n rows, and in rows whose target is
+// negative (null: all have one).  The hidden states and the weight in one launch: of few rows a launch is all that it costs.
+struct PadJob {
+  const char* in;
+  const int32_t* target;
+  char* out;
+  int64_t n, rows;
+  uint32_t blocks;  // 0: nothing to do
+};
 template <int T>
-__global__ __launch_bounds__(kBlock) void k_xent_pad(const char* __restrict__ in, int64_t n, int32_t dim, const int32_t* __restrict__ target,
-                                                     int64_t rows, char* __restrict__ out, int32_t width) {
-  const int64_t step = (int64_t)gridDim.x * kBlock;
+__global__ __launch_bounds__(kBlock) void k_xent_pad(PadJob first, PadJob second, int32_t dim, int32_t width) {
+  const bool one = blockIdx.x < first.blocks;
+  const PadJob& job = one ? first : second;
+  const int64_t step = (int64_t)job.blocks * kBlock;
   typedef typename Element<T>::M M;
   constexpr int E = 16 / (int)sizeof(M);  // (a row of the copy is a multiple of 16 bytes)
   const int32_t packs = width / E;
-  for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < rows * packs; i += step) {
+  for (int64_t i = (int64_t)(blockIdx.x - (one ? 0 : first.blocks)) * kBlock + threadIdx.x; i < job.rows * packs; i += step) {
     const int64_t row = i / packs;
     const int32_t c = (int32_t)(i - row * packs) * E;
-    const bool there = row < n && (target == nullptr || target[row] >= 0);
-    const M* from = (const M*)in + row * dim + c;
+    const bool there = row < job.n && (job.target == nullptr || job.target[row] >= 0);
+    const M* from = (const M*)job.in + row * dim + c;
     Pack<T, E> x;
     if (there && c + E <= dim) {
       x = Pack<T, E>::load(from);
@@ -880,7 +888,7 @@ __global__ __launch_bounds__(kBlock) void k_xent_pad(const char* __restrict__ in
 #pragma unroll
       for (int e = 0; e < E; ++e) x.x[e] = there && c + e < dim ? from[e] : (M)0.f;
     }
-    x.store((M*)out + row * width + c);
+    x.store((M*)job.out + row * width + c);
   }
 }
 
@@ -946,11 +954,13 @@ struct XentPlan {
   }
 };
 
-template <int T>
-void pad_rows(const void* in, int64_t n, int32_t dim, const int32_t* target, int64_t rows, const XentPlan& p, void* out, hipStream_t s) {
+PadJob pad_job(const void* in, int64_t n, const int32_t* target, int64_t rows, const XentPlan& p, void* out) {
   const int64_t blocks = (rows * p.ld / 16 + kBlock - 1) / kBlock;
-  COOP_LAUNCH(K_XENT_PAD, k_xent_pad<T>, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(kBlock), 0, s, (const char*)in, n, dim, target, rows,
-              (char*)out, (int32_t)p.width);
+  return PadJob{(const char*)in, target, (char*)out, n, rows, (uint32_t)(blocks < 8192 ? blocks : 8192)};
+}
+template <int T>
+void pad(const PadJob& first, const PadJob& second, int32_t dim, const XentPlan& p, hipStream_t s) {
+  COOP_LAUNCH(K_XENT_PAD, k_xent_pad<T>, dim3(first.blocks + second.blocks), dim3(kBlock), 0, s, first, second, dim, (int32_t)p.width);
 }
 
 // (blocks of more than 64 KB of LDS have to be allowed, once for each kernel and device; it costs a fraction of a microsecond)
@@ -997,8 +1007,7 @@ template <int T>
 int forward(const XentPlan& p, const void* hidden, const void* weight, int32_t dim, const int32_t* targets, float alpha, int32_t ignore,
             float* loss, float* lse, char* ws, int32_t* bad, hipStream_t s) {
   if (p.pad) {
-    pad_rows<T>(hidden, p.n, dim, nullptr, p.n, p, ws + p.h, s);
-    pad_rows<T>(weight, p.vocab, dim, nullptr, p.vocab, p, ws + p.w, s);
+    pad<T>(pad_job(hidden, p.n, nullptr, p.n, p, ws + p.h), pad_job(weight, p.vocab, nullptr, p.vocab, p, ws + p.w), dim, p, s);
     hidden = ws + p.h;
     weight = ws + p.w;
   }
@@ -1107,11 +1116,8 @@ int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t 
   if (n_tops != 0) COOP_LAUNCH(K_XENT_TERMS, k_xent_top, dim3(n_tops), dim3(1024), 0, s, targets, ignore, dloss, alpha, p.n, p.vocab, tops);
   COOP_LAUNCH(K_XENT_TERMS, (k_xent_terms<T != COOP_F32>), dim3((unsigned)((p.rows + 1023) / 1024)), dim3(1024), 0, s, targets, ignore, lse, dloss,
               alpha, kOne<T>, p.n, p.rows, p.vocab, tops, n_tops, term, unlift, bad);
-  pad_rows<T>(hidden, p.n, dim, term.target, p.rows, p, ws + p.h, s);
-  if (p.pad) {
-    pad_rows<T>(weight, p.vocab, dim, nullptr, p.vocab, p, ws + p.w, s);
-    weight = ws + p.w;
-  }
+  pad<T>(pad_job(hidden, p.n, term.target, p.rows, p, ws + p.h), p.pad ? pad_job(weight, p.vocab, nullptr, p.vocab, p, ws + p.w) : PadJob{}, dim, p, s);
+  if (p.pad) weight = ws + p.w;
   hidden = ws + p.h;
   const Operand w{(const char*)weight, p.ld, p.vocab, p.ld}, h{(const char*)hidden, p.ld, p.n, p.ld};
   if constexpr (T != COOP_F32)
