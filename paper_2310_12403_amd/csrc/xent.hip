@@ -919,15 +919,14 @@ struct XentPlan {
     pad = !aligned || width != dim;
     narrow = es == 2 && width <= 128 && (grad || n > 32);
     few = n <= 32 && !narrow;
-    tile = narrow || few || (es == 2 && ((n + 255) / 256) * ((vocab + 255) / 256) >= 256) ? 256 : 128;
+    tile = narrow || (es == 2 || few) && ((n + 255) / 256) * ((vocab + 255) / 256) >= 256 ? 256 : 128;
     rows = few ? 32 : round_up(n, tile);
     const int blocks = 256 * (narrow || few || tile == 128 ? 2 : 1);
     const int64_t row_tiles = few ? 1 : rows / tile, vocab_tiles = (vocab + tile - 1) / tile;
     vocab_rows = vocab_tiles * tile;
     // blocks: two of a narrow kernel or of few rows on a CU, one of the others; a multiple of 8 splits where there are so many, so that
     // the blocks of an XCD have the same splits' tiles of W
-    const int64_t few_tiles = (vocab + 255) / 256;
-    if (few) splits = at_most((few_tiles + (few_tiles + 511) / 512 - 1) / ((few_tiles + 511) / 512), 512);  // (of as many tiles each)
+    if (few) splits = at_most((vocab_tiles + (vocab_tiles + 511) / 512 - 1) / ((vocab_tiles + 511) / 512), 512);  // (of as many tiles each)
     else splits = at_most(blocks / row_tiles, narrow ? (vocab + 63) / 64 : vocab_tiles);
     if (!few && splits > 8) splits = splits / 8 * 8;
     piece = kPieceBytes / (rows * es) / tile * tile;
@@ -1015,7 +1014,7 @@ int forward(const XentPlan& p, const void* hidden, const void* weight, int32_t d
   RowStat* part = (RowStat*)(ws + p.part);
   bool ok = true;
   if (p.few) {
-    ok = launch_stats<T, 4, 1, 2, 1>(p, w, h, alpha, targets, part, s);
+    ok = p.tile == 128 ? launch_stats<T, 4, 1, 1, 1>(p, w, h, alpha, targets, part, s) : launch_stats<T, 4, 1, 2, 1>(p, w, h, alpha, targets, part, s);
   } else if (!p.narrow && p.tile == 128) {
     ok = launch_stats<T, 2, 2, 2, 2>(p, w, h, alpha, targets, part, s);
   } else if (!p.narrow) {
@@ -1133,7 +1132,8 @@ int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t 
   typedef std::integral_constant<int, 1> One;
   typedef std::integral_constant<int, 2> Two;
   typedef std::integral_constant<int, 4> Four;
-  if (p.few) pieces(Four(), One(), Two(), One());
+  if (p.few && p.tile == 128) pieces(Four(), One(), One(), One());
+  else if (p.few) pieces(Four(), One(), Two(), One());
   else if (p.tile == 128) pieces(Two(), Two(), Two(), Two());
   else if constexpr (T != COOP_F32) pieces(Two(), Two(), Four(), Four());
   if (!ok) return COOP_E_HIP;
