@@ -415,7 +415,7 @@ struct RowStage {
   static constexpr int kRows = 64, kRowBytes = KS * 32, kChunks = KS * 2, kBytes = kRows * kRowBytes, kMine = kBytes / 4096;
   static __device__ __forceinline__ int swizzle(int row) {
     const int r0 = row & 1, r1 = row >> 1 & 1, r2 = row >> 2 & 1, r3 = row >> 3 & 1;
-    return KS == 8 ? r2 | r0 << 1 | r1 << 2 | r3 << 3 : KS == 4 ? r2 | (r0 ^ r3) << 1 | r1 << 2 : r2 | (r1 ^ r3) << 1;
+    return KS == 16 ? r2 | r0 << 1 | r1 << 2 : KS == 8 ? r2 | r0 << 1 | r1 << 2 | r3 << 3 : KS == 4 ? r2 | (r0 ^ r3) << 1 | r1 << 2 : r2 | (r1 ^ r3) << 1;
   }
   // A lane's places in what it reads (from step to step and tile to tile they are an exclusive or with a few bits) and in what it loads:
   // 16 bytes of a row, the other loads of a stage in the same chunk as many rows further on.
@@ -428,7 +428,7 @@ struct RowStage {
       rows = (uint32_t)(r * kRowBytes + (((lane >> 5) ^ swizzle(r)) << 4));
       across = (uint32_t)(q * kRowBytes + (((c >> 3) ^ swizzle(q)) << 4) + (c & 7) * 2);
       const int place = wave * kWave + lane, row = place / kChunks, chunk = (place % kChunks) ^ swizzle(row);
-      static_assert(4096 / kRowBytes % 16 == 0, "the exchange of chunks goes by the row's last four bits");
+      static_assert(4096 / kRowBytes % (KS == 16 ? 8 : 16) == 0, "the exchange of chunks goes by the row's last three or four bits");
       load = chunk * 16 < ld ? row * ld + chunk * 16 : 0x3FFFFFFF;
     }
   };
@@ -465,7 +465,7 @@ __device__ __forceinline__ int lane_anew() {
 template <int T, int KS, bool TERMS, bool SUMS>
 struct RowStream {
   typedef RowStage<T, KS> S;
-  static constexpr int kStages = 4, kStage = S::kBytes + (TERMS ? 1024 : 0), kLds = kStages * kStage + (SUMS ? 4096 : 0), kLoads = S::kMine + (TERMS ? 1 : 0);
+  static constexpr int kStages = KS == 16 ? 2 : 4, kStage = S::kBytes + (TERMS ? 1024 : 0), kLds = kStages * kStage + (SUMS ? 4096 : 0), kLoads = S::kMine + (TERMS ? 1 : 0);
   const char* base;   // of the next stage
   const char* terms;  // of its rows: a wave has one of the three arrays (the last one the first again: all waves have as many loads)
   int left, step;     // rows that there are from the next stage's first (or less than none); from stage to stage
@@ -917,18 +917,18 @@ struct XentPlan {
     width = round_up(dim, 16 / es);
     ld = width * es;
     pad = !aligned || width != dim;
-    narrow = es == 2 && width <= 128 && (grad || n > 32);
+    narrow = es == 2 && width <= (grad ? 128 : 256) && (grad || n > 32);
     few = n <= 32 && !narrow;
     tile = narrow || (es == 2 || few) && ((n + 255) / 256) * ((vocab + 255) / 256) >= 256 ? 256 : 128;
     rows = few ? 32 : round_up(n, tile);
     const int blocks = 256 * (narrow || few || tile == 128 ? 2 : 1);
     const int64_t row_tiles = few ? 1 : rows / tile, vocab_tiles = (vocab + tile - 1) / tile;
     vocab_rows = vocab_tiles * tile;
-    // blocks: two of a narrow kernel or of few rows on a CU, one of the others; a multiple of 8 splits where there are so many, so that
-    // the blocks of an XCD have the same splits' tiles of W
+    // blocks: two of a narrow kernel or of few rows on a CU, one of the others; a multiple of 8 splits where that leaves out at most
+    // an eighth of them, so that the blocks of an XCD have the same splits' tiles of W
     if (few) splits = at_most((vocab_tiles + (vocab_tiles + 511) / 512 - 1) / ((vocab_tiles + 511) / 512), 512);  // (of as many tiles each)
     else splits = at_most(blocks / row_tiles, narrow ? (vocab + 63) / 64 : vocab_tiles);
-    if (!few && splits > 8) splits = splits / 8 * 8;
+    if (!few && splits / 8 * 8 * 8 >= splits * 7) splits = splits / 8 * 8;
     piece = kPieceBytes / (rows * es) / tile * tile;
     if (piece < tile) piece = tile;
     if (piece > vocab_rows) piece = vocab_rows;
@@ -994,12 +994,13 @@ bool launch_stats(const XentPlan& p, Operand w, Operand h, float alpha, const in
   return true;
 }
 
-// f(KS), for the steps of 16 elements that a narrow row is padded to
-template <typename F>
+// f(KS), for the steps of 16 elements that a row of up to MOST steps is padded to
+template <int MOST, typename F>
 void with_steps(int64_t width, F&& f) {
   if (width <= 32) f(std::integral_constant<int, 2>());
   else if (width <= 64) f(std::integral_constant<int, 4>());
-  else f(std::integral_constant<int, 8>());
+  else if (width <= 128) f(std::integral_constant<int, 8>());
+  else if constexpr (MOST > 8) f(std::integral_constant<int, MOST>());
 }
 
 template <int T>
@@ -1020,7 +1021,7 @@ int forward(const XentPlan& p, const void* hidden, const void* weight, int32_t d
   } else if (!p.narrow) {
     if constexpr (T != COOP_F32) ok = launch_stats<T, 2, 2, 4, 4>(p, w, h, alpha, targets, part, s);
   } else if constexpr (T != COOP_F32) {
-    with_steps(p.width, [&](auto ks) {
+    with_steps<16>(p.width, [&](auto ks) {
       constexpr int KS = decltype(ks)::value, lds = RowStream<T, KS, false, false>::kLds;
       const auto kernel = k_xent_stats_narrow<T, KS>;
       ok = allow_lds(kernel, lds);
@@ -1047,7 +1048,7 @@ template <int T>
 bool backward_narrow(const XentPlan& p, const Operand& w, const Operand& h, int32_t dim, float alpha, const RowTerms& term, const float* unlift,
                      void* dhidden, void* dweight, float* sums, hipStream_t s) {
   bool ok = true;
-  with_steps(p.width, [&](auto ks) {
+  with_steps<8>(p.width, [&](auto ks) {
     constexpr int KS = decltype(ks)::value, lds_h = RowStream<T, KS, false, true>::kLds, lds_w = RowStream<T, KS, true, true>::kLds;
     const auto kh = k_xent_dh_narrow<T, KS>;
     const auto kw = k_xent_dw_narrow<T, KS>;
