@@ -377,22 +377,25 @@ __global__ __launch_bounds__(kOutWaves* kWave) void k_xent_out(const float* __re
   }
 }
 
-// dW of the piece: rows v_first .. of the weight's gradient
+// dW of the piece, rows v_first .. of the weight's gradient: to out, or, split over H's rows, to sums[split][row of the piece][width].
 template <int T, int WA, int WB, int TA, int TB>
-__global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1))) void k_xent_dw(Operand ht, Operand gt, int64_t k, int64_t vocab, int64_t v_first, int32_t dim,
-                                                            uint32_t tiles_a, const float* __restrict__ unlift, char* __restrict__ out) {
+__global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1))) void k_xent_dw(
+    Operand ht, Operand gt, int64_t k, int splits, int64_t vocab, int64_t v_first, int32_t dim, uint32_t tiles_a, const float* __restrict__ unlift,
+    char* __restrict__ out, float* __restrict__ sums, int64_t rows, int64_t width) {
   typedef Product<T, WA, WB, TA, TB, true, true, kNarrow> P;
   extern __shared__ char lds[];
-  const int64_t col0 = (int64_t)(blockIdx.x % tiles_a) * P::kRowsA, piece0 = (int64_t)(blockIdx.x / tiles_a) * P::kRowsB;
+  const uint32_t tile = blockIdx.x / splits, split = blockIdx.x % splits;
+  const int64_t col0 = (int64_t)(tile % tiles_a) * P::kRowsA, piece0 = (int64_t)(tile / tiles_a) * P::kRowsB;
+  const int64_t stages = (k + P::kK - 1) / P::kK;
   P p;
-  p.begin(ht, gt, col0, piece0, 0, k, 0, lds);
+  p.begin(ht, gt, col0, piece0, stages * split / splits * P::kK, stages * (split + 1) / splits * P::kK, 0, lds);
   p.zero();
   p.tile();
   P::end();
   const float u = *unlift;
 #pragma unroll
   for (int j = 0; j < TB; ++j) {
-    const int64_t v = v_first + piece0 + P::b0() + j * 32 + (lane_id() & 31);
+    const int64_t at = piece0 + P::b0() + j * 32 + (lane_id() & 31), v = v_first + at;
     if (v >= vocab) continue;
 #pragma unroll
     for (int a = 0; a < TA; ++a)
@@ -401,8 +404,9 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
         const int64_t c = col0 + P::a0() + P::own_row() + a * 32 + P::row_of(4 * q);
         float f[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = p.acc[a][j][4 * q + e] * u;
-        put_columns<T>(out, v, c, dim, f);
+        for (int e = 0; e < 4; ++e) f[e] = sums == nullptr ? p.acc[a][j][4 * q + e] * u : p.acc[a][j][4 * q + e];
+        if (sums == nullptr) put_columns<T>(out, v, c, dim, f);
+        else if (c < width) store_elements<COOP_F32, 4>(sums + ((int64_t)split * rows + at) * width + c, f);
       }
   }
 }
@@ -906,11 +910,11 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 //   128 x 128, two blocks on a CU (2,236 rows, 170 vertices, 768 elements of bf16: 148 -> 82 us).  Few rows' gradients take tiles of 32 rows.
 struct XentPlan {
   int64_t n, vocab, width, ld;  // width: elements of a padded row
-  int64_t rows, piece, vocab_rows;
+  int64_t rows, piece, vocab_rows, dw_rows;
   int64_t g_ld;  // bytes from row to row of G: not a power of two, or a tile's rows would all lie in the same few channels of memory
   int splits, dh_splits, dw_splits, tile;
   bool few, narrow, pad;
-  size_t h, w, part, coef, lse2, target, unlift, tops, g, sums, bytes;
+  size_t h, w, part, coef, lse2, target, unlift, tops, g, sums, dw_sums, bytes;
   static int at_most(int64_t x, int64_t most) { return (int)(x < 1 ? 1 : x < most ? x : most); }
   XentPlan(int64_t n_, int64_t vocab_, int32_t dim, int dtype, bool aligned, bool grad) : n(n_), vocab(vocab_) {
     const int es = element_bytes(dtype);
@@ -933,8 +937,11 @@ struct XentPlan {
     if (piece < tile) piece = tile;
     if (piece > vocab_rows) piece = vocab_rows;
     const int64_t dh_tiles = row_tiles * ((width + tile - 1) / tile), first = piece < vocab ? piece : vocab;
-    dh_splits = narrow ? splits : at_most(at_most(blocks / dh_tiles, 64), (first * es + kWide - 1) / kWide);
-    dw_splits = narrow ? at_most(512 / vocab_tiles, (n + 63) / 64) : 1;
+    dh_splits = narrow ? splits : at_most(blocks / dh_tiles, (first * es + 4 * kWide - 1) / (4 * kWide));
+    const int dw_tile = few ? 128 : tile;
+    const int64_t dw_tiles = (first + dw_tile - 1) / dw_tile * ((width + dw_tile - 1) / dw_tile);
+    dw_rows = narrow ? vocab_rows : round_up(first, dw_tile);
+    dw_splits = narrow ? at_most(512 / vocab_tiles, (n + 63) / 64) : at_most((dw_tile == 128 ? 512 : 256) / dw_tiles, (n * es + 8 * kNarrow - 1) / (8 * kNarrow));
     size_t at = 0;
     auto take = [&](size_t b) { const size_t o = at; at += (b + 255) & ~(size_t)255; return o; };
     h = take(grad ? (size_t)rows * ld : pad ? (size_t)n * ld : 0);
@@ -947,8 +954,8 @@ struct XentPlan {
     tops = take(grad ? 256 * sizeof(float) : 0);
     g_ld = piece * es + 256;
     g = take(grad && !narrow ? (size_t)rows * g_ld : 0);
-    const size_t dh = (size_t)dh_splits * rows * width * 4, dw = dw_splits > 1 ? (size_t)dw_splits * vocab_rows * width * 4 : 0;
-    sums = take(grad ? (dh > dw ? dh : dw) : 0);
+    sums = take(grad ? (size_t)dh_splits * rows * width * 4 : 0);
+    dw_sums = take(grad && dw_splits > 1 ? (size_t)dw_splits * dw_rows * width * 4 : 0);
     bytes = at + 256;
   }
 };
@@ -1046,7 +1053,7 @@ void write_out(const float* sums, int splits, int64_t rows, const XentPlan& p, i
 
 template <int T>
 bool backward_narrow(const XentPlan& p, const Operand& w, const Operand& h, int32_t dim, float alpha, const RowTerms& term, const float* unlift,
-                     void* dhidden, void* dweight, float* sums, hipStream_t s) {
+                     void* dhidden, void* dweight, float* sums, float* dw_sums, hipStream_t s) {
   bool ok = true;
   with_steps<8>(p.width, [&](auto ks) {
     constexpr int KS = decltype(ks)::value, lds_h = RowStream<T, KS, false, true>::kLds, lds_w = RowStream<T, KS, true, true>::kLds;
@@ -1060,10 +1067,10 @@ bool backward_narrow(const XentPlan& p, const Operand& w, const Operand& h, int3
       write_out<T>(sums, p.dh_splits, p.rows, p, p.n, dim, unlift, dhidden, s);
     }
     if (dweight != nullptr) {
-      float* parts = p.dw_splits > 1 ? sums : nullptr;
+      float* parts = p.dw_splits > 1 ? dw_sums : nullptr;
       COOP_LAUNCH(K_XENT_DW, kw, dim3((unsigned)(p.vocab_rows / p.tile * p.dw_splits)), dim3(256), lds_w, s, w, h, p.vocab, alpha * kLog2e, term, p.dw_splits,
-                  unlift, dim, (char*)dweight, parts, p.vocab_rows, (int32_t)p.width);
-      if (parts != nullptr) write_out<T>(parts, p.dw_splits, p.vocab_rows, p, p.vocab, dim, unlift, dweight, s);
+                  unlift, dim, (char*)dweight, parts, p.dw_rows, (int32_t)p.width);
+      if (parts != nullptr) write_out<T>(parts, p.dw_splits, p.dw_rows, p, p.vocab, dim, unlift, dweight, s);
     }
   });
   return ok;
@@ -1072,7 +1079,7 @@ bool backward_narrow(const XentPlan& p, const Operand& w, const Operand& h, int3
 // tiles of W's (or G's) rows or columns by H's rows: WA x WB waves of TA x TB; the weight's gradient in square ones
 template <int T, int WA, int WB, int TA, int TB>
 bool backward_pieces(const XentPlan& p, const Operand& w, const Operand& h, int32_t dim, float alpha, const RowTerms& term, const float* unlift,
-                     void* dhidden, void* dweight, char* g, float* sums, hipStream_t s) {
+                     void* dhidden, void* dweight, char* g, float* sums, float* dw_sums, hipStream_t s) {
   constexpr int N = TA == 4 ? 4 : 2;
   typedef Product<T, WA, WB, TA, TB, false, false, kWide> G;
   typedef Product<T, WA, WB, TA, TB, true, false, kWide> H;
@@ -1098,8 +1105,10 @@ bool backward_pieces(const XentPlan& p, const Operand& w, const Operand& h, int3
     }
     if (dweight != nullptr) {
       const Operand ht{h.base, p.ld, p.ld, p.n}, gt{g, p.g_ld, g_bytes, p.rows};
-      COOP_LAUNCH(K_XENT_DW, kw, dim3(tiles_of(len, W::kRowsB) * w_tiles), dim3(W::kThreads), W::kLds, s, ht, gt, p.n, p.vocab, v, dim, w_tiles, unlift,
-                  (char*)dweight);
+      float* parts = p.dw_splits > 1 ? dw_sums : nullptr;
+      COOP_LAUNCH(K_XENT_DW, kw, dim3(tiles_of(len, W::kRowsB) * w_tiles * p.dw_splits), dim3(W::kThreads), W::kLds, s, ht, gt, p.n, p.dw_splits, p.vocab,
+                  v, dim, w_tiles, unlift, (char*)dweight, parts, p.dw_rows, p.width);
+      if (parts != nullptr) write_out<T>(parts, p.dw_splits, p.dw_rows, p, len, dim, unlift, (char*)dweight + v * dim * kElem<T>, s);
     }
   }
   return true;
@@ -1110,7 +1119,7 @@ int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t 
              const float* lse, const float* dloss, void* dhidden, void* dweight, char* ws, int32_t* bad, hipStream_t s) {
   const RowTerms term{(float*)(ws + p.coef), (float*)(ws + p.lse2), (int32_t*)(ws + p.target)};
   float* unlift = (float*)(ws + p.unlift);
-  float* sums = (float*)(ws + p.sums);
+  float *sums = (float*)(ws + p.sums), *dw_sums = (float*)(ws + p.dw_sums);
   float* tops = (float*)(ws + p.tops);
   const int n_tops = T == COOP_F32 || p.n <= kTopRows ? 0 : 256;
   if (n_tops != 0) COOP_LAUNCH(K_XENT_TERMS, k_xent_top, dim3(n_tops), dim3(1024), 0, s, targets, ignore, dloss, alpha, p.n, p.vocab, tops);
@@ -1122,13 +1131,13 @@ int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t 
   const Operand w{(const char*)weight, p.ld, p.vocab, p.ld}, h{(const char*)hidden, p.ld, p.n, p.ld};
   if constexpr (T != COOP_F32)
     if (p.narrow) {
-      if (!backward_narrow<T>(p, w, h, dim, alpha, term, unlift, dhidden, dweight, sums, s)) return COOP_E_HIP;
+      if (!backward_narrow<T>(p, w, h, dim, alpha, term, unlift, dhidden, dweight, sums, dw_sums, s)) return COOP_E_HIP;
       return hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
     }
   bool ok = true;
   const auto pieces = [&](auto wa, auto wb, auto ta, auto tb) {
     ok = backward_pieces<T, decltype(wa)::value, decltype(wb)::value, decltype(ta)::value, decltype(tb)::value>(p, w, h, dim, alpha, term, unlift, dhidden,
-                                                                                                       dweight, ws + p.g, sums, s);
+                                                                                                       dweight, ws + p.g, sums, dw_sums, s);
   };
   typedef std::integral_constant<int, 1> One;
   typedef std::integral_constant<int, 2> Two;
