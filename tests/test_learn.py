@@ -309,7 +309,7 @@ def test_softmax_xent(dtype, n, vocab, dim):
 # for the largest coefficient, of a few classes; rows that end in each quarter of a stage
 @gpu
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
-@pytest.mark.parametrize("n,vocab,dim", [(4097, 4100, 200), (16384, 20000, 136), (300, 140000, 40), (200, 131100, 128), (40000, 47, 24), (33000, 70, 200),
+@pytest.mark.parametrize("n,vocab,dim", [(4097, 4100, 200), (16384, 20000, 136), (300, 140000, 40), (200, 131100, 128), (40000, 47, 24), (33000, 70, 200), (1200001, 300, 136),
                                          (16, 70, 8), (17, 81, 24), (48, 113, 72), (63, 127, 120)])
 def test_softmax_xent_of_many_and_of_few(dtype, n, vocab, dim):
     check_xent(dtype, n, vocab, dim, 0.8)
