@@ -162,16 +162,9 @@ constexpr float kLift = T == COOP_F16 ? 13.f : 0.f;
 template <int T>
 constexpr float kOne = T == COOP_F16 ? 8192.f : 1.f;
 
-// the largest |coef| among the rows first, first + step, .. that count, of a block
-__device__ __forceinline__ float block_top(const int32_t* __restrict__ targets, int32_t ignore, const float* __restrict__ dloss, float alpha,
-                                           int64_t first, int64_t step, int64_t n, int64_t vocab) {
+// the largest among a block's 1024 threads
+__device__ __forceinline__ float block_max(float top) {
   __shared__ float lds[16];
-  float top = 0.f;
-  for (int64_t i = first; i < n; i += step) {
-    const int32_t t = targets[i];
-    const float c = fabsf(alpha * dloss[i]);
-    if (t != ignore && (uint64_t)(int64_t)t < (uint64_t)vocab && c < __builtin_inff()) top = fmaxf(top, c);
-  }
 #pragma unroll
   for (int off = 1; off < kWave; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
   if (lane_id() == 0) lds[wave_in_block()] = top;
@@ -180,13 +173,24 @@ __device__ __forceinline__ float block_top(const int32_t* __restrict__ targets, 
   for (int w = 0; w < 16; ++w) top = fmaxf(top, lds[w]);
   return top;
 }
+// the largest |coef| among a thread's rows first, first + step, .. that count
+__device__ __forceinline__ float rows_top(const int32_t* __restrict__ targets, int32_t ignore, const float* __restrict__ dloss, float alpha,
+                                          int64_t first, int64_t step, int64_t n, int64_t vocab) {
+  float top = 0.f;
+  for (int64_t i = first; i < n; i += step) {
+    const int32_t t = targets[i];
+    const float c = fabsf(alpha * dloss[i]);
+    if (t != ignore && (uint64_t)(int64_t)t < (uint64_t)vocab && c < __builtin_inff()) top = fmaxf(top, c);
+  }
+  return top;
+}
 
 // Up to kTopRows rows every block of k_xent_terms looks for the largest itself, which costs less than a launch; of more rows, up to 256
 // blocks do, and it looks through theirs.
 constexpr int64_t kTopRows = 32768;
 __global__ __launch_bounds__(1024) void k_xent_top(const int32_t* __restrict__ targets, int32_t ignore, const float* __restrict__ dloss, float alpha,
                                                    int64_t n, int64_t vocab, float* __restrict__ tops) {
-  const float top = block_top(targets, ignore, dloss, alpha, (int64_t)blockIdx.x * 1024 + threadIdx.x, (int64_t)gridDim.x * 1024, n, vocab);
+  const float top = block_max(rows_top(targets, ignore, dloss, alpha, (int64_t)blockIdx.x * 1024 + threadIdx.x, (int64_t)gridDim.x * 1024, n, vocab));
   if (threadIdx.x == 0) tops[blockIdx.x] = top;
 }
 
@@ -196,8 +200,9 @@ __global__ __launch_bounds__(1024) void k_xent_terms(const int32_t* __restrict__
                                                      const float* __restrict__ tops, int n_tops, RowTerms term, float* __restrict__ unlift, int32_t* __restrict__ bad) {
   float top = 0.f;
   if constexpr (LIFT) {
-    if (n_tops == 0) top = block_top(targets, ignore, dloss, alpha, threadIdx.x, 1024, n, vocab);
-    for (int b = 0; b < n_tops; ++b) top = fmaxf(top, tops[b]);
+    if (n_tops == 0) top = rows_top(targets, ignore, dloss, alpha, threadIdx.x, 1024, n, vocab);
+    else if ((int)threadIdx.x < n_tops) top = tops[threadIdx.x];
+    top = block_max(top);
     if (top < 0x1p-100f) top = 0x1p-100f;
     if (top > 0x1p100f) top = 0x1p100f;
   }
