@@ -4,6 +4,8 @@
 //
 // Bound by HBM: parameter, gradient and moments are read once and written once.  All arithmetic is in 32 bits; every product and sum
 // is rounded on its own (the file is compiled without contraction).
+// 300 tensors, 100 million parameters in fp32, gradients and copies in bf16: 545 us, 2.8 GB at 5.1 TB/s.  500,000 of 2.45 million rows of
+// 100 parameters, moments in 8 bits: 279 us for 0.8 GB, 1.07 GB with the whole 128-byte lines of rows of 400 and of 100 bytes.
 //
 // Moments in 8 bits.  m, and the root of v (half the exponents, and never negative), are kept as 8-bit floats of 4 exponent and 3
 // mantissa bits (OCP E4M3) over a 32-bit scale for each 256 neighbouring elements of a row: scale = largest magnitude / 448, so the

@@ -9,10 +9,19 @@
 // The logits are computed as vocabulary x hidden: a lane then holds many logits of one row of H, and neither maximum, sum nor target
 // takes another lane until the end.
 //
-// Rows of up to 128 elements of 16 bits (narrow) go another way: there the exponentials weigh as much as the products, and G would be
-// written and read for little arithmetic.  A wave keeps 64 rows of one operand in its registers as fragments, the other operand streams
-// through LDS, and G never leaves the registers: the 32 x 32 tile of logits that a product leaves is, rounded and packed, a fragment of
-// the next product, if that takes its k in the order in which the first one left its rows.
+// Rows of up to 128 elements of 16 bits (narrow; forward, up to 256) go another way: there the exponentials weigh as much as the products,
+// and G would be written and read for little arithmetic.  A wave keeps 64 rows of one operand in its registers as fragments, the other
+// operand streams through LDS, and G never leaves the registers: the 32 x 32 tile of logits that a product leaves is, rounded and packed, a
+// fragment of the next product, if that takes its k in the order in which the first one left its rows.  The logits are then computed three
+// times (five products in the place of four), and nothing of the size of G is moved.  Backward with 256 elements the sums would not fit.
+//
+// Rates (2 n vocab dim for a product; a library product of 8192^3 reaches 1,382 TFLOP/s in bf16 and 153 in fp32):
+//   8,192 x 232,965 x 128 bf16, narrow: statistics 525 us, 930 TFLOP/s (the matrix units at work 46% of the time; the exponentials and the
+//     maximum beside them); dH, two products, 807 us, 1,210 (61%); dW 921 us, 1,060 (55%; 64 more factors a lane and stage, coef of the rows).
+//   8,192 x 131,072 x 1,024 bf16: statistics 2,059 us, 1,070 (49%); G 2,427 us, 906, the 2.1 GB that it writes among it; dH 1,861, 1,180;
+//     dW 1,734, 1,270.  A wave has its SIMD to itself (its sums are half of all registers): what follows a tile's products is not hidden.
+//   1,021 x 50,021 x 100 fp32: 125 to 150 us each, 70 to 82 TFLOP/s: the units at work 80 to 90% of the time, on rows taken as 128 elements.
+//   24 x 232,965 x 128 bf16: 13 us, W's 60 MB at 4.5 TB/s.
 #include <type_traits>
 
 #include "coop_internal.h"
@@ -32,6 +41,10 @@ constexpr float kNoMax = -3.402823466e38f;
 struct TilePair {
   uint32_t a, b;
   __device__ __forceinline__ TilePair(uint32_t na, uint32_t nb, int64_t tile_bytes) {
+    if (nb == 1) {
+      a = blockIdx.x, b = 0;
+      return;
+    }
     const uint32_t fit = (uint32_t)((2 << 20) / tile_bytes), strip = fit < 4 ? 4 : fit;
     const uint32_t i = xcd_runs(blockIdx.x, gridDim.x), first = i / (na * strip) * strip, at = i - first * na, rows = nb - first < strip ? nb - first : strip;
     a = at / rows;
@@ -49,7 +62,7 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
                                                                const int32_t* __restrict__ targets, int splits, RowStat* __restrict__ part) {
   typedef Product<T, WA, WB, TA, TB, false, false, kWide> P;
   extern __shared__ char lds[];
-  const TilePair tiles(splits, gridDim.x / splits, P::kRowsB * h.ld);
+  const TilePair tiles(splits, WB * TB == 1 ? 1 : gridDim.x / splits, P::kRowsB * h.ld);  // (few rows: one tile of them)
   const int split = tiles.a;
   const int64_t row0 = (int64_t)tiles.b * P::kRowsB;
   P p;
@@ -270,7 +283,7 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
                                                            uint32_t tiles_a, RowTerms term, char* __restrict__ g, int64_t ld) {
   typedef Product<T, WA, WB, TA, TB, false, false, kWide> P;
   extern __shared__ char lds[];
-  const TilePair tiles(tiles_a, gridDim.x / tiles_a, P::kRowsB * h.ld);
+  const TilePair tiles(tiles_a, WB * TB == 1 ? 1 : gridDim.x / tiles_a, P::kRowsB * h.ld);
   const int64_t piece0 = (int64_t)tiles.a * P::kRowsA, row0 = (int64_t)tiles.b * P::kRowsB;
   P p;
   p.begin(w, h, v_first + piece0, row0, 0, k, 0, lds);
@@ -433,7 +446,7 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
   }
 }
 
-// ---- narrow: rows of up to 128 elements of 16 bits -----------------------------------------------------------------------------
+// ---- narrow: rows of up to 128 (forward 256) elements of 16 bits -----------------------------------------------------------------------------
 // A stage: 64 rows of 16 KS elements, in LDS as their chunks of 16 bytes, exchanged by the row's number: what 8 or 16 lanes read of one
 // chunk of successive rows lies in different banks, and so does what they read of four rows' same 16 elements (transposed).
 template <int T, int KS>
@@ -485,7 +498,7 @@ __device__ __forceinline__ int lane_anew() {
   return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, none));
 }
 
-// The stages of rows first, first + step, .. of an operand, four in LDS as in Product; with TERMS the rows' coef, lse2 and target go with
+// The stages of rows first, first + step, .. of an operand, four in LDS (two of 32 KB); with TERMS the rows' coef, lse2 and target go with
 // them.  Four waves.  SUMS: the waves keep sums beside their rows, and there are no registers for the lanes' places: they lie in LDS, and are
 // read each stage.  (Spilled, a wait for them would be a wait for the loads of the stages ahead; made anew they cost 4% of dW's time.)
 template <int T, int KS, bool TERMS, bool SUMS>
@@ -583,7 +596,8 @@ __device__ __forceinline__ void pack(const f32x16& x, u32x4 (&f)[2]) {
   }
 }
 
-// Forward: as k_xent_stats; a block has 256 rows of H, a wave 64 of them, and every splits-th stage of 64 rows of W.
+// Forward: as k_xent_stats; a block has 256 rows of H, a wave 64 of them, and every splits-th stage of 64 rows of W.  (10,784 rows, 11,256
+// vertices, 256 elements of bf16: 70 us; in tiles of 256 x 256, whose exponentials nothing hides, 121.)
 template <int T, int KS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_xent_stats_narrow(
     Operand w, Operand h, int64_t n, int64_t vocab, float scale2, const int32_t* __restrict__ targets, int splits, RowStat* __restrict__ part) {
@@ -926,10 +940,12 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 // How a call is cut, and what of the workspace it uses for what.
 //   few:    up to 32 rows.  W is read once and that is all there is to it: tiles of 32 rows of H, as many blocks as there are tiles of W.
-//   narrow: more rows, of up to 128 elements of 16 bits (above).
+//   narrow: rows of up to 128 elements of 16 bits, forward up to 256 where there are more than 32 of them (above).
 //   else products in tiles, a piece of the vocabulary at a time.  Of 256 x 256, what a wave's registers hold, where there are enough of
 //   them for the chip: the matrix units then take all that LDS gives.  Else, and in fp32, where they are sixteen times slower, of
-//   128 x 128, two blocks on a CU (2,236 rows, 170 vertices, 768 elements of bf16: 148 -> 82 us).  Few rows' gradients take tiles of 32 rows.
+//   128 x 128, two blocks on a CU (2,236 rows, 170 vertices, 768 elements of bf16: 148 -> 82 us).
+//   Of few rows' tiles of W there are twice as many, half as large, where they would not fill the chip (16,048 vertices, 1,024 elements of
+//   fp32: 43 -> 28 us).  dW is split over the rows where it has few tiles (14,644 rows, 6,570 vertices, 1 element of fp32: 885 -> 194 us).
 struct XentPlan {
   int64_t n, vocab, width, ld;  // width: elements of a padded row
   int64_t rows, piece, vocab_rows, dw_rows;
