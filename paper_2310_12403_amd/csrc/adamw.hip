@@ -52,7 +52,7 @@ struct Listed : Whole {
 
 struct Hyper { float keep1, take1, keep2, take2, decay, rate, undo, eps; };
 
-// A launch's tensors are its arguments (at most 4 KB): nothing is copied to the device ahead of it, and nothing is kept.  (63 tensors
+// A launch's tensors are its arguments (at most 4 KB): nothing is copied to the device ahead of it, and nothing is kept.  (62 tensors
 // with 32-bit moments and without a list: 300 of them in 5 launches in the place of 12, 647 -> 558 us with non-temporal accesses.)
 template <typename Tensor>
 struct Step {
