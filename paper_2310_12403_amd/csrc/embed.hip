@@ -85,7 +85,7 @@ constexpr int kDigits = 1 << kDigitBits;
 constexpr int64_t kOwnTiles = 512;
 
 // The zeros of a dense gradient, written by blocks of the sort's launches behind those that sort: a launch less where there are few (76 -> 71
-// us for 50,021 rows of 75), and where there are many the sort goes on beside them (944 MB and 3,853 tokens: 230 -> 199 us).  In pieces of
+// us for 50,021 rows of 75), and where there are many the sort goes on beside them (944 MB and 3,853 tokens: 230 -> 199 us, sums and all).  In pieces of
 // 16 bytes; `head` bytes in front of the first and `tail` behind the last, 2 a thread.
 struct Zeros {
   char* p;
@@ -375,7 +375,7 @@ __global__ __launch_bounds__(kFewTokens) void k_sort_few(SortInput in, int n, ui
 // whole spans of 32 and of 1,024 chunks, whose partial sums k_embed_spans adds up ahead, and k_embed_join adds a row's chunks and
 // spans in their order.  No order depends on time: the same input gives the same bits.
 // 1,019,311 tokens of 128 elements of bf16, 572,596 rows of fp32: the sums 112 us, 261 MB read and 304 written at 5.0 TB/s; rows' numbers
-// (k_embed_heads) 8, spans 6, join 18 us.  A scaled dense gradient of 65,537 tokens of 75 elements is seven launches of 5 to 19 us.
+// (k_embed_heads) 8, spans 6, join 18 us.  A scaled dense gradient of 65,537 tokens of 75 elements is seven launches of 5 to 14 us.
 constexpr int kChunk = 32;
 constexpr int kAhead = 8;      // rows in flight per group
 constexpr int kSpan = 32;      // chunks
@@ -466,7 +466,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_sum(const uint32_t* __restrict
     for (int u = 0; u < kAhead; ++u) {
       const int64_t j = i + u < end ? i + u : end - 1;
       next_place[u] = places[j];
-      next_key[u] = i + u < end ? keys[j] : sh.n_rows;
+      next_key[u] = keys[j];
     }
   };
   look_ahead(beg);
@@ -474,10 +474,16 @@ __global__ __launch_bounds__(kBlock) void k_embed_sum(const uint32_t* __restrict
     uint32_t key[kAhead];
     In x[kAhead];
     float s[kAhead];
+    if (scale != nullptr) {  // (one branch for all of them: behind a branch each, each would be waited for by itself)
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) s[u] = scale[next_place[u]];
+    } else {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) s[u] = 1.f;
+    }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       key[u] = next_key[u];
-      s[u] = scale != nullptr ? scale[next_place[u]] * alpha : alpha;
       x[u] = In::load(dout + ((int64_t)next_place[u] * sh.dim + col) * (int64_t)sizeof(typename In::M));
     }
     if (i + kAhead < end) look_ahead(i + kAhead);
@@ -499,7 +505,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_sum(const uint32_t* __restrict
         float f[E];
         x[u].get(f);
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = __builtin_fmaf(f[e], s[u], acc[e]);
+        for (int e = 0; e < E; ++e) acc[e] = __builtin_fmaf(f[e], s[u] * alpha, acc[e]);
       }
     }
   }
