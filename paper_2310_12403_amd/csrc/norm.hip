@@ -107,15 +107,28 @@ struct RowPacks {
   }
 };
 
-template <int T, int E>
-__device__ __forceinline__ void load_row(const char* p, int32_t at, bool live, float (&f)[E]) {
-  if (live) {
-    load_elements<T, E>(p + (int64_t)at * (int64_t)sizeof(typename Element<T>::M), f);
-  } else {
+// A lane's columns of the weight or the bias: kept in registers over all rows, or read anew for each.  Kept with two packs a lane, whose
+// reads would wait for each other (445,906 rows of 602 elements of bf16 372 -> 281 us forward, 444 -> 374 backward; 32,768 of 8,192 of fp32
+// forward 410 -> 365), but not beside the sums of rows on sixteen waves (16,384 of 16,384 of bf16 backward 456 -> 587); of one pack they are
+// as soon read (2,097,152 rows of 128 of fp32 forward 420, kept 450).
+template <int W, int E, int K, bool kKept>
+struct LaneWeights {
+  float x[kKept ? K : 1][E];
+  const char* p;
+  __device__ __forceinline__ LaneWeights(const char* p_, int lane, int lanes, int32_t dim) : p(p_) {
+    if (!kKept || p == nullptr) return;
 #pragma unroll
-    for (int e = 0; e < E; ++e) f[e] = 0.f;
+    for (int k = 0; k < (kKept ? K : 0); ++k) load_elements<W, E>(p + (int64_t)Columns<E>(lane + k * lanes, dim).at * (int64_t)sizeof(typename Element<W>::M), x[k]);
   }
-}
+  __device__ __forceinline__ void get(int k, int32_t at, float (&f)[E]) const {  // (only where there are any)
+    if constexpr (kKept) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) f[e] = x[k][e];
+    } else {
+      load_elements<W, E>(p + (int64_t)at * (int64_t)sizeof(typename Element<W>::M), f);
+    }
+  }
+};
 
 template <int T, int W, int E, int K, int WAVES>
 __global__ __launch_bounds__(kNormBlock<WAVES>) void k_norm(const char* __restrict__ x, NormShape sh, const char* __restrict__ weight,
@@ -126,6 +139,7 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_norm(const char* __restri
   const int lanes = rows.lanes(sh);
   const int64_t row_bytes = (int64_t)sh.dim * (int64_t)sizeof(typename Element<T>::M);
   const float n = (float)sh.dim;
+  const LaneWeights<W, E, K, K == 2> w_of(weight, rows.lane, lanes, sh.dim), b_of(bias, rows.lane, lanes, sh.dim);
   RowPacks<T, E, K> next;  // (the next row is on its way while this one is worked on)
   if (rows.first < sh.rows) next.load(x + rows.first * row_bytes, rows.lane, lanes, sh.dim);
   for (int64_t r = rows.first; r < sh.rows; r += rows.step) {
@@ -157,8 +171,8 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_norm(const char* __restri
       const Columns<E> c(rows.lane + k * lanes, sh.dim);
       if (!c.live) continue;
       float w[E], b[E];
-      if (weight != nullptr) load_row<W, E>(weight, c.at, true, w);
-      if (bias != nullptr) load_row<W, E>(bias, c.at, true, b);
+      if (weight != nullptr) w_of.get(k, c.at, w);
+      if (bias != nullptr) b_of.get(k, c.at, b);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         float v = f[k][e] * rstd;
@@ -177,7 +191,11 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_norm(const char* __restri
   }
 }
 
-// part: [gridDim.x][2][dim], the block's sums of dy h and of dy (null: not asked for)
+// Rows on sixteen waves with 32 columns a lane or more: the sums for the weight's gradient do not fit beside them into the 128 registers of
+// a lane, and are a kernel's of their own.  (16,384 rows of 16,384 elements of bf16, 16 columns: 458 us, and 500 with the second kernel.)
+template <int E, int K, int WAVES> constexpr bool kSumsApart = WAVES == 16 && E * K >= 32;
+
+// part: [gridDim.x][2][dim], the block's sums of dy h and of dy (null: not asked for, or not here)
 template <int T, int W, int E, int K, int WAVES>
 __global__ __launch_bounds__(kNormBlock<WAVES>) void k_norm_grad(const char* __restrict__ dy, const char* __restrict__ x, NormShape sh,
                                                                  const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
@@ -189,6 +207,7 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_norm_grad(const char* __r
   const int lanes = rows.lanes(sh);
   const int64_t row_bytes = (int64_t)sh.dim * (int64_t)sizeof(typename Element<T>::M);
   const float n = (float)sh.dim;
+  const LaneWeights<W, E, K, K == 2 && WAVES < 16> w_of(weight, rows.lane, lanes, sh.dim);
   float dw[K][E], db[K][E];
 #pragma unroll
   for (int k = 0; k < K; ++k)
@@ -217,12 +236,14 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_norm_grad(const char* __r
     for (int k = 0; k < K; ++k) {
       const Columns<E> c(rows.lane + k * lanes, sh.dim);
       float w[E];
-      if (weight != nullptr) load_row<W, E>(weight, c.at, c.live, w);
+      if (weight != nullptr) w_of.get(k, c.at, w);  // (of a lane without columns those of the first: it writes nothing, and its sums count nothing)
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         h[k][e] = (h[k][e] - mean) * rstd;
-        dw[k][e] += d[k][e] * h[k][e];
-        db[k][e] += d[k][e];
+        if constexpr (!kSumsApart<E, K, WAVES>) {
+          dw[k][e] += d[k][e] * h[k][e];
+          db[k][e] += d[k][e];
+        }
         if (weight != nullptr) d[k][e] *= w[e];
         s1 += e >= c.own ? d[k][e] : 0.f;
         s2 += e >= c.own ? d[k][e] * h[k][e] : 0.f;
@@ -242,7 +263,7 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_norm_grad(const char* __r
       out.store_nt(dx + r * row_bytes + (int64_t)c.at * (int64_t)sizeof(typename Element<T>::M));
     }
   }
-  if (part == nullptr) return;
+  if (kSumsApart<E, K, WAVES> || part == nullptr) return;
   float* to = part + (int64_t)blockIdx.x * 2 * sh.dim;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
@@ -265,6 +286,44 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_norm_grad(const char* __r
         for (int e = 0; e < E; ++e)
           if (e >= c.own) to[(int64_t)q * sh.dim + c.at + e] = sums[e];
     }
+  }
+}
+
+// part[split]: the sums of dy h and of dy over every splits-th four rows, of 64 E columns a block; a wave has every fourth row.  (8,192 rows of
+// 32,768 elements of bf16, weight and all: 1,587 -> 686 us, x and dy read twice.)
+template <int T, int E>
+__global__ __launch_bounds__(kBlock) void k_norm_sums(const char* __restrict__ dy, const char* __restrict__ x, NormShape sh,
+                                                      const float* __restrict__ mean, const float* __restrict__ rstd, float* __restrict__ part) {
+  __shared__ float lds[kWavesPerBlock][2 * E][kWave];
+  const Columns<E> c((int32_t)blockIdx.x * kWave + lane_id(), sh.dim);
+  const int64_t row_bytes = (int64_t)sh.dim * (int64_t)sizeof(typename Element<T>::M), at = (int64_t)c.at * (int64_t)sizeof(typename Element<T>::M);
+  const int wave = uniform_wave_in_block();
+  float sums[2 * E];
+#pragma unroll
+  for (int e = 0; e < 2 * E; ++e) sums[e] = 0.f;
+#pragma unroll 4
+  for (int64_t r = (int64_t)blockIdx.y * kWavesPerBlock + wave; r < sh.rows; r += (int64_t)gridDim.y * kWavesPerBlock) {
+    const float m = mean[r], s = rstd[r];
+    float h[E], d[E];
+    Pack<T, E>::load_nt(x + r * row_bytes + at).get(h);
+    Pack<T, E>::load_nt(dy + r * row_bytes + at).get(d);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      sums[e] += d[e] * ((h[e] - m) * s);
+      sums[E + e] += d[e];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 2 * E; ++e) lds[wave][e][lane_id()] = sums[e];
+  __syncthreads();
+  if (wave != 0 || !c.live) return;
+  float* to = part + (int64_t)blockIdx.y * 2 * sh.dim;
+#pragma unroll
+  for (int e = 0; e < 2 * E; ++e) {
+    float t = sums[e];
+#pragma unroll
+    for (int w = 1; w < kWavesPerBlock; ++w) t += lds[w][e][lane_id()];
+    if (e % E >= c.own) to[(int64_t)(e / E) * sh.dim + c.at + e % E] = t;
   }
 }
 
@@ -401,14 +460,22 @@ extern "C" int coop_layer_norm_grad(const void* dy, const void* x, int64_t n_row
   if (sums && (workspace_bytes < coop_layer_norm_grad_workspace_bytes(n_rows, dim, dtype) || ((uintptr_t)workspace & 15) != 0)) return COOP_E_ARG;
   hipStream_t s = (hipStream_t)stream;
   const NormShape sh{n_rows, dim, l.lanes, l.lanes_log2, 0.f};
-  const int64_t blocks = norm_blocks(n_rows, l, true);
+  int64_t blocks = norm_blocks(n_rows, l, true);
   float* part = sums ? (float*)workspace : nullptr;
   if (n_rows > 0)
     with_types(dtype, weight_dtype, [&](auto t, auto w) {
       constexpr int T = decltype(t)::value, W = decltype(w)::value;
       with_layout<T, W>(l, [&](auto e, auto k, auto waves) {
         constexpr int E = decltype(e)::value, K = decltype(k)::value, N = decltype(waves)::value;
-        COOP_LAUNCH(K_NORM_GRAD, (k_norm_grad<T, W, E, K, N>), dim3((unsigned)blocks), dim3(kNormBlock<N>), 0, s, (const char*)dy, (const char*)x,
+        const unsigned grid = (unsigned)blocks;
+        if constexpr (kSumsApart<E, K, N>)
+          if (sums) {  // (before dx, which may lie where dy does; no more splits than the workspace has rows for, some 2,048 blocks)
+            const int64_t tiles = (dim + kWave * E - 1) / (kWave * E), splits = 2048 / tiles + 1;
+            if (splits < blocks) blocks = splits;
+            COOP_LAUNCH(K_NORM_GRAD, (k_norm_sums<T, E>), dim3((unsigned)tiles, (unsigned)blocks), dim3(kBlock), 0, s, (const char*)dy, (const char*)x, sh,
+                        mean, rstd, part);
+          }
+        COOP_LAUNCH(K_NORM_GRAD, (k_norm_grad<T, W, E, K, N>), dim3(grid), dim3(kNormBlock<N>), 0, s, (const char*)dy, (const char*)x,
                     sh, mean, rstd, (const char*)weight, (char*)dx, part);
       });
     });
