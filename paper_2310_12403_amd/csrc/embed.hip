@@ -33,22 +33,15 @@ __global__ __launch_bounds__(kBlock) void k_embed(const char* __restrict__ table
   int32_t id[kUnroll];
   float s[kUnroll];
   int32_t col[kUnroll];
-  int64_t r[kUnroll];
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
     uint32_t item;
     row[u] = items.row_of((uint32_t)(u * kBlock) + threadIdx.x, rs, &item);
-    r[u] = row[u] < sh.n_ids ? row[u] : sh.n_ids - 1;
-    id[u] = ids[r[u]];
+    const int64_t r = row[u] < sh.n_ids ? row[u] : sh.n_ids - 1;
+    id[u] = ids[r];
+    s[u] = scale != nullptr ? scale[r] * alpha : alpha;
     const int64_t c = (int64_t)item * E, last = sh.dim - E;
     col[u] = (int32_t)(c < last ? c : last);
-  }
-  if (scale != nullptr) {  // (one branch for all of them: behind a branch each, each would be waited for by itself)
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) s[u] = scale[r[u]];
-  } else {
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) s[u] = 1.f;
   }
   In x[kUnroll];
   bool ok[kUnroll];
@@ -64,7 +57,7 @@ __global__ __launch_bounds__(kBlock) void k_embed(const char* __restrict__ table
     float f[E];
     x[u].get(f);
 #pragma unroll
-    for (int e = 0; e < E; ++e) f[e] = ok[u] ? f[e] * (s[u] * alpha) : 0.f;
+    for (int e = 0; e < E; ++e) f[e] = ok[u] ? f[e] * s[u] : 0.f;
     Out y;
     y.set(f);
     y.store_nt(out + (row[u] * sh.dim + col[u]) * (int64_t)sizeof(typename Out::M));
@@ -481,7 +474,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_sum(const uint32_t* __restrict
     uint32_t key[kAhead];
     In x[kAhead];
     float s[kAhead];
-    if (scale != nullptr) {  // (as in k_embed)
+    if (scale != nullptr) {  // (one branch for all of them: behind a branch each, each would be waited for by itself)
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) s[u] = scale[next_place[u]];
     } else {
