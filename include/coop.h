@@ -336,7 +336,7 @@ int coop_embed(const void* table, int64_t n_rows, int32_t dim, int dtype, const 
 
 /*
  * The table's gradient: grad[v, :] = sum over the places i with ids[i] = v of s_i dout[i, :], in the order of the places in
- * parts of up to 32 whose sums are added in their order; 0 for a row that no place has.  Places with `pad` and ids out of
+ * parts of up to 32, whose sums are added in an order that the ids alone decide; 0 for a row that no place has.  Places with `pad` and ids out of
  * range (reported) are left out.
  *   dout       device [n_ids, dim] of dtype, n_ids <= 2^30
  *   grad       device [n_rows, dim] of grad_dtype, all of it written

@@ -18,9 +18,9 @@
 // Rates (2 n vocab dim for a product; a library product of 8192^3 reaches 1,382 TFLOP/s in bf16 and 153 in fp32):
 //   8,192 x 232,965 x 128 bf16, narrow: statistics 525 us, 930 TFLOP/s (the matrix units at work 46% of the time; the exponentials and the
 //     maximum beside them); dH, two products, 807 us, 1,210 (61%); dW 921 us, 1,060 (55%; 64 more factors a lane and stage, coef of the rows).
-//   8,192 x 131,072 x 1,024 bf16: statistics 2,059 us, 1,070 (49%); G 2,427 us, 906, the 2.1 GB that it writes among it; dH 1,861, 1,180;
+//   8,192 x 131,072 x 1,024 bf16: statistics 2,059 us, 1,070 (51%); G 2,427 us, 906 (45%), the 2.1 GB that it writes among it; dH 1,861, 1,180;
 //     dW 1,734, 1,270.  A wave has its SIMD to itself (its sums are half of all registers): what follows a tile's products is not hidden.
-//   1,021 x 50,021 x 100 fp32: 125 to 150 us each, 70 to 82 TFLOP/s: the units at work 80 to 90% of the time, on rows taken as 128 elements.
+//   1,021 x 50,021 x 100 fp32: 100 to 150 us each, 68 to 100 TFLOP/s: the units at work 80 to 88% of the time (G 67%), on rows taken as 128 elements.
 //   24 x 232,965 x 128 bf16: 13 us, W's 60 MB at 4.5 TB/s.
 #include <type_traits>
 
