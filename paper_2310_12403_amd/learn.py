@@ -268,17 +268,19 @@ class AdamW:
         assert all(0 <= i < len(self.params) for i in rows)
         for i, g in enumerate(self.grads):
             assert g is not None or i in rows, "parameter %d has no gradient" % i
-        for i, (ids, g, count) in rows.items():
-            n_rows, dim = self.shapes[i]
+        listed = []
+        for i, (ids, g, count) in rows.items():  # (all of them are looked at before the plan is changed for the call)
             assert self.by_rows[i] or self.bits == 32 and self.params[i].dim() == 2
             n_rows, dim = self.params[i].shape
-            _matrix(g, "row gradients", ids.numel(), dim)
-            c = self._c[i]
-            c.n_rows, c.dim, c.grad, c.grad_dtype = n_rows, dim, g.data_ptr(), _DTYPES[g.dtype]
-            c.rows, c.n_list = _vector(ids, ids.numel(), torch.int32, "rows") or 1, ids.numel()  # (an empty list has no address)
-            c.n_list_dev = None if count is None else _vector(count, 1, torch.int32, "count")
+            listed.append((self._c[i], dict(
+                n_rows=n_rows, dim=dim, grad=_matrix(g, "row gradients", ids.numel(), dim), grad_dtype=_DTYPES[g.dtype],
+                rows=_vector(ids, ids.numel(), torch.int32, "rows") or 1, n_list=ids.numel(),  # (an empty list has no address)
+                n_list_dev=None if count is None else _vector(count, 1, torch.int32, "count"))))
         gs = None if grad_scale is None else _vector(grad_scale, 1, torch.float32, "grad_scale")
         try:
+            for c, fields in listed:
+                for name, value in fields.items():
+                    setattr(c, name, value)
             _check(lib().coop_adamw(self._c, len(self.params), self.bits, lr, beta1, beta2, eps, weight_decay, step, seed, gs, _stream_ptr(stream)))
         finally:
             for i in rows:

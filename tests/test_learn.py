@@ -6,6 +6,7 @@ the last place of the type that a result is stored in (for fp16 also of its smal
 import ctypes as C
 import importlib.util
 import os
+import types
 
 import numpy as np
 import pytest
@@ -843,3 +844,37 @@ def test_refusals_of_the_binding():
     assert e.value.code == -4
     with pytest.raises(P.CoopError):
         P.AdamW([x], [x.clone()]).step(0, 1e-3)
+
+
+class OnDevice:
+    """A tensor of the host that says it is the device's: what a refusal leaves behind can be looked at without a GPU."""
+
+    def __init__(self, t):
+        self.t, self.is_cuda = t, True
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+def host_adamw(params, bits=32, **kw):
+    n = [p.numel() for p in params]
+    state = {"m": [OnDevice(torch.zeros(k)) for k in n], "v": [OnDevice(torch.zeros(k)) for k in n]}
+    return P.AdamW([OnDevice(p) for p in params], bits=bits, state=state, **kw)
+
+
+def test_a_refused_step_leaves_the_plan_as_it_was():
+    """Whatever is wrong with a step's rows, the next step's tensors, addresses and sizes are those of before."""
+    x, y = torch.zeros((8, 6)), torch.zeros((5, 4))
+    opt = host_adamw([x, y], grads=[OnDevice(torch.zeros((8, 6))), OnDevice(torch.zeros((5, 4)))], by_rows=True)
+    before = bytes(opt._c)
+    ids, g = OnDevice(torch.zeros(2, dtype=torch.int32)), OnDevice(torch.zeros((2, 6)))
+    g4, count = OnDevice(torch.zeros((2, 4))), OnDevice(torch.zeros(1, dtype=torch.int32))
+    wide = OnDevice(torch.zeros(2, dtype=torch.int64))
+    for rows, kw in (({0: (wide, g, None)}, {}), ({0: (ids, g4, None)}, {}), ({0: (ids, g, wide)}, {}), ({0: (ids, g, count), 1: (ids, g, None)}, {}),
+                     ({0: (ids, g, count), 1: (wide, g4, None)}, {}), ({0: (ids, g, None)}, {"grad_scale": wide}), ({0: (ids, g, None)}, {"grad_scale": ids})):
+        with pytest.raises(AssertionError):
+            opt.step(1, 1e-3, rows=rows, **kw)
+        assert bytes(opt._c) == before
+    with pytest.raises(P.CoopError):         # (by the library, before it launches anything)
+        opt.step(0, 1e-3, rows={0: (ids, g, count), 1: (ids, g4, None)}, stream=types.SimpleNamespace(cuda_stream=None))
+    assert bytes(opt._c) == before
