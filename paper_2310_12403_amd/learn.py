@@ -253,12 +253,13 @@ class AdamW:
         self.set_grads([None] * n if grads is None else grads)
 
     def set_grads(self, grads):
-        self.grads = list(grads)
-        assert len(self.grads) == len(self.params)
-        for c, p, g in zip(self._c, self.params, self.grads):
-            if g is not None:
-                assert g.is_cuda and g.is_contiguous() and g.numel() == p.numel() and g.dtype in _DTYPES
-                c.grad, c.grad_dtype = g.data_ptr(), _DTYPES[g.dtype]
+        grads = list(grads)
+        assert len(grads) == len(self.params)
+        for p, g in zip(self.params, grads):
+            assert g is None or g.is_cuda and g.is_contiguous() and g.numel() == p.numel() and g.dtype in _DTYPES
+        self.grads = grads  # (none is taken before all are looked at: the ones in the plan are those that are kept)
+        for c, g in zip(self._c, grads):
+            c.grad, c.grad_dtype = (None, 0) if g is None else (g.data_ptr(), _DTYPES[g.dtype])
 
     def step(self, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, rows=None, seed=0, grad_scale=None, stream=None):
         """One step; `step` counts from 1.  rows: {parameter's place in the list: (rows, gradients, count or None)}, as

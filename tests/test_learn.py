@@ -878,3 +878,17 @@ def test_a_refused_step_leaves_the_plan_as_it_was():
     with pytest.raises(P.CoopError):         # (by the library, before it launches anything)
         opt.step(0, 1e-3, rows={0: (ids, g, count), 1: (ids, g4, None)}, stream=types.SimpleNamespace(cuda_stream=None))
     assert bytes(opt._c) == before
+
+
+def test_refused_gradients_leave_the_ones_that_are_kept():
+    """set_grads takes all of its gradients or none: the plan's addresses are those of the tensors that the optimizer keeps."""
+    x, y = torch.zeros((8, 6)), torch.zeros((5, 4))
+    kept = [OnDevice(torch.zeros((8, 6))), OnDevice(torch.zeros((5, 4)))]
+    opt = host_adamw([x, y], grads=kept)
+    before = bytes(opt._c)
+    for bad in (torch.zeros((5, 5)), torch.zeros((5, 4), dtype=torch.float64), torch.zeros((4, 5)).t()):
+        with pytest.raises(AssertionError):
+            opt.set_grads([OnDevice(torch.zeros((8, 6))), OnDevice(bad)])
+        assert bytes(opt._c) == before and all(a is b for a, b in zip(opt.grads, kept))
+    opt.set_grads([None, kept[1]])
+    assert opt._c[0].grad is None and opt._c[1].grad == kept[1].data_ptr()
