@@ -216,7 +216,10 @@ class AdamW:
     rows are given to step.  by_rows (one for all, or one for each parameter): 8-bit moments are scaled within the rows of a
     2-d parameter, which is what lets a step touch some rows only; else the parameter is one row.  copies: tensors that get
     the new parameters as well, rounded to their type.  state: lists "m", "v" (and "m_scale", "v_scale") of existing moments;
-    otherwise they begin at zero."""
+    otherwise they begin at zero.
+
+    Every step works on the memory that parameters, copies and moments have when the optimizer is made: new values go there
+    by copy_; a tensor put in the place of one of them (p.data = ..., state["m"][0] = ...) is not seen."""
 
     def __init__(self, params, grads=None, bits=32, by_rows=False, copies=None, state=None):
         assert bits in (8, 32)
@@ -250,10 +253,12 @@ class AdamW:
             if copy is not None:
                 assert copy.is_cuda and copy.is_contiguous() and copy.numel() == k and copy.dtype in _DTYPES
                 c.copy, c.copy_dtype = copy.data_ptr(), _DTYPES[copy.dtype]
+        # (what the plan's addresses point to stays, whatever becomes of the tensors)
+        self._memory = [t.untyped_storage() for ts in (self.params, self.copies, *self.state.values()) for t in ts if t is not None]
         self.set_grads([None] * n if grads is None else grads)
 
     def set_grads(self, grads):
-        grads = list(grads)
+        grads = tuple(grads)
         assert len(grads) == len(self.params)
         for p, g in zip(self.params, grads):
             assert g is None or g.is_cuda and g.is_contiguous() and g.numel() == p.numel() and g.dtype in _DTYPES

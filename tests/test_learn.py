@@ -4,9 +4,11 @@ targets where they can go wrong; gradients against the formulas and against diff
 Tolerances are bounds, elementwise: u = 2^-24 for an operation in 32 bits, the sums' worst order included, and half a unit in
 the last place of the type that a result is stored in (for fp16 also of its smallest numbers)."""
 import ctypes as C
+import gc
 import importlib.util
 import os
 import types
+import weakref
 
 import numpy as np
 import pytest
@@ -892,3 +894,21 @@ def test_refused_gradients_leave_the_ones_that_are_kept():
         assert bytes(opt._c) == before and all(a is b for a, b in zip(opt.grads, kept))
     opt.set_grads([None, kept[1]])
     assert opt._c[0].grad is None and opt._c[1].grad == kept[1].data_ptr()
+
+
+def test_the_memory_that_the_plan_points_to_stays():
+    """... when a parameter gets other memory (as .data = does) and the moments are replaced in their lists."""
+    class Memory(np.ndarray):
+        pass
+    arrays = [np.zeros((8, 6), dtype=np.float32).view(Memory) for _ in range(4)]
+    p, copy, m, v = (OnDevice(torch.from_numpy(a)) for a in arrays)
+    opt = P.AdamW([p], copies=[copy], state={"m": [m], "v": [v]})
+    alive = [weakref.ref(a) for a in arrays]
+    p.t.data = torch.zeros((8, 6))
+    opt.state["m"][0] = opt.state["v"][0] = opt.copies[0] = None
+    del arrays, p, copy, m, v
+    gc.collect()
+    assert all(a() is not None for a in alive)
+    del opt
+    gc.collect()
+    assert not any(a() is not None for a in alive)
