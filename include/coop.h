@@ -434,7 +434,9 @@ typedef struct {
 /*   tensors     host, read before the call returns
  *   step        1 for the first one
  *   grad_scale  device float, or NULL
- * A tensor or list has at most 2^35 elements. */
+ * A tensor, or the list of its rows, has at most 2^27 blocks of 256 neighbouring elements of a row, what is left of a row being a
+ * block as well: 2^35 elements in rows of a multiple of 256.  Rows of up to 128, 64 or 32 elements are a half, a quarter or an
+ * eighth of a block. */
 int coop_adamw(const coop_adamw_tensor* tensors, int n, int bits, double lr, double beta1, double beta2, double eps, double weight_decay,
                int64_t step, uint64_t seed, const float* grad_scale, void* stream);
 

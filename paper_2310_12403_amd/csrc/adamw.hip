@@ -31,6 +31,13 @@ constexpr int kMomentBlock = 256;  // elements that share a scale: 4 neighbourin
 constexpr int kPerLane = 4;
 constexpr int kBlocksPerWave = 4;
 constexpr int kBlocksPerGroup = kWavesPerBlock * kBlocksPerWave;
+constexpr int64_t kMostGroups = (int64_t)1 << 23;  // of a tensor: with those in front of it in its launch fewer than 2^32 threads
+
+int lanes_log2_of(int64_t dim) { return dim <= 32 ? 3 : dim <= 64 ? 4 : dim <= 128 ? 5 : 6; }
+int64_t groups_of(int64_t blocks, int lanes_log2) {
+  const int64_t per_group = (int64_t)kBlocksPerGroup << (6 - lanes_log2);
+  return (blocks + per_group - 1) / per_group;
+}
 
 // What every tensor needs, and what only 8-bit moments or listed rows do.
 struct Whole {
@@ -277,7 +284,7 @@ void launch_steps(const coop_adamw_tensor* tensors, int n, const Hyper& h, int64
     d.row_blocks = (uint32_t)((t.dim - 1) / kMomentBlock + 1);
     d.n_blocks = (uint32_t)(rows * d.row_blocks);
     d.first_group = groups;
-    d.lanes_log2 = t.dim <= 32 ? 3 : t.dim <= 64 ? 4 : t.dim <= 128 ? 5 : 6;
+    d.lanes_log2 = (uint8_t)lanes_log2_of(t.dim);
     d.param_type = (int8_t)t.param_dtype, d.grad_type = (int8_t)t.grad_dtype, d.copy_type = (int8_t)t.copy_dtype;
     if constexpr (std::is_same<Tensor, Listed>::value) {
       d.m_scale = t.m_scale, d.v_scale = t.v_scale, d.rows = t.rows, d.n_active = t.n_list_dev, d.n_rows = t.n_rows;
@@ -285,9 +292,8 @@ void launch_steps(const coop_adamw_tensor* tensors, int n, const Hyper& h, int64
       const uint32_t key[2] = {(uint32_t)seed, (uint32_t)(seed >> 32)};
       philox4x32_10(ctr, key, d.key);
     }
-    const uint32_t per_group = kBlocksPerGroup << (6 - d.lanes_log2);
-    groups += (d.n_blocks + per_group - 1) / per_group;
-    if (++st.n == Step<Tensor>::kTensors || groups >= (1u << 22)) flush();
+    groups += (uint32_t)groups_of(d.n_blocks, d.lanes_log2);
+    if (++st.n == Step<Tensor>::kTensors || groups >= kMostGroups / 2) flush();
   }
   flush();
 }
@@ -312,8 +318,7 @@ extern "C" int coop_adamw(const coop_adamw_tensor* tensors, int n, int bits, dou
     if (rows == 0 || t.dim == 0) continue;
     if (t.dim > INT64_MAX / 8 / (t.n_rows > 0 ? t.n_rows : 1)) return COOP_E_ARG;
     const int64_t row_blocks = (t.dim - 1) / kMomentBlock + 1;
-    // (a launch has fewer than 2^32 threads, a quarter of them for all blocks of a wave)
-    if (row_blocks >= ((int64_t)1 << 27) || rows * row_blocks > ((int64_t)1 << 27)) return COOP_E_ARG;
+    if (row_blocks > ((int64_t)1 << 27) || groups_of(rows * row_blocks, lanes_log2_of(t.dim)) > kMostGroups) return COOP_E_ARG;
     if (!t.param || !t.grad || !t.m || !t.v || (bits == 8 && (!t.m_scale || !t.v_scale))) return COOP_E_NULL;
     if (!aligned_for(t.param, t.param_dtype) || !aligned_for(t.grad, t.grad_dtype) || (t.copy && !aligned_for(t.copy, t.copy_dtype))) return COOP_E_ARG;
     if ((bits == 32 && (((uintptr_t)t.m | (uintptr_t)t.v) & 3) != 0) || (((uintptr_t)t.m_scale | (uintptr_t)t.v_scale) & 3) != 0) return COOP_E_ARG;

@@ -912,3 +912,49 @@ def test_the_memory_that_the_plan_points_to_stays():
     del opt
     gc.collect()
     assert not any(a() is not None for a in alive)
+
+
+def test_adamw_most_rows():
+    """A tensor has at most 2^27 blocks of 256 elements of a row, short rows being less than one.  (A second tensor without addresses:
+    what is let through is refused as well, by another name, and nothing is launched.)"""
+    L, A = learn.lib(), 0x1000
+    t = (learn._CAdamWTensor * 2)()
+    t[1].n_rows, t[1].dim = 1, 1
+    for x in ("param", "grad", "m", "v", "m_scale", "v_scale"):
+        setattr(t[0], x, A)
+    for bits in (8, 32):
+        for dim, most in ((1, 1 << 30), (32, 1 << 30), (33, 1 << 29), (64, 1 << 29), (65, 1 << 28), (128, 1 << 28), (129, 1 << 27), (256, 1 << 27),
+                          (257, 1 << 26), (100000, (1 << 27) // 391), (1 << 35, 1)):
+            for rows, code in ((most, -1), (most + 1, -4)):
+                for listed in (None, A):
+                    t[0].dim, t[0].n_rows, t[0].n_list, t[0].rows = dim, (1 << 31) - 1 if listed and dim < 1 << 20 else rows, rows if listed else 0, listed
+                    assert L.coop_adamw(t, 2, bits, 1e-3, 0.9, 0.99, 1e-8, 0.0, 1, 0, None, None) == code, (dim, rows, listed)
+    t[0].rows, t[0].n_list, t[0].n_rows, t[0].dim = None, 0, 1, (1 << 35) + 1
+    assert L.coop_adamw(t, 2, 32, 1e-3, 0.9, 0.99, 1e-8, 0.0, 1, 0, None, None) == -4
+
+
+@gpu
+@pytest.mark.parametrize("bits", [8, 32])
+def test_adamw_more_short_rows_than_whole_blocks(bits):
+    """More than 2^27 rows, eight to a wave: those at either end and around 2^27 change as they would alone."""
+    torch.cuda.empty_cache()
+    n, dim = 2 ** 27 + 2 ** 20 + 5, 8
+    spots = [slice(0, 300), slice(2 ** 27 - 150, 2 ** 27 + 150), slice(n - 300, n)]
+    g = rng(23)
+    p, grad = torch.ones((n, dim), dtype=torch.bfloat16, device="cuda"), torch.zeros((n, dim), dtype=torch.bfloat16, device="cuda")
+    for s in spots:
+        grad[s] = normal(g, s.stop - s.start, dim, dtype=torch.bfloat16)
+    opt = P.AdamW([p], [grad], bits=bits, by_rows=True)
+    opt.step(1, **HYPER)
+    for s in spots:
+        want, m, v, move = plain_adamw(torch.ones((s.stop - s.start, dim), dtype=torch.float64, device="cuda"), grad[s].double(), 0.0, 0.0, 1, **HYPER)
+        within(p[s], want, 64 * U + want.abs() * HALF[torch.bfloat16])
+        got = opt.state["m"][0].view(n, dim)[s].float()
+        if bits == 32:
+            within(got, m, 8 * U * m.abs())
+        else:
+            scale = opt.state["m_scale"][0][s].double()
+            within(scale, m.abs().amax(1) / 448, 16 * U * m.abs().amax(1) / 448)
+            within(got * scale[:, None], m, m.abs() * 2.0 ** -3 * 1.01 + scale[:, None] * 2.0 ** -9 * 1.01)
+    still = torch.cat([p[300:2 ** 20], p[2 ** 27 + 150:2 ** 27 + 2 ** 20 - 300]])
+    assert bool((still == still[0, 0]).all()) and not bool(opt.state["m"][0].view(torch.uint8).view(n, -1)[300:2 ** 20].any())
