@@ -60,6 +60,7 @@ enum KernelId {
   K_XENT_LOSS,       // ... joined, the loss
   K_XENT_TERMS,      // ... gradient: what a row's part of it needs
   K_XENT_G,          // ... the logits' gradient for a piece of the vocabulary
+  K_XENT_LOWER,      // ... in fp16: rows that were lifted for the next product, as they are for the one behind it
   K_XENT_DH,         // ... its product with the weight
   K_XENT_DW,         // ... its product with the hidden states
   K_XENT_OUT,        // ... sums of a product's parts, rounded

@@ -27,7 +27,7 @@ const char* const kKernelNames[K_COUNT_] = {
     "unique_insert", "unique_flag", "unique_filter", "unique_collect", "unique_relabel", "unique_part_count", "unique_part_scatter", "unique_part_first", "copy_ids", "gather", "gather_mean", "owner_count", "owner_scatter", "validate_csr",
     "cache_lookup", "cache_select", "cache_evict", "cache_miss_rows", "cache_hit_rows",
     "embed", "sort_count", "sort_place", "embed_heads", "embed_sum", "embed_spans", "embed_join", "layer_norm", "layer_norm_grad", "layer_norm_join", "adamw",
-    "xent_pad", "xent_stats", "xent_loss", "xent_terms", "xent_g", "xent_dh", "xent_dw", "xent_out"};
+    "xent_pad", "xent_stats", "xent_loss", "xent_terms", "xent_g", "xent_lower", "xent_dh", "xent_dw", "xent_out"};
 
 hipEvent_t take_event() {
   if (!g_prof.pool.empty()) { hipEvent_t e = g_prof.pool.back(); g_prof.pool.pop_back(); return e; }

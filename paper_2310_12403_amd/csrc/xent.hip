@@ -179,12 +179,18 @@ __global__ __launch_bounds__(kBlock) void k_xent_loss(const RowStat* __restrict_
 
 // ---- backward ------------------------------------------------------------------------------------------------------------
 // What the rows of G need, all of them filled up to a multiple of a tile; target -1: the row has none, coef is 0, and its hidden state is
-// taken as zeros whatever it holds.
-struct RowTerms { float *coef, *lse2; int32_t* target; };
+// taken as zeros whatever it holds.  undo (null: 1): what the row's coef is to be multiplied by, a power of two.
+struct RowTerms { float *coef, *lse2; int32_t* target; float* undo; };
 
 // In 16 bits G holds coef over the largest |coef| (and times 2^13 in fp16, whose exponents would otherwise not reach from 1 to a
 // probability times dloss): where all rows count alike, as in a mean, the factor is 1 (a power of two), and so a target's p - 1 of a
 // small p is not rounded away from -1 twice; with dloss itself in G, dH and dW of the mean were off by 3.0e-3 instead of 2.0e-3 (bf16).
+// G in memory in fp16: a coef below 2^-10 of the largest is lifted above that by a power of two, or its row's probabilities would be lost
+// below fp16's least numbers (131,072 vertices, 136 elements, rows of 1e-6 of the largest dloss: their dH off by 4e-3 to 5e-3, of 1e-7 by
+// 4e-2; lifted by 3e-4 to 5e-4, as the other rows').  dH's row gets the power back when it is rounded; G's own ahead of the product for dW,
+// whose sums over the rows have one scale: a launch of 2 us where no row was lifted, 70 of 1,040 us where half of them were (4,096 rows,
+// 50,257 vertices, 768 elements).
+constexpr int kLeast = 10;
 template <int T>
 constexpr float kLift = T == COOP_F16 ? 13.f : 0.f;
 template <int T>
@@ -237,12 +243,20 @@ __global__ __launch_bounds__(1024) void k_xent_terms(const int32_t* __restrict__
   if (blockIdx.x == 0 && threadIdx.x == 0) *unlift = LIFT ? top / most : 1.f;
   const int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x;
   if (i >= rows) return;
-  float coef = 0.f, lse2 = 0.f;
+  float coef = 0.f, lse2 = 0.f, undo = 1.f;
   int32_t target = -1;
   if (i < n) {
     const int32_t t = targets[i];
     if (t != ignore && (uint64_t)(int64_t)t < (uint64_t)vocab) {
-      coef = LIFT ? alpha * dloss[i] / top * most : alpha * dloss[i];
+      const float part = LIFT ? alpha * dloss[i] / top : alpha * dloss[i];
+      coef = LIFT ? part * most : part;
+      if (term.undo != nullptr) {
+        const int below = 127 - (int)(__float_as_uint(part) >> 23 & 0xFFu) - kLeast;  // (at most 117; a NaN's or an infinity's is negative)
+        if (below > 0 && part != 0.f) {
+          undo = __uint_as_float((uint32_t)(127 - below) << 23);
+          coef *= __uint_as_float((uint32_t)(127 + below) << 23);
+        }
+      }
       lse2 = lse[i] * kLog2e;
       target = t;
     } else if (t != ignore) {
@@ -252,6 +266,7 @@ __global__ __launch_bounds__(1024) void k_xent_terms(const int32_t* __restrict__
   term.coef[i] = coef;
   term.lse2[i] = lse2;
   term.target[i] = target;
+  if (term.undo != nullptr) term.undo[i] = undo;
 }
 
 template <int T>
@@ -326,6 +341,25 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
   }
 }
 
+// The powers of two that G's rows (fp16) were lifted by taken back: 64 rows a block, most of which have none, blockIdx.y for parts of their
+// columns.
+__global__ __launch_bounds__(kBlock) void k_xent_lower(const float* __restrict__ undo, int64_t n, int64_t bytes, int64_t ld, char* __restrict__ g) {
+  const int64_t row0 = (int64_t)blockIdx.x * kWave;
+  const float mine = row0 + lane_id() < n ? undo[row0 + lane_id()] : 1.f;
+  for (uint64_t left = ballot64(mine != 1.f); left != 0; left &= left - 1) {
+    const int r = __builtin_ctzll(left);
+    const float u = __shfl(mine, r, kWave);
+    for (int64_t at = ((int64_t)blockIdx.y * kBlock + threadIdx.x) * 16; at < bytes; at += (int64_t)gridDim.y * (kBlock * 16)) {
+      char* p = g + (row0 + r) * ld + at;
+      float f[8];
+      load_elements<COOP_F16, 8>(p, f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] *= u;
+      store_elements<COOP_F16, 8>(p, f);
+    }
+  }
+}
+
 // dH: sums[split][row][dim] (+)= the split's part of G W over the piece
 template <int T, int WA, int WB, int TA, int TB>
 __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1))) void k_xent_dh(Operand wt, Operand g, int64_t k, int splits, uint32_t tiles_a, uint32_t tiles_b,
@@ -372,12 +406,13 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
       }
 }
 
-// out[row, :] = the splits' sums of the row, times *unlift.  A wave has 64 packs of four columns; where there are many splits the block's
+// out[row, :] = the splits' sums of the row, times *unlift and (not null) undo[row].  A wave has 64 packs of four columns; where there are many splits the block's
 // waves deal those of the same packs among themselves (`share` of them), and the first adds up what they have, in their order.
 constexpr int kOutWaves = 8;
 template <int T>
 __global__ __launch_bounds__(kOutWaves* kWave) void k_xent_out(const float* __restrict__ sums, int splits, int share, int64_t rows, int32_t width,
-                                                               int64_t n, int32_t dim, const float* __restrict__ unlift, char* __restrict__ out) {
+                                                               int64_t n, int32_t dim, const float* __restrict__ unlift, const float* __restrict__ undo,
+                                                               char* __restrict__ out) {
   __shared__ float lds[4][kOutWaves][kWave];
   const int32_t packs = (dim + 3) / 4;
   const float u = *unlift;
@@ -408,6 +443,11 @@ __global__ __launch_bounds__(kOutWaves* kWave) void k_xent_out(const float* __re
       for (int e = 0; e < 4; ++e) s[e] += lds[e][wave + w][lane];
 #pragma unroll
     for (int e = 0; e < 4; ++e) s[e] *= u;
+    if (undo != nullptr) {
+      const float back = undo[row];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] *= back;
+    }
     put_columns<T>(out, row, c, dim, s);
   }
 }
@@ -951,8 +991,8 @@ struct XentPlan {
   int64_t rows, piece, vocab_rows, dw_rows;
   int64_t g_ld;  // bytes from row to row of G: not a power of two, or a tile's rows would all lie in the same few channels of memory
   int splits, dh_splits, dw_splits, tile;
-  bool few, narrow, pad;
-  size_t h, w, part, coef, lse2, target, unlift, tops, g, sums, dw_sums, bytes;
+  bool few, narrow, pad, lift;  // lift: G is in memory, in fp16
+  size_t h, w, part, coef, lse2, target, undo, unlift, tops, g, sums, dw_sums, bytes;
   static int at_most(int64_t x, int64_t most) { return (int)(x < 1 ? 1 : x < most ? x : most); }
   XentPlan(int64_t n_, int64_t vocab_, int32_t dim, int dtype, bool aligned, bool grad) : n(n_), vocab(vocab_) {
     const int es = element_bytes(dtype);
@@ -961,6 +1001,7 @@ struct XentPlan {
     pad = !aligned || width != dim;
     narrow = es == 2 && width <= (grad ? 128 : 256) && (grad || n > 32);
     few = n <= 32 && !narrow;
+    lift = grad && dtype == COOP_F16 && !narrow;
     tile = narrow || (es == 2 || few) && ((n + 255) / 256) * ((vocab + 255) / 256) >= 256 ? 256 : 128;
     rows = few ? 32 : round_up(n, tile);
     const int blocks = 256 * (narrow || few || tile == 128 ? 2 : 1);
@@ -988,6 +1029,7 @@ struct XentPlan {
     coef = take(grad ? (size_t)rows * 4 : 0);
     lse2 = take(grad ? (size_t)rows * 4 : 0);
     target = take(grad ? (size_t)rows * 4 : 0);
+    undo = take(lift ? (size_t)rows * 4 : 0);
     unlift = take(grad ? sizeof(float) : 0);
     tops = take(grad ? 256 * sizeof(float) : 0);
     g_ld = piece * es + 256;
@@ -1084,11 +1126,12 @@ int forward(const XentPlan& p, const void* hidden, const void* weight, int32_t d
 }
 
 template <int T>
-void write_out(const float* sums, int splits, int64_t rows, const XentPlan& p, int64_t n, int32_t dim, const float* unlift, void* out, hipStream_t s) {
+void write_out(const float* sums, int splits, int64_t rows, const XentPlan& p, int64_t n, int32_t dim, const float* unlift, const float* undo, void* out,
+               hipStream_t s) {
   const int share = splits >= kOutWaves ? kOutWaves : 1, each = kOutWaves / share * kWave;
   const int64_t blocks = (n * ((dim + 3) / 4) + each - 1) / each;
   COOP_LAUNCH(K_XENT_OUT, k_xent_out<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(kOutWaves * kWave), 0, s, sums, splits, share, rows, (int32_t)p.width, n, dim,
-              unlift, (char*)out);
+              unlift, undo, (char*)out);
 }
 
 template <int T>
@@ -1104,13 +1147,13 @@ bool backward_narrow(const XentPlan& p, const Operand& w, const Operand& h, int3
     if (dhidden != nullptr) {
       COOP_LAUNCH(K_XENT_DH, kh, dim3((unsigned)(p.rows / p.tile * p.dh_splits)), dim3(256), lds_h, s, w, h, p.rows, p.vocab, alpha * kLog2e, term,
                   p.dh_splits, sums, (int32_t)p.width);
-      write_out<T>(sums, p.dh_splits, p.rows, p, p.n, dim, unlift, dhidden, s);
+      write_out<T>(sums, p.dh_splits, p.rows, p, p.n, dim, unlift, nullptr, dhidden, s);
     }
     if (dweight != nullptr) {
       float* parts = p.dw_splits > 1 ? dw_sums : nullptr;
       COOP_LAUNCH(K_XENT_DW, kw, dim3((unsigned)(p.vocab_rows / p.tile * p.dw_splits)), dim3(256), lds_w, s, w, h, p.vocab, alpha * kLog2e, term, p.dw_splits,
                   unlift, dim, (char*)dweight, parts, p.dw_rows, (int32_t)p.width);
-      if (parts != nullptr) write_out<T>(parts, p.dw_splits, p.dw_rows, p, p.vocab, dim, unlift, dweight, s);
+      if (parts != nullptr) write_out<T>(parts, p.dw_splits, p.dw_rows, p, p.vocab, dim, unlift, nullptr, dweight, s);
     }
   });
   return ok;
@@ -1144,11 +1187,16 @@ bool backward_pieces(const XentPlan& p, const Operand& w, const Operand& h, int3
                   v != 0, sums, p.width);
     }
     if (dweight != nullptr) {
+      if (term.undo != nullptr) {
+        const int64_t groups = (p.n + kWave - 1) / kWave, most = (g_bytes + kBlock * 16 - 1) / (kBlock * 16);  // (some 1,024 blocks)
+        COOP_LAUNCH(K_XENT_LOWER, k_xent_lower, dim3((unsigned)groups, (unsigned)XentPlan::at_most(1024 / groups, most)), dim3(kBlock), 0, s,
+                    (const float*)term.undo, p.n, g_bytes, p.g_ld, g);
+      }
       const Operand ht{h.base, p.ld, p.ld, p.n}, gt{g, p.g_ld, g_bytes, p.rows};
       float* parts = p.dw_splits > 1 ? dw_sums : nullptr;
       COOP_LAUNCH(K_XENT_DW, kw, dim3(tiles_of(len, W::kRowsB) * w_tiles * p.dw_splits), dim3(W::kThreads), W::kLds, s, ht, gt, p.n, p.dw_splits, p.vocab,
                   v, dim, w_tiles, unlift, (char*)dweight, parts, p.dw_rows, p.width);
-      if (parts != nullptr) write_out<T>(parts, p.dw_splits, p.dw_rows, p, len, dim, unlift, (char*)dweight + v * dim * kElem<T>, s);
+      if (parts != nullptr) write_out<T>(parts, p.dw_splits, p.dw_rows, p, len, dim, unlift, nullptr, (char*)dweight + v * dim * kElem<T>, s);
     }
   }
   return true;
@@ -1157,7 +1205,7 @@ bool backward_pieces(const XentPlan& p, const Operand& w, const Operand& h, int3
 template <int T>
 int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t dim, const int32_t* targets, float alpha, int32_t ignore,
              const float* lse, const float* dloss, void* dhidden, void* dweight, char* ws, int32_t* bad, hipStream_t s) {
-  const RowTerms term{(float*)(ws + p.coef), (float*)(ws + p.lse2), (int32_t*)(ws + p.target)};
+  const RowTerms term{(float*)(ws + p.coef), (float*)(ws + p.lse2), (int32_t*)(ws + p.target), p.lift ? (float*)(ws + p.undo) : nullptr};
   float* unlift = (float*)(ws + p.unlift);
   float *sums = (float*)(ws + p.sums), *dw_sums = (float*)(ws + p.dw_sums);
   float* tops = (float*)(ws + p.tops);
@@ -1187,7 +1235,7 @@ int backward(const XentPlan& p, const void* hidden, const void* weight, int32_t 
   else if (p.tile == 128) pieces(Two(), Two(), Two(), Two());
   else if constexpr (T != COOP_F32) pieces(Two(), Two(), Four(), Four());
   if (!ok) return COOP_E_HIP;
-  if (dhidden != nullptr) write_out<T>(sums, p.dh_splits, p.rows, p, p.n, dim, unlift, dhidden, s);
+  if (dhidden != nullptr) write_out<T>(sums, p.dh_splits, p.rows, p, p.n, dim, unlift, term.undo, dhidden, s);
   return hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
 }
 

@@ -958,3 +958,46 @@ def test_adamw_more_short_rows_than_whole_blocks(bits):
             within(got * scale[:, None], m, m.abs() * 2.0 ** -3 * 1.01 + scale[:, None] * 2.0 ** -9 * 1.01)
     still = torch.cat([p[300:2 ** 20], p[2 ** 27 + 150:2 ** 27 + 2 ** 20 - 300]])
     assert bool((still == still[0, 0]).all()) and not bool(opt.state["m"][0].view(torch.uint8).view(n, -1)[300:2 ** 20].any())
+
+
+# rows that stay in registers; few rows; tiles of 128; tiles of 256; a vocabulary in three pieces
+@gpu
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,vocab,dim", [(24, 20000, 120), (300, 20000, 128), (24, 20000, 136), (300, 20000, 136), (4097, 4100, 200), (16384, 20000, 136)])
+def test_softmax_xent_grad_of_rows_that_count_little(dtype, n, vocab, dim):
+    """A row's gradient is as exact as its own dloss allows, however much larger another row's is: the bound is the row's own."""
+    g = rng(n + dim)
+    h, w = normal(g, n, dim, dtype=dtype), normal(g, vocab, dim, dtype=dtype, scale=2 * dim ** -0.5)
+    t = torch.randint(0, vocab, (n,), generator=g, device="cuda", dtype=torch.int32)
+    # dloss from 2^11 down to 2^-11 (what fp16 holds both gradients of), and a row of none
+    dloss = torch.exp2(11.0 - 22.0 * torch.rand(n, generator=g, device="cuda")) * torch.where(torch.rand(n, generator=g, device="cuda") < 0.5, -1.0, 1.0)
+    dloss[0], dloss[1] = 2.0 ** 11, 0.0
+    _, lse = P.coop_softmax_xent(h, w, t)
+    dh, dw = P.coop_softmax_xent_grad(h, w, t, lse, dloss)
+    z = h.double() @ w.double().t()
+    ez, _ = xent_bounds(h, w, z, lse.double(), 1.0)
+    c = dloss.double()
+    off = 4 * U * (lse.double().abs() + z.abs().amax(1)) + 4 * U
+    G = torch.exp(z.sub_(lse.double()[:, None]))
+    ep = G * (ez + off)[:, None]
+    G.scatter_add_(1, t.long()[:, None], torch.full((n, 1), -1.0, dtype=torch.float64, device="cuda"))
+    # G's rounding, relative to the row: 2^-25 of 2^13 times what the row's coefficient is lifted to, at least 2^-10 of the largest
+    eG = ep + (G.abs() + ep) * (HALF[dtype] + 4 * U) + (2.0 ** -28 if dtype == torch.float16 else 0.0)
+    W = w.double()
+    e = eG @ W.abs()
+    e += (vocab + 272) * U * (G.abs() @ W.abs() + e)
+    want = (G @ W) * c[:, None]
+    e *= c.abs()[:, None]
+    within(dh, want, e + (want.abs() + e) * HALF[dtype] + TINY[dtype])
+    # dW's sums over the rows have one scale: that of the largest coefficient
+    eG = eG * c.abs()[:, None]
+    if dtype == torch.float16:
+        eG = eG + 1.5 * c.abs().max() * 2.0 ** -38
+    G = G * c[:, None]
+    H = h.double()
+    want, e, size = G.t().contiguous() @ H, eG.t().contiguous() @ H.abs(), G.abs().t().contiguous() @ H.abs()
+    e += (n + 272) * U * (size + e)
+    within(dw, want, e + (want.abs() + e) * HALF[dtype] + TINY[dtype])
+    assert bool(torch.isfinite(dh).all()) and not dh[1].any()
+    assert torch.equal(P.coop_softmax_xent_grad(h, w, t, lse, dloss, want_weight=False)[0], dh)
+    assert torch.equal(P.coop_softmax_xent_grad(h, w, t, lse, dloss, want_hidden=False)[1], dw)
