@@ -1001,3 +1001,38 @@ def test_softmax_xent_grad_of_rows_that_count_little(dtype, n, vocab, dim):
     assert bool(torch.isfinite(dh).all()) and not dh[1].any()
     assert torch.equal(P.coop_softmax_xent_grad(h, w, t, lse, dloss, want_weight=False)[0], dh)
     assert torch.equal(P.coop_softmax_xent_grad(h, w, t, lse, dloss, want_hidden=False)[1], dw)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,dim", [(60, 72), (60, 136), (20, 136)])
+def test_softmax_xent_grad_along_the_gradient(dtype, n, dim):
+    """The loss' slope along the gradient's own direction, where it is the gradient's length: by differences in 64 bits, and by what came
+    back, whose errors are bounded element by element and together are less than a fiftieth of the slope."""
+    g = rng(dim + n)
+    vocab, step = 700, 1e-4
+    h, w = normal(g, n, dim, dtype=dtype), normal(g, vocab, dim, dtype=dtype, scale=0.2)
+    t = torch.randint(-1, vocab, (n,), generator=g, device="cuda", dtype=torch.int32)
+    dloss = torch.rand(n, generator=g, device="cuda") + 0.5
+    loss, lse = P.coop_softmax_xent(h, w, t)
+    grads = P.coop_softmax_xent_grad(h, w, t, lse, dloss)
+    _, want_lse, z = plain_xent(h, w, t, 1.0)
+    ez, el = xent_bounds(h, w, z, want_lse, 1.0)
+    H, W, c = h.double(), w.double(), torch.where(t >= 0, dloss.double(), 0.0)
+    p = torch.exp(z - want_lse[:, None])
+    G = p.scatter_add(1, t.long().clamp(min=0)[:, None], torch.full((n, 1), -1.0, dtype=torch.float64, device="cuda")) * c[:, None]
+    ep = p * ((ez + el + 4 * U * (want_lse.abs() + z.abs().amax(1)) + 4 * U) * c)[:, None]
+    eG = ep + (G.abs() + ep) * (HALF[dtype] + 4 * U) + (c.max() * 2.0 ** -38 if dtype == torch.float16 else 0.0)
+    for k, (want, e, size, terms) in enumerate(((G @ W, eG @ W.abs(), G.abs() @ W.abs(), vocab),
+                                                (G.t().contiguous() @ H, eG.t().contiguous() @ H.abs(), G.abs().t().contiguous() @ H.abs(), n))):
+        e = e + (terms + 272) * U * (size + e)
+        e = e + (want.abs() + e) * HALF[dtype] + TINY[dtype]
+        way = want / want.norm()
+        losses = []
+        for sign in (1, -1):
+            args = [H, W]
+            args[k] = args[k] + sign * step * way
+            losses.append((plain_xent(*args, t, 1.0)[0] * dloss.double()).sum())
+        slope, got, bound = (losses[0] - losses[1]) / (2 * step), (grads[k].double() * way).sum(), (e * way.abs()).sum()
+        assert float(slope) > 0 and float(bound) < float(slope) / 50
+        assert abs(float(got - slope)) <= float(bound) + 1e-6 * float(slope)       # (the differences: step^2 of the third derivative)
