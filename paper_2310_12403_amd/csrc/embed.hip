@@ -15,6 +15,9 @@ namespace {
 // 2,592,327 rows of 128 elements of fp16 out of 7.1 GB: 236 us, 1.35 GB at 5.7 TB/s; 24 rows of 100: 2.5 us, a wait for memory or two.
 constexpr int kUnroll = 4;
 
+// An id that has no row is reported unless it is the one that says so; COOP_NO_PAD says that there is none, and is no id itself.
+__device__ __forceinline__ bool wrong_id(int32_t id, int32_t pad) { return id != pad || pad == COOP_NO_PAD; }
+
 struct EmbedShape {
   int64_t n_rows, n_ids;
   int32_t dim, pad;
@@ -61,7 +64,7 @@ __global__ __launch_bounds__(kBlock) void k_embed(const char* __restrict__ table
     Out y;
     y.set(f);
     y.store_nt(out + (row[u] * sh.dim + col[u]) * (int64_t)sizeof(typename Out::M));
-    if (!ok[u] && id[u] != sh.pad && col[u] == 0) atomicOr(bad, 1);
+    if (!ok[u] && wrong_id(id[u], sh.pad) && col[u] == 0) atomicOr(bad, 1);
   }
 }
 
@@ -125,7 +128,7 @@ struct SortInput {  // the first pass reads the ids, the others the (key, place)
     if (ids == nullptr) return pairs[i];
     const int32_t id = ids[i];
     const bool row = id != pad && (uint64_t)(int64_t)id < (uint64_t)n_rows;
-    *wrong |= !row && id != pad;
+    *wrong |= !row && wrong_id(id, pad);
     return u32x2{row ? (uint32_t)id : (uint32_t)n_rows, (uint32_t)i};
   }
 };

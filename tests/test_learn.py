@@ -1036,3 +1036,18 @@ def test_softmax_xent_grad_along_the_gradient(dtype, n, dim):
         slope, got, bound = (losses[0] - losses[1]) / (2 * step), (grads[k].double() * way).sum(), (e * way.abs()).sum()
         assert float(slope) > 0 and float(bound) < float(slope) / 50
         assert abs(float(got - slope)) <= float(bound) + 1e-6 * float(slope)       # (the differences: step^2 of the third derivative)
+
+
+@gpu
+def test_the_least_id_is_reported_where_there_is_no_padding():
+    """COOP_NO_PAD is the least int32, which as an id is as wrong as any other negative one."""
+    least = torch.full((600,), -2 ** 31, dtype=torch.int32, device="cuda")
+    least[5] = 3
+    table, x = torch.ones((10, 8), device="cuda"), torch.ones((600, 8), device="cuda")
+    for ids in (least[4:6].contiguous(), least):                 # (the sort of few tokens, and of more)
+        for call in (lambda: P.coop_embed(table, ids), lambda: P.coop_embed_grad(x[:ids.numel()], ids, 10),
+                     lambda: P.coop_embed_grad_rows(x[:ids.numel()], ids, 10)[1]):
+            assert float(call().sum()) == 8 and status_is(-2) and status_is(0)
+        assert float(P.coop_embed(table, ids, pad=-1).sum()) == 8 and status_is(-2)
+    least[:5] = least[6:] = -1
+    assert float(P.coop_embed(table, least, pad=-1).sum()) == 8 and status_is(0)
