@@ -325,7 +325,7 @@ int coop_cache_vertices(const coop_cache* c, const int32_t** vertex_of_out, int6
 
 /*
  * Learned rows: out[i, :] = s_i table[ids[i], :] with s_i = alpha scale[i] (alpha where scale is NULL).
- *   table  device [n_rows, dim] of dtype; out device [n_ids, dim] of out_dtype
+ *   table  device [n_rows, dim] of dtype, n_rows >= 1 where there are ids; out device [n_ids, dim] of out_dtype
  *   ids    device int32 [n_ids]; the id `pad` (COOP_NO_PAD: none) stands for a place without a row: zeros.  Other ids
  *          outside [0, n_rows) give zeros and are reported
  *   scale  device float [n_ids], or NULL
@@ -338,7 +338,7 @@ int coop_embed(const void* table, int64_t n_rows, int32_t dim, int dtype, const 
  * The table's gradient: grad[v, :] = sum over the places i with ids[i] = v of s_i dout[i, :], in the order of the places in
  * parts of up to 32, whose sums are added in an order that the ids alone decide; 0 for a row that no place has.  Places with `pad` and ids out of
  * range (reported) are left out.
- *   dout       device [n_ids, dim] of dtype, n_ids <= 2^30
+ *   dout       device [n_ids, dim] of dtype, n_ids <= 2^30, dim <= 16776960
  *   grad       device [n_rows, dim] of grad_dtype, all of it written
  *   workspace  at least coop_embed_grad_workspace_bytes(n_ids, dim) bytes
  */

@@ -386,6 +386,7 @@ constexpr int kSpan2 = 1024;
 constexpr int kHeadTile = 4096;                      // tokens
 constexpr int kTileChunks = kHeadTile / kChunk;
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;     // of a gradient: its launches stay below 2^32 threads
+constexpr int32_t kMaxDim = 65535 * 4 * kWave;       // ... and have as many column tiles at most as a grid has rows
 
 struct ReduceShape {
   int64_t n_ids, n_chunks;
@@ -708,7 +709,7 @@ int grad_launch(const void* dout, int dtype, const int32_t* ids, int64_t n, cons
                 int32_t dim, void* grad, int grad_dtype, int32_t* rows_out, int32_t* count, bool rows_form, void* workspace, size_t ws_bytes,
                 hipStream_t s) {
   if (!known_dtype(dtype) || !known_dtype(grad_dtype)) return COOP_E_ARG;
-  if (n < 0 || n > kMaxTokens || n_rows < 0 || n_rows >= ((int64_t)1 << 31) || dim < 1) return COOP_E_ARG;
+  if (n < 0 || n > kMaxTokens || n_rows < 0 || n_rows >= ((int64_t)1 << 31) || dim < 1 || dim > kMaxDim) return COOP_E_ARG;
   if (rows_form && !count) return COOP_E_NULL;
   if (n > 0 && (!dout || !ids || !workspace)) return COOP_E_NULL;
   if ((rows_form ? (n < n_rows ? n : n_rows) : n_rows) > 0 && (!grad || (rows_form && !rows_out))) return COOP_E_NULL;
@@ -789,7 +790,7 @@ extern "C" int coop_embed(const void* table, int64_t n_rows, int32_t dim, int dt
       constexpr int TI = decltype(ti)::value, TO = decltype(to)::value, E = TI == COOP_F32 || TO == COOP_F32 ? 4 : 8;
       const auto go = [&](auto e) {
         constexpr int N = decltype(e)::value;
-        const uint32_t vecs = (uint32_t)((dim + N - 1) / N);
+        const uint32_t vecs = (uint32_t)(((int64_t)dim + N - 1) / N);
         constexpr int64_t per_block = kBlock * kUnroll;
         const int64_t most = kSliceBlocks * per_block / (int64_t)vecs;  // ids of a launch of fewer than 2^32 threads
         for (int64_t i = 0; i < n_ids; i += most) {
@@ -808,7 +809,7 @@ extern "C" int coop_embed(const void* table, int64_t n_rows, int32_t dim, int dt
 }
 
 extern "C" size_t coop_embed_grad_workspace_bytes(int64_t n_ids, int32_t dim) {
-  if (n_ids < 0 || n_ids > kMaxTokens || dim < 1) return 0;
+  if (n_ids < 0 || n_ids > kMaxTokens || dim < 1 || dim > kMaxDim) return 0;
   return GradPlan(n_ids, dim).bytes;
 }
 

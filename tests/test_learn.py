@@ -1051,3 +1051,28 @@ def test_the_least_id_is_reported_where_there_is_no_padding():
         assert float(P.coop_embed(table, ids, pad=-1).sum()) == 8 and status_is(-2)
     least[:5] = least[6:] = -1
     assert float(P.coop_embed(table, least, pad=-1).sum()) == 8 and status_is(0)
+
+
+def test_embed_grad_widest_rows_refused():
+    """As many column tiles as a grid has rows, and no more: refused before anything is launched.  (Without tokens: what is let through is
+    refused as well, by another name.)"""
+    L, A, most = learn.lib(), 0x1000, 16776960
+    assert L.coop_embed_grad_workspace_bytes(100, most) > 0 and L.coop_embed_grad_workspace_bytes(100, most + 1) == 0
+    for dim, code in ((most, -1), (most + 1, -4), (2 ** 31 - 1, -4)):
+        assert L.coop_embed_grad(None, 0, A, 100, None, 1.0, 0, 10, dim, A, 0, A, 1 << 40, None) == code
+        assert L.coop_embed_grad_rows(None, 0, A, 100, None, 1.0, 0, 10, dim, A, A, 0, A, A, 1 << 40, None) == code
+
+
+@gpu
+def test_embed_widest_rows():
+    torch.cuda.empty_cache()
+    dim, ids = 16776960, torch.tensor([2, 0, 2], dtype=torch.int32, device="cuda")
+    dout = torch.arange(dim, device="cuda").remainder(1000).float() * torch.tensor([[1.0], [2.0], [3.0]], device="cuda")
+    grad = P.coop_embed_grad(dout, ids, 3)
+    assert torch.equal(grad[0], dout[1]) and not grad[1].any() and torch.equal(grad[2], dout[0] * 4)
+    del dout, grad
+    dim = 2 ** 31 - 5                          # 4.3 GB, the last items' numbers close to 2^31
+    table = torch.zeros((1, dim), dtype=torch.float16, device="cuda")
+    table[0, ::1001] = 1.0
+    table[0, -1] = 2.0
+    assert torch.equal(P.coop_embed(table, torch.zeros(1, dtype=torch.int32, device="cuda")), table) and status_is(0)
