@@ -130,9 +130,10 @@ struct LaneWeights {
   }
 };
 
+// (y may be x: neither is told to be apart from the other.  A row is read whole before any of it is written.)
 template <int T, int W, int E, int K, int WAVES>
-__global__ __launch_bounds__(kNormBlock<WAVES>) void k_norm(const char* __restrict__ x, NormShape sh, const char* __restrict__ weight,
-                                                            const char* __restrict__ bias, char* __restrict__ y, float* __restrict__ mean_out,
+__global__ __launch_bounds__(kNormBlock<WAVES>) void k_norm(const char* x, NormShape sh, const char* __restrict__ weight,
+                                                            const char* __restrict__ bias, char* y, float* __restrict__ mean_out,
                                                             float* __restrict__ rstd_out) {
   __shared__ float lds[WAVES];
   const Rows<WAVES> rows(sh);
@@ -195,11 +196,11 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_norm(const char* __restri
 // a lane, and are a kernel's of their own.  (16,384 rows of 16,384 elements of bf16, 16 columns: 458 us, and 500 with the second kernel.)
 template <int E, int K, int WAVES> constexpr bool kSumsApart = WAVES == 16 && E * K >= 32;
 
-// part: [gridDim.x][2][dim], the block's sums of dy h and of dy (null: not asked for, or not here)
+// part: [gridDim.x][2][dim], the block's sums of dy h and of dy (null: not asked for, or not here).  (dx may be dy, as y may be x above.)
 template <int T, int W, int E, int K, int WAVES>
-__global__ __launch_bounds__(kNormBlock<WAVES>) void k_norm_grad(const char* __restrict__ dy, const char* __restrict__ x, NormShape sh,
+__global__ __launch_bounds__(kNormBlock<WAVES>) void k_norm_grad(const char* dy, const char* __restrict__ x, NormShape sh,
                                                                  const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
-                                                                 const char* __restrict__ weight, char* __restrict__ dx,
+                                                                 const char* __restrict__ weight, char* dx,
                                                                  float* __restrict__ part) {
   constexpr int kLds = WAVES == 1 ? kBlock * E : 2 * WAVES;
   __shared__ float lds[kLds];

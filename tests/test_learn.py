@@ -1076,3 +1076,17 @@ def test_embed_widest_rows():
     table[0, ::1001] = 1.0
     table[0, -1] = 2.0
     assert torch.equal(P.coop_embed(table, torch.zeros(1, dtype=torch.int32, device="cuda")), table) and status_is(0)
+
+
+@gpu
+@pytest.mark.parametrize("rows,dim", [(5000, 3), (3000, 75), (2500, 100), (2100, 602), (1100, 1500), (700, 8191), (300, 20001), (550, 32768)])
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_layer_norm_in_place(rows, dim, dtype):
+    """y in the place of x, dx in that of dy: the same bits, in every layout of a row, with more rows than groups that share them."""
+    g = rng(dim)
+    x, dy, w, b = normal(g, rows, dim, dtype=dtype), normal(g, rows, dim, dtype=dtype), 1 + normal(g, dim, scale=0.2), normal(g, dim)
+    y, mean, rstd = P.coop_layer_norm(x, w, b)
+    dx, dw, db = P.coop_layer_norm_grad(dy, x, mean, rstd, w)
+    got, dgot = unaligned(x), unaligned(dy)
+    assert all(torch.equal(s, t) for s, t in zip(P.coop_layer_norm(got, w, b, out=got), (y, mean, rstd)))
+    assert all(torch.equal(s, t) for s, t in zip(P.coop_layer_norm_grad(dgot, x, mean, rstd, w, out=dgot), (dx, dw, db)))
