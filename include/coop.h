@@ -396,10 +396,14 @@ int coop_softmax_xent(const void* hidden, int64_t n, const void* weight, int64_t
  * Its gradient, for dloss device float [n] and the forward call's lse: with
  * G_iv = alpha dloss_i (exp(z_iv - lse_i) - [v = targets[i]]), dhidden = G weight and dweight = transposed G hidden.  The
  * logits are computed again; G is held for a piece of the vocabulary at a time, as dtype (the products' operands have one
- * type; in 16 bits over the largest |alpha dloss_i|, and in fp16, for dhidden, rows of less than 2^-10 of that over a power of two of their
- * own: a row's gradient is as exact as others' however little it counts, while dweight's sums are exact to 2^-38 of the largest).
+ * type): in 16 bits it is rounded to them, over the largest |alpha dloss_i|, and in fp16, for dhidden, rows of less than 2^-10 of that
+ * over a power of two of their own, so that a row's gradient is as exact as others' however little it counts; a term of dweight's sums
+ * is then exact to 2^-38 of the largest.
  *   dhidden, dweight  device, of dtype, all of it written; either may be NULL
- *   workspace         at least coop_softmax_xent_workspace_bytes(n, vocab, dim, dtype, aligned, 1) bytes (up to 512 MB for G, where n <= 2^20)
+ *   workspace         at least coop_softmax_xent_workspace_bytes(n, vocab, dim, dtype, aligned, 1) bytes: with n rounded up to 256, a copy of
+ *                     hidden (and of weight, where it is copied), dhidden in fp32 (or 64 MB, if that is more), up to 64 MB of dweight's
+ *                     sums, and G: 512 MB (or 512 bytes a row, if that is more) and 256 bytes a row; nothing for G with up to 128 elements
+ *                     of 16 bits
  */
 int coop_softmax_xent_grad(const void* hidden, int64_t n, const void* weight, int64_t vocab, int32_t dim, int dtype,
                            const int32_t* targets, float alpha, int32_t ignore, const float* lse, const float* dloss, void* dhidden,

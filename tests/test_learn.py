@@ -1090,3 +1090,21 @@ def test_layer_norm_in_place(rows, dim, dtype):
     got, dgot = unaligned(x), unaligned(dy)
     assert all(torch.equal(s, t) for s, t in zip(P.coop_layer_norm(got, w, b, out=got), (y, mean, rstd)))
     assert all(torch.equal(s, t) for s, t in zip(P.coop_layer_norm_grad(dgot, x, mean, rstd, w, out=dgot), (dx, dw, db)))
+
+
+def test_softmax_xent_grad_workspace_is_what_is_said():
+    """... of its size, in coop.h: over rows, vocabularies, widths and types, the sum of what it is said to hold is enough and not far more."""
+    L, MB = learn.lib(), 1 << 20
+    for n in (1, 24, 32, 33, 300, 4096, 8192, 100000, 500000, 1000000, (1 << 20) - 1, 1 << 20, (1 << 24) - 1):
+        for vocab in (1, 170, 20000, 131072, 17000001):
+            for dim in (1, 75, 128, 136, 602, 1024, 4096):
+                for dtype, es in ((0, 4), (1, 2), (2, 2)):
+                    for aligned in (0, 1):
+                        width = -(-dim * es // 16) * 16 // es
+                        narrow = es == 2 and width <= 128
+                        rows = 32 if n <= 32 and not narrow else -(-n // 256) * 256
+                        copies = rows * width * es + (vocab * width * es if width != dim or not aligned else 0)
+                        sums = max(64 * MB, rows * width * 4) + 64 * MB
+                        g = 0 if narrow else max(512 * MB, 512 * rows) + 256 * rows
+                        need = L.coop_softmax_xent_workspace_bytes(n, vocab, dim, dtype, aligned, 1)
+                        assert 0 < need <= copies + sums + g + 16 * rows + 8192, (n, vocab, dim, dtype, aligned)
