@@ -2,13 +2,16 @@
 up with a scale and their gradient, layer norm, softmax cross entropy over a large vocabulary, AdamW.
 
 Marshalling only, as in binding.py: the results and the workspaces are torch's, the work is the library's.
+
+stream: a stream to work on in the place of torch's current one.  What is given has to be ready on it and to stay until it is through; what
+comes back is ready when it is.
 """
 import ctypes as C
 
 import torch
 
 from . import binding
-from .binding import COOP_F16, COOP_F32, _check, _dev_ptr, _stream_ptr, _used_on
+from .binding import COOP_F16, COOP_F32, _check, _dev_ptr, _stream_ptr, _torch_stream
 
 COOP_BF16 = 2
 COOP_NO_PAD = -(1 << 31)
@@ -63,9 +66,19 @@ def _vector(t, n, dtype, what):
     return t.data_ptr()
 
 
+# What the calls take from torch is the memory of the stream that they work on: memory of torch's current stream may still be in use there by
+# what was queued before the tensor over it went.  Of results torch is told that its current stream uses them too.
+def _scratch(shape, dtype, device, stream):
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(_torch_stream(stream)):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _new(shape, dtype, device, stream):
-    t = torch.empty(shape, dtype=dtype, device=device)
-    _used_on(stream, t)
+    t = _scratch(shape, dtype, device, stream)
+    if stream is not None:
+        t.record_stream(torch.cuda.current_stream(device))
     return t
 
 
@@ -76,7 +89,7 @@ def _workspace(nbytes, given, device, stream):
         return given, given.data_ptr(), given.numel() * given.element_size()
     if nbytes == 0:
         return None, None, 0
-    t = _new(nbytes, torch.uint8, device, stream)
+    t = _scratch(nbytes, torch.uint8, device, stream)
     return t, t.data_ptr(), nbytes
 
 

@@ -1108,3 +1108,58 @@ def test_softmax_xent_grad_workspace_is_what_is_said():
                         g = 0 if narrow else max(512 * MB, 512 * rows) + 256 * rows
                         need = L.coop_softmax_xent_workspace_bytes(n, vocab, dim, dtype, aligned, 1)
                         assert 0 < need <= copies + sums + g + 16 * rows + 8192, (n, vocab, dim, dtype, aligned)
+
+
+def test_memory_of_a_call_is_that_of_its_stream(monkeypatch):
+    """Results and workspaces come from torch while the stream that writes them is the current one, and torch is told that the stream which
+    was current uses the results."""
+    now, made = ["main"], []
+
+    class Current:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            now.append(self.stream)
+
+        def __exit__(self, *error):
+            now.pop()
+
+    class Buffer:
+        def __init__(self, *shape, **kw):
+            self.of, self.used_on = now[-1], []
+            made.append(self)
+
+        def data_ptr(self):
+            return 0x1000
+
+        def record_stream(self, stream):
+            self.used_on.append(stream)
+
+    monkeypatch.setattr(learn.torch, "empty", Buffer)
+    monkeypatch.setattr(learn.torch.cuda, "stream", Current)
+    monkeypatch.setattr(learn.torch.cuda, "current_stream", lambda device=None: now[-1])
+    for module in (learn, learn.binding):
+        monkeypatch.setattr(module, "_torch_stream", lambda stream: stream, raising=False)
+    learn._new((3, 4), torch.float32, "cuda", None)
+    learn._new((3, 4), torch.float32, "cuda", "side")
+    learn._workspace(1024, None, "cuda", "side")
+    assert [(b.of, b.used_on) for b in made] == [("main", []), ("side", ["main"]), ("side", [])] and now == ["main"]
+
+
+@gpu
+def test_memory_that_the_current_stream_still_uses_is_not_written():
+    """Work that waits on torch's current stream, over memory that has been given back, does not meet a call's on another stream."""
+    g = rng(31)
+    table, ids = normal(g, 3000, 256), torch.randint(0, 3000, (20000,), generator=g, device="cuda", dtype=torch.int32)
+    want = P.coop_embed(table, ids)
+    side = torch.cuda.Stream()
+    old = torch.empty_like(want)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)        # (some ten milliseconds)
+    old.fill_(7.0)
+    del old
+    got = P.coop_embed(table, ids, stream=side)
+    grad = P.coop_embed_grad(want, ids, 3000, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(grad, P.coop_embed_grad(want, ids, 3000))
