@@ -151,7 +151,7 @@ def coop_embed_grad_rows(dout, ids, n_rows, scale=None, alpha=1.0, pad=None, dty
 
 def _weight_dtype(x, *weights):
     given = {w.dtype for w in weights if w is not None}
-    assert len(given) <= 1, "weight and bias have one type"
+    assert len(given) <= 1 and given <= set(_DTYPES), "weight and bias have one type: fp32, fp16 or bf16"
     return _DTYPES[given.pop()] if given else COOP_F32
 
 

@@ -1163,3 +1163,11 @@ def test_memory_that_the_current_stream_still_uses_is_not_written():
     grad = P.coop_embed_grad(want, ids, 3000, stream=side)
     torch.cuda.synchronize()
     assert torch.equal(got, want) and torch.equal(grad, P.coop_embed_grad(want, ids, 3000))
+
+
+def test_norm_weights_of_unknown_types_are_refused_like_other_arguments():
+    x, w = torch.zeros((2, 4)), torch.zeros(4)
+    assert learn._weight_dtype(x) == learn._weight_dtype(x, w, w) == P.COOP_F32 and learn._weight_dtype(x, w.half()) == P.COOP_F16
+    for weights in ((w.double(),), (w.int(), w.int()), (w, w.half())):
+        with pytest.raises(AssertionError):
+            learn._weight_dtype(x, *weights)
