@@ -316,10 +316,13 @@ int coop_cache_vertices(const coop_cache* c, const int32_t** vertex_of_out, int6
 /*
  * Operators of learned vertex representations: what a program that trains rows for the vertices (in the place of, or on top
  * of, given features) does with sampled blocks.  Elements are COOP_F32, COOP_F16 or COOP_BF16; arithmetic, sums and
- * statistics are in 32 bits and are rounded once, to nearest, when a result is stored.  Pointers need the alignment of their
+ * statistics are in 32 bits and are rounded once, to nearest, when a result is stored.  Two things are rounded besides: the
+ * logits' gradient between the products of coop_softmax_xent_grad, to the operands' type, and moments that are kept in 8 bits.  Pointers need the alignment of their
  * elements only, workspaces 256 bytes; rows are dense.  All calls are asynchronous on `stream`, allocate nothing, copy
  * nothing to or from the host, and give the same bits for the same input on every call (no sum's order depends on time), so
- * that they can be captured into a graph.  A workspace's contents are undefined before and after; calls that overlap need
+ * that they can be captured into a graph.  (coop_adamw's step, rates and seed are numbers of the call, though: every replay of
+ * a captured one is the same step again, with that step's bias corrections and random numbers.  A program that trains by replays
+ * captures the gradients, and steps outside.)  A workspace's contents are undefined before and after; calls that overlap need
  * one each.  Ids and targets outside their range are reported by coop_gather_status.
  */
 
@@ -420,7 +423,8 @@ int coop_softmax_xent_grad(const void* hidden, int64_t n, const void* weight, in
  * and 3 mantissa bits, OCP E4M3) of the parameter's shape, and m_scale, v_scale float arrays [n_rows, ceil(dim / 256)]: a
  * value is the 8-bit float times the scale of its 256 neighbouring elements of a row.  They are rounded up or down at random,
  * with the value itself as the mean, by a hash of (seed, step, place of the tensor in the list, element): the same arguments
- * give the same bits.  All zeros are the state before step 1, either way.
+ * give the same bits.  (But a root of v below 2^-9 of its scale, the least 8-bit float, is rounded up to that: never to zero.  And
+ * m is divided by the root, before they are rounded, through the hardware's approximate reciprocal, of 1 unit in the last place.)  All zeros are the state before step 1, either way.
  */
 typedef struct {
   void* param;            /* device, param_dtype */

@@ -282,7 +282,8 @@ class AdamW:
     def step(self, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, rows=None, seed=0, grad_scale=None, stream=None):
         """One step; `step` counts from 1.  rows: {parameter's place in the list: (rows, gradients, count or None)}, as
         coop_embed_grad_rows returns them, for parameters of which only these rows change.  grad_scale: fp32 [1] on the device,
-        multiplied into every gradient."""
+        multiplied into every gradient.  Captured into a graph, every replay is this same step again: step, rates and seed are
+        the captured ones."""
         rows = rows or {}
         assert all(0 <= i < len(self.params) for i in rows)
         for i, g in enumerate(self.grads):
