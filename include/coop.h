@@ -449,6 +449,58 @@ typedef struct {
 int coop_adamw(const coop_adamw_tensor* tensors, int n, int bits, double lr, double beta1, double beta2, double eps, double weight_decay,
                int64_t step, uint64_t seed, const float* grad_scale, void* stream);
 
+/*
+ * Layers of a model on such rows: a dense layer with its epilogue, and the gated block's two projections.  Elements of all operands are of one
+ * dtype; what the activation is of (the products plus their biases) can be kept in 32 bits, pre_out, for the gradient calls, which
+ * otherwise compute it again.  dz, the gradient of that, is rounded to dtype, being an operand of the matrix units.
+ *
+ * coop_linear: out = alpha act(x transposed(weight) + bias) + residual.
+ *   x         device [n, k], weight device [m, k], bias device [m] or NULL, residual device [n, m] or NULL (may be out); all of dtype
+ *   out       device [n, m] of dtype; pre_out device float [n, m] or NULL
+ *   workspace at least coop_linear_workspace_bytes(n, k, m, dtype, aligned) bytes, aligned = 1 if x and weight are multiples of 16, else 0.
+ *             (Operands that are not, or whose rows are no multiple of 16 bytes, are copied into the workspace; up to 32 MB are for parts of
+ *             products that have too few tiles for the chip.)
+ * n <= 2^31 - 512; k, m <= 2^18 (and together no more than 2^31 tiles).  COOP_ACT_GELU is z Phi(z) with the normal distribution's Phi, COOP_ACT_SILU z / (1 + exp(-z)).
+ */
+#define COOP_ACT_NONE 0
+#define COOP_ACT_RELU 1
+#define COOP_ACT_GELU 2
+#define COOP_ACT_SILU 3
+size_t coop_linear_workspace_bytes(int64_t n, int32_t k, int32_t m, int dtype, int aligned);
+int coop_linear(const void* x, int64_t n, int32_t k, const void* weight, int32_t m, int dtype, const void* bias, int act, float alpha,
+                const void* residual, void* out, float* pre_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its gradient: dz = alpha dout act'(pre), dx = dz weight, dweight = transposed(dz) x, dbias = sum over the rows of dz.  (The residual's is dout.)
+ *   pre       what coop_linear kept; NULL: computed again (bias is read then only); not read without an activation
+ *   dx        device [n, k] of dtype; dweight device [m, k] of grad_dtype (COOP_F32 or dtype); dbias device float [m]; each may be NULL
+ *   workspace at least coop_linear_grad_workspace_bytes(n, k, m, dtype, act, has_pre, aligned) bytes, aligned = 1 if dout, x and weight
+ *             are multiples of 16, else 0
+ */
+size_t coop_linear_grad_workspace_bytes(int64_t n, int32_t k, int32_t m, int dtype, int act, int has_pre, int aligned);
+int coop_linear_grad(const void* dout, const void* x, int64_t n, int32_t k, const void* weight, int32_t m, int dtype, const void* bias, int act,
+                     float alpha, const float* pre, void* dx, void* dweight, int grad_dtype, float* dbias, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
+/*
+ * The gated block's projections: with g = x transposed(gate) + gate_bias and u = x transposed(up) + up_bias, out = act(g) u.
+ *   gate, up  device [f, k]; gate_bias, up_bias device [f] or NULL; out device [n, f]
+ *   pre_out   device float [2, n, f]: g and u; or NULL
+ *   workspace as coop_linear's: aligned is about x, gate and up
+ */
+size_t coop_gated_workspace_bytes(int64_t n, int32_t k, int32_t f, int dtype, int aligned);
+int coop_gated(const void* x, int64_t n, int32_t k, const void* gate, const void* up, int32_t f, int dtype, const void* gate_bias,
+               const void* up_bias, int act, void* out, float* pre_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its gradient: dg = dout u act'(g), du = dout act(g), dx = dg gate + du up, dgate = transposed(dg) x, dup = transposed(du) x, the biases' the
+ * sums of dg and of du over the rows.  dx may be NULL, and dgate with dup, and dgate_bias with dup_bias.  pre: as above.
+ */
+size_t coop_gated_grad_workspace_bytes(int64_t n, int32_t k, int32_t f, int dtype, int has_pre, int aligned);
+int coop_gated_grad(const void* dout, const void* x, int64_t n, int32_t k, const void* gate, const void* up, int32_t f, int dtype,
+                    const void* gate_bias, const void* up_bias, int act, const float* pre, void* dx, void* dgate, void* dup, int grad_dtype,
+                    float* dgate_bias, float* dup_bias, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Name of an error code (static string). */
 const char* coop_strerror(int code);
 

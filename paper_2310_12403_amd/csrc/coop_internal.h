@@ -64,6 +64,20 @@ enum KernelId {
   K_XENT_DH,         // ... its product with the weight
   K_XENT_DW,         // ... its product with the hidden states
   K_XENT_OUT,        // ... sums of a product's parts, rounded
+  K_DENSE_PAD,       // dense layers: operands into rows of a multiple of 16 bytes
+  K_LINEAR,          // ... the product of a layer, or its slope
+  K_GATED,           // ... both products of a gated block, or their slopes
+  K_DENSE_JOIN,      // ... a split product's parts added up
+  K_DENSE_SLOPE,     // ... the products' gradient from what the forward call kept
+  K_DENSE_COLUMNS,   // ... the biases' gradient, from partial sums
+  K_DENSE_DX,        // ... the input's gradient
+  K_DENSE_DW,        // ... the weight's
+  K_SEAM,            // residual norm
+  K_SEAM_GRAD,       // ... its gradient
+  K_SEAM_JOIN,       // ... the weights', from the blocks' partial sums
+  K_GRAD_NORM,       // squares of the gradients
+  K_GRAD_FACTOR,     // ... their norm and the factor that clips it
+  K_GRAD_SCALE,      // gradients times a factor
   K_COUNT_
 };
 

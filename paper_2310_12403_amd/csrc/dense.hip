@@ -1,0 +1,758 @@
+// Dense layers on rows: y = alpha act(x W' + b) + residual, and the gated block's h = act(x Wg' + bg) (x Wu' + bu), with their gradients.
+//
+// Backward, with z the products plus their biases: dz = alpha dy act'(z) (gated: dg = dh u act'(g), du = dh act(g)), then dx = dz W,
+// dW = dz' x, db = sum over the rows of dz.  dz is an operand of the matrix units and so rounded to the operands' type; db is summed from it
+// before that.  z is either what the forward call kept, in 32 bits, or computed again.
+//
+// All products are tiles of C = A B' (products.h): A has the columns of the result, so that a lane's registers hold neighbouring ones, and B
+// its rows.  The gated product's two weights are one operand with 32 rows of each in turn: a wave has the gate's and the up projection's sums
+// of the same elements, and x is read once for both.  A tile leaves its sums through LDS, so that what follows reads and writes whole rows.
+// Where there are few tiles for the chip, k is split: the parts are left in 32 bits and a second kernel adds them up, in their order, ahead
+// of the same epilogue.
+#include <type_traits>
+#include <utility>
+
+#include "activations.h"
+#include "coop_internal.h"
+#include "dealing.h"
+#include "products.h"
+
+namespace coop {
+namespace {
+
+int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+int64_t at_most(int64_t x, int64_t most) { return x < 1 ? 1 : x < most ? x : most; }
+
+// f of 0 .. N - 1 as compile-time constants: a loop that indexes registers, whatever is in it
+template <typename F, int... I>
+__device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>()), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each_of(F&& f) {
+  each_of(f, std::make_integer_sequence<int, N>());
+}
+
+template <int T> constexpr int kE = 16 / kElem<T>;  // elements of a pack of 16 bytes
+
+// Columns col .. col + E - 1 of a row of `dim`: those that there are; the others read as zeros.
+template <int T, int E>
+__device__ __forceinline__ void load_columns(const void* row, int32_t col, int32_t dim, float (&f)[E]) {
+  typedef typename Element<T>::M M;
+  const M* p = (const M*)row + col;
+  if (col + E <= dim) {
+    load_elements<T, E>(p, f);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) f[e] = col + e < dim ? (float)p[e] : 0.f;
+  }
+}
+template <int T, int E>
+__device__ __forceinline__ void store_columns(void* row, int32_t col, int32_t dim, const float (&f)[E]) {
+  typedef typename Element<T>::M M;
+  M* p = (M*)row + col;
+  if (col + E <= dim) {
+    store_elements<T, E>(p, f);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (col + e < dim) p[e] = (M)f[e];
+  }
+}
+
+// ---- what becomes of a product's sums --------------------------------------------------------------------------------------
+// put(lane, row, v, u): E neighbouring columns of a row of the first product, and of a pair's second.  A lane keeps its columns.
+
+// the forward result
+template <int T, bool PAIR>
+struct Forward {
+  static constexpr bool kSums = false;
+  const char *bias, *bias2, *residual;
+  float *pre, *pre2;  // null: not kept
+  char* out;
+  int64_t rows;
+  int32_t cols;
+  float alpha;
+  int act;
+  template <int E>
+  struct Lane {
+    int32_t col;
+    float b[E], b2[E];
+  };
+  template <int E>
+  __device__ __forceinline__ void begin(Lane<E>& l, int32_t col) const {
+    l.col = col;
+#pragma unroll
+    for (int e = 0; e < E; ++e) l.b[e] = l.b2[e] = 0.f;
+    if (bias != nullptr) load_columns<T, E>(bias, col, cols, l.b);
+    if (PAIR && bias2 != nullptr) load_columns<T, E>(bias2, col, cols, l.b2);
+  }
+  template <int E>
+  __device__ __forceinline__ void put(Lane<E>& l, int64_t row, float (&v)[E], float (&u)[E]) const {
+    if (row >= rows || l.col >= cols) return;
+    const int64_t at = row * cols;
+    if (bias != nullptr) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] += l.b[e];
+    }
+    if (PAIR && bias2 != nullptr) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) u[e] += l.b2[e];
+    }
+    if (pre != nullptr) {
+      store_columns<COOP_F32, E>(pre + at, l.col, cols, v);
+      if (PAIR) store_columns<COOP_F32, E>(pre2 + at, l.col, cols, u);
+    }
+    if (out == nullptr) return;  // (computed again, for its gradient)
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = PAIR ? act_value(v[e], act) * u[e] : act_value(v[e], act) * alpha;
+    if (!PAIR && residual != nullptr) {
+      float r[E];
+      load_columns<T, E>(residual + at * kElem<T>, l.col, cols, r);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] += r[e];
+    }
+    store_columns<T, E>(out + at * kElem<T>, l.col, cols, v);
+  }
+};
+
+// dz of what the forward product is once more, as an operand (rows of `ld` elements, zeros up to the next pack behind `cols`; a pair's
+// second part begins at `second`), and the sums of its columns over the rows that a wave has.
+template <int T, bool PAIR>
+struct Slope {
+  static constexpr bool kSums = true;
+  const char *bias, *bias2, *dout;
+  char* dz;
+  float *part, *part2;  // [waves of rows][cols], or null
+  int64_t rows, ld, second;
+  int32_t cols;
+  float alpha;
+  int act;
+  template <int E>
+  struct Lane {
+    int32_t col;
+    float b[E], b2[E], s[E], s2[E];
+  };
+  template <int E>
+  __device__ __forceinline__ void begin(Lane<E>& l, int32_t col) const {
+    l.col = col;
+#pragma unroll
+    for (int e = 0; e < E; ++e) l.b[e] = l.b2[e] = l.s[e] = l.s2[e] = 0.f;
+    if (bias != nullptr) load_columns<T, E>(bias, col, cols, l.b);
+    if (PAIR && bias2 != nullptr) load_columns<T, E>(bias2, col, cols, l.b2);
+  }
+  // v, u: the products' sums with their biases (behind the last column: anything)
+  template <int E>
+  __device__ __forceinline__ void slope(Lane<E>& l, int64_t row, const float (&v)[E], const float (&u)[E]) const {
+    float d[E], d2[E];
+    load_columns<T, E>(dout + row * cols * kElem<T>, l.col, cols, d);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const bool there = l.col + e < cols;
+      float value;
+      const float s = act_slope(v[e], act, &value);
+      if (PAIR) {
+        d2[e] = there ? d[e] * value : 0.f;
+        d[e] = there ? d[e] * u[e] * s : 0.f;
+        l.s2[e] += d2[e];
+        l.s[e] += d[e];
+      } else {  // (without an activation the factor is the results', and dz the gradient as it came)
+        const float scaled = there ? d[e] * alpha * s : 0.f;
+        if (act != COOP_ACT_NONE) d[e] = scaled;
+        l.s[e] += scaled;
+      }
+    }
+    if (dz == nullptr) return;
+    store_elements<T, E>(dz + (row * ld + l.col) * kElem<T>, d);
+    if (PAIR) store_elements<T, E>(dz + (row * ld + second + l.col) * kElem<T>, d2);
+  }
+  template <int E>
+  __device__ __forceinline__ void put(Lane<E>& l, int64_t row, float (&v)[E], float (&u)[E]) const {
+    if (row >= rows || l.col >= cols) return;
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] += l.b[e], u[e] += PAIR ? l.b2[e] : 0.f;
+    slope(l, row, v, u);
+  }
+  // the lanes of a wave whose numbers differ in the bits from `lanes` on have the same columns
+  template <int E>
+  __device__ __forceinline__ void end(Lane<E>& l, int lanes, int64_t part_row) const {
+    if (part == nullptr) return;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      for (int off = lanes; off < kWave; off <<= 1) {
+        l.s[e] += __shfl_xor(l.s[e], off, kWave);
+        if (PAIR) l.s2[e] += __shfl_xor(l.s2[e], off, kWave);
+      }
+    if (lane_id() >= lanes || l.col >= cols) return;
+    store_columns<COOP_F32, E>(part + part_row * cols, l.col, cols, l.s);
+    if (PAIR) store_columns<COOP_F32, E>(part2 + part_row * cols, l.col, cols, l.s2);
+  }
+};
+
+// a gradient, times `scale`; rows from `second` on are another array's (each has `rows` of them)
+struct Gradient {
+  static constexpr bool kSums = false;
+  char *out, *out2;
+  int64_t rows, second;
+  int32_t cols;
+  float scale;
+  int type;
+  template <int E> struct Lane { int32_t col; };
+  template <int E>
+  __device__ __forceinline__ void begin(Lane<E>& l, int32_t col) const { l.col = col; }
+  template <int E>
+  __device__ __forceinline__ void put(Lane<E>& l, int64_t row, float (&v)[E], float (&)[E]) const {
+    char* to = out;
+    if (out2 != nullptr && row >= second) row -= second, to = out2;
+    if (row >= rows || l.col >= cols) return;
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] *= scale;
+    if (type == COOP_F32) store_columns<COOP_F32, E>(to + row * cols * 4, l.col, cols, v);
+    else if (type == COOP_F16) store_columns<COOP_F16, E>(to + row * cols * 2, l.col, cols, v);
+    else store_columns<COOP_BF16, E>(to + row * cols * 2, l.col, cols, v);
+  }
+};
+
+// a split's part: [split][rows][width], of a pair the second product `width / 2` columns behind the first
+template <bool PAIR>
+struct Part {
+  static constexpr bool kSums = false;
+  float* sums;
+  int64_t rows, width, split_rows;
+  template <int E> struct Lane { int32_t col; };
+  template <int E>
+  __device__ __forceinline__ void begin(Lane<E>& l, int32_t col) const { l.col = col; }
+  template <int E>
+  __device__ __forceinline__ void put(Lane<E>& l, int64_t row, float (&v)[E], float (&u)[E]) const {
+    const int64_t half = PAIR ? width / 2 : width;
+    if (row >= rows || l.col >= half) return;
+    float* to = sums + (split_rows + row) * width + l.col;
+    store_elements<COOP_F32, E>(to, v);
+    if (PAIR) store_elements<COOP_F32, E>(to + half, u);
+  }
+};
+
+// ---- products ------------------------------------------------------------------------------------------------------------------
+// FORM: one operand A; a pair of them (their rows in turn); or two, one behind the other along k, where B's k goes on.
+enum { kOne, kPair, kTwo };
+
+// Which tiles a block has: those of a split are dealt out in strips of kStrip of B's, so that the 32 blocks that an XCD runs at a time have
+// neighbouring ones of both operands.
+constexpr uint32_t kStrip = 4;
+struct Tiles {
+  uint32_t a, b, splits;
+  struct Mine { uint32_t a, b, split; };
+  __device__ __forceinline__ Mine mine() const {
+    const uint32_t i = xcd_runs(blockIdx.x, gridDim.x), split = i / (a * b), t = i - split * (a * b);
+    const uint32_t first = t / (a * kStrip) * kStrip, at = t - first * a, rows = b - first < kStrip ? b - first : kStrip;
+    return Mine{at / rows, first + at % rows, split};
+  }
+};
+
+template <int T, int WA, int WB, int TA, int TB, bool SA, bool SB, int SIZE, int FORM, typename Fin>
+__global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1))) void k_dense(Operand a, Operand a2, Operand b, Operand b2, int64_t k,
+                                                                                               Tiles tiles, Fin fin) {
+  typedef Product<T, WA, WB, TA, TB, SA, SB, SIZE, FORM == kPair> P;
+  extern __shared__ char lds[];
+  constexpr int kColsA = FORM == kPair ? P::kRowsA / 2 : P::kRowsA;  // of the result
+  const Tiles::Mine mine = tiles.mine();
+  const int64_t col0 = (int64_t)mine.a * kColsA, row0 = (int64_t)mine.b * P::kRowsB;
+  const int64_t stages = (k + P::kK - 1) / P::kK;
+  const int64_t k0 = stages * mine.split / tiles.splits * P::kK, k1 = stages * (mine.split + 1) / tiles.splits * P::kK;
+  P p;
+  if constexpr (FORM == kTwo) {
+    p.begin_two(a, b, a2, b2, col0, row0, k0, k1, lds);
+    p.zero();
+    p.tile();
+    p.tile();
+  } else {
+    p.begin(a, b, col0, row0, k0, k1, 0, lds);
+    p.zero();
+    p.tile();
+  }
+  P::end();
+  if constexpr (std::is_same<Fin, Part<FORM == kPair>>::value) fin.split_rows = mine.split * fin.rows;
+  // Through LDS, a wave for itself: 32 rows at a time, written by columns, read by rows.
+  constexpr int E = kE<T>, kLdsCols = TA * 32, kCols = FORM == kPair ? kLdsCols / 2 : kLdsCols, kRow = kLdsCols + 4;  // (rows begin in different banks)
+  constexpr int kLanes = kCols / E, kEach = kWave / kLanes;  // lanes of a row, rows at a time
+  static_assert(P::kWaves * 32 * kRow * 4 <= P::kLds && kLanes <= kWave, "the waves' rows lie where the stages were");
+  float* const own = reinterpret_cast<float*>(lds) + uniform_wave_in_block() * (32 * kRow);
+  const int lane = lane_id(), mine_col = lane % kLanes * E;
+  typename Fin::template Lane<E> at;
+  fin.begin(at, (int32_t)(col0 + P::a0() / (kLdsCols / kCols)) + mine_col);
+  each_of<TB>([&](auto number) {
+    constexpr int j = decltype(number)::value;
+#pragma unroll
+    for (int i = 0; i < TA; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float f[4] = {p.acc[i][j][4 * q], p.acc[i][j][4 * q + 1], p.acc[i][j][4 * q + 2], p.acc[i][j][4 * q + 3]};
+        const int col = (FORM == kPair ? (i & 1) * kCols + (i >> 1) * 32 : i * 32) + P::row_of(4 * q) + P::own_row();
+        store_elements<COOP_F32, 4>(own + (lane & 31) * kRow + col, f);
+      }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 4
+    for (int i = 0; i < 32 / kEach; ++i) {
+      const int r = i * kEach + lane / kLanes;
+      float v[E], u[E];
+      load_elements<COOP_F32, E>(own + r * kRow + mine_col, v);
+      if constexpr (FORM == kPair) load_elements<COOP_F32, E>(own + r * kRow + kCols + mine_col, u);
+      else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) u[e] = 0.f;
+      }
+      fin.put(at, row0 + P::b0() + j * 32 + r, v, u);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  });
+  if constexpr (Fin::kSums) fin.end(at, kLanes, (int64_t)mine.b * WB + uniform_wave_in_block() % WB);
+}
+
+// The splits' parts added up in their order, and the epilogue.  A thread has E columns of a row.
+template <int T, bool PAIR, typename Fin>
+__global__ __launch_bounds__(kBlock) void k_dense_join(const float* __restrict__ sums, int splits, int64_t rows, int64_t width, int32_t cols, Fin fin) {
+  constexpr int E = 4;
+  const int32_t packs = (cols + E - 1) / E;
+  const int64_t half = PAIR ? width / 2 : 0;
+  for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < rows * packs; i += (int64_t)gridDim.x * kBlock) {
+    const int64_t row = i / packs;
+    const int32_t c = (int32_t)(i - row * packs) * E;
+    float v[E] = {0.f, 0.f, 0.f, 0.f}, u[E] = {0.f, 0.f, 0.f, 0.f};
+    const float* from = sums + row * width + c;
+#pragma unroll 4
+    for (int q = 0; q < splits; ++q, from += rows * width) {
+      float f[E];
+      load_elements<COOP_F32, E>(from, f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] += f[e];
+      if constexpr (PAIR) {
+        load_elements<COOP_F32, E>(from + half, f);
+#pragma unroll
+        for (int e = 0; e < E; ++e) u[e] += f[e];
+      }
+    }
+    typename Fin::template Lane<E> at;
+    fin.begin(at, c);
+    fin.put(at, row, v, u);
+  }
+}
+
+// dz from what the forward call kept (pre null: there is no activation), or only the sums of its columns (dz null).  2^lanes_log2 lanes share
+// a row, blockIdx.x for parts of the columns, blockIdx.y deals the rows; part[blockIdx.y * 4 + wave].
+template <int T, bool PAIR>
+__global__ __launch_bounds__(kBlock) void k_dense_slope(const float* __restrict__ pre, const float* __restrict__ pre2, int lanes_log2, Slope<T, PAIR> fin) {
+  constexpr int E = kE<T>;
+  const int lanes = 1 << lanes_log2, lane = lane_id() & (lanes - 1);
+  typename Slope<T, PAIR>::template Lane<E> at;
+  fin.begin(at, ((int32_t)blockIdx.x * lanes + lane) * E);
+  const int64_t step = (int64_t)gridDim.y * (kBlock >> lanes_log2);
+  if (at.col < fin.cols) {
+#pragma unroll 2
+    for (int64_t r = (int64_t)blockIdx.y * (kBlock >> lanes_log2) + (threadIdx.x >> lanes_log2); r < fin.rows; r += step) {
+      float v[E], u[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = u[e] = 0.f;
+      if (pre != nullptr) load_columns<COOP_F32, E>(pre + r * fin.cols, at.col, fin.cols, v);
+      if (PAIR) load_columns<COOP_F32, E>(pre2 + r * fin.cols, at.col, fin.cols, u);
+      fin.slope(at, r, v, u);
+    }
+  }
+  fin.end(at, lanes, (int64_t)blockIdx.y * kWavesPerBlock + uniform_wave_in_block());
+}
+
+// out[y][c] = sum of the y-th share of part's rows; 64 columns a block, its waves deal the rows among themselves.  Of two parts one behind the
+// other (as many rows each) the second's sums are out2's.
+constexpr int kJoinWaves = 16;
+__global__ __launch_bounds__(kJoinWaves* kWave) void k_dense_columns(const float* __restrict__ part, const float* __restrict__ part2, int64_t rows, int32_t cols,
+                                                                    float* __restrict__ out, float* __restrict__ out2) {
+  __shared__ float lds[kJoinWaves][kWave];
+  if (blockIdx.z == 1) part = part2, out = out2;
+  const int32_t c = (int32_t)blockIdx.x * kWave + lane_id();
+  const int64_t first = rows * blockIdx.y / gridDim.y, last = rows * (blockIdx.y + 1) / gridDim.y;
+  float sum = 0.f;
+  if (c < cols) {
+#pragma unroll 8
+    for (int64_t r = first + wave_in_block(); r < last; r += kJoinWaves) sum += part[r * cols + c];
+  }
+  lds[wave_in_block()][lane_id()] = sum;
+  __syncthreads();
+  if (wave_in_block() != 0 || c >= cols) return;
+  sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < kJoinWaves; ++w) sum += lds[w][lane_id()];
+  out[(int64_t)blockIdx.y * cols + c] = sum;
+}
+
+// Rows of `dim` elements into rows of `width`, a multiple of 16 bytes, zeros behind a row's end.  Up to four arrays in one launch.
+struct Copy {
+  const char* in;
+  char* out;
+  int64_t rows;
+  int32_t dim, width;
+  uint32_t first_block;
+};
+struct Copies {
+  Copy c[4];
+  int n;
+};
+template <int T>
+__global__ __launch_bounds__(kBlock) void k_dense_pad(Copies jobs, uint32_t blocks) {
+  typedef typename Element<T>::M M;
+  constexpr int E = kE<T>;
+  int j = 0;
+  while (j + 1 < jobs.n && blockIdx.x >= jobs.c[j + 1].first_block) ++j;
+  const Copy& c = jobs.c[j];
+  const uint32_t end = j + 1 < jobs.n ? jobs.c[j + 1].first_block : blocks;
+  const int32_t packs = c.width / E;
+  for (int64_t i = (int64_t)(blockIdx.x - c.first_block) * kBlock + threadIdx.x; i < c.rows * packs; i += (int64_t)(end - c.first_block) * kBlock) {
+    const int64_t row = i / packs;
+    const int32_t col = (int32_t)(i - row * packs) * E;
+    float f[E];
+    load_columns<T, E>((const M*)c.in + row * c.dim, col, c.dim, f);
+    store_elements<T, E>((M*)c.out + row * c.width + col, f);
+  }
+}
+
+// ---- how a call is cut ------------------------------------------------------------------------------------------------------------
+// A product of rows x cols over k.  Tiles of 256 x 256, what a wave's registers hold, where 16-bit operands have enough of them for the chip;
+// else of 128 x 128, two blocks on a CU.  k is split where there are fewer tiles than blocks that run at a time, as long as every part has four
+// stages.
+struct Cut {
+  int64_t rows, cols, width;  // width: of a row of parts
+  int tile;
+  uint32_t tiles_a, tiles_b, splits;
+  size_t part_bytes;
+  Cut() {}
+  Cut(int64_t rows_, int64_t cols_, int64_t k, int dtype, bool pair) : rows(rows_), cols(cols_) {
+    const int per_tile = pair ? 2 : 1;
+    const auto tiles_of = [&](int t) { return ((cols * per_tile + t - 1) / t) * ((rows + t - 1) / t); };
+    tile = dtype != COOP_F32 && tiles_of(256) >= 256 ? 256 : 128;
+    tiles_a = (uint32_t)((cols * per_tile + tile - 1) / tile);
+    tiles_b = (uint32_t)((rows + tile - 1) / tile);
+    const int64_t stages = k * element_bytes(dtype) / kWide;
+    splits = (uint32_t)at_most((tile == 128 ? 512 : 256) / at_most(tiles_of(tile), 512), stages / 4 < 1 ? 1 : stages / 4);
+    width = round_up(cols, 8) * per_tile;
+    part_bytes = splits > 1 ? (size_t)splits * (size_t)rows * (size_t)width * 4 : 0;
+  }
+  uint64_t blocks() const { return (uint64_t)tiles_a * tiles_b * splits; }
+};
+
+bool fits(const Cut& c) { return c.blocks() < ((uint64_t)1 << 31); }
+
+// The parts of a call, and where in the workspace they are.  GATED: two weights of m rows.
+struct DensePlan {
+  int64_t n, k, m, kw, mw;  // kw, mw: elements of a row of k or m, up to a multiple of 16 bytes
+  int64_t dz_ld;            // elements; a pair's second part begins at mw
+  bool gated, pad, slope, again;  // slope: dz is not dout itself; again: the forward product is computed again
+  Cut forward, back, weight;      // (dx and dW)
+  int64_t sum_rows;               // of the columns' partial sums
+  int lanes_log2;
+  uint32_t slope_x, slope_y, join_y;
+  size_t x, w, w2, dz, pre, part, part2, join, sums, bytes;
+  DensePlan(int64_t n_, int32_t k_, int32_t m_, int dtype, bool gated_, bool aligned, bool grad, bool keeps, int act) : n(n_), k(k_), m(m_), gated(gated_) {
+    const int es = element_bytes(dtype), e = 16 / es;
+    kw = round_up(k, e);
+    mw = round_up(m, e);
+    pad = !aligned || kw != k;
+    size_t at = 0;
+    auto take = [&](size_t b) { const size_t o = at; at += (b + 255) & ~(size_t)255; return o; };
+    x = take(pad ? (size_t)n * kw * es : 0);
+    w = take(pad ? (size_t)m * kw * es : 0);
+    w2 = take(pad && gated ? (size_t)m * kw * es : 0);
+    forward = Cut(n, m, kw, dtype, gated);
+    size_t parts = forward.part_bytes;
+    dz = pre = part = part2 = join = 0;
+    slope = again = false;
+    if (grad) {
+      again = !keeps && (gated || act != COOP_ACT_NONE);
+      slope = gated || act != COOP_ACT_NONE || !aligned || mw != m;
+      dz_ld = gated ? 2 * mw : mw;
+      if (dz_ld * es % 2048 == 0) dz_ld += 256 / es;  // (or a tile's rows would all lie in the same few channels of memory)
+      dz = take(slope ? (size_t)n * dz_ld * es : 0);
+      pre = take(again && forward.splits > 1 ? (size_t)n * m * 4 * (gated ? 2 : 1) : 0);
+      back = Cut(n, k, mw, dtype, false);
+      weight = Cut(gated ? 2 * mw : m, k, n, dtype, false);
+      if (!again) parts = 0;
+      if (back.part_bytes > parts) parts = back.part_bytes;
+      if (weight.part_bytes > parts) parts = weight.part_bytes;
+      // the columns' sums: by the product's waves of rows, or by the blocks that go over the rows
+      const int64_t packs = mw / e;
+      lanes_log2 = 0;
+      while (lanes_log2 < 6 && 1 << lanes_log2 < packs) ++lanes_log2;
+      slope_x = (uint32_t)((packs + (1 << lanes_log2) - 1) >> lanes_log2);
+      const int64_t groups = (n + (kBlock >> lanes_log2) - 1) / (kBlock >> lanes_log2);
+      slope_y = (uint32_t)at_most(groups, 4096 / slope_x + 1);
+      sum_rows = again && forward.splits == 1 ? (int64_t)forward.tiles_b * 2 : (int64_t)slope_y * kWavesPerBlock;
+      const size_t sum_bytes = (size_t)sum_rows * (size_t)m * 4;
+      part = take(sum_bytes);
+      part2 = take(gated ? sum_bytes : 0);
+      join_y = (uint32_t)at_most(sum_rows / 256, 64);
+      join = take(join_y > 1 ? (size_t)join_y * (size_t)m * 4 * (gated ? 2 : 1) : 0);
+    }
+    sums = take(parts);
+    bytes = at + 256;
+  }
+  bool fit(bool grad) const { return fits(forward) && (!grad || (fits(back) && fits(weight))); }
+};
+
+// (blocks of more than 64 KB of LDS have to be allowed, once for each kernel and device; it costs a fraction of a microsecond)
+template <typename K>
+bool allow_lds(K kernel, int bytes) {
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess;
+}
+
+template <int T, int N, bool SA, bool SB, int SIZE, int FORM, typename Fin>
+bool launch_tiles(int id, const Cut& c, const Operand& a, const Operand& a2, const Operand& b, const Operand& b2, int64_t k, const Fin& fin, hipStream_t s) {
+  typedef Product<T, 2, 2, N, N, SA, SB, SIZE, FORM == kPair> P;
+  const auto kernel = k_dense<T, 2, 2, N, N, SA, SB, SIZE, FORM, Fin>;
+  if (!allow_lds(kernel, P::kLds)) return false;
+  COOP_LAUNCH(id, kernel, dim3((unsigned)c.blocks()), dim3(P::kThreads), P::kLds, s, a, a2, b, b2, k, Tiles{c.tiles_a, c.tiles_b, c.splits}, fin);
+  return true;
+}
+template <int T, bool SA, bool SB, int SIZE, int FORM, typename Fin>
+bool launch_product(int id, const Cut& c, const Operand& a, const Operand& a2, const Operand& b, const Operand& b2, int64_t k, const Fin& fin, hipStream_t s) {
+  if constexpr (T != COOP_F32)
+    if (c.tile == 256) return launch_tiles<T, 4, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, fin, s);
+  return launch_tiles<T, 2, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, fin, s);
+}
+
+// A product and its epilogue, through parts where k is split.
+template <int T, bool SA, bool SB, int SIZE, int FORM, typename Fin>
+bool product(int id, const Cut& c, const Operand& a, const Operand& a2, const Operand& b, const Operand& b2, int64_t k, const Fin& fin, float* sums, hipStream_t s) {
+  if (c.splits == 1) return launch_product<T, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, fin, s);
+  if (!launch_product<T, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, Part<FORM == kPair>{sums, c.rows, c.width, 0}, s)) return false;
+  if constexpr (!Fin::kSums) {
+    const int64_t blocks = (c.rows * ((c.cols + 3) / 4) + kBlock - 1) / kBlock;
+    COOP_LAUNCH(K_DENSE_JOIN, (k_dense_join<T, FORM == kPair, Fin>), dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(kBlock), 0, s, (const float*)sums,
+                (int)c.splits, c.rows, c.width, (int32_t)c.cols, fin);
+  }
+  return true;
+}
+
+struct Arrays {  // what the products read: the caller's, or copies
+  const char *x, *w, *w2;
+};
+template <int T>
+Arrays operands(const DensePlan& p, const void* x, const void* w, const void* w2, bool want_x, char* ws, hipStream_t s) {
+  if (!p.pad) return Arrays{(const char*)x, (const char*)w, (const char*)w2};
+  Copies jobs;
+  jobs.n = 0;
+  uint32_t blocks = 0;
+  const auto add = [&](const void* in, size_t at, int64_t rows) {
+    const int64_t need = (rows * (p.kw / kE<T>) + kBlock - 1) / kBlock;
+    jobs.c[jobs.n++] = Copy{(const char*)in, ws + at, rows, (int32_t)p.k, (int32_t)p.kw, blocks};
+    blocks += (uint32_t)at_most(need, 8192);
+  };
+  if (want_x) add(x, p.x, p.n);
+  add(w, p.w, p.m);
+  if (p.gated) add(w2, p.w2, p.m);
+  COOP_LAUNCH(K_DENSE_PAD, k_dense_pad<T>, dim3(blocks), dim3(kBlock), 0, s, jobs, blocks);
+  return Arrays{ws + p.x, ws + p.w, ws + p.w2};
+}
+
+template <int T, bool PAIR, typename Fin>
+bool forward_product(const DensePlan& p, const Arrays& o, const Fin& fin, float* sums, hipStream_t s) {
+  const int64_t ld = p.kw * kElem<T>;
+  Operand a{o.w, ld, p.m, ld};
+  if (PAIR) a.other = o.w2 - o.w;
+  const Operand b{o.x, ld, p.n, ld};
+  return product<T, false, false, kWide, PAIR ? kPair : kOne>(PAIR ? K_GATED : K_LINEAR, p.forward, a, a, b, b, p.kw, fin, sums, s);
+}
+
+template <int T, bool PAIR>
+bool forward_all(const DensePlan& p, const void* x, const void* w, const void* w2, const Forward<T, PAIR>& fin, char* ws, hipStream_t s) {
+  const Arrays o = operands<T>(p, x, w, w2, true, ws, s);
+  return forward_product<T, PAIR>(p, o, fin, (float*)(ws + p.sums), s);
+}
+
+template <int T, bool PAIR>
+bool backward_all(const DensePlan& p, const void* dout, const void* x, const void* w, const void* w2, const void* bias, const void* bias2, const float* pre,
+                  int act, float alpha, void* dx, void* dw, void* dw2, int grad_dtype, float* db, float* db2, char* ws, hipStream_t s) {
+  const bool products = dx != nullptr || dw != nullptr;
+  float* const sums = (float*)(ws + p.sums);
+  Arrays o{(const char*)x, (const char*)w, (const char*)w2};
+  if (products || p.again) o = operands<T>(p, x, w, w2, dw != nullptr || p.again, ws, s);
+  Slope<T, PAIR> fin;
+  fin.bias = (const char*)bias, fin.bias2 = (const char*)bias2, fin.dout = (const char*)dout;
+  fin.dz = p.slope && products ? ws + p.dz : nullptr;
+  fin.part = db != nullptr || db2 != nullptr ? (float*)(ws + p.part) : nullptr;
+  fin.part2 = (float*)(ws + p.part2);
+  fin.rows = p.n, fin.ld = p.dz_ld, fin.second = p.mw, fin.cols = (int32_t)p.m;
+  fin.alpha = alpha, fin.act = act;
+  if (p.again && p.forward.splits == 1) {
+    if (!forward_product<T, PAIR>(p, o, fin, sums, s)) return false;
+  } else {
+    if (p.again) {
+      Forward<T, PAIR> keep{(const char*)bias, (const char*)bias2, nullptr, (float*)(ws + p.pre), (float*)(ws + p.pre) + p.n * p.m, nullptr, p.n, (int32_t)p.m, 1.f, act};
+      if (!forward_product<T, PAIR>(p, o, keep, sums, s)) return false;
+      pre = keep.pre;
+    }
+    if (fin.dz != nullptr || fin.part != nullptr)
+      COOP_LAUNCH(K_DENSE_SLOPE, (k_dense_slope<T, PAIR>), dim3(p.slope_x, p.slope_y), dim3(kBlock), 0, s, pre, PAIR ? pre + p.n * p.m : nullptr, p.lanes_log2, fin);
+  }
+  if (fin.part != nullptr) {
+    const float *from = fin.part, *from2 = fin.part2;
+    int64_t rows = p.sum_rows;
+    const unsigned x_blocks = (unsigned)((p.m + kWave - 1) / kWave), z = PAIR ? 2 : 1;
+    if (p.join_y > 1) {
+      float* to = (float*)(ws + p.join);
+      COOP_LAUNCH(K_DENSE_COLUMNS, k_dense_columns, dim3(x_blocks, p.join_y, z), dim3(kJoinWaves * kWave), 0, s, from, from2, rows, (int32_t)p.m, to,
+                  to + p.join_y * p.m);
+      from = to, from2 = to + p.join_y * p.m, rows = p.join_y;
+    }
+    COOP_LAUNCH(K_DENSE_COLUMNS, k_dense_columns, dim3(x_blocks, 1, z), dim3(kJoinWaves * kWave), 0, s, from, from2, rows, (int32_t)p.m, db, db2);
+  }
+  const int64_t ldk = p.kw * kElem<T>, ldz = p.slope ? p.dz_ld * kElem<T> : p.m * kElem<T>;
+  const char* dz = p.slope ? ws + p.dz : (const char*)dout;
+  const float scale = PAIR || act != COOP_ACT_NONE ? 1.f : alpha;
+  if (dx != nullptr) {
+    const Gradient g{(char*)dx, nullptr, p.n, 0, (int32_t)p.k, scale, T};
+    const Operand a{o.w, ldk, ldk, p.m}, a2{o.w2, ldk, ldk, p.m};
+    const Operand b{dz, ldz, p.n, p.mw * kElem<T>}, b2{dz + (PAIR ? p.mw * kElem<T> : 0), ldz, p.n, p.mw * kElem<T>};
+    if (!product<T, true, false, kWide, PAIR ? kTwo : kOne>(K_DENSE_DX, p.back, a, a2, b, b2, p.mw, g, sums, s)) return false;
+  }
+  if (dw != nullptr) {
+    const Gradient g{(char*)dw, PAIR ? (char*)dw2 : nullptr, p.m, p.mw, (int32_t)p.k, scale, grad_dtype};
+    const Operand a{o.x, ldk, ldk, p.n}, b{dz, ldz, (PAIR ? 2 * p.mw : p.mw) * kElem<T>, p.n};
+    if (!product<T, true, true, kNarrow, kOne>(K_DENSE_DW, p.weight, a, a, b, b, p.n, g, sums, s)) return false;
+  }
+  return true;
+}
+
+constexpr int32_t kMostWidth = 1 << 18;
+constexpr int64_t kMostRows = ((int64_t)1 << 31) - 512;
+
+bool known_act(int act) { return act == COOP_ACT_NONE || act == COOP_ACT_RELU || act == COOP_ACT_GELU || act == COOP_ACT_SILU; }
+
+int dense_check(int64_t n, int32_t k, int32_t m, int dtype, int act) {
+  if (!known_dtype(dtype) || !known_act(act)) return COOP_E_ARG;
+  if (n < 0 || n > kMostRows || k < 1 || k > kMostWidth || m < 1 || m > kMostWidth) return COOP_E_ARG;
+  return COOP_OK;
+}
+bool aligned16(const void* a, const void* b, const void* c = nullptr, const void* d = nullptr) {
+  return (((uintptr_t)a | (uintptr_t)b | (uintptr_t)c | (uintptr_t)d) & 15) == 0;
+}
+// sums over no rows
+int empty_sums(void* a, int64_t a_bytes, void* b, int64_t b_bytes, hipStream_t s) {
+  if (a != nullptr) clear_bytes(a, a_bytes, s);
+  if (b != nullptr) clear_bytes(b, b_bytes, s);
+  return hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
+}
+bool workspace_ok(const void* ws, size_t bytes, size_t need) { return bytes >= need && ((uintptr_t)ws & 255) == 0; }
+
+}  // namespace
+}  // namespace coop
+
+using namespace coop;
+
+extern "C" size_t coop_linear_workspace_bytes(int64_t n, int32_t k, int32_t m, int dtype, int aligned) {
+  if (dense_check(n, k, m, dtype, COOP_ACT_NONE) != COOP_OK) return 0;
+  return DensePlan(n, k, m, dtype, false, aligned != 0, false, false, COOP_ACT_NONE).bytes;
+}
+
+extern "C" int coop_linear(const void* x, int64_t n, int32_t k, const void* weight, int32_t m, int dtype, const void* bias, int act, float alpha,
+                           const void* residual, void* out, float* pre_out, void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = dense_check(n, k, m, dtype, act);
+  if (rc != COOP_OK) return rc;
+  if (n == 0) return COOP_OK;
+  if (!x || !weight || !out || !workspace) return COOP_E_NULL;
+  for (const void* p : {x, weight, bias, residual, (const void*)out})
+    if (!aligned_for(p, dtype)) return COOP_E_ARG;
+  if (((uintptr_t)pre_out & 3) != 0) return COOP_E_ARG;
+  const DensePlan p(n, k, m, dtype, false, aligned16(x, weight), false, false, act);
+  if (!p.fit(false) || !workspace_ok(workspace, workspace_bytes, p.bytes)) return COOP_E_ARG;
+  bool ok = true;
+  with_dtype(dtype, [&](auto t) {
+    constexpr int T = decltype(t)::value;
+    const Forward<T, false> fin{(const char*)bias, nullptr, (const char*)residual, pre_out, nullptr, (char*)out, n, m, alpha, act};
+    ok = forward_all<T, false>(p, x, weight, nullptr, fin, (char*)workspace, (hipStream_t)stream);
+  });
+  return ok && hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
+}
+
+extern "C" size_t coop_linear_grad_workspace_bytes(int64_t n, int32_t k, int32_t m, int dtype, int act, int has_pre, int aligned) {
+  if (dense_check(n, k, m, dtype, act) != COOP_OK) return 0;
+  return DensePlan(n, k, m, dtype, false, aligned != 0, true, has_pre != 0, act).bytes;
+}
+
+extern "C" int coop_linear_grad(const void* dout, const void* x, int64_t n, int32_t k, const void* weight, int32_t m, int dtype, const void* bias, int act,
+                                float alpha, const float* pre, void* dx, void* dweight, int grad_dtype, float* dbias, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+  const int rc = dense_check(n, k, m, dtype, act);
+  if (rc != COOP_OK) return rc;
+  if (grad_dtype != COOP_F32 && grad_dtype != dtype) return COOP_E_ARG;
+  if ((!dx || n == 0) && !dweight && !dbias) return COOP_OK;
+  if ((n > 0 && (!dout || !x || !weight)) || !workspace) return COOP_E_NULL;
+  for (const void* p : {dout, x, weight, bias, (const void*)dx})
+    if (!aligned_for(p, dtype)) return COOP_E_ARG;
+  if (!aligned_for(dweight, grad_dtype) || (((uintptr_t)pre | (uintptr_t)dbias) & 3) != 0) return COOP_E_ARG;
+  const DensePlan p(n, k, m, dtype, false, aligned16(x, weight, dout), true, pre != nullptr, act);
+  if (!p.fit(true) || !workspace_ok(workspace, workspace_bytes, p.bytes)) return COOP_E_ARG;
+  if (n == 0) return empty_sums(dweight, (int64_t)m * k * element_bytes(grad_dtype), dbias, (int64_t)m * 4, (hipStream_t)stream);
+  bool ok = true;
+  with_dtype(dtype, [&](auto t) {
+    constexpr int T = decltype(t)::value;
+    ok = backward_all<T, false>(p, dout, x, weight, nullptr, bias, nullptr, pre, act, alpha, dx, dweight, nullptr, grad_dtype, dbias, nullptr,
+                                (char*)workspace, (hipStream_t)stream);
+  });
+  return ok && hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
+}
+
+extern "C" size_t coop_gated_workspace_bytes(int64_t n, int32_t k, int32_t f, int dtype, int aligned) {
+  if (dense_check(n, k, f, dtype, COOP_ACT_NONE) != COOP_OK) return 0;
+  return DensePlan(n, k, f, dtype, true, aligned != 0, false, false, COOP_ACT_NONE).bytes;
+}
+
+extern "C" int coop_gated(const void* x, int64_t n, int32_t k, const void* gate, const void* up, int32_t f, int dtype, const void* gate_bias,
+                          const void* up_bias, int act, void* out, float* pre_out, void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = dense_check(n, k, f, dtype, act);
+  if (rc != COOP_OK) return rc;
+  if (n == 0) return COOP_OK;
+  if (!x || !gate || !up || !out || !workspace) return COOP_E_NULL;
+  for (const void* p : {x, gate, up, gate_bias, up_bias, (const void*)out})
+    if (!aligned_for(p, dtype)) return COOP_E_ARG;
+  if (((uintptr_t)pre_out & 3) != 0) return COOP_E_ARG;
+  const DensePlan p(n, k, f, dtype, true, aligned16(x, gate, up), false, false, act);
+  if (!p.fit(false) || !workspace_ok(workspace, workspace_bytes, p.bytes)) return COOP_E_ARG;
+  bool ok = true;
+  with_dtype(dtype, [&](auto t) {
+    constexpr int T = decltype(t)::value;
+    const Forward<T, true> fin{(const char*)gate_bias, (const char*)up_bias, nullptr, pre_out, pre_out ? pre_out + n * f : nullptr, (char*)out, n, f, 1.f, act};
+    ok = forward_all<T, true>(p, x, gate, up, fin, (char*)workspace, (hipStream_t)stream);
+  });
+  return ok && hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
+}
+
+extern "C" size_t coop_gated_grad_workspace_bytes(int64_t n, int32_t k, int32_t f, int dtype, int has_pre, int aligned) {
+  if (dense_check(n, k, f, dtype, COOP_ACT_NONE) != COOP_OK) return 0;
+  return DensePlan(n, k, f, dtype, true, aligned != 0, true, has_pre != 0, COOP_ACT_NONE).bytes;
+}
+
+extern "C" int coop_gated_grad(const void* dout, const void* x, int64_t n, int32_t k, const void* gate, const void* up, int32_t f, int dtype,
+                               const void* gate_bias, const void* up_bias, int act, const float* pre, void* dx, void* dgate, void* dup, int grad_dtype,
+                               float* dgate_bias, float* dup_bias, void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = dense_check(n, k, f, dtype, act);
+  if (rc != COOP_OK) return rc;
+  if (grad_dtype != COOP_F32 && grad_dtype != dtype) return COOP_E_ARG;
+  if ((dgate == nullptr) != (dup == nullptr) || (dgate_bias == nullptr) != (dup_bias == nullptr)) return COOP_E_ARG;
+  if ((!dx || n == 0) && !dgate && !dgate_bias) return COOP_OK;
+  if ((n > 0 && (!dout || !x || !gate || !up)) || !workspace) return COOP_E_NULL;
+  for (const void* p : {dout, x, gate, up, gate_bias, up_bias, (const void*)dx})
+    if (!aligned_for(p, dtype)) return COOP_E_ARG;
+  if (!aligned_for(dgate, grad_dtype) || !aligned_for(dup, grad_dtype)) return COOP_E_ARG;
+  if ((((uintptr_t)pre | (uintptr_t)dgate_bias | (uintptr_t)dup_bias) & 3) != 0) return COOP_E_ARG;
+  const DensePlan p(n, k, f, dtype, true, aligned16(x, gate, up), true, pre != nullptr, act);
+  if (!p.fit(true) || !workspace_ok(workspace, workspace_bytes, p.bytes)) return COOP_E_ARG;
+  if (n == 0) {
+    const int64_t bytes = (int64_t)f * k * element_bytes(grad_dtype);
+    const int rc2 = empty_sums(dgate, bytes, dup, bytes, (hipStream_t)stream);
+    return rc2 != COOP_OK ? rc2 : empty_sums(dgate_bias, (int64_t)f * 4, dup_bias, (int64_t)f * 4, (hipStream_t)stream);
+  }
+  bool ok = true;
+  with_dtype(dtype, [&](auto t) {
+    constexpr int T = decltype(t)::value;
+    ok = backward_all<T, true>(p, dout, x, gate, up, gate_bias, up_bias, pre, act, 1.f, dx, dgate, dup, grad_dtype, dgate_bias, dup_bias,
+                               (char*)workspace, (hipStream_t)stream);
+  });
+  return ok && hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
+}

@@ -39,14 +39,17 @@ __device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
 struct Operand {
   const char* base;
   int64_t ld, rows, k;
+  int64_t other = 0;  // of a pair: bytes from this one to the other
 };
 
 // How a stage of R rows of an operand lies in LDS, in 16-byte slots filled in order by the loads, 64 to a wave's load.
 //   k contiguous: a row's 4 or 8 chunks, exchanged by the row's number so that what 8 or 16 lanes read together lies in different banks;
 //   k strided: a row of k holds R elements; its chunks are exchanged by k so that what one fragment reads lies in different banks.
 // Both exchanges are an exclusive or with bits that neither the next tile of 32 rows nor the next step of k changes.
-template <int T, int R, bool STRIDED, int SIZE, int WAVES>
+// PAIR: the rows are those of two operands of one shape, 32 of the one and the same 32 of the other in turn; rows are counted in either.
+template <int T, int R, bool STRIDED, int SIZE, int WAVES, bool PAIR = false>
 struct Staged {
+  static_assert(!PAIR || (!STRIDED && R % 64 == 0 && 64 * 16 * WAVES == 32 * SIZE), "a load of all waves has 32 rows of one of the two");
   static constexpr int kBytes = R * SIZE, kK = SIZE / kElem<T>;
   static constexpr int kChunks = STRIDED ? R * kElem<T> / 16 : SIZE / 16;  // of a row
   static constexpr int kAll = kBytes / 1024;                                      // loads of a stage
@@ -60,11 +63,13 @@ struct Staged {
   // A stage that is to be loaded: where it begins in memory, how many of the memory layout's rows there are, and bytes in each.
   struct Place {
     const char* p;
+    int64_t other;  // PAIR: from one operand to the other
     int there, in_row;
     __device__ __forceinline__ Place() {}
     __device__ __forceinline__ Place(const Operand& op, int64_t row0, int64_t k0) {
       const int64_t most = 0x7FFFFFFF, rows = STRIDED ? op.k - k0 : op.rows - row0, bytes = STRIDED ? op.rows - row0 * kElem<T> : op.k - k0 * kElem<T>;
       p = op.base + (STRIDED ? k0 * op.ld + row0 * kElem<T> : row0 * op.ld + k0 * kElem<T>);
+      other = PAIR ? op.other : 0;
       there = (int)(rows < 0 ? 0 : rows < most ? rows : most);
       in_row = (int)(bytes < 0 ? 0 : bytes < most ? bytes : most);
     }
@@ -85,26 +90,31 @@ struct Staged {
       for (int i = 0; i < kMine; ++i) {
         const int slot = (i * WAVES + wave) * kWave + lane, row = slot / kChunks;
         chunk = ((slot % kChunks) ^ swizzle(row)) * 16;  // (k contiguous: the same for all of a lane's loads)
-        at[i] = row * ld + chunk;
+        at[i] = (PAIR ? (row >> 6) * 32 + (row & 31) : row) * ld + chunk;
         if (STRIDED && chunk >= first.in_row) at[i] = kNowhere;
       }
     }
     // what the loads of a stage have in common
     struct Stage {
-      __amdgpu_buffer_rsrc_t rsrc;
+      __amdgpu_buffer_rsrc_t rsrc, rsrc2;
       int off;
     };
     __device__ __forceinline__ Stage stage(const Place& s) const {
-      constexpr int kRows = STRIDED ? kK : R;
+      constexpr int kRows = STRIDED ? kK : PAIR ? R / 2 : R;
       const int rows = s.there < kRows ? s.there : kRows, in_row = s.in_row < ld ? s.in_row : ld, last = (rows - 1) * ld + in_row;
       const int records = (rows < in_row ? rows : in_row) > 0 ? last : 0;
-      return Stage{__builtin_amdgcn_make_buffer_rsrc((void*)s.p, 0, records, 0x00020000), !STRIDED && chunk >= s.in_row ? kNowhere : 0};
+      return Stage{__builtin_amdgcn_make_buffer_rsrc((void*)s.p, 0, records, 0x00020000),
+                   __builtin_amdgcn_make_buffer_rsrc((void*)(s.p + (PAIR ? s.other : 0)), 0, records, 0x00020000), !STRIDED && chunk >= s.in_row ? kNowhere : 0};
     }
     __device__ __forceinline__ void start(const Stage& s, char* lds, int i) const {
       const int l = i * WAVES + uniform_wave_in_block();
       if (kAll < WAVES && l >= kAll) return;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(s.rsrc, (__attribute__((address_space(3))) void*)(LdsByte*)(lds + l * 1024), 16,
-                                               STRIDED ? at[i] : at[i] + s.off, 0, 0, 0);
+      const int at_lds = l * 1024, from = STRIDED ? at[i] : at[i] + s.off;
+      if (PAIR && (i & 1) != 0) {  // (a load has rows of one of the two, and all waves of the same)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(s.rsrc2, (__attribute__((address_space(3))) void*)(LdsByte*)(lds + at_lds), 16, from, 0, 0, 0);
+        return;
+      }
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(s.rsrc, (__attribute__((address_space(3))) void*)(LdsByte*)(lds + at_lds), 16, from, 0, 0, 0);
     }
   };
   // the fragment of rows row .. row + 31 at step kk of the stage
@@ -142,12 +152,12 @@ struct Staged {
 
 // A block's tile of C: WA x WB waves with TA x TB tiles of 32 x 32 each, rows of A by rows of B.  The stages of all of a block's tiles
 // are one stream: while one is multiplied the next kStages - 1 are on their way, the first of the next tile among them.
-template <int T, int WA, int WB, int TA, int TB, bool SA, bool SB, int SIZE>
+template <int T, int WA, int WB, int TA, int TB, bool SA, bool SB, int SIZE, bool PAIR = false>
 struct Product {
   static constexpr int kWaves = WA * WB, kThreads = kWaves * kWave;
   static constexpr int kRowsA = WA * TA * 32, kRowsB = WB * TB * 32;
   static constexpr int kK = SIZE / kElem<T>, kSteps = SIZE / 32, kStages = 256 / SIZE;
-  typedef Staged<T, kRowsA, SA, SIZE, kWaves> A;
+  typedef Staged<T, kRowsA, SA, SIZE, kWaves, PAIR> A;
   typedef Staged<T, kRowsB, SB, SIZE, kWaves> B;
   static constexpr int kStage = A::kBytes + B::kBytes, kLds = kStages * kStage;
   f32x16 acc[TA][TB];
@@ -265,6 +275,24 @@ struct Product {
     next_a.p += step_bytes;
     next_a.there -= step;
     if (step == 0) next_a.there = next_b.there = 0;  // (behind the only tile there is nothing to load)
+    start_stream();
+  }
+  // The same for one tile whose k has two parts, of operands of their own and as long as each other: tile() twice.
+  __device__ __forceinline__ void begin_two(const Operand& op_a, const Operand& op_b, const Operand& then_a, const Operand& then_b, int64_t row_a,
+                                            int64_t row_b, int64_t k0, int64_t k1, char* lds_) {
+    lds = lds_;
+    step_rows = 1 << 30;  // (more than there are: behind the second part there is nothing to load)
+    step_bytes = 0;
+    left = stages = (int)((k1 - k0 + kK - 1) / kK);
+    a = typename A::Place(op_a, row_a, k0);
+    b = typename B::Place(op_b, row_b, k0);
+    loads_a.begin(op_a, a);
+    loads_b.begin(op_b, b);
+    next_a = typename A::Place(then_a, row_a, k0);
+    next_b = typename B::Place(then_b, row_b, k0);
+    start_stream();
+  }
+  __device__ __forceinline__ void start_stream() {
     slot = kStages - 1;
     sa = loads_a.stage(a);
     sb = loads_b.stage(b);
