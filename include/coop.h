@@ -501,6 +501,65 @@ int coop_gated_grad(const void* dout, const void* x, int64_t n, int32_t k, const
                     const void* gate_bias, const void* up_bias, int act, const float* pre, void* dx, void* dgate, void* dup, int grad_dtype,
                     float* dgate_bias, float* dup_bias, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * The seam between two blocks of a residual model: with N the norm of coop_layer_norm, or with COOP_NORM_RMS the same without a mean,
+ *   r = alpha x + gate N_after(f),   y = N_before(r)    (of r in 32 bits, before it is rounded to the stream's type).
+ *   x, r_out   device [n_rows, dim] of stream_dtype (COOP_F32 or dtype): the residual stream in front and behind; may be the same array
+ *   f, y_out   device [n_rows, dim] of dtype: a block's output, the next block's input; may be the same array; dim <= 8192 (COOP_F32) or 16384
+ *   gate       COOP_GATE_COLUMNS: device [dim] of weight_dtype; COOP_GATE_ELEMENTS: device [n_rows, dim] of dtype; COOP_GATE_NONE: NULL, 1
+ *   norms      COOP_NORM_AFTER, COOP_NORM_BEFORE or both, and COOP_NORM_RMS for either; without the first N_after(f) is f, without the second
+ *              there is no y_out (it may be NULL)
+ *   weights and biases  device [dim] of weight_dtype (COOP_F32 or dtype), or NULL: 1 and 0; no bias with COOP_NORM_RMS
+ *   stats_out  device float [4, n_rows]: mean and rstd of N_after, mean and rstd of N_before, for the gradient call
+ */
+#define COOP_NORM_AFTER 1
+#define COOP_NORM_BEFORE 2
+#define COOP_NORM_RMS 4
+#define COOP_GATE_NONE 0
+#define COOP_GATE_COLUMNS 1
+#define COOP_GATE_ELEMENTS 2
+int coop_residual_norm(const void* x, const void* f, int64_t n_rows, int32_t dim, int dtype, int stream_dtype, const void* gate,
+                       int gate_form, float alpha, int norms, const void* after_weight, const void* after_bias, const void* before_weight,
+                       const void* before_bias, int weight_dtype, float eps, void* r_out, void* y_out, float* stats_out, void* stream);
+
+/*
+ * Its gradient, for dr (of r, along the stream; NULL: zeros, only with COOP_NORM_BEFORE) and dy (of y; not read without COOP_NORM_BEFORE).
+ *   x, f      as they were given (x is not read without COOP_NORM_BEFORE); stats as they came
+ *   dx        device [n_rows, dim] of stream_dtype (may be dr), df of dtype (may be dy)
+ *   dgate     COOP_GATE_COLUMNS: device float [dim]; COOP_GATE_ELEMENTS: device [n_rows, dim] of dtype; COOP_GATE_NONE: NULL
+ *   dafter_weight, dafter_bias, dbefore_weight, dbefore_bias  device float [dim]; each may be NULL, and is without its norm, or its bias
+ *             with COOP_NORM_RMS
+ *   workspace at least coop_residual_norm_grad_workspace_bytes(n_rows, dim, dtype) bytes (NULL where none of these is asked for and the
+ *             gate is not the columns')
+ */
+size_t coop_residual_norm_grad_workspace_bytes(int64_t n_rows, int32_t dim, int dtype);
+int coop_residual_norm_grad(const void* dr, const void* dy, const void* x, const void* f, int64_t n_rows, int32_t dim, int dtype,
+                            int stream_dtype, const float* stats, const void* gate, int gate_form, float alpha, int norms,
+                            const void* after_weight, const void* after_bias, const void* before_weight, int weight_dtype, void* dx, void* df,
+                            void* dgate, float* dafter_weight, float* dafter_bias, float* dbefore_weight, float* dbefore_bias, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/*
+ * The norm of many gradients together, and the factor that clips them: norm = |s| sqrt(sum of g^2) with s = *grad_scale (1 where it is
+ * NULL), factor = s min(1, max_norm / (norm + 1e-6)).  coop_adamw takes the factor as its grad_scale; coop_grad_scale multiplies the
+ * gradients by it where they lie.  Squares are added up in 64 bits.  A gradient that is not finite makes the norm so, and the factor 0
+ * (infinities) or no number.
+ */
+typedef struct {
+  void* grad;                /* device, n_rows rows of dim elements (a tensor without rows: one row) */
+  const int32_t* n_rows_dev; /* device, or NULL: only the first *n_rows_dev rows are there (coop_embed_grad_rows) */
+  int64_t n_rows, dim;       /* at most 2^38 elements */
+  int32_t dtype, reserved;
+} coop_grad_tensor;
+/*   tensors    host, read before the call returns
+ *   norm_out, factor_out  device float, either may be NULL
+ *   workspace  at least coop_grad_norm_workspace_bytes(tensors, n) bytes */
+size_t coop_grad_norm_workspace_bytes(const coop_grad_tensor* tensors, int n);
+int coop_grad_norm(const coop_grad_tensor* tensors, int n, double max_norm, const float* grad_scale, float* norm_out, float* factor_out,
+                   void* workspace, size_t workspace_bytes, void* stream);
+/* g <- g * *factor, rounded to the gradient's type; nothing is written where the factor is 1 */
+int coop_grad_scale(const coop_grad_tensor* tensors, int n, const float* factor, void* stream);
+
 /* Name of an error code (static string). */
 const char* coop_strerror(int code);
 

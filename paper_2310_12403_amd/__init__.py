@@ -12,4 +12,5 @@ from .learn import (  # noqa: F401
     COOP_BF16, COOP_NO_PAD, AdamW, coop_embed, coop_embed_grad, coop_embed_grad_rows, coop_layer_norm, coop_layer_norm_grad,
     coop_softmax_xent, coop_softmax_xent_grad)
 from .layers import (  # noqa: F401
-    COOP_ACT_GELU, COOP_ACT_NONE, COOP_ACT_RELU, COOP_ACT_SILU, coop_gated, coop_gated_grad, coop_linear, coop_linear_grad)
+    COOP_ACT_GELU, COOP_ACT_NONE, COOP_ACT_RELU, COOP_ACT_SILU, GradNorm, coop_gated, coop_gated_grad, coop_linear, coop_linear_grad, coop_residual_norm,
+    coop_residual_norm_grad)

@@ -12,6 +12,12 @@ from .binding import _check, _stream_ptr
 from .learn import _DTYPES, _matrix, _new, _vector, _workspace
 
 COOP_ACT_NONE, COOP_ACT_RELU, COOP_ACT_GELU, COOP_ACT_SILU = 0, 1, 2, 3
+_AFTER, _BEFORE, _RMS = 1, 2, 4
+
+
+class _CGradTensor(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("n_rows_dev", C.c_void_p), ("n_rows", C.c_int64), ("dim", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
 
 _P, _I, _L, _F, _S = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_size_t
 _SIGNATURES = {
@@ -23,6 +29,12 @@ _SIGNATURES = {
     "coop_gated": (C.c_int, [_P, _L, _I, _P, _P, _I, C.c_int, _P, _P, C.c_int, _P, _P, _P, _S, _P]),
     "coop_gated_grad_workspace_bytes": (_S, [_L, _I, _I, C.c_int, C.c_int, C.c_int]),
     "coop_gated_grad": (C.c_int, [_P, _P, _L, _I, _P, _P, _I, C.c_int, _P, _P, C.c_int, _P, _P, _P, _P, C.c_int, _P, _P, _P, _S, _P]),
+    "coop_residual_norm": (C.c_int, [_P, _P, _L, _I, C.c_int, C.c_int, _P, C.c_int, _F, C.c_int] + [_P] * 4 + [C.c_int, _F] + [_P] * 4),
+    "coop_residual_norm_grad_workspace_bytes": (_S, [_L, _I, C.c_int]),
+    "coop_residual_norm_grad": (C.c_int, [_P] * 4 + [_L, _I, C.c_int, C.c_int, _P, _P, C.c_int, _F, C.c_int] + [_P] * 3 + [C.c_int] + [_P] * 8 + [_S, _P]),
+    "coop_grad_norm_workspace_bytes": (_S, [_P, C.c_int]),
+    "coop_grad_norm": (C.c_int, [_P, C.c_int, C.c_double, _P, _P, _P, _P, _S, _P]),
+    "coop_grad_scale": (C.c_int, [_P, C.c_int, _P, _P]),
 }
 _lib = None
 
@@ -120,3 +132,93 @@ def coop_gated_grad(dout, x, gate, up, gate_bias=None, up_bias=None, pre=None, a
                                  _kept(pre, (2, n, f)), dx.data_ptr() if want_x else None, *(w.data_ptr() if want_weight else None for w in dw),
                                  _DTYPES[grad_dtype], *(b.data_ptr() if want_bias else None for b in db), sp, sb, _stream_ptr(stream)))
     return (dx, *dw, *db)
+
+
+def _seam(x, f, gate, after, after_weight, after_bias, before, before_weight, before_bias, rms):
+    """(shape, types, gate form, flags, addresses) that both calls have in common"""
+    fp, (n, dim) = _matrix(f, "f"), f.shape
+    weights = [after_weight, after_bias, before_weight, before_bias]
+    assert after or after_weight is None and after_bias is None, "without the norm behind the block it has no weights"
+    assert before or before_weight is None and before_bias is None, "without the norm in front of the next block it has no weights"
+    assert not rms or after_bias is None and before_bias is None, "a root-mean-square norm has no bias"
+    columns = gate is not None and gate.dim() == 1
+    weight_dtype = learn._weight_dtype(f, *weights, gate if columns else None)
+    gp = None if gate is None else _vector(gate, dim, gate.dtype, "gate") if columns else _same(gate, f, "gate", n, dim)
+    ps = [None if w is None else _vector(w, dim, w.dtype, "weight") for w in weights]
+    return fp, n, dim, weight_dtype, gp, 0 if gate is None else 1 if columns else 2, after * _AFTER | before * _BEFORE | rms * _RMS, ps
+
+
+def coop_residual_norm(x, f, gate=None, alpha=1.0, after=True, after_weight=None, after_bias=None, before=True, before_weight=None, before_bias=None,
+                       rms=False, eps=1e-5, out=None, stream=None):
+    """(r, y, stats): r = alpha x + gate N_after(f), the residual stream behind a block, and y = N_before(r), the next block's input (None with
+    before=False; after=False: f itself).  x [n, dim]: of f's type or fp32; gate: None, [dim] (of the weights' type) or [n, dim] (of f's); out: for r."""
+    fp, n, dim, weight_dtype, gp, form, norms, ps = _seam(x, f, gate, after, after_weight, after_bias, before, before_weight, before_bias, rms)
+    xp = _matrix(x, "x", n, dim)
+    assert x.dtype in (torch.float32, f.dtype), "x: fp32 or f's type"
+    if out is None:
+        out = _new((n, dim), x.dtype, x.device, stream)
+    op = _same(out, x, "out", n, dim)
+    y = _new((n, dim), f.dtype, x.device, stream) if before else None
+    stats = _new((4, n), torch.float32, x.device, stream)
+    _check(lib().coop_residual_norm(xp, fp, n, dim, _DTYPES[f.dtype], _DTYPES[x.dtype], gp, form, alpha, norms, *ps, weight_dtype, eps, op,
+                                    y.data_ptr() if before else None, stats.data_ptr(), _stream_ptr(stream)))
+    return out, y, stats
+
+
+def coop_residual_norm_grad(dr, dy, x, f, stats, gate=None, alpha=1.0, after=True, after_weight=None, after_bias=None, before=True, before_weight=None,
+                            rms=False, want_weight=True, workspace=None, stream=None):
+    """(dx, df, dgate, dafter_weight, dafter_bias, dbefore_weight, dbefore_bias) of coop_residual_norm, from the gradients of r (None: zeros)
+    and y; x, f as they were given, and what the gate and the norms had.  None for what there is not, and for the last four with
+    want_weight=False; those and the gradient of a gate [dim] are fp32."""
+    fp, n, dim, weight_dtype, gp, form, norms, ps = _seam(x, f, gate, after, after_weight, after_bias, before, before_weight, None, rms)
+    xp = _matrix(x, "x", n, dim)
+    assert x.dtype in (torch.float32, f.dtype), "x: fp32 or f's type"
+    rp = None if dr is None else _same(dr, x, "dr", n, dim)
+    yp = _same(dy, f, "dy", n, dim) if before else None
+    assert before or dr is not None, "without the norm in front of the next block r's gradient is all there is"
+    assert stats.is_cuda and stats.is_contiguous() and stats.dtype == torch.float32 and tuple(stats.shape) == (4, n), "stats: as coop_residual_norm gives them"
+    dx, df = _new((n, dim), x.dtype, x.device, stream), _new((n, dim), f.dtype, x.device, stream)
+    dgate = None if gate is None else _new(gate.shape, torch.float32 if form == 1 else f.dtype, x.device, stream)
+    there = (after, after and not rms, before, before and not rms)
+    grads = [_new(dim, torch.float32, x.device, stream) if want_weight and t else None for t in there]
+    need = lib().coop_residual_norm_grad_workspace_bytes(n, dim, _DTYPES[f.dtype]) if want_weight or form == 1 else 0
+    keep, wp, wb = _workspace(need, workspace, x.device, stream)
+    _check(lib().coop_residual_norm_grad(rp, yp, xp, fp, n, dim, _DTYPES[f.dtype], _DTYPES[x.dtype], stats.data_ptr(), gp, form, alpha, norms, *ps[:3],
+                                         weight_dtype, dx.data_ptr(), df.data_ptr(), None if gate is None else dgate.data_ptr(),
+                                         *(None if g is None else g.data_ptr() for g in grads), wp, wb, _stream_ptr(stream)))
+    return (dx, df, dgate, *grads)
+
+
+class GradNorm:
+    """The norm of many gradients together and the factor that clips it (coop_grad_norm), over the tensors that hold the gradients at every step
+    (set_grads replaces them).  A gradient of touched rows, as coop_embed_grad_rows returns it without waiting, is given as (gradients, count)."""
+
+    def __init__(self, grads):
+        self.set_grads(grads)
+
+    def set_grads(self, grads):
+        grads = [g if isinstance(g, (tuple, list)) else (g, None) for g in grads]
+        for g, count in grads:
+            assert g.is_cuda and g.is_contiguous() and g.dtype in _DTYPES and (count is None or g.dim() == 2)
+            assert count is None or _vector(count, 1, torch.int32, "count")
+        c = (_CGradTensor * max(len(grads), 1))()
+        for t, (g, count) in zip(c, grads):
+            t.grad, t.dtype = g.data_ptr(), _DTYPES[g.dtype]
+            t.n_rows, t.dim = g.shape if count is not None else (1, g.numel())
+            t.n_rows_dev = None if count is None else count.data_ptr()
+        self.grads, self._c, self._n = grads, c, len(grads)
+        self._bytes = lib().coop_grad_norm_workspace_bytes(c, self._n)
+        self._device = grads[0][0].device if grads else torch.device("cuda")
+
+    def measure(self, max_norm=float("inf"), grad_scale=None, workspace=None, stream=None):
+        """(norm, factor), fp32 [1] on the device: norm = |s| sqrt(sum of g^2) with s = grad_scale (fp32 [1] on the device; None: 1) and
+        factor = s min(1, max_norm / (norm + 1e-6)): AdamW.step's grad_scale, or apply's factor."""
+        norm, factor = (_new(1, torch.float32, self._device, stream) for _ in range(2))
+        gs = None if grad_scale is None else _vector(grad_scale, 1, torch.float32, "grad_scale")
+        keep, wp, wb = _workspace(self._bytes, workspace, self._device, stream)
+        _check(lib().coop_grad_norm(self._c, self._n, max_norm, gs, norm.data_ptr(), factor.data_ptr(), wp, wb, _stream_ptr(stream)))
+        return norm, factor
+
+    def apply(self, factor, stream=None):
+        """The gradients times the factor (fp32 [1] on the device), where they lie."""
+        _check(lib().coop_grad_scale(self._c, self._n, _vector(factor, 1, torch.float32, "factor"), _stream_ptr(stream)))

@@ -182,3 +182,189 @@ def test_activations_over_their_range(act):
     finite = slice(0, -2)
     within(dx[finite], slope[finite], 40 * U)
     assert math.isnan(dx[-1]) == (act != P.COOP_ACT_NONE)
+
+
+# ---- the seam between two blocks -------------------------------------------------------------------------------------------------
+class Norm64:
+    """A norm of the rows of v, which is known to `ev`, and how far 32 bits may be from what follows."""
+
+    def __init__(self, v, ev, w, b, rms, eps):
+        n = v.shape[1]
+        self.rms, self.n = rms, n
+        one = torch.ones(n, dtype=torch.float64, device=v.device)
+        self.w, self.b = one if w is None else w.double(), 0 * one if b is None else b.double()
+        size = v.abs().mean(1, keepdim=True)
+        mean = 0 * size if rms else v.mean(1, keepdim=True)
+        emean = 0 * size if rms else ev.mean(1, keepdim=True) + (n + 2) * U * (size + ev.mean(1, keepdim=True))
+        c = v - mean
+        ec = ev + emean + U * (c.abs() + ev + emean)
+        var = (c * c).mean(1, keepdim=True)
+        evar = (2 * c.abs() * ec + ec * ec).mean(1, keepdim=True) + (n + 4) * U * ((c.abs() + ec) ** 2).mean(1, keepdim=True)
+        self.rstd = 1 / (var + eps).sqrt()
+        # (1 / sqrt falls by at most this from what is `evar` lower, or eps)
+        low = (var - evar).clamp(min=0) + eps
+        self.erstd = (1 / low.sqrt() - 1 / (var + evar + eps).sqrt()) + 6 * U / low.sqrt()
+        self.h = c * self.rstd
+        self.eh = ec * (self.rstd + self.erstd) + c.abs() * self.erstd + 2 * U * (c.abs() + ec) * (self.rstd + self.erstd)
+        self.y = self.h * self.w + self.b
+        self.ey = self.eh * self.w.abs() + 4 * U * ((self.h.abs() + self.eh) * self.w.abs() + self.b.abs())
+        self.mean, self.emean = mean, emean
+
+    def back(self, d, ed):
+        """(gradient through the norm, how far 32 bits may be), for d that is known to ed"""
+        n, dw, edw = self.n, d * self.w, (ed + 2 * U * (d.abs() + ed)) * self.w.abs()
+        top = dw.abs() + edw
+        s1 = 0 if self.rms else dw.mean(1, keepdim=True)
+        es1 = 0 if self.rms else edw.mean(1, keepdim=True) + (n + 2) * U * top.mean(1, keepdim=True)
+        s2 = (dw * self.h).mean(1, keepdim=True)
+        es2 = (edw * (self.h.abs() + self.eh) + dw.abs() * self.eh).mean(1, keepdim=True) + (n + 4) * U * (top * (self.h.abs() + self.eh)).mean(1, keepdim=True)
+        inner = dw - s1 - self.h * s2
+        einner = edw + es1 + self.eh * (s2.abs() + es2) + self.h.abs() * es2
+        einner = einner + 4 * U * (top + (self.h.abs() + self.eh) * (s2.abs() + es2) + (0 if self.rms else s1.abs() + es1))
+        return inner * self.rstd, einner * (self.rstd + self.erstd) + inner.abs() * self.erstd + U * (inner.abs() + einner) * self.rstd
+
+
+SEAM_SIZES = [(0, 8), (1, 1), (3, 2), (5, 7), (1, 8), (65, 9), (700, 75), (33, 100), (257, 128), (3000, 96), (129, 511), (40, 513), (19, 1024), (21, 1031), (9, 2050),
+              (300, 4096), (11, 5000), (5, 8191)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,dim", SEAM_SIZES + [(3, 16384), (2, 9001)])
+def test_residual_norm(dtype, n, dim):
+    if dtype == torch.float32 and dim > 8192:
+        dim //= 2
+    g = rng(n + dim)
+    eps = 1e-3
+    for i, (norms, rms, gated) in enumerate([("both", False, "columns"), ("both", True, "rows"), ("after", False, "rows"), ("before", False, "columns"),
+                                             ("both", False, None), ("after", True, "columns"), ("before", True, "rows")]):
+        after, before = norms != "before", norms != "after"
+        stream, wt = (torch.float32, dtype)[(i + n) % 2], (torch.float32, dtype)[(i // 2 + dim) % 2]
+        place = unaligned if (i + dim) % 2 else (lambda t: t)
+        x, f = place(normal(g, n, dim, dtype=stream)), place((normal(g, n, dim) + normal(g, n, 1)).to(dtype))
+        gate = None if gated is None else place((0.5 + normal(g, *((dim,) if gated == "columns" else (n, dim)), scale=0.3)).to(wt if gated == "columns" else dtype))
+        w1, w2 = (place((1 + normal(g, dim, scale=0.3)).to(wt)) if there and i != 4 else None for there in (after, before))
+        b1, b2 = (place(normal(g, dim, scale=0.3).to(wt)) if there and not rms and i != 4 else None for there in (after, before))
+        dr, dy = place(normal(g, n, dim, dtype=stream)) if i != 4 else None, place(normal(g, n, dim, dtype=dtype))
+        alpha = 0.9 if i % 2 else 1.0
+        kw = dict(gate=gate, alpha=alpha, after=after, after_weight=w1, after_bias=b1, before=before, before_weight=w2, rms=rms)
+        r, y, stats = P.coop_residual_norm(x, f, before_bias=b2, eps=eps, **kw)
+        # forward
+        zero = torch.zeros((n, dim), dtype=torch.float64, device="cuda")
+        N1 = Norm64(f.double(), zero, w1, b1, rms, eps) if after else None
+        p, ep = (N1.y, N1.ey) if after else (f.double(), zero)
+        gg = torch.ones(dim, dtype=torch.float64, device="cuda") if gate is None else gate.double()
+        r64 = alpha * x.double() + gg * p
+        er = gg.abs() * ep + 4 * U * (alpha * x.double().abs() + gg.abs() * (p.abs() + ep))
+        within(r, r64, rounded(r64, er, stream), "r")
+        N2 = Norm64(r64, er, w2, b2, rms, eps) if before else None
+        if before:
+            within(y, N2.y, rounded(N2.y, N2.ey, dtype), "y")
+        else:
+            assert y is None
+        for k, N in ((0, N1), (2, N2)):
+            if N is not None:
+                within(stats[k], N.mean[:, 0], N.emean[:, 0], "mean")
+                within(stats[k + 1], N.rstd[:, 0], N.erstd[:, 0], "rstd")
+        # backward
+        dx, df, dgate, dw1, db1, dw2, db2 = P.coop_residual_norm_grad(dr, dy if before else None, x, f, stats, **kw)
+        d, ed = (zero if dr is None else dr.double()), zero
+        if before:
+            back, eback = N2.back(dy.double(), zero)
+            d, ed = d + back, eback
+            ed = ed + U * (d.abs() + ed + (0 if dr is None else dr.double().abs()))
+        e, ee = d * gg, ed * gg.abs() + U * (d.abs() + ed) * gg.abs()
+        within(dx, alpha * d, rounded(alpha * d, alpha * ed + U * (d.abs() + ed), stream), "dx")
+        want, bound = N1.back(e, ee) if after else (e, ee)
+        within(df, want, rounded(want, bound, dtype), "df")
+
+        def sums(a, ea, b, eb, factor):     # of a b over the rows, times a factor of the column
+            terms, off = (a.abs() + ea) * (b.abs() + eb), ea * (b.abs() + eb) + a.abs() * eb
+            return (a * b).sum(0) * factor, (off.sum(0) + (n + 8) * U * terms.sum(0)) * abs(factor)
+
+        one = torch.ones_like(zero)
+        if gated == "rows":
+            assert dgate.dtype == dtype
+            within(dgate, d * p, rounded(d * p, ed * (p.abs() + ep) + d.abs() * ep + U * (d.abs() + ed) * (p.abs() + ep), dtype), "dgate")
+        elif gated == "columns":
+            if after:
+                (s1, e1), (s0, e0) = sums(d, ed, N1.h, N1.eh, N1.w), sums(d, ed, one, 0 * one, N1.b)
+                within(dgate, s1 + s0, e1 + e0 + 4 * U * (s1.abs() + s0.abs()), "dgate")
+            else:
+                within(dgate, *sums(d, ed, p, ep, 1.0), "dgate")
+        else:
+            assert dgate is None
+        if after:
+            per = gated == "rows"
+            within(dw1, *sums(e if per else d, ee if per else ed, N1.h, N1.eh, 1.0 if per else gg), "dw1")
+            if not rms:
+                within(db1, *sums(e if per else d, ee if per else ed, one, 0 * one, 1.0 if per else gg), "db1")
+        if before:
+            within(dw2, *sums(dy.double(), zero, N2.h, N2.eh, 1.0), "dw2")
+            if not rms:
+                within(db2, *sums(dy.double(), zero, one, 0 * one, 1.0), "db2")
+        assert (dw1 is None) == (not after) and (dw2 is None) == (not before) and (db1 is None) == (rms or not after) and (db2 is None) == (rms or not before)
+
+
+# ---- the gradients' norm ------------------------------------------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("sizes", [[1], [0], [], [7, 0, 16384, 16385, 3], [1000003], [5] * 1000, [40000, 1, 2, 300000]])
+def test_grad_norm(sizes):
+    g = rng(len(sizes))
+    grads = [unaligned(normal(g, k, dtype=TYPES[i % 3], scale=10.0 ** (i % 5 - 2))) for i, k in enumerate(sizes)]
+    plan = P.GradNorm(grads)
+    want = math.sqrt(sum(float((x.double() ** 2).sum()) for x in grads))
+    for scale in (None, torch.tensor([-0.25], device="cuda")):
+        s = 1.0 if scale is None else -0.25
+        for bound in (float("inf"), want * 0.1, 0.0):
+            norm, factor = plan.measure(bound, grad_scale=scale)
+            f = s * min(1.0, bound / (abs(s) * want + 1e-6))
+            # (64 bits throughout: what is off is the rounding of the result)
+            assert abs(float(norm) - abs(s) * want) <= 2 * U * abs(s) * want and abs(float(factor) - f) <= 2 * U * abs(f)
+    norm, factor = plan.measure(want * 0.5)
+    before = [x.clone() for x in grads]
+    plan.apply(factor)
+    for x, b in zip(grads, before):
+        assert torch.equal(x, (b.float() * factor).to(b.dtype))
+    plan.apply(torch.ones(1, device="cuda"))
+    for x, b in zip(grads, before):
+        assert torch.equal(x, (b.float() * factor).to(b.dtype))
+
+
+@gpu
+def test_grad_norm_of_extremes_and_of_what_is_not_finite():
+    for dtype, value in ((torch.float32, 3e38), (torch.float32, 1e-45), (torch.bfloat16, 3e38), (torch.bfloat16, 1e-40), (torch.float16, 65504.0), (torch.float16, 6e-8)):
+        x = torch.full((9,), value, device="cuda").to(dtype)
+        norm, factor = P.GradNorm([x]).measure(1.0)
+        want = 3 * float(x[0])
+        assert (math.isinf(float(norm)) if want > 3.4028236e38 else abs(float(norm) - want) <= 2 * U * want + 2.0 ** -150), (dtype, value)
+        assert abs(float(factor) - min(1.0, 1 / (want + 1e-6))) <= 2 * U + 2.0 ** -149
+    x = torch.ones(100, device="cuda")
+    x[57] = float("inf")
+    norm, factor = P.GradNorm([torch.ones(3, device="cuda"), x]).measure(1.0)
+    assert math.isinf(float(norm)) and float(factor) == 0.0
+    x[3] = float("nan")
+    norm, factor = P.GradNorm([x]).measure(1.0)
+    assert math.isnan(float(norm)) and math.isnan(float(factor))
+
+
+@gpu
+def test_grad_norm_of_touched_rows_and_the_step_that_it_scales():
+    """The rows that coop_embed_grad_rows gives, without waiting for their number: what lies behind them does not count and stays."""
+    g = rng(5)
+    ids = torch.randint(0, 40, (300,), generator=g, device="cuda", dtype=torch.int32)
+    dout, dense = normal(g, 300, 75), normal(g, 33, dtype=torch.bfloat16)
+    rows, grad, count = P.coop_embed_grad_rows(dout, ids, 50, wait=False)
+    k = int(count)
+    grad[k:] = 1e9
+    plan = P.GradNorm([(grad, count), dense])
+    norm, factor = plan.measure(1.0)
+    want = math.sqrt(float((grad[:k].double() ** 2).sum() + (dense.double() ** 2).sum()))
+    assert abs(float(norm) - want) <= 2 * U * want
+    tables = [normal(rng(6), 50, 75) for _ in range(2)]
+    opts = [P.AdamW([t], by_rows=True) for t in tables]
+    opts[0].step(1, 1e-2, rows={0: (rows, grad, count)}, grad_scale=factor)
+    plan.apply(factor)
+    assert float(grad[k:].min()) == float(torch.tensor(1e9)) and abs(float(P.GradNorm([(grad, count), dense]).measure()[0]) - 1.0) < 1e-2
+    opts[1].step(1, 1e-2, rows={0: (rows, grad, count)})
+    assert torch.equal(tables[0], tables[1])
