@@ -414,9 +414,9 @@ __global__ __launch_bounds__(kBlock) void k_dense_pad(Copies jobs, uint32_t bloc
 }
 
 // ---- how a call is cut ------------------------------------------------------------------------------------------------------------
-// A product of rows x cols over k.  Tiles of 256 x 256, what a wave's registers hold, where 16-bit operands have enough of them for the chip;
-// else of 128 x 128, two blocks on a CU.  k is split where there are fewer tiles than blocks that run at a time, as long as every part has four
-// stages.
+// A product of rows x cols over k, in tiles of 256 x 256, what a wave's registers hold, one block to a CU, or of 128 x 128, two blocks, which
+// take as long for half as much (LDS gives them only half of what the matrix units take): the former for 16-bit operands where that is fewer
+// rounds of the chip.  k is split where there are fewer tiles than blocks that run at a time, as long as every part has four stages.
 struct Cut {
   int64_t rows, cols, width;  // width: of a row of parts
   int tile;
@@ -426,7 +426,8 @@ struct Cut {
   Cut(int64_t rows_, int64_t cols_, int64_t k, int dtype, bool pair) : rows(rows_), cols(cols_) {
     const int per_tile = pair ? 2 : 1;
     const auto tiles_of = [&](int t) { return ((cols * per_tile + t - 1) / t) * ((rows + t - 1) / t); };
-    tile = dtype != COOP_F32 && tiles_of(256) >= 256 ? 256 : 128;
+    const auto rounds_of = [&](int t, int each) { return (tiles_of(t) + 256 * each - 1) / (256 * each); };
+    tile = dtype != COOP_F32 && tiles_of(256) >= 256 && rounds_of(256, 1) < rounds_of(128, 2) ? 256 : 128;
     tiles_a = (uint32_t)((cols * per_tile + tile - 1) / tile);
     tiles_b = (uint32_t)((rows + tile - 1) / tile);
     const int64_t stages = k * element_bytes(dtype) / kWide;
