@@ -1,5 +1,7 @@
 // Activations of the dense operators and their slopes, in 32 bits.
 #pragma once
+#include <type_traits>
+
 #include "device_utils.h"
 
 namespace coop {
@@ -56,6 +58,30 @@ __device__ __forceinline__ float act_slope(float z, int act, float* value) {
   }
   *value = z;
   return 1.f;
+}
+
+// The same of E values, in their places; which activation it is, is asked once.
+template <int E>
+__device__ __forceinline__ void act_values(float (&z)[E], int act) {
+  const auto all = [&](auto a) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) z[e] = act_value(z[e], decltype(a)::value);
+  };
+  if (act == COOP_ACT_GELU) all(std::integral_constant<int, COOP_ACT_GELU>());
+  else if (act == COOP_ACT_SILU) all(std::integral_constant<int, COOP_ACT_SILU>());
+  else if (act == COOP_ACT_RELU) all(std::integral_constant<int, COOP_ACT_RELU>());
+}
+// z: the slopes in its place; value: act(z)
+template <int E>
+__device__ __forceinline__ void act_slopes(float (&z)[E], float (&value)[E], int act) {
+  const auto all = [&](auto a) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) z[e] = act_slope(z[e], decltype(a)::value, &value[e]);
+  };
+  if (act == COOP_ACT_GELU) all(std::integral_constant<int, COOP_ACT_GELU>());
+  else if (act == COOP_ACT_SILU) all(std::integral_constant<int, COOP_ACT_SILU>());
+  else if (act == COOP_ACT_RELU) all(std::integral_constant<int, COOP_ACT_RELU>());
+  else all(std::integral_constant<int, COOP_ACT_NONE>());
 }
 
 }  // namespace coop

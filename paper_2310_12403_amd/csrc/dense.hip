@@ -104,8 +104,9 @@ struct Forward {
       if (PAIR) store_columns<COOP_F32, E>(pre2 + at, l.col, cols, u);
     }
     if (out == nullptr) return;  // (computed again, for its gradient)
+    act_values(v, act);
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = PAIR ? act_value(v[e], act) * u[e] : act_value(v[e], act) * alpha;
+    for (int e = 0; e < E; ++e) v[e] *= PAIR ? u[e] : alpha;
     if (!PAIR && residual != nullptr) {
       float r[E];
       load_columns<T, E>(residual + at * kElem<T>, l.col, cols, r);
@@ -141,23 +142,22 @@ struct Slope {
     if (bias != nullptr) load_columns<T, E>(bias, col, cols, l.b);
     if (PAIR && bias2 != nullptr) load_columns<T, E>(bias2, col, cols, l.b2);
   }
-  // v, u: the products' sums with their biases (behind the last column: anything)
+  // v, u: the products' sums with their biases (behind the last column: anything); they are lost
   template <int E>
-  __device__ __forceinline__ void slope(Lane<E>& l, int64_t row, const float (&v)[E], const float (&u)[E]) const {
-    float d[E], d2[E];
+  __device__ __forceinline__ void slope(Lane<E>& l, int64_t row, float (&v)[E], const float (&u)[E]) const {
+    float d[E], d2[E], value[E];
     load_columns<T, E>(dout + row * cols * kElem<T>, l.col, cols, d);
+    act_slopes(v, value, act);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const bool there = l.col + e < cols;
-      float value;
-      const float s = act_slope(v[e], act, &value);
       if (PAIR) {
-        d2[e] = there ? d[e] * value : 0.f;
-        d[e] = there ? d[e] * u[e] * s : 0.f;
+        d2[e] = there ? d[e] * value[e] : 0.f;
+        d[e] = there ? d[e] * u[e] * v[e] : 0.f;
         l.s2[e] += d2[e];
         l.s[e] += d[e];
       } else {  // (without an activation the factor is the results', and dz the gradient as it came)
-        const float scaled = there ? d[e] * alpha * s : 0.f;
+        const float scaled = there ? d[e] * alpha * v[e] : 0.f;
         if (act != COOP_ACT_NONE) d[e] = scaled;
         l.s[e] += scaled;
       }
@@ -308,29 +308,54 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
   if constexpr (Fin::kSums) fin.end(at, kLanes, (int64_t)mine.b * WB + uniform_wave_in_block() % WB);
 }
 
-// The splits' parts added up in their order, and the epilogue.  A thread has E columns of a row.
+// The splits' parts added up, and the epilogue.  A wave has 64 packs of four columns; where there are many splits the block's waves deal those of
+// the same packs among themselves (`share` of them), and the first adds up what they have, in their order.  (512 splits of 128 x 128 by one wave
+// each: 41 us.)
+constexpr int kSumWaves = 16;
 template <int T, bool PAIR, typename Fin>
-__global__ __launch_bounds__(kBlock) void k_dense_join(const float* __restrict__ sums, int splits, int64_t rows, int64_t width, int32_t cols, Fin fin) {
-  constexpr int E = 4;
+__global__ __launch_bounds__(kSumWaves* kWave) void k_dense_join(const float* __restrict__ sums, int splits, int share, int64_t rows, int64_t width, int32_t cols,
+                                                                 Fin fin) {
+  constexpr int E = 4, kValues = PAIR ? 2 * E : E;
+  __shared__ float lds[kValues][kSumWaves][kWave];
   const int32_t packs = (cols + E - 1) / E;
   const int64_t half = PAIR ? width / 2 : 0;
-  for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < rows * packs; i += (int64_t)gridDim.x * kBlock) {
-    const int64_t row = i / packs;
+  const int wave = uniform_wave_in_block(), lane = lane_id(), mine = wave % share, each = kSumWaves / share * kWave;
+  for (int64_t first = (int64_t)blockIdx.x * each; first < rows * packs; first += (int64_t)gridDim.x * each) {
+    const int64_t i = first + wave / share * kWave + lane, row = i / packs;
     const int32_t c = (int32_t)(i - row * packs) * E;
+    const bool live = row < rows;
     float v[E] = {0.f, 0.f, 0.f, 0.f}, u[E] = {0.f, 0.f, 0.f, 0.f};
-    const float* from = sums + row * width + c;
-#pragma unroll 4
-    for (int q = 0; q < splits; ++q, from += rows * width) {
-      float f[E];
-      load_elements<COOP_F32, E>(from, f);
+    if (live) {
+      const float* from = sums + (mine * rows + row) * width + c;
+#pragma unroll 8
+      for (int q = mine; q < splits; q += share, from += share * rows * width) {
+        float f[E];
+        load_elements<COOP_F32, E>(from, f);
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] += f[e];
-      if constexpr (PAIR) {
-        load_elements<COOP_F32, E>(from + half, f);
+        for (int e = 0; e < E; ++e) v[e] += f[e];
+        if constexpr (PAIR) {
+          load_elements<COOP_F32, E>(from + half, f);
 #pragma unroll
-        for (int e = 0; e < E; ++e) u[e] += f[e];
+          for (int e = 0; e < E; ++e) u[e] += f[e];
+        }
       }
     }
+    if (share > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        lds[e][wave][lane] = v[e];
+        if constexpr (PAIR) lds[E + e][wave][lane] = u[e];
+      }
+      __syncthreads();
+    }
+    if (mine != 0 || !live) continue;
+    for (int w = 1; w < share; ++w)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        v[e] += lds[e][wave + w][lane];
+        if constexpr (PAIR) u[e] += lds[E + e][wave + w][lane];
+      }
     typename Fin::template Lane<E> at;
     fin.begin(at, c);
     fin.put(at, row, v, u);
@@ -413,6 +438,8 @@ __global__ __launch_bounds__(kBlock) void k_dense_pad(Copies jobs, uint32_t bloc
   }
 }
 
+#include "dense_narrow.h"
+
 // ---- how a call is cut ------------------------------------------------------------------------------------------------------------
 // A product of rows x cols over k, in tiles of 256 x 256, what a wave's registers hold, one block to a CU, or of 128 x 128, two blocks, which
 // take as long for half as much (LDS gives them only half of what the matrix units take): the former for 16-bit operands where that is fewer
@@ -440,11 +467,32 @@ struct Cut {
 
 bool fits(const Cut& c) { return c.blocks() < ((uint64_t)1 << 31); }
 
+// f(KS, MT) for the steps of 16 of k and the tiles of 32 of m
+template <typename F>
+void with_narrow(int64_t k, int64_t m, F&& f) {
+  const auto mt = [&](auto ks) {
+    if (m <= 32) f(ks, std::integral_constant<int, 1>());
+    else if (m <= 64) f(ks, std::integral_constant<int, 2>());
+    else f(ks, std::integral_constant<int, 4>());
+  };
+  if (k <= 32) mt(std::integral_constant<int, 2>());
+  else if (k <= 64) mt(std::integral_constant<int, 4>());
+  else mt(std::integral_constant<int, 8>());
+}
+
+int narrow_shares(int64_t k, int64_t m) {
+  int shares = 1;
+  with_narrow(k, m, [&](auto ks, auto mt) { shares = NarrowBackward<COOP_BF16, decltype(ks)::value, decltype(mt)::value>::kShares; });
+  return shares;
+}
+
 // The parts of a call, and where in the workspace they are.  GATED: two weights of m rows.
 struct DensePlan {
   int64_t n, k, m, kw, mw;  // kw, mw: elements of a row of k or m, up to a multiple of 16 bytes
   int64_t dz_ld;            // elements; a pair's second part begins at mw
   bool gated, pad, slope, again;  // slope: dz is not dout itself; again: the forward product is computed again
+  bool narrow;                    // 8 to 128 by 8 to 128 in 16 bits: the kernels of dense_narrow.h (but not from what was kept)
+  uint32_t narrow_tiles, narrow_blocks;
   Cut forward, back, weight;      // (dx and dW)
   int64_t sum_rows;               // of the columns' partial sums
   int lanes_log2;
@@ -454,17 +502,22 @@ struct DensePlan {
     const int es = element_bytes(dtype), e = 16 / es;
     kw = round_up(k, e);
     mw = round_up(m, e);
-    pad = !aligned || kw != k;
+    narrow = es == 2 && !gated && k >= 8 && k <= 128 && m >= 8 && m <= 128 && !(grad && keeps && act != COOP_ACT_NONE);
+    narrow_tiles = (uint32_t)((n + 31) / 32);
+    narrow_blocks = (uint32_t)at_most((narrow_tiles + 7) / 8, 256);
+    pad = !narrow && (!aligned || kw != k);
     size_t at = 0;
     auto take = [&](size_t b) { const size_t o = at; at += (b + 255) & ~(size_t)255; return o; };
     x = take(pad ? (size_t)n * kw * es : 0);
     w = take(pad ? (size_t)m * kw * es : 0);
     w2 = take(pad && gated ? (size_t)m * kw * es : 0);
     forward = Cut(n, m, kw, dtype, gated);
-    size_t parts = forward.part_bytes;
+    size_t parts = narrow ? 0 : forward.part_bytes;
     dz = pre = part = part2 = join = 0;
     slope = again = false;
-    if (grad) {
+    if (grad && narrow) {
+      parts = (size_t)narrow_blocks * (size_t)narrow_shares(k, m) * (size_t)m * (size_t)(round_up(k, 8) + kNarrowSums) * 4;
+    } else if (grad) {
       again = !keeps && (gated || act != COOP_ACT_NONE);
       slope = gated || act != COOP_ACT_NONE || !aligned || mw != m;
       dz_ld = gated ? 2 * mw : mw;
@@ -517,16 +570,20 @@ bool launch_product(int id, const Cut& c, const Operand& a, const Operand& a2, c
   return launch_tiles<T, 2, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, fin, s);
 }
 
+template <int T, bool PAIR, typename Fin>
+void join(const float* sums, int splits, int64_t rows, int64_t width, int32_t cols, const Fin& fin, hipStream_t s) {
+  const int share = splits >= kSumWaves ? kSumWaves : 1, each = kSumWaves / share * kWave;
+  const int64_t blocks = (rows * ((cols + 3) / 4) + each - 1) / each;
+  COOP_LAUNCH(K_DENSE_JOIN, (k_dense_join<T, PAIR, Fin>), dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(kSumWaves * kWave), 0, s, sums, splits, share,
+              rows, width, cols, fin);
+}
+
 // A product and its epilogue, through parts where k is split.
 template <int T, bool SA, bool SB, int SIZE, int FORM, typename Fin>
 bool product(int id, const Cut& c, const Operand& a, const Operand& a2, const Operand& b, const Operand& b2, int64_t k, const Fin& fin, float* sums, hipStream_t s) {
   if (c.splits == 1) return launch_product<T, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, fin, s);
   if (!launch_product<T, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, Part<FORM == kPair>{sums, c.rows, c.width, 0}, s)) return false;
-  if constexpr (!Fin::kSums) {
-    const int64_t blocks = (c.rows * ((c.cols + 3) / 4) + kBlock - 1) / kBlock;
-    COOP_LAUNCH(K_DENSE_JOIN, (k_dense_join<T, FORM == kPair, Fin>), dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(kBlock), 0, s, (const float*)sums,
-                (int)c.splits, c.rows, c.width, (int32_t)c.cols, fin);
-  }
+  if constexpr (!Fin::kSums) join<T, FORM == kPair>(sums, (int)c.splits, c.rows, c.width, (int32_t)c.cols, fin, s);
   return true;
 }
 
@@ -560,8 +617,64 @@ bool forward_product(const DensePlan& p, const Arrays& o, const Fin& fin, float*
   return product<T, false, false, kWide, PAIR ? kPair : kOne>(PAIR ? K_GATED : K_LINEAR, p.forward, a, a, b, b, p.kw, fin, sums, s);
 }
 
+template <int T>
+void sums_of_columns(const DensePlan& p, const float* from, const float* from2, float* db, float* db2, bool pair, char* ws, hipStream_t s) {
+  int64_t rows = p.sum_rows;
+  const unsigned x_blocks = (unsigned)((p.m + kWave - 1) / kWave), z = pair ? 2 : 1;
+  if (p.join_y > 1) {
+    float* to = (float*)(ws + p.join);
+    COOP_LAUNCH(K_DENSE_COLUMNS, k_dense_columns, dim3(x_blocks, p.join_y, z), dim3(kJoinWaves * kWave), 0, s, from, from2, rows, (int32_t)p.m, to,
+                to + p.join_y * p.m);
+    from = to, from2 = to + p.join_y * p.m, rows = p.join_y;
+  }
+  COOP_LAUNCH(K_DENSE_COLUMNS, k_dense_columns, dim3(x_blocks, 1, z), dim3(kJoinWaves * kWave), 0, s, from, from2, rows, (int32_t)p.m, db, db2);
+}
+
+// a row of the narrow gradient's parts: dW's columns, and behind them the bias's
+struct NarrowGradient {
+  Gradient g;
+  float* db;
+  int32_t db_col;
+  template <int E> using Lane = typename Gradient::Lane<E>;
+  template <int E>
+  __device__ __forceinline__ void begin(Lane<E>& l, int32_t col) const { l.col = col; }
+  template <int E>
+  __device__ __forceinline__ void put(Lane<E>& l, int64_t row, float (&v)[E], float (&u)[E]) const {
+    if (l.col < db_col) g.put(l, row, v, u);
+    else if (db != nullptr) db[row] = v[0];
+  }
+};
+
+template <int T>
+bool backward_narrow(const DensePlan& p, const NarrowLayer& l, const void* dout, void* dx, void* dw, int grad_dtype, float* db, char* ws, hipStream_t s) {
+  bool ok = true;
+  float* const sums = dw != nullptr || db != nullptr ? (float*)(ws + p.sums) : nullptr;
+  const int32_t db_col = dw != nullptr ? (int32_t)round_up(p.k, 8) : 0, width = db_col + kNarrowSums;
+  with_narrow(p.k, p.m, [&](auto ks, auto mt) {
+    constexpr int KS = decltype(ks)::value, MT = decltype(mt)::value, lds = NarrowBackward<T, KS, MT>::kLds;
+    const auto kernel = p.k == KS * 16 && p.m == MT * 32 ? k_narrow_grad<T, KS, MT, true> : k_narrow_grad<T, KS, MT, false>;
+    ok = allow_lds(kernel, lds);
+    if (ok) COOP_LAUNCH(K_DENSE_DX, kernel, dim3(p.narrow_blocks), dim3(512), lds, s, l, (const char*)dout, (char*)dx, sums, width, p.narrow_tiles);
+  });
+  if (!ok || sums == nullptr) return ok;
+  const Gradient g{(char*)dw, nullptr, p.m, 0, (int32_t)p.k, l.act == COOP_ACT_NONE ? l.alpha : 1.f, grad_dtype};
+  join<T, false>(sums, (int)p.narrow_blocks * narrow_shares(p.k, p.m), p.m, width, db_col + 1, NarrowGradient{g, db, db_col}, s);
+  return true;
+}
+
 template <int T, bool PAIR>
 bool forward_all(const DensePlan& p, const void* x, const void* w, const void* w2, const Forward<T, PAIR>& fin, char* ws, hipStream_t s) {
+  if constexpr (T != COOP_F32 && !PAIR)
+    if (p.narrow) {
+      const NarrowLayer l{(const char*)x, (const char*)w, fin.bias, p.n, (int32_t)p.k, (int32_t)p.m, fin.alpha, fin.act};
+      with_narrow(p.k, p.m, [&](auto ks, auto mt) {
+        constexpr int KS = decltype(ks)::value, MT = decltype(mt)::value;
+        const auto kernel = p.k == KS * 16 && p.m == MT * 32 ? k_narrow<T, KS, MT, true> : k_narrow<T, KS, MT, false>;
+        COOP_LAUNCH(K_LINEAR, kernel, dim3(p.narrow_blocks), dim3(kNarrowForwardWaves * kWave), 0, s, l,
+                    fin.residual, fin.out, fin.pre, p.narrow_tiles);
+      });
+      return true;
+    }
   const Arrays o = operands<T>(p, x, w, w2, true, ws, s);
   return forward_product<T, PAIR>(p, o, fin, (float*)(ws + p.sums), s);
 }
@@ -569,6 +682,11 @@ bool forward_all(const DensePlan& p, const void* x, const void* w, const void* w
 template <int T, bool PAIR>
 bool backward_all(const DensePlan& p, const void* dout, const void* x, const void* w, const void* w2, const void* bias, const void* bias2, const float* pre,
                   int act, float alpha, void* dx, void* dw, void* dw2, int grad_dtype, float* db, float* db2, char* ws, hipStream_t s) {
+  if constexpr (T != COOP_F32 && !PAIR)
+    if (p.narrow) {
+      const NarrowLayer l{(const char*)x, (const char*)w, (const char*)bias, p.n, (int32_t)p.k, (int32_t)p.m, alpha, act};
+      return backward_narrow<T>(p, l, dout, dx, dw, grad_dtype, db, ws, s);
+    }
   const bool products = dx != nullptr || dw != nullptr;
   float* const sums = (float*)(ws + p.sums);
   Arrays o{(const char*)x, (const char*)w, (const char*)w2};
@@ -591,18 +709,7 @@ bool backward_all(const DensePlan& p, const void* dout, const void* x, const voi
     if (fin.dz != nullptr || fin.part != nullptr)
       COOP_LAUNCH(K_DENSE_SLOPE, (k_dense_slope<T, PAIR>), dim3(p.slope_x, p.slope_y), dim3(kBlock), 0, s, pre, PAIR ? pre + p.n * p.m : nullptr, p.lanes_log2, fin);
   }
-  if (fin.part != nullptr) {
-    const float *from = fin.part, *from2 = fin.part2;
-    int64_t rows = p.sum_rows;
-    const unsigned x_blocks = (unsigned)((p.m + kWave - 1) / kWave), z = PAIR ? 2 : 1;
-    if (p.join_y > 1) {
-      float* to = (float*)(ws + p.join);
-      COOP_LAUNCH(K_DENSE_COLUMNS, k_dense_columns, dim3(x_blocks, p.join_y, z), dim3(kJoinWaves * kWave), 0, s, from, from2, rows, (int32_t)p.m, to,
-                  to + p.join_y * p.m);
-      from = to, from2 = to + p.join_y * p.m, rows = p.join_y;
-    }
-    COOP_LAUNCH(K_DENSE_COLUMNS, k_dense_columns, dim3(x_blocks, 1, z), dim3(kJoinWaves * kWave), 0, s, from, from2, rows, (int32_t)p.m, db, db2);
-  }
+  if (fin.part != nullptr) sums_of_columns<T>(p, fin.part, fin.part2, db, db2, PAIR, ws, s);
   const int64_t ldk = p.kw * kElem<T>, ldz = p.slope ? p.dz_ld * kElem<T> : p.m * kElem<T>;
   const char* dz = p.slope ? ws + p.dz : (const char*)dout;
   const float scale = PAIR || act != COOP_ACT_NONE ? 1.f : alpha;

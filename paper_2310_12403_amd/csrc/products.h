@@ -118,8 +118,7 @@ struct Staged {
     }
   };
   // the fragment of rows row .. row + 31 at step kk of the stage
-  static __device__ __forceinline__ u32x4 fragment(const char* lds, int row, int kk) {
-    const int lane = lane_id();
+  static __device__ __forceinline__ u32x4 fragment(const char* lds, int row, int kk, int lane = lane_id()) {
     if constexpr (!STRIDED) {
       const int r = row + (lane & 31), chunk = kk * 2 + (lane >> 5);
       return *reinterpret_cast<const u32x4*>(lds + r * SIZE + ((chunk ^ swizzle(r)) << 4));

@@ -101,7 +101,7 @@ def gradients64(dzs, edzs, x, weights, dtype, grad_dtype, rounds):
 
 # (one tile, none whole, many rows, many columns, long k, tiles of 256 in each of the products)
 SIZES = [(0, 5, 3), (1, 1, 1), (3, 7, 5), (1, 4096, 64), (17, 2000, 300), (33, 64, 128), (130, 100, 75), (257, 129, 300), (300, 602, 41), (1000, 16, 8),
-         (20000, 33, 40), (70001, 24, 20), (4097, 72, 4100), (4097, 4100, 72), (72, 4100, 4104), (1, 2, 9000), (2, 9000, 1)]
+         (20000, 33, 40), (5000, 128, 128), (70000, 128, 64), (2049, 32, 128), (64, 127, 121), (31, 8, 8), (3000, 64, 31), (70001, 24, 20), (4097, 72, 4100), (4097, 4100, 72), (72, 4100, 4104), (1, 2, 9000), (2, 9000, 1)]
 
 
 @gpu
