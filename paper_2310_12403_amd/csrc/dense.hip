@@ -467,6 +467,9 @@ struct Cut {
 
 bool fits(const Cut& c) { return c.blocks() < ((uint64_t)1 << 31); }
 
+bool aligned16(const void* a, const void* b, const void* c = nullptr, const void* d = nullptr) {
+  return (((uintptr_t)a | (uintptr_t)b | (uintptr_t)c | (uintptr_t)d) & 15) == 0;
+}
 // f(KS, MT) for the steps of 16 of k and the tiles of 32 of m
 template <typename F>
 void with_narrow(int64_t k, int64_t m, F&& f) {
@@ -504,7 +507,7 @@ struct DensePlan {
     mw = round_up(m, e);
     narrow = es == 2 && !gated && k >= 8 && k <= 128 && m >= 8 && m <= 128 && !(grad && keeps && act != COOP_ACT_NONE);
     narrow_tiles = (uint32_t)((n + 31) / 32);
-    narrow_blocks = (uint32_t)at_most((narrow_tiles + 7) / 8, 256);
+    narrow_blocks = (uint32_t)(grad ? at_most((narrow_tiles + 7) / 8, 256) : at_most((narrow_tiles + kNarrowForwardWaves - 1) / kNarrowForwardWaves, 512));
     pad = !narrow && (!aligned || kw != k);
     size_t at = 0;
     auto take = [&](size_t b) { const size_t o = at; at += (b + 255) & ~(size_t)255; return o; };
@@ -652,7 +655,8 @@ bool backward_narrow(const DensePlan& p, const NarrowLayer& l, const void* dout,
   const int32_t db_col = dw != nullptr ? (int32_t)round_up(p.k, 8) : 0, width = db_col + kNarrowSums;
   with_narrow(p.k, p.m, [&](auto ks, auto mt) {
     constexpr int KS = decltype(ks)::value, MT = decltype(mt)::value, lds = NarrowBackward<T, KS, MT>::kLds;
-    const auto kernel = p.k == KS * 16 && p.m == MT * 32 ? k_narrow_grad<T, KS, MT, true> : k_narrow_grad<T, KS, MT, false>;
+    const bool exact = p.k == KS * 16 && p.m == MT * 32 && aligned16(l.x, dout, dx);
+    const auto kernel = exact ? k_narrow_grad<T, KS, MT, true> : k_narrow_grad<T, KS, MT, false>;
     ok = allow_lds(kernel, lds);
     if (ok) COOP_LAUNCH(K_DENSE_DX, kernel, dim3(p.narrow_blocks), dim3(512), lds, s, l, (const char*)dout, (char*)dx, sums, width, p.narrow_tiles);
   });
@@ -669,7 +673,8 @@ bool forward_all(const DensePlan& p, const void* x, const void* w, const void* w
       const NarrowLayer l{(const char*)x, (const char*)w, fin.bias, p.n, (int32_t)p.k, (int32_t)p.m, fin.alpha, fin.act};
       with_narrow(p.k, p.m, [&](auto ks, auto mt) {
         constexpr int KS = decltype(ks)::value, MT = decltype(mt)::value;
-        const auto kernel = p.k == KS * 16 && p.m == MT * 32 ? k_narrow<T, KS, MT, true> : k_narrow<T, KS, MT, false>;
+        const bool exact = p.k == KS * 16 && p.m == MT * 32 && aligned16(l.x, fin.residual, fin.out);
+        const auto kernel = exact ? k_narrow<T, KS, MT, true> : k_narrow<T, KS, MT, false>;
         COOP_LAUNCH(K_LINEAR, kernel, dim3(p.narrow_blocks), dim3(kNarrowForwardWaves * kWave), 0, s, l,
                     fin.residual, fin.out, fin.pre, p.narrow_tiles);
       });
@@ -736,9 +741,6 @@ int dense_check(int64_t n, int32_t k, int32_t m, int dtype, int act) {
   if (!known_dtype(dtype) || !known_act(act)) return COOP_E_ARG;
   if (n < 0 || n > kMostRows || k < 1 || k > kMostWidth || m < 1 || m > kMostWidth) return COOP_E_ARG;
   return COOP_OK;
-}
-bool aligned16(const void* a, const void* b, const void* c = nullptr, const void* d = nullptr) {
-  return (((uintptr_t)a | (uintptr_t)b | (uintptr_t)c | (uintptr_t)d) & 15) == 0;
 }
 // sums over no rows
 int empty_sums(void* a, int64_t a_bytes, void* b, int64_t b_bytes, hipStream_t s) {

@@ -9,25 +9,13 @@
 
 // 16 bytes of a row of dim >= 8 columns from column `col` on, of rows of any alignment.  Where the row ends before them: the row's last 16, to be
 // put right by mend_chunk when they have arrived.
-// EXACT, here and below: a row has as many columns as the kernel's tiles.
-template <int T, bool EXACT>
+template <int T>
 __device__ __forceinline__ u32x4 load_chunk(const char* row, int col, int dim) {
-  const int at = EXACT || col < dim - 8 ? col : dim - 8;
+  const int at = col < dim - 8 ? col : dim - 8;
   return __builtin_bit_cast(u32x4, Pack<T, 8>::load(row + at * 2));
 }
-// The rows of a wave's tile: where its first is, and the lane's offset (a row behind the last one reads as the last one, a tile as the last one).
-struct NarrowRows {
-  const char* base;
-  int at;
-  __device__ __forceinline__ NarrowRows(const char* p, uint32_t tile, uint32_t tiles, int64_t n, int dim) {
-    const uint32_t t = tile < tiles ? tile : tiles - 1;
-    const int64_t row = (int64_t)t * 32, last = n - 1 - row;
-    const int r = lane_id() & 31;
-    base = p + row * dim * 2;
-    at = (r < last ? r : (int)last) * dim * 2;
-  }
-};
 // columns col .. col + 7 of what load_chunk has read, zeros behind column `dim` (16 * step: the first column of the lanes' chunks)
+// EXACT, here and below: a row has as many columns as the kernel's tiles.
 template <bool EXACT>
 __device__ __forceinline__ u32x4 mend_chunk(u32x4 v, int step, int half, int dim) {
   if (EXACT || step * 16 + 16 <= dim) return v;
@@ -37,11 +25,11 @@ __device__ __forceinline__ u32x4 mend_chunk(u32x4 v, int step, int half, int dim
   typedef unsigned __int128 Bits;
   return __builtin_bit_cast(u32x4, __builtin_bit_cast(Bits, v) >> (16 * lost));
 }
-template <int T, bool EXACT>
+template <int T>
 __device__ __forceinline__ void store_chunk(char* row, int step, int half, int dim, u32x4 v) {
   const int col = step * 16 + half * 8;
   char* const at = row + col * 2;
-  if (EXACT || step * 16 + 16 <= dim || col + 8 <= dim) {
+  if (step * 16 + 16 <= dim || col + 8 <= dim) {
     __builtin_bit_cast(Pack<T, 8>, v).store(at);
     return;
   }
@@ -52,6 +40,41 @@ __device__ __forceinline__ void store_chunk(char* row, int step, int half, int d
   if (there & 2) Pack<T, 2>(__builtin_bit_cast(Pack<T, 2>, v[0])).store(at + i * 2), v[0] = v[1], i += 2;
   if (there & 1) Pack<T, 1>(__builtin_bit_cast(Pack<T, 1>, (uint16_t)v[0])).store(at + i * 2);
 }
+
+// The rows of a wave's tile, chunk by chunk: 16 columns' two, one of them the lane's.  EXACT: at addresses of multiples of 16, and what lies behind
+// the last row is neither read (zeros) nor written, without a branch: a wait for a load then counts exactly what was sent behind it.  Else a row
+// behind the last one reads as the last one, and a tile as the last one.
+template <int T, bool EXACT>
+struct NarrowRows {
+  char* base;  // the lane's row, or the tile's first
+  int at, dim;
+  bool live;
+  __amdgpu_buffer_rsrc_t rsrc;
+  __device__ __forceinline__ NarrowRows(const void* p, uint32_t tile, uint32_t tiles, int64_t n, int dim_, int lane) : dim(dim_) {
+    const int64_t row = (int64_t)tile * 32;
+    if constexpr (EXACT) {
+      const int64_t left = n - row;
+      base = (char*)p + row * dim * 2;
+      rsrc = __builtin_amdgcn_make_buffer_rsrc(base, 0, left <= 0 ? 0 : (left < 32 ? (int)left : 32) * dim * 2, 0x00020000);
+      at = (lane & 31) * dim * 2 + (lane >> 5) * 16;
+    } else {
+      const uint32_t t = tile < tiles ? tile : tiles - 1;
+      const int64_t last = n - 1 - (int64_t)t * 32;
+      const int r = lane & 31;
+      live = row + r < n;
+      base = (char*)p + (int64_t)t * 32 * dim * 2;
+      at = (r < last ? r : (int)last) * dim * 2;
+    }
+  }
+  __device__ __forceinline__ u32x4 load(int step, int half) const {
+    if constexpr (EXACT) return __builtin_amdgcn_raw_buffer_load_b128(rsrc, at + step * 32, 0, 0);
+    else return load_chunk<T>(base + at, step * 16 + half * 8, dim);
+  }
+  __device__ __forceinline__ void store(int step, int half, u32x4 v) const {
+    if constexpr (EXACT) __builtin_amdgcn_raw_buffer_store_b128(v, rsrc, at + step * 32, 0, 0);
+    else if (live) store_chunk<T>(base + at, step, half, dim, v);
+  }
+};
 
 // Columns 16 h + {0..3, 8..11} (lanes 0 to 31) and 16 h + {4..7, 12..15} (the others), packed, into 16 h + {0..7} and 16 h + {8..15}: what a
 // tile's registers hold into 16 bytes of a row; and back, being its own reverse.
@@ -74,7 +97,7 @@ __device__ __forceinline__ void place_weight(const NarrowLayer& l, char* lds) {
   for (int i = threadIdx.x; i < MT * KS * 64; i += blockDim.x) {
     const int lane = i & 63, f = i >> 6, row = f / KS * 32 + (lane & 31), col = f % KS * 16 + (lane >> 5) * 8;
     *reinterpret_cast<u32x4*>(lds + i * 16) =
-        row < l.m ? mend_chunk<false>(load_chunk<T, false>(l.w + (int64_t)row * l.k * 2, col, l.k), f % KS, lane >> 5, l.k) : u32x4{0, 0, 0, 0};
+        row < l.m ? mend_chunk<false>(load_chunk<T>(l.w + (int64_t)row * l.k * 2, col, l.k), f % KS, lane >> 5, l.k) : u32x4{0, 0, 0, 0};
   }
 }
 template <int T, int MT>
@@ -106,7 +129,7 @@ __device__ __forceinline__ void unpack8(u32x4 v, float (&f)[8]) {
   __builtin_bit_cast(Pack<T, 8>, v).get(f);
 }
 
-constexpr int kNarrowForwardWaves = 8;
+constexpr int kNarrowForwardWaves = 4;
 template <int T, int KS, int MT, bool EXACT>
 __global__ __launch_bounds__(kNarrowForwardWaves* kWave) void k_narrow(NarrowLayer l, const char* __restrict__ residual, char* __restrict__ out,
                                                                        float* __restrict__ pre, uint32_t tiles) {
@@ -121,15 +144,15 @@ __global__ __launch_bounds__(kNarrowForwardWaves* kWave) void k_narrow(NarrowLay
   if (tile >= tiles) return;
   u32x4 xf[KS], res[2 * MT];
   const auto load_x = [&](uint32_t to) {
-    const NarrowRows r(l.x, to, tiles, l.n, l.k);
+    const NarrowRows<T, EXACT> r(l.x, to, tiles, l.n, l.k, lane);
 #pragma unroll
-    for (int s = 0; s < KS; ++s) xf[s] = load_chunk<T, EXACT>(r.base + r.at, s * 16 + half * 8, l.k);
+    for (int s = 0; s < KS; ++s) xf[s] = r.load(s, half);
   };
   load_x(tile);
   if (residual != nullptr) {
-    const NarrowRows r(residual, tile, tiles, l.n, l.m);
+    const NarrowRows<T, EXACT> r(residual, tile, tiles, l.n, l.m, lane);
 #pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) res[i] = load_chunk<T, EXACT>(r.base + r.at, i * 16 + half * 8, l.m);
+    for (int i = 0; i < 2 * MT; ++i) res[i] = r.load(i, half);
   }
   for (; tile < tiles; tile += step) {
     const int64_t row = (int64_t)tile * 32 + (lane & 31);
@@ -145,7 +168,7 @@ __global__ __launch_bounds__(kNarrowForwardWaves* kWave) void k_narrow(NarrowLay
       if (s & 1) __builtin_amdgcn_sched_barrier(0);
     }
     load_x(tile + step);
-    const NarrowRows next(residual, tile + step, tiles, l.n, l.m);
+    const NarrowRows<T, EXACT> next(residual, tile + step, tiles, l.n, l.m, lane), to(out, tile, tiles, l.n, l.m, lane);
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -164,12 +187,11 @@ __global__ __launch_bounds__(kNarrowForwardWaves* kWave) void k_narrow(NarrowLay
         for (int e = 0; e < 8; ++e) v[e] *= l.alpha;
         if (residual != nullptr) {
           unpack8<T>(swap_halves(mend_chunk<EXACT>(res[c], c, half, l.m)), r);
-          res[c] = load_chunk<T, EXACT>(next.base + next.at, c * 16 + half * 8, l.m);
+          res[c] = next.load(c, half);
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] += r[e];
         }
-        const u32x4 to = swap_halves(pack8<T>(v));
-        if (live) store_chunk<T, EXACT>(out + row * l.m * 2, c, half, l.m, to);
+        to.store(c, half, swap_halves(pack8<T>(v)));
         __builtin_amdgcn_sched_barrier(0);  // (or the compiler spreads the chunks' work over more registers than there are)
       }
   }
@@ -222,7 +244,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   for (int i = threadIdx.x; i < MT * 32 * KS * 2; i += 512) {
     const int row = i / (KS * 2), chunk = i % (KS * 2);
     *reinterpret_cast<u32x4*>(lds + row * (KS * 32) + ((chunk ^ B::X::swizzle(row)) << 4)) =
-        row < l.m ? mend_chunk<false>(load_chunk<T, false>(l.w + (int64_t)row * l.k * 2, chunk * 8, l.k), chunk >> 1, chunk & 1, l.k) : u32x4{0, 0, 0, 0};
+        row < l.m ? mend_chunk<false>(load_chunk<T>(l.w + (int64_t)row * l.k * 2, chunk * 8, l.k), chunk >> 1, chunk & 1, l.k) : u32x4{0, 0, 0, 0};
   }
   // biases as a product's operand: times a column of ones
   uint32_t bias[MT];
@@ -247,16 +269,16 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     for (int e = 0; e < 4; ++e) db[i][0][e] = db[i][1][e] = 0.f;
   u32x4 xf[KS], dy[2 * MT];
   const auto load_x = [&](uint32_t to) {
-    const NarrowRows r(l.x, to, tiles, l.n, l.k);
-    const int half = anew(lane) >> 5;
+    const int lane = anew(lane_id());
+    const NarrowRows<T, EXACT> r(l.x, to, tiles, l.n, l.k, lane);
 #pragma unroll
-    for (int s = 0; s < KS; ++s) xf[s] = load_chunk<T, EXACT>(r.base + r.at, s * 16 + half * 8, l.k);
+    for (int s = 0; s < KS; ++s) xf[s] = r.load(s, lane >> 5);
   };
   const auto load_dy = [&](uint32_t to) {
-    const NarrowRows r(dout, to, tiles, l.n, l.m);
-    const int half = anew(lane) >> 5;
+    const int lane = anew(lane_id());
+    const NarrowRows<T, EXACT> r(dout, to, tiles, l.n, l.m, lane);
 #pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) dy[i] = load_chunk<T, EXACT>(r.base + r.at, i * 16 + half * 8, l.m);
+    for (int i = 0; i < 2 * MT; ++i) dy[i] = r.load(i, lane >> 5);
   };
   // (a wave whose tile there is not goes along with zeros: the block's waves meet)
   uint32_t first = blockIdx.x * B::kWaves;
@@ -272,7 +294,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       xf[s] = mend_chunk<EXACT>(xf[s], s, anew(lane) >> 5, l.k);
-      if (!whole && !live) xf[s] = u32x4{0, 0, 0, 0};
+      if (!EXACT && !whole && !live) xf[s] = u32x4{0, 0, 0, 0};
     }
 #pragma unroll
     for (int s = 0; s < KS; ++s)
@@ -293,7 +315,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       for (int h = 0; h < 2; ++h) {
         const int c = 2 * i + h;
         dz[c] = mend_chunk<EXACT>(dy[c], c, anew(lane) >> 5, l.m);
-        if (!whole && !live) dz[c] = u32x4{0, 0, 0, 0};
+        if (!EXACT && !whole && !live) dz[c] = u32x4{0, 0, 0, 0};
         float d[8];
         unpack8<T>(swap_halves(dz[c]), d);
         if (l.act != COOP_ACT_NONE) {
@@ -317,6 +339,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     load_x(next);
     if (dx != nullptr) {
       const int at = anew(lane);
+      const NarrowRows<T, EXACT> to(dx, first + wave, tiles, l.n, l.k, at);
       const float scale = l.act == COOP_ACT_NONE ? l.alpha : 1.f;
 #pragma unroll
       for (int t = 0; t < KT; ++t) {
@@ -330,8 +353,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
           float f[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) f[e] = v[8 * h + e] * scale;
-          const u32x4 to = swap_halves(pack8<T>(f));
-          if (live) store_chunk<T, EXACT>(dx + row * l.k * 2, 2 * t + h, at >> 5, l.k, to);
+          to.store(2 * t + h, at >> 5, swap_halves(pack8<T>(f)));
         }
         __builtin_amdgcn_sched_barrier(0);
       }

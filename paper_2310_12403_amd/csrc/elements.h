@@ -60,11 +60,27 @@ __device__ __forceinline__ void store_elements(void* p, const float (&f)[E]) {
   }
 }
 
-// Sum over each aligned group of `lanes` lanes (a power of two up to 64); every lane of the group has it.
+// v + that of another lane, by a move within rows of 16 lanes
+template <int CONTROL>
+__device__ __forceinline__ float add_moved(float v) {
+  return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CONTROL, 0xF, 0xF, true));
+}
+// Sum over each aligned group of `lanes` lanes (a power of two up to 64); every lane of the group has it.  Pairs, then pairs of pairs, and so on:
+// once the lanes of a group agree any lane of the next group is as good as the one across, so that moves within the registers do (a mirrored
+// half row, a mirrored row, two rows or the wave's halves exchanged) where a shuffle goes through LDS.
 __device__ __forceinline__ float group_sum(float v, int lanes) {
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1)
-    if (off < lanes) v += __shfl_xor(v, off, kWave);
+  if (lanes > 1) v = add_moved<0xB1>(v);   // lanes 1 0 3 2
+  if (lanes > 2) v = add_moved<0x4E>(v);   // lanes 2 3 0 1
+  if (lanes > 4) v = add_moved<0x141>(v);  // a half row from its other end
+  if (lanes > 8) v = add_moved<0x140>(v);  // a row from its other end
+  if (lanes > 16) {
+    const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+  }
+  if (lanes > 32) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+  }
   return v;
 }
 

@@ -52,6 +52,40 @@ __device__ __forceinline__ void row_sums(float& a, float& b, int lanes, float* l
   }
 }
 
+// The same with one barrier: two parts of LDS take turns, and whoever writes one again has met the others behind their reads of it.
+template <int WAVES>
+struct RowSums {
+  float* lds;  // [4 WAVES]
+  int turn;
+  __device__ __forceinline__ explicit RowSums(float* lds_) : lds(lds_), turn(0) {}
+  __device__ __forceinline__ void operator()(float& a, float& b, int lanes) {
+    a = group_sum(a, WAVES == 1 ? lanes : kWave);
+    b = group_sum(b, WAVES == 1 ? lanes : kWave);
+    if constexpr (WAVES > 1) {
+      float* const to = lds + turn * 2 * WAVES;
+      turn ^= 1;
+      if (lane_id() == 0) to[2 * wave_in_block()] = a, to[2 * wave_in_block() + 1] = b;
+      __syncthreads();
+      a = b = 0.f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) a += to[2 * w], b += to[2 * w + 1];
+    }
+  }
+  __device__ __forceinline__ float operator()(float a, int lanes) {
+    a = group_sum(a, WAVES == 1 ? lanes : kWave);
+    if constexpr (WAVES > 1) {
+      float* const to = lds + turn * 2 * WAVES;
+      turn ^= 1;
+      if (lane_id() == 0) to[wave_in_block()] = a;
+      __syncthreads();
+      a = 0.f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) a += to[w];
+    }
+    return a;
+  }
+};
+
 template <int WAVES> constexpr int kNormBlock = WAVES == 1 ? kBlock : WAVES * kWave;
 
 // which rows a block takes: its first group's row, rows from group to group of the grid, and this lane's group in the block

@@ -64,42 +64,57 @@ __device__ __forceinline__ void put_pack(char* at, const float (&f)[E]) {
   }
 }
 
-// A lane's columns of a vector of weights (`other` where there is none): kept in registers, or read anew for each row.
-template <int T, int E, int K, bool kKept>
+// The vectors of weights that there are, in 32 bits one behind the other in LDS: read anew for each row, and not from memory, where a read would wait
+// for all of the next row, which was asked for before it.  (Rows too wide for that read them from memory.)
+struct SeamWeightPointers { const char *gate, *w1, *b1, *w2, *b2; };
+constexpr int32_t kSeamLdsDim = 4096;
+template <int T, int E, bool WHOLE>
 struct SeamWeights {
-  float x[kKept ? K : 1][E];
   const char* p;
+  const float* lds;  // null: from memory
   bool wide;
-  float other;
-  __device__ __forceinline__ void read(int32_t at, float (&f)[E]) const {
+  float other;  // where there is no such vector
+  // all threads of the block; `next` is moved behind it
+  __device__ __forceinline__ SeamWeights(const char* p_, bool wide_, float other_, int32_t dim, float*& next) : p(p_), lds(nullptr), wide(wide_), other(other_) {
+    if (p == nullptr || dim > kSeamLdsDim) return;
+    for (int32_t i = threadIdx.x; i < dim; i += blockDim.x) next[i] = wide ? ((const float*)p)[i] : (float)((const typename Element<T>::M*)p)[i];
+    lds = next;
+    next += (dim + 3) & ~3;
+  }
+  __device__ __forceinline__ void get(int32_t at, float (&f)[E]) const {
     if (p == nullptr) {
 #pragma unroll
       for (int e = 0; e < E; ++e) f[e] = other;
+    } else if (lds != nullptr) {
+      typedef float Four __attribute__((ext_vector_type(4)));
+      if constexpr (WHOLE && E % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < E; i += 4) {
+          const Four x = *reinterpret_cast<const Four*>(lds + at + i);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) f[i + e] = x[e];
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) f[e] = lds[at + e];
+      }
     } else if (wide) {
       load_elements<COOP_F32, E>(p + (int64_t)at * 4, f);
     } else {
       load_elements<T, E>(p + (int64_t)at * (int64_t)sizeof(typename Element<T>::M), f);
     }
   }
-  __device__ __forceinline__ SeamWeights(const char* p_, bool wide_, float other_, int lane, int lanes, int32_t dim) : p(p_), wide(wide_), other(other_) {
-    if constexpr (kKept) {
-#pragma unroll
-      for (int k = 0; k < K; ++k) read(Columns<E>(lane + k * lanes, dim).at, x[k]);
-    }
-  }
-  __device__ __forceinline__ void get(int k, int32_t at, float (&f)[E]) const {
-    if constexpr (kKept) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) f[e] = x[k][e];
-    } else {
-      read(at, f);
-    }
-  }
 };
+inline int seam_lds(const SeamWeightPointers& wp, bool columns, int32_t dim) {
+  if (dim > kSeamLdsDim) return 0;
+  const int n = (columns && wp.gate != nullptr) + (wp.w1 != nullptr) + (wp.b1 != nullptr) + (wp.w2 != nullptr) + (wp.b2 != nullptr);
+  return n * ((dim + 3) & ~3) * 4;
+}
 
 // mean and 1 / size of a row, and v left as v - mean (root mean square: mean 0)
-template <int E, int K, int WAVES>
-__device__ __forceinline__ void row_statistics(float (&v)[K][E], const Rows<WAVES>& rows, int lanes, const SeamShape& sh, float* lds, float* mean_out, float* rstd_out) {
+template <int E, int K, int WAVES, bool WHOLE>
+__device__ __forceinline__ void row_statistics(float (&v)[K][E], const Rows<WAVES>& rows, int lanes, const SeamShape& sh, RowSums<WAVES>& sums, float* mean_out,
+                                               float* rstd_out) {
   const float n = (float)sh.dim;
   float mean = 0.f;
   if (!sh.rms) {
@@ -108,9 +123,9 @@ __device__ __forceinline__ void row_statistics(float (&v)[K][E], const Rows<WAVE
     for (int k = 0; k < K; ++k) {
       const Columns<E> c(rows.lane + k * lanes, sh.dim);
 #pragma unroll
-      for (int e = 0; e < E; ++e) sum += e >= c.own ? v[k][e] : 0.f;
+      for (int e = 0; e < E; ++e) sum += WHOLE || e >= c.own ? v[k][e] : 0.f;
     }
-    mean = row_sum<WAVES>(sum, lanes, lds) / n;
+    mean = sums(sum, lanes) / n;
   }
   float square = 0.f;
 #pragma unroll
@@ -119,30 +134,34 @@ __device__ __forceinline__ void row_statistics(float (&v)[K][E], const Rows<WAVE
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       v[k][e] -= mean;
-      square += e >= c.own ? v[k][e] * v[k][e] : 0.f;
+      square += WHOLE || e >= c.own ? v[k][e] * v[k][e] : 0.f;
     }
   }
   *mean_out = mean;
-  *rstd_out = 1.f / sqrtf(row_sum<WAVES>(square, lanes, lds) / n + sh.eps);
+  *rstd_out = 1.f / sqrtf(sums(square, lanes) / n + sh.eps);
 }
 
-template <int WAVES, int K> constexpr bool kSeamKept = K == 1;
-
-struct SeamWeightPointers { const char *gate, *w1, *b1, *w2, *b2; };
+// Waves of a SIMD that a kernel's registers are cut for, and that its grid fills.  (A gradient in 16 bits for 3, with 26 registers spilled, 572,596
+// rows of 128: 320 us for 309 forward and backward; 3 blocks a CU where 2 fit: 393.)
+constexpr int seam_waves(int e, int k, int waves, bool grad) { return k > 1 ? 2 : !grad ? 4 : waves == 8 || e == 8 ? 2 : 3; }
 
 // stats: [4][rows], mean and rstd of N_after, mean and rstd of N_before.  (Outputs are not told to be apart from the inputs: a row is read whole
 // before any of it is written.)
-template <int T, int S, int E, int K, int WAVES>
-__global__ __launch_bounds__(kNormBlock<WAVES>) void k_seam(const char* x, const char* f, SeamWeightPointers wp, SeamShape sh, char* r_out, char* y,
+template <int T, int S, int E, int K, int WAVES, bool WHOLE>
+__global__ __launch_bounds__(kNormBlock<WAVES>) __attribute__((amdgpu_waves_per_eu(seam_waves(E, K, WAVES, false)))) void k_seam(const char* x, const char* f, SeamWeightPointers wp, SeamShape sh, char* r_out, char* y,
                                                             float* __restrict__ stats) {
-  __shared__ float lds[WAVES];
+  __shared__ float lds[4 * WAVES];
+  RowSums<WAVES> row_sums(lds);
   constexpr int64_t kT = (int64_t)sizeof(typename Element<T>::M), kS = (int64_t)sizeof(typename Element<S>::M);
   const Rows<WAVES> rows(sh);
   const int lanes = rows.lanes(sh);
-  constexpr bool kKept = kSeamKept<WAVES, K>;
-  const SeamWeights<T, E, K, kKept> gate_of(sh.gate == kColumnGate ? wp.gate : nullptr, sh.wide_w, 1.f, rows.lane, lanes, sh.dim);
-  const SeamWeights<T, E, K, kKept> w1_of(wp.w1, sh.wide_w, 1.f, rows.lane, lanes, sh.dim), b1_of(wp.b1, sh.wide_w, 0.f, rows.lane, lanes, sh.dim);
-  const SeamWeights<T, E, K, kKept> w2_of(wp.w2, sh.wide_w, 1.f, rows.lane, lanes, sh.dim), b2_of(wp.b2, sh.wide_w, 0.f, rows.lane, lanes, sh.dim);
+  extern __shared__ __attribute__((aligned(16))) float weights[];
+  float* next_weights = weights;
+  typedef SeamWeights<T, E, WHOLE> Weights;
+  const Weights gate_of(sh.gate == kColumnGate ? wp.gate : nullptr, sh.wide_w, 1.f, sh.dim, next_weights), w1_of(wp.w1, sh.wide_w, 1.f, sh.dim, next_weights);
+  const Weights b1_of(wp.b1, sh.wide_w, 0.f, sh.dim, next_weights), w2_of(wp.w2, sh.wide_w, 1.f, sh.dim, next_weights);
+  const Weights b2_of(wp.b2, sh.wide_w, 0.f, sh.dim, next_weights);
+  __syncthreads();
   SeamPacks<S, E, K> next_x;  // (the next row is on its way while this one is worked on)
   SeamPacks<T, E, K> next_f, next_g;
   const auto look_ahead = [&](int64_t r) {
@@ -159,18 +178,18 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_seam(const char* x, const
       next_x.get(k, v[k]);
       next_f.get(k, p[k]);
       if (sh.gate == kRowGate) next_g.get(k, g[k]);
-      else gate_of.get(k, c.at, g[k]);
+      else gate_of.get(c.at, g[k]);
     }
     if (r + rows.step < sh.rows) look_ahead(r + rows.step);
     float mean1 = 0.f, rstd1 = 1.f, mean2 = 0.f, rstd2 = 1.f;
     if (sh.after) {
-      row_statistics<E, K, WAVES>(p, rows, lanes, sh, lds, &mean1, &rstd1);
+      row_statistics<E, K, WAVES, WHOLE>(p, rows, lanes, sh, row_sums, &mean1, &rstd1);
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const Columns<E> c(rows.lane + k * lanes, sh.dim);
         float w[E], b[E];
-        w1_of.get(k, c.at, w);
-        b1_of.get(k, c.at, b);
+        w1_of.get(c.at, w);
+        b1_of.get(c.at, b);
 #pragma unroll
         for (int e = 0; e < E; ++e) p[k][e] = p[k][e] * rstd1 * w[e] + b[e];
       }
@@ -180,7 +199,7 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_seam(const char* x, const
       const Columns<E> c(rows.lane + k * lanes, sh.dim);
 #pragma unroll
       for (int e = 0; e < E; ++e) v[k][e] = v[k][e] * sh.alpha + p[k][e] * g[k][e];
-      if (sh.before || !c.live) continue;
+      if (sh.before || (!WHOLE && !c.live)) continue;
       put_pack<S, E>(r_out + (r * sh.dim + c.at) * kS, v[k]);
     }
     if (sh.before) {
@@ -189,14 +208,14 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_seam(const char* x, const
       for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int e = 0; e < E; ++e) out[k][e] = v[k][e];
-      row_statistics<E, K, WAVES>(out, rows, lanes, sh, lds, &mean2, &rstd2);
+      row_statistics<E, K, WAVES, WHOLE>(out, rows, lanes, sh, row_sums, &mean2, &rstd2);
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const Columns<E> c(rows.lane + k * lanes, sh.dim);
-        if (!c.live) continue;
+        if (!WHOLE && !c.live) continue;
         float w[E], b[E];
-        w2_of.get(k, c.at, w);
-        b2_of.get(k, c.at, b);
+        w2_of.get(c.at, w);
+        b2_of.get(c.at, b);
 #pragma unroll
         for (int e = 0; e < E; ++e) out[k][e] = out[k][e] * rstd2 * w[e] + b[e];
         put_pack<S, E>(r_out + (r * sh.dim + c.at) * kS, v[k]);
@@ -214,20 +233,23 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_seam(const char* x, const
 
 // part: [gridDim.x][4][dim]: the block's sums of d h1 and of d (of e, where the gate is an element's; h1 is f where there is no norm behind it),
 // of dy h2 and of dy; null: not asked for.
-template <int T, int S, int E, int K, int WAVES>
-__global__ __launch_bounds__(kNormBlock<WAVES>) void k_seam_grad(const char* dr, const char* dy, const char* __restrict__ x, const char* __restrict__ f,
+template <int T, int S, int E, int K, int WAVES, bool WHOLE>
+__global__ __launch_bounds__(kNormBlock<WAVES>) __attribute__((amdgpu_waves_per_eu(seam_waves(E, K, WAVES, true)))) void k_seam_grad(const char* dr, const char* dy, const char* __restrict__ x, const char* __restrict__ f,
                                                                  const float* __restrict__ stats, SeamWeightPointers wp, SeamShape sh, char* dx, char* df,
                                                                  char* dgate, float* __restrict__ part) {
-  constexpr int kLds = WAVES == 1 ? kBlock * E : 2 * WAVES;
+  constexpr int kLds = WAVES == 1 ? kBlock * E : 4 * WAVES;
   __shared__ float lds[kLds];
+  RowSums<WAVES> row_sums(lds);
   constexpr int64_t kT = (int64_t)sizeof(typename Element<T>::M), kS = (int64_t)sizeof(typename Element<S>::M);
   const Rows<WAVES> rows(sh);
   const int lanes = rows.lanes(sh);
   const float n = (float)sh.dim;
-  constexpr bool kKept = kSeamKept<WAVES, K>;
-  const SeamWeights<T, E, K, kKept> gate_of(sh.gate == kColumnGate ? wp.gate : nullptr, sh.wide_w, 1.f, rows.lane, lanes, sh.dim);
-  const SeamWeights<T, E, K, kKept> w1_of(wp.w1, sh.wide_w, 1.f, rows.lane, lanes, sh.dim), b1_of(wp.b1, sh.wide_w, 0.f, rows.lane, lanes, sh.dim);
-  const SeamWeights<T, E, K, kKept> w2_of(wp.w2, sh.wide_w, 1.f, rows.lane, lanes, sh.dim);
+  extern __shared__ __attribute__((aligned(16))) float weights[];
+  float* next_weights = weights;
+  typedef SeamWeights<T, E, WHOLE> Weights;
+  const Weights gate_of(sh.gate == kColumnGate ? wp.gate : nullptr, sh.wide_w, 1.f, sh.dim, next_weights), w1_of(wp.w1, sh.wide_w, 1.f, sh.dim, next_weights);
+  const Weights b1_of(wp.b1, sh.wide_w, 0.f, sh.dim, next_weights), w2_of(wp.w2, sh.wide_w, 1.f, sh.dim, next_weights);
+  __syncthreads();
   float sums[4][K][E];
 #pragma unroll
   for (int q = 0; q < 4; ++q)
@@ -260,7 +282,7 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_seam_grad(const char* dr,
       next_f.get(k, h1[k]);
       if (sh.before) next_x.get(k, h2[k]), next_dy.get(k, t[k]);
       if (sh.gate == kRowGate) next_g.get(k, g[k]);
-      else gate_of.get(k, c.at, g[k]);
+      else gate_of.get(c.at, g[k]);
       if (dr != nullptr) next_dr.get(k, d[k]);
       else {
 #pragma unroll
@@ -278,26 +300,26 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_seam_grad(const char* dr,
       }
       if (!sh.before) continue;
       if (sh.after) {
-        w1_of.get(k, c.at, w);
-        b1_of.get(k, c.at, b);
+        w1_of.get(c.at, w);
+        b1_of.get(c.at, b);
       }
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float p = sh.after ? h1[k][e] * w[e] + b[e] : h1[k][e];
         h2[k][e] = (h2[k][e] * sh.alpha + p * g[k][e] - mean2) * rstd2;
       }
-      w2_of.get(k, c.at, w);
+      w2_of.get(c.at, w);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         sums[2][k][e] += t[k][e] * h2[k][e];
         sums[3][k][e] += t[k][e];
         t[k][e] *= w[e];
-        s1 += e >= c.own ? t[k][e] : 0.f;
-        s2 += e >= c.own ? t[k][e] * h2[k][e] : 0.f;
+        s1 += WHOLE || e >= c.own ? t[k][e] : 0.f;
+        s2 += WHOLE || e >= c.own ? t[k][e] * h2[k][e] : 0.f;
       }
     }
     if (sh.before) {
-      row_sums<WAVES>(s1, s2, lanes, lds);
+      row_sums(s1, s2, lanes);
       s1 = sh.rms ? 0.f : s1 / n;
       s2 /= n;
 #pragma unroll
@@ -310,8 +332,8 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_seam_grad(const char* dr,
     for (int k = 0; k < K; ++k) {
       const Columns<E> c(rows.lane + k * lanes, sh.dim);
       float w[E], b[E];
-      if (sh.after) w1_of.get(k, c.at, w);
-      if (sh.gate == kRowGate && sh.after) b1_of.get(k, c.at, b);
+      if (sh.after) w1_of.get(c.at, w);
+      if (sh.gate == kRowGate && sh.after) b1_of.get(c.at, b);
       float out[E];
 #pragma unroll
       for (int e = 0; e < E; ++e) {
@@ -321,10 +343,10 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_seam_grad(const char* dr,
         sums[0][k][e] += summed * h1[k][e];
         sums[1][k][e] += summed;
         t[k][e] = sh.after ? ee * w[e] : ee;
-        s1 += e >= c.own ? t[k][e] : 0.f;
-        s2 += e >= c.own ? t[k][e] * h1[k][e] : 0.f;
+        s1 += WHOLE || e >= c.own ? t[k][e] : 0.f;
+        s2 += WHOLE || e >= c.own ? t[k][e] * h1[k][e] : 0.f;
       }
-      if (!c.live) continue;
+      if (!WHOLE && !c.live) continue;
       if (!sh.after) {
         put_pack<S, E>(dx + (r * sh.dim + c.at) * kS, out);
         put_pack<T, E>(df + (r * sh.dim + c.at) * kT, t[k]);
@@ -336,13 +358,13 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) void k_seam_grad(const char* dr,
       }
     }
     if (!sh.after) continue;
-    row_sums<WAVES>(s1, s2, lanes, lds);
+    row_sums(s1, s2, lanes);
     s1 = sh.rms ? 0.f : s1 / n;
     s2 /= n;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const Columns<E> c(rows.lane + k * lanes, sh.dim);
-      if (!c.live) continue;
+      if (!WHOLE && !c.live) continue;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         t[k][e] = (t[k][e] - s1 - h1[k][e] * s2) * rstd1;
@@ -417,46 +439,49 @@ __global__ __launch_bounds__(kSeamJoinWaves* kWave) void k_seam_join(const float
   if (out.dgate != nullptr) out.dgate[c] = sh.after ? value(wp.w1, 1.f) * a + value(wp.b1, 0.f) * b : a;
 }
 
-// How a row is shared: K packs a lane on one wave or less, on 4 or on 8 waves.
+// How a row is shared: a pack a lane on one wave or less, on 2, 4 or 8 waves, and wider ones 2 or 4 packs a lane on 8.  (A pack a lane, for the
+// registers: what a gradient holds for each column is 4 sums and 5 values besides the next row's.)
 struct SeamLayout { int e, k, waves, lanes, lanes_log2; };
 bool seam_layout(int32_t dim, int dtype, SeamLayout* out) {
   const int e = dtype == COOP_F32 ? 4 : 8;
   SeamLayout l{dim >= e ? e : 1, 1, 1, 1, 0};
   const int32_t packs = (dim + l.e - 1) / l.e;
-  if (packs <= 2 * kWave) {
-    while (l.lanes < packs && l.lanes < kWave) l.lanes *= 2, ++l.lanes_log2;
-  } else {
-    l.waves = packs <= 2 * 4 * kWave ? 4 : 8;
-    l.lanes = l.waves * kWave;
-  }
+  while (l.lanes < packs && l.lanes < 8 * kWave) l.lanes *= 2, ++l.lanes_log2;
+  if (l.lanes > kWave) l.waves = l.lanes / kWave;
   while (l.k * l.lanes < packs) l.k *= 2;
   *out = l;
-  return l.k <= (l.waves == 8 ? 4 : 2);
+  return l.k <= 4;
 }
 
-// Blocks of a pass: as many as are on the chip at once, and for a gradient no more than leave each group two rows.
+// Blocks of a pass: as many as are on the chip at once, and for a gradient no more
+// than leave each group two rows.
 int64_t seam_blocks(int64_t rows, const SeamLayout& l, bool grad) {
   const int64_t per_block = l.waves == 1 ? kBlock / l.lanes : 1;
   int64_t b = (rows + per_block - 1) / per_block;
-  const int64_t each = l.waves == 8 ? (grad ? 1 : 2) : l.k == 1 ? (grad ? 3 : 4) : (grad ? 2 : 3), most = 256 * each;
+  const int64_t most = 256 * 4 * seam_waves(l.e, l.k, l.waves, grad) / (l.waves == 1 ? kWavesPerBlock : l.waves);
   if (b > most) b = most;
   if (grad && b > rows / (2 * per_block) + 1) b = rows / (2 * per_block) + 1;
   return b;
 }
 
 template <int T, typename F>
-void with_seam_layout(const SeamLayout& l, F&& f) {
+void with_seam_layout(const SeamLayout& l, int32_t dim, F&& f) {
   constexpr int E = T == COOP_F32 ? 4 : 8;
-  const auto call = [&](auto e, auto k, auto waves) { f(e, k, waves); };
+  const auto call = [&](auto e, auto k, auto waves) {
+    constexpr int EE = decltype(e)::value, K = decltype(k)::value;
+    if (dim == EE * K * l.lanes) f(e, k, waves, std::integral_constant<bool, true>());
+    else f(e, k, waves, std::integral_constant<bool, false>());
+  };
   const std::integral_constant<int, E> wide;
   const std::integral_constant<int, 1> one;
   const std::integral_constant<int, 2> two;
   const std::integral_constant<int, 4> four;
   const std::integral_constant<int, 8> eight;
   if (l.e == 1) call(one, one, one);
-  else if (l.waves == 1) l.k == 1 ? call(wide, one, one) : call(wide, two, one);
-  else if (l.waves == 4) l.k == 1 ? call(wide, one, four) : call(wide, two, four);
-  else l.k <= 2 ? call(wide, two, eight) : call(wide, four, eight);
+  else if (l.waves == 1) call(wide, one, one);
+  else if (l.waves == 2) call(wide, one, two);
+  else if (l.waves == 4) call(wide, one, four);
+  else l.k == 1 ? call(wide, one, eight) : l.k == 2 ? call(wide, two, eight) : call(wide, four, eight);
 }
 template <typename F>
 void with_seam_types(int dtype, int stream_dtype, F&& f) {
@@ -506,11 +531,14 @@ extern "C" int coop_residual_norm(const void* x, const void* f, int64_t n_rows, 
   const SeamShape sh = seam_shape(n_rows, dim, l, alpha, eps, norms, gate_form, weight_dtype);
   const SeamWeightPointers wp{(const char*)gate, (const char*)after_weight, (const char*)after_bias, (const char*)before_weight, (const char*)before_bias};
   const dim3 grid((unsigned)seam_blocks(n_rows, l, false));
+  const int weights = seam_lds(wp, gate_form == COOP_GATE_COLUMNS, dim);
   with_seam_types(dtype, stream_dtype, [&](auto t, auto st) {
     constexpr int T = decltype(t)::value, S = decltype(st)::value;
-    with_seam_layout<T>(l, [&](auto e, auto k, auto waves) {
+    with_seam_layout<T>(l, dim, [&](auto e, auto k, auto waves, auto whole) {
       constexpr int E = decltype(e)::value, K = decltype(k)::value, N = decltype(waves)::value;
-      COOP_LAUNCH(K_SEAM, (k_seam<T, S, E, K, N>), grid, dim3(kNormBlock<N>), 0, (hipStream_t)stream, (const char*)x, (const char*)f, wp, sh, (char*)r_out,
+      const auto kernel = k_seam<T, S, E, K, N, decltype(whole)::value>;
+      if (weights > 64 * 1024 - 512) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, weights);
+      COOP_LAUNCH(K_SEAM, kernel, grid, dim3(kNormBlock<N>), weights, (hipStream_t)stream, (const char*)x, (const char*)f, wp, sh, (char*)r_out,
                   (char*)y_out, stats_out);
     });
   });
@@ -555,13 +583,16 @@ extern "C" int coop_residual_norm_grad(const void* dr, const void* dy, const voi
   const hipStream_t s = (hipStream_t)stream;
   const SeamWeightPointers wp{(const char*)gate, (const char*)after_weight, (const char*)after_bias, (const char*)before_weight, nullptr};
   const int64_t blocks = seam_blocks(n_rows, l, true);
+  const int weights = seam_lds(wp, gate_form == COOP_GATE_COLUMNS, dim);
   float* part = sums ? (float*)workspace : nullptr;
   if (n_rows > 0)
     with_seam_types(dtype, stream_dtype, [&](auto t, auto st) {
       constexpr int T = decltype(t)::value, S = decltype(st)::value;
-      with_seam_layout<T>(l, [&](auto e, auto k, auto waves) {
+      with_seam_layout<T>(l, dim, [&](auto e, auto k, auto waves, auto whole) {
         constexpr int E = decltype(e)::value, K = decltype(k)::value, N = decltype(waves)::value;
-        COOP_LAUNCH(K_SEAM_GRAD, (k_seam_grad<T, S, E, K, N>), dim3((unsigned)blocks), dim3(kNormBlock<N>), 0, s, (const char*)dr, (const char*)dy,
+        const auto kernel = k_seam_grad<T, S, E, K, N, decltype(whole)::value>;
+        if (weights > 64 * 1024 - 8192) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, weights);
+        COOP_LAUNCH(K_SEAM_GRAD, kernel, dim3((unsigned)blocks), dim3(kNormBlock<N>), weights, s, (const char*)dr, (const char*)dy,
                     (const char*)x, (const char*)f, stats, wp, sh, (char*)dx, (char*)df, (char*)dgate, part);
       });
     });
