@@ -9,6 +9,7 @@
 // of the same elements, and x is read once for both.  A tile leaves its sums through LDS, so that what follows reads and writes whole rows.
 // Where there are few tiles for the chip, k is split: the parts are left in 32 bits and a second kernel adds them up, in their order, ahead
 // of the same epilogue.
+#include <atomic>
 #include <type_traits>
 #include <utility>
 
@@ -438,31 +439,36 @@ __global__ __launch_bounds__(kBlock) void k_dense_pad(Copies jobs, uint32_t bloc
   }
 }
 
+#include "dense_few.h"
 #include "dense_narrow.h"
 
 // ---- how a call is cut ------------------------------------------------------------------------------------------------------------
 // A product of rows x cols over k, in tiles of 256 x 256, what a wave's registers hold, one block to a CU, or of 128 x 128, two blocks, which
 // take as long for half as much (LDS gives them only half of what the matrix units take): the former for 16-bit operands where that is fewer
-// rounds of the chip.  k is split where there are fewer tiles than blocks that run at a time, as long as every part has four stages.
+// rounds of the chip.  k is split where there are fewer tiles than blocks that run at a time, as long as every part has four stages.  Where even so
+// half of the chip would be idle the tiles are of 64 x 64 (a pair's 64 x 128): a quarter of the work for each to do one after the other.
 struct Cut {
   int64_t rows, cols, width;  // width: of a row of parts
-  int tile;
+  int tile_a, tile_b;
   uint32_t tiles_a, tiles_b, splits;
   size_t part_bytes;
-  Cut() {}
+  Cut() : rows(0), cols(0), width(0), tile_a(0), tile_b(0), tiles_a(0), tiles_b(0), splits(0), part_bytes(0) {}
   Cut(int64_t rows_, int64_t cols_, int64_t k, int dtype, bool pair) : rows(rows_), cols(cols_) {
     const int per_tile = pair ? 2 : 1;
-    const auto tiles_of = [&](int t) { return ((cols * per_tile + t - 1) / t) * ((rows + t - 1) / t); };
-    const auto rounds_of = [&](int t, int each) { return (tiles_of(t) + 256 * each - 1) / (256 * each); };
-    tile = dtype != COOP_F32 && tiles_of(256) >= 256 && rounds_of(256, 1) < rounds_of(128, 2) ? 256 : 128;
-    tiles_a = (uint32_t)((cols * per_tile + tile - 1) / tile);
-    tiles_b = (uint32_t)((rows + tile - 1) / tile);
-    const int64_t stages = k * element_bytes(dtype) / kWide;
-    splits = (uint32_t)at_most((tile == 128 ? 512 : 256) / at_most(tiles_of(tile), 512), stages / 4 < 1 ? 1 : stages / 4);
+    const auto tiles_of = [&](int a, int b) { return ((cols * per_tile + a - 1) / a) * ((rows + b - 1) / b); };
+    const auto rounds_of = [&](int t, int each) { return (tiles_of(t, t) + 256 * each - 1) / (256 * each); };
+    const int64_t stages = k * element_bytes(dtype) / kWide, most = stages / 4 < 1 ? 1 : stages / 4;
+    const auto splits_of = [&](int a, int b) { return at_most((a == 256 ? 256 : 512) / at_most(tiles_of(a, b), 512), most); };
+    tile_a = tile_b = dtype != COOP_F32 && tiles_of(256, 256) >= 256 && rounds_of(256, 1) < rounds_of(128, 2) ? 256 : 128;
+    if (tile_a == 128 && tiles_of(128, 128) * splits_of(128, 128) <= 256) tile_a = 64, tile_b = pair ? 128 : 64;
+    tiles_a = (uint32_t)((cols * per_tile + tile_a - 1) / tile_a);
+    tiles_b = (uint32_t)((rows + tile_b - 1) / tile_b);
+    splits = (uint32_t)splits_of(tile_a, tile_b);
     width = round_up(cols, 8) * per_tile;
     part_bytes = splits > 1 ? (size_t)splits * (size_t)rows * (size_t)width * 4 : 0;
   }
   uint64_t blocks() const { return (uint64_t)tiles_a * tiles_b * splits; }
+  int64_t sum_rows(bool pair) const { return (int64_t)tiles_b * (pair && tile_a == 64 ? 4 : 2); }  // of a block's waves, those side by side along the rows
 };
 
 bool fits(const Cut& c) { return c.blocks() < ((uint64_t)1 << 31); }
@@ -494,6 +500,7 @@ struct DensePlan {
   int64_t n, k, m, kw, mw;  // kw, mw: elements of a row of k or m, up to a multiple of 16 bytes
   int64_t dz_ld;            // elements; a pair's second part begins at mw
   bool gated, pad, slope, again;  // slope: dz is not dout itself; again: the forward product is computed again
+  bool few;                       // up to 32 rows, forward: the kernel of dense_few.h
   bool narrow;                    // 8 to 128 by 8 to 128 in 16 bits: the kernels of dense_narrow.h (but not from what was kept)
   uint32_t narrow_tiles, narrow_blocks;
   Cut forward, back, weight;      // (dx and dW)
@@ -505,17 +512,18 @@ struct DensePlan {
     const int es = element_bytes(dtype), e = 16 / es;
     kw = round_up(k, e);
     mw = round_up(m, e);
-    narrow = es == 2 && !gated && k >= 8 && k <= 128 && m >= 8 && m <= 128 && !(grad && keeps && act != COOP_ACT_NONE);
+    few = !grad && n <= kFewRows;
+    narrow = !few && es == 2 && !gated && k >= 8 && k <= 128 && m >= 8 && m <= 128 && !(grad && keeps && act != COOP_ACT_NONE);
     narrow_tiles = (uint32_t)((n + 31) / 32);
     narrow_blocks = (uint32_t)(grad ? at_most((narrow_tiles + 7) / 8, 256) : at_most((narrow_tiles + kNarrowForwardWaves - 1) / kNarrowForwardWaves, 512));
-    pad = !narrow && (!aligned || kw != k);
+    pad = !narrow && !few && (!aligned || kw != k);
     size_t at = 0;
     auto take = [&](size_t b) { const size_t o = at; at += (b + 255) & ~(size_t)255; return o; };
     x = take(pad ? (size_t)n * kw * es : 0);
     w = take(pad ? (size_t)m * kw * es : 0);
     w2 = take(pad && gated ? (size_t)m * kw * es : 0);
     forward = Cut(n, m, kw, dtype, gated);
-    size_t parts = narrow ? 0 : forward.part_bytes;
+    size_t parts = narrow || few ? 0 : forward.part_bytes;
     dz = pre = part = part2 = join = 0;
     slope = again = false;
     if (grad && narrow) {
@@ -539,7 +547,7 @@ struct DensePlan {
       slope_x = (uint32_t)((packs + (1 << lanes_log2) - 1) >> lanes_log2);
       const int64_t groups = (n + (kBlock >> lanes_log2) - 1) / (kBlock >> lanes_log2);
       slope_y = (uint32_t)at_most(groups, 4096 / slope_x + 1);
-      sum_rows = again && forward.splits == 1 ? (int64_t)forward.tiles_b * 2 : (int64_t)slope_y * kWavesPerBlock;
+      sum_rows = again && forward.splits == 1 ? forward.sum_rows(gated) : (int64_t)slope_y * kWavesPerBlock;
       const size_t sum_bytes = (size_t)sum_rows * (size_t)m * 4;
       part = take(sum_bytes);
       part2 = take(gated ? sum_bytes : 0);
@@ -549,28 +557,37 @@ struct DensePlan {
     sums = take(parts);
     bytes = at + 256;
   }
-  bool fit(bool grad) const { return fits(forward) && (!grad || (fits(back) && fits(weight))); }
+  bool fit(bool grad) const { return few || narrow || (fits(forward) && (!grad || (fits(back) && fits(weight)))); }
 };
 
-// (blocks of more than 64 KB of LDS have to be allowed, once for each kernel and device; it costs a fraction of a microsecond)
-template <typename K>
-bool allow_lds(K kernel, int bytes) {
-  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess;
+// Blocks of more than 64 KB of LDS have to be allowed, once for each kernel and device.
+template <auto kernel>
+bool allow_lds(int bytes) {
+  static std::atomic<uint64_t> allowed{0};
+  int device = 0;
+  if (hipGetDevice(&device) != hipSuccess) return false;
+  const uint64_t bit = (uint64_t)1 << (device & 63);
+  if (device < 64 && (allowed.load(std::memory_order_relaxed) & bit) != 0) return true;
+  if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return false;
+  allowed.fetch_or(bit, std::memory_order_relaxed);
+  return true;
 }
 
-template <int T, int N, bool SA, bool SB, int SIZE, int FORM, typename Fin>
+template <int T, int WA, int WB, int TA, int TB, bool SA, bool SB, int SIZE, int FORM, typename Fin>
 bool launch_tiles(int id, const Cut& c, const Operand& a, const Operand& a2, const Operand& b, const Operand& b2, int64_t k, const Fin& fin, hipStream_t s) {
-  typedef Product<T, 2, 2, N, N, SA, SB, SIZE, FORM == kPair> P;
-  const auto kernel = k_dense<T, 2, 2, N, N, SA, SB, SIZE, FORM, Fin>;
-  if (!allow_lds(kernel, P::kLds)) return false;
+  typedef Product<T, WA, WB, TA, TB, SA, SB, SIZE, FORM == kPair> P;
+  constexpr auto kernel = k_dense<T, WA, WB, TA, TB, SA, SB, SIZE, FORM, Fin>;
+  if (!allow_lds<kernel>(P::kLds)) return false;
   COOP_LAUNCH(id, kernel, dim3((unsigned)c.blocks()), dim3(P::kThreads), P::kLds, s, a, a2, b, b2, k, Tiles{c.tiles_a, c.tiles_b, c.splits}, fin);
   return true;
 }
 template <int T, bool SA, bool SB, int SIZE, int FORM, typename Fin>
 bool launch_product(int id, const Cut& c, const Operand& a, const Operand& a2, const Operand& b, const Operand& b2, int64_t k, const Fin& fin, hipStream_t s) {
   if constexpr (T != COOP_F32)
-    if (c.tile == 256) return launch_tiles<T, 4, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, fin, s);
-  return launch_tiles<T, 2, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, fin, s);
+    if (c.tile_a == 256) return launch_tiles<T, 2, 2, 4, 4, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, fin, s);
+  if (c.tile_a == 128) return launch_tiles<T, 2, 2, 2, 2, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, fin, s);
+  if constexpr (FORM == kPair) return launch_tiles<T, 1, 4, 2, 1, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, fin, s);  // (a wave has columns of both)
+  else return launch_tiles<T, 2, 2, 1, 1, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, fin, s);
 }
 
 template <int T, bool PAIR, typename Fin>
@@ -657,7 +674,7 @@ bool backward_narrow(const DensePlan& p, const NarrowLayer& l, const void* dout,
     constexpr int KS = decltype(ks)::value, MT = decltype(mt)::value, lds = NarrowBackward<T, KS, MT>::kLds;
     const bool exact = p.k == KS * 16 && p.m == MT * 32 && aligned16(l.x, dout, dx);
     const auto kernel = exact ? k_narrow_grad<T, KS, MT, true> : k_narrow_grad<T, KS, MT, false>;
-    ok = allow_lds(kernel, lds);
+    ok = exact ? allow_lds<k_narrow_grad<T, KS, MT, true>>(lds) : allow_lds<k_narrow_grad<T, KS, MT, false>>(lds);
     if (ok) COOP_LAUNCH(K_DENSE_DX, kernel, dim3(p.narrow_blocks), dim3(512), lds, s, l, (const char*)dout, (char*)dx, sums, width, p.narrow_tiles);
   });
   if (!ok || sums == nullptr) return ok;
@@ -668,6 +685,12 @@ bool backward_narrow(const DensePlan& p, const NarrowLayer& l, const void* dout,
 
 template <int T, bool PAIR>
 bool forward_all(const DensePlan& p, const void* x, const void* w, const void* w2, const Forward<T, PAIR>& fin, char* ws, hipStream_t s) {
+  if (p.few) {
+    const auto kernel = p.n <= 16 ? k_few<T, 1, PAIR> : k_few<T, 2, PAIR>;
+    COOP_LAUNCH(PAIR ? K_GATED : K_LINEAR, kernel, dim3((unsigned)((p.m + 15) / 16)), dim3(kFewWaves * kWave), 0, s, (const char*)x, (const char*)w,
+                (const char*)w2, (int32_t)p.n, (int32_t)p.k, fin);
+    return true;
+  }
   if constexpr (T != COOP_F32 && !PAIR)
     if (p.narrow) {
       const NarrowLayer l{(const char*)x, (const char*)w, fin.bias, p.n, (int32_t)p.k, (int32_t)p.m, fin.alpha, fin.act};
