@@ -500,7 +500,7 @@ struct DensePlan {
   int64_t n, k, m, kw, mw;  // kw, mw: elements of a row of k or m, up to a multiple of 16 bytes
   int64_t dz_ld;            // elements; a pair's second part begins at mw
   bool gated, pad, slope, again;  // slope: dz is not dout itself; again: the forward product is computed again
-  bool few;                       // up to 32 rows, forward: the kernel of dense_few.h
+  bool few;                       // forward, of few rows or small: the kernel of dense_few.h
   bool narrow;                    // 8 to 128 by 8 to 128 in 16 bits: the kernels of dense_narrow.h (but not from what was kept)
   uint32_t narrow_tiles, narrow_blocks;
   Cut forward, back, weight;      // (dx and dW)
@@ -512,7 +512,10 @@ struct DensePlan {
     const int es = element_bytes(dtype), e = 16 / es;
     kw = round_up(k, e);
     mw = round_up(m, e);
-    few = !grad && n <= kFewRows;
+    // (its blocks read, all together and mostly from L2, some times what tiles do, which need copies for alignment and a launch that joins parts.
+    // bf16, forward: 1,021 x 602 x 75, 9 MB: 4.1 us for 12.1; 1,024 x 1,024 x 256, 48 MB: 8.8 for 10.3; 2,048 x 512 x 512, 96 MB: 13.3 both)
+    const int64_t few_bytes = ((m + 15) / 16) * ((n + kFewRows - 1) / kFewRows) * ((gated ? 32 : 16) + kFewRows) * k * es;
+    few = !grad && (n <= kFewRows || few_bytes <= 48 << 20);
     narrow = !few && es == 2 && !gated && k >= 8 && k <= 128 && m >= 8 && m <= 128 && !(grad && keeps && act != COOP_ACT_NONE);
     narrow_tiles = (uint32_t)((n + 31) / 32);
     narrow_blocks = (uint32_t)(grad ? at_most((narrow_tiles + 7) / 8, 256) : at_most((narrow_tiles + kNarrowForwardWaves - 1) / kNarrowForwardWaves, 512));
@@ -546,7 +549,7 @@ struct DensePlan {
       while (lanes_log2 < 6 && 1 << lanes_log2 < packs) ++lanes_log2;
       slope_x = (uint32_t)((packs + (1 << lanes_log2) - 1) >> lanes_log2);
       const int64_t groups = (n + (kBlock >> lanes_log2) - 1) / (kBlock >> lanes_log2);
-      slope_y = (uint32_t)at_most(groups, 4096 / slope_x + 1);
+      slope_y = (uint32_t)at_most(groups, n * m <= 1 << 19 ? 64 : 4096 / slope_x + 1);  // (of little, so few that one launch adds up what they have)
       sum_rows = again && forward.splits == 1 ? forward.sum_rows(gated) : (int64_t)slope_y * kWavesPerBlock;
       const size_t sum_bytes = (size_t)sum_rows * (size_t)m * 4;
       part = take(sum_bytes);
@@ -686,9 +689,10 @@ bool backward_narrow(const DensePlan& p, const NarrowLayer& l, const void* dout,
 template <int T, bool PAIR>
 bool forward_all(const DensePlan& p, const void* x, const void* w, const void* w2, const Forward<T, PAIR>& fin, char* ws, hipStream_t s) {
   if (p.few) {
-    const auto kernel = p.n <= 16 ? k_few<T, 1, PAIR> : k_few<T, 2, PAIR>;
-    COOP_LAUNCH(PAIR ? K_GATED : K_LINEAR, kernel, dim3((unsigned)((p.m + 15) / 16)), dim3(kFewWaves * kWave), 0, s, (const char*)x, (const char*)w,
-                (const char*)w2, (int32_t)p.n, (int32_t)p.k, fin);
+    const bool many = p.k * kElem<T> > 1024;  // (a wave has 128 bytes of a row at least)
+    const auto kernel = many ? (p.n <= 16 ? k_few<T, 1, PAIR, 16> : k_few<T, 2, PAIR, 16>) : (p.n <= 16 ? k_few<T, 1, PAIR, 4> : k_few<T, 2, PAIR, 4>);
+    COOP_LAUNCH(PAIR ? K_GATED : K_LINEAR, kernel, dim3((unsigned)((p.m + 15) / 16), (unsigned)((p.n + kFewRows - 1) / kFewRows)), dim3((many ? 16 : 4) * kWave),
+                0, s, (const char*)x, (const char*)w, (const char*)w2, p.n, (int32_t)p.k, fin);
     return true;
   }
   if constexpr (T != COOP_F32 && !PAIR)

@@ -1,9 +1,9 @@
-// Dense layers of up to 32 rows, one token first of all: bound by the weight, which is read once and straight into the matrix units' registers.
-// Included by dense.hip.
+// Dense layers forward, of few rows (one token first of all) or small altogether: operands straight from memory, of any alignment, into the matrix
+// units' registers, and one launch.  Included by dense.hip.
 //
-// A block has 16 columns of the result, so that there are blocks for every CU, and all of k: its 16 waves deal it among themselves, 128 bytes of
-// a row at a time, and their sums meet in LDS.  One launch; with k dealt to blocks in its place a second one that joins them (4,096 x 4,096 in
-// bf16, one row: 13.2 us on the GPU, 14.8 a call).
+// A block has 16 columns by 32 rows of the result, so that there are blocks for every CU, and all of k: its waves deal it among themselves, 128
+// bytes of a row at a time, and their sums meet in LDS.  Of few rows it is the weight that bounds it, and that is read once.  (4,096 x 4,096 in
+// bf16, one row: 8.1 us; tiles with k dealt to blocks, and a second launch that joins them: 13.2.)
 #pragma once
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -22,23 +22,24 @@ __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
   }
 }
 
-constexpr int kFewRows = 32, kFewWaves = 16;
+constexpr int kFewRows = 32;
 
 // NT: tiles of 16 rows of x
-template <int T, int NT, bool PAIR>
-__global__ __launch_bounds__(kFewWaves* kWave) void k_few(const char* __restrict__ x, const char* __restrict__ w, const char* __restrict__ w2, int32_t n, int32_t k,
+template <int T, int NT, bool PAIR, int WAVES>
+__global__ __launch_bounds__(WAVES* kWave) void k_few(const char* __restrict__ x, const char* __restrict__ w, const char* __restrict__ w2, int64_t n, int32_t k,
                                                            Forward<T, PAIR> fin) {
   typedef typename Element<T>::M M;
   constexpr int E = kE<T>, P = PAIR ? 2 : 1, kStep = 4 * E, kAhead = 2;  // elements of k in a step; pairs of steps on their way at a time
-  __shared__ __attribute__((aligned(16))) float part[kFewWaves][P][NT * 16][16];
+  __shared__ __attribute__((aligned(16))) float part[WAVES][P][NT * 16][16];
   const int wave = uniform_wave_in_block(), lane = lane_id(), r16 = lane & 15, quarter = lane >> 4;
   const int32_t col0 = (int32_t)blockIdx.x * 16;
+  const int64_t row0 = (int64_t)blockIdx.y * kFewRows;
   const int32_t col = col0 + r16 < fin.cols ? col0 + r16 : fin.cols - 1;  // (what is not there: the last one's, and nothing is stored)
   const int64_t ld = (int64_t)k * kElem<T>;
   const char* const from_w[2] = {w + col * ld, PAIR ? w2 + col * ld : nullptr};
   const char* from_x[NT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) from_x[t] = x + (t * 16 + r16 < n ? t * 16 + r16 : n - 1) * ld;
+  for (int t = 0; t < NT; ++t) from_x[t] = x + (row0 + t * 16 + r16 < n ? row0 + t * 16 + r16 : n - 1) * ld;
   f32x4 acc[P][NT];
 #pragma unroll
   for (int p = 0; p < P; ++p)
@@ -46,7 +47,7 @@ __global__ __launch_bounds__(kFewWaves* kWave) void k_few(const char* __restrict
     for (int t = 0; t < NT; ++t) acc[p][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int steps = k / kStep;  // whole ones
   const auto chunk = [&](const char* row, int step) { return __builtin_bit_cast(u32x4, Pack<T, E>::load(row + (int64_t)step * 64 + quarter * 16)); };
-  constexpr int kStride = kFewWaves * 2;
+  constexpr int kStride = WAVES * 2;
   for (int base = wave * 2; base < steps; base += kStride * kAhead) {
     u32x4 a[P][2 * kAhead], b[NT][2 * kAhead];
 #pragma unroll
@@ -71,7 +72,7 @@ __global__ __launch_bounds__(kFewWaves* kWave) void k_few(const char* __restrict
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[p][t] = mma16<T>(a[p][i], b[t][i], acc[p][t]);
   }
-  if (steps * kStep < k && wave == kFewWaves - 1) {  // the rest of k, by elements
+  if (steps * kStep < k && wave == WAVES - 1) {  // the rest of k, by elements
     const auto rest = [&](const char* row) {
       Pack<T, E> v;
 #pragma unroll
@@ -99,12 +100,12 @@ __global__ __launch_bounds__(kFewWaves* kWave) void k_few(const char* __restrict
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     f32x4 sum = *reinterpret_cast<const f32x4*>(&part[0][p][row][c]);
-#pragma unroll 5
-    for (int q = 1; q < kFewWaves; ++q) sum += *reinterpret_cast<const f32x4*>(&part[q][p][row][c]);
+#pragma unroll 3
+    for (int q = 1; q < WAVES; ++q) sum += *reinterpret_cast<const f32x4*>(&part[q][p][row][c]);
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[p][e] = sum[e];
   }
   typename Forward<T, PAIR>::template Lane<4> at;
   fin.begin(at, col0 + c);
-  fin.put(at, row, v[0], v[P - 1]);
+  fin.put(at, row0 + row, v[0], v[P - 1]);
 }
