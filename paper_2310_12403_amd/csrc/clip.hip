@@ -15,17 +15,21 @@ constexpr int64_t kMostPieces = (int64_t)1 << 24;
 struct Grad {
   char* p;
   int64_t n;             // elements
-  const int32_t* rows;   // null: all; else that many rows of dim elements
-  int64_t dim;
   uint32_t first_piece;  // of the launch's
-  int32_t type;
+  int16_t type;
+  int16_t touched;       // -1: all of them; else which of the launch's counts says how many
+};
+struct Touched {
+  const int32_t* rows;  // that many rows of dim elements
+  int64_t dim;
 };
 struct Grads {
-  static constexpr int kTensors = (4096 - 64) / (int)sizeof(Grad);
+  static constexpr int kTouched = 16, kTensors = (4096 - 64 - kTouched * (int)sizeof(Touched)) / (int)sizeof(Grad);
   const float* factor;
   double* part;
-  int n;
+  int n, n_touched;
   uint32_t pieces;
+  Touched touched[kTouched];
   Grad t[kTensors];
 };
 static_assert(sizeof(Grads) <= 4096, "kernel arguments");
@@ -43,8 +47,9 @@ struct Mine {
     }
     t = &g.t[lo];
     int64_t n = t->n;
-    if (t->rows != nullptr) {
-      const int64_t there = *t->rows * t->dim;
+    if (t->touched >= 0) {
+      const Touched& of = g.touched[t->touched];
+      const int64_t there = *of.rows * of.dim;
       n = there < n ? there < 0 ? 0 : there : n;
     }
     first = (int64_t)(piece - t->first_piece) * kPiece;
@@ -56,6 +61,11 @@ template <int T, typename F>
 __device__ __forceinline__ void over(char* p, int64_t first, int64_t last, F&& f) {
   constexpr int E = 16 / (int)sizeof(typename Element<T>::M);
   typedef typename Element<T>::M M;
+  if (last - first == kPiece) {  // (all of its loads are on their way at once)
+#pragma unroll
+    for (int i = 0; i < kPiece / (kBlock * E); ++i) f(std::integral_constant<int, E>(), (M*)p + first + (i * kBlock + (int)threadIdx.x) * E);
+    return;
+  }
   const int64_t whole = first + (last - first) / E * E;
 #pragma unroll 4
   for (int64_t i = first + threadIdx.x * E; i < whole; i += kBlock * E) f(std::integral_constant<int, E>(), (M*)p + i);
@@ -135,20 +145,21 @@ void in_launches(const coop_grad_tensor* tensors, int n, F&& f) {
   Grads g;
   g.factor = nullptr;
   g.part = nullptr;
-  g.n = 0;
+  g.n = g.n_touched = 0;
   g.pieces = 0;
   const auto flush = [&] {
     if (g.n > 0) f(g, blocks_of(g.pieces));
-    g.n = 0;
+    g.n = g.n_touched = 0;
     g.pieces = 0;
   };
   for (int i = 0; i < n; ++i) {
     const coop_grad_tensor& t = tensors[i];
     if (t.n_rows == 0 || t.dim == 0) continue;
     const int64_t count = t.n_rows * t.dim;
-    g.t[g.n++] = Grad{(char*)t.grad, count, t.n_rows_dev, t.dim, g.pieces, t.dtype};
+    if (t.n_rows_dev != nullptr) g.touched[g.n_touched] = Touched{t.n_rows_dev, t.dim};
+    g.t[g.n++] = Grad{(char*)t.grad, count, g.pieces, (int16_t)t.dtype, (int16_t)(t.n_rows_dev != nullptr ? g.n_touched++ : -1)};
     g.pieces += (uint32_t)((count + kPiece - 1) / kPiece);
-    if (g.n == Grads::kTensors || g.pieces >= kMostPieces) flush();
+    if (g.n == Grads::kTensors || g.n_touched == Grads::kTouched || g.pieces >= kMostPieces) flush();
   }
   flush();
 }

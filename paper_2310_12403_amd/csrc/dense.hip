@@ -558,7 +558,7 @@ struct DensePlan {
       join = take(join_y > 1 ? (size_t)join_y * (size_t)m * 4 * (gated ? 2 : 1) : 0);
     }
     sums = take(parts);
-    bytes = at + 256;
+    bytes = at;
   }
   bool fit(bool grad) const { return few || narrow || (fits(forward) && (!grad || (fits(back) && fits(weight)))); }
 };
@@ -775,7 +775,7 @@ int empty_sums(void* a, int64_t a_bytes, void* b, int64_t b_bytes, hipStream_t s
   if (b != nullptr) clear_bytes(b, b_bytes, s);
   return hipGetLastError() == hipSuccess ? COOP_OK : COOP_E_HIP;
 }
-bool workspace_ok(const void* ws, size_t bytes, size_t need) { return bytes >= need && ((uintptr_t)ws & 255) == 0; }
+bool workspace_ok(const void* ws, size_t bytes, size_t need) { return need == 0 || (bytes >= need && ((uintptr_t)ws & 255) == 0); }
 
 }  // namespace
 }  // namespace coop
@@ -792,11 +792,12 @@ extern "C" int coop_linear(const void* x, int64_t n, int32_t k, const void* weig
   const int rc = dense_check(n, k, m, dtype, act);
   if (rc != COOP_OK) return rc;
   if (n == 0) return COOP_OK;
-  if (!x || !weight || !out || !workspace) return COOP_E_NULL;
+  if (!x || !weight || !out) return COOP_E_NULL;
   for (const void* p : {x, weight, bias, residual, (const void*)out})
     if (!aligned_for(p, dtype)) return COOP_E_ARG;
   if (((uintptr_t)pre_out & 3) != 0) return COOP_E_ARG;
   const DensePlan p(n, k, m, dtype, false, aligned16(x, weight), false, false, act);
+  if (p.bytes > 0 && !workspace) return COOP_E_NULL;
   if (!p.fit(false) || !workspace_ok(workspace, workspace_bytes, p.bytes)) return COOP_E_ARG;
   bool ok = true;
   with_dtype(dtype, [&](auto t) {
@@ -819,11 +820,12 @@ extern "C" int coop_linear_grad(const void* dout, const void* x, int64_t n, int3
   if (rc != COOP_OK) return rc;
   if (grad_dtype != COOP_F32 && grad_dtype != dtype) return COOP_E_ARG;
   if ((!dx || n == 0) && !dweight && !dbias) return COOP_OK;
-  if ((n > 0 && (!dout || !x || !weight)) || !workspace) return COOP_E_NULL;
+  if (n > 0 && (!dout || !x || !weight)) return COOP_E_NULL;
   for (const void* p : {dout, x, weight, bias, (const void*)dx})
     if (!aligned_for(p, dtype)) return COOP_E_ARG;
   if (!aligned_for(dweight, grad_dtype) || (((uintptr_t)pre | (uintptr_t)dbias) & 3) != 0) return COOP_E_ARG;
   const DensePlan p(n, k, m, dtype, false, aligned16(x, weight, dout), true, pre != nullptr, act);
+  if (p.bytes > 0 && !workspace) return COOP_E_NULL;
   if (!p.fit(true) || !workspace_ok(workspace, workspace_bytes, p.bytes)) return COOP_E_ARG;
   if (n == 0) return empty_sums(dweight, (int64_t)m * k * element_bytes(grad_dtype), dbias, (int64_t)m * 4, (hipStream_t)stream);
   bool ok = true;
@@ -845,11 +847,12 @@ extern "C" int coop_gated(const void* x, int64_t n, int32_t k, const void* gate,
   const int rc = dense_check(n, k, f, dtype, act);
   if (rc != COOP_OK) return rc;
   if (n == 0) return COOP_OK;
-  if (!x || !gate || !up || !out || !workspace) return COOP_E_NULL;
+  if (!x || !gate || !up || !out) return COOP_E_NULL;
   for (const void* p : {x, gate, up, gate_bias, up_bias, (const void*)out})
     if (!aligned_for(p, dtype)) return COOP_E_ARG;
   if (((uintptr_t)pre_out & 3) != 0) return COOP_E_ARG;
   const DensePlan p(n, k, f, dtype, true, aligned16(x, gate, up), false, false, act);
+  if (p.bytes > 0 && !workspace) return COOP_E_NULL;
   if (!p.fit(false) || !workspace_ok(workspace, workspace_bytes, p.bytes)) return COOP_E_ARG;
   bool ok = true;
   with_dtype(dtype, [&](auto t) {
@@ -873,12 +876,13 @@ extern "C" int coop_gated_grad(const void* dout, const void* x, int64_t n, int32
   if (grad_dtype != COOP_F32 && grad_dtype != dtype) return COOP_E_ARG;
   if ((dgate == nullptr) != (dup == nullptr) || (dgate_bias == nullptr) != (dup_bias == nullptr)) return COOP_E_ARG;
   if ((!dx || n == 0) && !dgate && !dgate_bias) return COOP_OK;
-  if ((n > 0 && (!dout || !x || !gate || !up)) || !workspace) return COOP_E_NULL;
+  if (n > 0 && (!dout || !x || !gate || !up)) return COOP_E_NULL;
   for (const void* p : {dout, x, gate, up, gate_bias, up_bias, (const void*)dx})
     if (!aligned_for(p, dtype)) return COOP_E_ARG;
   if (!aligned_for(dgate, grad_dtype) || !aligned_for(dup, grad_dtype)) return COOP_E_ARG;
   if ((((uintptr_t)pre | (uintptr_t)dgate_bias | (uintptr_t)dup_bias) & 3) != 0) return COOP_E_ARG;
   const DensePlan p(n, k, f, dtype, true, aligned16(x, gate, up), true, pre != nullptr, act);
+  if (p.bytes > 0 && !workspace) return COOP_E_NULL;
   if (!p.fit(true) || !workspace_ok(workspace, workspace_bytes, p.bytes)) return COOP_E_ARG;
   if (n == 0) {
     const int64_t bytes = (int64_t)f * k * element_bytes(grad_dtype);

@@ -56,6 +56,10 @@ def _same(t, like, what, rows=None, dim=None):
     return p
 
 
+def _new_like(t, stream):
+    return torch.empty_like(t) if stream is None else _new(t.shape, t.dtype, t.device, stream)
+
+
 def _bias(b, n, like, what):
     return None if b is None else _vector(b, n, like.dtype, what)
 
@@ -90,7 +94,7 @@ def coop_linear_grad(dout, x, weight, bias=None, pre=None, act=COOP_ACT_NONE, al
     (n, k), m, dtype = x.shape, weight.shape[0], _DTYPES[x.dtype]
     dp = _same(dout, x, "dout", n, m)
     grad_dtype = grad_dtype or x.dtype
-    dx = _new((n, k), x.dtype, x.device, stream) if want_x else None
+    dx = _new_like(x, stream) if want_x else None
     dw = _new((m, k), grad_dtype, x.device, stream) if want_weight else None
     db = _new(m, torch.float32, x.device, stream) if want_bias else None
     need = lib().coop_linear_grad_workspace_bytes(n, k, m, dtype, act, pre is not None, (xp | wp | dp) & 15 == 0)
@@ -123,7 +127,7 @@ def coop_gated_grad(dout, x, gate, up, gate_bias=None, up_bias=None, pre=None, a
     (n, k), f, dtype = x.shape, gate.shape[0], _DTYPES[x.dtype]
     upp, dp = _same(up, x, "up", f, k), _same(dout, x, "dout", n, f)
     grad_dtype = grad_dtype or x.dtype
-    dx = _new((n, k), x.dtype, x.device, stream) if want_x else None
+    dx = _new_like(x, stream) if want_x else None
     dw = [_new((f, k), grad_dtype, x.device, stream) for _ in range(2)] if want_weight else [None] * 2
     db = [_new(f, torch.float32, x.device, stream) for _ in range(2)] if want_bias else [None] * 2
     need = lib().coop_gated_grad_workspace_bytes(n, k, f, dtype, pre is not None, (xp | gp | upp) & 15 == 0)
@@ -156,9 +160,9 @@ def coop_residual_norm(x, f, gate=None, alpha=1.0, after=True, after_weight=None
     xp = _matrix(x, "x", n, dim)
     assert x.dtype in (torch.float32, f.dtype), "x: fp32 or f's type"
     if out is None:
-        out = _new((n, dim), x.dtype, x.device, stream)
+        out = _new_like(x, stream)
     op = _same(out, x, "out", n, dim)
-    y = _new((n, dim), f.dtype, x.device, stream) if before else None
+    y = _new_like(f, stream) if before else None
     stats = _new((4, n), torch.float32, x.device, stream)
     _check(lib().coop_residual_norm(xp, fp, n, dim, _DTYPES[f.dtype], _DTYPES[x.dtype], gp, form, alpha, norms, *ps, weight_dtype, eps, op,
                                     y.data_ptr() if before else None, stats.data_ptr(), _stream_ptr(stream)))
@@ -177,7 +181,7 @@ def coop_residual_norm_grad(dr, dy, x, f, stats, gate=None, alpha=1.0, after=Tru
     yp = _same(dy, f, "dy", n, dim) if before else None
     assert before or dr is not None, "without the norm in front of the next block r's gradient is all there is"
     assert stats.is_cuda and stats.is_contiguous() and stats.dtype == torch.float32 and tuple(stats.shape) == (4, n), "stats: as coop_residual_norm gives them"
-    dx, df = _new((n, dim), x.dtype, x.device, stream), _new((n, dim), f.dtype, x.device, stream)
+    dx, df = _new_like(x, stream), _new_like(f, stream)
     dgate = None if gate is None else _new(gate.shape, torch.float32 if form == 1 else f.dtype, x.device, stream)
     there = (after, after and not rms, before, before and not rms)
     grads = [_new(dim, torch.float32, x.device, stream) if want_weight and t else None for t in there]

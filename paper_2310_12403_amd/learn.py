@@ -76,9 +76,10 @@ def _scratch(shape, dtype, device, stream):
 
 
 def _new(shape, dtype, device, stream):
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
     t = _scratch(shape, dtype, device, stream)
-    if stream is not None:
-        t.record_stream(torch.cuda.current_stream(device))
+    t.record_stream(torch.cuda.current_stream(device))
     return t
 
 
