@@ -441,6 +441,7 @@ __global__ __launch_bounds__(kBlock) void k_dense_pad(Copies jobs, uint32_t bloc
 
 #include "dense_few.h"
 #include "dense_narrow.h"
+#include "dense_small.h"
 
 // ---- how a call is cut ------------------------------------------------------------------------------------------------------------
 // A product of rows x cols over k, in tiles of 256 x 256, what a wave's registers hold, one block to a CU, or of 128 x 128, two blocks, which
@@ -501,6 +502,7 @@ struct DensePlan {
   int64_t dz_ld;            // elements; a pair's second part begins at mw
   bool gated, pad, slope, again;  // slope: dz is not dout itself; again: the forward product is computed again
   bool few;                       // forward, of few rows or small: the kernel of dense_few.h
+  bool small;                     // gradient, of what is small: the kernels of dense_small.h
   bool narrow;                    // 8 to 128 by 8 to 128 in 16 bits: the kernels of dense_narrow.h (but not from what was kept)
   uint32_t narrow_tiles, narrow_blocks;
   Cut forward, back, weight;      // (dx and dW)
@@ -512,14 +514,22 @@ struct DensePlan {
     const int es = element_bytes(dtype), e = 16 / es;
     kw = round_up(k, e);
     mw = round_up(m, e);
-    // (its blocks read, all together and mostly from L2, some times what tiles do, which need copies for alignment and a launch that joins parts.
-    // bf16, forward: 1,021 x 602 x 75, 9 MB: 4.1 us for 12.1; 1,024 x 1,024 x 256, 48 MB: 8.8 for 10.3; 2,048 x 512 x 512, 96 MB: 13.3 both)
-    const int64_t few_bytes = ((m + 15) / 16) * ((n + kFewRows - 1) / kFewRows) * ((gated ? 32 : 16) + kFewRows) * k * es;
-    few = !grad && (n <= kFewRows || few_bytes <= 48 << 20);
-    narrow = !few && es == 2 && !gated && k >= 8 && k <= 128 && m >= 8 && m <= 128 && !(grad && keeps && act != COOP_ACT_NONE);
+    // Its blocks read, all together and mostly from L2, some times what tiles do, which need copies for alignment and a launch that joins parts; and
+    // there may not be many more than run at a time.  (bf16, forward: 1,021 x 602 x 75, 9 MB: 4.1 us for 12.1; 1,024 x 1,024 x 256, 48 MB: 8.8 for
+    // 10.3; 2,048 x 512 x 512, 96 MB: 13.3 both)
+    const auto little = [&](int64_t blocks, int64_t rows, int64_t length, int64_t most) { return blocks <= most && blocks * rows * length * es <= 48 << 20; };
+    const int64_t n_tiles = (n + kFewRows - 1) / kFewRows, k_tiles = (k + 15) / 16, both = gated ? 2 * mw : m;
+    const bool few_fits = little((m + 15) / 16 * n_tiles, (gated ? 32 : 16) + kFewRows, k, (int64_t)k * es > kFewMany ? 2048 : 8192);
+    few = !grad && (n <= kFewRows || few_fits);
+    // (its gradient, kept products: 1,024 x 256 x 256 13.8 us for 20.5, 1,021 x 602 x 75 19.8 for 23.0, 64 x 1,024 x 1,024 21.8 for 18.4; and 2 launches
+    // for 6, 3 us each to whoever launches them)
+    again = grad && !keeps && (gated || act != COOP_ACT_NONE);
+    small = grad && n * es <= kSmallLength && both * es <= kSmallLength && little(k_tiles * n_tiles, 16 + kSmallRows, both, 2048) &&
+            little(k_tiles * ((both + kSmallRows - 1) / kSmallRows), 16 + kSmallRows, n, 2048) && (!again || few_fits);
+    narrow = !few && !small && es == 2 && !gated && k >= 8 && k <= 128 && m >= 8 && m <= 128 && !(grad && keeps && act != COOP_ACT_NONE);
     narrow_tiles = (uint32_t)((n + 31) / 32);
     narrow_blocks = (uint32_t)(grad ? at_most((narrow_tiles + 7) / 8, 256) : at_most((narrow_tiles + kNarrowForwardWaves - 1) / kNarrowForwardWaves, 512));
-    pad = !narrow && !few && (!aligned || kw != k);
+    pad = !narrow && !few && !small && (!aligned || kw != k);
     size_t at = 0;
     auto take = [&](size_t b) { const size_t o = at; at += (b + 255) & ~(size_t)255; return o; };
     x = take(pad ? (size_t)n * kw * es : 0);
@@ -528,39 +538,38 @@ struct DensePlan {
     forward = Cut(n, m, kw, dtype, gated);
     size_t parts = narrow || few ? 0 : forward.part_bytes;
     dz = pre = part = part2 = join = 0;
-    slope = again = false;
+    slope = false;
     if (grad && narrow) {
       parts = (size_t)narrow_blocks * (size_t)narrow_shares(k, m) * (size_t)m * (size_t)(round_up(k, 8) + kNarrowSums) * 4;
     } else if (grad) {
-      again = !keeps && (gated || act != COOP_ACT_NONE);
-      slope = gated || act != COOP_ACT_NONE || !aligned || mw != m;
+      slope = gated || act != COOP_ACT_NONE || (!small && (!aligned || mw != m));
       dz_ld = gated ? 2 * mw : mw;
       if (dz_ld * es % 2048 == 0) dz_ld += 256 / es;  // (or a tile's rows would all lie in the same few channels of memory)
       dz = take(slope ? (size_t)n * dz_ld * es : 0);
-      pre = take(again && forward.splits > 1 ? (size_t)n * m * 4 * (gated ? 2 : 1) : 0);
+      pre = take(again && !small && forward.splits > 1 ? (size_t)n * m * 4 * (gated ? 2 : 1) : 0);
       back = Cut(n, k, mw, dtype, false);
       weight = Cut(gated ? 2 * mw : m, k, n, dtype, false);
-      if (!again) parts = 0;
-      if (back.part_bytes > parts) parts = back.part_bytes;
-      if (weight.part_bytes > parts) parts = weight.part_bytes;
+      if (!again || small) parts = 0;
+      if (!small && back.part_bytes > parts) parts = back.part_bytes;
+      if (!small && weight.part_bytes > parts) parts = weight.part_bytes;
       // the columns' sums: by the product's waves of rows, or by the blocks that go over the rows
       const int64_t packs = mw / e;
       lanes_log2 = 0;
       while (lanes_log2 < 6 && 1 << lanes_log2 < packs) ++lanes_log2;
       slope_x = (uint32_t)((packs + (1 << lanes_log2) - 1) >> lanes_log2);
       const int64_t groups = (n + (kBlock >> lanes_log2) - 1) / (kBlock >> lanes_log2);
-      slope_y = (uint32_t)at_most(groups, n * m <= 1 << 19 ? 64 : 4096 / slope_x + 1);  // (of little, so few that one launch adds up what they have)
-      sum_rows = again && forward.splits == 1 ? forward.sum_rows(gated) : (int64_t)slope_y * kWavesPerBlock;
+      slope_y = (uint32_t)at_most(groups, small ? 128 : n * m <= 1 << 19 ? 64 : 4096 / slope_x + 1);  // (of little, so few that one launch adds up what they have)
+      sum_rows = again && small ? (n + kSmallRows - 1) / kSmallRows * 2 : again && forward.splits == 1 ? forward.sum_rows(gated) : (int64_t)slope_y * kWavesPerBlock;
       const size_t sum_bytes = (size_t)sum_rows * (size_t)m * 4;
       part = take(sum_bytes);
       part2 = take(gated ? sum_bytes : 0);
-      join_y = (uint32_t)at_most(sum_rows / 256, 64);
+      join_y = small ? 1 : (uint32_t)at_most(sum_rows / 256, 64);
       join = take(join_y > 1 ? (size_t)join_y * (size_t)m * 4 * (gated ? 2 : 1) : 0);
     }
     sums = take(parts);
     bytes = at;
   }
-  bool fit(bool grad) const { return few || narrow || (fits(forward) && (!grad || (fits(back) && fits(weight)))); }
+  bool fit(bool grad) const { return few || small || narrow || (fits(forward) && (!grad || (fits(back) && fits(weight)))); }
 };
 
 // Blocks of more than 64 KB of LDS have to be allowed, once for each kernel and device.
@@ -640,6 +649,14 @@ bool forward_product(const DensePlan& p, const Arrays& o, const Fin& fin, float*
   return product<T, false, false, kWide, PAIR ? kPair : kOne>(PAIR ? K_GATED : K_LINEAR, p.forward, a, a, b, b, p.kw, fin, sums, s);
 }
 
+template <int T, bool PAIR, typename Fin>
+void few_product(const DensePlan& p, const void* x, const void* w, const void* w2, const Fin& fin, hipStream_t s) {
+  const bool many = p.k * kElem<T> > kFewMany, one = !Fin::kSums && p.n <= 16;
+  const auto kernel = many ? (one ? k_few<T, 1, PAIR, 16, Fin> : k_few<T, 2, PAIR, 16, Fin>) : (one ? k_few<T, 1, PAIR, 4, Fin> : k_few<T, 2, PAIR, 4, Fin>);
+  COOP_LAUNCH(PAIR ? K_GATED : K_LINEAR, kernel, dim3((unsigned)((p.m + 15) / 16), (unsigned)((p.n + kFewRows - 1) / kFewRows)), dim3((many ? 16 : 4) * kWave), 0, s,
+              (const char*)x, (const char*)w, (const char*)w2, p.n, (int32_t)p.k, fin);
+}
+
 template <int T>
 void sums_of_columns(const DensePlan& p, const float* from, const float* from2, float* db, float* db2, bool pair, char* ws, hipStream_t s) {
   int64_t rows = p.sum_rows;
@@ -689,10 +706,7 @@ bool backward_narrow(const DensePlan& p, const NarrowLayer& l, const void* dout,
 template <int T, bool PAIR>
 bool forward_all(const DensePlan& p, const void* x, const void* w, const void* w2, const Forward<T, PAIR>& fin, char* ws, hipStream_t s) {
   if (p.few) {
-    const bool many = p.k * kElem<T> > 1024;  // (a wave has 128 bytes of a row at least)
-    const auto kernel = many ? (p.n <= 16 ? k_few<T, 1, PAIR, 16> : k_few<T, 2, PAIR, 16>) : (p.n <= 16 ? k_few<T, 1, PAIR, 4> : k_few<T, 2, PAIR, 4>);
-    COOP_LAUNCH(PAIR ? K_GATED : K_LINEAR, kernel, dim3((unsigned)((p.m + 15) / 16), (unsigned)((p.n + kFewRows - 1) / kFewRows)), dim3((many ? 16 : 4) * kWave),
-                0, s, (const char*)x, (const char*)w, (const char*)w2, p.n, (int32_t)p.k, fin);
+    few_product<T, PAIR>(p, x, w, w2, fin, s);
     return true;
   }
   if constexpr (T != COOP_F32 && !PAIR)
@@ -722,7 +736,7 @@ bool backward_all(const DensePlan& p, const void* dout, const void* x, const voi
   const bool products = dx != nullptr || dw != nullptr;
   float* const sums = (float*)(ws + p.sums);
   Arrays o{(const char*)x, (const char*)w, (const char*)w2};
-  if (products || p.again) o = operands<T>(p, x, w, w2, dw != nullptr || p.again, ws, s);
+  if (!p.small && (products || p.again)) o = operands<T>(p, x, w, w2, dw != nullptr || p.again, ws, s);
   Slope<T, PAIR> fin;
   fin.bias = (const char*)bias, fin.bias2 = (const char*)bias2, fin.dout = (const char*)dout;
   fin.dz = p.slope && products ? ws + p.dz : nullptr;
@@ -730,7 +744,9 @@ bool backward_all(const DensePlan& p, const void* dout, const void* x, const voi
   fin.part2 = (float*)(ws + p.part2);
   fin.rows = p.n, fin.ld = p.dz_ld, fin.second = p.mw, fin.cols = (int32_t)p.m;
   fin.alpha = alpha, fin.act = act;
-  if (p.again && p.forward.splits == 1) {
+  if (p.again && p.small) {
+    few_product<T, PAIR>(p, x, w, w2, fin, s);
+  } else if (p.again && p.forward.splits == 1) {
     if (!forward_product<T, PAIR>(p, o, fin, sums, s)) return false;
   } else {
     if (p.again) {
@@ -740,6 +756,17 @@ bool backward_all(const DensePlan& p, const void* dout, const void* x, const voi
     }
     if (fin.dz != nullptr || fin.part != nullptr)
       COOP_LAUNCH(K_DENSE_SLOPE, (k_dense_slope<T, PAIR>), dim3(p.slope_x, p.slope_y), dim3(kBlock), 0, s, pre, PAIR ? pre + p.n * p.m : nullptr, p.lanes_log2, fin);
+  }
+  if (p.small) {
+    const float scale = PAIR || act != COOP_ACT_NONE ? 1.f : alpha;
+    const int64_t ld = (p.slope ? p.dz_ld : p.m) * kElem<T>, both = PAIR ? p.mw + p.m : p.m;
+    const uint32_t k_tiles = (uint32_t)((p.k + 15) / 16), n_tiles = (uint32_t)((p.n + kSmallRows - 1) / kSmallRows), m_tiles = (uint32_t)((both + kSmallRows - 1) / kSmallRows);
+    const SmallGrad g{p.slope ? ws + p.dz : (const char*)dout, (const char*)x, (const char*)w, (const char*)w2, p.n, ld, p.mw, (int32_t)p.k, (int32_t)p.m,
+                      dx != nullptr ? k_tiles * n_tiles : 0, dw != nullptr ? k_tiles * m_tiles : 0, k_tiles, fin.part, fin.part2, p.sum_rows, db, db2};
+    const Gradient to_x{(char*)dx, nullptr, p.n, 0, (int32_t)p.k, scale, T}, to_w{(char*)dw, PAIR ? (char*)dw2 : nullptr, p.m, p.mw, (int32_t)p.k, scale, grad_dtype};
+    const uint32_t blocks = g.dx_blocks + g.dw_blocks + (fin.part != nullptr ? (uint32_t)((p.m + kWave - 1) / kWave) * (PAIR ? 2 : 1) : 0);
+    if (blocks > 0) COOP_LAUNCH(K_DENSE_DX, (k_small_grad<T, PAIR>), dim3(blocks), dim3(kSmallWaves * kWave), 0, s, g, to_x, to_w);
+    return true;
   }
   if (fin.part != nullptr) sums_of_columns<T>(p, fin.part, fin.part2, db, db2, PAIR, ws, s);
   const int64_t ldk = p.kw * kElem<T>, ldz = p.slope ? p.dz_ld * kElem<T> : p.m * kElem<T>;

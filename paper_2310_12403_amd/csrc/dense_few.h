@@ -22,12 +22,13 @@ __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
   }
 }
 
-constexpr int kFewRows = 32;
+constexpr int kFewRows = 32, kFewMany = 1024;  // bytes of a row from which on a block has 16 waves, of less 4: a wave has 128 bytes at least
 
 // NT: tiles of 16 rows of x
-template <int T, int NT, bool PAIR, int WAVES>
+// Fin: what becomes of the sums (Slope's columns: a part for every 16 rows)
+template <int T, int NT, bool PAIR, int WAVES, typename Fin>
 __global__ __launch_bounds__(WAVES* kWave) void k_few(const char* __restrict__ x, const char* __restrict__ w, const char* __restrict__ w2, int64_t n, int32_t k,
-                                                           Forward<T, PAIR> fin) {
+                                                           Fin fin) {
   typedef typename Element<T>::M M;
   constexpr int E = kE<T>, P = PAIR ? 2 : 1, kStep = 4 * E, kAhead = 2;  // elements of k in a step; pairs of steps on their way at a time
   __shared__ __attribute__((aligned(16))) float part[WAVES][P][NT * 16][16];
@@ -105,7 +106,8 @@ __global__ __launch_bounds__(WAVES* kWave) void k_few(const char* __restrict__ x
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[p][e] = sum[e];
   }
-  typename Forward<T, PAIR>::template Lane<4> at;
+  typename Fin::template Lane<4> at;
   fin.begin(at, col0 + c);
   fin.put(at, row0 + row, v[0], v[P - 1]);
+  if constexpr (Fin::kSums) fin.end(at, 4, (int64_t)blockIdx.y * NT + wave);
 }

@@ -1,0 +1,158 @@
+// The gradient of a dense layer that is small altogether, where launches cost more than products: one kernel makes dz (or none, where it is dout),
+// and one has the input's gradient, the weight's and the bias's in blocks of their own.  Included by dense.hip.
+//
+// As in dense_few.h a block has 16 columns by 32 rows of a result and its 16 waves deal the common dimension among themselves.  An operand that
+// has that dimension as its row number comes 16 bytes of a row at a time, 16 columns of a step, and is turned in the wave's own LDS.
+#pragma once
+
+struct SmallGrad {
+  const char *dz, *x, *w, *w2;
+  int64_t n, ld, second;  // dz: bytes of a row, elements from a pair's first part to its second
+  int32_t k, m;
+  uint32_t dx_blocks, dw_blocks, k_tiles;  // (and behind them 64 columns of the bias's gradient a block)
+  const float *part, *part2;
+  int64_t part_rows;
+  float *db, *db2;
+};
+
+// kSmallLength: bytes of the common dimension, 6 steps for each wave (longer ones take too long in the few blocks of a weight's gradient: 8,192 rows of 64,
+// 36.6 us for the 16.2 of dense_narrow.h)
+constexpr int kSmallWaves = 16, kSmallRows = 32, kSmallLength = 6 * kSmallWaves * 64;
+
+// 16 bytes of a row from column `col` on, zeros behind column `dim`
+template <int T>
+__device__ __forceinline__ u32x4 load_some(const char* row, int64_t col, int64_t dim) {
+  typedef typename Element<T>::M M;
+  constexpr int E = kE<T>;
+  if (col + E <= dim) return __builtin_bit_cast(u32x4, Pack<T, E>::load((const M*)row + col));
+  Pack<T, E> v;
+#pragma unroll
+  for (int e = 0; e < E; ++e) v.x[e] = col + e < dim ? ((const M*)row)[col + e] : (M)0.f;
+  return __builtin_bit_cast(u32x4, v);
+}
+
+// What a lane loads of a step of an operand whose rows are the common dimension, and the fragment that it is (lds: the wave's kilobyte).
+template <int T>
+__device__ __forceinline__ u32x4 load_strided(const char* base, int64_t ld, int64_t row0, int64_t rows, int64_t col0, int64_t dim) {
+  constexpr int E = kE<T>, kEach = 16 / E;  // lanes of a row
+  const int64_t r = row0 + lane_id() / kEach;
+  return r < rows ? load_some<T>(base + r * ld, col0 + lane_id() % kEach * E, dim) : u32x4{0, 0, 0, 0};
+}
+template <int T>
+__device__ __forceinline__ u32x4 turned(char* lds, u32x4 v) {
+  const int lane = lane_id(), t = lane & 15, quarter = lane >> 4;
+  asm volatile("" ::: "memory");  // (a wave's reads and writes of LDS are done in their order)
+  *reinterpret_cast<u32x4*>(lds + lane * 16) = v;
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  u32x4 f;
+  if constexpr (T == COOP_F32) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = *reinterpret_cast<const uint32_t*>(lds + (quarter * 4 + j) * 64 + t * 4);
+  } else {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const char* at = lds + (quarter * 8 + q * 4 + (t >> 2)) * 32 + (t & 3) * 8;
+      const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(LdsByte*)at));
+      f[2 * q] = y[0];
+      f[2 * q + 1] = y[1];
+    }
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  return f;
+}
+
+template <int T, bool PAIR>
+__global__ __launch_bounds__(kSmallWaves* kWave) void k_small_grad(SmallGrad g, Gradient to_x, Gradient to_w) {
+  constexpr int E = kE<T>, kStep = 4 * E, kAhead = 2;
+  __shared__ __attribute__((aligned(16))) char lds[kSmallWaves * 3 * 1024];
+  static_assert(kSmallWaves * kSmallRows * 16 * 4 <= (int)sizeof(lds), "the sums lie where the fragments did");
+  const int wave = uniform_wave_in_block(), lane = lane_id(), r16 = lane & 15, quarter = lane >> 4;
+  char* const own = lds + wave * 3 * 1024;
+  uint32_t block = blockIdx.x;
+  if (block >= g.dx_blocks + g.dw_blocks) {  // the bias's gradient: the waves deal the parts' rows
+    block -= g.dx_blocks + g.dw_blocks;
+    const uint32_t each = (uint32_t)((g.m + kWave - 1) / kWave);
+    const bool second = block >= each;
+    const float* part = second ? g.part2 : g.part;
+    const int32_t c = (int32_t)(second ? block - each : block) * kWave + lane;
+    float(*const sums)[kWave] = reinterpret_cast<float(*)[kWave]>(lds);
+    float sum = 0.f;
+    if (c < g.m) {
+#pragma unroll 8
+      for (int64_t r = wave; r < g.part_rows; r += kSmallWaves) sum += part[r * g.m + c];
+    }
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave != 0 || c >= g.m) return;
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kSmallWaves; ++w) sum += sums[w][lane];
+    (second ? g.db2 : g.db)[c] = sum;
+    return;
+  }
+  const bool of_x = block < g.dx_blocks;
+  if (!of_x) block -= g.dx_blocks;
+  const int64_t col0 = (int64_t)(block % g.k_tiles) * 16, row0 = (int64_t)(block / g.k_tiles) * kSmallRows, ldk = (int64_t)g.k * kElem<T>;
+  f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+  if (of_x) {  // dz by its rows, the weight turned
+    const char* rows[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int64_t r = row0 + t * 16 + r16;
+      rows[t] = g.dz + (r < g.n ? r : g.n - 1) * g.ld;  // (what is not there: the last one's, and nothing is stored)
+    }
+    const int steps = (g.m + kStep - 1) / kStep, all = PAIR ? 2 * steps : steps;
+    for (int first = wave; first < all; first += kSmallWaves * kAhead) {
+      u32x4 a[kAhead], b[kAhead][2];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        int s = first + i * kSmallWaves;
+        const bool there = s < all, other = PAIR && s >= steps;
+        if (other) s -= steps;
+        a[i] = there ? load_strided<T>(other ? g.w2 : g.w, ldk, (int64_t)s * kStep, g.m, col0, g.k) : u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          b[i][t] = there ? load_some<T>(rows[t] + (other ? g.second * kElem<T> : 0), (int64_t)s * kStep + quarter * E, g.m) : u32x4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const u32x4 f = turned<T>(own, a[i]);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) acc[t] = mma16<T>(f, b[i][t], acc[t]);
+      }
+    }
+  } else {  // x and dz turned
+    const int64_t steps = (g.n + kStep - 1) / kStep, cols = PAIR ? g.second + g.m : g.m;
+    for (int64_t first = wave; first < steps; first += kSmallWaves * kAhead) {
+      u32x4 a[kAhead], b[kAhead][2];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int64_t s = first + i * kSmallWaves;  // (behind the last one: rows that are not there)
+        a[i] = load_strided<T>(g.x, ldk, s * kStep, g.n, col0, g.k);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) b[i][t] = load_strided<T>(g.dz, g.ld, s * kStep, g.n, row0 + t * 16, cols);
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const u32x4 f = turned<T>(own, a[i]);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) acc[t] = mma16<T>(f, turned<T>(own + (1 + t) * 1024, b[i][t]), acc[t]);
+      }
+    }
+  }
+  __syncthreads();
+  float(*const sums)[kSmallRows][16] = reinterpret_cast<float(*)[kSmallRows][16]>(lds);
+#pragma unroll
+  for (int t = 0; t < 2; ++t) *reinterpret_cast<f32x4*>(&sums[wave][t * 16 + r16][quarter * 4]) = acc[t];
+  __syncthreads();
+  if (threadIdx.x >= kSmallRows * 4) return;
+  const int row = threadIdx.x >> 2, c = (threadIdx.x & 3) * 4;
+  f32x4 sum = *reinterpret_cast<const f32x4*>(&sums[0][row][c]);
+#pragma unroll 3
+  for (int q = 1; q < kSmallWaves; ++q) sum += *reinterpret_cast<const f32x4*>(&sums[q][row][c]);
+  float v[4] = {sum[0], sum[1], sum[2], sum[3]}, none[4] = {0.f, 0.f, 0.f, 0.f};
+  const Gradient& fin = of_x ? to_x : to_w;
+  typename Gradient::Lane<4> at;
+  fin.begin(at, (int32_t)col0 + c);
+  fin.put(at, row0 + row, v, none);
+}
