@@ -521,11 +521,11 @@ struct DensePlan {
     const int64_t n_tiles = (n + kFewRows - 1) / kFewRows, k_tiles = (k + 15) / 16, both = gated ? 2 * mw : m;
     const bool few_fits = little((m + 15) / 16 * n_tiles, (gated ? 32 : 16) + kFewRows, k, (int64_t)k * es > kFewMany ? 2048 : 8192);
     few = !grad && (n <= kFewRows || few_fits);
-    // (its gradient, kept products: 1,024 x 256 x 256 13.8 us for 20.5, 1,021 x 602 x 75 19.8 for 23.0, 64 x 1,024 x 1,024 21.8 for 18.4; and 2 launches
+    // (its gradient, kept products: 1,024 x 256 x 256 11.0 us for 20.5, 1,021 x 602 x 75 12.9 for 23.0, 64 x 1,024 x 1,024 16.3 for 18.4; and 2 launches
     // for 6, 3 us each to whoever launches them)
     again = grad && !keeps && (gated || act != COOP_ACT_NONE);
-    small = grad && n * es <= kSmallLength && both * es <= kSmallLength && little(k_tiles * n_tiles, 16 + kSmallRows, both, 2048) &&
-            little(k_tiles * ((both + kSmallRows - 1) / kSmallRows), 16 + kSmallRows, n, 2048) && (!again || few_fits);
+    small = grad && n * es <= kSmallLength && both * es <= kSmallLength && little(k_tiles * n_tiles, 16 + kSmallRows, both, 4096) &&
+            little(k_tiles * ((both + kSmallRows - 1) / kSmallRows), 16 + kSmallRows, n, 4096) && (!again || few_fits);
     narrow = !few && !small && es == 2 && !gated && k >= 8 && k <= 128 && m >= 8 && m <= 128 && !(grad && keeps && act != COOP_ACT_NONE);
     narrow_tiles = (uint32_t)((n + 31) / 32);
     narrow_blocks = (uint32_t)(grad ? at_most((narrow_tiles + 7) / 8, 256) : at_most((narrow_tiles + kNarrowForwardWaves - 1) / kNarrowForwardWaves, 512));

@@ -1,7 +1,7 @@
 // The gradient of a dense layer that is small altogether, where launches cost more than products: one kernel makes dz (or none, where it is dout),
 // and one has the input's gradient, the weight's and the bias's in blocks of their own.  Included by dense.hip.
 //
-// As in dense_few.h a block has 16 columns by 32 rows of a result and its 16 waves deal the common dimension among themselves.  An operand that
+// As in dense_few.h a block has 16 columns by 32 rows of a result and its waves deal the common dimension among themselves.  An operand that
 // has that dimension as its row number comes 16 bytes of a row at a time, 16 columns of a step, and is turned in the wave's own LDS.
 #pragma once
 
@@ -15,9 +15,10 @@ struct SmallGrad {
   float *db, *db2;
 };
 
-// kSmallLength: bytes of the common dimension, 6 steps for each wave (longer ones take too long in the few blocks of a weight's gradient: 8,192 rows of 64,
-// 36.6 us for the 16.2 of dense_narrow.h)
-constexpr int kSmallWaves = 16, kSmallRows = 32, kSmallLength = 6 * kSmallWaves * 64;
+// kSmallLength: bytes of the common dimension, 12 steps for each wave (longer ones take too long in the few blocks of a weight's gradient: 8,192 rows
+// of 64 by 64, 36.6 us for the 16.2 of dense_narrow.h).  8 waves for 16, which are idle where it is short: bf16 1,024 x 256 x 256 11.0 us for 13.1,
+// 256 x 1,024 x 512 13.1 for 19.9; 4: 12.5 and 12.5, and 31.5 for 26.4 with 3,001 rows.
+constexpr int kSmallWaves = 8, kSmallRows = 32, kSmallLength = 12 * 8 * 64;
 
 // 16 bytes of a row from column `col` on, zeros behind column `dim`
 template <int T>
@@ -90,8 +91,8 @@ __global__ __launch_bounds__(kSmallWaves* kWave) void k_small_grad(SmallGrad g, 
     (second ? g.db2 : g.db)[c] = sum;
     return;
   }
-  const bool of_x = block < g.dx_blocks;
-  if (!of_x) block -= g.dx_blocks;
+  const bool of_x = block >= g.dw_blocks;  // (the weight's first: they take longer)
+  if (of_x) block -= g.dw_blocks;
   const int64_t col0 = (int64_t)(block % g.k_tiles) * 16, row0 = (int64_t)(block / g.k_tiles) * kSmallRows, ldk = (int64_t)g.k * kElem<T>;
   f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
   if (of_x) {  // dz by its rows, the weight turned
