@@ -111,6 +111,16 @@ inline int seam_lds(const SeamWeightPointers& wp, bool columns, int32_t dim) {
   return n * ((dim + 3) & ~3) * 4;
 }
 
+// What a row's other lanes write to when its last pack overlaps the one in front, in place: it is here before the lanes meet.  (Within a wave loads
+// and stores are in order.)
+template <bool WHOLE, int WAVES, int E>
+__device__ __forceinline__ void arrived(float (&v)[E]) {
+  if constexpr (!WHOLE && WAVES > 1) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) asm volatile("" : "+v"(v[e]));
+  }
+}
+
 // mean and 1 / size of a row, and v left as v - mean (root mean square: mean 0)
 template <int E, int K, int WAVES, bool WHOLE>
 __device__ __forceinline__ void row_statistics(float (&v)[K][E], const Rows<WAVES>& rows, int lanes, const SeamShape& sh, RowSums<WAVES>& sums, float* mean_out,
@@ -176,6 +186,7 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) __attribute__((amdgpu_waves_per_
     for (int k = 0; k < K; ++k) {
       const Columns<E> c(rows.lane + k * lanes, sh.dim);
       next_x.get(k, v[k]);
+      arrived<WHOLE, WAVES>(v[k]);
       next_f.get(k, p[k]);
       if (sh.gate == kRowGate) next_g.get(k, g[k]);
       else gate_of.get(c.at, g[k]);
@@ -283,8 +294,10 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) __attribute__((amdgpu_waves_per_
       if (sh.before) next_x.get(k, h2[k]), next_dy.get(k, t[k]);
       if (sh.gate == kRowGate) next_g.get(k, g[k]);
       else gate_of.get(c.at, g[k]);
-      if (dr != nullptr) next_dr.get(k, d[k]);
-      else {
+      if (dr != nullptr) {
+        next_dr.get(k, d[k]);
+        arrived<WHOLE, WAVES>(d[k]);
+      } else {
 #pragma unroll
         for (int e = 0; e < E; ++e) d[k][e] = 0.f;
       }

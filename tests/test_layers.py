@@ -368,3 +368,494 @@ def test_grad_norm_of_touched_rows_and_the_step_that_it_scales():
     assert float(grad[k:].min()) == float(torch.tensor(1e9)) and abs(float(P.GradNorm([(grad, count), dense]).measure()[0]) - 1.0) < 1e-2
     opts[1].step(1, 1e-2, rows={0: (rows, grad, count)})
     assert torch.equal(tables[0], tables[1])
+
+
+# ---- every path of them: streams, graphs, workspaces, memory, rows by themselves -------------------------------------------------------
+# (small, few rows; narrow, whole and ragged; tiles of 64, of 128 with k split, of 256)
+PATHS = [(torch.bfloat16, 24, 64, 96), (torch.float32, 500, 70, 33), (torch.bfloat16, 40000, 128, 64), (torch.float16, 40000, 100, 77), (torch.float32, 4000, 72, 80),
+         (torch.float16, 3500, 300, 520), (torch.bfloat16, 4100, 520, 4100), (torch.float32, 7, 3000, 40)]
+
+
+def dense_calls(dtype, n, k, m, seed=0):
+    """The calls' arguments, and f(stream, workspace of bytes) that makes all of them"""
+    g = rng(seed + n)
+    x, w, w2 = normal(g, n, k, dtype=dtype), normal(g, m, k, dtype=dtype, scale=k ** -0.5), normal(g, m, k, dtype=dtype, scale=k ** -0.5)
+    b, res, dy = normal(g, m, dtype=dtype), normal(g, n, m, dtype=dtype), normal(g, n, m, dtype=dtype)
+
+    def everything(stream=None, ws=lambda need: None):
+        L, t, al = layers.lib(), layers._DTYPES[dtype], int(all(v.data_ptr() % 16 == 0 for v in (x, w, w2, dy)))
+        need = [L.coop_linear_workspace_bytes(n, k, m, t, al), L.coop_gated_workspace_bytes(n, k, m, t, al)]
+        out, pre = P.coop_linear(x, w, b, act=P.COOP_ACT_GELU, residual=res, want_pre=True, workspace=ws(need[0]), stream=stream)
+        h, pre2 = P.coop_gated(x, w, w2, b, None, want_pre=True, workspace=ws(need[1]), stream=stream)
+        got = [out, pre, h, pre2]
+        for act, kept in ((P.COOP_ACT_GELU, pre), (P.COOP_ACT_GELU, None), (P.COOP_ACT_NONE, None)):
+            need = L.coop_linear_grad_workspace_bytes(n, k, m, t, act, kept is not None, al)
+            got += P.coop_linear_grad(dy, x, w, b, pre=kept, act=act, alpha=0.5, workspace=ws(need), stream=stream)
+        for kept in (pre2, None):
+            need = L.coop_gated_grad_workspace_bytes(n, k, m, t, kept is not None, al)
+            got += P.coop_gated_grad(dy, x, w, w2, b, None, pre=kept, workspace=ws(need), stream=stream)
+        return got
+
+    return (x, w, w2, b, res, dy), everything
+
+
+def seam_calls(dtype, n, dim, seed=0):
+    g = rng(seed + dim)
+    x, f, gate, dr, dy = normal(g, n, dim), normal(g, n, dim, dtype=dtype), normal(g, n, dim, dtype=dtype), normal(g, n, dim), normal(g, n, dim, dtype=dtype)
+    w = [normal(g, dim) for _ in range(5)]
+
+    def everything(stream=None, ws=lambda need: None):
+        got = []
+        for gt, kw in ((gate, {}), (w[4], {}), (None, dict(before=False)), (w[4], dict(after=False))):
+            a = dict(after_weight=w[0], after_bias=w[1]) if kw.get("after", True) else {}
+            b = dict(before_weight=w[2]) if kw.get("before", True) else {}
+            r, y, stats = P.coop_residual_norm(x, f, gate=gt, before_bias=w[3] if b else None, stream=stream, **kw, **a, **b)
+            need = layers.lib().coop_residual_norm_grad_workspace_bytes(n, dim, layers._DTYPES[dtype])
+            got += [r, y, stats, *P.coop_residual_norm_grad(dr, dy if b else None, x, f, stats, gate=gt, workspace=ws(need), stream=stream, **kw, **a, **b)]
+        return [v for v in got if v is not None]
+
+    return (x, f, gate, dr, dy), everything
+
+
+def clip_calls(seed=0):
+    g = rng(seed)
+    grads = [normal(g, k, dtype=TYPES[i % 3]) for i, k in enumerate((5, 16384, 70001, 300))]
+    plan = P.GradNorm(grads)
+
+    def everything(stream=None, ws=lambda need: None):
+        return list(plan.measure(1.0, workspace=ws(plan._bytes), stream=stream))
+
+    return tuple(grads), everything
+
+
+CALLS = [lambda p=p: dense_calls(*p) for p in PATHS] + [lambda p=p: seam_calls(*p) for p in ((torch.bfloat16, 900, 100), (torch.float16, 300, 2050), (torch.float32, 70, 1000),
+                                                                                             (torch.bfloat16, 30, 9000))] + [clip_calls]
+CALL_IDS = ["%s-%d-%d-%d" % ((str(p[0])[6:],) + p[1:]) for p in PATHS] + ["seam-100", "seam-2050", "seam-1000", "seam-9000", "clip"]
+
+
+def same(a, b):
+    return len(a) == len(b) and all(x is y or torch.equal(x, y) for x, y in zip(a, b))
+
+
+@gpu
+@pytest.mark.parametrize("calls", CALLS, ids=CALL_IDS)
+def test_same_bits_on_another_stream_with_any_workspace_and_in_a_graph(calls):
+    inputs, everything = calls()
+    kept = [v.clone() for v in inputs]
+    want = everything()
+    assert same(inputs, kept)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = everything(stream=side)
+    assert same(want, everything())            # (beside the other stream's)
+    side.synchronize()
+    assert same(want, got)
+    # (a workspace holds what it comes with, and not a byte behind it is written)
+    kept_ws = []
+
+    def given(need):
+        ws = torch.full((need + 4096,), 0xFF, dtype=torch.uint8, device="cuda")
+        kept_ws.append((ws, need))
+        return ws[:need] if need else None
+
+    assert same(want, everything(ws=given))
+    assert all((ws[need:] == 0xFF).all() for ws, need in kept_ws)
+    side.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = everything()
+    for i in range(3):
+        for v in out:
+            if v is not None:
+                v.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(want, out), i
+        assert same(want, everything())
+        torch.ones(1 << 20, device="cuda").sum()
+    # other inputs in the same places
+    for v in inputs:
+        v.mul_(0.5)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert same(everything(), out)
+
+
+@gpu
+@pytest.mark.parametrize("path", PATHS, ids=CALL_IDS[:len(PATHS)])
+def test_what_is_asked_for_alone_is_the_same(path):
+    """Each gradient by itself, and results at an address of their own with nothing written around them."""
+    (x, w, w2, b, res, dy), _ = dense_calls(*path, seed=3)
+    dtype, n, k, m = path
+    for act in (P.COOP_ACT_NONE, P.COOP_ACT_SILU):
+        want = P.coop_linear_grad(dy, x, w, b, act=act)
+        for i, names in enumerate(("want_x", "want_weight", "want_bias")):
+            only = dict(want_x=False, want_weight=False, want_bias=False)
+            only[names] = True
+            got = P.coop_linear_grad(dy, x, w, b, act=act, **only)
+            assert torch.equal(got[i], want[i]) and sum(v is not None for v in got) == 1
+    want = P.coop_gated_grad(dy, x, w, w2, b, b)
+    got = P.coop_gated_grad(dy, x, w, w2, b, b, want_x=False, want_bias=False)
+    assert torch.equal(got[1], want[1]) and torch.equal(got[2], want[2]) and got[0] is None and got[3] is None
+    got = P.coop_gated_grad(dy, x, w, w2, b, b, want_x=False, want_weight=False)
+    assert torch.equal(got[3], want[3]) and torch.equal(got[4], want[4])
+    assert torch.equal(P.coop_gated_grad(dy, x, w, w2, b, b, want_weight=False, want_bias=False)[0], want[0])
+    for shift in (0, 1):    # (elements; the residual is where the result goes)
+        place = torch.full((n * m + 1024 + shift,), 3.0, dtype=dtype, device="cuda")
+        out = place[512 + shift:512 + shift + n * m].view(n, m)
+        out.copy_(res)
+        got = P.coop_linear(x, w, b, act=P.COOP_ACT_GELU, residual=out, out=out)
+        assert (place[:512 + shift] == 3).all() and (place[512 + shift + n * m:] == 3).all()
+        assert torch.equal(got, P.coop_linear(x, w, b, act=P.COOP_ACT_GELU, residual=res))
+        out.fill_(3.0)
+        P.coop_gated(x, w, w2, b, b, out=out)
+        assert (place[:512 + shift] == 3).all() and (place[512 + shift + n * m:] == 3).all()
+
+
+@gpu
+@pytest.mark.parametrize("path", PATHS, ids=CALL_IDS[:len(PATHS)])
+def test_rows_are_by_themselves(path):
+    """What is no number in a row stays in that row, of the results and of the input's gradient."""
+    (x, w, w2, b, res, dy), _ = dense_calls(*path, seed=5)
+    n = x.shape[0]
+    bad = sorted({0, n // 2, n - 1})
+    good = torch.ones(n, dtype=torch.bool, device="cuda")
+    good[bad] = False
+    calls = [lambda: P.coop_linear(x, w, b, act=P.COOP_ACT_SILU, residual=res), lambda: P.coop_gated(x, w, w2, b, b),
+             lambda: P.coop_linear_grad(dy, x, w, b, act=P.COOP_ACT_SILU)[0], lambda: P.coop_gated_grad(dy, x, w, w2, b, b)[0],
+             lambda: P.coop_linear_grad(dy, x, w, b)[0]]
+    want = [call() for call in calls]
+    x[bad[0], 3], x[bad[-1], 0] = float("nan"), float("inf")
+    dy[bad] = float("nan")
+    for i, (call, before) in enumerate(zip(calls, want)):
+        got = call()
+        assert torch.equal(got[good], before[good]), i
+        assert torch.isnan(got[bad[0]]).any(), i
+
+
+@gpu
+@pytest.mark.parametrize("n,dim,dtype", [(300, 1027, torch.bfloat16), (300, 523, torch.float32), (500, 100, torch.float16), (40, 4096, torch.bfloat16), (9, 16384, torch.float16)])
+def test_residual_norm_in_place(n, dim, dtype):
+    g = rng(dim)
+    x, f, dr, dy, w = normal(g, n, dim, dtype=dtype), normal(g, n, dim, dtype=dtype), normal(g, n, dim, dtype=dtype), normal(g, n, dim, dtype=dtype), normal(g, dim)
+    L, t = layers.lib(), layers._DTYPES[dtype]
+    for norms in (1, 2, 3, 3 | 4):
+        a, b = (w.data_ptr() if norms & 1 else None), (w.data_ptr() if norms & 2 else None)
+
+        def forward(xx, ff, r, y):
+            stats = torch.empty((4, n), device="cuda")
+            assert L.coop_residual_norm(xx.data_ptr(), ff.data_ptr(), n, dim, t, t, w.data_ptr(), 1, 0.9, norms, a, None, b, None, 0, 1e-5, r.data_ptr(), y.data_ptr(),
+                                        stats.data_ptr(), None) == 0
+            return stats
+
+        def backward(d, e, stats, dx, df):
+            dgate = torch.empty(dim, device="cuda")
+            ws = torch.empty(L.coop_residual_norm_grad_workspace_bytes(n, dim, t), dtype=torch.uint8, device="cuda")
+            assert L.coop_residual_norm_grad(d.data_ptr(), e.data_ptr(), x.data_ptr(), f.data_ptr(), n, dim, t, t, stats.data_ptr(), w.data_ptr(), 1, 0.9, norms, a, None, b,
+                                             0, dx.data_ptr(), df.data_ptr(), dgate.data_ptr(), None, None, None, None, ws.data_ptr(), ws.numel(), None) == 0
+            torch.cuda.synchronize()
+            return dgate
+
+        torch.cuda.synchronize()
+        r, y, r2, y2 = torch.empty_like(x), torch.zeros_like(f), x.clone(), f.clone()
+        torch.cuda.synchronize()
+        stats = forward(x, f, r, y)
+        assert torch.equal(stats, forward(r2, y2, r2, y2)) and torch.equal(r, r2) and (not norms & 2 or torch.equal(y, y2))
+        dx, df, dx2, df2 = torch.empty_like(x), torch.empty_like(f), dr.clone(), dy.clone()
+        torch.cuda.synchronize()
+        assert torch.equal(backward(dr, dy, stats, dx, df), backward(dx2, df2, stats, dx2, df2)) and torch.equal(dx, dx2) and torch.equal(df, df2)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,n,k,m", [(torch.bfloat16, (1 << 31) // 128 + 4099, 128, 128), (torch.float16, (1 << 31) // 100 + 77, 100, 75),
+                                         (torch.float32, (1 << 30) // 64 + 4099, 64, 72)])
+def test_dense_offsets_beyond_32_bits(dtype, n, k, m):
+    """The last rows of an input of more than 2^32 bytes, against the same rows alone: their own, in the input's gradient and the result."""
+    torch.cuda.empty_cache()
+    g = rng(8)
+    x, dy = torch.empty((n, k), dtype=dtype, device="cuda"), torch.empty((n, m), dtype=dtype, device="cuda")
+    x[:1 << 20], dy[:1 << 20] = normal(g, 1 << 20, k, dtype=dtype), normal(g, 1 << 20, m, dtype=dtype)
+    for a in (x, dy):
+        for i in range(1 << 20, n, 1 << 20):
+            a[i:i + (1 << 20)] = a[:min(1 << 20, n - i)]
+    w, b = normal(g, m, k, dtype=dtype, scale=k ** -0.5), normal(g, m, dtype=dtype)
+    out = P.coop_linear(x, w, b, act=P.COOP_ACT_SILU)
+    dx, dw, db = P.coop_linear_grad(dy, x, w, b, act=P.COOP_ACT_SILU)
+    first, part = n - (n % (1 << 20)) - (1 << 20), slice(0, 1 << 20)
+    want, wants = P.coop_linear(x[part], w, b, act=P.COOP_ACT_SILU), P.coop_linear_grad(dy[part], x[part], w, b, act=P.COOP_ACT_SILU)
+    for i in (first, 0, 1 << 20):
+        assert torch.equal(out[i:i + (1 << 20)], want) and torch.equal(dx[i:i + (1 << 20)], wants[0])
+    # whole copies of the first 2^20 rows, and what is left: the weight's gradient is theirs added up, each rounded to the type, and 32 bits' sums
+    rest, copies = slice(n - n % (1 << 20), n), n >> 20
+    tail = P.coop_linear_grad(dy[rest], x[rest], w, b, act=P.COOP_ACT_SILU, grad_dtype=torch.float32)
+    whole = P.coop_linear_grad(dy[part], x[part], w, b, act=P.COOP_ACT_SILU, grad_dtype=torch.float32)
+    z, _ = product64(x[:1 << 18], w, b)
+    dz = dy[:1 << 18].double() * act64(z, P.COOP_ACT_SILU)[1]
+    size = (dz.abs().t().contiguous() @ x[:1 << 18].double().abs()) * (n / (1 << 18)) * 1.05
+    value = whole[1].double() * copies + tail[1].double()
+    # (sums in order of at most 2^10 parts of at most n / 2^10 rows and the tiles' own: some 2^15 roundings of a random sign at worst one after the other)
+    bound = rounded(value, 2.0 ** 15 * U * size, dtype)
+    # (fp16 has no numbers of 65,520 and more: of a value that may be one its infinity is right)
+    over = torch.isinf(dw) & (value.abs() + bound >= torch.finfo(dtype).max) & (torch.sign(dw) == torch.sign(value))
+    within(torch.where(over, value, dw.double()), value, bound, "dw")
+    within(db, whole[2].double() * copies + tail[2].double(), 2.0 ** 15 * U * dz.abs().sum(0) * (n / (1 << 18)) * 1.05, "db")
+
+
+@gpu
+def test_residual_norm_offsets_beyond_32_bits():
+    torch.cuda.empty_cache()
+    n, dim = (1 << 31) // 128 + 1001, 128
+    g = rng(9)
+    x = torch.empty((n, dim), dtype=torch.bfloat16, device="cuda")
+    x.view(-1).copy_(torch.arange(n * dim, device="cuda", dtype=torch.int32).bitwise_and_(1023).sub_(500))
+    x[-1000:] = normal(g, 1000, dim, dtype=torch.bfloat16)
+    gate, w = normal(g, dim), normal(g, dim)
+    kw = dict(gate=gate, after_weight=w, before_weight=w)
+    r, y, stats = P.coop_residual_norm(x, x, **kw)
+    got = P.coop_residual_norm_grad(x, x, x, x, stats, want_weight=False, **kw)
+    last = x[-1000:].clone()
+    r2, y2, stats2 = P.coop_residual_norm(last, last, **kw)
+    want = P.coop_residual_norm_grad(last, last, last, last, stats2, want_weight=False, **kw)
+    assert torch.equal(r[-1000:], r2) and torch.equal(y[-1000:], y2) and torch.equal(stats[:, -1000:], stats2)
+    assert torch.equal(got[0][-1000:], want[0]) and torch.equal(got[1][-1000:], want[1])
+
+
+# ---- gradients against differences, and all of them together --------------------------------------------------------------------------
+def model64(table, ids, target, blocks, out):
+    """A residual feed-forward model on learned rows in 64 bits: its loss, a mean."""
+    def norm(v, w, b, eps=1e-5):
+        c = v - v.mean(1, keepdim=True)
+        return c / (c.square().mean(1, keepdim=True) + eps).sqrt() * w + b
+
+    r = table[ids]
+    y = norm(r, *blocks[0]["before"])
+    for i, p in enumerate(blocks):
+        g, u = y @ p["gate"].t() + p["gate_bias"], y @ p["up"].t() + p["up_bias"]
+        h = g * torch.sigmoid(g) * u
+        f = h @ p["down"].t() + p["down_bias"]
+        r = 0.9 * r + norm(f, *p["after"]) * p["scale"]
+        y = norm(r, *blocks[i + 1]["before"]) if i + 1 < len(blocks) else norm(r, *p["last"])
+    return torch.nn.functional.cross_entropy(y @ out.t(), target)
+
+
+@gpu
+def test_a_model_of_them_together():
+    """Forward, backward, clipping and a step, as a training program has them: gradients against those of 64 bits and against differences of the
+    64-bit loss, the norm, and a captured step against an eager one.
+
+    Bound: each operator's gradients hold to some 2^-17 of the sizes of the terms that they are sums of (64 terms of 2 u and the activations'
+    40 u, in the tests above); behind ten operators in a row whose gradients' terms cancel to an eighth at worst that is 2^-11 of the largest."""
+    g = rng(12)
+    n, vocab, dim, ff = 300, 90, 40, 56
+    table, out = normal(g, vocab, dim), normal(g, vocab, dim, scale=dim ** -0.5)
+    ids = torch.randint(0, vocab, (n,), generator=g, device="cuda", dtype=torch.int32)
+    target = torch.randint(0, vocab, (n,), generator=g, device="cuda", dtype=torch.int32)
+    vector = lambda: (1 + normal(g, dim, scale=0.2), normal(g, dim, scale=0.2))  # noqa: E731
+    blocks = [dict(before=vector(), after=vector(), last=vector(), scale=1 + normal(g, dim, scale=0.2), gate=normal(g, ff, dim, scale=dim ** -0.5),
+                   up=normal(g, ff, dim, scale=dim ** -0.5), gate_bias=normal(g, ff, scale=0.1), up_bias=normal(g, ff, scale=0.1),
+                   down=normal(g, dim, ff, scale=ff ** -0.5), down_bias=normal(g, dim, scale=0.1)) for _ in range(2)]
+    params = [table, out, *blocks[0]["before"], *blocks[1]["last"]]
+    for p in blocks:
+        params += [p["gate"], p["up"], p["gate_bias"], p["up_bias"], p["down"], p["down_bias"], *p["after"], p["scale"]]
+    params += list(blocks[1]["before"])
+
+    def gradients():
+        r = P.coop_embed(table, ids)
+        y, mean, rstd = P.coop_layer_norm(r, *blocks[0]["before"])
+        first, kept = (r, mean, rstd), []
+        for i, p in enumerate(blocks):
+            h, pre = P.coop_gated(y, p["gate"], p["up"], p["gate_bias"], p["up_bias"], want_pre=True)
+            f = P.coop_linear(h, p["down"], p["down_bias"])
+            bw, bb = blocks[i + 1]["before"] if i + 1 < len(blocks) else p["last"]
+            kw = dict(gate=p["scale"], alpha=0.9, after_weight=p["after"][0], after_bias=p["after"][1], before_weight=bw)
+            r2, y2, stats = P.coop_residual_norm(r, f, before_bias=bb, **kw)
+            kept.append((r, y, h, pre, f, stats, kw))
+            r, y = r2, y2
+        loss, lse = P.coop_softmax_xent(y, out, target)
+        dy, dout = P.coop_softmax_xent_grad(y, out, target, lse, torch.full_like(loss, 1.0 / n))
+        dr, found = None, {}
+        for i in reversed(range(len(blocks))):
+            p, (r0, y0, h, pre, f, stats, kw) = blocks[i], kept[i]
+            dr, df, dscale, daw, dab, dbw, dbb = P.coop_residual_norm_grad(dr, dy, r0, f, stats, **kw)
+            dh, ddown, ddown_bias = P.coop_linear_grad(df, h, p["down"], p["down_bias"])
+            dy, dgate, dup, dgb, dub = P.coop_gated_grad(dh, y0, p["gate"], p["up"], p["gate_bias"], p["up_bias"], pre=pre)
+            found[i] = [dgate, dup, dgb, dub, ddown, ddown_bias, daw, dab, dscale], [dbw, dbb]
+        dx, dw, db = P.coop_layer_norm_grad(dy, *first, blocks[0]["before"][0])
+        dtable = P.coop_embed_grad(dx + dr, ids, vocab)
+        return loss.mean(), [dtable, dout, dw, db, *found[1][1], *found[0][0], *found[1][0], *found[0][1]]
+
+    loss, grads = gradients()
+    wide = {id(p): p.double().requires_grad_() for p in params}
+    blocks64 = [{k: tuple(wide.get(id(x), x.double()) for x in v) if isinstance(v, tuple) else wide[id(v)] for k, v in p.items()} for p in blocks]
+    loss64 = model64(wide[id(table)], ids.long(), target.long(), blocks64, wide[id(out)])
+    wants = torch.autograd.grad(loss64, [wide[id(p)] for p in params])
+    assert abs(float(loss) - float(loss64.detach())) <= 2.0 ** -17 * float(loss64.detach())
+    for i, (have, want) in enumerate(zip(grads, wants)):
+        assert have.shape == want.shape
+        within(have, want, 2.0 ** -11 * want.abs().max() + 0 * want, i)
+    # along a direction: the loss 64 bits' differences (error: a step's square times a third derivative, which is of the size of the loss)
+    v = [normal(g, *p.shape).double() for p in params]
+    for p, d in zip(params, v):
+        d *= float(p.abs().max())
+    with torch.no_grad():
+        def at(h):
+            moved = {id(p): p.double() + h * d for p, d in zip(params, v)}
+            b64 = [{k: tuple(moved.get(id(x), x.double()) for x in q) if isinstance(q, tuple) else moved[id(q)] for k, q in p.items()} for p in blocks]
+            return float(model64(moved[id(table)], ids.long(), target.long(), b64, moved[id(out)]))
+        slope = (at(1e-5) - at(-1e-5)) / 2e-5
+    got = sum(float((gr.double() * d).sum()) for gr, d in zip(grads, v))
+    size = sum(float((gr.double() * d).abs().sum()) for gr, d in zip(grads, v))
+    assert abs(got - slope) <= 2.0 ** -11 * size
+    # clipping and the step, eager and captured
+    want_norm = math.sqrt(sum(float(w.square().sum()) for w in wants))
+    copies = [[p.clone() for p in params] for _ in range(2)]
+    eager, again = (P.AdamW(c, grads) for c in copies)
+    plan = P.GradNorm(grads)
+    norm, factor = plan.measure(0.1 * want_norm)
+    assert abs(float(norm) - want_norm) <= 2.0 ** -11 * want_norm and abs(float(factor) - 0.1) <= 2.0 ** -10
+    eager.step(1, 1e-2, grad_scale=factor)
+    torch.cuda.synchronize()
+    kept = [x.clone() for x in grads]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss2, captured = gradients()
+        captured_plan = P.GradNorm(captured)
+        norm2, factor2 = captured_plan.measure(0.1 * want_norm)
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(kept, captured) and torch.equal(norm, norm2) and torch.equal(factor, factor2) and torch.equal(loss, loss2)
+        assert same(kept, gradients()[1])
+    again.step(1, 1e-2, grad_scale=factor2)
+    assert same(copies[0], copies[1])
+
+
+# ---- refusals ----------------------------------------------------------------------------------------------------------------------------
+def test_refusals_of_the_c_abi():
+    """What the host can see is refused before anything is launched."""
+    L = layers.lib()
+    A, N = 0x1000, None
+    need = L.coop_linear_workspace_bytes(5000, 3001, 3001, 2, 0)
+    assert need > 0 and L.coop_linear_workspace_bytes(1, 4096, 4096, 2, 1) == 0     # (a call that is small takes none)
+    assert L.coop_linear_workspace_bytes(-1, 8, 8, 2, 1) == L.coop_linear_workspace_bytes(5000, 0, 8, 2, 1) == L.coop_linear_workspace_bytes(5000, 8, 8, 3, 1) == 0
+    good = dict(x=A, n=5000, k=3001, w=A, m=3001, dtype=2, bias=N, act=0, res=N, out=A, pre=N, ws=A, wb=need)
+
+    def linear(**kw):
+        a = dict(good, **kw)
+        return L.coop_linear(a["x"], a["n"], a["k"], a["w"], a["m"], a["dtype"], a["bias"], a["act"], 1.0, a["res"], a["out"], a["pre"], a["ws"], a["wb"], N)
+
+    for kw in (dict(dtype=3), dict(act=4), dict(act=-1), dict(n=-1), dict(n=1 << 31), dict(k=0), dict(m=0), dict(k=(1 << 18) + 1), dict(m=(1 << 18) + 1), dict(x=A + 1),
+               dict(w=A + 1), dict(bias=A + 1), dict(res=A + 1), dict(out=A + 1), dict(pre=A + 2), dict(wb=need - 1), dict(ws=A + 16)):
+        assert linear(**kw) == -4, kw
+    for kw in (dict(x=N), dict(w=N), dict(out=N), dict(ws=N)):
+        assert linear(**kw) == -1, kw
+    assert linear(n=0, x=N, out=N, ws=N) == 0
+    need = L.coop_linear_grad_workspace_bytes(5000, 3001, 3001, 2, 2, 0, 0)
+    good = dict(dout=A, x=A, n=5000, k=3001, w=A, m=3001, dtype=2, bias=N, act=2, pre=N, dx=A, dw=A, gd=2, db=A, ws=A, wb=need)
+
+    def grad(**kw):
+        a = dict(good, **kw)
+        return L.coop_linear_grad(a["dout"], a["x"], a["n"], a["k"], a["w"], a["m"], a["dtype"], a["bias"], a["act"], 1.0, a["pre"], a["dx"], a["dw"], a["gd"], a["db"],
+                                  a["ws"], a["wb"], N)
+
+    for kw in (dict(dtype=3), dict(act=4), dict(n=-1), dict(k=0), dict(m=(1 << 18) + 1), dict(gd=1), dict(gd=7), dict(dout=A + 1), dict(x=A + 1), dict(w=A + 1), dict(bias=A + 1),
+               dict(dx=A + 1), dict(dw=A + 1), dict(gd=0, dw=A + 2), dict(db=A + 2), dict(pre=A + 2), dict(wb=need - 1), dict(ws=A + 16)):
+        assert grad(**kw) == -4, kw
+    for kw in (dict(dout=N), dict(x=N), dict(w=N), dict(ws=N)):
+        assert grad(**kw) == -1, kw
+    assert grad(dx=N, dw=N, db=N, ws=N) == 0 and grad(n=0, dw=N, db=N, dout=N, x=N, ws=N) == 0      # nothing asked for
+    need = L.coop_gated_workspace_bytes(5000, 3001, 3001, 2, 0)
+    good = dict(x=A, n=5000, k=3001, g=A, u=A, f=3001, dtype=2, gb=N, ub=N, act=3, out=A, pre=N, ws=A, wb=need)
+
+    def gated(**kw):
+        a = dict(good, **kw)
+        return L.coop_gated(a["x"], a["n"], a["k"], a["g"], a["u"], a["f"], a["dtype"], a["gb"], a["ub"], a["act"], a["out"], a["pre"], a["ws"], a["wb"], N)
+
+    for kw in (dict(dtype=-1), dict(act=9), dict(n=-5), dict(f=0), dict(g=A + 1), dict(u=A + 1), dict(gb=A + 1), dict(ub=A + 1), dict(out=A + 1), dict(pre=A + 1), dict(wb=0)):
+        assert gated(**kw) == -4, kw
+    for kw in (dict(x=N), dict(g=N), dict(u=N), dict(out=N), dict(ws=N)):
+        assert gated(**kw) == -1, kw
+    need = L.coop_gated_grad_workspace_bytes(5000, 3001, 3001, 2, 0, 0)
+    good = dict(dout=A, x=A, n=5000, k=3001, g=A, u=A, f=3001, dtype=2, gb=N, ub=N, act=3, pre=N, dx=A, dg=A, du=A, gd=0, dgb=A, dub=A, ws=A, wb=need)
+
+    def gated_grad(**kw):
+        a = dict(good, **kw)
+        return L.coop_gated_grad(a["dout"], a["x"], a["n"], a["k"], a["g"], a["u"], a["f"], a["dtype"], a["gb"], a["ub"], a["act"], a["pre"], a["dx"], a["dg"], a["du"],
+                                 a["gd"], a["dgb"], a["dub"], a["ws"], a["wb"], N)
+
+    for kw in (dict(dg=N), dict(du=N), dict(dgb=N), dict(dub=N), dict(gd=1), dict(dg=A + 2), dict(dub=A + 1), dict(wb=need - 1), dict(act=5)):
+        assert gated_grad(**kw) == -4, kw
+    for kw in (dict(dout=N), dict(u=N), dict(ws=N)):
+        assert gated_grad(**kw) == -1, kw
+    good = dict(x=A, f=A, n=5, dim=8, dtype=2, st=0, gate=A, form=1, norms=3, aw=A, ab=A, bw=A, bb=A, wt=0, eps=1e-5, r=A, y=A, stats=A)
+
+    def seam(**kw):
+        a = dict(good, **kw)
+        return L.coop_residual_norm(a["x"], a["f"], a["n"], a["dim"], a["dtype"], a["st"], a["gate"], a["form"], 1.0, a["norms"], a["aw"], a["ab"], a["bw"], a["bb"], a["wt"],
+                                    a["eps"], a["r"], a["y"], a["stats"], N)
+
+    for kw in (dict(dtype=4), dict(st=1), dict(wt=1), dict(norms=0), dict(norms=4), dict(norms=8), dict(norms=7), dict(norms=1), dict(norms=2), dict(dim=0), dict(dim=16385), dict(n=-1),
+               dict(dtype=0, dim=8193), dict(form=0), dict(form=3), dict(gate=N), dict(eps=-1.0), dict(eps=float("nan")), dict(x=A + 2), dict(f=A + 1), dict(gate=A + 2), dict(aw=A + 2),
+               dict(r=A + 2), dict(y=A + 1), dict(stats=A + 2)):
+        assert seam(**kw) == -4, kw
+    for kw in (dict(x=N), dict(f=N), dict(r=N), dict(y=N), dict(stats=N)):
+        assert seam(**kw) == -1, kw
+    assert seam(n=0, x=N, f=N, r=N, y=N, stats=N) == 0
+    need = L.coop_residual_norm_grad_workspace_bytes(5, 8, 2)
+    assert need > 0 and L.coop_residual_norm_grad_workspace_bytes(5, 16385, 2) == 0
+    good = dict(dr=A, dy=A, x=A, f=A, n=5, dim=8, dtype=2, st=0, stats=A, gate=A, form=1, norms=3, aw=A, ab=A, bw=A, wt=0, dx=A, df=A, dgate=A, daw=A, dab=A, dbw=A, dbb=A, ws=A, wb=need)
+
+    def seam_grad(**kw):
+        a = dict(good, **kw)
+        return L.coop_residual_norm_grad(a["dr"], a["dy"], a["x"], a["f"], a["n"], a["dim"], a["dtype"], a["st"], a["stats"], a["gate"], a["form"], 1.0, a["norms"], a["aw"], a["ab"],
+                                         a["bw"], a["wt"], a["dx"], a["df"], a["dgate"], a["daw"], a["dab"], a["dbw"], a["dbb"], a["ws"], a["wb"], N)
+
+    for kw in (dict(norms=1), dict(norms=2), dict(norms=7), dict(gate=N), dict(dgate=N), dict(form=0), dict(dim=0), dict(wb=need - 1), dict(ws=A + 8), dict(dx=A + 2), dict(df=A + 1),
+               dict(dgate=A + 2), dict(dbb=A + 1)):
+        assert seam_grad(**kw) == -4, kw
+    for kw in (dict(dy=N), dict(x=N), dict(f=N), dict(stats=N), dict(dx=N), dict(df=N), dict(ws=N)):
+        assert seam_grad(**kw) == -1, kw
+    t = (layers._CGradTensor * 2)()
+    need = L.coop_grad_norm_workspace_bytes(t, 0)
+    norm = lambda n=1, bound=1.0, ts=t, scale=N, out=A, ws=A, wb=1 << 20: L.coop_grad_norm(ts, n, bound, scale, out, A, ws, wb, N)  # noqa: E731
+    assert norm(n=-1) == -4 and norm(ts=N) == -1 and norm(bound=-1.0) == -4 and norm(bound=float("nan")) == -4 and norm(ws=N) == -1 and norm(ws=A + 4) == -4
+    assert norm(out=A + 2) == -4 and norm(scale=A + 1) == -4 and need > 0 and norm(n=0, wb=need - 1) == -4
+    t[0].n_rows, t[0].dim = 3, 7
+    assert norm() == -1 and L.coop_grad_scale(t, 1, A, N) == -1             # elements without an address
+    t[0].grad, t[0].dtype = A, 3
+    assert norm() == -4 and L.coop_grad_scale(t, 1, A, N) == -4
+    t[0].dtype, t[0].grad = 0, A + 2
+    assert norm() == -4
+    t[0].grad, t[0].n_rows_dev = A, A + 1
+    assert norm() == -4
+    t[0].n_rows_dev, t[0].n_rows, t[0].dim = None, 1 << 30, 1 << 30
+    assert norm() == -4 and L.coop_grad_norm_workspace_bytes(t, 1) == 0
+    t[0].n_rows = -1
+    assert norm() == -4
+    t[0].n_rows = 3
+    assert L.coop_grad_scale(t, 0, N, N) == 0 and L.coop_grad_scale(t, 1, N, N) == -1 and L.coop_grad_scale(t, 1, A + 2, N) == -4
+
+
+@gpu
+def test_refusals_of_the_binding():
+    x, w, v = torch.zeros((8, 6), device="cuda"), torch.zeros((5, 6), device="cuda"), torch.zeros(6, device="cuda")
+    y, stats = torch.zeros((8, 5), device="cuda"), torch.zeros((4, 8), device="cuda")
+    for call in (lambda: P.coop_linear(x[:, ::2], w), lambda: P.coop_linear(x, w.half()), lambda: P.coop_linear(x, w[:, :4].contiguous()), lambda: P.coop_linear(x.double(), w.double()),
+                 lambda: P.coop_linear(x, w, v), lambda: P.coop_linear(x, w, residual=x), lambda: P.coop_linear(x, w, out=x), lambda: P.coop_linear(x.cpu(), w),
+                 lambda: P.coop_linear_grad(x, x, w), lambda: P.coop_linear_grad(y, x, w, pre=y.half(), act=1), lambda: P.coop_linear_grad(y, x, w, pre=x, act=1),
+                 lambda: P.coop_gated(x, w, w[:4]), lambda: P.coop_gated(x, w, w.half()), lambda: P.coop_gated_grad(x, x, w, w), lambda: P.coop_gated_grad(y, x, w, w, pre=y),
+                 lambda: P.coop_residual_norm(x, y), lambda: P.coop_residual_norm(x.half(), x), lambda: P.coop_residual_norm(x, x, gate=v[:5]),
+                 lambda: P.coop_residual_norm(x, x, gate=y), lambda: P.coop_residual_norm(x, x, after_weight=v.double()), lambda: P.coop_residual_norm(x, x, rms=True, after_bias=v),
+                 lambda: P.coop_residual_norm(x, x, after=False, after_weight=v), lambda: P.coop_residual_norm(x, x, before=False, before_bias=v),
+                 lambda: P.coop_residual_norm_grad(x, None, x, x, stats), lambda: P.coop_residual_norm_grad(None, x, x, x, stats, before=False),
+                 lambda: P.coop_residual_norm_grad(x, x, x, x, stats[:2]), lambda: P.GradNorm([x[:, ::2]]), lambda: P.GradNorm([x.double()]),
+                 lambda: P.GradNorm([(x, v[:1])]), lambda: P.GradNorm([x]).measure(1.0, grad_scale=v), lambda: P.GradNorm([x]).apply(v)):
+        with pytest.raises((AssertionError, AttributeError, TypeError)):
+            call()
+    for call in (lambda: P.coop_linear(x, w, act=7), lambda: P.coop_residual_norm(x, x, after=False, before=False), lambda: P.coop_residual_norm(x, x, eps=-1.0),
+                 lambda: P.GradNorm([x]).measure(-1.0), lambda: P.GradNorm([x]).measure(1.0, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(P.CoopError) as e:
+            call()
+        assert e.value.code == -4
