@@ -130,6 +130,7 @@ struct Slope {
   int32_t cols;
   float alpha;
   int act;
+  int64_t rest;  // bytes from dz to what it lost to its type; 0: that is not kept
   template <int E>
   struct Lane {
     int32_t col;
@@ -166,6 +167,12 @@ struct Slope {
     if (dz == nullptr) return;
     store_elements<T, E>(dz + (row * ld + l.col) * kElem<T>, d);
     if (PAIR) store_elements<T, E>(dz + (row * ld + second + l.col) * kElem<T>, d2);
+    if (T == COOP_F32 || rest == 0) return;
+    typedef typename Element<T>::M M;
+#pragma unroll
+    for (int e = 0; e < E; ++e) d[e] -= (float)(M)d[e], d2[e] = PAIR ? d2[e] - (float)(M)d2[e] : 0.f;  // (of what is not finite: no number, as it is)
+    store_elements<T, E>(dz + rest + (row * ld + l.col) * kElem<T>, d);
+    if (PAIR) store_elements<T, E>(dz + rest + (row * ld + second + l.col) * kElem<T>, d2);
   }
   template <int E>
   __device__ __forceinline__ void put(Lane<E>& l, int64_t row, float (&v)[E], float (&u)[E]) const {
@@ -503,6 +510,7 @@ struct DensePlan {
   bool gated, pad, slope, again;  // slope: dz is not dout itself; again: the forward product is computed again
   bool few;                       // forward, of few rows or small: the kernel of dense_few.h
   bool small;                     // gradient, of what is small: the kernels of dense_small.h
+  bool rest;                      // and with what dz loses to its type
   bool narrow;                    // 8 to 128 by 8 to 128 in 16 bits: the kernels of dense_narrow.h (but not from what was kept)
   uint32_t narrow_tiles, narrow_blocks;
   Cut forward, back, weight;      // (dx and dW)
@@ -538,14 +546,15 @@ struct DensePlan {
     forward = Cut(n, m, kw, dtype, gated);
     size_t parts = narrow || few ? 0 : forward.part_bytes;
     dz = pre = part = part2 = join = 0;
-    slope = false;
+    slope = rest = false;
     if (grad && narrow) {
       parts = (size_t)narrow_blocks * (size_t)narrow_shares(k, m) * (size_t)m * (size_t)(round_up(k, 8) + kNarrowSums) * 4;
     } else if (grad) {
       slope = gated || act != COOP_ACT_NONE || (!small && (!aligned || mw != m));
       dz_ld = gated ? 2 * mw : mw;
       if (dz_ld * es % 2048 == 0) dz_ld += 256 / es;  // (or a tile's rows would all lie in the same few channels of memory)
-      dz = take(slope ? (size_t)n * dz_ld * es : 0);
+      rest = small && slope && es == 2 && n * both <= kRestMost;
+      dz = take(slope ? (size_t)n * dz_ld * (rest ? 4 : es) : 0);
       pre = take(again && !small && forward.splits > 1 ? (size_t)n * m * 4 * (gated ? 2 : 1) : 0);
       back = Cut(n, k, mw, dtype, false);
       weight = Cut(gated ? 2 * mw : m, k, n, dtype, false);
@@ -744,6 +753,7 @@ bool backward_all(const DensePlan& p, const void* dout, const void* x, const voi
   fin.part2 = (float*)(ws + p.part2);
   fin.rows = p.n, fin.ld = p.dz_ld, fin.second = p.mw, fin.cols = (int32_t)p.m;
   fin.alpha = alpha, fin.act = act;
+  fin.rest = p.rest ? p.n * p.dz_ld * kElem<T> : 0;
   if (p.again && p.small) {
     few_product<T, PAIR>(p, x, w, w2, fin, s);
   } else if (p.again && p.forward.splits == 1) {
@@ -761,11 +771,14 @@ bool backward_all(const DensePlan& p, const void* dout, const void* x, const voi
     const float scale = PAIR || act != COOP_ACT_NONE ? 1.f : alpha;
     const int64_t ld = (p.slope ? p.dz_ld : p.m) * kElem<T>, both = PAIR ? p.mw + p.m : p.m;
     const uint32_t k_tiles = (uint32_t)((p.k + 15) / 16), n_tiles = (uint32_t)((p.n + kSmallRows - 1) / kSmallRows), m_tiles = (uint32_t)((both + kSmallRows - 1) / kSmallRows);
-    const SmallGrad g{p.slope ? ws + p.dz : (const char*)dout, (const char*)x, (const char*)w, (const char*)w2, p.n, ld, p.mw, (int32_t)p.k, (int32_t)p.m,
+    const SmallGrad g{p.slope ? ws + p.dz : (const char*)dout, (const char*)x, (const char*)w, (const char*)w2, p.n, ld, p.mw, fin.rest, (int32_t)p.k, (int32_t)p.m,
                       dx != nullptr ? k_tiles * n_tiles : 0, dw != nullptr ? k_tiles * m_tiles : 0, k_tiles, fin.part, fin.part2, p.sum_rows, db, db2};
     const Gradient to_x{(char*)dx, nullptr, p.n, 0, (int32_t)p.k, scale, T}, to_w{(char*)dw, PAIR ? (char*)dw2 : nullptr, p.m, p.mw, (int32_t)p.k, scale, grad_dtype};
     const uint32_t blocks = g.dx_blocks + g.dw_blocks + (fin.part != nullptr ? (uint32_t)((p.m + kWave - 1) / kWave) * (PAIR ? 2 : 1) : 0);
-    if (blocks > 0) COOP_LAUNCH(K_DENSE_DX, (k_small_grad<T, PAIR>), dim3(blocks), dim3(kSmallWaves * kWave), 0, s, g, to_x, to_w);
+    auto kernel = k_small_grad<T, PAIR, false>;
+    if constexpr (T != COOP_F32)
+      if (p.rest) kernel = k_small_grad<T, PAIR, true>;
+    if (blocks > 0) COOP_LAUNCH(K_DENSE_DX, kernel, dim3(blocks), dim3(kSmallWaves * kWave), 0, s, g, to_x, to_w);
     return true;
   }
   if (fin.part != nullptr) sums_of_columns<T>(p, fin.part, fin.part2, db, db2, PAIR, ws, s);

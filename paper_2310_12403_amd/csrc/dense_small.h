@@ -3,11 +3,15 @@
 //
 // As in dense_few.h a block has 16 columns by 32 rows of a result and its waves deal the common dimension among themselves.  An operand that
 // has that dimension as its row number comes 16 bytes of a row at a time, 16 columns of a step, and is turned in the wave's own LDS.
+//
+// Of few values dz is kept as the sum of two numbers of the operands' type, what it rounds to and the rest (REST), and multiplied by both.  Of many
+// that rounding adds to the result's own as noise does, 1.41 times; of one row it may be most of what a result is off by (bf16, one row: 2.6 times).
+// (All of them so: 3,001 x 100 x 275 gated both ways 55 us for 39, 1,024 x 256 x 256 14.1 for 11.0.)
 #pragma once
 
 struct SmallGrad {
   const char *dz, *x, *w, *w2;
-  int64_t n, ld, second;  // dz: bytes of a row, elements from a pair's first part to its second
+  int64_t n, ld, second, rest;  // dz: bytes of a row, elements from a pair's first part to its second, bytes to its rest
   int32_t k, m;
   uint32_t dx_blocks, dw_blocks, k_tiles;  // (and behind them 64 columns of the bias's gradient a block)
   const float *part, *part2;
@@ -18,6 +22,7 @@ struct SmallGrad {
 // kSmallLength: bytes of the common dimension, 12 steps for each wave (longer ones take too long in the few blocks of a weight's gradient: 8,192 rows
 // of 64 by 64, 36.6 us for the 16.2 of dense_narrow.h).  8 waves for 16, which are idle where it is short: bf16 1,024 x 256 x 256 11.0 us for 13.1,
 // 256 x 1,024 x 512 13.1 for 19.9; 4: 12.5 and 12.5, and 31.5 for 26.4 with 3,001 rows.
+constexpr int64_t kRestMost = 1 << 16;  // values of dz
 constexpr int kSmallWaves = 8, kSmallRows = 32, kSmallLength = 12 * 8 * 64;
 
 // 16 bytes of a row from column `col` on, zeros behind column `dim`
@@ -62,9 +67,9 @@ __device__ __forceinline__ u32x4 turned(char* lds, u32x4 v) {
   return f;
 }
 
-template <int T, bool PAIR>
+template <int T, bool PAIR, bool REST>
 __global__ __launch_bounds__(kSmallWaves* kWave) void k_small_grad(SmallGrad g, Gradient to_x, Gradient to_w) {
-  constexpr int E = kE<T>, kStep = 4 * E, kAhead = 2;
+  constexpr int E = kE<T>, kStep = 4 * E, kAhead = 2, Z = REST ? 4 : 2;  // Z: fragments of dz
   __shared__ __attribute__((aligned(16))) char lds[kSmallWaves * 3 * 1024];
   static_assert(kSmallWaves * kSmallRows * 16 * 4 <= (int)sizeof(lds), "the sums lie where the fragments did");
   const int wave = uniform_wave_in_block(), lane = lane_id(), r16 = lane & 15, quarter = lane >> 4;
@@ -104,7 +109,7 @@ __global__ __launch_bounds__(kSmallWaves* kWave) void k_small_grad(SmallGrad g, 
     }
     const int steps = (g.m + kStep - 1) / kStep, all = PAIR ? 2 * steps : steps;
     for (int first = wave; first < all; first += kSmallWaves * kAhead) {
-      u32x4 a[kAhead], b[kAhead][2];
+      u32x4 a[kAhead], b[kAhead][Z];
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         int s = first + i * kSmallWaves;
@@ -112,32 +117,33 @@ __global__ __launch_bounds__(kSmallWaves* kWave) void k_small_grad(SmallGrad g, 
         if (other) s -= steps;
         a[i] = there ? load_strided<T>(other ? g.w2 : g.w, ldk, (int64_t)s * kStep, g.m, col0, g.k) : u32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-          b[i][t] = there ? load_some<T>(rows[t] + (other ? g.second * kElem<T> : 0), (int64_t)s * kStep + quarter * E, g.m) : u32x4{0, 0, 0, 0};
+        for (int t = 0; t < Z; ++t)
+          b[i][t] = there ? load_some<T>(rows[t & 1] + (other ? g.second * kElem<T> : 0) + (t & 2 ? g.rest : 0), (int64_t)s * kStep + quarter * E, g.m)
+                          : u32x4{0, 0, 0, 0};
       }
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         const u32x4 f = turned<T>(own, a[i]);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) acc[t] = mma16<T>(f, b[i][t], acc[t]);
+        for (int t = 0; t < Z; ++t) acc[t & 1] = mma16<T>(f, b[i][t], acc[t & 1]);
       }
     }
   } else {  // x and dz turned
     const int64_t steps = (g.n + kStep - 1) / kStep, cols = PAIR ? g.second + g.m : g.m;
     for (int64_t first = wave; first < steps; first += kSmallWaves * kAhead) {
-      u32x4 a[kAhead], b[kAhead][2];
+      u32x4 a[kAhead], b[kAhead][Z];
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         const int64_t s = first + i * kSmallWaves;  // (behind the last one: rows that are not there)
         a[i] = load_strided<T>(g.x, ldk, s * kStep, g.n, col0, g.k);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) b[i][t] = load_strided<T>(g.dz, g.ld, s * kStep, g.n, row0 + t * 16, cols);
+        for (int t = 0; t < Z; ++t) b[i][t] = load_strided<T>(g.dz + (t & 2 ? g.rest : 0), g.ld, s * kStep, g.n, row0 + (t & 1) * 16, cols);
       }
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         const u32x4 f = turned<T>(own, a[i]);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) acc[t] = mma16<T>(f, turned<T>(own + (1 + t) * 1024, b[i][t]), acc[t]);
+        for (int t = 0; t < Z; ++t) acc[t & 1] = mma16<T>(f, turned<T>(own + (1 + (t & 1)) * 1024, b[i][t]), acc[t & 1]);
       }
     }
   }
