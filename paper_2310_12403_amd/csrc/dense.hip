@@ -169,8 +169,12 @@ struct Slope {
     if (PAIR) store_elements<T, E>(dz + (row * ld + second + l.col) * kElem<T>, d2);
     if (T == COOP_F32 || rest == 0) return;
     typedef typename Element<T>::M M;
+    const auto lost = [](float v) {
+      const float r = v - (float)(M)v;
+      return fabsf(r) < __builtin_inff() ? r : 0.f;  // (what is not finite, or not in the type, has none)
+    };
 #pragma unroll
-    for (int e = 0; e < E; ++e) d[e] -= (float)(M)d[e], d2[e] = PAIR ? d2[e] - (float)(M)d2[e] : 0.f;  // (of what is not finite: no number, as it is)
+    for (int e = 0; e < E; ++e) d[e] = lost(d[e]), d2[e] = PAIR ? lost(d2[e]) : 0.f;
     store_elements<T, E>(dz + rest + (row * ld + l.col) * kElem<T>, d);
     if (PAIR) store_elements<T, E>(dz + rest + (row * ld + second + l.col) * kElem<T>, d2);
   }

@@ -4,12 +4,13 @@ a gated feed-forward block, the norms and the residual between two blocks, and t
 Marshalling only, as in binding.py and learn.py; streams are as there.
 """
 import ctypes as C
+import functools
 
 import torch
 
-from . import binding, learn
+from . import binding
 from .binding import _check, _stream_ptr
-from .learn import _DTYPES, _matrix, _new, _vector, _workspace
+from .learn import COOP_F32, _DTYPES, _matrix, _new, _vector, _workspace
 
 COOP_ACT_NONE, COOP_ACT_RELU, COOP_ACT_GELU, COOP_ACT_SILU = 0, 1, 2, 3
 _AFTER, _BEFORE, _RMS = 1, 2, 4
@@ -50,14 +51,23 @@ def lib():
     return _lib
 
 
+@functools.lru_cache(maxsize=4096)
+def _need(call, *sizes):
+    """Bytes of workspace that a call of these sizes takes."""
+    return getattr(lib(), call + "_workspace_bytes")(*sizes)
+
+
 def _same(t, like, what, rows=None, dim=None):
     p = _matrix(t, what, rows, dim)
     assert t.dtype == like.dtype, "%s: %s" % (what, like.dtype)
     return p
 
 
-def _new_like(t, stream):
-    return torch.empty_like(t) if stream is None else _new(t.shape, t.dtype, t.device, stream)
+# (of a result like an argument; torch.empty with a type and a device takes half a microsecond more)
+def _new_like(t, stream, shape=None):
+    if stream is None:
+        return torch.empty_like(t) if shape is None else t.new_empty(shape)
+    return _new(shape or t.shape, t.dtype, t.device, stream)
 
 
 def _bias(b, n, like, what):
@@ -76,11 +86,11 @@ def coop_linear(x, weight, bias=None, act=COOP_ACT_NONE, alpha=1.0, residual=Non
     xp, wp = _matrix(x, "x"), _same(weight, x, "weight", dim=x.shape[1])
     (n, k), m, dtype = x.shape, weight.shape[0], _DTYPES[x.dtype]
     if out is None:
-        out = _new((n, m), x.dtype, x.device, stream)
+        out = _new_like(x, stream, (n, m))
     op = _same(out, x, "out", n, m)
     pre = _new((n, m), torch.float32, x.device, stream) if want_pre else None
     rp = None if residual is None else _same(residual, x, "residual", n, m)
-    keep, sp, sb = _workspace(lib().coop_linear_workspace_bytes(n, k, m, dtype, (xp | wp) & 15 == 0), workspace, x.device, stream)
+    keep, sp, sb = _workspace(_need("coop_linear", n, k, m, dtype, (xp | wp) & 15 == 0), workspace, x.device, stream)
     _check(lib().coop_linear(xp, n, k, wp, m, dtype, _bias(bias, m, x, "bias"), act, alpha, rp, op, pre.data_ptr() if want_pre else None, sp, sb,
                              _stream_ptr(stream)))
     return (out, pre) if want_pre else out
@@ -97,7 +107,7 @@ def coop_linear_grad(dout, x, weight, bias=None, pre=None, act=COOP_ACT_NONE, al
     dx = _new_like(x, stream) if want_x else None
     dw = _new((m, k), grad_dtype, x.device, stream) if want_weight else None
     db = _new(m, torch.float32, x.device, stream) if want_bias else None
-    need = lib().coop_linear_grad_workspace_bytes(n, k, m, dtype, act, pre is not None, (xp | wp | dp) & 15 == 0)
+    need = _need("coop_linear_grad", n, k, m, dtype, act, pre is not None, (xp | wp | dp) & 15 == 0)
     keep, sp, sb = _workspace(need, workspace, x.device, stream)
     _check(lib().coop_linear_grad(dp, xp, n, k, wp, m, dtype, _bias(bias, m, x, "bias"), act, alpha, _kept(pre, (n, m)),
                                   dx.data_ptr() if want_x else None, dw.data_ptr() if want_weight else None, _DTYPES[grad_dtype],
@@ -111,10 +121,10 @@ def coop_gated(x, gate, up, gate_bias=None, up_bias=None, act=COOP_ACT_SILU, wan
     (n, k), f, dtype = x.shape, gate.shape[0], _DTYPES[x.dtype]
     upp = _same(up, x, "up", f, k)
     if out is None:
-        out = _new((n, f), x.dtype, x.device, stream)
+        out = _new_like(x, stream, (n, f))
     op = _same(out, x, "out", n, f)
     pre = _new((2, n, f), torch.float32, x.device, stream) if want_pre else None
-    keep, sp, sb = _workspace(lib().coop_gated_workspace_bytes(n, k, f, dtype, (xp | gp | upp) & 15 == 0), workspace, x.device, stream)
+    keep, sp, sb = _workspace(_need("coop_gated", n, k, f, dtype, (xp | gp | upp) & 15 == 0), workspace, x.device, stream)
     _check(lib().coop_gated(xp, n, k, gp, upp, f, dtype, _bias(gate_bias, f, x, "gate_bias"), _bias(up_bias, f, x, "up_bias"), act, op,
                             pre.data_ptr() if want_pre else None, sp, sb, _stream_ptr(stream)))
     return (out, pre) if want_pre else out
@@ -130,7 +140,7 @@ def coop_gated_grad(dout, x, gate, up, gate_bias=None, up_bias=None, pre=None, a
     dx = _new_like(x, stream) if want_x else None
     dw = [_new((f, k), grad_dtype, x.device, stream) for _ in range(2)] if want_weight else [None] * 2
     db = [_new(f, torch.float32, x.device, stream) for _ in range(2)] if want_bias else [None] * 2
-    need = lib().coop_gated_grad_workspace_bytes(n, k, f, dtype, pre is not None, (xp | gp | upp) & 15 == 0)
+    need = _need("coop_gated_grad", n, k, f, dtype, pre is not None, (xp | gp | upp) & 15 == 0)
     keep, sp, sb = _workspace(need, workspace, x.device, stream)
     _check(lib().coop_gated_grad(dp, xp, n, k, gp, upp, f, dtype, _bias(gate_bias, f, x, "gate_bias"), _bias(up_bias, f, x, "up_bias"), act,
                                  _kept(pre, (2, n, f)), dx.data_ptr() if want_x else None, *(w.data_ptr() if want_weight else None for w in dw),
@@ -141,15 +151,24 @@ def coop_gated_grad(dout, x, gate, up, gate_bias=None, up_bias=None, pre=None, a
 def _seam(x, f, gate, after, after_weight, after_bias, before, before_weight, before_bias, rms):
     """(shape, types, gate form, flags, addresses) that both calls have in common"""
     fp, (n, dim) = _matrix(f, "f"), f.shape
-    weights = [after_weight, after_bias, before_weight, before_bias]
     assert after or after_weight is None and after_bias is None, "without the norm behind the block it has no weights"
     assert before or before_weight is None and before_bias is None, "without the norm in front of the next block it has no weights"
     assert not rms or after_bias is None and before_bias is None, "a root-mean-square norm has no bias"
     columns = gate is not None and gate.dim() == 1
-    weight_dtype = learn._weight_dtype(f, *weights, gate if columns else None)
-    gp = None if gate is None else _vector(gate, dim, gate.dtype, "gate") if columns else _same(gate, f, "gate", n, dim)
-    ps = [None if w is None else _vector(w, dim, w.dtype, "weight") for w in weights]
-    return fp, n, dim, weight_dtype, gp, 0 if gate is None else 1 if columns else 2, after * _AFTER | before * _BEFORE | rms * _RMS, ps
+    dtype, ps = None, []
+    for w in (gate if columns else None, after_weight, after_bias, before_weight, before_bias):
+        if w is None:
+            ps.append(None)
+            continue
+        if dtype is None:
+            dtype = w.dtype
+            assert dtype in _DTYPES, "weights, biases and the columns' gate have one type: fp32, fp16 or bf16"
+        ps.append(_vector(w, dim, dtype, "weight"))
+    gp = ps.pop(0)
+    if gate is not None and not columns:
+        gp = _same(gate, f, "gate", n, dim)
+    return (fp, n, dim, COOP_F32 if dtype is None else _DTYPES[dtype], gp, 0 if gate is None else 1 if columns else 2,
+            after * _AFTER | before * _BEFORE | rms * _RMS, ps)
 
 
 def coop_residual_norm(x, f, gate=None, alpha=1.0, after=True, after_weight=None, after_bias=None, before=True, before_weight=None, before_bias=None,
@@ -185,7 +204,7 @@ def coop_residual_norm_grad(dr, dy, x, f, stats, gate=None, alpha=1.0, after=Tru
     dgate = None if gate is None else _new(gate.shape, torch.float32 if form == 1 else f.dtype, x.device, stream)
     there = (after, after and not rms, before, before and not rms)
     grads = [_new(dim, torch.float32, x.device, stream) if want_weight and t else None for t in there]
-    need = lib().coop_residual_norm_grad_workspace_bytes(n, dim, _DTYPES[f.dtype]) if want_weight or form == 1 else 0
+    need = _need("coop_residual_norm_grad", n, dim, _DTYPES[f.dtype]) if want_weight or form == 1 else 0
     keep, wp, wb = _workspace(need, workspace, x.device, stream)
     _check(lib().coop_residual_norm_grad(rp, yp, xp, fp, n, dim, _DTYPES[f.dtype], _DTYPES[x.dtype], stats.data_ptr(), gp, form, alpha, norms, *ps[:3],
                                          weight_dtype, dx.data_ptr(), df.data_ptr(), None if gate is None else dgate.data_ptr(),

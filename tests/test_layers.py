@@ -535,6 +535,22 @@ def test_rows_are_by_themselves(path):
 
 
 @gpu
+@pytest.mark.parametrize("n", [4, 3500])
+@pytest.mark.parametrize("dtype", TYPES[1:], ids=IDS[1:])
+def test_gradients_that_leave_the_type(dtype, n):
+    """An infinity in dout, and (fp16) a dz beyond its numbers, are infinities in the gradients, of a call of any size."""
+    g = rng(4)
+    x, w, dy = normal(g, n, 16, dtype=dtype).abs() + 1, normal(g, 24, 16, dtype=dtype).abs() + 0.5, normal(g, n, 24, dtype=dtype)
+    dy[1, 5], dy[2, 7] = float("inf"), -60000.0
+    for dx, dw, db in (P.coop_linear_grad(dy, x, w, act=P.COOP_ACT_RELU, alpha=2.0), P.coop_linear_grad(dy, x, w, act=P.COOP_ACT_SILU, alpha=2.0)):
+        assert (dx[1] == float("inf")).all() and (dw[5] == float("inf")).all() and math.isinf(db[5]) and float(db[7]) < -1e5
+        rows = [i for i in range(n) if i not in (1, 2)]
+        assert torch.isfinite(dx[rows]).all()
+        if dtype == torch.float16:
+            assert (dx[2] == -float("inf")).all() and (dw[7] == -float("inf")).all()
+
+
+@gpu
 @pytest.mark.parametrize("n,dim,dtype", [(300, 1027, torch.bfloat16), (300, 523, torch.float32), (500, 100, torch.float16), (40, 4096, torch.bfloat16), (9, 16384, torch.float16)])
 def test_residual_norm_in_place(n, dim, dtype):
     g = rng(dim)
