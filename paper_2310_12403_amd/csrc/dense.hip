@@ -455,10 +455,13 @@ __global__ __launch_bounds__(kBlock) void k_dense_pad(Copies jobs, uint32_t bloc
 #include "dense_small.h"
 
 // ---- how a call is cut ------------------------------------------------------------------------------------------------------------
-// A product of rows x cols over k, in tiles of 256 x 256, what a wave's registers hold, one block to a CU, or of 128 x 128, two blocks, which
-// take as long for half as much (LDS gives them only half of what the matrix units take): the former for 16-bit operands where that is fewer
-// rounds of the chip.  k is split where there are fewer tiles than blocks that run at a time, as long as every part has four stages.  Where even so
-// half of the chip would be idle the tiles are of 64 x 64 (a pair's 64 x 128): a quarter of the work for each to do one after the other.
+// A product of rows x cols over k, in tiles of 256 x 256 (16 bits; what a wave's registers hold, a block to a CU), of 128 x 128 (two blocks) or of
+// 64 x 64 (five; a pair's 64 x 128, three).  Which, by the rounds of the chip that the tiles take, and what a round takes: what a tile begins and
+// ends with, which nothing hides in a block that is alone, and its stages of 128 bytes of k, which larger tiles read less of LDS for.  (bf16:
+// 8,192 x 4,096 over 4,096 239 us in tiles of 256, 289 of 128; 100,000 x 768 over 128 77, 58, of 64 70; 40,000 x 512 over 1,024 72, 51, 72; 100,000
+// x 64 over 768 54, 34, 29.  fp32: 50,000 x 64 over 768 98 of 128, 55 of 64.)
+// k is split where there are fewer tiles than blocks that run at a time, as long as every part has four stages.  Where even so half of the chip
+// would be idle the tiles are of 64: a quarter of the work for each to do one after the other.
 struct Cut {
   int64_t rows, cols, width;  // width: of a row of parts
   int tile_a, tile_b;
@@ -468,11 +471,19 @@ struct Cut {
   Cut(int64_t rows_, int64_t cols_, int64_t k, int dtype, bool pair) : rows(rows_), cols(cols_) {
     const int per_tile = pair ? 2 : 1;
     const auto tiles_of = [&](int a, int b) { return ((cols * per_tile + a - 1) / a) * ((rows + b - 1) / b); };
-    const auto rounds_of = [&](int t, int each) { return (tiles_of(t, t) + 256 * each - 1) / (256 * each); };
     const int64_t stages = k * element_bytes(dtype) / kWide, most = stages / 4 < 1 ? 1 : stages / 4;
     const auto splits_of = [&](int a, int b) { return at_most((a == 256 ? 256 : 512) / at_most(tiles_of(a, b), 512), most); };
-    tile_a = tile_b = dtype != COOP_F32 && tiles_of(256, 256) >= 256 && rounds_of(256, 1) < rounds_of(128, 2) ? 256 : 128;
-    if (tile_a == 128 && tiles_of(128, 128) * splits_of(128, 128) <= 256) tile_a = 64, tile_b = pair ? 128 : 64;
+    // (microseconds; of splits the stages that each has, and the launch that joins them)
+    const auto time_of = [&](int a, int b, int64_t slots, double ends, double stage) {
+      const int64_t parts = splits_of(a, b), blocks = tiles_of(a, b) * parts;
+      return (double)((blocks + slots - 1) / slots) * (ends + stage * (double)(stages < parts ? 1 : stages / parts)) + (parts > 1 ? 6 : 0);
+    };
+    const bool wide = dtype == COOP_F32;
+    const int small_b = pair ? 128 : 64;
+    const double of_256 = time_of(256, 256, 256, 12, 1.7), of_128 = time_of(128, 128, 512, wide ? 6 : 4, wide ? 4.1 : 1.02);
+    const double of_64 = time_of(64, small_b, pair ? 768 : 1280, 3, pair ? (wide ? 2.5 : 0.8) : (wide ? 2.4 : 0.95));
+    tile_a = tile_b = !wide && of_256 < of_128 ? 256 : 128;
+    if (tile_a == 128 && (tiles_of(128, 128) * splits_of(128, 128) <= 256 || of_64 < of_128)) tile_a = 64, tile_b = small_b;
     tiles_a = (uint32_t)((cols * per_tile + tile_a - 1) / tile_a);
     tiles_b = (uint32_t)((rows + tile_b - 1) / tile_b);
     splits = (uint32_t)splits_of(tile_a, tile_b);
