@@ -201,9 +201,12 @@ def coop_residual_norm_grad(dr, dy, x, f, stats, gate=None, alpha=1.0, after=Tru
     assert before or dr is not None, "without the norm in front of the next block r's gradient is all there is"
     assert stats.is_cuda and stats.is_contiguous() and stats.dtype == torch.float32 and tuple(stats.shape) == (4, n), "stats: as coop_residual_norm gives them"
     dx, df = _new_like(x, stream), _new_like(f, stream)
-    dgate = None if gate is None else _new(gate.shape, torch.float32 if form == 1 else f.dtype, x.device, stream)
-    there = (after, after and not rms, before, before and not rms)
-    grads = [_new(dim, torch.float32, x.device, stream) if want_weight and t else None for t in there]
+    # (the sums over the rows, fp32 [dim]: one allocation for all of them)
+    there = (form == 1, *(want_weight and t for t in (after, after and not rms, before, before and not rms)))
+    sums = iter(_new((sum(there), dim), torch.float32, x.device, stream).unbind() if any(there) else ())
+    dgate, *grads = (next(sums) if t else None for t in there)
+    if form == 2:
+        dgate = _new_like(gate, stream)
     need = _need("coop_residual_norm_grad", n, dim, _DTYPES[f.dtype]) if want_weight or form == 1 else 0
     keep, wp, wb = _workspace(need, workspace, x.device, stream)
     _check(lib().coop_residual_norm_grad(rp, yp, xp, fp, n, dim, _DTYPES[f.dtype], _DTYPES[x.dtype], stats.data_ptr(), gp, form, alpha, norms, *ps[:3],
