@@ -576,14 +576,14 @@ struct DensePlan {
       if (!again || small) parts = 0;
       if (!small && back.part_bytes > parts) parts = back.part_bytes;
       if (!small && weight.part_bytes > parts) parts = weight.part_bytes;
-      // the columns' sums: by the product's waves of rows, or by the blocks that go over the rows (some 1,024 of them: 8,192 x 4,096 bf16 18.4 us
-      // with the parts' sum; 4,096: 26.9)
+      // the columns' sums: by the product's waves of rows, or by the blocks that go over the rows (where they do nothing else some 1,024
+      // of them: 8,192 x 4,096 bf16 18.4 us with the parts' sum; 4,096: 26.9.  With dz to write, 8,192 x 5,632 gated: 156, and 138)
       const int64_t packs = mw / e;
       lanes_log2 = 0;
       while (lanes_log2 < 6 && 1 << lanes_log2 < packs) ++lanes_log2;
       slope_x = (uint32_t)((packs + (1 << lanes_log2) - 1) >> lanes_log2);
       const int64_t groups = (n + (kBlock >> lanes_log2) - 1) / (kBlock >> lanes_log2);
-      slope_y = (uint32_t)at_most(groups, small ? 128 : n * m <= 1 << 19 ? 64 : 1024 / slope_x + 1);  // (of little, so few that one launch adds up what they have)
+      slope_y = (uint32_t)at_most(groups, small ? 128 : n * m <= 1 << 19 ? 64 : (slope ? 4096 : 1024) / slope_x + 1);  // (of little, so few that one launch adds up what they have)
       sum_rows = again && small ? (n + kSmallRows - 1) / kSmallRows * 2 : again && forward.splits == 1 ? forward.sum_rows(gated) : (int64_t)slope_y * kWavesPerBlock;
       const size_t sum_bytes = (size_t)sum_rows * (size_t)m * 4;
       part = take(sum_bytes);

@@ -99,9 +99,9 @@ def gradients64(dzs, edzs, x, weights, dtype, grad_dtype, rounds):
     return out
 
 
-# (one tile, none whole, many rows, many columns, long k, tiles of 256 in each of the products)
+# (one tile, none whole, many rows, many columns, long k, tiles of 64, 128 and 256 in each of the products, with k in parts and whole)
 SIZES = [(0, 5, 3), (1, 1, 1), (3, 7, 5), (1, 4096, 64), (17, 2000, 300), (33, 64, 128), (130, 100, 75), (257, 129, 300), (300, 602, 41), (1000, 16, 8),
-         (20000, 33, 40), (5000, 128, 128), (70000, 128, 64), (2049, 32, 128), (64, 127, 121), (31, 8, 8), (3000, 64, 31), (70001, 24, 20), (4097, 72, 4100), (4097, 4100, 72), (72, 4100, 4104), (1, 2, 9000), (2, 9000, 1)]
+         (20000, 33, 40), (5000, 128, 128), (70000, 128, 64), (2049, 32, 128), (64, 127, 121), (31, 8, 8), (3000, 64, 31), (70001, 24, 20), (4097, 72, 4100), (4097, 4100, 72), (72, 4100, 4104), (1, 2, 9000), (2, 9000, 1), (33000, 1024, 2048)]
 
 
 @gpu
