@@ -460,7 +460,7 @@ int coop_adamw(const coop_adamw_tensor* tensors, int n, int bits, double lr, dou
  *   out       device [n, m] of dtype; pre_out device float [n, m] or NULL
  *   workspace at least coop_linear_workspace_bytes(n, k, m, dtype, aligned) bytes, aligned = 1 if x and weight are multiples of 16, else 0.
  *             and a multiple of 256; none, and NULL, where that is 0.  (Where a call is not small or narrow, operands that are not aligned, or whose
- *             rows are no multiple of 16 bytes, are copied into the workspace; up to 32 MB are for parts of products that have too few tiles.)
+ *             rows are no multiple of 16 bytes, are copied into the workspace; up to 68 MB are for parts of products that have too few tiles.)
  * n <= 2^31 - 512; k, m <= 2^18 (and together no more than 2^31 tiles).  COOP_ACT_GELU is z Phi(z) with the normal distribution's Phi, COOP_ACT_SILU z / (1 + exp(-z)).
  */
 #define COOP_ACT_NONE 0
