@@ -429,8 +429,8 @@ def clip_calls(seed=0):
 
 
 CALLS = [lambda p=p: dense_calls(*p) for p in PATHS] + [lambda p=p: seam_calls(*p) for p in ((torch.bfloat16, 900, 100), (torch.float16, 300, 2050), (torch.float32, 70, 1000),
-                                                                                             (torch.bfloat16, 30, 9000))] + [clip_calls]
-CALL_IDS = ["%s-%d-%d-%d" % ((str(p[0])[6:],) + p[1:]) for p in PATHS] + ["seam-100", "seam-2050", "seam-1000", "seam-9000", "clip"]
+                                                                                             (torch.bfloat16, 30, 9000), (torch.bfloat16, 600, 4096))] + [clip_calls]
+CALL_IDS = ["%s-%d-%d-%d" % ((str(p[0])[6:],) + p[1:]) for p in PATHS] + ["seam-100", "seam-2050", "seam-1000", "seam-9000", "seam-4096", "clip"]
 
 
 def same(a, b):
