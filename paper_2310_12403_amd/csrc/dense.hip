@@ -568,7 +568,7 @@ struct DensePlan {
       slope = gated || act != COOP_ACT_NONE || (!small && (!aligned || mw != m));
       dz_ld = gated ? 2 * mw : mw;
       if (dz_ld * es % 2048 == 0) dz_ld += 256 / es;  // (or a tile's rows would all lie in the same few channels of memory)
-      rest = small && slope && es == 2 && n * both <= kRestMost;
+      rest = small && slope && es == 2 && (n * both <= kRestMost || k <= 16);
       dz = take(slope ? (size_t)n * dz_ld * (rest ? 4 : es) : 0);
       pre = take(again && !small && forward.splits > 1 ? (size_t)n * m * 4 * (gated ? 2 : 1) : 0);
       back = Cut(n, k, mw, dtype, false);

@@ -4,8 +4,9 @@
 // As in dense_few.h a block has 16 columns by 32 rows of a result and its waves deal the common dimension among themselves.  An operand that
 // has that dimension as its row number comes 16 bytes of a row at a time, 16 columns of a step, and is turned in the wave's own LDS.
 //
-// Of few values dz is kept as the sum of two numbers of the operands' type, what it rounds to and the rest (REST), and multiplied by both.  Of many
-// that rounding adds to the result's own as noise does, 1.41 times; of one row it may be most of what a result is off by (bf16, one row: 2.6 times).
+// Of few values, or where the results are one tile of columns, dz is kept as the sum of two numbers of the operands' type, what it rounds to and the
+// rest (REST), and multiplied by both.  Of many that rounding adds to the result's own as noise does, 1.41 times; of one row it may be most of what a
+// result is off by (bf16, one row: 2.6 times).
 // (All of them so: 3,001 x 100 x 275 gated both ways 55 us for 39, 1,024 x 256 x 256 14.1 for 11.0.)
 #pragma once
 
