@@ -452,8 +452,9 @@ int coop_adamw(const coop_adamw_tensor* tensors, int n, int bits, double lr, dou
 /*
  * Layers of a model on such rows: a dense layer with its epilogue, and the gated block's two projections.  Elements of all operands are of one
  * dtype; what the activation is of (the products plus their biases) can be kept in 32 bits, pre_out, for the gradient calls, which
- * otherwise compute it again.  dz, the gradient of that, is rounded to dtype, being an operand of the matrix units; of few
- * values (up to 2^16, or k <= 16, in a small call) what it loses by that is kept and multiplied too.
+ * otherwise compute it again.  dz, the gradient of that, is rounded to dtype, being an operand of the matrix units (which takes dx and the weight's gradient
+ * 1.41 times as far from exact as their own rounding); where it has up to 2^16 values (of a gated block: both parts'), or min(n, m) k <= 2^12, so that
+ * dx or the weight's gradient has few, what it loses by that is kept and multiplied too.
  *
  * coop_linear: out = alpha act(x transposed(weight) + bias) + residual.
  *   x         device [n, k], weight device [m, k], bias device [m] or NULL, residual device [n, m] or NULL (may be out); all of dtype

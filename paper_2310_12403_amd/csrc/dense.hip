@@ -1,8 +1,8 @@
 // Dense layers on rows: y = alpha act(x W' + b) + residual, and the gated block's h = act(x Wg' + bg) (x Wu' + bu), with their gradients.
 //
 // Backward, with z the products plus their biases: dz = alpha dy act'(z) (gated: dg = dh u act'(g), du = dh act(g)), then dx = dz W,
-// dW = dz' x, db = sum over the rows of dz.  dz is an operand of the matrix units and so rounded to the operands' type; db is summed from it
-// before that.  z is either what the forward call kept, in 32 bits, or computed again.
+// dW = dz' x, db = sum over the rows of dz.  dz is an operand of the matrix units and so rounded to the operands' type (of few values: the sum of
+// two numbers of it); db is summed from it before that.  z is either what the forward call kept, in 32 bits, or computed again.
 //
 // All products are tiles of C = A B' (products.h): A has the columns of the result, so that a lane's registers hold neighbouring ones, and B
 // its rows.  The gated product's two weights are one operand with 32 rows of each in turn: a wave has the gate's and the up projection's sums
@@ -59,6 +59,13 @@ __device__ __forceinline__ void store_columns(void* row, int32_t col, int32_t di
     for (int e = 0; e < E; ++e)
       if (col + e < dim) p[e] = (M)f[e];
   }
+}
+
+// what a value loses when it is rounded to the type
+template <int T>
+__device__ __forceinline__ float lost_to(float v) {
+  const float r = v - (float)(typename Element<T>::M)v;
+  return fabsf(r) < __builtin_inff() ? r : 0.f;  // (what is not finite, or not in the type, has none)
 }
 
 // ---- what becomes of a product's sums --------------------------------------------------------------------------------------
@@ -130,7 +137,7 @@ struct Slope {
   int32_t cols;
   float alpha;
   int act;
-  int64_t rest;  // bytes from dz to what it lost to its type; 0: that is not kept
+  int64_t rest;  // bytes from dz to what it lost to its type, in the same row; 0: that is not kept
   template <int E>
   struct Lane {
     int32_t col;
@@ -168,13 +175,8 @@ struct Slope {
     store_elements<T, E>(dz + (row * ld + l.col) * kElem<T>, d);
     if (PAIR) store_elements<T, E>(dz + (row * ld + second + l.col) * kElem<T>, d2);
     if (T == COOP_F32 || rest == 0) return;
-    typedef typename Element<T>::M M;
-    const auto lost = [](float v) {
-      const float r = v - (float)(M)v;
-      return fabsf(r) < __builtin_inff() ? r : 0.f;  // (what is not finite, or not in the type, has none)
-    };
 #pragma unroll
-    for (int e = 0; e < E; ++e) d[e] = lost(d[e]), d2[e] = PAIR ? lost(d2[e]) : 0.f;
+    for (int e = 0; e < E; ++e) d[e] = lost_to<T>(d[e]), d2[e] = PAIR ? lost_to<T>(d2[e]) : 0.f;
     store_elements<T, E>(dz + rest + (row * ld + l.col) * kElem<T>, d);
     if (PAIR) store_elements<T, E>(dz + rest + (row * ld + second + l.col) * kElem<T>, d2);
   }
@@ -261,10 +263,11 @@ struct Tiles {
   }
 };
 
-template <int T, int WA, int WB, int TA, int TB, bool SA, bool SB, int SIZE, int FORM, typename Fin>
+// TWICE: B with what is added to it.
+template <int T, int WA, int WB, int TA, int TB, bool SA, bool SB, int SIZE, int FORM, bool TWICE, typename Fin>
 __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1))) void k_dense(Operand a, Operand a2, Operand b, Operand b2, int64_t k,
                                                                                                Tiles tiles, Fin fin) {
-  typedef Product<T, WA, WB, TA, TB, SA, SB, SIZE, FORM == kPair> P;
+  typedef Product<T, WA, WB, TA, TB, SA, SB, SIZE, FORM == kPair, TWICE> P;
   extern __shared__ char lds[];
   constexpr int kColsA = FORM == kPair ? P::kRowsA / 2 : P::kRowsA;  // of the result
   const Tiles::Mine mine = tiles.mine();
@@ -461,14 +464,15 @@ __global__ __launch_bounds__(kBlock) void k_dense_pad(Copies jobs, uint32_t bloc
 // 8,192 x 4,096 over 4,096 239 us in tiles of 256, 289 of 128; 100,000 x 768 over 128 77, 58, of 64 70; 40,000 x 512 over 1,024 72, 51, 72; 100,000
 // x 64 over 768 54, 34, 29.  fp32: 50,000 x 64 over 768 98 of 128, 55 of 64.)
 // k is split where there are fewer tiles than blocks that run at a time, as long as every part has four stages.  Where even so half of the chip
-// would be idle the tiles are of 64: a quarter of the work for each to do one after the other.
+// would be idle the tiles are of 64: a quarter of the work for each to do one after the other.  `twice`: every stage is multiplied by both parts of B (few
+// values, or few results: not in tiles of 256).
 struct Cut {
   int64_t rows, cols, width;  // width: of a row of parts
   int tile_a, tile_b;
   uint32_t tiles_a, tiles_b, splits;
   size_t part_bytes;
   Cut() : rows(0), cols(0), width(0), tile_a(0), tile_b(0), tiles_a(0), tiles_b(0), splits(0), part_bytes(0) {}
-  Cut(int64_t rows_, int64_t cols_, int64_t k, int dtype, bool pair) : rows(rows_), cols(cols_) {
+  Cut(int64_t rows_, int64_t cols_, int64_t k, int dtype, bool pair, bool twice = false) : rows(rows_), cols(cols_) {
     const int per_tile = pair ? 2 : 1;
     const auto tiles_of = [&](int a, int b) { return ((cols * per_tile + a - 1) / a) * ((rows + b - 1) / b); };
     const int64_t stages = k * element_bytes(dtype) / kWide, most = stages / 4 < 1 ? 1 : stages / 4;
@@ -476,13 +480,13 @@ struct Cut {
     // (microseconds; of splits the stages that each has, and the launch that joins them)
     const auto time_of = [&](int a, int b, int64_t slots, double ends, double stage) {
       const int64_t parts = splits_of(a, b), blocks = tiles_of(a, b) * parts;
-      return (double)((blocks + slots - 1) / slots) * (ends + stage * (double)(stages < parts ? 1 : stages / parts)) + (parts > 1 ? 6 : 0);
+      return (double)((blocks + slots - 1) / slots) * (ends + stage * (double)((stages < parts ? 1 : stages / parts) * (twice ? 2 : 1))) + (parts > 1 ? 6 : 0);
     };
     const bool wide = dtype == COOP_F32;
     const int small_b = pair ? 128 : 64;
     const double of_256 = time_of(256, 256, 256, 12, 1.7), of_128 = time_of(128, 128, 512, wide ? 6 : 4, wide ? 4.1 : 1.02);
     const double of_64 = time_of(64, small_b, pair ? 768 : 1280, 3, pair ? (wide ? 2.5 : 0.8) : (wide ? 2.4 : 0.95));
-    tile_a = tile_b = !wide && of_256 < of_128 ? 256 : 128;
+    tile_a = tile_b = !wide && !twice && of_256 < of_128 ? 256 : 128;
     if (tile_a == 128 && (tiles_of(128, 128) * splits_of(128, 128) <= 256 || of_64 < of_128)) tile_a = 64, tile_b = small_b;
     tiles_a = (uint32_t)((cols * per_tile + tile_a - 1) / tile_a);
     tiles_b = (uint32_t)((rows + tile_b - 1) / tile_b);
@@ -512,20 +516,29 @@ void with_narrow(int64_t k, int64_t m, F&& f) {
   else mt(std::integral_constant<int, 8>());
 }
 
+// whether what dz loses fits the narrow gradient's LDS
+constexpr bool narrow_rest(int64_t k, int64_t m) { return k <= 32 || m <= 64; }
+
 int narrow_shares(int64_t k, int64_t m) {
   int shares = 1;
   with_narrow(k, m, [&](auto ks, auto mt) { shares = NarrowBackward<COOP_BF16, decltype(ks)::value, decltype(mt)::value>::kShares; });
   return shares;
 }
 
+// Of 16 bits dz is an operand of the matrix units, rounded to the type, or the sum of two numbers of the type, and the products take both.  Rounded once it
+// makes a gradient 1.41 times as far from 64 bits as its own rounding does, whatever the sizes, as noise of the same size does; but of few results that is 1.41 give or take
+// much (worst of 8 draws, both types: 64 values of dW 2.2 times, 256 1.7, 1,024 1.6, 2,048 1.5, from 4,096 on 1.46).  So both are kept where a result, dx
+// or one weight's gradient, has few values, and where dz itself has so few that it costs next to nothing.
+constexpr int64_t kRestResults = 1 << 12, kRestValues = 1 << 16;
+
 // The parts of a call, and where in the workspace they are.  GATED: two weights of m rows.
 struct DensePlan {
   int64_t n, k, m, kw, mw;  // kw, mw: elements of a row of k or m, up to a multiple of 16 bytes
-  int64_t dz_ld;            // elements; a pair's second part begins at mw
+  int64_t dz_ld, half;      // elements; a pair's second part begins at mw, what dz loses to its type at half
   bool gated, pad, slope, again;  // slope: dz is not dout itself; again: the forward product is computed again
   bool few;                       // forward, of few rows or small: the kernel of dense_few.h
   bool small;                     // gradient, of what is small: the kernels of dense_small.h
-  bool rest;                      // and with what dz loses to its type
+  bool rest;                      // gradient with what dz loses to its type
   bool narrow;                    // 8 to 128 by 8 to 128 in 16 bits: the kernels of dense_narrow.h (but not from what was kept)
   uint32_t narrow_tiles, narrow_blocks;
   Cut forward, back, weight;      // (dx and dW)
@@ -549,7 +562,9 @@ struct DensePlan {
     again = grad && !keeps && (gated || act != COOP_ACT_NONE);
     small = grad && n * es <= kSmallLength && both * es <= kSmallLength && little(k_tiles * n_tiles, 16 + kSmallRows, both, 4096) &&
             little(k_tiles * ((both + kSmallRows - 1) / kSmallRows), 16 + kSmallRows, n, 4096) && (!again || few_fits);
-    narrow = !few && !small && es == 2 && !gated && k >= 8 && k <= 128 && m >= 8 && m <= 128 && !(grad && keeps && act != COOP_ACT_NONE);
+    // (by what is computed alone, and not by which kernels do it)
+    rest = grad && es == 2 && (gated || act != COOP_ACT_NONE) && (n * m * (gated ? 2 : 1) <= kRestValues || (n < m ? n : m) * k <= kRestResults);
+    narrow = !few && !small && es == 2 && !gated && k >= 8 && k <= 128 && m >= 8 && m <= 128 && !(grad && keeps && act != COOP_ACT_NONE) && (!rest || narrow_rest(k, m));
     narrow_tiles = (uint32_t)((n + 31) / 32);
     narrow_blocks = (uint32_t)(grad ? at_most((narrow_tiles + 7) / 8, 256) : at_most((narrow_tiles + kNarrowForwardWaves - 1) / kNarrowForwardWaves, 512));
     pad = !narrow && !few && !small && (!aligned || kw != k);
@@ -561,18 +576,19 @@ struct DensePlan {
     forward = Cut(n, m, kw, dtype, gated);
     size_t parts = narrow || few ? 0 : forward.part_bytes;
     dz = pre = part = part2 = join = 0;
-    slope = rest = false;
+    slope = false;
+    half = 0;
     if (grad && narrow) {
       parts = (size_t)narrow_blocks * (size_t)narrow_shares(k, m) * (size_t)m * (size_t)(round_up(k, 8) + kNarrowSums) * 4;
     } else if (grad) {
       slope = gated || act != COOP_ACT_NONE || (!small && (!aligned || mw != m));
-      dz_ld = gated ? 2 * mw : mw;
+      half = gated ? 2 * mw : mw;
+      dz_ld = rest ? 2 * half : half;
       if (dz_ld * es % 2048 == 0) dz_ld += 256 / es;  // (or a tile's rows would all lie in the same few channels of memory)
-      rest = small && slope && es == 2 && (n * both <= kRestMost || k <= 16);
-      dz = take(slope ? (size_t)n * dz_ld * (rest ? 4 : es) : 0);
+      dz = take(slope ? (size_t)n * dz_ld * es : 0);
       pre = take(again && !small && forward.splits > 1 ? (size_t)n * m * 4 * (gated ? 2 : 1) : 0);
-      back = Cut(n, k, mw, dtype, false);
-      weight = Cut(gated ? 2 * mw : m, k, n, dtype, false);
+      back = Cut(n, k, mw, dtype, false, rest);
+      weight = Cut(gated ? 2 * mw : m, k, n, dtype, false, rest);
       if (!again || small) parts = 0;
       if (!small && back.part_bytes > parts) parts = back.part_bytes;
       if (!small && weight.part_bytes > parts) parts = weight.part_bytes;
@@ -610,21 +626,21 @@ bool allow_lds(int bytes) {
   return true;
 }
 
-template <int T, int WA, int WB, int TA, int TB, bool SA, bool SB, int SIZE, int FORM, typename Fin>
+template <int T, int WA, int WB, int TA, int TB, bool SA, bool SB, int SIZE, int FORM, bool TWICE, typename Fin>
 bool launch_tiles(int id, const Cut& c, const Operand& a, const Operand& a2, const Operand& b, const Operand& b2, int64_t k, const Fin& fin, hipStream_t s) {
   typedef Product<T, WA, WB, TA, TB, SA, SB, SIZE, FORM == kPair> P;
-  constexpr auto kernel = k_dense<T, WA, WB, TA, TB, SA, SB, SIZE, FORM, Fin>;
+  constexpr auto kernel = k_dense<T, WA, WB, TA, TB, SA, SB, SIZE, FORM, TWICE, Fin>;
   if (!allow_lds<kernel>(P::kLds)) return false;
   COOP_LAUNCH(id, kernel, dim3((unsigned)c.blocks()), dim3(P::kThreads), P::kLds, s, a, a2, b, b2, k, Tiles{c.tiles_a, c.tiles_b, c.splits}, fin);
   return true;
 }
-template <int T, bool SA, bool SB, int SIZE, int FORM, typename Fin>
+template <int T, bool SA, bool SB, int SIZE, int FORM, bool TWICE, typename Fin>
 bool launch_product(int id, const Cut& c, const Operand& a, const Operand& a2, const Operand& b, const Operand& b2, int64_t k, const Fin& fin, hipStream_t s) {
-  if constexpr (T != COOP_F32)
-    if (c.tile_a == 256) return launch_tiles<T, 2, 2, 4, 4, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, fin, s);
-  if (c.tile_a == 128) return launch_tiles<T, 2, 2, 2, 2, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, fin, s);
-  if constexpr (FORM == kPair) return launch_tiles<T, 1, 4, 2, 1, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, fin, s);  // (a wave has columns of both)
-  else return launch_tiles<T, 2, 2, 1, 1, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, fin, s);
+  if constexpr (T != COOP_F32 && !TWICE)
+    if (c.tile_a == 256) return launch_tiles<T, 2, 2, 4, 4, SA, SB, SIZE, FORM, false>(id, c, a, a2, b, b2, k, fin, s);
+  if (c.tile_a == 128) return launch_tiles<T, 2, 2, 2, 2, SA, SB, SIZE, FORM, TWICE>(id, c, a, a2, b, b2, k, fin, s);
+  if constexpr (FORM == kPair) return launch_tiles<T, 1, 4, 2, 1, SA, SB, SIZE, FORM, TWICE>(id, c, a, a2, b, b2, k, fin, s);  // (a wave has columns of both)
+  else return launch_tiles<T, 2, 2, 1, 1, SA, SB, SIZE, FORM, TWICE>(id, c, a, a2, b, b2, k, fin, s);
 }
 
 template <int T, bool PAIR, typename Fin>
@@ -636,12 +652,21 @@ void join(const float* sums, int splits, int64_t rows, int64_t width, int32_t co
 }
 
 // A product and its epilogue, through parts where k is split.
-template <int T, bool SA, bool SB, int SIZE, int FORM, typename Fin>
+template <int T, bool SA, bool SB, int SIZE, int FORM, bool TWICE = false, typename Fin>
 bool product(int id, const Cut& c, const Operand& a, const Operand& a2, const Operand& b, const Operand& b2, int64_t k, const Fin& fin, float* sums, hipStream_t s) {
-  if (c.splits == 1) return launch_product<T, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, fin, s);
-  if (!launch_product<T, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, Part<FORM == kPair>{sums, c.rows, c.width, 0}, s)) return false;
+  if (c.splits == 1) return launch_product<T, SA, SB, SIZE, FORM, TWICE>(id, c, a, a2, b, b2, k, fin, s);
+  if (!launch_product<T, SA, SB, SIZE, FORM, TWICE>(id, c, a, a2, b, b2, k, Part<FORM == kPair>{sums, c.rows, c.width, 0}, s)) return false;
   if constexpr (!Fin::kSums) join<T, FORM == kPair>(sums, (int)c.splits, c.rows, c.width, (int32_t)c.cols, fin, s);
   return true;
+}
+
+// The same where B may have a rest (16 bits).
+template <int T, bool SA, bool SB, int SIZE, int FORM, typename Fin>
+bool product_of_dz(int id, const Cut& c, bool rest, const Operand& a, const Operand& a2, const Operand& b, const Operand& b2, int64_t k, const Fin& fin, float* sums,
+                   hipStream_t s) {
+  if constexpr (T != COOP_F32)
+    if (rest) return product<T, SA, SB, SIZE, FORM, true>(id, c, a, a2, b, b2, k, fin, sums, s);
+  return product<T, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, fin, sums, s);
 }
 
 struct Arrays {  // what the products read: the caller's, or copies
@@ -716,11 +741,20 @@ bool backward_narrow(const DensePlan& p, const NarrowLayer& l, const void* dout,
   float* const sums = dw != nullptr || db != nullptr ? (float*)(ws + p.sums) : nullptr;
   const int32_t db_col = dw != nullptr ? (int32_t)round_up(p.k, 8) : 0, width = db_col + kNarrowSums;
   with_narrow(p.k, p.m, [&](auto ks, auto mt) {
-    constexpr int KS = decltype(ks)::value, MT = decltype(mt)::value, lds = NarrowBackward<T, KS, MT>::kLds;
-    const bool exact = p.k == KS * 16 && p.m == MT * 32 && aligned16(l.x, dout, dx);
-    const auto kernel = exact ? k_narrow_grad<T, KS, MT, true> : k_narrow_grad<T, KS, MT, false>;
-    ok = exact ? allow_lds<k_narrow_grad<T, KS, MT, true>>(lds) : allow_lds<k_narrow_grad<T, KS, MT, false>>(lds);
-    if (ok) COOP_LAUNCH(K_DENSE_DX, kernel, dim3(p.narrow_blocks), dim3(512), lds, s, l, (const char*)dout, (char*)dx, sums, width, p.narrow_tiles);
+    constexpr int KS = decltype(ks)::value, MT = decltype(mt)::value;
+    const auto launch = [&](auto exact, auto rest) {
+      constexpr auto kernel = k_narrow_grad<T, KS, MT, decltype(exact)::value, decltype(rest)::value>;
+      constexpr int lds = NarrowBackward<T, KS, MT, decltype(rest)::value>::kLds;
+      ok = allow_lds<kernel>(lds);
+      if (ok) COOP_LAUNCH(K_DENSE_DX, kernel, dim3(p.narrow_blocks), dim3(512), lds, s, l, (const char*)dout, (char*)dx, sums, width, p.narrow_tiles);
+    };
+    const auto either = [&](auto rest) {
+      if (p.k == KS * 16 && p.m == MT * 32 && aligned16(l.x, dout, dx)) launch(std::true_type(), rest);
+      else launch(std::false_type(), rest);
+    };
+    if constexpr (narrow_rest(KS * 16, MT * 32))
+      if (p.rest) return either(std::true_type());
+    either(std::false_type());
   });
   if (!ok || sums == nullptr) return ok;
   const Gradient g{(char*)dw, nullptr, p.m, 0, (int32_t)p.k, l.act == COOP_ACT_NONE ? l.alpha : 1.f, grad_dtype};
@@ -769,7 +803,7 @@ bool backward_all(const DensePlan& p, const void* dout, const void* x, const voi
   fin.part2 = (float*)(ws + p.part2);
   fin.rows = p.n, fin.ld = p.dz_ld, fin.second = p.mw, fin.cols = (int32_t)p.m;
   fin.alpha = alpha, fin.act = act;
-  fin.rest = p.rest ? p.n * p.dz_ld * kElem<T> : 0;
+  fin.rest = p.rest ? p.half * kElem<T> : 0;
   if (p.again && p.small) {
     few_product<T, PAIR>(p, x, w, w2, fin, s);
   } else if (p.again && p.forward.splits == 1) {
@@ -804,13 +838,13 @@ bool backward_all(const DensePlan& p, const void* dout, const void* x, const voi
   if (dx != nullptr) {
     const Gradient g{(char*)dx, nullptr, p.n, 0, (int32_t)p.k, scale, T};
     const Operand a{o.w, ldk, ldk, p.m}, a2{o.w2, ldk, ldk, p.m};
-    const Operand b{dz, ldz, p.n, p.mw * kElem<T>}, b2{dz + (PAIR ? p.mw * kElem<T> : 0), ldz, p.n, p.mw * kElem<T>};
-    if (!product<T, true, false, kWide, PAIR ? kTwo : kOne>(K_DENSE_DX, p.back, a, a2, b, b2, p.mw, g, sums, s)) return false;
+    const Operand b{dz, ldz, p.n, p.mw * kElem<T>, fin.rest}, b2{dz + (PAIR ? p.mw * kElem<T> : 0), ldz, p.n, p.mw * kElem<T>, fin.rest};
+    if (!product_of_dz<T, true, false, kWide, PAIR ? kTwo : kOne>(K_DENSE_DX, p.back, p.rest, a, a2, b, b2, p.mw, g, sums, s)) return false;
   }
   if (dw != nullptr) {
     const Gradient g{(char*)dw, PAIR ? (char*)dw2 : nullptr, p.m, p.mw, (int32_t)p.k, scale, grad_dtype};
-    const Operand a{o.x, ldk, ldk, p.n}, b{dz, ldz, (PAIR ? 2 * p.mw : p.mw) * kElem<T>, p.n};
-    if (!product<T, true, true, kNarrow, kOne>(K_DENSE_DW, p.weight, a, a, b, b, p.n, g, sums, s)) return false;
+    const Operand a{o.x, ldk, ldk, p.n}, b{dz, ldz, (PAIR ? 2 * p.mw : p.mw) * kElem<T>, p.n, fin.rest};
+    if (!product_of_dz<T, true, true, kNarrow, kOne>(K_DENSE_DW, p.weight, p.rest, a, a, b, b, p.n, g, sums, s)) return false;
   }
   return true;
 }

@@ -199,16 +199,16 @@ __global__ __launch_bounds__(kNarrowForwardWaves* kWave) void k_narrow(NarrowLay
 
 // The whole gradient in one pass over x and dout: z once more, dz, dx, and the sums for the weight's gradient and the bias's.  A block has 32 rows
 // for each of its eight waves at a time, two to a SIMD, so that one's activations (some 130 cycles a value of gelu's slope: as much as the memory takes)
-// run beside the other's products.  dW is dealt to the waves by tiles of 32 x 32 (of few tiles, by parts of the rows too): the rows of x and dz of all of
+// run beside the other's products.  (REST: what dz loses to its type is multiplied too, and meets it in LDS.)  dW is dealt to the waves by tiles of 32 x 32 (of few tiles, by parts of the rows too): the rows of x and dz of all of
 // them meet in LDS, where the product over the rows reads them transposed; so is the weight, which is there once, for dx.
-template <int T, int KS, int MT>
+template <int T, int KS, int MT, bool REST = false>
 struct NarrowBackward {
   static constexpr int kWaves = 8, KT = KS / 2, kTiles = KT * MT;
   static constexpr int kMine = kTiles > kWaves ? kTiles / kWaves : 1;     // tiles of dW that a wave has, neighbours along m
   static constexpr int kShares = kTiles < kWaves ? kWaves / kTiles : 1;   // waves that share a tile, by their rows
   typedef Staged<T, MT * 32, true, kNarrow, 1> Z;
   typedef Staged<T, KT * 32, true, kNarrow, 1> X;
-  static constexpr int kWeight = MT * KS * 1024, kLds = kWeight + kWaves * (Z::kBytes + X::kBytes);
+  static constexpr int kZ = (REST ? 2 : 1) * Z::kBytes, kOwn = kZ + X::kBytes, kWeight = MT * KS * 1024, kLds = kWeight + kWaves * kOwn;
   static_assert(kLds <= 160 * 1024 && kWaves * MT * 32 * 4 <= kLds - kWeight, "a CU's LDS");
 };
 constexpr int kNarrowSums = 8;  // columns behind those of dW in a part: the bias's gradient in the first of them
@@ -229,17 +229,17 @@ __device__ __forceinline__ int anew(int x) {
 }
 
 // parts: [blocks][kShares][m][width], of the `width - kNarrowSums` columns of dW (none: it is not asked for) and db's; null: neither is.
-template <int T, int KS, int MT, bool EXACT>
+template <int T, int KS, int MT, bool EXACT, bool REST>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_narrow_grad(NarrowLayer l, const char* __restrict__ dout, char* __restrict__ dx,
                                                                                                 float* __restrict__ parts, int32_t width, uint32_t tiles) {
-  typedef NarrowBackward<T, KS, MT> B;
+  typedef NarrowBackward<T, KS, MT, REST> B;
   typedef typename Element<T>::M M;
-  constexpr int KT = B::KT, kOwn = B::Z::kBytes + B::X::kBytes;
+  constexpr int KT = B::KT, kOwn = B::kOwn;
   extern __shared__ char lds[];
   const int wave = uniform_wave_in_block(), lane = lane_id(), half = lane >> 5, r32 = lane & 31;
-  char* const staged = lds + B::kWeight;  // of each wave: dz, then x
+  char* const staged = lds + B::kWeight;  // of each wave: dz, what it lost, then x
   char* const own_z = staged + wave * kOwn;
-  char* const own_x = own_z + B::Z::kBytes;
+  char* const own_x = own_z + B::kZ;
   // the weight, row by row, as the product over its rows reads it
   for (int i = threadIdx.x; i < MT * 32 * KS * 2; i += 512) {
     const int row = i / (KS * 2), chunk = i % (KS * 2);
@@ -326,6 +326,11 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
           for (int e = 0; e < 8; ++e) d[e] = whole || live ? d[e] * l.alpha * s[e] : 0.f;
           dz[c] = swap_halves(pack8<T>(d));
+          if constexpr (REST) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e] = lost_to<T>(d[e]);
+            *reinterpret_cast<u32x4*>(own_z + B::Z::kBytes + r * (MT * 64) + (((2 * c + half) ^ B::Z::swizzle(r)) << 4)) = swap_halves(pack8<T>(s));
+          }
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -347,7 +352,14 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
         for (int e = 0; e < 16; ++e) v[e] = 0.f;
 #pragma unroll
-        for (int s = 0; s < 2 * MT; ++s) v = mma<T>(B::X::fragment(lds, t * 32, s, at), dz[s], v);
+        for (int s = 0; s < 2 * MT; ++s) {
+          const u32x4 w = B::X::fragment(lds, t * 32, s, at);
+          v = mma<T>(w, dz[s], v);
+          if constexpr (REST) {  // (what the lane has written)
+            const int row = at & 31;
+            v = mma<T>(w, *reinterpret_cast<const u32x4*>(own_z + B::Z::kBytes + row * (MT * 64) + (((2 * s + (at >> 5)) ^ B::Z::swizzle(row)) << 4)), v);
+          }
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           float f[8];
@@ -366,9 +378,12 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         const char* z = staged + w * kOwn;
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
-          const u32x4 a = B::X::fragment(z + B::Z::kBytes, mine_t * 32, kk, at);
+          const u32x4 a = B::X::fragment(z + B::kZ, mine_t * 32, kk, at);
 #pragma unroll
-          for (int i = 0; i < B::kMine; ++i) dw[i] = mma<T>(a, B::Z::fragment(z, (mine_i + i) * 32, kk, at), dw[i]);
+          for (int i = 0; i < B::kMine; ++i) {
+            dw[i] = mma<T>(a, B::Z::fragment(z, (mine_i + i) * 32, kk, at), dw[i]);
+            if constexpr (REST) dw[i] = mma<T>(a, B::Z::fragment(z + B::Z::kBytes, (mine_i + i) * 32, kk, at), dw[i]);
+          }
         }
       }
       narrow_meet();

@@ -4,10 +4,8 @@
 // As in dense_few.h a block has 16 columns by 32 rows of a result and its waves deal the common dimension among themselves.  An operand that
 // has that dimension as its row number comes 16 bytes of a row at a time, 16 columns of a step, and is turned in the wave's own LDS.
 //
-// Of few values, or where the results are one tile of columns, dz is kept as the sum of two numbers of the operands' type, what it rounds to and the
-// rest (REST), and multiplied by both.  Of many that rounding adds to the result's own as noise does, 1.41 times; of one row it may be most of what a
-// result is off by (bf16, one row: 2.6 times).
-// (All of them so: 3,001 x 100 x 275 gated both ways 55 us for 39, 1,024 x 256 x 256 14.1 for 11.0.)
+// With REST dz is the sum of two numbers of the operands' type and multiplied by both.  (All of them so: 3,001 x 100 x 275 gated both ways 55 us for 39, 1,024 x
+// 256 x 256 14.1 for 11.0.)
 #pragma once
 
 struct SmallGrad {
@@ -23,7 +21,6 @@ struct SmallGrad {
 // kSmallLength: bytes of the common dimension, 12 steps for each wave (longer ones take too long in the few blocks of a weight's gradient: 8,192 rows
 // of 64 by 64, 36.6 us for the 16.2 of dense_narrow.h).  8 waves for 16, which are idle where it is short: bf16 1,024 x 256 x 256 11.0 us for 13.1,
 // 256 x 1,024 x 512 13.1 for 19.9; 4: 12.5 and 12.5, and 31.5 for 26.4 with 3,001 rows.
-constexpr int64_t kRestMost = 1 << 16;  // values of dz
 constexpr int kSmallWaves = 8, kSmallRows = 32, kSmallLength = 12 * 8 * 64;
 
 // 16 bytes of a row from column `col` on, zeros behind column `dim`

@@ -39,7 +39,7 @@ __device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
 struct Operand {
   const char* base;
   int64_t ld, rows, k;
-  int64_t other = 0;  // of a pair: bytes from this one to the other
+  int64_t other = 0;  // of a pair, or of two parts that are added up: bytes from this one to the other
 };
 
 // How a stage of R rows of an operand lies in LDS, in 16-byte slots filled in order by the loads, 64 to a wave's load.
@@ -151,11 +151,13 @@ struct Staged {
 
 // A block's tile of C: WA x WB waves with TA x TB tiles of 32 x 32 each, rows of A by rows of B.  The stages of all of a block's tiles
 // are one stream: while one is multiplied the next kStages - 1 are on their way, the first of the next tile among them.
-template <int T, int WA, int WB, int TA, int TB, bool SA, bool SB, int SIZE, bool PAIR = false>
+// TWICE: B is the sum of two operands of one layout, and every stage of A is multiplied by both of its stages of B, one after the other (A's comes from L2
+// the second time).
+template <int T, int WA, int WB, int TA, int TB, bool SA, bool SB, int SIZE, bool PAIR = false, bool TWICE = false>
 struct Product {
   static constexpr int kWaves = WA * WB, kThreads = kWaves * kWave;
   static constexpr int kRowsA = WA * TA * 32, kRowsB = WB * TB * 32;
-  static constexpr int kK = SIZE / kElem<T>, kSteps = SIZE / 32, kStages = 256 / SIZE;
+  static constexpr int kK = SIZE / kElem<T>, kSteps = SIZE / 32, kStages = 256 / SIZE, kTimes = TWICE ? 2 : 1;
   typedef Staged<T, kRowsA, SA, SIZE, kWaves, PAIR> A;
   typedef Staged<T, kRowsB, SB, SIZE, kWaves> B;
   static constexpr int kStage = A::kBytes + B::kBytes, kLds = kStages * kStage;
@@ -172,6 +174,7 @@ struct Product {
   int stages;
   int step_rows;                // from tile to tile, of A; 0: there is one tile
   int64_t step_bytes;
+  int64_t to_rest;              // TWICE: bytes from B to what is added to it
   char* lds;
 
   __device__ __forceinline__ static int a0() { return uniform_wave_in_block() / WB * (TA * 32); }
@@ -182,6 +185,15 @@ struct Product {
 
   // to the next stage of the stream
   __device__ __forceinline__ void next() {
+    if constexpr (TWICE) {
+      if ((left-- & 1) == 0) {  // (an even number are left ahead of a stage's first time)
+        b.p += to_rest;
+        sb = loads_b.stage(b);
+        return;
+      }
+      b.p -= to_rest;
+      ++left;
+    }
     a.next(loads_a.ld);
     b.next(loads_b.ld);
     --left;
@@ -264,7 +276,8 @@ struct Product {
     lds = lds_;
     step_rows = step;
     step_bytes = step * op_a.ld;
-    left = stages = (int)((k1 - k0 + kK - 1) / kK);
+    to_rest = op_b.other;
+    left = stages = (int)((k1 - k0 + kK - 1) / kK) * kTimes;
     a = typename A::Place(op_a, row_a, k0);
     b = typename B::Place(op_b, row_b, k0);
     loads_a.begin(op_a, a);
@@ -282,7 +295,8 @@ struct Product {
     lds = lds_;
     step_rows = 1 << 30;  // (more than there are: behind the second part there is nothing to load)
     step_bytes = 0;
-    left = stages = (int)((k1 - k0 + kK - 1) / kK);
+    to_rest = op_b.other;
+    left = stages = (int)((k1 - k0 + kK - 1) / kK) * kTimes;
     a = typename A::Place(op_a, row_a, k0);
     b = typename B::Place(op_b, row_b, k0);
     loads_a.begin(op_a, a);

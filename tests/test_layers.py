@@ -184,6 +184,65 @@ def test_activations_over_their_range(act):
     assert math.isnan(dx[-1]) == (act != P.COOP_ACT_NONE)
 
 
+# ---- what dz loses to a type of 16 bits --------------------------------------------------------------------------------------------
+# Where dz has up to 2^16 values, or a result (dx, or one weight's gradient) up to 2^12, dz is multiplied as the sum of two numbers of the type, whichever
+# kernels do it: (n, k, m) of the small ones, of products in tiles with k whole and in parts, of the narrow ones, whole and ragged, and of few rows of
+# wide layers, on both sides of what those kernels are chosen by.
+KEPT_REST = [(1, 1, 1), (3, 7, 5), (15, 16, 17), (33, 31, 64), (1, 1024, 2048), (300, 64, 200), (1, 1024, 3080), (1, 64, 3100), (1, 4096, 520), (2, 2000, 6000), (20, 17, 3200),
+             (24, 1030, 2000), (3100, 1, 20), (3080, 16, 16), (6000, 1024, 3), (20000, 300, 9), (70001, 24, 20), (20000, 33, 40), (5000, 64, 64), (4100, 128, 32), (4100, 128, 16),
+             (9000, 100, 40), (9000, 32, 128), (5000, 30, 120), (5000, 40, 100), (20000, 128, 7), (3100, 1, 1024), (70000, 4, 600)]
+
+
+def keeps_rest(n, k, m, both):
+    return n * both <= 1 << 16 or min(n, m) * k <= 1 << 12
+
+
+def nearly_rounded_once(got, want, dtype, what):
+    """The results' distance from 64 bits is what rounding them to the type makes, and a tenth more; of results in 32 bits, a 16th of half a unit of dz's type.
+    (In two parts a dz is off by HALF^2 of itself and by 32 bits' own, z's among them: some 64 u, 2^-18.  A result whose terms' signs are random is off by as
+    much of itself, and is rounded to another number than 64 bits' only where it lies that near to the middle of two.  One rounding of dz alone makes 0.4 HALF.)"""
+    off, want = float((got.double() - want).norm()), want.double()
+    if got.dtype == torch.float32:
+        assert off <= HALF[dtype] / 16 * float(want.norm()), "%s: %g of the most" % (what, off / (HALF[dtype] / 16 * float(want.norm())))
+    else:
+        once = float((want.to(dtype).double() - want).norm())
+        assert off <= 1.1 * once + 2.0 ** -18 * float(want.norm()) + TINY[dtype], "%s: %g times one rounding" % (what, off / max(once, 1e-300))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES[1:], ids=IDS[1:])
+@pytest.mark.parametrize("n,k,m", KEPT_REST)
+def test_few_values_or_results_keep_what_dz_loses(dtype, n, k, m):
+    assert keeps_rest(n, k, m, m)
+    for place in (lambda t: t, unaligned):
+        g = rng(n + 3 * k + m)
+        x, dy = place(normal(g, n, k, dtype=dtype)), place(normal(g, n, m, dtype=dtype))
+        w, w2 = (place(normal(g, m, k, dtype=dtype, scale=1 / math.sqrt(k))) for _ in range(2))
+        b = place(normal(g, m, dtype=dtype, scale=0.3))
+        for act in (P.COOP_ACT_GELU, P.COOP_ACT_SILU):
+            z, ez = product64(x, w, b)
+            dz = dy.double() * act64(z, act)[1]
+            dx, dw = dz @ w.double(), dz.t().contiguous() @ x.double()
+            _, pre = P.coop_linear(x, w, b, act=act, want_pre=True)
+            for kept in (pre, None):
+                for grad_dtype in (dtype, torch.float32):
+                    got = P.coop_linear_grad(dy, x, w, b, pre=kept, act=act, grad_dtype=grad_dtype)
+                    for name, have, want in zip(("dx", "dw"), got, (dx, dw)):
+                        nearly_rounded_once(have, want, dtype, "%s, act %d, kept %s" % (name, act, kept is not None))
+        if not keeps_rest(n, k, m, 2 * m):
+            continue
+        (zg, _), (zu, _) = product64(x, w, b), product64(x, w2, None)
+        a, slope = act64(zg, P.COOP_ACT_SILU)
+        dg, du = dy.double() * zu * slope, dy.double() * a
+        wants = dg @ w.double() + du @ w2.double(), dg.t().contiguous() @ x.double(), du.t().contiguous() @ x.double()
+        _, pre = P.coop_gated(x, w, w2, b, None, want_pre=True)
+        for kept in (pre, None):
+            for grad_dtype in (dtype, torch.float32):
+                got = P.coop_gated_grad(dy, x, w, w2, b, None, pre=kept, grad_dtype=grad_dtype)
+                for name, have, want in zip(("dx", "dgate", "dup"), got, wants):
+                    nearly_rounded_once(have, want, dtype, "gated %s, kept %s" % (name, kept is not None))
+
+
 # ---- the seam between two blocks -------------------------------------------------------------------------------------------------
 class Norm64:
     """A norm of the rows of v, which is known to `ev`, and how far 32 bits may be from what follows."""
@@ -532,6 +591,19 @@ def test_rows_are_by_themselves(path):
         got = call()
         assert torch.equal(got[good], before[good]), i
         assert torch.isnan(got[bad[0]]).any(), i
+
+
+# (what dz loses is kept: tiles with k whole, and in parts, of few rows; narrow, whole and ragged; tiles where the narrow kernel's memory is too small; tiles of many rows)
+REST_PATHS = [(torch.bfloat16, 1, 1024, 3080), (torch.float16, 20, 72, 3200), (torch.bfloat16, 4100, 128, 32), (torch.float16, 9000, 100, 40), (torch.bfloat16, 5000, 40, 100),
+              (torch.float16, 20000, 300, 9)]
+
+
+@gpu
+@pytest.mark.parametrize("path", REST_PATHS, ids=["%s-%d-%d-%d" % ((str(p[0])[6:],) + p[1:]) for p in REST_PATHS])
+def test_paths_that_keep_what_dz_loses(path):
+    test_same_bits_on_another_stream_with_any_workspace_and_in_a_graph(lambda: dense_calls(*path))
+    test_what_is_asked_for_alone_is_the_same(path)
+    test_rows_are_by_themselves(path)
 
 
 @gpu
