@@ -474,6 +474,8 @@ int coop_linear(const void* x, int64_t n, int32_t k, const void* weight, int32_t
 
 /*
  * Its gradient: dz = alpha dout act'(pre), dx = dz weight, dweight = transposed(dz) x, dbias = sum over the rows of dz.  (The residual's is dout.)
+ * What is rounded to dtype on the way is dout act'(pre), times alpha only where that is above 1 (and there is an activation); a number beyond dtype's is an
+ * infinity there.
  *   pre       what coop_linear kept; NULL: computed again (bias is read then only); not read without an activation
  *   dx        device [n, k] of dtype; dweight device [m, k] of grad_dtype (COOP_F32 or dtype); dbias device float [m]; each may be NULL
  *   workspace at least coop_linear_grad_workspace_bytes(n, k, m, dtype, act, has_pre, aligned) bytes, aligned = 1 if dout, x and weight

@@ -135,7 +135,7 @@ struct Slope {
   float *part, *part2;  // [waves of rows][cols], or null
   int64_t rows, ld, second;
   int32_t cols;
-  float alpha;
+  float alpha, into;  // (the factor, and what of it is multiplied into dz)
   int act;
   int64_t rest;  // bytes from dz to what it lost to its type, in the same row; 0: that is not kept
   template <int E>
@@ -165,10 +165,9 @@ struct Slope {
         d[e] = there ? d[e] * u[e] * v[e] : 0.f;
         l.s2[e] += d2[e];
         l.s[e] += d[e];
-      } else {  // (without an activation the factor is the results', and dz the gradient as it came)
-        const float scaled = there ? d[e] * alpha * v[e] : 0.f;
-        if (act != COOP_ACT_NONE) d[e] = scaled;
-        l.s[e] += scaled;
+      } else {  // (without an activation dz is the gradient as it came)
+        l.s[e] += there ? d[e] * alpha * v[e] : 0.f;
+        if (act != COOP_ACT_NONE) d[e] = there ? d[e] * into * v[e] : 0.f;
       }
     }
     if (dz == nullptr) return;
@@ -669,6 +668,13 @@ bool product_of_dz(int id, const Cut& c, bool rest, const Operand& a, const Oper
   return product<T, SA, SB, SIZE, FORM>(id, c, a, a2, b, b2, k, fin, sums, s);
 }
 
+// alpha is left to the results, so that of one below 1 no dz is lost below the numbers of its type.  (One above 1 is multiplied into dz, for the same reason: what
+// falls below them is lost without a trace, and what is beyond them is an infinity that a program sees.)  Without an activation dz is dout, and all of it left to them.
+struct Alpha { float into, results; };
+Alpha split_alpha(float alpha, int act) {
+  return act != COOP_ACT_NONE && fabsf(alpha) > 1.f ? Alpha{alpha, 1.f} : Alpha{1.f, alpha};
+}
+
 struct Arrays {  // what the products read: the caller's, or copies
   const char *x, *w, *w2;
 };
@@ -757,7 +763,7 @@ bool backward_narrow(const DensePlan& p, const NarrowLayer& l, const void* dout,
     either(std::false_type());
   });
   if (!ok || sums == nullptr) return ok;
-  const Gradient g{(char*)dw, nullptr, p.m, 0, (int32_t)p.k, l.act == COOP_ACT_NONE ? l.alpha : 1.f, grad_dtype};
+  const Gradient g{(char*)dw, nullptr, p.m, 0, (int32_t)p.k, l.results, grad_dtype};
   join<T, false>(sums, (int)p.narrow_blocks * narrow_shares(p.k, p.m), p.m, width, db_col + 1, NarrowGradient{g, db, db_col}, s);
   return true;
 }
@@ -770,7 +776,7 @@ bool forward_all(const DensePlan& p, const void* x, const void* w, const void* w
   }
   if constexpr (T != COOP_F32 && !PAIR)
     if (p.narrow) {
-      const NarrowLayer l{(const char*)x, (const char*)w, fin.bias, p.n, (int32_t)p.k, (int32_t)p.m, fin.alpha, fin.act};
+      const NarrowLayer l{(const char*)x, (const char*)w, fin.bias, p.n, (int32_t)p.k, (int32_t)p.m, fin.alpha, 1.f, fin.act};
       with_narrow(p.k, p.m, [&](auto ks, auto mt) {
         constexpr int KS = decltype(ks)::value, MT = decltype(mt)::value;
         const bool exact = p.k == KS * 16 && p.m == MT * 32 && aligned16(l.x, fin.residual, fin.out);
@@ -789,7 +795,8 @@ bool backward_all(const DensePlan& p, const void* dout, const void* x, const voi
                   int act, float alpha, void* dx, void* dw, void* dw2, int grad_dtype, float* db, float* db2, char* ws, hipStream_t s) {
   if constexpr (T != COOP_F32 && !PAIR)
     if (p.narrow) {
-      const NarrowLayer l{(const char*)x, (const char*)w, (const char*)bias, p.n, (int32_t)p.k, (int32_t)p.m, alpha, act};
+      const Alpha factor = split_alpha(alpha, act);
+      const NarrowLayer l{(const char*)x, (const char*)w, (const char*)bias, p.n, (int32_t)p.k, (int32_t)p.m, factor.into, factor.results, act};
       return backward_narrow<T>(p, l, dout, dx, dw, grad_dtype, db, ws, s);
     }
   const bool products = dx != nullptr || dw != nullptr;
@@ -802,7 +809,8 @@ bool backward_all(const DensePlan& p, const void* dout, const void* x, const voi
   fin.part = db != nullptr || db2 != nullptr ? (float*)(ws + p.part) : nullptr;
   fin.part2 = (float*)(ws + p.part2);
   fin.rows = p.n, fin.ld = p.dz_ld, fin.second = p.mw, fin.cols = (int32_t)p.m;
-  fin.alpha = alpha, fin.act = act;
+  const float scale = PAIR ? 1.f : split_alpha(alpha, act).results;
+  fin.alpha = alpha, fin.into = split_alpha(alpha, act).into, fin.act = act;
   fin.rest = p.rest ? p.half * kElem<T> : 0;
   if (p.again && p.small) {
     few_product<T, PAIR>(p, x, w, w2, fin, s);
@@ -818,7 +826,6 @@ bool backward_all(const DensePlan& p, const void* dout, const void* x, const voi
       COOP_LAUNCH(K_DENSE_SLOPE, (k_dense_slope<T, PAIR>), dim3(p.slope_x, p.slope_y), dim3(kBlock), 0, s, pre, PAIR ? pre + p.n * p.m : nullptr, p.lanes_log2, fin);
   }
   if (p.small) {
-    const float scale = PAIR || act != COOP_ACT_NONE ? 1.f : alpha;
     const int64_t ld = (p.slope ? p.dz_ld : p.m) * kElem<T>, both = PAIR ? p.mw + p.m : p.m;
     const uint32_t k_tiles = (uint32_t)((p.k + 15) / 16), n_tiles = (uint32_t)((p.n + kSmallRows - 1) / kSmallRows), m_tiles = (uint32_t)((both + kSmallRows - 1) / kSmallRows);
     const SmallGrad g{p.slope ? ws + p.dz : (const char*)dout, (const char*)x, (const char*)w, (const char*)w2, p.n, ld, p.mw, fin.rest, (int32_t)p.k, (int32_t)p.m,
@@ -834,7 +841,6 @@ bool backward_all(const DensePlan& p, const void* dout, const void* x, const voi
   if (fin.part != nullptr) sums_of_columns<T>(p, fin.part, fin.part2, db, db2, PAIR, ws, s);
   const int64_t ldk = p.kw * kElem<T>, ldz = p.slope ? p.dz_ld * kElem<T> : p.m * kElem<T>;
   const char* dz = p.slope ? ws + p.dz : (const char*)dout;
-  const float scale = PAIR || act != COOP_ACT_NONE ? 1.f : alpha;
   if (dx != nullptr) {
     const Gradient g{(char*)dx, nullptr, p.n, 0, (int32_t)p.k, scale, T};
     const Operand a{o.w, ldk, ldk, p.m}, a2{o.w2, ldk, ldk, p.m};

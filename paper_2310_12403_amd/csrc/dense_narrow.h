@@ -87,7 +87,7 @@ struct NarrowLayer {
   const char *x, *w, *bias;
   int64_t n;
   int32_t k, m;
-  float alpha;
+  float alpha, results;  // (of a gradient: what is multiplied into dz, and what into the results)
   int act;
 };
 
@@ -345,7 +345,6 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     if (dx != nullptr) {
       const int at = anew(lane);
       const NarrowRows<T, EXACT> to(dx, first + wave, tiles, l.n, l.k, at);
-      const float scale = l.act == COOP_ACT_NONE ? l.alpha : 1.f;
 #pragma unroll
       for (int t = 0; t < KT; ++t) {
         f32x16 v;
@@ -364,7 +363,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int h = 0; h < 2; ++h) {
           float f[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = v[8 * h + e] * scale;
+          for (int e = 0; e < 8; ++e) f[e] = v[8 * h + e] * l.results;
           to.store(2 * t + h, at >> 5, swap_halves(pack8<T>(f)));
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -393,7 +392,6 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   // (the staged rows are read: the waves meet behind their last reads, or have read none)
   float* const sums = reinterpret_cast<float*>(staged);
   narrow_meet();
-  const float scale = l.act == COOP_ACT_NONE ? l.alpha : 1.f;
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -426,7 +424,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     float v[4] = {0.f, 0.f, 0.f, 0.f};
     if (part == 0)
       for (int w = 0; w < B::kWaves; ++w) v[0] += sums[w * (MT * 32) + m];
-    v[0] *= scale;
+    v[0] *= l.results;
     store_elements<COOP_F32, 4>(parts + (((int64_t)blockIdx.x * B::kShares + part) * l.m + m) * width + width - kNarrowSums, v);
   }
 }

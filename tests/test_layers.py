@@ -623,6 +623,34 @@ def test_gradients_that_leave_the_type(dtype, n):
 
 
 @gpu
+@pytest.mark.parametrize("alpha", [2.0 ** -18, 2.0 ** -24, 3.0 * 2.0 ** 12, -2.0 ** -20])
+@pytest.mark.parametrize("n,k,m", [(300, 64, 200), (1, 1024, 3080), (5000, 128, 120), (9000, 100, 40), (4000, 300, 260), (700, 600, 9), (2049, 130, 1024)])
+def test_factors_that_take_dz_out_of_fp16(n, k, m, alpha):
+    """alpha far from 1, of which dout (of a large one) or the weight (of a small one) makes up, so that gradients are well within fp16: a dz that is below its numbers, with
+    alpha or without, is still within half a unit of itself."""
+    dtype = torch.float16
+    g = rng(n + m)
+    up = max(abs(alpha), 1.0)
+    x, dy = normal(g, n, k, dtype=dtype, scale=2.0 ** -10), normal(g, n, m, dtype=dtype, scale=2 / up)
+    w = normal(g, m, k, dtype=dtype, scale=2.0 ** 11 / math.sqrt(k))
+    for act in (P.COOP_ACT_GELU, P.COOP_ACT_RELU):
+        z, ez = product64(x, w, None)
+        slope, es = act64(z, act)[1], act_bound(z, ez, act)[1]
+        d = dy.double() * alpha
+        dz, edz = d * slope, d.abs() * (es + 4 * U * (slope.abs() + es))
+        # (rounded as dz / alpha, or as dz: what TINY is of)
+        off = edz + (dz.abs() + edz) * HALF[dtype] + TINY[dtype] * min(1.0, abs(alpha))
+        _, pre = P.coop_linear(x, w, act=act, want_pre=True)
+        for kept in (pre, None):
+            dx, dw, db = P.coop_linear_grad(dy, x, w, pre=kept, act=act, alpha=alpha, grad_dtype=torch.float32)
+            want = dz.t().contiguous() @ x.double()
+            within(dw, want, off.t().contiguous() @ x.double().abs() + 2 * (n + 8) * U * ((dz.abs() + off).t().contiguous() @ x.double().abs()), "dw")
+            want, size = dz @ w.double(), (dz.abs() + off) @ w.double().abs()
+            within(dx, want, rounded(want, off @ w.double().abs() + 2 * (m + 8) * U * size, dtype), "dx")
+            within(db, dz.sum(0), edz.sum(0) + (n + 8) * U * (dz.abs() + edz).sum(0), "db")
+
+
+@gpu
 @pytest.mark.parametrize("n,dim,dtype", [(300, 1027, torch.bfloat16), (300, 523, torch.float32), (500, 100, torch.float16), (40, 4096, torch.bfloat16), (9, 16384, torch.float16)])
 def test_residual_norm_in_place(n, dim, dtype):
     g = rng(dim)
