@@ -547,7 +547,7 @@ int coop_residual_norm_grad(const void* dr, const void* dy, const void* x, const
  * The norm of many gradients together, and the factor that clips them: norm = |s| sqrt(sum of g^2) with s = *grad_scale (1 where it is
  * NULL), factor = s min(1, max_norm / (norm + 1e-6)).  coop_adamw takes the factor as its grad_scale; coop_grad_scale multiplies the
  * gradients by it where they lie.  Squares are added up in 64 bits.  A gradient that is not finite makes the norm so, and the factor 0
- * (infinities) or no number.
+ * (infinities, with an infinite max_norm too; what is infinite is then no number times that factor) or no number.
  */
 typedef struct {
   void* grad;                /* device, n_rows rows of dim elements (a tensor without rows: one row) */

@@ -113,7 +113,8 @@ __global__ __launch_bounds__(1024) void k_grad_factor(const double* __restrict__
   sum = 0.0;
 #pragma unroll
   for (int w = 0; w < 16; ++w) sum += lds[w];
-  const double s = scale != nullptr ? (double)*scale : 1.0, norm = fabs(s) * sqrt(sum), over = max_norm / (norm + 1e-6);
+  const double s = scale != nullptr ? (double)*scale : 1.0, norm = fabs(s) * sqrt(sum);
+  const double over = norm < __builtin_inf() || norm != norm ? max_norm / (norm + 1e-6) : 0.0;  // (an infinite norm is above any bound, an infinite one too)
   if (norm_out != nullptr) *norm_out = (float)norm;
   if (factor_out != nullptr) *factor_out = (float)(over >= 1.0 ? s : s * over);  // (of a norm that is no number: no number)
 }

@@ -408,6 +408,25 @@ def test_grad_norm_of_extremes_and_of_what_is_not_finite():
 
 
 @gpu
+@pytest.mark.parametrize("bound", [0.0, 1.0, 1e30, float("inf")])
+def test_grad_norm_that_is_not_finite_by_any_bound(bound):
+    """The factor of an infinite norm is 0 and of what is no number none, by a bound of infinity as by any other."""
+    x = torch.ones(100, device="cuda", dtype=torch.bfloat16)
+    x[57] = -float("inf")
+    scale = torch.tensor([-2.0], device="cuda")
+    for s in (None, scale):
+        norm, factor = P.GradNorm([torch.ones(3, device="cuda"), x]).measure(bound, grad_scale=s)
+        assert float(norm) == float("inf") and float(factor) == 0.0
+    x[3] = float("nan")
+    norm, factor = P.GradNorm([x]).measure(bound)
+    assert math.isnan(float(norm)) and math.isnan(float(factor))
+    x[:] = 3e38     # (a norm beyond 32 bits of gradients that are finite)
+    norm, factor = P.GradNorm([x]).measure(bound)
+    want = float(x[0].double()) * 10
+    assert float(norm) == float("inf") and abs(float(factor) - min(1.0, bound / want)) <= 2 * U * min(1.0, bound / want) + 2.0 ** -149
+
+
+@gpu
 def test_grad_norm_of_touched_rows_and_the_step_that_it_scales():
     """The rows that coop_embed_grad_rows gives, without waiting for their number: what lies behind them does not count and stays."""
     g = rng(5)
