@@ -33,7 +33,7 @@ extern "C" {
 #define COOP_E_RANGE (-2)     /* a vertex id / seed is outside [0, n_vertices) */
 #define COOP_E_DUPSEED (-3)   /* the seed list holds a vertex twice */
 #define COOP_E_ARG (-4)       /* bad scalar argument (L < 1, fanout < 1, unknown sampler/dtype, ...) */
-#define COOP_E_NOMEM (-5)     /* the allocator callback returned NULL */
+#define COOP_E_NOMEM (-5)     /* the allocator callback returned NULL, or the host has no memory for a call */
 #define COOP_E_CAPACITY (-6)  /* a fixed-size workspace would overflow */
 #define COOP_E_HIP (-7)       /* a HIP runtime call failed */
 #define COOP_E_GRAPH (-8)     /* malformed CSR (COOP_VALIDATE), or a graph registered with COOP_SYMMETRIC is not symmetric */
@@ -561,7 +561,8 @@ typedef struct {
 size_t coop_grad_norm_workspace_bytes(const coop_grad_tensor* tensors, int n);
 int coop_grad_norm(const coop_grad_tensor* tensors, int n, double max_norm, const float* grad_scale, float* norm_out, float* factor_out,
                    void* workspace, size_t workspace_bytes, void* stream);
-/* g <- g * *factor, rounded to the gradient's type; nothing is written where the factor is 1 */
+/* g <- g * *factor, rounded to the gradient's type; nothing is written where the factor is 1.  Tensors that have elements in common are refused (COOP_E_ARG; the norm counts
+ * what is given twice twice) */
 int coop_grad_scale(const coop_grad_tensor* tensors, int n, const float* factor, void* stream);
 
 /* Name of an error code (static string). */

@@ -3,6 +3,11 @@
 //
 // Bound by HBM: every gradient is read once.  Squares are added up in 64 bits, where those of numbers of 24 bits are exact, nothing overflows and
 // nothing is lost, in an order that the sizes alone decide: a lane's, a block's, and then one block's over all of them.
+#include <algorithm>
+#include <memory>
+#include <new>
+#include <utility>
+
 #include "coop_internal.h"
 #include "elements.h"
 
@@ -179,6 +184,23 @@ int grads_check(const coop_grad_tensor* tensors, int n) {
   return COOP_OK;
 }
 
+// Whether no two of them have an element in common (COOP_OK): blocks that multiply the same one meet in memory.
+int grads_apart(const coop_grad_tensor* tensors, int n) {
+  typedef std::pair<uintptr_t, uintptr_t> Range;
+  const std::unique_ptr<Range[]> at(new (std::nothrow) Range[(size_t)n]);
+  if (!at) return COOP_E_NOMEM;
+  int k = 0;
+  for (int i = 0; i < n; ++i) {
+    const uintptr_t p = (uintptr_t)tensors[i].grad;
+    const int64_t count = tensors[i].n_rows * tensors[i].dim;
+    if (count > 0) at[k++] = Range(p, p + (uintptr_t)count * (uintptr_t)element_bytes(tensors[i].dtype));
+  }
+  std::sort(at.get(), at.get() + k);
+  for (int i = 1; i < k; ++i)
+    if (at[i].first < at[i - 1].second) return COOP_E_ARG;
+  return COOP_OK;
+}
+
 }  // namespace
 }  // namespace coop
 
@@ -218,6 +240,8 @@ extern "C" int coop_grad_scale(const coop_grad_tensor* tensors, int n, const flo
   if (n == 0) return COOP_OK;
   if (!factor) return COOP_E_NULL;
   if (((uintptr_t)factor & 3) != 0) return COOP_E_ARG;
+  const int apart = grads_apart(tensors, n);
+  if (apart != COOP_OK) return apart;
   const hipStream_t s = (hipStream_t)stream;
   in_launches(tensors, n, [&](Grads& g, uint32_t blocks) {
     g.factor = factor;

@@ -973,6 +973,36 @@ def test_refusals_of_the_c_abi():
     assert L.coop_grad_scale(t, 0, N, N) == 0 and L.coop_grad_scale(t, 1, N, N) == -1 and L.coop_grad_scale(t, 1, A + 2, N) == -4
 
 
+def test_gradients_with_elements_in_common_are_not_scaled():
+    """One given twice, one within another and one that begins within another are refused before anything is launched, in any order."""
+    L = layers.lib()
+    A = 0x10000
+
+    def common(*tensors):
+        t = (layers._CGradTensor * len(tensors))()
+        for c, (at, rows, dim, dtype) in zip(t, tensors):
+            c.grad, c.n_rows, c.dim, c.dtype = at, rows, dim, dtype
+        return L.coop_grad_scale(t, len(tensors), A, None) == -4
+
+    one = (A, 4, 8, 0)                       # 128 bytes
+    for other in (one, (A + 124, 1, 1, 0), (A - 4, 1, 2, 0), (A + 64, 1, 8, 2), (A - 64, 1, 1000, 1)):
+        assert common(one, other) and common(other, one) and common(one, (A + 4096, 1, 8, 0), (A - 4096, 0, 8, 0), other)
+
+
+@gpu
+def test_gradients_side_by_side_are_scaled():
+    """Neighbours in memory have nothing in common, nor has one of no elements, in any order."""
+    flat = torch.ones(96, device="cuda")
+    parts = [flat[64:96], flat[0:32], flat[16:16], flat[32:64], flat[40:40]]
+    P.GradNorm(parts).apply(torch.full((1,), 0.5, device="cuda"))
+    assert (flat == 0.5).all()
+    with pytest.raises(P.CoopError) as e:
+        P.GradNorm([flat, flat[:1]]).apply(torch.full((1,), 0.5, device="cuda"))
+    assert e.value.code == -4 and (flat == 0.5).all()
+    norm, _ = P.GradNorm([flat, flat]).measure()
+    assert abs(float(norm) - math.sqrt(48.0)) <= 2 * U * 7
+
+
 @gpu
 def test_refusals_of_the_binding():
     x, w, v = torch.zeros((8, 6), device="cuda"), torch.zeros((5, 6), device="cuda"), torch.zeros(6, device="cuda")
