@@ -278,6 +278,7 @@ __global__ __launch_bounds__(WA* WB* kWave) __attribute__((amdgpu_waves_per_eu(1
     p.begin_two(a, b, a2, b2, col0, row0, k0, k1, lds);
     p.zero();
     p.tile();
+    p.last();
     p.tile();
   } else {
     p.begin(a, b, col0, row0, k0, k1, 0, lds);

@@ -289,11 +289,11 @@ struct Product {
     if (step == 0) next_a.there = next_b.there = 0;  // (behind the only tile there is nothing to load)
     start_stream();
   }
-  // The same for one tile whose k has two parts, of operands of their own and as long as each other: tile() twice.
+  // The same for one tile whose k has two parts, of operands of their own and as long as each other: tile(), last(), tile().
   __device__ __forceinline__ void begin_two(const Operand& op_a, const Operand& op_b, const Operand& then_a, const Operand& then_b, int64_t row_a,
                                             int64_t row_b, int64_t k0, int64_t k1, char* lds_) {
     lds = lds_;
-    step_rows = 1 << 30;  // (more than there are: behind the second part there is nothing to load)
+    step_rows = 0;
     step_bytes = 0;
     to_rest = op_b.other;
     left = stages = (int)((k1 - k0 + kK - 1) / kK) * kTimes;
@@ -304,6 +304,15 @@ struct Product {
     next_a = typename A::Place(then_a, row_a, k0);
     next_b = typename B::Place(then_b, row_b, k0);
     start_stream();
+  }
+  // What is loaded next is the second part's, from its second stage on: behind it there is nothing to load.
+  __device__ __forceinline__ void last() {
+    next_a.there = next_b.there = 0;
+    if (left == stages) {  // (it has one stage)
+      a.there = b.there = 0;
+      sa = loads_a.stage(a);
+      sb = loads_b.stage(b);
+    }
   }
   __device__ __forceinline__ void start_stream() {
     slot = kStages - 1;
