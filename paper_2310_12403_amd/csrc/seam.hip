@@ -28,6 +28,7 @@ struct SeamShape {
   bool after, before, rms;
   int gate;     // COOP_GATE_..
   bool wide_w;  // weights, biases and the columns' gate are fp32
+  bool last_in_lds;  // N_before's bias is, where the others are
 };
 
 constexpr int kColumnGate = COOP_GATE_COLUMNS, kRowGate = COOP_GATE_ELEMENTS;
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(kNormBlock<WAVES>) __attribute__((amdgpu_waves_per_
   typedef SeamWeights<T, E, WHOLE> Weights;
   const Weights gate_of(sh.gate == kColumnGate ? wp.gate : nullptr, sh.wide_w, 1.f, sh.dim, next_weights), w1_of(wp.w1, sh.wide_w, 1.f, sh.dim, next_weights);
   const Weights b1_of(wp.b1, sh.wide_w, 0.f, sh.dim, next_weights), w2_of(wp.w2, sh.wide_w, 1.f, sh.dim, next_weights);
-  const Weights b2_of(wp.b2, sh.wide_w, 0.f, sh.dim, next_weights);
+  const Weights b2_of(wp.b2, sh.wide_w, 0.f, sh.last_in_lds ? sh.dim : kSeamLdsDim + 1, next_weights);
   __syncthreads();
   SeamPacks<S, E, K> next_x;  // (the next row is on its way while this one is worked on)
   SeamPacks<T, E, K> next_f, next_g;
@@ -452,6 +453,8 @@ __global__ __launch_bounds__(kSeamJoinWaves* kWave) void k_seam_join(const float
   if (out.dgate != nullptr) out.dgate[c] = sh.after ? value(wp.w1, 1.f) * a + value(wp.b1, 0.f) * b : a;
 }
 
+constexpr int kLdsPiece = 1280;  // what a block's LDS is a multiple of
+
 // How a row is shared: a pack a lane on one wave or less, on 2, 4 or 8 waves, and wider ones 2 or 4 packs a lane on 8.  (A pack a lane, for the
 // registers: what a gradient holds for each column is 4 sums and 5 values besides the next row's.)
 struct SeamLayout { int e, k, waves, lanes, lanes_log2; };
@@ -466,12 +469,21 @@ bool seam_layout(int32_t dim, int dtype, SeamLayout* out) {
   return l.k <= 4;
 }
 
+// Blocks of a CU, by its registers, and of a forward call by what its weights take of the LDS too.  (A gradient's blocks have more registers, and fit.  A grid for the
+// registers alone takes a second round for what does not fit.  bf16, a gate for each column and all weights and biases: 32,768 rows of 2,048 141 us, for 109, 65,536 of
+// 1,024 157, for 108; 16,384 of 4,096 142, one block a CU 136, and with the last bias from memory two, 110.)
+int64_t seam_resident(const SeamLayout& l, bool grad, int weights) {
+  const int64_t most = 4 * seam_waves(l.e, l.k, l.waves, grad) / (l.waves == 1 ? kWavesPerBlock : l.waves);
+  if (grad) return most;
+  const int64_t fit = 160 * 1024 / ((weights + 16 * l.waves + kLdsPiece - 1) / kLdsPiece * kLdsPiece);
+  return fit < most ? fit : most;
+}
 // Blocks of a pass: as many as are on the chip at once, and for a gradient no more
 // than leave each group two rows.
-int64_t seam_blocks(int64_t rows, const SeamLayout& l, bool grad) {
+int64_t seam_blocks(int64_t rows, const SeamLayout& l, bool grad, int weights = 0) {
   const int64_t per_block = l.waves == 1 ? kBlock / l.lanes : 1;
   int64_t b = (rows + per_block - 1) / per_block;
-  const int64_t most = 256 * 4 * seam_waves(l.e, l.k, l.waves, grad) / (l.waves == 1 ? kWavesPerBlock : l.waves);
+  const int64_t most = 256 * seam_resident(l, grad, weights);
   if (b > most) b = most;
   if (grad && b > rows / (2 * per_block) + 1) b = rows / (2 * per_block) + 1;
   return b;
@@ -516,7 +528,7 @@ int seam_check(int64_t rows, int32_t dim, int dtype, int stream_dtype, int weigh
 }
 SeamShape seam_shape(int64_t rows, int32_t dim, const SeamLayout& l, float alpha, float eps, int norms, int gate_form, int weight_dtype) {
   return SeamShape{rows, dim, l.lanes, l.lanes_log2, eps, alpha, (norms & COOP_NORM_AFTER) != 0, (norms & COOP_NORM_BEFORE) != 0, (norms & COOP_NORM_RMS) != 0,
-                   gate_form, weight_dtype == COOP_F32};
+                   gate_form, weight_dtype == COOP_F32, true};
 }
 
 }  // namespace
@@ -541,10 +553,14 @@ extern "C" int coop_residual_norm(const void* x, const void* f, int64_t n_rows, 
     if (!aligned_for(p, weight_dtype)) return COOP_E_ARG;
   if (gate && !aligned_for(gate, gate_form == COOP_GATE_COLUMNS ? weight_dtype : dtype)) return COOP_E_ARG;
   if (((uintptr_t)stats_out & 3) != 0) return COOP_E_ARG;
-  const SeamShape sh = seam_shape(n_rows, dim, l, alpha, eps, norms, gate_form, weight_dtype);
+  SeamShape sh = seam_shape(n_rows, dim, l, alpha, eps, norms, gate_form, weight_dtype);
   const SeamWeightPointers wp{(const char*)gate, (const char*)after_weight, (const char*)after_bias, (const char*)before_weight, (const char*)before_bias};
-  const dim3 grid((unsigned)seam_blocks(n_rows, l, false));
-  const int weights = seam_lds(wp, gate_form == COOP_GATE_COLUMNS, dim);
+  int weights = seam_lds(wp, gate_form == COOP_GATE_COLUMNS, dim);
+  if (before_bias && weights > 0) {  // (a block would be alone on its CU for the last of its vectors: that is read from memory)
+    const int without = weights - ((dim + 3) & ~3) * 4;
+    if (seam_resident(l, false, weights) == 1 && seam_resident(l, false, without) > 1) weights = without, sh.last_in_lds = false;
+  }
+  const dim3 grid((unsigned)seam_blocks(n_rows, l, false, weights));
   with_seam_types(dtype, stream_dtype, [&](auto t, auto st) {
     constexpr int T = decltype(t)::value, S = decltype(st)::value;
     with_seam_layout<T>(l, dim, [&](auto e, auto k, auto waves, auto whole) {

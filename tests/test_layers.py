@@ -365,6 +365,23 @@ def test_residual_norm(dtype, n, dim):
         assert (dw1 is None) == (not after) and (dw2 is None) == (not before) and (db1 is None) == (rms or not after) and (db2 is None) == (rms or not before)
 
 
+@gpu
+@pytest.mark.parametrize("dim", [512, 1024, 1500, 2048, 4060, 4096])
+@pytest.mark.parametrize("wt", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_residual_norm_of_more_rows_than_are_on_the_chip_at_once(dim, wt):
+    """With all weights and biases, which take the most of LDS: the same as the rows a few at a time, bit for bit."""
+    g = rng(dim)
+    n = 5000
+    x, f = normal(g, n, dim, dtype=torch.bfloat16), normal(g, n, dim, dtype=torch.bfloat16)
+    w = [normal(g, dim, dtype=wt) for _ in range(5)]
+    kw = dict(gate=w[0], after_weight=w[1], after_bias=w[2], before_weight=w[3], before_bias=w[4])
+    r, y, stats = P.coop_residual_norm(x, f, **kw)
+    for at in (0, 1777, n - 100):
+        part = slice(at, at + 100)
+        some = P.coop_residual_norm(x[part], f[part], **kw)
+        assert torch.equal(r[part], some[0]) and torch.equal(y[part], some[1]) and torch.equal(stats[:, part], some[2])
+
+
 # ---- the gradients' norm ------------------------------------------------------------------------------------------------------------
 @gpu
 @pytest.mark.parametrize("sizes", [[1], [0], [], [7, 0, 16384, 16385, 3], [1000003], [5] * 1000, [40000, 1, 2, 300000]])
