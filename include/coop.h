@@ -316,8 +316,9 @@ int coop_cache_vertices(const coop_cache* c, const int32_t** vertex_of_out, int6
 /*
  * Operators of learned vertex representations: what a program that trains rows for the vertices (in the place of, or on top
  * of, given features) does with sampled blocks.  Elements are COOP_F32, COOP_F16 or COOP_BF16; arithmetic, sums and
- * statistics are in 32 bits and are rounded once, to nearest, when a result is stored.  Two things are rounded besides: the
- * logits' gradient between the products of coop_softmax_xent_grad, to the operands' type, and moments that are kept in 8 bits.  Pointers need the alignment of their
+ * statistics are in 32 bits and are rounded once, to nearest, when a result is stored.  Three things are rounded besides: the
+ * logits' gradient between the products of coop_softmax_xent_grad and that of a dense layer's activation, to the operands' type, and moments that are kept in 8 bits.  Results
+ * lie apart from what a call reads, and from each other, but where it says otherwise.  Pointers need the alignment of their
  * elements only, workspaces 256 bytes; rows are dense.  All calls are asynchronous on `stream`, allocate nothing, copy
  * nothing to or from the host, and give the same bits for the same input on every call (no sum's order depends on time), so
  * that they can be captured into a graph.  (coop_adamw's step, rates and seed are numbers of the call, though: every replay of

@@ -18,8 +18,10 @@ struct SmallGrad {
   float *db, *db2;
 };
 
-// kSmallLength: bytes of the common dimension, 12 steps for each wave (longer ones take too long in the few blocks of a weight's gradient: 8,192 rows
-// of 64 by 64, 36.6 us for the 16.2 of dense_narrow.h).  8 waves for 16, which are idle where it is short: bf16 1,024 x 256 x 256 11.0 us for 13.1,
+// kSmallLength: bytes of the common dimension, 12 steps for each wave: longer ones take too long in the few blocks of a weight's gradient.  (Against tiles, 16 bits: 100 x
+// 275 gated, 3,000 rows 30.0 us for 37.5, 3,700 34.9 for 39.2, with what was kept 41.5 for 40.5; 64 x 200 3,000 18.9 for 26.6, 4,500 26.2 both, 5,500 30.3 for 26.6.
+// fp32, 100 x 100 gated, 1,500 rows 21.4 for 34.2, 2,300 27.7 for 34.0, 3,000 36.0 for 35.7.  Against dense_narrow.h it ends earlier: 64 x 64, 1,500 rows 15.0 for
+// 16.5, 2,200 17.8 for 15.6, 3,000 20.4 for 15.5.)  8 waves for 16, which are idle where it is short: bf16 1,024 x 256 x 256 11.0 us for 13.1,
 // 256 x 1,024 x 512 13.1 for 19.9; 4: 12.5 and 12.5, and 31.5 for 26.4 with 3,001 rows.
 constexpr int kSmallWaves = 8, kSmallRows = 32, kSmallLength = 12 * 8 * 64;
 

@@ -1,6 +1,9 @@
 """Layers on learned vertex rows (see include/coop.h for the contract of every call): a dense layer with its epilogue, the projections of
 a gated feed-forward block, the norms and the residual between two blocks, and the gradients' norm ahead of an AdamW step.
 
+What an activation was of is worth keeping (want_pre, then pre=) for rows of some 1,000 elements and more; for shorter ones the gradient call makes it
+again in less time than 32 bits of it take to be written and read, and in no memory.
+
 Marshalling only, as in binding.py and learn.py; streams are as there.
 """
 import ctypes as C
