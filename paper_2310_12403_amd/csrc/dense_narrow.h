@@ -199,8 +199,9 @@ __global__ __launch_bounds__(kNarrowForwardWaves* kWave) void k_narrow(NarrowLay
 
 // The whole gradient in one pass over x and dout: z once more, dz, dx, and the sums for the weight's gradient and the bias's.  A block has 32 rows
 // for each of its eight waves at a time, two to a SIMD, so that one's activations (some 130 cycles a value of gelu's slope: as much as the memory takes)
-// run beside the other's products.  (REST: what dz loses to its type is multiplied too, and meets it in LDS.)  dW is dealt to the waves by tiles of 32 x 32 (of few tiles, by parts of the rows too): the rows of x and dz of all of
-// them meet in LDS, where the product over the rows reads them transposed; so is the weight, which is there once, for dx.
+// run beside the other's products.  dW is dealt to the waves by tiles of 32 x 32 (of few tiles, by parts of the rows too): the rows of x and dz of all of
+// them meet in LDS, where the product over the rows reads them transposed; so is the weight, which is there once, for dx.  (REST: what dz loses to its type lies
+// beside it there, and is multiplied too.)
 template <int T, int KS, int MT, bool REST = false>
 struct NarrowBackward {
   static constexpr int kWaves = 8, KT = KS / 2, kTiles = KT * MT;
